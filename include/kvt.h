@@ -372,6 +372,110 @@ int32_t kvt_hash_tokens(const uint32_t *d_tokens, uint64_t n_tokens, uint64_t ha
 int32_t kvt_hash_tokens_noalloc(const uint32_t *d_tokens, uint64_t n_tokens, uint64_t hash_seed,
                                 uint64_t *d_keys, void *stream);
 
+/* ---- model-side operators on the HBM pool ------------------------------------------------------- */
+/* What a model does with the slots the calls above hand out: it writes the keys and values of its new tokens into
+ * them (kvt_append_kv) and attends over everything its contexts hold there (kvt_attend). The paper's engine leaves both
+ * to the serving stack (Section 7); they are offered here for the pool layouts of this engine. Both calls
+ *   - take elem_bytes = 2 engines with a payload pool; the element type is named per call (KVT_KV_*), all tensors of
+ *     a call have it;
+ *   - read all lengths, positions and block tables from device memory, allocate nothing, do not synchronise and can
+ *     be captured into a CUDA graph (a replay uses the values the arrays hold by then). Calls of one engine may run on
+ *     different streams at once as long as nothing writes what another reads and each has its own scratch;
+ *   - run on the device the engine was created on, whichever is current.
+ *
+ * A block table row lists the slots of one sequence: entry b holds tokens [16 b, 16 b + 16). A slot id below
+ * n_hbm_blocks is a slot of the HBM tier (kvt_get_block_map reports them); n_hbm_blocks + i is tail block i (see
+ * kvt_set_tail_pool). Ids beyond both set the sticky error word read by kvt_kv_check; nothing is written for them and
+ * their keys and values read as zeros. */
+#define KVT_KV_BF16 0u
+#define KVT_KV_FP16 1u
+
+/* The new tokens of a batch: n_tokens rows, those of sequence s being rows [q_start[s], q_start[s+1]). After this
+ * step sequence s holds kv_len[s] tokens, the new ones last: its i-th new token has index
+ * kv_len[s] - (q_start[s+1] - q_start[s]) + i in the sequence. Rows behind q_start[n_seqs] belong to nobody: they are
+ * neither read nor written (a padded batch). Starts that decrease or pass n_tokens and lengths beyond the table row
+ * are cut to what fits and set the error word. */
+typedef struct kvt_batch {
+  uint32_t n_seqs;
+  uint32_t n_tokens;
+  uint32_t max_blocks;          /* entries of a block table row */
+  uint32_t max_q_len;           /* most new tokens of one sequence (0: not known). A hint that chooses the kernel of
+                                   kvt_attend; results do not depend on it */
+  uint64_t table_stride;        /* elements between two rows of block_table */
+  const uint32_t *q_start;      /* device, n_seqs + 1 */
+  const uint32_t *kv_len;       /* device, n_seqs */
+  const uint32_t *block_table;  /* device */
+} kvt_batch;
+
+/* kvt_append_args.flags */
+#define KVT_ROPE_INTERLEAVED 1u /* pair j is (2j, 2j+1); without it (j, j + rot_dim/2) */
+
+typedef struct kvt_append_args {
+  kvt_batch b;
+  uint32_t layer, dtype;        /* dtype: KVT_KV_* */
+  uint32_t n_q_heads;           /* 0: no queries */
+  uint32_t flags;               /* KVT_ROPE_* */
+  uint32_t rot_dim;             /* leading elements of a head that are rotated; even, <= head_dim; 0: none */
+  uint32_t n_axes;              /* rows of `positions` */
+  const void *q, *k, *v;        /* device; element (token, head, d) at token * _ts + head * _hs + d */
+  void *q_out;                  /* rotated queries; may be q itself with the same strides */
+  uint64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, qo_ts, qo_hs;   /* strides in elements */
+  const double *freqs;          /* device, rot_dim/2: pair j of a token turns by position * freqs[j] radians */
+  const uint8_t *axis_of;       /* device, rot_dim/2: the row of `positions` pair j takes (>= n_axes reads as 0 and sets the
+                                   error word); NULL: row 0 */
+  const int32_t *positions;     /* device, n_axes rows of n_tokens; NULL: the token's index in its sequence */
+  uint64_t pos_stride;          /* elements between two rows of `positions` */
+} kvt_append_args;
+
+/* Writes the new tokens' keys (rotated by their positions) and values into the blocks of `layer`, and the rotated
+ * queries into q_out. Angles are formed and reduced in 64 bits, sines and the rotation in 32, rounded once. If two
+ * tokens of a batch land in the same place (a slot listed twice), either may win. Errors: KVT_E_INVAL (NULL or
+ * misaligned pointer, bad layer / dtype / rot_dim, engine without payload or with elem_bytes != 2). Asynchronous. */
+int32_t kvt_append_kv(kvt_engine *e, const kvt_append_args *a, void *stream);
+
+/* kvt_attend_args.flags */
+#define KVT_ATTN_FULL 1u        /* every query sees all kv_len keys; without it those up to and with its own index */
+
+typedef struct kvt_attend_args {
+  kvt_batch b;
+  uint32_t layer, dtype;
+  uint32_t n_q_heads;           /* a multiple of n_kv_heads; query heads [g*h, g*h + g) read KV head h */
+  uint32_t flags;
+  uint32_t window;              /* > 0: a query sees the last `window` of its keys only (not with KVT_ATTN_FULL). Blocks
+                                   no query of a sequence sees are not read and need no valid slot */
+  float scale;                  /* of the scores; 0: 1 / sqrt(head_dim) */
+  const void *q;                /* device; element (token, head, d) at token * q_ts + head * q_hs + d */
+  void *out;                    /* the same with o_ts, o_hs */
+  float *lse;                   /* optional, [n_tokens][n_q_heads]: natural log of the sum of exponentials */
+  uint64_t q_ts, q_hs, o_ts, o_hs;
+  void *scratch;                /* device, 16-byte aligned, kvt_attend_scratch_bytes(e, a) bytes; contents are
+                                   irrelevant before and after the call */
+  uint64_t scratch_bytes;
+} kvt_attend_args;
+
+/* softmax(scale q k^T) v of the new tokens over their sequences' keys and values in the pool (their own included:
+ * append first). A row that sees no key gives zeros and lse = -inf. Scores, sums and the output are held in 32 bits;
+ * the probabilities are rounded to the element type for the second product. Keys a row does not see have no effect,
+ * whatever their values, with one exception: a value that is Inf or NaN in a token that other rows of the
+ * sequence see may reach all of that sequence's new rows. What lies in a block behind kv_len has no effect. Errors: KVT_E_INVAL as above
+ * (head_dim above 256, heads that do not divide, window with KVT_ATTN_FULL, scale that is negative or not finite),
+ * KVT_E_BUFSZ scratch too small. Asynchronous. */
+int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *a, void *stream);
+/* Depends on sizes only (n_seqs, n_tokens, max_blocks, max_q_len, n_q_heads), not on what device arrays hold.
+ * 0 for arguments kvt_attend refuses and where none is needed. */
+uint64_t kvt_attend_scratch_bytes(kvt_engine *e, const kvt_attend_args *a);
+
+/* The engine gives slots to full, admitted blocks only. KV of a context's last, partly filled block, of blocks that
+ * bypassed admission and of tokens still being generated lies in tail blocks: a device buffer of the caller
+ * (block-major, 16-byte aligned, bytes / block_bytes blocks) that no tier operation touches. NULL / 0 removes it.
+ * Calls enqueued or captured earlier keep the buffer they were given. */
+int32_t kvt_set_tail_pool(kvt_engine *e, void *pool, uint64_t bytes);
+
+/* Synchronises, then reports and clears what the calls above found on the device: KVT_E_RANGE (a slot id outside the
+ * pools, or lengths, starts or axes that had to be cut), KVT_E_DEVICE (a wait inside a kernel ran out; the outputs of
+ * that call are not to be used), KVT_OK. */
+int32_t kvt_kv_check(kvt_engine *e, void *stream);
+
 /* ---- introspection ------------------------------------------------------------------------------ */
 typedef struct kvt_stats {
   uint64_t clock;            /* logical clock */

@@ -24,13 +24,16 @@ POLICY_NO_LIFECYCLE, POLICY_INCLUSIVE, POLICY_ORPHANS_DEAD = 1, 2, 4
 OPF_TOKENS_ON_DEVICE = 1
 MAP_LOOKUP, MAP_ADMIT = 0, 1
 IDS_ON_DEVICE = 1
+KV_BF16, KV_FP16 = 0, 1
+ROPE_INTERLEAVED, ATTN_FULL = 1, 1
 
 EXPORTS = ("kvt_query_sizes", "kvt_create", "kvt_destroy", "kvt_apply_op", "kvt_map_blocks", "kvt_get_block_map",
            "kvt_classify", "kvt_get_states", "kvt_select_victims", "kvt_offload", "kvt_reload", "kvt_release",
            "kvt_compact", "kvt_copy_blocks", "kvt_hash_scratch_bytes", "kvt_hash_tokens", "kvt_get_stats",
            "kvt_last_error", "kvt_get_entries", "kvt_debug_load_resident", "kvt_set_profiling",
            "kvt_hash_tokens_noalloc", "kvt_debug_set_mover_variant", "kvt_exchange", "kvt_debug_set_lookup_variant", "kvt_move", "kvt_set_mover_ctas",
-           "kvt_debug_set_wait_limit", "kvt_debug_set_classify_mode", "kvt_set_l2_residency", "kvt_debug_set_copy_delay")
+           "kvt_debug_set_wait_limit", "kvt_debug_set_classify_mode", "kvt_set_l2_residency", "kvt_debug_set_copy_delay",
+           "kvt_append_kv", "kvt_attend", "kvt_attend_scratch_bytes", "kvt_set_tail_pool", "kvt_kv_check")
 
 
 class KvtError(RuntimeError):
@@ -57,6 +60,25 @@ class Config(C.Structure):
 class Op(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in ("op", "ctx", "parent", "msg_start", "msg_end", "n_tokens", "flags",
                                            "reserved")] + [("tokens", C.c_void_p)]
+
+
+class Batch(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("n_seqs", "n_tokens", "max_blocks", "max_q_len")] + \
+               [("table_stride", C.c_uint64)] + [(n, C.c_void_p) for n in ("q_start", "kv_len", "block_table")]
+
+
+class AppendArgs(C.Structure):
+    _fields_ = [("b", Batch)] + [(n, C.c_uint32) for n in ("layer", "dtype", "n_q_heads", "flags", "rot_dim", "n_axes")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "v", "q_out")] + \
+               [(n, C.c_uint64) for n in ("q_ts", "q_hs", "k_ts", "k_hs", "v_ts", "v_hs", "qo_ts", "qo_hs")] + \
+               [(n, C.c_void_p) for n in ("freqs", "axis_of", "positions")] + [("pos_stride", C.c_uint64)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("b", Batch)] + [(n, C.c_uint32) for n in ("layer", "dtype", "n_q_heads", "flags", "window")] + \
+               [("scale", C.c_float)] + [(n, C.c_void_p) for n in ("q", "out", "lse")] + \
+               [(n, C.c_uint64) for n in ("q_ts", "q_hs", "o_ts", "o_hs")] + \
+               [("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
 
 
 CALL_INFO_DTYPE = np.dtype([(n, np.uint32) for n in ("n_blocks", "hit_len", "n_hit_hbm", "n_hit_host",
@@ -124,6 +146,10 @@ def load_library():
             "kvt_debug_set_copy_delay": [vp, u32],
             "kvt_get_entries": [vp, u32, vp, vp, vp, vp, vp, u32, vp],
             "kvt_debug_load_resident": [vp, vp, vp, vp, vp, vp, u32, u32, vp],
+            "kvt_append_kv": [vp, vp, vp],
+            "kvt_attend": [vp, vp, vp],
+            "kvt_set_tail_pool": [vp, vp, u64],
+            "kvt_kv_check": [vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
@@ -131,6 +157,8 @@ def load_library():
             fn.restype = i32
         lib.kvt_hash_scratch_bytes.argtypes = [u64]
         lib.kvt_hash_scratch_bytes.restype = u64
+        lib.kvt_attend_scratch_bytes.argtypes = [vp, vp]
+        lib.kvt_attend_scratch_bytes.restype = u64
         _lib = lib
     return _lib
 
@@ -174,6 +202,37 @@ def hash_tokens_noalloc(tokens_dev, keys_out, seed: int = 0) -> int:
     return lib.kvt_hash_tokens_noalloc(tokens_dev.data_ptr(), tokens_dev.numel(), seed, keys_out.data_ptr(), _stream())
 
 
+class Rope:
+    """The rotation `Engine.append_kv` applies: pair j of the leading `rot_dim` elements of a head turns by
+    position * freqs[j] radians. Frequencies are theta ** (-2 j / rot_dim) unless `freqs` (rot_dim / 2 numbers) gives
+    others. `sections` shares the pairs out among several position axes (time, height, width): so many consecutive
+    pairs per axis, adding up to rot_dim / 2; `axis_of` names the axis of each pair instead. `interleaved`: pairs are
+    neighbours (2j, 2j + 1); otherwise (j, j + rot_dim / 2)."""
+
+    def __init__(self, rot_dim, theta=10000.0, sections=None, axis_of=None, interleaved=False, freqs=None, device="cuda"):
+        import torch
+        if rot_dim < 0 or rot_dim % 2:
+            raise ValueError("Rope: rot_dim must be even")
+        half = rot_dim // 2
+        if freqs is None:
+            freqs = [theta ** (-2.0 * j / rot_dim) for j in range(half)]
+        if len(freqs) != half:
+            raise ValueError(f"Rope: {half} frequencies expected, got {len(freqs)}")
+        if sections is not None:
+            if axis_of is not None or any(n < 0 for n in sections) or sum(sections) != half:
+                raise ValueError(f"Rope: sections must add up to {half}, without axis_of")
+            axis_of = [i for i, n in enumerate(sections) for _ in range(n)]
+        self.rot_dim, self.interleaved = rot_dim, bool(interleaved)
+        self.freqs = torch.as_tensor(freqs, dtype=torch.float64).to(device).contiguous()
+        self.n_axes, self.axis_of = 1, None
+        if axis_of is not None:
+            axis_of = [int(x) for x in axis_of]
+            if len(axis_of) != half or any(not 0 <= x < 256 for x in axis_of):
+                raise ValueError(f"Rope: axis_of needs {half} axes below 256")
+            self.n_axes = len(sections) if sections is not None else max(axis_of, default=0) + 1
+            self.axis_of = torch.tensor(axis_of, dtype=torch.uint8).to(device)
+
+
 class Engine:
     """One cache engine on the current CUDA device. Allocates the pools and arenas with torch and
     hands raw pointers to the library."""
@@ -182,7 +241,7 @@ class Engine:
                  n_hbm_blocks=128, n_host_blocks=512, max_contexts=64, hash_seed=0, suspended_order=ORDER_MRU,
                  metadata_only=False, table_capacity=None, max_messages=1 << 16, max_batch_blocks=None,
                  max_tokens=1 << 22, max_key_blocks=None, host_pool_on_device=False, zero_pools=True, policy_flags=0,
-                 n_remote_blocks=0, stage_mib=256, device="cuda"):
+                 n_remote_blocks=0, stage_mib=256, device="cuda", n_tail_blocks=0):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("paper_2609_39819_b200 needs a CUDA device (there is no CPU fallback)")
@@ -250,6 +309,10 @@ class Engine:
         if rc:
             raise KvtError(rc, "create")
         self.h = h
+        self.tail_pool = None
+        if n_tail_blocks:       # blocks outside every tier: slot ids n_hbm_blocks + i of append_kv and attend
+            self.set_tail_pool((torch.zeros if zero_pools else torch.empty)(n_tail_blocks * self.block_bytes, dtype=torch.uint8,
+                                                                            device=self.device))
 
     @staticmethod
     def _align(t):
@@ -259,7 +322,7 @@ class Engine:
         if getattr(self, "h", None):
             self.L.kvt_destroy(self.h)
             self.h = None
-            self.hbm_pool = self.host_pool = self.remote_pool = self.meta = self.tokens = self.stage_buf = None   # release the memory
+            self.hbm_pool = self.host_pool = self.remote_pool = self.meta = self.tokens = self.stage_buf = self.tail_pool = None   # release the memory
 
     def __del__(self):
         try:
@@ -432,6 +495,131 @@ class Engine:
             s, d = _u32(src), _u32(dst)
             rc = self.L.kvt_copy_blocks(self.h, src_tier, _p(s), dst_tier, _p(d), len(s), 0, _stream())
         self._check(rc, "copy_blocks")
+
+    # ---- model-side operators on the HBM pool -----------------------------------------------------
+    def set_tail_pool(self, pool):
+        """Tail blocks (slot ids n_hbm_blocks + i): a uint8 device tensor of whole blocks, block-major; None removes it."""
+        if pool is not None and (pool.device.type != "cuda" or pool.dtype != self.torch.uint8 or not pool.is_contiguous()):
+            raise ValueError("set_tail_pool: a contiguous uint8 tensor on the engine's device expected")
+        self._check(self.L.kvt_set_tail_pool(self.h, pool.data_ptr() if pool is not None else None,
+                                             pool.numel() if pool is not None else 0), "set_tail_pool")
+        self.tail_pool = pool
+
+    def _kv_dtype(self, x, what):
+        torch = self.torch
+        code = KV_BF16 if x.dtype == torch.bfloat16 else KV_FP16 if x.dtype == torch.float16 else None
+        if code is None:
+            raise ValueError(f"{what}: bfloat16 or float16 expected, got {x.dtype}")
+        return code
+
+    def _kv_tensor(self, x, what, shape, dtype):
+        """(address, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
+        if x.dtype != dtype or x.shape != shape or x.device != self._dev:
+            raise ValueError(f"{what}: {dtype} tensor {tuple(shape)} on {self._dev} expected, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        ts, hs, es = x.stride()
+        if es != 1 and shape[2] > 1:
+            raise ValueError(f"{what}: the elements of a head must be consecutive")
+        return x.data_ptr(), ts, hs
+
+    def _kv_batch(self, what, n_tokens, block_table, q_start, kv_len, max_q_len):
+        i32, dev = self.torch.int32, self._dev
+        if block_table.dtype != i32 or q_start.dtype != i32 or kv_len.dtype != i32 or block_table.dim() != 2 or \
+                q_start.dim() != 1 or kv_len.dim() != 1:
+            raise ValueError(f"{what}: block_table [sequences, blocks], q_start and kv_len must be int32")
+        n, m = block_table.shape
+        if kv_len.shape[0] != n or q_start.shape[0] != n + 1 or (m > 1 and block_table.stride(1) != 1) or \
+                (n and q_start.stride(0) != 1) or (n > 1 and kv_len.stride(0) != 1):
+            raise ValueError(f"{what}: {n} table rows need {n} lengths and {n + 1} starts, with consecutive elements")
+        if block_table.device != dev or q_start.device != dev or kv_len.device != dev:
+            raise ValueError(f"{what}: block_table, q_start and kv_len must be on {dev}")
+        return Batch(n, n_tokens, m, max_q_len or 0, block_table.stride(0), q_start.data_ptr(), kv_len.data_ptr(),
+                     block_table.data_ptr())
+
+    @property
+    def _dev(self):
+        d = self.__dict__.get("_dev_")
+        if d is None:
+            d = self._dev_ = self.meta.device
+        return d
+
+    def _kv_stream(self):
+        return self.torch.cuda.current_stream(self._dev).cuda_stream
+
+    def append_kv(self, layer, k, v, block_table, q_start, kv_len, rope=None, positions=None, q=None, q_out=None):
+        """Writes the new tokens' keys (rotated) and values into the blocks of `layer` and returns the rotated queries
+        (in `q_out`, which may be `q`, or a new tensor; None without q). k, v: [tokens, n_kv_heads, head_dim], q:
+        [tokens, heads, head_dim], bf16 or fp16, any strides with consecutive elements. Sequence s brings rows
+        [q_start[s], q_start[s+1]) and holds kv_len[s] tokens with them; block_table[s, b] is the slot of its b-th
+        16-token block (below n_hbm_blocks: HBM tier; above: tail block). positions: int32 [tokens] or [axes, tokens],
+        by default the tokens' indices in their sequences. Asynchronous on the current stream; ids and lengths outside
+        their ranges are skipped and reported by kv_check()."""
+        torch = self.torch
+        dt = self._kv_dtype(k, "append_kv")
+        t, h, d = k.shape[0], self.n_kv_heads, self.head_dim
+        kp, kts, khs = self._kv_tensor(k, "append_kv: k", (t, h, d), k.dtype)
+        vp, vts, vhs = self._kv_tensor(v, "append_kv: v", (t, h, d), k.dtype)
+        a = AppendArgs(self._kv_batch("append_kv", t, block_table, q_start, kv_len, 0), layer, dt, 0, 0, 0, 0,
+                       None, kp, vp, None, 0, 0, kts, khs, vts, vhs)
+        if q is not None:
+            hq = q.shape[1] if q.dim() == 3 else 0
+            a.n_q_heads = hq
+            a.q, a.q_ts, a.q_hs = self._kv_tensor(q, "append_kv: q", (t, hq, d), k.dtype)
+            if q_out is None:
+                q_out = torch.empty((t, hq, d), dtype=k.dtype, device=self._dev)
+            a.q_out, a.qo_ts, a.qo_hs = self._kv_tensor(q_out, "append_kv: q_out", (t, hq, d), k.dtype)
+            if a.q == a.q_out and (a.q_ts, a.q_hs) != (a.qo_ts, a.qo_hs):
+                raise ValueError("append_kv: q_out in the place of q needs its strides")
+        elif q_out is not None:
+            raise ValueError("append_kv: q_out without q")
+        if rope is not None:
+            if rope.freqs.device != self._dev:
+                raise ValueError(f"append_kv: rope is on {rope.freqs.device}, the engine on {self._dev}")
+            a.rot_dim, a.flags, a.freqs = rope.rot_dim, ROPE_INTERLEAVED if rope.interleaved else 0, rope.freqs.data_ptr()
+            a.n_axes = rope.n_axes
+            a.axis_of = rope.axis_of.data_ptr() if rope.axis_of is not None else None
+            if positions is None and rope.n_axes > 1:
+                raise ValueError(f"append_kv: {rope.n_axes} axes need positions")
+        if positions is not None:
+            p2 = positions if positions.dim() == 2 else positions[None]
+            if rope is None or p2.dtype != torch.int32 or p2.shape != (rope.n_axes, t) or p2.device != self._dev or \
+                    (t > 1 and p2.stride(1) != 1):
+                raise ValueError(f"append_kv: positions must be int32 [{rope.n_axes if rope else 1}, {t}] on {self._dev}, with a rope")
+            a.positions, a.pos_stride = p2.data_ptr(), p2.stride(0)
+        self._check(self.L.kvt_append_kv(self.h, C.byref(a), self._kv_stream()), "append_kv")
+        return q_out
+
+    def attend(self, layer, q, block_table, q_start, kv_len, max_q_len=None, causal=True, window=None, scale=None, out=None,
+               lse=None):
+        """softmax(scale q k^T) v of the new tokens' queries over everything their sequences hold in `layer` (append
+        first: the new tokens are among the kv_len[s]). q: [tokens, heads, head_dim], heads a multiple of n_kv_heads;
+        batch as in append_kv. causal: a query sees the keys up to its own, with `window` the last `window` of them;
+        causal=False: all kv_len keys. scale: 1 / sqrt(head_dim) by default. max_q_len: most new tokens of one sequence,
+        if known (chooses the kernel, not the result). out, lse ([tokens, heads] float32, contiguous): written if
+        given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream."""
+        torch = self.torch
+        dt = self._kv_dtype(q, "attend")
+        t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
+        qp, qts, qhs = self._kv_tensor(q, "attend: q", (t, hq, self.head_dim), q.dtype)
+        if out is None:
+            out = torch.empty((t, hq, d), dtype=q.dtype, device=self._dev)
+        op, ots, ohs = self._kv_tensor(out, "attend: out", (t, hq, d), q.dtype)
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (t, hq) or lse.device != self._dev or
+                                not lse.is_contiguous()):
+            raise ValueError(f"attend: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
+        a = AttendArgs(self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len), layer, dt, hq,
+                       0 if causal else ATTN_FULL, window or 0, scale or 0.0, qp, op,
+                       lse.data_ptr() if lse is not None else None, qts, qhs, ots, ohs)
+        n = self.L.kvt_attend_scratch_bytes(self.h, C.byref(a))
+        if n:
+            scratch = torch.empty(n, dtype=torch.uint8, device=self._dev)   # from the current stream's pool, or the capture's
+            a.scratch, a.scratch_bytes = scratch.data_ptr(), n
+        self._check(self.L.kvt_attend(self.h, C.byref(a), self._kv_stream()), "attend")
+        return out
+
+    def kv_check(self):
+        """Waits for the current stream and raises if append_kv or attend met an id or a length outside its range."""
+        self._check(self.L.kvt_kv_check(self.h, self._kv_stream()), "kv_check")
 
     # ---- introspection --------------------------------------------------------------------------
     def get_stats(self):

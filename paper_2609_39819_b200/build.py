@@ -7,10 +7,10 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libkvt.so")
-SOURCES = ["kvt_engine.cu"]
-DEPS = ["kvt_kernels.cuh", os.path.join("..", "..", "include", "kvt.h")]
+SOURCES = ["kvt_engine.cu", "kvt_attend.cu"]
+DEPS = ["kvt_kernels.cuh", "kvt_attend.h", os.path.join("..", "..", "include", "kvt.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-              "-Xcompiler", "-fPIC"]
+              "-Xcompiler", "-fPIC", "--threads", "2"]
 DEFINES: list = []
 
 

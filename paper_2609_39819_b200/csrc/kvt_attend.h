@@ -1,0 +1,49 @@
+// kvt_attend.h — what the entry points in kvt_engine.cu hand to the kernels in kvt_attend.cu.
+#pragma once
+#include <cstdint>
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+namespace kvt {
+
+// bits of the sticky error word of the model-side operators
+enum : uint32_t { KVERR_RANGE = 1, KVERR_WAIT = 2 };
+
+// One chunk row (layer, K or V) of the pools: slot s < n_slots lies at base + s * slot_stride, slot n_slots + i is tail
+// block i at tail + i * tail_stride. Inside a block: [16 tokens][n_kv_heads][head_dim].
+struct KvRow { uint8_t *base, *tail; };
+struct KvPools {
+  KvRow k, v;
+  uint64_t slot_stride, tail_stride;
+  uint32_t n_slots, n_tail;
+  uint32_t n_kv_heads, head_dim;
+};
+
+struct KvBatch {
+  const uint32_t *q_start, *kv_len, *table;
+  uint64_t table_stride;
+  uint32_t n_seqs, n_tokens, max_blocks;
+};
+
+struct AppendArgs {
+  KvBatch b; KvPools p;
+  const void *q, *k, *v; void *q_out;
+  uint64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, qo_ts, qo_hs;
+  const double *freqs; const uint8_t *axis_of; const int32_t *positions; uint64_t pos_stride;
+  uint32_t n_q_heads, rot_dim, n_axes, interleaved, fp16;
+  uint32_t *err;
+};
+
+struct AttendArgs {
+  KvBatch b; KvPools p;
+  const void *q; void *out; float *lse;
+  uint64_t q_ts, q_hs, o_ts, o_hs;
+  uint32_t n_q_heads, group, window, full, fp16;
+  float scale_log2;                 // scale / ln 2: scores in powers of two
+  uint32_t *err;
+};
+
+cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, uint32_t *launches);
+cudaError_t launch_attend(const AttendArgs &a, int sm_count, cudaStream_t s, uint32_t *launches);
+
+}  // namespace kvt

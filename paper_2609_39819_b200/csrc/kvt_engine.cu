@@ -5,9 +5,11 @@
 // allocators for the caller-provided arenas, counts of free slots, and the logical clock. Token
 // values, block keys, the block table, per-block metadata and payloads live on the device and are
 // only touched by the kernels in kvt_kernels.cuh. There is no CPU fallback for any stage.
+#include "kvt_attend.h"
 #include "kvt_kernels.cuh"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -95,7 +97,7 @@ struct Ctx {
 struct DevLayout {
   u64 tab, e_key, e_stamp, e_depth, e_infl, e_cnt, e_tslot, e_mark, e_link, e_floor, cnt_chk, fresh, keys, status;
   u64 s0, s1, s2, s3, ids, ids2, pair_src, pair_dst, pair_src2, pair_dst2, freelist, freelist2, tiles, agg, carry, cflags, desc, ctxres;
-  u64 m_start, m_end, m_rank, keyA, keyB, valA, valB, rcounts, sel_cta, sel_args, slot_key, sel_hist, sel_state, out_slots, out_states, map_tier, map_slot;
+  u64 m_start, m_end, m_rank, keyA, keyB, valA, valB, rcounts, sel_cta, sel_args, slot_key, sel_hist, sel_state, out_slots, out_states, map_tier, map_slot, kv_err;
   u64 total;
   u64 LB, Nt, N;
 };
@@ -136,6 +138,7 @@ DevLayout make_layout(const kvt_config &c) {
   L.sel_state = take((SEL_MAX_LEVELS + 1) * sizeof(SelState));
   L.out_slots = take(Nt * 4); L.out_states = take(Nt);
   L.map_tier = take(B); L.map_slot = take(B * 4);
+  L.kv_err = take(4);   // sticky error word of the model-side operators
   L.total = off;
   return L;
 }
@@ -153,6 +156,8 @@ struct kvt_engine {
   u64 chunk_bytes, n_chunks, block_bytes;
   bool metadata_only;
   int sm_count = 148;
+  int device = 0;
+  u8 *tail_pool = nullptr; u32 n_tail = 0;   // blocks outside every tier (kvt_set_tail_pool)
   // host state
   std::vector<Ctx> ctxs;
   std::vector<KeySeg> segs;
@@ -1007,6 +1012,7 @@ int32_t kvt_create(const kvt_config *cfg, void *stream, kvt_engine **out) {
       else cudaGetLastError();
     }
   }
+  e->device = dev;
   cudaDeviceGetAttribute(&e->sm_count, cudaDevAttrMultiProcessorCount, dev);
   if (!meta_only && c.stage_buf && c.stage_bytes) {
     kvt_engine::Staging &g = e->stg;
@@ -1080,6 +1086,7 @@ int32_t kvt_create(const kvt_config *cfg, void *stream, kvt_engine **out) {
   // everything except the key arena and scratch must start at zero; the table needs ent = NONE
   ok = ok && cudaMemsetAsync(e->meta + L.e_key, 0, L.keys - L.e_key, s) == cudaSuccess;
   ok = ok && cudaMemsetAsync(e->d_status, 0, ST_WORDS * 4, s) == cudaSuccess;
+  ok = ok && cudaMemsetAsync(e->dp<u32>(L.kv_err), 0, 4, s) == cudaSuccess;
   ok = ok && cudaMemsetAsync(e->ent.link, 0xFF, N * 4, s) == cudaSuccess;   // no links
   if (ok) {
     KL(k_table_clear, cdiv((u64)c.table_capacity, TPB), TPB, s, e->tab);
@@ -2239,6 +2246,154 @@ int32_t kvt_copy_blocks(kvt_engine *e, uint32_t src_tier, const uint32_t *src, u
     ds = e->dp<u32>(e->L.ids); dd = e->dp<u32>(e->L.ids2);
   }
   return launch_mover(e, s, src_tier, ds, dst_tier, dd, n, nullptr);
+}
+
+// ---- model-side operators -----------------------------------------------------------------------------------
+namespace {
+
+// The engine's device is current while this lives.
+struct OnDevice {
+  int before = -1; bool ok;
+  explicit OnDevice(int dev) {
+    ok = cudaGetDevice(&before) == cudaSuccess;
+    if (ok && before != dev) ok = cudaSetDevice(dev) == cudaSuccess; else before = -1;
+  }
+  ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+
+const char *kv_engine_fault(const kvt_engine *e, u32 layer, u32 dtype) {
+  if (e->metadata_only) return "model-side operators need an engine with a payload pool";
+  if (e->cfg.elem_bytes != 2 || dtype > KVT_KV_FP16) return "element type: 16-bit pools only (KVT_KV_BF16, KVT_KV_FP16)";
+  if (layer >= e->cfg.n_layers) return "layer out of range";
+  return nullptr;
+}
+const char *kv_batch_fault(const kvt_batch &b) {
+  if (!b.n_seqs || !b.n_tokens) return nullptr;     // nothing to do
+  if (!b.q_start || !b.kv_len || !b.block_table || !b.max_blocks) return "batch without starts, lengths or block table";
+  if (((uintptr_t)b.q_start | (uintptr_t)b.kv_len | (uintptr_t)b.block_table) & 3) return "misaligned batch array";
+  if (b.table_stride < b.max_blocks && b.n_seqs > 1) return "table_stride below max_blocks";
+  if (b.n_seqs > 0x7FFFFFFFu / 2 || b.n_tokens > 0x7FFFFFFFu || b.max_blocks > 0x7FFFFFFFu / 16) return "batch too large";
+  return nullptr;
+}
+KvPools kv_pools(const kvt_engine *e, u32 layer) {
+  KvPools p{};
+  const u64 cs = e->chunk_bytes;
+  const bool lm = e->cfg.pool_layout == KVT_LAYOUT_LAYER_MAJOR;
+  u8 *const pool = (u8 *)e->cfg.hbm_pool;
+  const u64 step = lm ? cs * e->cfg.n_hbm_blocks : cs;       // from K of a layer to its V
+  p.k.base = pool + 2 * layer * step; p.v.base = p.k.base + step;
+  p.slot_stride = lm ? cs : e->block_bytes;
+  p.tail_stride = e->block_bytes;
+  if (e->tail_pool) { p.k.tail = e->tail_pool + 2 * layer * cs; p.v.tail = p.k.tail + cs; }
+  p.n_slots = e->cfg.n_hbm_blocks; p.n_tail = e->n_tail;
+  p.n_kv_heads = e->cfg.n_kv_heads; p.head_dim = e->cfg.head_dim;
+  return p;
+}
+KvBatch kv_batch(const kvt_batch &b) {
+  return KvBatch{b.q_start, b.kv_len, b.block_table, b.table_stride, b.n_seqs, b.n_tokens, b.max_blocks};
+}
+int32_t kv_launched(kvt_engine *e, cudaError_t x, u32 launches) {
+  e->st.kernel_launches += launches;
+  if (x == cudaSuccess) return KVT_OK;
+  e->err = std::string("kernel launch: ") + cudaGetErrorString(x);
+  return KVT_E_CUDA;
+}
+const char *attend_fault(const kvt_engine *e, const kvt_attend_args &a) {
+  if (const char *m = kv_engine_fault(e, a.layer, a.dtype)) return m;
+  if (e->cfg.head_dim > 256) return "attend: head_dim above 256";
+  if (!a.n_q_heads || a.n_q_heads % e->cfg.n_kv_heads) return "attend: n_q_heads is not a multiple of n_kv_heads";
+  if ((a.flags & ~KVT_ATTN_FULL) || ((a.flags & KVT_ATTN_FULL) && a.window)) return "attend: flags";
+  if (!(a.scale >= 0.0f) || a.scale > 3.0e38f) return "attend: scale";
+  return kv_batch_fault(a.b);
+}
+AttendArgs attend_args(kvt_engine *e, const kvt_attend_args &a) {
+  AttendArgs x{};
+  x.b = kv_batch(a.b); x.p = kv_pools(e, a.layer);
+  x.q = a.q; x.out = a.out; x.lse = a.lse;
+  x.q_ts = a.q_ts; x.q_hs = a.q_hs; x.o_ts = a.o_ts; x.o_hs = a.o_hs;
+  x.n_q_heads = a.n_q_heads; x.group = a.n_q_heads / e->cfg.n_kv_heads;
+  x.window = a.window; x.full = a.flags & KVT_ATTN_FULL; x.fp16 = a.dtype == KVT_KV_FP16;
+  const double scale = a.scale > 0.0f ? (double)a.scale : 1.0 / std::sqrt((double)e->cfg.head_dim);
+  x.scale_log2 = (float)(scale * 1.4426950408889634);
+  x.err = e->dp<u32>(e->L.kv_err);
+  return x;
+}
+
+}  // namespace
+
+int32_t kvt_append_kv(kvt_engine *e, const kvt_append_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_append_args &a = *args;
+  if (const char *m = kv_engine_fault(e, a.layer, a.dtype)) return fail(e, KVT_E_INVAL, m);
+  if (const char *m = kv_batch_fault(a.b)) return fail(e, KVT_E_INVAL, m);
+  if (a.flags & ~KVT_ROPE_INTERLEAVED) return fail(e, KVT_E_INVAL, "append: flags");
+  if ((a.rot_dim & 1) || a.rot_dim > e->cfg.head_dim) return fail(e, KVT_E_INVAL, "append: rot_dim");
+  if (!a.b.n_seqs || !a.b.n_tokens) return KVT_OK;
+  if (!a.k || !a.v || (a.n_q_heads && (!a.q || !a.q_out))) return fail(e, KVT_E_INVAL, "append: NULL tensor");
+  if (((uintptr_t)a.q | (uintptr_t)a.q_out | (uintptr_t)a.k | (uintptr_t)a.v) & 1) return fail(e, KVT_E_INVAL, "append: misaligned tensor");
+  if (a.rot_dim && (!a.freqs || ((uintptr_t)a.freqs & 7))) return fail(e, KVT_E_INVAL, "append: freqs");
+  if (((uintptr_t)a.positions & 3) || (a.positions && !a.n_axes)) return fail(e, KVT_E_INVAL, "append: positions");
+  if (a.positions && a.n_axes > 1 && a.pos_stride < a.b.n_tokens) return fail(e, KVT_E_INVAL, "append: pos_stride");
+  if ((u64)a.n_q_heads * e->cfg.head_dim > 0x7FFFFFFFu) return fail(e, KVT_E_INVAL, "append: too many query heads");
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "append: device");
+  AppendArgs x{};
+  x.b = kv_batch(a.b); x.p = kv_pools(e, a.layer);
+  x.q = a.q; x.k = a.k; x.v = a.v; x.q_out = a.q_out;
+  x.q_ts = a.q_ts; x.q_hs = a.q_hs; x.k_ts = a.k_ts; x.k_hs = a.k_hs;
+  x.v_ts = a.v_ts; x.v_hs = a.v_hs; x.qo_ts = a.qo_ts; x.qo_hs = a.qo_hs;
+  x.freqs = a.freqs; x.axis_of = a.positions ? a.axis_of : nullptr; x.positions = a.positions; x.pos_stride = a.pos_stride;
+  x.n_q_heads = a.n_q_heads; x.rot_dim = a.rot_dim; x.n_axes = a.n_axes;
+  x.interleaved = a.flags & KVT_ROPE_INTERLEAVED; x.fp16 = a.dtype == KVT_KV_FP16;
+  x.err = e->dp<u32>(e->L.kv_err);
+  u32 launches = 0;
+  const cudaError_t r = launch_append(x, (cudaStream_t)stream, &launches);
+  return kv_launched(e, r, launches);
+}
+
+uint64_t kvt_attend_scratch_bytes(kvt_engine *e, const kvt_attend_args *args) {
+  if (!e || !args || attend_fault(e, *args) || !args->b.n_seqs || !args->b.n_tokens) return 0;
+  return 0;
+}
+
+int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_attend_args &a = *args;
+  if (const char *m = attend_fault(e, a)) return fail(e, KVT_E_INVAL, m);
+  if (!a.b.n_seqs || !a.b.n_tokens) return KVT_OK;
+  if (!a.q || !a.out || (((uintptr_t)a.q | (uintptr_t)a.out) & 1) || ((uintptr_t)a.lse & 3))
+    return fail(e, KVT_E_INVAL, "attend: NULL or misaligned tensor");
+  if ((u64)a.b.n_tokens * a.n_q_heads > 0xFFFFFFFFull) return fail(e, KVT_E_INVAL, "attend: batch too large");
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "attend: device");
+  u32 launches = 0;
+  const cudaError_t r = launch_attend(attend_args(e, a), e->sm_count, (cudaStream_t)stream, &launches);
+  return kv_launched(e, r, launches);
+}
+
+int32_t kvt_set_tail_pool(kvt_engine *e, void *pool, uint64_t bytes) {
+  if (!e) return KVT_E_INVAL;
+  if (e->metadata_only) return fail(e, KVT_E_INVAL, "tail pool on a metadata-only engine");
+  if ((uintptr_t)pool & 15) return fail(e, KVT_E_INVAL, "tail pool: misaligned");
+  const u64 n = pool ? bytes / e->block_bytes : 0;
+  if (n + e->cfg.n_hbm_blocks >= 0x7FFFFFFFull) return fail(e, KVT_E_INVAL, "tail pool: too many blocks");
+  e->tail_pool = n ? (u8 *)pool : nullptr;
+  e->n_tail = (u32)n;
+  return KVT_OK;
+}
+
+int32_t kvt_kv_check(kvt_engine *e, void *stream) {
+  if (!e) return KVT_E_INVAL;
+  cudaStream_t s = (cudaStream_t)stream;
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "kv_check: device");
+  u32 bits = 0;
+  CU(cudaMemcpyAsync(&bits, e->dp<u32>(e->L.kv_err), 4, cudaMemcpyDeviceToHost, s));
+  CU(cudaMemsetAsync(e->dp<u32>(e->L.kv_err), 0, 4, s));
+  CU(cudaStreamSynchronize(s));
+  if (bits & KVERR_WAIT) return fail(e, KVT_E_DEVICE, "a wait inside a model-side kernel ran out");
+  if (bits) return fail(e, KVT_E_RANGE, "slot id, length, start or axis outside its range");
+  return KVT_OK;
 }
 
 // ---- stand-alone hasher -----------------------------------------------------------------------------------

@@ -1,0 +1,60 @@
+"""What of append_kv and attend can be checked without a GPU: struct layouts, NULL arguments, the Rope description."""
+import ctypes as C
+import re
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SIZES = {"uint32_t": 4, "uint64_t": 8, "float": 4, "pointer": 8}
+
+
+def header_struct(name):
+    """(field, size) in the header's order, nested batch included as one field."""
+    text = open(os.path.join(ROOT, "include", "kvt.h")).read()
+    body = text[text.index(f"typedef struct {name} {{"):text.index(f"}} {name};")]
+    body = re.sub(r"/\*.*?\*/", "", body, flags=re.S).split("{", 1)[1]
+    out = []
+    for decl in body.split(";"):
+        m = re.match(r"\s*(?:const\s+)?(\w+)\s+(.*)", decl.strip(), flags=re.S)
+        if not m:
+            continue
+        for x in m.group(2).split(","):
+            x = x.strip()
+            out.append((x.lstrip("*"), 8 if x.startswith("*") else SIZES.get(m.group(1), 0)))
+    return out
+
+
+@pytest.mark.parametrize("name,cls", [("kvt_batch", "Batch"), ("kvt_append_args", "AppendArgs"), ("kvt_attend_args", "AttendArgs")])
+def test_structs_follow_the_header(name, cls):
+    from paper_2609_39819_b200 import binding
+    want = header_struct(name)
+    got = getattr(binding, cls)._fields_
+    assert [f for f, _ in want] == [f[0] for f in got]
+    for (_, size), (_, ctype) in zip(want, got):
+        assert size in (0, C.sizeof(ctype))
+
+
+def test_null_arguments():
+    from paper_2609_39819_b200 import binding as B
+    lib = B.load_library()
+    a, t = B.AppendArgs(), B.AttendArgs()
+    assert lib.kvt_append_kv(None, C.byref(a), None) == B.E_INVAL
+    assert lib.kvt_attend(None, C.byref(t), None) == B.E_INVAL
+    assert lib.kvt_attend_scratch_bytes(None, C.byref(t)) == 0
+    assert lib.kvt_set_tail_pool(None, None, 0) == B.E_INVAL
+    assert lib.kvt_kv_check(None, None) == B.E_INVAL
+
+
+def test_rope_description():
+    from paper_2609_39819_b200 import binding as B
+    r = B.Rope(8, theta=100.0, sections=[1, 0, 3], device="cpu")
+    assert r.n_axes == 3 and r.axis_of.tolist() == [0, 2, 2, 2]
+    assert r.freqs.tolist() == pytest.approx([1.0, 100 ** -0.25, 0.1, 100 ** -0.75], rel=1e-15)
+    assert B.Rope(4, freqs=[1.0, 0.5], axis_of=[1, 0], device="cpu").n_axes == 2
+    assert B.Rope(0, device="cpu").freqs.numel() == 0
+    for bad in (dict(rot_dim=7), dict(rot_dim=8, sections=[1, 2]), dict(rot_dim=8, sections=[5, -1]),
+                dict(rot_dim=8, freqs=[1.0]), dict(rot_dim=8, axis_of=[0, 1]), dict(rot_dim=4, axis_of=[0, 256]),
+                dict(rot_dim=4, axis_of=[0, 1], sections=[1, 1])):
+        with pytest.raises(ValueError):
+            B.Rope(device="cpu", **bad)

@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 namespace kvt {
 
 typedef uint8_t u8;
@@ -286,14 +288,471 @@ __global__ void __launch_bounds__(ANY_THREADS) k_attend_any(AttendArgs a) {
   }
 }
 
-cudaError_t launch_attend(const AttendArgs &a, int sm_count, cudaStream_t s, u32 *launches) {
-  const u32 D = a.p.head_dim;
-  const u64 tiles = ((u64)a.b.n_tokens * a.group + ANY_ROWS - 1) / ANY_ROWS + a.b.n_seqs;   // no more than this many
-  const u32 smem = (ANY_ROWS * D + ANY_KEYS * (D + 1) + ANY_KEYS * D) * 4;
+// ------------------------------------------------------------------------------------------------------
+// Shared by the kernels that read the pool with TMA.
+// ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ u32 smem_addr(const void *p) { return (u32)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+__device__ __forceinline__ void bar_expect(u32 bar, u32 bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(u32 bar, u32 parity) {
+  u32 done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+// Waits for the barrier's phase, for a second at most (nothing a kernel waits for takes a millisecond).
+constexpr u64 WAIT_NS = 1000000000ull;
+__device__ __forceinline__ u64 now_ns() { u64 t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
+__device__ __noinline__ bool bar_wait_slow(u32 bar, u32 parity) {
+  const u64 t0 = now_ns();
+  do {
+    for (u32 i = 0; i < 64; ++i) if (bar_try(bar, parity)) return true;
+  } while (now_ns() - t0 < WAIT_NS);
+  return false;
+}
+__device__ __forceinline__ bool bar_wait(u32 bar, u32 parity) { return bar_try(bar, parity) || bar_wait_slow(bar, parity); }
+
+// One head of one block's K or V (chunk 2 * layer or 2 * layer + 1) into shared memory. A slot beyond both pools reads as
+// zeros: its coordinate lies behind the pool's last slot.
+__device__ __forceinline__ void load_block(const AttendArgs &a, const KvMaps &m, u32 dst, u32 bar, u32 slot, u32 chunk, u32 h, u32 halves) {
+  const bool tail = slot >= a.p.n_slots && slot - a.p.n_slots < a.p.n_tail;
+  const CUtensorMap *map = tail ? &m.tail : &m.pool;
+  u32 c3 = 2 * chunk, c4 = tail ? slot - a.p.n_slots : min(slot, a.p.n_slots);
+  if (!tail && a.layer_major) { c3 = 2 * c4; c4 = chunk; }
+  asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+               ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(h * halves), "r"(c3), "r"(c4), "r"(bar) : "memory");
+}
+
+// Pieces of work. The keys of a tile are cut into pieces when there are too few tiles to fill the GPU; every CTA works
+// the cut out for itself from the device-side lengths, so a captured launch follows them. A tile's blocks of keys are
+// bounded per sequence (whole sequence, or window plus the tokens of a tile).
+struct Piece { Seq q; u32 seq, tile, piece, pieces, part; };   // part: index of the piece's partial result, if pieces > 1
+__device__ __forceinline__ u32 seq_blocks(const AttendArgs &a, const Seq &q, u32 rows) {
+  u32 span = q.kv;
+  if (a.window) { const u64 w = (u64)a.window + min(q.n, rows / a.group + 2) + 2 * BT; span = (u32)min((u64)span, w); }
+  return (span + BT - 1) / BT;
+}
+template <u32 THREADS>
+__device__ __forceinline__ u32 block_scan(u32 n, u32 *s_sum, u32 &all) {     // exclusive
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u32 incl = n;
+#pragma unroll
+  for (u32 o = 1; o < 32; o *= 2) { const u32 y = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += y; }
+  __syncthreads();
+  if (lane == 31) s_sum[warp] = incl;
+  __syncthreads();
+  u32 before = 0; all = 0;
+#pragma unroll
+  for (u32 w = 0; w < THREADS / 32; ++w) { if (w < warp) before += s_sum[w]; all += s_sum[w]; }
+  return before + incl - n;
+}
+// plan_out[s] = {first partial, pieces} of every sequence, written by the CTA that is told to.
+template <u32 THREADS>
+__device__ bool find_piece(const AttendArgs &a, u32 rows, u32 min_chunk, u32 target, u32 want, uint2 *plan_out, Piece &out) {
+  __shared__ u32 s_sum[THREADS / 32], s_seq, s_item, s_pieces, s_part;
+  __shared__ unsigned long long s_work;
+  if (threadIdx.x == 0) { s_seq = 0xFFFFFFFFu; s_work = 0; }
+  __syncthreads();
+  auto tiles_of = [&](const Seq &x) { return (u32)(((u64)x.n * a.group + rows - 1) / rows); };
+  u64 mine = 0;
+  Seq first{0, 0, 0};
+  for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
+    const Seq x = load_seq(a.b, s, a.err);
+    if (s == threadIdx.x) first = x;
+    mine += (u64)tiles_of(x) * seq_blocks(a, x, rows);
+  }
+  if (mine) atomicAdd(&s_work, (unsigned long long)mine);
+  __syncthreads();
+  const u32 chunk = max(min_chunk, (u32)((s_work * a.p.n_kv_heads + target - 1) / target));
+  u32 item0 = 0, part0 = 0;
+  for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
+    const u32 s = s0 + threadIdx.x;
+    u32 items = 0, parts = 0, pieces = 1;
+    if (s < a.b.n_seqs) {
+      const Seq x = s0 ? load_seq(a.b, s, a.err) : first;
+      pieces = max(1u, (seq_blocks(a, x, rows) + chunk - 1) / chunk);
+      items = tiles_of(x) * pieces;
+      parts = pieces > 1 ? items : 0;
+    }
+    u32 all_items, all_parts;
+    const u32 at = item0 + block_scan<THREADS>(items, s_sum, all_items), pat = part0 + block_scan<THREADS>(parts, s_sum, all_parts);
+    if (want >= at && want < at + items) { s_seq = s; s_item = want - at; s_pieces = pieces; s_part = pat + (want - at); }
+    if (plan_out && s < a.b.n_seqs) plan_out[s] = make_uint2(pat, pieces);
+    item0 += all_items; part0 += all_parts;
+    if (!plan_out && want < item0) break;
+  }
+  __syncthreads();
+  if (s_seq == 0xFFFFFFFFu) return false;
+  out.seq = s_seq; out.pieces = s_pieces; out.part = s_part;
+  out.tile = s_item / s_pieces; out.piece = s_item % s_pieces;
+  out.q = load_seq(a.b, s_seq, a.err);
+  return true;
+}
+
+// Partial results: per piece and KV head `rows` rows of head_dim sums, then (maximum, sum) pairs of all pieces.
+__device__ __forceinline__ uint2 *scratch_plan(const AttendArgs &a) { return (uint2 *)a.scratch; }
+__device__ __forceinline__ float *scratch_sums(const AttendArgs &a) { return (float *)(a.scratch + ((a.b.n_seqs * 8ull + 255) & ~255ull)); }
+
+// Joins the pieces of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. One warp per row (token, head); rows of
+// sequences that were not cut are already written. Launched behind the piece kernel and waits for all of it.
+template <class T, u32 D>
+__global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u64 n_parts) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const u32 lane = threadIdx.x & 31;
+  const u64 id = (u64)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id % a.n_q_heads);
+  if (t >= a.b.n_tokens) return;
+  u32 seq = 0;                           // starts are cut like load_seq cuts them; the first sequence the token lies in
+  bool found = false;
+  for (u32 s0 = 0; s0 < a.b.n_seqs && !found; s0 += 32) {
+    const u32 s = s0 + lane;
+    const u32 hit = __ballot_sync(~0u, s < a.b.n_seqs && a.b.q_start[s] <= t && t < a.b.q_start[s + 1]);
+    if (hit) { seq = s0 + __ffs(hit) - 1; found = true; }
+  }
+  if (!found) return;
+  const uint2 plan = scratch_plan(a)[seq];
+  if (plan.y <= 1) return;
+  const u32 h = hq / a.group, r = (t - a.b.q_start[seq]) * a.group + hq % a.group, tile = r / rows, row = r % rows;
+  const u64 p0 = ((u64)plan.x + (u64)tile * plan.y) * a.p.n_kv_heads + h;
+  const float *sums = scratch_sums(a);
+  const float2 *ml = (const float2 *)(sums + n_parts * rows * D);
+  if (p0 + (u64)(plan.y - 1) * a.p.n_kv_heads >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); return; }
+  float m = -INFINITY;
+  for (u32 i = lane; i < plan.y; i += 32) m = fmaxf(m, ml[(p0 + (u64)i * a.p.n_kv_heads) * rows + row].x);
+#pragma unroll
+  for (u32 o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, acc[D / 32];
+#pragma unroll
+  for (u32 c = 0; c < D / 32; ++c) acc[c] = 0.0f;
+  for (u32 i = 0; i < plan.y; ++i) {
+    const u64 at = (p0 + (u64)i * a.p.n_kv_heads) * rows + row;
+    const float2 x = ml[at];
+    if (x.x == -INFINITY) continue;      // a piece without keys for this row has no sums
+    const float w = exp2f(x.x - ref);
+    l += w * x.y;
+    const float *o = sums + at * D + lane * (D / 32);
+#pragma unroll
+    for (u32 c = 0; c < D / 32; ++c) acc[c] += w * o[c];
+  }
+  const float inv = l > 0.0f ? 1.0f / l : l;
+  T *o = (T *)a.out + t * a.o_ts + hq * a.o_hs + lane * (D / 32);
+#pragma unroll
+  for (u32 c = 0; c < D / 32; ++c) o[c] = Elem<T>::down1(acc[c] * inv);
+  if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// ------------------------------------------------------------------------------------------------------
+// Few rows (one new token per sequence, small chunks): bound by reading K and V once. A CTA of four warps takes a piece of
+// the keys for up to 16 rows of one KV head, the height of a warp-level matrix instruction. Every warp has its own ring
+// of TMA loads (a block's K and V per stage) and its own running maximum and sums over every fourth block, so warps
+// never wait for one another until the end. Two CTAs per SM keep up to 192 KB of loads in flight.
+// ------------------------------------------------------------------------------------------------------
+constexpr u32 SPLIT_ROWS = 16, SPLIT_WARPS = 4, SPLIT_THREADS = SPLIT_WARPS * 32;
+template <u32 D> struct SplitShape {
+  static constexpr u32 BLOCK = BT * D * 2, STAGES = 3 * 128 / D, RING = STAGES * 2 * BLOCK, SMEM = SPLIT_WARPS * RING + 1024;
+};
+
+template <class T> __device__ __forceinline__ void mma16816(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1);
+template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldm4(u32 (&r)[4], u32 addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldm4t(u32 (&r)[4], u32 addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// Place of (token r, 16 bytes c of the head) in a loaded block: [r / 8][c / 8][r % 8][c % 8], swizzled.
+template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
+  return (r / 8) * (D * 16) + (c / 8) * 1024 + (r % 8) * 128 + (((c % 8) ^ (r % 8)) * 16);
+}
+
+template <class T, u32 D>
+__global__ void __launch_bounds__(SPLIT_THREADS, 2)
+k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 min_chunk, u32 target, u64 n_parts) {
+  typedef SplitShape<D> S;
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 bars[SPLIT_WARPS * S::STAGES];
+  __shared__ float s_ml[SPLIT_WARPS][SPLIT_ROWS][2];
+  asm volatile("griddepcontrol.launch_dependents;");
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
+  const u32 h = blockIdx.x % H, item = blockIdx.x / H;
+  const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8;
+  if (lane == 0) {
+    for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  Piece w;
+  if (!find_piece<SPLIT_THREADS>(a, SPLIT_ROWS, min_chunk, target, item, n_parts && blockIdx.x == 0 ? scratch_plan(a) : nullptr, w)) return;
+  const Seq q = w.q;
+  const u32 n_rows = q.n * a.group, r0 = w.tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
+  u32 first, last, all_lo, all_hi;       // keys any row sees; keys every row sees
+  row_range(a, q, r0 / a.group, first, all_hi);
+  row_range(a, q, r1 / a.group, all_lo, last);
+  // blocks of this piece
+  const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+  const u32 per = (nb + w.pieces - 1) / w.pieces;
+  const u32 b0 = b_first + min(w.piece * per, nb), b1 = b_first + min((w.piece + 1) * per, nb);
+  const u32 ring = ((smem_addr(smem_raw) + 1023) & ~1023u) + warp * S::RING;
+  const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
+  const u32 *row = a.b.table + w.seq * a.b.table_stride;
+  u32 slots = 0;                         // lane i: the slot of this warp's block number (i mod 32) of the current 32
+  auto fetch_slots = [&](u32 i0) { const u32 i = i0 + lane; slots = i < n_mine ? row[b0 + warp + i * SPLIT_WARPS] : 0; };
+  auto load = [&](u32 i) {               // i-th block of this warp; whole warp
+    if (i % 32 == 0) {
+      fetch_slots(i);
+      if (i + lane < n_mine && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+    }
+    const u32 slot = __shfl_sync(~0u, slots, i % 32);
+    if (lane == 0) {
+      const u32 st = i % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
+      bar_expect(bar, 2 * S::BLOCK);
+      load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
+      load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
+    }
+  };
+  const u32 n_pro = min(n_mine, S::STAGES);
+  for (u32 i = 0; i < n_pro; ++i) load(i);
+
+  // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
+  u32 qf[D / 16][4];
+  u32 lo[2], hi[2];
+#pragma unroll
+  for (u32 x = 0; x < 2; ++x) {
+    const u32 r = min(r0 + lane / 4 + 8 * x, r1);     // rows behind the last one repeat it and are not written
+    row_range(a, q, r / a.group, lo[x], hi[x]);
+    const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
+    const bool even = ((uintptr_t)src & 3) == 0;
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y) {
+        const u16 *p = src + k * 16 + y * 8;
+        qf[k][x + 2 * y] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+      }
+  }
+  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+    for (u32 x = 0; x < 4; ++x) o[n][x] = 0.0f;
+
+  bool ok = true;
+  for (u32 i = 0; i < n_mine; ++i) {
+    const u32 st = i % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
+    if (!bar_wait(bar0 + st * 8, (i / S::STAGES) & 1)) { ok = false; break; }
+    const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
+    // scores of 16 keys: two column groups of 8
+    float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k) {
+      u32 f[4];
+      ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
+      mma16816<T>(s[0], qf[k], f[0], f[1]);
+      mma16816<T>(s[1], qf[k], f[2], f[3]);
+    }
+    if (key0 + BT > q.kv) {              // the last block's tokens behind the length: whatever their values hold, weight 0
+      const u32 r = lane / 2;            // must not meet an Inf or a NaN
+      if (key0 + r >= q.kv)
+#pragma unroll
+        for (u32 c = 0; c < D / 16; ++c)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+      __syncwarp();
+    }
+    const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+      for (u32 x = 0; x < 4; ++x) {
+        const u32 key = key0 + n * 8 + (lane % 4) * 2 + (x & 1);
+        float v = s[n][x] * a.scale_log2;
+        if (!whole && (key < lo[x >> 1] || key >= hi[x >> 1])) v = -INFINITY;
+        s[n][x] = v;
+        top[x >> 1] = fmaxf(top[x >> 1], v);
+      }
+#pragma unroll
+    for (u32 x = 0; x < 2; ++x) {
+      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
+      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
+    }
+    // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
+    // those below 1, and most blocks then need no rescaling.
+    if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+#pragma unroll
+      for (u32 x = 0; x < 2; ++x) {
+        const float now = fmaxf(m[x], top[x]), f = now == -INFINITY ? 1.0f : ex2(m[x] - now);
+        m[x] = now; l[x] *= f;
+#pragma unroll
+        for (u32 n = 0; n < D / 8; ++n) { o[n][2 * x] *= f; o[n][2 * x + 1] *= f; }
+      }
+    }
+    const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+#pragma unroll
+    for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+      for (u32 x = 0; x < 4; ++x) { s[n][x] = ex2(s[n][x] - ref[x >> 1]); l[x >> 1] += s[n][x]; }
+    const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
+                      Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
+#pragma unroll
+    for (u32 n = 0; n < D / 16; ++n) {
+      u32 f[4];
+      ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
+      mma16816<T>(o[2 * n], p, f[0], f[1]);
+      mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+    }
+    __syncwarp();                        // the stage is read: refill it
+    if (i + S::STAGES < n_mine) load(i + S::STAGES);
+  }
+  if (!ok) {                             // let the copies in flight land, for a while, before the CTA ends
+    if (lane == 0) kv_err(a.err, KVERR_WAIT);
+    for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
+  }
+
+  // join the four warps: sums through the (now idle) rings. A ring whose wait ran out may still be written by a late copy:
+  // that only spoils a result already reported as lost.
+#pragma unroll
+  for (u32 x = 0; x < 2; ++x) {
+    l[x] += __shfl_xor_sync(~0u, l[x], 1);
+    l[x] += __shfl_xor_sync(~0u, l[x], 2);
+    if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * x][0] = m[x]; s_ml[warp][lane / 4 + 8 * x][1] = l[x]; }
+  }
+  constexpr u32 LD = D + 8;              // row pitch in floats: the four rows of a quarter warp fall on different banks
+  static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
+  float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
+#pragma unroll
+  for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+    for (u32 x = 0; x < 2; ++x)
+      *(float2 *)&so[(lane / 4 + 8 * x) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * x], o[n][2 * x + 1]);
+  __syncthreads();
+  const u32 r = tid / 8, c0 = (tid % 8) * 4;       // thread: row r, four columns out of every 32
+  float mm = -INFINITY, ll = 0.0f, f[SPLIT_WARPS];
+#pragma unroll
+  for (u32 x = 0; x < SPLIT_WARPS; ++x) mm = fmaxf(mm, s_ml[x][r][0]);
+  const float ref = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+  for (u32 x = 0; x < SPLIT_WARPS; ++x) { f[x] = ex2(s_ml[x][r][0] - ref); ll += f[x] * s_ml[x][r][1]; }
+  if (r0 + r > r1) return;
+  const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
+  const float *base = (const float *)(smem_raw + (ring - warp * S::RING - smem_addr(smem_raw))) + r * LD;
+  const u64 part = (u64)w.part * H + h;
+  const bool direct = w.pieces == 1;
+  if (!direct && part >= n_parts) { kv_err(a.err, KVERR_RANGE); return; }
+  const float inv = !direct ? 1.0f : ll > 0.0f ? 1.0f / ll : ll;
+  T *const out = (T *)a.out + t * a.o_ts + hq * a.o_hs;
+  float *const sums = scratch_sums(a) + (part * SPLIT_ROWS + r) * D;
+#pragma unroll
+  for (u32 c = c0; c < D; c += 32) {
+    float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (u32 x = 0; x < SPLIT_WARPS; ++x) {
+      const float4 y = *(const float4 *)(base + x * (S::RING / 4) + c);
+      v.x += f[x] * y.x; v.y += f[x] * y.y; v.z += f[x] * y.z; v.w += f[x] * y.w;
+    }
+    if (direct) {
+      const u32 p = Elem<T>::down(v.x * inv, v.y * inv), z = Elem<T>::down(v.z * inv, v.w * inv);
+      u16 *d = (u16 *)out + c;
+      if (((uintptr_t)d & 7) == 0) *(uint2 *)d = make_uint2(p, z);
+      else { d[0] = (u16)p; d[1] = (u16)(p >> 16); d[2] = (u16)z; d[3] = (u16)(z >> 16); }
+    } else {
+      *(float4 *)(sums + c) = v;
+    }
+  }
+  if (tid % 8 == 0) {
+    if (!direct) ((float2 *)(scratch_sums(a) + n_parts * SPLIT_ROWS * D))[part * SPLIT_ROWS + r] = make_float2(mm, ll);
+    else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (mm + log2f(ll)) * 0.69314718055994531f;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------------------
+bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 n_chunks, u64 n_kv_heads, u64 head_dim) {
+  typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                             const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  void *fn = nullptr;
+  cudaDriverEntryPointQueryResult got;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+      got != cudaDriverEntryPointSuccess || !fn) {
+    cudaGetLastError();
+    return false;
+  }
+  const u64 tok = n_kv_heads * head_dim * 2, chunk = BT * tok;
+  // 64 elements | 8 tokens | 64-element parts of a token's heads | halves of blocks | the other index
+  const cuuint64_t dims[5] = {64, 8, n_kv_heads * head_dim / 64, 2 * (layer_major ? n_slots : n_chunks), layer_major ? n_chunks : n_slots};
+  const cuuint64_t strides[4] = {tok, 128, 8 * tok, chunk * (layer_major ? n_slots : n_chunks)};
+  const cuuint32_t box[5] = {64, 8, (cuuint32_t)(head_dim / 64), 2, 1}, es[5] = {1, 1, 1, 1, 1};
+  return ((Encode)fn)(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Partial results a launch can leave, times KV heads.
+static u64 plan_parts(const AttendArgs &a, const AttendPlan &p) { return 2ull * p.target + 2 * a.p.n_kv_heads; }
+
+template <class T, u32 D>
+static cudaError_t launch_join(const AttendArgs &a, const AttendPlan &p, u64 parts, cudaStream_t s, u32 *launches) {
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3((u32)(((u64)a.b.n_tokens * a.n_q_heads + 3) / 4)); c.blockDim = dim3(128); c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at; c.numAttrs = 1;
+  ++*launches;
+  return cudaLaunchKernelEx(&c, k_attend_join<T, D>, a, p.rows, parts);
+}
+
+AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
+  AttendPlan p{};
+  const u64 H = a.p.n_kv_heads;
+  auto tiles = [&](u64 rows) { return ((u64)a.b.n_tokens * a.group + rows - 1) / rows + a.b.n_seqs; };   // no more than this many
+  if (a.p.head_dim != 64 && a.p.head_dim != 128) {
+    p.rows = ANY_ROWS;
+    p.grid = (u32)std::min<u64>(tiles(p.rows), 0x7FFFFFFFu);
+    return p;
+  }
+  p.kind = 1;
+  p.rows = SPLIT_ROWS; p.min_chunk = 16; p.target = 4 * sm_count;
+  // Cutting every sequence into ceil(blocks / chunk) pieces with chunk >= work / target gives at most target pieces more
+  // than there are tiles, and at most twice target pieces of sequences that are cut at all.
+  const bool cut = a.b.max_blocks > p.min_chunk;
+  p.grid = (u32)std::min<u64>(tiles(p.rows) * H + (cut ? p.target + H : 0), 0x7FFFFFFFu);
+  if (cut) p.scratch_bytes = ((a.b.n_seqs * 8ull + 255) & ~255ull) + plan_parts(a, p) * p.rows * (a.p.head_dim + 2) * 4;
+  return p;
+}
+
+template <class T, u32 D>
+static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
+  cudaError_t r = cudaFuncSetAttribute(k_attend_split<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitShape<D>::SMEM);
+  if (r != cudaSuccess) return r;
+  const u64 parts = p.scratch_bytes ? plan_parts(a, p) : 0;
+  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.min_chunk, p.target, parts);
+  ++*launches;
+  if ((r = cudaGetLastError()) != cudaSuccess || !parts) return r;
+  return launch_join<T, D>(a, p, parts, s, launches);
+}
+
+cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
+  if (p.kind == 1) {
+    if (a.p.head_dim == 64) return a.fp16 ? launch_split<__half, 64>(a, p, m, s, launches) : launch_split<__nv_bfloat16, 64>(a, p, m, s, launches);
+    return a.fp16 ? launch_split<__half, 128>(a, p, m, s, launches) : launch_split<__nv_bfloat16, 128>(a, p, m, s, launches);
+  }
+  const u32 D = a.p.head_dim, smem = (ANY_ROWS * D + ANY_KEYS * (D + 1) + ANY_KEYS * D) * 4;
   auto kern = a.fp16 ? k_attend_any<__half> : k_attend_any<__nv_bfloat16>;
   cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (r != cudaSuccess) return r;
-  kern<<<dim3((u32)tiles, a.p.n_kv_heads), ANY_THREADS, smem, s>>>(a);
+  kern<<<dim3(p.grid, a.p.n_kv_heads), ANY_THREADS, smem, s>>>(a);
   ++*launches;
   return cudaGetLastError();
 }

@@ -39,11 +39,31 @@ struct AttendArgs {
   const void *q; void *out; float *lse;
   uint64_t q_ts, q_hs, o_ts, o_hs;
   uint32_t n_q_heads, group, window, full, fp16;
+  uint32_t layer, layer_major;
+  uint8_t *scratch;
   float scale_log2;                 // scale / ln 2: scores in powers of two
   uint32_t *err;
 };
 
+// Tensor maps of the pool and of the tail blocks (tail = pool where there are none), for head sizes of 64 and 128: a box
+// is one head of a block's 16 tokens, and lands in shared memory as [2][head_dim / 64][8 tokens][64] with 128-byte
+// swizzle, the operand layout of the matrix instructions. A coordinate behind the last slot reads as zeros.
+struct KvMaps { CUtensorMap pool, tail; };
+bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, uint64_t n_slots, uint64_t n_chunks, uint64_t n_kv_heads,
+                 uint64_t head_dim);
+
+// What kvt_attend does, decided from sizes alone.
+struct AttendPlan {
+  uint32_t kind;             // 0 any head size, 1 few rows, split over the keys
+  uint32_t rows;             // rows of a tile
+  uint32_t min_chunk;        // a piece of a tile's keys is at least this many blocks
+  uint32_t target;           // pieces the whole batch is cut into, if it is long enough
+  uint32_t grid;             // work items times KV heads, at most
+  uint64_t scratch_bytes;
+};
+AttendPlan plan_attend(const AttendArgs &a, uint32_t max_q_len, int sm_count);
+
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, uint32_t *launches);
-cudaError_t launch_attend(const AttendArgs &a, int sm_count, cudaStream_t s, uint32_t *launches);
+cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint32_t *launches);
 
 }  // namespace kvt

@@ -157,6 +157,7 @@ struct kvt_engine {
   bool metadata_only;
   int sm_count = 148;
   int device = 0;
+  KvMaps kv_maps{}; bool kv_maps_ok = false;   // for head sizes of 64 and 128
   u8 *tail_pool = nullptr; u32 n_tail = 0;   // blocks outside every tier (kvt_set_tail_pool)
   // host state
   std::vector<Ctx> ctxs;
@@ -1014,6 +1015,11 @@ int32_t kvt_create(const kvt_config *cfg, void *stream, kvt_engine **out) {
   }
   e->device = dev;
   cudaDeviceGetAttribute(&e->sm_count, cudaDevAttrMultiProcessorCount, dev);
+  if (!meta_only && c.elem_bytes == 2 && (c.head_dim == 64 || c.head_dim == 128)) {
+    e->kv_maps_ok = make_kv_map(&e->kv_maps.pool, c.hbm_pool, c.pool_layout == KVT_LAYOUT_LAYER_MAJOR, c.n_hbm_blocks, n_chunks,
+                                c.n_kv_heads, c.head_dim);
+    e->kv_maps.tail = e->kv_maps.pool;
+  }
   if (!meta_only && c.stage_buf && c.stage_bytes) {
     kvt_engine::Staging &g = e->stg;
     g.buf = (u8 *)c.stage_buf;
@@ -2300,6 +2306,7 @@ int32_t kv_launched(kvt_engine *e, cudaError_t x, u32 launches) {
 }
 const char *attend_fault(const kvt_engine *e, const kvt_attend_args &a) {
   if (const char *m = kv_engine_fault(e, a.layer, a.dtype)) return m;
+  if ((e->cfg.head_dim == 64 || e->cfg.head_dim == 128) && !e->kv_maps_ok) return "attend: no tensor map of this pool (address, size or driver)";
   if (e->cfg.head_dim > 256) return "attend: head_dim above 256";
   if (!a.n_q_heads || a.n_q_heads % e->cfg.n_kv_heads) return "attend: n_q_heads is not a multiple of n_kv_heads";
   if ((a.flags & ~KVT_ATTN_FULL) || ((a.flags & KVT_ATTN_FULL) && a.window)) return "attend: flags";
@@ -2315,6 +2322,8 @@ AttendArgs attend_args(kvt_engine *e, const kvt_attend_args &a) {
   x.window = a.window; x.full = a.flags & KVT_ATTN_FULL; x.fp16 = a.dtype == KVT_KV_FP16;
   const double scale = a.scale > 0.0f ? (double)a.scale : 1.0 / std::sqrt((double)e->cfg.head_dim);
   x.scale_log2 = (float)(scale * 1.4426950408889634);
+  x.layer = a.layer; x.layer_major = e->cfg.pool_layout == KVT_LAYOUT_LAYER_MAJOR;
+  x.scratch = (u8 *)a.scratch;
   x.err = e->dp<u32>(e->L.kv_err);
   return x;
 }
@@ -2353,7 +2362,7 @@ int32_t kvt_append_kv(kvt_engine *e, const kvt_append_args *args, void *stream) 
 
 uint64_t kvt_attend_scratch_bytes(kvt_engine *e, const kvt_attend_args *args) {
   if (!e || !args || attend_fault(e, *args) || !args->b.n_seqs || !args->b.n_tokens) return 0;
-  return 0;
+  return plan_attend(attend_args(e, *args), args->b.max_q_len, e->sm_count).scratch_bytes;
 }
 
 int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *args, void *stream) {
@@ -2366,8 +2375,14 @@ int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *args, void *stream) {
   if ((u64)a.b.n_tokens * a.n_q_heads > 0xFFFFFFFFull) return fail(e, KVT_E_INVAL, "attend: batch too large");
   OnDevice on(e->device);
   if (!on.ok) return fail(e, KVT_E_CUDA, "attend: device");
+  const AttendArgs x = attend_args(e, a);
+  const AttendPlan p = plan_attend(x, a.b.max_q_len, e->sm_count);
+  if (p.scratch_bytes) {
+    if (!a.scratch || a.scratch_bytes < p.scratch_bytes) return fail(e, KVT_E_BUFSZ, "attend: scratch too small");
+    if ((uintptr_t)a.scratch & 15) return fail(e, KVT_E_INVAL, "attend: misaligned scratch");
+  }
   u32 launches = 0;
-  const cudaError_t r = launch_attend(attend_args(e, a), e->sm_count, (cudaStream_t)stream, &launches);
+  const cudaError_t r = launch_attend(x, p, e->kv_maps, (cudaStream_t)stream, &launches);
   return kv_launched(e, r, launches);
 }
 
@@ -2377,6 +2392,11 @@ int32_t kvt_set_tail_pool(kvt_engine *e, void *pool, uint64_t bytes) {
   if ((uintptr_t)pool & 15) return fail(e, KVT_E_INVAL, "tail pool: misaligned");
   const u64 n = pool ? bytes / e->block_bytes : 0;
   if (n + e->cfg.n_hbm_blocks >= 0x7FFFFFFFull) return fail(e, KVT_E_INVAL, "tail pool: too many blocks");
+  KvMaps m = e->kv_maps;
+  m.tail = m.pool;
+  if (n && e->kv_maps_ok && !make_kv_map(&m.tail, pool, false, n, e->n_chunks, e->cfg.n_kv_heads, e->cfg.head_dim))
+    return fail(e, KVT_E_CUDA, "tail pool: no tensor map");
+  e->kv_maps = m;
   e->tail_pool = n ? (u8 *)pool : nullptr;
   e->n_tail = (u32)n;
   return KVT_OK;

@@ -305,7 +305,7 @@ __device__ __forceinline__ bool bar_try(u32 bar, u32 parity) {
 // Waits for the barrier's phase, for a second at most (nothing a kernel waits for takes a millisecond).
 constexpr u64 WAIT_NS = 1000000000ull;
 __device__ __forceinline__ u64 now_ns() { u64 t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
-__device__ __noinline__ bool bar_wait_slow(u32 bar, u32 parity) {
+__device__ __forceinline__ bool bar_wait_slow(u32 bar, u32 parity) {
   const u64 t0 = now_ns();
   do {
     for (u32 i = 0; i < 64; ++i) if (bar_try(bar, parity)) return true;
@@ -349,11 +349,16 @@ __device__ __forceinline__ u32 block_scan(u32 n, u32 *s_sum, u32 &all) {     // 
   return before + incl - n;
 }
 // plan_out[s] = {first partial, pieces} of every sequence, written by the CTA that is told to.
-template <u32 THREADS>
-__device__ bool find_piece(const AttendArgs &a, u32 rows, u32 min_chunk, u32 target, u32 want, uint2 *plan_out, Piece &out) {
-  __shared__ u32 s_sum[THREADS / 32], s_seq, s_item, s_pieces, s_part;
+// Length of a piece in blocks. Work over target, or (WAVES) whatever makes the waves of one CTA per SM end soonest: of
+// the longest sequence cut into 1 .. MAX_CUTS pieces (and the others into pieces no longer), the one with the smallest
+// waves * (piece + what a piece costs besides), among those that leave at most `target` partial results per launch.
+constexpr u32 MAX_CUTS = 32, PIECE_COST = 32;
+template <u32 THREADS, bool WAVES>
+__device__ bool find_piece(const AttendArgs &a, u32 rows, u32 min_chunk, u32 target, u32 sms, u32 want, uint2 *plan_out, Piece &out) {
+  __shared__ u32 s_sum[THREADS / 32], s_seq, s_item, s_pieces, s_part, s_longest, s_items[MAX_CUTS], s_parts[MAX_CUTS], s_chunk;
   __shared__ unsigned long long s_work;
-  if (threadIdx.x == 0) { s_seq = 0xFFFFFFFFu; s_work = 0; }
+  if (threadIdx.x == 0) { s_seq = 0xFFFFFFFFu; s_work = 0; s_longest = 0; }
+  if (WAVES && threadIdx.x < MAX_CUTS) s_items[threadIdx.x] = s_parts[threadIdx.x] = 0;
   __syncthreads();
   auto tiles_of = [&](const Seq &x) { return (u32)(((u64)x.n * a.group + rows - 1) / rows); };
   u64 mine = 0;
@@ -361,11 +366,37 @@ __device__ bool find_piece(const AttendArgs &a, u32 rows, u32 min_chunk, u32 tar
   for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
     const Seq x = load_seq(a.b, s, a.err);
     if (s == threadIdx.x) first = x;
-    mine += (u64)tiles_of(x) * seq_blocks(a, x, rows);
+    mine += WAVES ? (x.n ? seq_blocks(a, x, rows) : 0) : (u64)tiles_of(x) * seq_blocks(a, x, rows);
+    if (WAVES) { atomicMax(&s_longest, (u32)mine); mine = 0; }
   }
-  if (mine) atomicAdd(&s_work, (unsigned long long)mine);
+  if (!WAVES && mine) atomicAdd(&s_work, (unsigned long long)mine);
   __syncthreads();
-  const u32 chunk = max(min_chunk, (u32)((s_work * a.p.n_kv_heads + target - 1) / target));
+  if (WAVES) {
+    const u32 longest = s_longest;
+    auto chunk_of = [&](u32 k) { return max(min_chunk, ((longest + k) / (k + 1) + 7) / 8 * 8); };     // whole tiles of 8 blocks
+    if (longest > min_chunk && target)
+      for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
+        const Seq x = s == threadIdx.x ? first : load_seq(a.b, s, a.err);
+        const u32 tiles = tiles_of(x), nb = seq_blocks(a, x, rows);
+        for (u32 k = 0; k < MAX_CUTS && tiles; ++k) {
+          const u32 c = chunk_of(k), n = max(1u, (nb + c - 1) / c);
+          atomicAdd(&s_items[k], tiles * n);
+          if (n > 1) atomicAdd(&s_parts[k], tiles * n);
+        }
+      }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      const u32 k = threadIdx.x, c = chunk_of(k);
+      u64 cost = (u64)((s_items[k] * a.p.n_kv_heads + sms - 1) / sms) * (c + PIECE_COST);
+      if (longest <= min_chunk || !target ? k > 0 : s_parts[k] * a.p.n_kv_heads > target && k > 0) cost = ~0ull >> 8;
+      cost = cost << 8 | k;
+#pragma unroll
+      for (u32 o = 16; o; o /= 2) { const u64 y = __shfl_xor_sync(~0u, cost, o); cost = y < cost ? y : cost; }
+      if (k == 0) s_chunk = (cost & 255) ? chunk_of((u32)(cost & 255)) : max(longest, 1u);
+    }
+    __syncthreads();
+  }
+  const u32 chunk = WAVES ? s_chunk : max(min_chunk, (u32)((s_work * a.p.n_kv_heads + target - 1) / target));
   u32 item0 = 0, part0 = 0;
   for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
     const u32 s = s0 + threadIdx.x;
@@ -378,16 +409,17 @@ __device__ bool find_piece(const AttendArgs &a, u32 rows, u32 min_chunk, u32 tar
     }
     u32 all_items, all_parts;
     const u32 at = item0 + block_scan<THREADS>(items, s_sum, all_items), pat = part0 + block_scan<THREADS>(parts, s_sum, all_parts);
-    if (want >= at && want < at + items) { s_seq = s; s_item = want - at; s_pieces = pieces; s_part = pat + (want - at); }
+    if (want >= at && want < at + items) { s_seq = s; s_item = want - at; s_pieces = pieces; s_part = pat; }
     if (plan_out && s < a.b.n_seqs) plan_out[s] = make_uint2(pat, pieces);
     item0 += all_items; part0 += all_parts;
     if (!plan_out && want < item0) break;
   }
   __syncthreads();
   if (s_seq == 0xFFFFFFFFu) return false;
-  out.seq = s_seq; out.pieces = s_pieces; out.part = s_part;
-  out.tile = s_item / s_pieces; out.piece = s_item % s_pieces;
   out.q = load_seq(a.b, s_seq, a.err);
+  out.seq = s_seq; out.pieces = s_pieces; out.piece = s_item % s_pieces;
+  out.tile = tiles_of(out.q) - 1 - s_item / s_pieces;     // last tokens first: with a causal mask they have the most keys
+  out.part = s_part + out.tile * s_pieces + out.piece;
   return true;
 }
 
@@ -493,7 +525,7 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   Piece w;
-  if (!find_piece<SPLIT_THREADS>(a, SPLIT_ROWS, min_chunk, target, item, n_parts && blockIdx.x == 0 ? scratch_plan(a) : nullptr, w)) return;
+  if (!find_piece<SPLIT_THREADS, false>(a, SPLIT_ROWS, min_chunk, target, 0, item, n_parts && blockIdx.x == 0 ? scratch_plan(a) : nullptr, w)) return;
   const Seq q = w.q;
   const u32 n_rows = q.n * a.group, r0 = w.tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
   u32 first, last, all_lo, all_hi;       // keys any row sees; keys every row sees
@@ -550,7 +582,7 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
   bool ok = true;
   for (u32 i = 0; i < n_mine; ++i) {
     const u32 st = i % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
-    if (!bar_wait(bar0 + st * 8, (i / S::STAGES) & 1)) { ok = false; break; }
+    if (!__all_sync(~0u, bar_wait(bar0 + st * 8, (i / S::STAGES) & 1))) { ok = false; break; }
     const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
     // scores of 16 keys: two column groups of 8
     float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -676,6 +708,366 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
 }
 
 // ------------------------------------------------------------------------------------------------------
+// Many rows (prompts, chunks of new tokens): bound by the tensor cores and the exponentials. A CTA takes up to 256 rows
+// of one KV head as two tiles of 128, the height of a tcgen05 matrix instruction, and walks over the keys 128 at a time.
+//   warp 9      (10 and 11 only give up their registers) loads K and V (TMA, one box per block) into a ring of 128-key stages
+//   warp 8      issues the matrix products: S = Q K^T and O += P V, both accumulated in tensor memory
+//   warps 0-7   one thread per row: maximum, powers, sum; P goes back to tensor memory in the place of S, as the first
+//               operand of the second product
+// The two tiles take turns: while one tile's powers are computed the tensor cores work on the other. Tensor memory: S0,
+// S1 (128 columns each), O0, O1 (head_dim columns each).
+// ------------------------------------------------------------------------------------------------------
+constexpr u32 TC_ROWS = 256, TC_TILE = 128, TC_KEYS = 128, TC_KB = TC_KEYS / BT, TC_THREADS = 384;
+template <u32 D> struct TcShape {
+  static constexpr u32 BLOCK = BT * D * 2, STAGE = TC_KEYS * D * 2, Q = TC_ROWS * D * 2, STAGES = (224 * 1024 - Q) / STAGE;
+  static constexpr u32 SMEM = Q + STAGES * STAGE + 1024;
+};
+
+__device__ __forceinline__ void bar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool elect_one() {
+  u32 p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ void tc_commit(u32 bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Shared-memory operand with 128-byte swizzle (bits 61-63 = 2; bit 46 = version 1): lbo, sbo = distances in bytes between 64-element
+// parts / between groups of 8 rows.
+__device__ __forceinline__ u64 tc_desc(u32 addr, u32 lbo, u32 sbo) {
+  return (u64)((addr & 0x3FFFF) >> 4) | (u64)(lbo >> 4) << 16 | (u64)(sbo >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Instruction descriptor of kind::f16: 32-bit sums, 128 rows, n columns; second operand with its columns (false: its sum
+// index) in the outer place of shared memory.
+__device__ __forceinline__ u32 tc_idesc(bool fp16, u32 n, bool b_transposed) {
+  const u32 t = fp16 ? 0u : 1u;
+  return 1u << 4 | t << 7 | t << 10 | (b_transposed ? 1u : 0u) << 16 | (n >> 3) << 17 | (TC_TILE >> 4) << 24;
+}
+__device__ __forceinline__ void tc_mma_ss(u32 d, u64 a, u64 b, u32 idesc, u32 acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(u32 d, u32 a, u64 b, u32 idesc, u32 acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+#define TC_R4(f, x, i) f(x[i]), f(x[i + 1]), f(x[i + 2]), f(x[i + 3])
+#define TC_R16(f, x, i) TC_R4(f, x, i), TC_R4(f, x, i + 4), TC_R4(f, x, i + 8), TC_R4(f, x, i + 12)
+__device__ __forceinline__ void tc_ld32(u32 *r, u32 addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+               "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : TC_R16("=r", r, 0), TC_R16("=r", r, 16) : "r"(addr));
+}
+__device__ __forceinline__ void tc_st32(u32 addr, const u32 *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+               "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+               ::"r"(addr), TC_R16("r", r, 0), TC_R16("r", r, 16) : "memory");
+}
+
+__device__ __forceinline__ void tc_ld16(u32 *r, u32 addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : TC_R16("=r", r, 0) : "r"(addr));
+}
+__device__ __forceinline__ void tc_st16(u32 addr, const u32 *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(addr), TC_R16("r", r, 0) : "memory");
+}
+
+// A wait that also ends when another warp of the CTA has given up; gives up itself after WAIT_NS.
+__device__ __forceinline__ bool tc_wait_slow(u32 bar, u32 parity, volatile u32 *lost) {
+  const u64 t0 = now_ns();
+  do {
+    for (u32 i = 0; i < 32; ++i) if (bar_try(bar, parity)) return true;
+    if (*lost) return false;
+  } while (now_ns() - t0 < WAIT_NS);
+  *lost = 1;
+  return false;
+}
+// Whole warps wait, and come back with one answer.
+__device__ __forceinline__ bool tc_wait(u32 bar, u32 parity, volatile u32 *lost) {
+  return __all_sync(~0u, bar_try(bar, parity) || tc_wait_slow(bar, parity, lost));
+}
+
+template <class T, u32 D>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 min_chunk, u32 target, u32 sms, u64 n_parts) {
+  typedef TcShape<D> S;
+  constexpr bool FP16 = sizeof(T) == 2 && !__is_same(T, __nv_bfloat16);
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2], s_qready, s_drain;
+  __shared__ u32 s_tmem;
+  __shared__ volatile u32 s_lost;
+  asm volatile("griddepcontrol.launch_dependents;");
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
+  const u32 h = blockIdx.x % H, item = blockIdx.x / H;
+  const u32 full = smem_addr(s_full), empty = smem_addr(s_empty), sready = smem_addr(s_sready), pready = smem_addr(s_pready),
+            qready = smem_addr(&s_qready), drain = smem_addr(&s_drain);
+  Piece w;
+  if (!find_piece<TC_THREADS, true>(a, TC_ROWS, min_chunk, target, sms, item, n_parts && blockIdx.x == 0 ? scratch_plan(a) : nullptr, w)) return;
+  if (tid == 0) {
+    for (u32 i = 0; i < S::STAGES; ++i) { bar_init(full + i * 8, 1); bar_init(empty + i * 8, 1); }
+    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(pready + i * 8, 4); }
+    bar_init(qready, 8); bar_init(drain, 1);
+    s_lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const u32 tmem = s_tmem;
+
+  const Seq q = w.q;
+  const u32 n_rows = q.n * a.group, r0 = w.tile * TC_ROWS, r1 = min(r0 + TC_ROWS, n_rows) - 1;
+  const u32 n_tiles = r1 - r0 >= TC_TILE ? 2 : 1;
+  u32 first, last, all_lo, all_hi;       // keys any row sees; keys every row sees
+  row_range(a, q, r0 / a.group, first, all_hi);
+  row_range(a, q, r1 / a.group, all_lo, last);
+  const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+  const u32 per = ((nb + w.pieces - 1) / w.pieces + TC_KB - 1) / TC_KB * TC_KB;       // whole stages
+  const u32 b0 = b_first + min(w.piece * per, nb), b1 = b_first + min((w.piece + 1) * per, nb);
+  const u32 n = (b1 - b0 + TC_KB - 1) / TC_KB;         // stages of keys
+  const u32 sq = (smem_addr(smem_raw) + 1023) & ~1023u, ring = sq + S::Q;
+  volatile u32 *const lost = &s_lost;
+
+  // registers: 168 for each of 384 threads at the launch; 224 for a thread that holds a row of S, 56 for the others
+  if (warp > 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  } else if (warp == 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // ---- loads: K0, V0, K1, V1, ...; blocks behind the piece's last one read as zeros (a slot behind both pools)
+    const u32 *row = a.b.table + w.seq * a.b.table_stride;
+    u32 slots = 0, it = 0;
+    bool ok = true;
+    for (u32 j = 0; j < n && ok; ++j) {
+      if (j % 4 == 0) {
+        const u32 b = b0 + j * TC_KB + lane;
+        slots = b < b1 ? row[b] : 0xFFFFFFFFu;
+        if (b < b1 && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+      }
+      const u32 slot = __shfl_sync(~0u, slots, (j % 4) * TC_KB + lane % TC_KB);
+      for (u32 kv = 0; kv < 2; ++kv, ++it) {
+        const u32 st = it % S::STAGES;
+        if (it >= S::STAGES && !tc_wait(empty + st * 8, (it / S::STAGES - 1) & 1, lost)) { ok = false; break; }
+        if (lane == 0) bar_expect(full + st * 8, S::STAGE);
+        __syncwarp();
+        if (lane < TC_KB) load_block(a, maps, ring + st * S::STAGE + lane * S::BLOCK, full + st * 8, slot, 2 * a.layer + kv, h, D / 64);
+        __syncwarp();
+      }
+    }
+    if (!ok)          // let the copies in flight land, for a while, before the CTA ends
+      for (u32 i = it > S::STAGES ? it - S::STAGES : 0; i < it; ++i) bar_wait(full + (i % S::STAGES) * 8, (i / S::STAGES) & 1);
+  } else if (warp == 8) {
+    // ---- matrix products
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const u32 id_s = tc_idesc(FP16, TC_KEYS, false), id_o = tc_idesc(FP16, D, true);
+    const bool leader = elect_one();
+    auto stage = [&](u32 it) { return ring + (it % S::STAGES) * S::STAGE; };
+    auto landed = [&](u32 it) { return tc_wait(full + (it % S::STAGES) * 8, (it / S::STAGES) & 1, lost); };
+    auto product_s = [&](u32 i, u32 it) {
+      const u32 qa = sq + i * (TC_TILE * D * 2), kb = stage(it);
+#pragma unroll
+      for (u32 k = 0; k < D / 16; ++k)
+        tc_mma_ss(tmem + i * 128, tc_desc(qa + (k / 4) * (TC_TILE * 128) + (k % 4) * 32, 16, 1024),
+                  tc_desc(kb + (k / 4) * 1024 + (k % 4) * 32, 16, D * 16), id_s, k > 0);
+    };
+    auto product_o = [&](u32 i, u32 it, bool acc) {
+      const u32 vb = stage(it);
+#pragma unroll
+      for (u32 k = 0; k < TC_KEYS / 16; ++k)
+        tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, tc_desc(vb + k * (D * 32), 1024, D * 16), id_o, acc || k > 0);
+    };
+    bool ok = n == 0 || (tc_wait(qready, 0, lost) && landed(0));
+    if (ok && n) {
+      tc_after();
+      if (leader) {
+        for (u32 i = 0; i < n_tiles; ++i) { product_s(i, 0); tc_commit(sready + i * 8); }
+        tc_commit(empty);
+      }
+      __syncwarp();
+    }
+    for (u32 j = 0; ok && j < n; ++j) {
+      const u32 iv = 2 * j + 1, ik = 2 * j + 2;
+      if (!(ok = landed(iv))) break;
+      if (j + 1 == n && b1 * BT > q.kv) {     // tokens behind the length in the last block: whatever their values hold,
+        const u32 r = lane / 2;               // weight 0 must not meet an Inf or a NaN
+        if ((b1 - 1) * BT + r >= q.kv)
+          for (u32 c = 0; c < D / 16; ++c)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
+                         ::"r"(stage(iv) + ((b1 - 1 - b0) % TC_KB) * S::BLOCK + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+      for (u32 i = 0; i < n_tiles; ++i) {
+        if (!(ok = tc_wait(pready + i * 8, j & 1, lost))) break;
+        tc_after();
+        if (leader) product_o(i, iv, j > 0);
+        __syncwarp();
+        if (j + 1 < n) {
+          if (i == 0 && !(ok = landed(ik))) break;
+          if (leader) product_s(i, ik);
+        }
+        if (leader) tc_commit(sready + i * 8);     // S of the next keys, or the finished sums
+        __syncwarp();
+      }
+      if (ok && leader && j + 1 < n) {       // nobody waits for the last stages
+        tc_commit(empty + (iv % S::STAGES) * 8);
+        tc_commit(empty + (ik % S::STAGES) * 8);
+      }
+      __syncwarp();
+    }
+    if (!ok) {
+      if (leader) tc_commit(drain);
+      __syncwarp();
+      bar_wait(drain, 0);
+    }
+  } else {
+    // ---- one thread per row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    const u32 i = warp / 4, rt = tid % TC_TILE, r = r0 + i * TC_TILE + rt;
+    const bool mine = r <= r1;
+    const u32 rr = min(r, r1), t = q.t0 + rr / a.group, hq = h * a.group + rr % a.group;   // rows behind the last one repeat it
+    u32 lo, hi;
+    row_range(a, q, rr / a.group, lo, hi);
+    if (i < n_tiles && n) {
+      const u16 *src = (const u16 *)a.q + (u64)t * a.q_ts + (u64)hq * a.q_hs;
+      const bool wide = ((uintptr_t)src & 15) == 0;
+#pragma unroll
+      for (u32 c = 0; c < D / 8; ++c) {
+        uint4 v;
+        if (wide) v = *(const uint4 *)(src + c * 8);
+        else {
+          u32 x[4];
+#pragma unroll
+          for (u32 y = 0; y < 4; ++y) x[y] = (u32)src[c * 8 + 2 * y] | (u32)src[c * 8 + 2 * y + 1] << 16;
+          v = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        const u32 dst = sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + rt * 128 + (((c % 8) ^ (rt % 8)) * 16);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) bar_arrive(qready);
+    if (i < n_tiles) {
+      const u32 lanes = (warp % 4) << 21, ts = tmem + lanes + i * 128, to = tmem + lanes + 256 + i * D;
+      float m = -INFINITY, l = 0.0f;
+      bool ok = true;
+      for (u32 j = 0; j < n; ++j) {
+        if (!(ok = tc_wait(sready + i * 8, j & 1, lost))) break;
+        tc_after();
+        u32 x[128];
+#pragma unroll
+        for (u32 c = 0; c < 4; ++c) tc_ld32(x + 32 * c, ts + 32 * c);
+        tc_wait_ld();
+        float *const s = reinterpret_cast<float *>(x);
+        const u32 key0 = (b0 + j * TC_KB) * BT;
+        if (key0 < all_lo || key0 + TC_KEYS > all_hi) {
+          const int from = (int)lo - (int)key0, to_ = (int)hi - (int)key0;
+#pragma unroll
+          for (int c = 0; c < 128; ++c) if (c < from || c >= to_) s[c] = -INFINITY;
+        }
+        float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (u32 c = 4; c < 128; c += 4)
+#pragma unroll
+          for (u32 y = 0; y < 4; ++y) top[y] = fmaxf(top[y], s[c + y]);
+        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+        // The sums stay relative to an old maximum until a score passes it by 2^8 (as in the kernel for few rows)
+        if (__any_sync(~0u, now > m + 8.0f)) {
+          const float next = fmaxf(m, now), f = next == -INFINITY ? 1.0f : ex2(m - next);
+          m = next; l *= f;
+          if (j > 0) {                   // the product before S of these keys has been waited for: O is at rest
+#pragma unroll
+            for (u32 c = 0; c < D / 16; ++c) {
+              u32 y[16];
+              tc_ld16(y, to + 16 * c);
+              tc_wait_ld();
+#pragma unroll
+              for (u32 z = 0; z < 16; ++z) y[z] = __float_as_uint(__uint_as_float(y[z]) * f);
+              tc_st16(to + 16 * c, y);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float sum[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (u32 b = 0; b < 4; ++b) {
+          u32 p[16];
+#pragma unroll
+          for (u32 c = 0; c < 16; ++c) {
+            const float p0 = ex2(fmaf(s[32 * b + 2 * c], a.scale_log2, -ref)), p1 = ex2(fmaf(s[32 * b + 2 * c + 1], a.scale_log2, -ref));
+            sum[c % 4] += p0 + p1;
+            p[c] = Elem<T>::down(p0, p1);
+          }
+          tc_st16(ts + 16 * b, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tc_wait_st();
+        tc_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(pready + i * 8);
+      }
+      // ---- results
+      if (ok && n) { ok = tc_wait(sready + i * 8, n & 1, lost); tc_after(); }
+      const u64 part = (u64)w.part * H + h;
+      const bool direct = w.pieces == 1;
+      if (!direct && part >= n_parts) { if (tid % TC_TILE == 0) kv_err(a.err, KVERR_RANGE); ok = false; }
+      if (ok) {
+        const float inv = !direct ? 1.0f : l > 0.0f ? 1.0f / l : l;
+        u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
+        const bool wide = ((uintptr_t)out & 15) == 0;
+        const u32 prow = i * TC_TILE + rt;
+        float *const sums = scratch_sums(a) + (part * TC_ROWS + prow) * D;
+#pragma unroll
+        for (u32 c = 0; c < D / 32; ++c) {
+          u32 y[32];
+          __syncwarp();
+          if (n) { tc_ld32(y, to + 32 * c); tc_wait_ld(); }
+          else {
+#pragma unroll
+            for (u32 z = 0; z < 32; ++z) y[z] = 0;
+          }
+          if (!mine) {
+          } else if (!direct) {
+#pragma unroll
+            for (u32 z = 0; z < 32; z += 4) *(uint4 *)(sums + 32 * c + z) = make_uint4(y[z], y[z + 1], y[z + 2], y[z + 3]);
+          } else {
+            u32 v[16];
+#pragma unroll
+            for (u32 z = 0; z < 16; ++z) v[z] = Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv);
+            if (wide) {
+#pragma unroll
+              for (u32 z = 0; z < 16; z += 4) *(uint4 *)(out + 32 * c + 2 * z) = make_uint4(v[z], v[z + 1], v[z + 2], v[z + 3]);
+            } else {
+#pragma unroll
+              for (u32 z = 0; z < 16; ++z) { out[32 * c + 2 * z] = (u16)v[z]; out[32 * c + 2 * z + 1] = (u16)(v[z] >> 16); }
+            }
+          }
+        }
+        if (mine) {
+          if (!direct) ((float2 *)(scratch_sums(a) + n_parts * TC_ROWS * D))[part * TC_ROWS + prow] = make_float2(m, l);
+          else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
+        }
+      }
+    }
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (tid == 0 && s_lost) kv_err(a.err, KVERR_WAIT);
+}
+
+// ------------------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------------------
 bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 n_chunks, u64 n_kv_heads, u64 head_dim) {
@@ -699,7 +1091,7 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 
 }
 
 // Partial results a launch can leave, times KV heads.
-static u64 plan_parts(const AttendArgs &a, const AttendPlan &p) { return 2ull * p.target + 2 * a.p.n_kv_heads; }
+static u64 plan_parts(const AttendArgs &a, const AttendPlan &p) { return (p.kind == 2 ? 1ull : 2ull) * p.target + 2 * a.p.n_kv_heads; }
 
 template <class T, u32 D>
 static cudaError_t launch_join(const AttendArgs &a, const AttendPlan &p, u64 parts, cudaStream_t s, u32 *launches) {
@@ -720,6 +1112,18 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
   if (a.p.head_dim != 64 && a.p.head_dim != 128) {
     p.rows = ANY_ROWS;
     p.grid = (u32)std::min<u64>(tiles(p.rows), 0x7FFFFFFFu);
+    return p;
+  }
+  p.sms = sm_count;
+  // Rows of a sequence and KV head: up to two tiles of the kernel for few rows cost less than one of the other, whose tile is
+  // 128 rows high at least.
+  if ((u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group > 2 * SPLIT_ROWS) {
+    p.kind = 2;
+    p.rows = TC_ROWS; p.min_chunk = 64; p.target = 4 * sm_count;
+    const bool cut = a.b.max_blocks > p.min_chunk;
+    if (!cut) p.target = 0;
+    p.grid = (u32)std::min<u64>(tiles(p.rows) * H + p.target, 0x7FFFFFFFu);
+    if (cut) p.scratch_bytes = ((a.b.n_seqs * 8ull + 255) & ~255ull) + plan_parts(a, p) * p.rows * (a.p.head_dim + 2) * 4;
     return p;
   }
   p.kind = 1;
@@ -743,7 +1147,22 @@ static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const 
   return launch_join<T, D>(a, p, parts, s, launches);
 }
 
+template <class T, u32 D>
+static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
+  cudaError_t r = cudaFuncSetAttribute(k_attend_tc<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<D>::SMEM);
+  if (r != cudaSuccess) return r;
+  const u64 parts = p.scratch_bytes ? plan_parts(a, p) : 0;
+  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.min_chunk, p.target, p.sms, parts);
+  ++*launches;
+  if ((r = cudaGetLastError()) != cudaSuccess || !parts) return r;
+  return launch_join<T, D>(a, p, parts, s, launches);
+}
+
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
+  if (p.kind == 2) {
+    if (a.p.head_dim == 64) return a.fp16 ? launch_tc<__half, 64>(a, p, m, s, launches) : launch_tc<__nv_bfloat16, 64>(a, p, m, s, launches);
+    return a.fp16 ? launch_tc<__half, 128>(a, p, m, s, launches) : launch_tc<__nv_bfloat16, 128>(a, p, m, s, launches);
+  }
   if (p.kind == 1) {
     if (a.p.head_dim == 64) return a.fp16 ? launch_split<__half, 64>(a, p, m, s, launches) : launch_split<__nv_bfloat16, 64>(a, p, m, s, launches);
     return a.fp16 ? launch_split<__half, 128>(a, p, m, s, launches) : launch_split<__nv_bfloat16, 128>(a, p, m, s, launches);

@@ -325,162 +325,195 @@ __device__ __forceinline__ void load_block(const AttendArgs &a, const KvMaps &m,
                ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(h * halves), "r"(c3), "r"(c4), "r"(bar) : "memory");
 }
 
-// Pieces of work. The keys of a tile are cut into pieces when there are too few tiles to fill the GPU; every CTA works
-// the cut out for itself from the device-side lengths, so a captured launch follows them. A tile's blocks of keys are
-// bounded per sequence (whole sequence, or window plus the tokens of a tile).
-struct Piece { Seq q; u32 seq, tile, piece, pieces, part; };   // part: index of the piece's partial result, if pieces > 1
+// Which CTA does what is worked out by every CTA for itself from the device-side lengths, so a captured launch follows
+// them. `unit`: one tile of rows of one sequence and KV head, against all its keys. Its number of blocks is bounded per
+// sequence (whole sequence, or window plus the tokens of a tile).
 __device__ __forceinline__ u32 seq_blocks(const AttendArgs &a, const Seq &q, u32 rows) {
   u32 span = q.kv;
   if (a.window) { const u64 w = (u64)a.window + min(q.n, rows / a.group + 2) + 2 * BT; span = (u32)min((u64)span, w); }
-  return (span + BT - 1) / BT;
+  return max(1u, (span + BT - 1) / BT);
 }
+__device__ __forceinline__ u32 seq_tiles(const AttendArgs &a, const Seq &q, u32 rows) { return (u32)(((u64)q.n * a.group + rows - 1) / rows); }
+
+// Exclusive prefix sum over the CTA's threads; `all`: the total. Ends without a barrier: s_sum is free after the next one.
 template <u32 THREADS>
-__device__ __forceinline__ u32 block_scan(u32 n, u32 *s_sum, u32 &all) {     // exclusive
+__device__ __forceinline__ u64 block_scan(u64 n, u64 *s_sum, u64 &all) {
   const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  u32 incl = n;
+  u64 incl = n;
 #pragma unroll
-  for (u32 o = 1; o < 32; o *= 2) { const u32 y = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += y; }
+  for (u32 o = 1; o < 32; o *= 2) { const u64 y = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += y; }
   __syncthreads();
   if (lane == 31) s_sum[warp] = incl;
   __syncthreads();
-  u32 before = 0; all = 0;
+  u64 before = 0; all = 0;
 #pragma unroll
   for (u32 w = 0; w < THREADS / 32; ++w) { if (w < warp) before += s_sum[w]; all += s_sum[w]; }
   return before + incl - n;
 }
-// plan_out[s] = {first partial, pieces} of every sequence, written by the CTA that is told to.
-// Length of a piece in blocks. Work over target, or (WAVES) whatever makes the waves of one CTA per SM end soonest: of
-// the longest sequence cut into 1 .. MAX_CUTS pieces (and the others into pieces no longer), the one with the smallest
-// waves * (piece + what a piece costs besides), among those that leave at most `target` partial results per launch.
-constexpr u32 MAX_CUTS = 32, PIECE_COST = 32;
-template <u32 THREADS, bool WAVES>
-__device__ bool find_piece(const AttendArgs &a, u32 rows, u32 min_chunk, u32 target, u32 sms, u32 want, uint2 *plan_out, Piece &out) {
-  __shared__ u32 s_sum[THREADS / 32], s_seq, s_item, s_pieces, s_part, s_longest, s_items[MAX_CUTS], s_parts[MAX_CUTS], s_chunk;
-  __shared__ unsigned long long s_work;
-  if (threadIdx.x == 0) { s_seq = 0xFFFFFFFFu; s_work = 0; s_longest = 0; }
-  if (WAVES && threadIdx.x < MAX_CUTS) s_items[threadIdx.x] = s_parts[threadIdx.x] = 0;
-  __syncthreads();
-  auto tiles_of = [&](const Seq &x) { return (u32)(((u64)x.n * a.group + rows - 1) / rows); };
-  u64 mine = 0;
-  Seq first{0, 0, 0};
-  for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
-    const Seq x = load_seq(a.b, s, a.err);
-    if (s == threadIdx.x) first = x;
-    mine += WAVES ? (x.n ? seq_blocks(a, x, rows) : 0) : (u64)tiles_of(x) * seq_blocks(a, x, rows);
-    if (WAVES) { atomicMax(&s_longest, (u32)mine); mine = 0; }
+
+// Partial results in scratch: a header, a plan record per sequence, `rows` rows of head_dim sums per partial result, then the
+// (maximum, sum) pairs of all of them.
+//   kind 1 (few rows): header {work per CTA, -}, record {first unit's place in the work (64 bits), blocks of a unit, -}
+//   kind 2:            header {any sequence cut, -}, record {first partial, pieces, tiles, -}
+__device__ __forceinline__ uint4 *scratch_plan(const AttendArgs &a) { return (uint4 *)a.scratch; }
+__host__ __device__ __forceinline__ u64 plan_bytes(u32 n_seqs) { return (16ull * (n_seqs + 1) + 255) & ~255ull; }
+__device__ __forceinline__ float *scratch_sums(const AttendArgs &a) { return (float *)(a.scratch + plan_bytes(a.b.n_seqs)); }
+
+// Kind 1: the blocks of all units, one after the other, are dealt out in equal stretches, one per CTA, so that every CTA
+// reads as much as any other whatever the lengths are; a unit that crosses a border is joined from its parts. A stretch is
+// `per` blocks, at least MIN_STRETCH. Order of units: sequence, tile, KV head.
+constexpr u32 MIN_STRETCH = 16;
+template <u32 THREADS>
+__device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publish, u64 &x, u64 &x_end, u32 &per, u32 &seq, u64 &base) {
+  __shared__ u64 s_sum[THREADS / 32], s_base;
+  __shared__ u32 s_seq;
+  auto units = [&](u32 s) -> u64 {
+    if (s >= a.b.n_seqs) return 0;
+    const Seq q = load_seq(a.b, s, a.err);
+    return (u64)seq_tiles(a, q, rows) * a.p.n_kv_heads * seq_blocks(a, q, rows);
+  };
+  u64 total = 0, all, mine = 0, at = 0;
+  for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
+    mine = units(s0 + threadIdx.x);
+    at = block_scan<THREADS>(mine, s_sum, all);
+    total += all;
   }
-  if (!WAVES && mine) atomicAdd(&s_work, (unsigned long long)mine);
-  __syncthreads();
-  if (WAVES) {
-    const u32 longest = s_longest;
-    auto chunk_of = [&](u32 k) { return max(min_chunk, ((longest + k) / (k + 1) + 7) / 8 * 8); };     // whole tiles of 8 blocks
-    if (longest > min_chunk && target)
-      for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
-        const Seq x = s == threadIdx.x ? first : load_seq(a.b, s, a.err);
-        const u32 tiles = tiles_of(x), nb = seq_blocks(a, x, rows);
-        for (u32 k = 0; k < MAX_CUTS && tiles; ++k) {
-          const u32 c = chunk_of(k), n = max(1u, (nb + c - 1) / c);
-          atomicAdd(&s_items[k], tiles * n);
-          if (n > 1) atomicAdd(&s_parts[k], tiles * n);
-        }
-      }
-    __syncthreads();
-    if (threadIdx.x < 32) {
-      const u32 k = threadIdx.x, c = chunk_of(k);
-      u64 cost = (u64)((s_items[k] * a.p.n_kv_heads + sms - 1) / sms) * (c + PIECE_COST);
-      if (longest <= min_chunk || !target ? k > 0 : s_parts[k] * a.p.n_kv_heads > target && k > 0) cost = ~0ull >> 8;
-      cost = cost << 8 | k;
-#pragma unroll
-      for (u32 o = 16; o; o /= 2) { const u64 y = __shfl_xor_sync(~0u, cost, o); cost = y < cost ? y : cost; }
-      if (k == 0) s_chunk = (cost & 255) ? chunk_of((u32)(cost & 255)) : max(longest, 1u);
-    }
-    __syncthreads();
-  }
-  const u32 chunk = WAVES ? s_chunk : max(min_chunk, (u32)((s_work * a.p.n_kv_heads + target - 1) / target));
-  u32 item0 = 0, part0 = 0;
+  const u64 n = max(1ull, min((unsigned long long)ctas, (unsigned long long)(total / MIN_STRETCH)));
+  per = (u32)((total + n - 1) / n);
+  x = (u64)blockIdx.x * per;
+  x_end = min((unsigned long long)total, (unsigned long long)(x + per));
+  const bool any = x < total;
+  if (publish && threadIdx.x == 0) scratch_plan(a)[0] = make_uint4(per, 0, 0, 0);
+  u64 base0 = 0;
   for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
     const u32 s = s0 + threadIdx.x;
-    u32 items = 0, parts = 0, pieces = 1;
-    if (s < a.b.n_seqs) {
-      const Seq x = s0 ? load_seq(a.b, s, a.err) : first;
-      pieces = max(1u, (seq_blocks(a, x, rows) + chunk - 1) / chunk);
-      items = tiles_of(x) * pieces;
-      parts = pieces > 1 ? items : 0;
-    }
-    u32 all_items, all_parts;
-    const u32 at = item0 + block_scan<THREADS>(items, s_sum, all_items), pat = part0 + block_scan<THREADS>(parts, s_sum, all_parts);
-    if (want >= at && want < at + items) { s_seq = s; s_item = want - at; s_pieces = pieces; s_part = pat; }
-    if (plan_out && s < a.b.n_seqs) plan_out[s] = make_uint2(pat, pieces);
-    item0 += all_items; part0 += all_parts;
-    if (!plan_out && want < item0) break;
+    if (a.b.n_seqs > THREADS) { mine = units(s); at = block_scan<THREADS>(mine, s_sum, all); }
+    at += base0;
+    if (mine && x >= at && x < at + mine) { s_seq = s; s_base = at; }
+    if (publish && s < a.b.n_seqs)
+      scratch_plan(a)[1 + s] = make_uint4((u32)at, (u32)(at >> 32), seq_blocks(a, load_seq(a.b, s, a.err), rows), 0);
+    base0 += all;
+    if (!publish && (!any || x < base0)) break;
   }
+  if (!any) return false;
   __syncthreads();
-  if (s_seq == 0xFFFFFFFFu) return false;
-  out.q = load_seq(a.b, s_seq, a.err);
-  out.seq = s_seq; out.pieces = s_pieces; out.piece = s_item % s_pieces;
-  out.tile = tiles_of(out.q) - 1 - s_item / s_pieces;     // last tokens first: with a causal mask they have the most keys
-  out.part = s_part + out.tile * s_pieces + out.piece;
+  seq = s_seq; base = s_base;
   return true;
 }
 
-// Partial results: per piece and KV head `rows` rows of head_dim sums, then (maximum, sum) pairs of all pieces.
-__device__ __forceinline__ uint2 *scratch_plan(const AttendArgs &a) { return (uint2 *)a.scratch; }
-__device__ __forceinline__ float *scratch_sums(const AttendArgs &a) { return (float *)(a.scratch + ((a.b.n_seqs * 8ull + 255) & ~255ull)); }
-
-// Joins the pieces of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. One warp per row (token, head); rows of
-// sequences that were not cut are already written. Launched behind the piece kernel and waits for all of it.
-template <class T, u32 D>
-__global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u64 n_parts) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+// Kind 2: tiles are cut into pieces of equal length, as many as make the rounds of one piece per SM end soonest: of the
+// longest sequence cut into 1 .. MAX_CUTS pieces (and the others into pieces no longer), the one with the smallest
+// rounds * (piece + what a piece costs besides), among those that leave at most `most` partial results. Returns the length
+// of a piece in blocks.
+constexpr u32 MAX_CUTS = 32, PIECE_COST = 24, MIN_PIECE = 64;
+template <u32 THREADS>
+__device__ u32 choose_piece(const AttendArgs &a, u32 rows, u32 most, u32 sms) {
+  __shared__ u32 s_longest, s_items[MAX_CUTS], s_parts[MAX_CUTS], s_piece;
   const u32 lane = threadIdx.x & 31;
-  const u64 id = (u64)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id % a.n_q_heads);
-  if (t >= a.b.n_tokens) return;
-  u32 seq = 0;                           // starts are cut like load_seq cuts them; the first sequence the token lies in
-  bool found = false;
-  for (u32 s0 = 0; s0 < a.b.n_seqs && !found; s0 += 32) {
-    const u32 s = s0 + lane;
-    const u32 hit = __ballot_sync(~0u, s < a.b.n_seqs && a.b.q_start[s] <= t && t < a.b.q_start[s + 1]);
-    if (hit) { seq = s0 + __ffs(hit) - 1; found = true; }
+  if (threadIdx.x == 0) s_longest = 1;
+  if (threadIdx.x < MAX_CUTS) s_items[threadIdx.x] = s_parts[threadIdx.x] = 0;
+  __syncthreads();
+  u32 mine = 0;
+  for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
+    const Seq q = load_seq(a.b, s, a.err);
+    if (q.n) mine = max(mine, seq_blocks(a, q, rows));
   }
-  if (!found) return;
-  const uint2 plan = scratch_plan(a)[seq];
-  if (plan.y <= 1) return;
-  const u32 h = hq / a.group, r = (t - a.b.q_start[seq]) * a.group + hq % a.group, tile = r / rows, row = r % rows;
-  const u64 p0 = ((u64)plan.x + (u64)tile * plan.y) * a.p.n_kv_heads + h;
+  if (mine) atomicMax(&s_longest, mine);
+  __syncthreads();
+  const u32 longest = s_longest;
+  if (longest <= MIN_PIECE || !most) return longest;
+  const u32 piece = max(MIN_PIECE, ((longest + lane) / (lane + 1) + 7) / 8 * 8);     // lane: one candidate each; whole stages
+  u32 items = 0, parts = 0;
+  for (u32 s = threadIdx.x / 32; s < a.b.n_seqs; s += THREADS / 32) {
+    const Seq q = load_seq(a.b, s, a.err);
+    const u32 tiles = seq_tiles(a, q, rows), n = (seq_blocks(a, q, rows) + piece - 1) / piece;
+    items += tiles * n;
+    if (n > 1) parts += tiles * n;
+  }
+  if (items) { atomicAdd(&s_items[lane], items); atomicAdd(&s_parts[lane], parts); }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    u64 cost = ((u64)s_items[lane] * a.p.n_kv_heads + sms - 1) / sms * (piece + PIECE_COST);
+    if ((u64)s_parts[lane] * a.p.n_kv_heads > most && lane) cost = ~0ull >> 8;
+    cost = cost << 8 | lane;
+#pragma unroll
+    for (u32 o = 16; o; o /= 2) { const u64 y = __shfl_xor_sync(~0u, cost, o); cost = y < cost ? y : cost; }
+    const u32 best = __shfl_sync(~0u, piece, (u32)(cost & 31));
+    if (lane == 0) s_piece = (cost & 31) ? best : longest;
+  }
+  __syncthreads();
+  return s_piece;
+}
+
+// Joins the parts of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. One warp per row (token, head) at a time;
+// rows of units that were not cut are already written. Launched behind the kernel that leaves the parts, waits for all of it.
+template <class T, u32 D, u32 KIND>
+__global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u32 n_parts) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const u32 lane = threadIdx.x & 31, H = a.p.n_kv_heads;
+  const u32 head = scratch_plan(a)[0].x;
+  if (KIND == 2 && !head) return;
   const float *sums = scratch_sums(a);
-  const float2 *ml = (const float2 *)(sums + n_parts * rows * D);
-  if (p0 + (u64)(plan.y - 1) * a.p.n_kv_heads >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); return; }
-  float m = -INFINITY;
-  for (u32 i = lane; i < plan.y; i += 32) m = fmaxf(m, ml[(p0 + (u64)i * a.p.n_kv_heads) * rows + row].x);
+  const float2 *ml = (const float2 *)(sums + (u64)n_parts * rows * D);
+  const u64 n_rows = (u64)a.b.n_tokens * a.n_q_heads, step = (u64)gridDim.x * 4;
+  for (u64 id = (u64)blockIdx.x * 4 + (threadIdx.x >> 5); id < n_rows; id += step) {
+    const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id % a.n_q_heads);
+    u32 seq = 0;                         // the first sequence the token lies in
+    bool found = false;
+    for (u32 s0 = 0; s0 < a.b.n_seqs && !found; s0 += 32) {
+      const u32 s = s0 + lane;
+      const u32 hit = __ballot_sync(~0u, s < a.b.n_seqs && a.b.q_start[s] <= t && t < a.b.q_start[s + 1]);
+      if (hit) { seq = s0 + __ffs(hit) - 1; found = true; }
+    }
+    if (!found) continue;
+    const uint4 plan = scratch_plan(a)[1 + seq];
+    const u32 h = hq / a.group, r = (t - a.b.q_start[seq]) * a.group + hq % a.group, tile = r / rows, row = r % rows;
+    u64 c0 = 0, c1 = 0, p0, stride, n;     // partial i: p0 + i * stride, but for kind 1 the first may lie elsewhere
+    u64 odd = 0;
+    if (KIND == 1) {
+      const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z, e = s + plan.z;
+      c0 = s / head; c1 = (e - 1) / head;
+      p0 = 2 * c0; stride = 2; n = c1 - c0 + 1;
+      odd = s > c0 * head;
+    } else {
+      p0 = ((u64)plan.x + tile) * H + h; stride = (u64)plan.z * H; n = plan.y;
+    }
+    if (n <= 1) continue;
+    if (p0 + (n - 1) * stride >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
+    auto place = [&](u64 i) { return (p0 + i * stride + (i == 0 ? odd : 0)) * rows + row; };
+    float m = -INFINITY;
+    for (u64 i = lane; i < n; i += 32) m = fmaxf(m, ml[place(i)].x);
 #pragma unroll
-  for (u32 o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-  const float ref = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, acc[D / 32];
+    for (u32 o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, acc[D / 32];
 #pragma unroll
-  for (u32 c = 0; c < D / 32; ++c) acc[c] = 0.0f;
-  for (u32 i = 0; i < plan.y; ++i) {
-    const u64 at = (p0 + (u64)i * a.p.n_kv_heads) * rows + row;
-    const float2 x = ml[at];
-    if (x.x == -INFINITY) continue;      // a piece without keys for this row has no sums
-    const float w = exp2f(x.x - ref);
-    l += w * x.y;
-    const float *o = sums + at * D + lane * (D / 32);
+    for (u32 c = 0; c < D / 32; ++c) acc[c] = 0.0f;
+#pragma unroll 4
+    for (u64 i = 0; i < n; ++i) {
+      const u64 at = place(i);
+      const float2 x = ml[at];
+      const float w = x.x == -INFINITY ? 0.0f : exp2f(x.x - ref);      // a part without keys for this row holds zeros
+      l += w * x.y;
+      const float *o = sums + at * D + lane * (D / 32);
+      float v[D / 32];
+      if (D == 128) *(float4 *)v = *(const float4 *)o; else *(float2 *)v = *(const float2 *)o;
 #pragma unroll
-    for (u32 c = 0; c < D / 32; ++c) acc[c] += w * o[c];
+      for (u32 c = 0; c < D / 32; ++c) acc[c] += w * v[c];
+    }
+    const float inv = l > 0.0f ? 1.0f / l : l;
+    T *o = (T *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + lane * (D / 32);
+#pragma unroll
+    for (u32 c = 0; c < D / 32; ++c) o[c] = Elem<T>::down1(acc[c] * inv);
+    if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
   }
-  const float inv = l > 0.0f ? 1.0f / l : l;
-  T *o = (T *)a.out + t * a.o_ts + hq * a.o_hs + lane * (D / 32);
-#pragma unroll
-  for (u32 c = 0; c < D / 32; ++c) o[c] = Elem<T>::down1(acc[c] * inv);
-  if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
 }
 
 // ------------------------------------------------------------------------------------------------------
 // Few rows (one new token per sequence, small chunks): bound by reading K and V once. A CTA of four warps takes a piece of
 // the keys for up to 16 rows of one KV head, the height of a warp-level matrix instruction. Every warp has its own ring
 // of TMA loads (a block's K and V per stage) and its own running maximum and sums over every fourth block, so warps
-// never wait for one another until the end. Two CTAs per SM keep up to 192 KB of loads in flight.
+// never wait for one another until the end of a unit. Two CTAs per SM keep up to 192 KB of loads in flight.
 // ------------------------------------------------------------------------------------------------------
 constexpr u32 SPLIT_ROWS = 16, SPLIT_WARPS = 4, SPLIT_THREADS = SPLIT_WARPS * 32;
 template <u32 D> struct SplitShape {
@@ -510,200 +543,220 @@ template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(SPLIT_THREADS, 2)
-k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 min_chunk, u32 target, u64 n_parts) {
+k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts) {
   typedef SplitShape<D> S;
   extern __shared__ u8 smem_raw[];
   __shared__ __align__(8) u64 bars[SPLIT_WARPS * S::STAGES];
   __shared__ float s_ml[SPLIT_WARPS][SPLIT_ROWS][2];
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
-  const u32 h = blockIdx.x % H, item = blockIdx.x / H;
   const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8;
   if (lane == 0) {
     for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  Piece w;
-  if (!find_piece<SPLIT_THREADS, false>(a, SPLIT_ROWS, min_chunk, target, 0, item, n_parts && blockIdx.x == 0 ? scratch_plan(a) : nullptr, w)) return;
-  const Seq q = w.q;
-  const u32 n_rows = q.n * a.group, r0 = w.tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
-  u32 first, last, all_lo, all_hi;       // keys any row sees; keys every row sees
-  row_range(a, q, r0 / a.group, first, all_hi);
-  row_range(a, q, r1 / a.group, all_lo, last);
-  // blocks of this piece
-  const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
-  const u32 per = (nb + w.pieces - 1) / w.pieces;
-  const u32 b0 = b_first + min(w.piece * per, nb), b1 = b_first + min((w.piece + 1) * per, nb);
-  const u32 ring = ((smem_addr(smem_raw) + 1023) & ~1023u) + warp * S::RING;
-  const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
-  const u32 *row = a.b.table + w.seq * a.b.table_stride;
-  u32 slots = 0;                         // lane i: the slot of this warp's block number (i mod 32) of the current 32
-  auto fetch_slots = [&](u32 i0) { const u32 i = i0 + lane; slots = i < n_mine ? row[b0 + warp + i * SPLIT_WARPS] : 0; };
-  auto load = [&](u32 i) {               // i-th block of this warp; whole warp
-    if (i % 32 == 0) {
-      fetch_slots(i);
-      if (i + lane < n_mine && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
-    }
-    const u32 slot = __shfl_sync(~0u, slots, i % 32);
-    if (lane == 0) {
-      const u32 st = i % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
-      bar_expect(bar, 2 * S::BLOCK);
-      load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
-      load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
-    }
-  };
-  const u32 n_pro = min(n_mine, S::STAGES);
-  for (u32 i = 0; i < n_pro; ++i) load(i);
+  u64 x, x_end, base;
+  u32 per, seq;
+  if (!find_stretch<SPLIT_THREADS>(a, SPLIT_ROWS, gridDim.x, n_parts && blockIdx.x == 0, x, x_end, per, seq, base)) return;
+  const u64 x_begin = x;
+  const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
+  Seq q = load_seq(a.b, seq, a.err);
+  u32 tiles = seq_tiles(a, q, SPLIT_ROWS), unit = seq_blocks(a, q, SPLIT_ROWS);
+  u32 it = 0;                            // stages this warp has used
+  bool ok = true;
 
-  // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
-  u32 qf[D / 16][4];
-  u32 lo[2], hi[2];
+  for (bool more = true; more;) {
+    // the unit x lies in, and the part of it in this stretch
+    while (x >= base + (u64)tiles * H * unit) {
+      base += (u64)tiles * H * unit;
+      if (++seq >= a.b.n_seqs) return;   // cannot happen: x < x_end <= all work
+      q = load_seq(a.b, seq, a.err);
+      tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS);
+    }
+    const u32 u = (u32)((x - base) / unit), tile = u / H, h = u % H;
+    const u64 u0 = base + (u64)u * unit, x1 = min((unsigned long long)x_end, (unsigned long long)(u0 + unit));
+    const bool direct = x == u0 && x1 == u0 + unit;
+    const u32 part = 2 * blockIdx.x + (x == u0 && x > x_begin);
+    const u32 n_rows = q.n * a.group, r0 = tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
+    u32 first, last, all_lo, all_hi;     // keys any row sees; keys every row sees
+    row_range(a, q, r0 / a.group, first, all_hi);
+    row_range(a, q, r1 / a.group, all_lo, last);
+    const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+    const u32 b0 = b_first + min((u32)(x - u0), nb), b1 = b_first + min((u32)(x1 - u0), nb);
+    const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
+    const u32 *row = a.b.table + seq * a.b.table_stride;
+    u32 slots = 0;                       // lane i: the slot of this warp's block number (i mod 32) of the current 32
+    auto load = [&](u32 i) {             // i-th block of this warp here; whole warp
+      if (i % 32 == 0) {
+        slots = i + lane < n_mine ? row[b0 + warp + (i + lane) * SPLIT_WARPS] : 0;
+        if (i + lane < n_mine && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+      }
+      const u32 slot = __shfl_sync(~0u, slots, i % 32);
+      if (lane == 0) {
+        const u32 st = (it + i) % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
+        bar_expect(bar, 2 * S::BLOCK);
+        load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
+        load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
+      }
+    };
+    const u32 n_pro = min(n_mine, S::STAGES);
+    for (u32 i = 0; i < n_pro; ++i) load(i);
+
+    // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
+    u32 qf[D / 16][4];
+    u32 lo[2], hi[2];
 #pragma unroll
-  for (u32 x = 0; x < 2; ++x) {
-    const u32 r = min(r0 + lane / 4 + 8 * x, r1);     // rows behind the last one repeat it and are not written
-    row_range(a, q, r / a.group, lo[x], hi[x]);
-    const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
-    const bool even = ((uintptr_t)src & 3) == 0;
+    for (u32 y = 0; y < 2; ++y) {
+      const u32 r = min(r0 + lane / 4 + 8 * y, r1);     // rows behind the last one repeat it and are not written
+      row_range(a, q, r / a.group, lo[y], hi[y]);
+      const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
+      const bool even = ((uintptr_t)src & 3) == 0;
 #pragma unroll
-    for (u32 k = 0; k < D / 16; ++k)
+      for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (u32 z = 0; z < 2; ++z) {
+          const u16 *p = src + k * 16 + z * 8;
+          qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+        }
+    }
+    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) o[n][y] = 0.0f;
+
+    for (u32 i = 0; ok && i < n_mine; ++i) {
+      const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
+      if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
+      const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
+      // scores of 16 keys: two column groups of 8
+      float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+      for (u32 k = 0; k < D / 16; ++k) {
+        u32 f[4];
+        ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
+        mma16816<T>(s[0], qf[k], f[0], f[1]);
+        mma16816<T>(s[1], qf[k], f[2], f[3]);
+      }
+      if (key0 + BT > q.kv) {            // the last block's tokens behind the length: whatever their values hold, weight 0
+        const u32 r = lane / 2;          // must not meet an Inf or a NaN
+        if (key0 + r >= q.kv)
+#pragma unroll
+          for (u32 c = 0; c < D / 16; ++c)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+        __syncwarp();
+      }
+      const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
+      float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) {
+          const u32 key = key0 + n * 8 + (lane % 4) * 2 + (y & 1);
+          float v = s[n][y] * a.scale_log2;
+          if (!whole && (key < lo[y >> 1] || key >= hi[y >> 1])) v = -INFINITY;
+          s[n][y] = v;
+          top[y >> 1] = fmaxf(top[y >> 1], v);
+        }
 #pragma unroll
       for (u32 y = 0; y < 2; ++y) {
-        const u16 *p = src + k * 16 + y * 8;
-        qf[k][x + 2 * y] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+        top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 1));
+        top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 2));
       }
-  }
-  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+      // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
+      // those below 1, and most blocks then need no rescaling.
+      if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
 #pragma unroll
-  for (u32 n = 0; n < D / 8; ++n)
+        for (u32 y = 0; y < 2; ++y) {
+          const float now = fmaxf(m[y], top[y]), f = now == -INFINITY ? 1.0f : ex2(m[y] - now);
+          m[y] = now; l[y] *= f;
 #pragma unroll
-    for (u32 x = 0; x < 4; ++x) o[n][x] = 0.0f;
+          for (u32 n = 0; n < D / 8; ++n) { o[n][2 * y] *= f; o[n][2 * y + 1] *= f; }
+        }
+      }
+      const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+#pragma unroll
+      for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
+      const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
+                        Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
+#pragma unroll
+      for (u32 n = 0; n < D / 16; ++n) {
+        u32 f[4];
+        ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
+        mma16816<T>(o[2 * n], p, f[0], f[1]);
+        mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+      }
+      __syncwarp();                      // the stage is read: refill it
+      if (i + S::STAGES < n_mine) load(i + S::STAGES);
+    }
+    it += n_mine;
 
-  bool ok = true;
-  for (u32 i = 0; i < n_mine; ++i) {
-    const u32 st = i % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
-    if (!__all_sync(~0u, bar_wait(bar0 + st * 8, (i / S::STAGES) & 1))) { ok = false; break; }
-    const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
-    // scores of 16 keys: two column groups of 8
-    float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    // join the four warps: sums through the (now idle) rings
 #pragma unroll
-    for (u32 k = 0; k < D / 16; ++k) {
-      u32 f[4];
-      ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
-      mma16816<T>(s[0], qf[k], f[0], f[1]);
-      mma16816<T>(s[1], qf[k], f[2], f[3]);
+    for (u32 y = 0; y < 2; ++y) {
+      l[y] += __shfl_xor_sync(~0u, l[y], 1);
+      l[y] += __shfl_xor_sync(~0u, l[y], 2);
+      if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * y][0] = m[y]; s_ml[warp][lane / 4 + 8 * y][1] = l[y]; }
     }
-    if (key0 + BT > q.kv) {              // the last block's tokens behind the length: whatever their values hold, weight 0
-      const u32 r = lane / 2;            // must not meet an Inf or a NaN
-      if (key0 + r >= q.kv)
+    constexpr u32 LD = D + 8;            // row pitch in floats: the four rows of a quarter warp fall on different banks
+    static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
+    float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
 #pragma unroll
-        for (u32 c = 0; c < D / 16; ++c)
-          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
-      __syncwarp();
-    }
-    const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
-    float top[2] = {-INFINITY, -INFINITY};
+    for (u32 n = 0; n < D / 8; ++n)
 #pragma unroll
-    for (u32 n = 0; n < 2; ++n)
+      for (u32 y = 0; y < 2; ++y)
+        *(float2 *)&so[(lane / 4 + 8 * y) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * y], o[n][2 * y + 1]);
+    if (__syncthreads_or(!ok)) { ok = false; break; }      // a wait ran out somewhere: nothing is written
+    const u32 r = tid / 8, c0 = (tid % 8) * 4;             // thread: row r, four columns out of every 32
+    if (r0 + r <= r1 && (direct || part < n_parts)) {
+      float mm = -INFINITY, ll = 0.0f, f[SPLIT_WARPS];
 #pragma unroll
-      for (u32 x = 0; x < 4; ++x) {
-        const u32 key = key0 + n * 8 + (lane % 4) * 2 + (x & 1);
-        float v = s[n][x] * a.scale_log2;
-        if (!whole && (key < lo[x >> 1] || key >= hi[x >> 1])) v = -INFINITY;
-        s[n][x] = v;
-        top[x >> 1] = fmaxf(top[x >> 1], v);
+      for (u32 y = 0; y < SPLIT_WARPS; ++y) mm = fmaxf(mm, s_ml[y][r][0]);
+      const float ref = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+      for (u32 y = 0; y < SPLIT_WARPS; ++y) { f[y] = ex2(s_ml[y][r][0] - ref); ll += f[y] * s_ml[y][r][1]; }
+      const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
+      const float *sum = (const float *)(smem_raw + (ring0 - smem_addr(smem_raw))) + r * LD;
+      const float inv = !direct ? 1.0f : ll > 0.0f ? 1.0f / ll : ll;
+      u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
+      float *const sums = scratch_sums(a) + ((u64)part * SPLIT_ROWS + r) * D;
+#pragma unroll
+      for (u32 c = c0; c < D; c += 32) {
+        float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (u32 y = 0; y < SPLIT_WARPS; ++y) {
+          const float4 z = *(const float4 *)(sum + y * (S::RING / 4) + c);
+          v.x += f[y] * z.x; v.y += f[y] * z.y; v.z += f[y] * z.z; v.w += f[y] * z.w;
+        }
+        if (direct) {
+          const u32 p0 = Elem<T>::down(v.x * inv, v.y * inv), p1 = Elem<T>::down(v.z * inv, v.w * inv);
+          u16 *d = out + c;
+          if (((uintptr_t)d & 7) == 0) *(uint2 *)d = make_uint2(p0, p1);
+          else { d[0] = (u16)p0; d[1] = (u16)(p0 >> 16); d[2] = (u16)p1; d[3] = (u16)(p1 >> 16); }
+        } else {
+          *(float4 *)(sums + c) = v;
+        }
       }
-#pragma unroll
-    for (u32 x = 0; x < 2; ++x) {
-      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
-      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
-    }
-    // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
-    // those below 1, and most blocks then need no rescaling.
-    if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
-#pragma unroll
-      for (u32 x = 0; x < 2; ++x) {
-        const float now = fmaxf(m[x], top[x]), f = now == -INFINITY ? 1.0f : ex2(m[x] - now);
-        m[x] = now; l[x] *= f;
-#pragma unroll
-        for (u32 n = 0; n < D / 8; ++n) { o[n][2 * x] *= f; o[n][2 * x + 1] *= f; }
+      if (tid % 8 == 0) {
+        if (!direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * SPLIT_ROWS * D))[part * SPLIT_ROWS + r] = make_float2(mm, ll);
+        else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (mm + log2f(ll)) * 0.69314718055994531f;
       }
+    } else if (r0 + r <= r1 && tid == 0) {
+      kv_err(a.err, KVERR_RANGE);        // cannot happen: two parts per CTA
     }
-    const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-#pragma unroll
-    for (u32 n = 0; n < 2; ++n)
-#pragma unroll
-      for (u32 x = 0; x < 4; ++x) { s[n][x] = ex2(s[n][x] - ref[x >> 1]); l[x >> 1] += s[n][x]; }
-    const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
-                      Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
-#pragma unroll
-    for (u32 n = 0; n < D / 16; ++n) {
-      u32 f[4];
-      ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
-      mma16816<T>(o[2 * n], p, f[0], f[1]);
-      mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+    x = x1;
+    more = x < x_end;
+    if (more) {                          // the rings are read: loads may write them again
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncthreads();
     }
-    __syncwarp();                        // the stage is read: refill it
-    if (i + S::STAGES < n_mine) load(i + S::STAGES);
   }
   if (!ok) {                             // let the copies in flight land, for a while, before the CTA ends
     if (lane == 0) kv_err(a.err, KVERR_WAIT);
     for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
-  }
-
-  // join the four warps: sums through the (now idle) rings. A ring whose wait ran out may still be written by a late copy:
-  // that only spoils a result already reported as lost.
-#pragma unroll
-  for (u32 x = 0; x < 2; ++x) {
-    l[x] += __shfl_xor_sync(~0u, l[x], 1);
-    l[x] += __shfl_xor_sync(~0u, l[x], 2);
-    if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * x][0] = m[x]; s_ml[warp][lane / 4 + 8 * x][1] = l[x]; }
-  }
-  constexpr u32 LD = D + 8;              // row pitch in floats: the four rows of a quarter warp fall on different banks
-  static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
-  float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
-#pragma unroll
-  for (u32 n = 0; n < D / 8; ++n)
-#pragma unroll
-    for (u32 x = 0; x < 2; ++x)
-      *(float2 *)&so[(lane / 4 + 8 * x) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * x], o[n][2 * x + 1]);
-  __syncthreads();
-  const u32 r = tid / 8, c0 = (tid % 8) * 4;       // thread: row r, four columns out of every 32
-  float mm = -INFINITY, ll = 0.0f, f[SPLIT_WARPS];
-#pragma unroll
-  for (u32 x = 0; x < SPLIT_WARPS; ++x) mm = fmaxf(mm, s_ml[x][r][0]);
-  const float ref = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll
-  for (u32 x = 0; x < SPLIT_WARPS; ++x) { f[x] = ex2(s_ml[x][r][0] - ref); ll += f[x] * s_ml[x][r][1]; }
-  if (r0 + r > r1) return;
-  const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
-  const float *base = (const float *)(smem_raw + (ring - warp * S::RING - smem_addr(smem_raw))) + r * LD;
-  const u64 part = (u64)w.part * H + h;
-  const bool direct = w.pieces == 1;
-  if (!direct && part >= n_parts) { kv_err(a.err, KVERR_RANGE); return; }
-  const float inv = !direct ? 1.0f : ll > 0.0f ? 1.0f / ll : ll;
-  T *const out = (T *)a.out + t * a.o_ts + hq * a.o_hs;
-  float *const sums = scratch_sums(a) + (part * SPLIT_ROWS + r) * D;
-#pragma unroll
-  for (u32 c = c0; c < D; c += 32) {
-    float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-    for (u32 x = 0; x < SPLIT_WARPS; ++x) {
-      const float4 y = *(const float4 *)(base + x * (S::RING / 4) + c);
-      v.x += f[x] * y.x; v.y += f[x] * y.y; v.z += f[x] * y.z; v.w += f[x] * y.w;
-    }
-    if (direct) {
-      const u32 p = Elem<T>::down(v.x * inv, v.y * inv), z = Elem<T>::down(v.z * inv, v.w * inv);
-      u16 *d = (u16 *)out + c;
-      if (((uintptr_t)d & 7) == 0) *(uint2 *)d = make_uint2(p, z);
-      else { d[0] = (u16)p; d[1] = (u16)(p >> 16); d[2] = (u16)z; d[3] = (u16)(z >> 16); }
-    } else {
-      *(float4 *)(sums + c) = v;
-    }
-  }
-  if (tid % 8 == 0) {
-    if (!direct) ((float2 *)(scratch_sums(a) + n_parts * SPLIT_ROWS * D))[part * SPLIT_ROWS + r] = make_float2(mm, ll);
-    else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (mm + log2f(ll)) * 0.69314718055994531f;
   }
 }
 
@@ -792,26 +845,35 @@ __device__ __forceinline__ bool tc_wait(u32 bar, u32 parity, volatile u32 *lost)
   return __all_sync(~0u, bar_try(bar, parity) || tc_wait_slow(bar, parity, lost));
 }
 
+// A piece of a tile, as the scheduling warp hands it to the others.
+struct Job {
+  u32 t0, kv, seq, h;        // first token row, length and number of the sequence; KV head
+  u32 r0, r1;                // rows of the tile, counted in the sequence: first and last
+  u32 shift;                 // index in the sequence of its first new token, as a signed number
+  u32 b0, b1, all_lo, all_hi;// blocks of keys [b0, b1); keys every row sees
+  u32 part, direct, last;    // place of the partial result, or the whole result at once; last: no job, the end
+};
+constexpr u32 TC_JOBS = 4;
+
 template <class T, u32 D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
-k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 min_chunk, u32 target, u32 sms, u64 n_parts) {
+k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 most_parts, u32 n_parts) {
   typedef TcShape<D> S;
-  constexpr bool FP16 = sizeof(T) == 2 && !__is_same(T, __nv_bfloat16);
+  constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
   extern __shared__ u8 smem_raw[];
-  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2], s_qready, s_drain;
+  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2], s_qready[2], s_drain, s_jfull[TC_JOBS], s_jempty[TC_JOBS];
   __shared__ u32 s_tmem;
   __shared__ volatile u32 s_lost;
+  __shared__ Job s_job[TC_JOBS];
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
-  const u32 h = blockIdx.x % H, item = blockIdx.x / H;
   const u32 full = smem_addr(s_full), empty = smem_addr(s_empty), sready = smem_addr(s_sready), pready = smem_addr(s_pready),
-            qready = smem_addr(&s_qready), drain = smem_addr(&s_drain);
-  Piece w;
-  if (!find_piece<TC_THREADS, true>(a, TC_ROWS, min_chunk, target, sms, item, n_parts && blockIdx.x == 0 ? scratch_plan(a) : nullptr, w)) return;
+            qready = smem_addr(s_qready), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
   if (tid == 0) {
     for (u32 i = 0; i < S::STAGES; ++i) { bar_init(full + i * 8, 1); bar_init(empty + i * 8, 1); }
-    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(pready + i * 8, 4); }
-    bar_init(qready, 8); bar_init(drain, 1);
+    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(pready + i * 8, 4); bar_init(qready + i * 8, 4); }
+    for (u32 i = 0; i < TC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 10); }
+    bar_init(drain, 1);
     s_lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -820,51 +882,126 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
+  const u32 piece = choose_piece<TC_THREADS>(a, TC_ROWS, most_parts, gridDim.x);
   tc_before();
   __syncthreads();
   tc_after();
   const u32 tmem = s_tmem;
-
-  const Seq q = w.q;
-  const u32 n_rows = q.n * a.group, r0 = w.tile * TC_ROWS, r1 = min(r0 + TC_ROWS, n_rows) - 1;
-  const u32 n_tiles = r1 - r0 >= TC_TILE ? 2 : 1;
-  u32 first, last, all_lo, all_hi;       // keys any row sees; keys every row sees
-  row_range(a, q, r0 / a.group, first, all_hi);
-  row_range(a, q, r1 / a.group, all_lo, last);
-  const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
-  const u32 per = ((nb + w.pieces - 1) / w.pieces + TC_KB - 1) / TC_KB * TC_KB;       // whole stages
-  const u32 b0 = b_first + min(w.piece * per, nb), b1 = b_first + min((w.piece + 1) * per, nb);
-  const u32 n = (b1 - b0 + TC_KB - 1) / TC_KB;         // stages of keys
   const u32 sq = (smem_addr(smem_raw) + 1023) & ~1023u, ring = sq + S::Q;
   volatile u32 *const lost = &s_lost;
+  // the next job, for a whole warp; false: no more, or a wait ran out
+  u32 jobs = 0;
+  auto next_job = [&](Job &j) {
+    const u32 at = jobs % TC_JOBS;
+    if (!tc_wait(jfull + at * 8, (jobs / TC_JOBS) & 1, lost)) return false;
+    j = s_job[at];
+    __syncwarp();
+    if (lane == 0) bar_arrive(jempty + at * 8);
+    ++jobs;
+    return j.last == 0;
+  };
 
   // registers: 168 for each of 384 threads at the launch; 224 for a thread that holds a row of S, 56 for the others
-  if (warp > 9) {
+  if (warp == 11) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  } else if (warp == 9) {
+  } else if (warp == 10) {
+    // ---- scheduling: this CTA's jobs, one per round of the grid, every other round in reverse so that the long first jobs of
+    // a causal prompt even out. Jobs of a sequence: piece, tile (last tokens first), KV head; those that run at the same
+    // time then mostly read the same keys.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    // ---- loads: K0, V0, K1, V1, ...; blocks behind the piece's last one read as zeros (a slot behind both pools)
-    const u32 *row = a.b.table + w.seq * a.b.table_stride;
-    u32 slots = 0, it = 0;
-    bool ok = true;
-    for (u32 j = 0; j < n && ok; ++j) {
-      if (j % 4 == 0) {
-        const u32 b = b0 + j * TC_KB + lane;
-        slots = b < b1 ? row[b] : 0xFFFFFFFFu;
-        if (b < b1 && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+    u64 base = 0;                        // first job and first partial of the 32 sequences in hand
+    u32 part0 = 0, s0 = 0;
+    Seq q{0, 0, 0};
+    u32 tiles = 0, pieces = 0;
+    u64 my_jobs = 0, at = 0, all = 0; u32 my_part = 0, all_parts = 0;
+    auto take = [&]() {                  // lane: one of the sequences s0 .. s0 + 31
+      const u32 s = s0 + lane;
+      tiles = pieces = 0;
+      if (s < a.b.n_seqs) {
+        q = load_seq(a.b, s, a.err);
+        tiles = seq_tiles(a, q, TC_ROWS);
+        pieces = (seq_blocks(a, q, TC_ROWS) + piece - 1) / piece;
       }
-      const u32 slot = __shfl_sync(~0u, slots, (j % 4) * TC_KB + lane % TC_KB);
-      for (u32 kv = 0; kv < 2; ++kv, ++it) {
-        const u32 st = it % S::STAGES;
-        if (it >= S::STAGES && !tc_wait(empty + st * 8, (it / S::STAGES - 1) & 1, lost)) { ok = false; break; }
-        if (lane == 0) bar_expect(full + st * 8, S::STAGE);
-        __syncwarp();
-        if (lane < TC_KB) load_block(a, maps, ring + st * S::STAGE + lane * S::BLOCK, full + st * 8, slot, 2 * a.layer + kv, h, D / 64);
-        __syncwarp();
+      my_jobs = (u64)tiles * pieces * H;
+      const u32 parts = pieces > 1 ? tiles * pieces : 0;
+      u64 incl = my_jobs; u32 pincl = parts;
+#pragma unroll
+      for (u32 o = 1; o < 32; o *= 2) {
+        const u64 y = __shfl_up_sync(~0u, incl, o); const u32 z = __shfl_up_sync(~0u, pincl, o);
+        if (lane >= o) { incl += y; pincl += z; }
+      }
+      at = base + incl - my_jobs; my_part = part0 + pincl - parts;
+      all = __shfl_sync(~0u, incl, 31); all_parts = __shfl_sync(~0u, pincl, 31);
+      if (blockIdx.x == 0 && n_parts && s < a.b.n_seqs) {
+        scratch_plan(a)[1 + s] = make_uint4(my_part, pieces, tiles, 0);
+        if (pieces > 1) scratch_plan(a)[0].x = 1;
+      }
+    };
+    if (blockIdx.x == 0 && n_parts) { if (lane == 0) scratch_plan(a)[0] = make_uint4(0, 0, 0, 0); __syncwarp(); }
+    take();
+    bool ok = true;
+    for (u32 k = 0;; ++k) {
+      const u64 want = (u64)k * gridDim.x + (k % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      while (want >= base + all && s0 + 32 < a.b.n_seqs) { base += all; part0 += all_parts; s0 += 32; take(); }
+      const u32 hit = __ballot_sync(~0u, want >= at && want < at + my_jobs);
+      const u32 slot = k % TC_JOBS;
+      if (k >= TC_JOBS && !(ok = tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost))) break;
+      if (hit && lane == __ffs(hit) - 1) {
+        Job j;
+        u64 i = want - at;
+        const u32 h = (u32)(i % H); i /= H;
+        const u32 tile = tiles - 1 - (u32)(i % tiles), pc = (u32)(i / tiles);
+        j.t0 = q.t0; j.kv = q.kv; j.seq = s0 + lane; j.h = h; j.shift = q.kv - q.n;
+        j.r0 = tile * TC_ROWS; j.r1 = min(j.r0 + TC_ROWS, q.n * a.group) - 1;
+        u32 first, last;                 // keys any row sees
+        row_range(a, q, j.r0 / a.group, first, j.all_hi);
+        row_range(a, q, j.r1 / a.group, j.all_lo, last);
+        const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+        const u32 per = ((nb + pieces - 1) / pieces + TC_KB - 1) / TC_KB * TC_KB;       // whole stages
+        j.b0 = b_first + min(pc * per, nb); j.b1 = b_first + min((pc + 1) * per, nb);
+        j.direct = pieces == 1;
+        j.part = (my_part + pc * tiles + tile) * H + h;
+        j.last = 0;
+        if (!j.direct && j.part >= n_parts) { kv_err(a.err, KVERR_RANGE); j.part = 0; j.b1 = j.b0; }     // cannot happen
+        s_job[slot] = j;
+      } else if (!hit && lane == 0) {
+        s_job[slot].last = 1;
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(jfull + slot * 8);
+      if (!hit) {                        // behind the last job; block 0 still has the plan of the other sequences to write
+        if (blockIdx.x == 0 && n_parts) while (s0 + 32 < a.b.n_seqs) { base += all; part0 += all_parts; s0 += 32; take(); }
+        break;
       }
     }
-    if (!ok)          // let the copies in flight land, for a while, before the CTA ends
-      for (u32 i = it > S::STAGES ? it - S::STAGES : 0; i < it; ++i) bar_wait(full + (i % S::STAGES) * 8, (i / S::STAGES) & 1);
+  } else if (warp == 9) {
+    // ---- loads: K0, V0, K1, V1, ...; blocks behind the piece's last one read as zeros (a slot behind both pools)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    u32 it = 0;
+    bool ok = true;
+    for (Job j; ok && next_job(j);) {
+      const u32 *row = a.b.table + j.seq * a.b.table_stride;
+      const u32 n = (j.b1 - j.b0 + TC_KB - 1) / TC_KB;
+      u32 slots = 0;
+      for (u32 s = 0; s < n && ok; ++s) {
+        if (s % 4 == 0) {
+          const u32 b = j.b0 + s * TC_KB + lane;
+          slots = b < j.b1 ? row[b] : 0xFFFFFFFFu;
+          if (b < j.b1 && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+        }
+        const u32 slot = __shfl_sync(~0u, slots, (s % 4) * TC_KB + lane % TC_KB);
+        for (u32 kv = 0; kv < 2; ++kv, ++it) {
+          const u32 st = it % S::STAGES;
+          if (it >= S::STAGES && !tc_wait(empty + st * 8, (it / S::STAGES - 1) & 1, lost)) { ok = false; break; }
+          if (lane == 0) bar_expect(full + st * 8, S::STAGE);
+          __syncwarp();
+          if (lane < TC_KB) load_block(a, maps, ring + st * S::STAGE + lane * S::BLOCK, full + st * 8, slot, 2 * a.layer + kv, j.h, D / 64);
+          __syncwarp();
+        }
+      }
+    }
+    // whatever was loaded has landed before the CTA ends, if the products have waited for it or not
+    for (u32 i = it > S::STAGES ? it - S::STAGES : 0; i < it; ++i) bar_wait(full + (i % S::STAGES) * 8, (i / S::STAGES) & 1);
   } else if (warp == 8) {
     // ---- matrix products
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -885,107 +1022,123 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       for (u32 k = 0; k < TC_KEYS / 16; ++k)
         tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, tc_desc(vb + k * (D * 32), 1024, D * 16), id_o, acc || k > 0);
     };
-    bool ok = n == 0 || (tc_wait(qready, 0, lost) && landed(0));
-    if (ok && n) {
-      tc_after();
-      if (leader) {
-        for (u32 i = 0; i < n_tiles; ++i) { product_s(i, 0); tc_commit(sready + i * 8); }
-        tc_commit(empty);
-      }
-      __syncwarp();
-    }
-    for (u32 j = 0; ok && j < n; ++j) {
-      const u32 iv = 2 * j + 1, ik = 2 * j + 2;
-      if (!(ok = landed(iv))) break;
-      if (j + 1 == n && b1 * BT > q.kv) {     // tokens behind the length in the last block: whatever their values hold,
-        const u32 r = lane / 2;               // weight 0 must not meet an Inf or a NaN
-        if ((b1 - 1) * BT + r >= q.kv)
-          for (u32 c = 0; c < D / 16; ++c)
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
-                         ::"r"(stage(iv) + ((b1 - 1 - b0) % TC_KB) * S::BLOCK + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-      }
+    u32 it = 0, seen_q[2] = {0, 0}, seen_p[2] = {0, 0};
+    bool ok = true;
+    for (Job j; ok && next_job(j);) {
+      const u32 n = (j.b1 - j.b0 + TC_KB - 1) / TC_KB, n_tiles = j.r1 - j.r0 >= TC_TILE ? 2 : 1;
+      if (!n) continue;
+      if (!(ok = landed(it))) break;
       for (u32 i = 0; i < n_tiles; ++i) {
-        if (!(ok = tc_wait(pready + i * 8, j & 1, lost))) break;
+        if (!(ok = tc_wait(qready + i * 8, seen_q[i]++ & 1, lost))) break;
         tc_after();
-        if (leader) product_o(i, iv, j > 0);
+        if (leader) { product_s(i, it); tc_commit(sready + i * 8); }
         __syncwarp();
-        if (j + 1 < n) {
-          if (i == 0 && !(ok = landed(ik))) break;
-          if (leader) product_s(i, ik);
+      }
+      if (!ok) break;
+      if (leader) tc_commit(empty + (it % S::STAGES) * 8);
+      __syncwarp();
+      for (u32 s = 0; ok && s < n; ++s) {
+        const u32 iv = it + 2 * s + 1, ik = iv + 1;
+        if (!(ok = landed(iv))) break;
+        if (s + 1 == n && j.b1 * BT > j.kv) {    // tokens behind the length in the last block: whatever their values hold,
+          const u32 r = lane / 2;                // weight 0 must not meet an Inf or a NaN
+          if ((j.b1 - 1) * BT + r >= j.kv)
+            for (u32 c = 0; c < D / 16; ++c)
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
+                           ::"r"(stage(iv) + ((j.b1 - 1 - j.b0) % TC_KB) * S::BLOCK + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
         }
-        if (leader) tc_commit(sready + i * 8);     // S of the next keys, or the finished sums
+        for (u32 i = 0; i < n_tiles; ++i) {
+          if (!(ok = tc_wait(pready + i * 8, seen_p[i]++ & 1, lost))) break;
+          tc_after();
+          if (leader) product_o(i, iv, s > 0);
+          __syncwarp();
+          if (s + 1 < n) {
+            if (i == 0 && !(ok = landed(ik))) break;
+            if (leader) product_s(i, ik);
+          }
+          if (leader) tc_commit(sready + i * 8);     // S of the next keys, or the finished sums
+          __syncwarp();
+        }
+        if (ok && leader) {
+          tc_commit(empty + (iv % S::STAGES) * 8);
+          if (s + 1 < n) tc_commit(empty + (ik % S::STAGES) * 8);
+        }
         __syncwarp();
       }
-      if (ok && leader && j + 1 < n) {       // nobody waits for the last stages
-        tc_commit(empty + (iv % S::STAGES) * 8);
-        tc_commit(empty + (ik % S::STAGES) * 8);
-      }
-      __syncwarp();
+      it += 2 * n;
     }
-    if (!ok) {
-      if (leader) tc_commit(drain);
-      __syncwarp();
-      bar_wait(drain, 0);
-    }
+    // all products and their arrivals are done before the CTA ends
+    if (leader) tc_commit(drain);
+    __syncwarp();
+    bar_wait(drain, 0);
   } else {
     // ---- one thread per row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    const u32 i = warp / 4, rt = tid % TC_TILE, r = r0 + i * TC_TILE + rt;
-    const bool mine = r <= r1;
-    const u32 rr = min(r, r1), t = q.t0 + rr / a.group, hq = h * a.group + rr % a.group;   // rows behind the last one repeat it
-    u32 lo, hi;
-    row_range(a, q, rr / a.group, lo, hi);
-    if (i < n_tiles && n) {
-      const u16 *src = (const u16 *)a.q + (u64)t * a.q_ts + (u64)hq * a.q_hs;
-      const bool wide = ((uintptr_t)src & 15) == 0;
-#pragma unroll
-      for (u32 c = 0; c < D / 8; ++c) {
-        uint4 v;
-        if (wide) v = *(const uint4 *)(src + c * 8);
-        else {
-          u32 x[4];
-#pragma unroll
-          for (u32 y = 0; y < 4; ++y) x[y] = (u32)src[c * 8 + 2 * y] | (u32)src[c * 8 + 2 * y + 1] << 16;
-          v = make_uint4(x[0], x[1], x[2], x[3]);
-        }
-        const u32 dst = sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + rt * 128 + (((c % 8) ^ (rt % 8)) * 16);
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    const u32 i = warp / 4, rt = tid % TC_TILE;
+    const u32 lanes = (warp % 4) << 21, ts = tmem + lanes + i * 128, to = tmem + lanes + 256 + i * D;
+    u32 seen = 0;                        // completions of sready[i]
+    bool ok = true;
+    for (Job j; ok && next_job(j);) {
+      const u32 n_tiles = j.r1 - j.r0 >= TC_TILE ? 2 : 1, n = (j.b1 - j.b0 + TC_KB - 1) / TC_KB;
+      if (i >= n_tiles) continue;
+      const u32 r = j.r0 + i * TC_TILE + rt, rr = min(r, j.r1);     // rows behind the last one repeat it and are not written
+      const bool mine = r <= j.r1;
+      const u32 tok = rr / a.group, t = j.t0 + tok, hq = j.h * a.group + rr % a.group;
+      u32 lo, hi;
+      {
+        const long long own = (long long)(int)j.shift + tok;
+        hi = a.full ? j.kv : own < 0 ? 0u : (u32)own + 1;
+        lo = a.window && hi > a.window ? hi - a.window : 0u;
       }
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) bar_arrive(qready);
-    if (i < n_tiles) {
-      const u32 lanes = (warp % 4) << 21, ts = tmem + lanes + i * 128, to = tmem + lanes + 256 + i * D;
+      if (n) {
+        const u16 *src = (const u16 *)a.q + (u64)t * a.q_ts + (u64)hq * a.q_hs;
+        const bool wide = ((uintptr_t)src & 15) == 0;
+#pragma unroll
+        for (u32 c = 0; c < D / 8; ++c) {
+          uint4 v;
+          if (wide) v = *(const uint4 *)(src + c * 8);
+          else {
+            u32 x[4];
+#pragma unroll
+            for (u32 y = 0; y < 4; ++y) x[y] = (u32)src[c * 8 + 2 * y] | (u32)src[c * 8 + 2 * y + 1] << 16;
+            v = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+          const u32 dst = sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + rt * 128 + (((c % 8) ^ (rt % 8)) * 16);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(qready + i * 8);
+      }
       float m = -INFINITY, l = 0.0f;
-      bool ok = true;
-      for (u32 j = 0; j < n; ++j) {
-        if (!(ok = tc_wait(sready + i * 8, j & 1, lost))) break;
+      for (u32 s = 0; s < n; ++s) {
+        if (!(ok = tc_wait(sready + i * 8, seen++ & 1, lost))) break;
         tc_after();
         u32 x[128];
 #pragma unroll
         for (u32 c = 0; c < 4; ++c) tc_ld32(x + 32 * c, ts + 32 * c);
         tc_wait_ld();
-        float *const s = reinterpret_cast<float *>(x);
-        const u32 key0 = (b0 + j * TC_KB) * BT;
-        if (key0 < all_lo || key0 + TC_KEYS > all_hi) {
+        float *const v = reinterpret_cast<float *>(x);
+        const u32 key0 = (j.b0 + s * TC_KB) * BT;
+        if (key0 < j.all_lo || key0 + TC_KEYS > j.all_hi) {
           const int from = (int)lo - (int)key0, to_ = (int)hi - (int)key0;
 #pragma unroll
-          for (int c = 0; c < 128; ++c) if (c < from || c >= to_) s[c] = -INFINITY;
+          for (int c = 0; c < 128; ++c) if (c < from || c >= to_) v[c] = -INFINITY;
         }
-        float top[4] = {s[0], s[1], s[2], s[3]};
+        float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
         for (u32 c = 4; c < 128; c += 4)
 #pragma unroll
-          for (u32 y = 0; y < 4; ++y) top[y] = fmaxf(top[y], s[c + y]);
+          for (u32 y = 0; y < 4; ++y) top[y] = fmaxf(top[y], v[c + y]);
         const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
         // The sums stay relative to an old maximum until a score passes it by 2^8 (as in the kernel for few rows)
         if (__any_sync(~0u, now > m + 8.0f)) {
           const float next = fmaxf(m, now), f = next == -INFINITY ? 1.0f : ex2(m - next);
           m = next; l *= f;
-          if (j > 0) {                   // the product before S of these keys has been waited for: O is at rest
+          if (s > 0) {                   // the product before S of these keys has been waited for: O is at rest
 #pragma unroll
             for (u32 c = 0; c < D / 16; ++c) {
               u32 y[16];
@@ -1004,7 +1157,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
           u32 p[16];
 #pragma unroll
           for (u32 c = 0; c < 16; ++c) {
-            const float p0 = ex2(fmaf(s[32 * b + 2 * c], a.scale_log2, -ref)), p1 = ex2(fmaf(s[32 * b + 2 * c + 1], a.scale_log2, -ref));
+            const float p0 = ex2(fmaf(v[32 * b + 2 * c], a.scale_log2, -ref)), p1 = ex2(fmaf(v[32 * b + 2 * c + 1], a.scale_log2, -ref));
             sum[c % 4] += p0 + p1;
             p[c] = Elem<T>::down(p0, p1);
           }
@@ -1017,47 +1170,44 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         if (lane == 0) bar_arrive(pready + i * 8);
       }
       // ---- results
-      if (ok && n) { ok = tc_wait(sready + i * 8, n & 1, lost); tc_after(); }
-      const u64 part = (u64)w.part * H + h;
-      const bool direct = w.pieces == 1;
-      if (!direct && part >= n_parts) { if (tid % TC_TILE == 0) kv_err(a.err, KVERR_RANGE); ok = false; }
-      if (ok) {
-        const float inv = !direct ? 1.0f : l > 0.0f ? 1.0f / l : l;
-        u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
-        const bool wide = ((uintptr_t)out & 15) == 0;
-        const u32 prow = i * TC_TILE + rt;
-        float *const sums = scratch_sums(a) + (part * TC_ROWS + prow) * D;
+      if (ok && n) { ok = tc_wait(sready + i * 8, seen++ & 1, lost); tc_after(); }
+      if (!ok) break;
+      const float inv = !j.direct ? 1.0f : l > 0.0f ? 1.0f / l : l;
+      u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
+      const bool wide = ((uintptr_t)out & 15) == 0;
+      const u32 prow = i * TC_TILE + rt;
+      float *const sums = scratch_sums(a) + ((u64)j.part * TC_ROWS + prow) * D;
 #pragma unroll
-        for (u32 c = 0; c < D / 32; ++c) {
-          u32 y[32];
-          __syncwarp();
-          if (n) { tc_ld32(y, to + 32 * c); tc_wait_ld(); }
-          else {
+      for (u32 c = 0; c < D / 32; ++c) {
+        u32 y[32];
+        __syncwarp();
+        if (n) { tc_ld32(y, to + 32 * c); tc_wait_ld(); }
+        else {
 #pragma unroll
-            for (u32 z = 0; z < 32; ++z) y[z] = 0;
-          }
-          if (!mine) {
-          } else if (!direct) {
-#pragma unroll
-            for (u32 z = 0; z < 32; z += 4) *(uint4 *)(sums + 32 * c + z) = make_uint4(y[z], y[z + 1], y[z + 2], y[z + 3]);
-          } else {
-            u32 v[16];
-#pragma unroll
-            for (u32 z = 0; z < 16; ++z) v[z] = Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv);
-            if (wide) {
-#pragma unroll
-              for (u32 z = 0; z < 16; z += 4) *(uint4 *)(out + 32 * c + 2 * z) = make_uint4(v[z], v[z + 1], v[z + 2], v[z + 3]);
-            } else {
-#pragma unroll
-              for (u32 z = 0; z < 16; ++z) { out[32 * c + 2 * z] = (u16)v[z]; out[32 * c + 2 * z + 1] = (u16)(v[z] >> 16); }
-            }
-          }
+          for (u32 z = 0; z < 32; ++z) y[z] = 0;
         }
-        if (mine) {
-          if (!direct) ((float2 *)(scratch_sums(a) + n_parts * TC_ROWS * D))[part * TC_ROWS + prow] = make_float2(m, l);
-          else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
+        if (!mine) {
+        } else if (!j.direct) {
+#pragma unroll
+          for (u32 z = 0; z < 32; z += 4) *(uint4 *)(sums + 32 * c + z) = make_uint4(y[z], y[z + 1], y[z + 2], y[z + 3]);
+        } else {
+          u32 e[16];
+#pragma unroll
+          for (u32 z = 0; z < 16; ++z) e[z] = Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv);
+          if (wide) {
+#pragma unroll
+            for (u32 z = 0; z < 16; z += 4) *(uint4 *)(out + 32 * c + 2 * z) = make_uint4(e[z], e[z + 1], e[z + 2], e[z + 3]);
+          } else {
+#pragma unroll
+            for (u32 z = 0; z < 16; ++z) { out[32 * c + 2 * z] = (u16)e[z]; out[32 * c + 2 * z + 1] = (u16)(e[z] >> 16); }
+          }
         }
       }
+      if (mine) {
+        if (!j.direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * TC_ROWS * D))[j.part * TC_ROWS + prow] = make_float2(m, l);
+        else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
+      }
+      __syncwarp();
     }
   }
   tc_before();
@@ -1090,49 +1240,44 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Partial results a launch can leave, times KV heads.
-static u64 plan_parts(const AttendArgs &a, const AttendPlan &p) { return (p.kind == 2 ? 1ull : 2ull) * p.target + 2 * a.p.n_kv_heads; }
-
-template <class T, u32 D>
-static cudaError_t launch_join(const AttendArgs &a, const AttendPlan &p, u64 parts, cudaStream_t s, u32 *launches) {
+template <class T, u32 D, u32 KIND>
+static cudaError_t launch_join(const AttendArgs &a, const AttendPlan &p, cudaStream_t s, u32 *launches) {
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((u32)(((u64)a.b.n_tokens * a.n_q_heads + 3) / 4)); c.blockDim = dim3(128); c.stream = s;
+  c.gridDim = dim3((u32)std::min<u64>(((u64)a.b.n_tokens * a.n_q_heads + 3) / 4, 16ull * p.sms)); c.blockDim = dim3(128); c.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   c.attrs = &at; c.numAttrs = 1;
   ++*launches;
-  return cudaLaunchKernelEx(&c, k_attend_join<T, D>, a, p.rows, parts);
+  return cudaLaunchKernelEx(&c, k_attend_join<T, D, KIND>, a, p.rows, p.parts);
 }
 
 AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
   AttendPlan p{};
   const u64 H = a.p.n_kv_heads;
-  auto tiles = [&](u64 rows) { return ((u64)a.b.n_tokens * a.group + rows - 1) / rows + a.b.n_seqs; };   // no more than this many
+  p.sms = sm_count;
+  // no more tiles than this: every sequence adds less than one to the quotient
+  auto tiles = [&](u64 rows) { return ((u64)a.b.n_tokens * a.group + a.b.n_seqs * (rows - 1)) / rows; };
   if (a.p.head_dim != 64 && a.p.head_dim != 128) {
     p.rows = ANY_ROWS;
     p.grid = (u32)std::min<u64>(tiles(p.rows), 0x7FFFFFFFu);
     return p;
   }
-  p.sms = sm_count;
-  // Rows of a sequence and KV head: up to two tiles of the kernel for few rows cost less than one of the other, whose tile is
-  // 128 rows high at least.
-  if ((u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group > 2 * SPLIT_ROWS) {
+  // One tile of 16 rows reads K and V once; with more rows than that the other kernel's taller tiles still do.
+  if ((u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group <= SPLIT_ROWS) {
+    p.kind = 1;
+    p.rows = SPLIT_ROWS;
+    const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, a.b.max_blocks / MIN_STRETCH);
+    p.grid = (u32)std::max<u64>(1, std::min<u64>(2ull * sm_count, units * pieces));
+    p.parts = p.grid > 1 ? 2 * p.grid : 0;      // one CTA takes every unit whole
+  } else {
     p.kind = 2;
-    p.rows = TC_ROWS; p.min_chunk = 64; p.target = 4 * sm_count;
-    const bool cut = a.b.max_blocks > p.min_chunk;
-    if (!cut) p.target = 0;
-    p.grid = (u32)std::min<u64>(tiles(p.rows) * H + p.target, 0x7FFFFFFFu);
-    if (cut) p.scratch_bytes = ((a.b.n_seqs * 8ull + 255) & ~255ull) + plan_parts(a, p) * p.rows * (a.p.head_dim + 2) * 4;
-    return p;
+    p.rows = TC_ROWS;
+    const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, (a.b.max_blocks + MIN_PIECE - 1) / MIN_PIECE);
+    p.grid = (u32)std::max<u64>(1, std::min<u64>(sm_count, units * pieces));
+    p.parts = pieces > 1 ? 4 * sm_count : 0;
   }
-  p.kind = 1;
-  p.rows = SPLIT_ROWS; p.min_chunk = 16; p.target = 4 * sm_count;
-  // Cutting every sequence into ceil(blocks / chunk) pieces with chunk >= work / target gives at most target pieces more
-  // than there are tiles, and at most twice target pieces of sequences that are cut at all.
-  const bool cut = a.b.max_blocks > p.min_chunk;
-  p.grid = (u32)std::min<u64>(tiles(p.rows) * H + (cut ? p.target + H : 0), 0x7FFFFFFFu);
-  if (cut) p.scratch_bytes = ((a.b.n_seqs * 8ull + 255) & ~255ull) + plan_parts(a, p) * p.rows * (a.p.head_dim + 2) * 4;
+  if (p.parts) p.scratch_bytes = plan_bytes(a.b.n_seqs) + (u64)p.parts * p.rows * (a.p.head_dim + 2) * 4;
   return p;
 }
 
@@ -1140,22 +1285,20 @@ template <class T, u32 D>
 static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
   cudaError_t r = cudaFuncSetAttribute(k_attend_split<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitShape<D>::SMEM);
   if (r != cudaSuccess) return r;
-  const u64 parts = p.scratch_bytes ? plan_parts(a, p) : 0;
-  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.min_chunk, p.target, parts);
+  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts);
   ++*launches;
-  if ((r = cudaGetLastError()) != cudaSuccess || !parts) return r;
-  return launch_join<T, D>(a, p, parts, s, launches);
+  if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
+  return launch_join<T, D, 1>(a, p, s, launches);
 }
 
 template <class T, u32 D>
 static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
   cudaError_t r = cudaFuncSetAttribute(k_attend_tc<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<D>::SMEM);
   if (r != cudaSuccess) return r;
-  const u64 parts = p.scratch_bytes ? plan_parts(a, p) : 0;
-  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.min_chunk, p.target, p.sms, parts);
+  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts, p.parts);
   ++*launches;
-  if ((r = cudaGetLastError()) != cudaSuccess || !parts) return r;
-  return launch_join<T, D>(a, p, parts, s, launches);
+  if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
+  return launch_join<T, D, 2>(a, p, s, launches);
 }
 
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {

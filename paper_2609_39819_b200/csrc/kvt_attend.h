@@ -56,10 +56,8 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, uint64_t n_slots,
 struct AttendPlan {
   uint32_t kind;             // 0 any head size, 1 few rows (warp-level matrix instructions), 2 many rows (tcgen05)
   uint32_t rows;             // rows of a tile
-  uint32_t min_chunk;        // a piece of a tile's keys is at least this many blocks
-  uint32_t target;           // pieces the whole batch is cut into, if it is long enough
-  uint32_t sms;
-  uint32_t grid;             // work items times KV heads, at most
+  uint32_t sms, grid;
+  uint32_t parts;            // partial results there is room for; 0: nothing can be cut
   uint64_t scratch_bytes;
 };
 AttendPlan plan_attend(const AttendArgs &a, uint32_t max_q_len, int sm_count);

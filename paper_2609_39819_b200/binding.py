@@ -309,6 +309,12 @@ class Engine:
         if rc:
             raise KvtError(rc, "create")
         self.h = h
+        self._dev = self.meta.device
+        self._dev_index = self._dev.index
+        self._kv_dtypes = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
+        # the address of the device's current stream, without a Stream object around it (2 us of a call of 10)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
         self.tail_pool = None
         if n_tail_blocks:       # blocks outside every tier: slot ids n_hbm_blocks + i of append_kv and attend
             self.set_tail_pool((torch.zeros if zero_pools else torch.empty)(n_tail_blocks * self.block_bytes, dtype=torch.uint8,
@@ -506,15 +512,14 @@ class Engine:
         self.tail_pool = pool
 
     def _kv_dtype(self, x, what):
-        torch = self.torch
-        code = KV_BF16 if x.dtype == torch.bfloat16 else KV_FP16 if x.dtype == torch.float16 else None
+        code = self._kv_dtypes.get(x.dtype)
         if code is None:
             raise ValueError(f"{what}: bfloat16 or float16 expected, got {x.dtype}")
         return code
 
     def _kv_tensor(self, x, what, shape, dtype):
         """(address, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
-        if x.dtype != dtype or x.shape != shape or x.device != self._dev:
+        if x.dtype is not dtype or x.shape != shape or x.get_device() != self._dev_index:
             raise ValueError(f"{what}: {dtype} tensor {tuple(shape)} on {self._dev} expected, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
         ts, hs, es = x.stride()
@@ -523,28 +528,21 @@ class Engine:
         return x.data_ptr(), ts, hs
 
     def _kv_batch(self, what, n_tokens, block_table, q_start, kv_len, max_q_len):
-        i32, dev = self.torch.int32, self._dev
-        if block_table.dtype != i32 or q_start.dtype != i32 or kv_len.dtype != i32 or block_table.dim() != 2 or \
-                q_start.dim() != 1 or kv_len.dim() != 1:
+        i32, dev = self.torch.int32, self._dev_index
+        if block_table.dtype is not i32 or q_start.dtype is not i32 or kv_len.dtype is not i32 or \
+                block_table.dim() != 2 or q_start.dim() != 1 or kv_len.dim() != 1:
             raise ValueError(f"{what}: block_table [sequences, blocks], q_start and kv_len must be int32")
         n, m = block_table.shape
-        if kv_len.shape[0] != n or q_start.shape[0] != n + 1 or (m > 1 and block_table.stride(1) != 1) or \
-                (n and q_start.stride(0) != 1) or (n > 1 and kv_len.stride(0) != 1):
+        ts, es = block_table.stride()
+        if kv_len.numel() != n or q_start.numel() != n + 1 or (es != 1 and m > 1) or not q_start.is_contiguous() or \
+                not kv_len.is_contiguous():
             raise ValueError(f"{what}: {n} table rows need {n} lengths and {n + 1} starts, with consecutive elements")
-        if block_table.device != dev or q_start.device != dev or kv_len.device != dev:
-            raise ValueError(f"{what}: block_table, q_start and kv_len must be on {dev}")
-        return Batch(n, n_tokens, m, max_q_len or 0, block_table.stride(0), q_start.data_ptr(), kv_len.data_ptr(),
-                     block_table.data_ptr())
-
-    @property
-    def _dev(self):
-        d = self.__dict__.get("_dev_")
-        if d is None:
-            d = self._dev_ = self.meta.device
-        return d
+        if block_table.get_device() != dev or q_start.get_device() != dev or kv_len.get_device() != dev:
+            raise ValueError(f"{what}: block_table, q_start and kv_len must be on {self._dev}")
+        return Batch(n, n_tokens, m, max_q_len or 0, ts, q_start.data_ptr(), kv_len.data_ptr(), block_table.data_ptr())
 
     def _kv_stream(self):
-        return self.torch.cuda.current_stream(self._dev).cuda_stream
+        return self._raw_stream(self._dev_index)
 
     def append_kv(self, layer, k, v, block_table, q_start, kv_len, rope=None, positions=None, q=None, q_out=None):
         """Writes the new tokens' keys (rotated) and values into the blocks of `layer` and returns the rotated queries
@@ -566,14 +564,16 @@ class Engine:
             a.n_q_heads = hq
             a.q, a.q_ts, a.q_hs = self._kv_tensor(q, "append_kv: q", (t, hq, d), k.dtype)
             if q_out is None:
-                q_out = torch.empty((t, hq, d), dtype=k.dtype, device=self._dev)
+                q_out = q.new_empty((t, hq, d))
             a.q_out, a.qo_ts, a.qo_hs = self._kv_tensor(q_out, "append_kv: q_out", (t, hq, d), k.dtype)
+            if (a.qo_ts == 0 and t > 1) or (a.qo_hs == 0 and hq > 1):
+                raise ValueError("append_kv: q_out is a broadcast tensor")
             if a.q == a.q_out and (a.q_ts, a.q_hs) != (a.qo_ts, a.qo_hs):
                 raise ValueError("append_kv: q_out in the place of q needs its strides")
         elif q_out is not None:
             raise ValueError("append_kv: q_out without q")
         if rope is not None:
-            if rope.freqs.device != self._dev:
+            if rope.freqs.get_device() != self._dev_index:
                 raise ValueError(f"append_kv: rope is on {rope.freqs.device}, the engine on {self._dev}")
             a.rot_dim, a.flags, a.freqs = rope.rot_dim, ROPE_INTERLEAVED if rope.interleaved else 0, rope.freqs.data_ptr()
             a.n_axes = rope.n_axes
@@ -582,7 +582,7 @@ class Engine:
                 raise ValueError(f"append_kv: {rope.n_axes} axes need positions")
         if positions is not None:
             p2 = positions if positions.dim() == 2 else positions[None]
-            if rope is None or p2.dtype != torch.int32 or p2.shape != (rope.n_axes, t) or p2.device != self._dev or \
+            if rope is None or p2.dtype != torch.int32 or p2.shape != (rope.n_axes, t) or p2.get_device() != self._dev_index or \
                     (t > 1 and p2.stride(1) != 1):
                 raise ValueError(f"append_kv: positions must be int32 [{rope.n_axes if rope else 1}, {t}] on {self._dev}, with a rope")
             a.positions, a.pos_stride = p2.data_ptr(), p2.stride(0)
@@ -602,9 +602,13 @@ class Engine:
         t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
         qp, qts, qhs = self._kv_tensor(q, "attend: q", (t, hq, self.head_dim), q.dtype)
         if out is None:
-            out = torch.empty((t, hq, d), dtype=q.dtype, device=self._dev)
-        op, ots, ohs = self._kv_tensor(out, "attend: out", (t, hq, d), q.dtype)
-        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (t, hq) or lse.device != self._dev or
+            out = q.new_empty((t, hq, d))
+            op, ots, ohs = out.data_ptr(), hq * d, d
+        else:
+            op, ots, ohs = self._kv_tensor(out, "attend: out", (t, hq, d), q.dtype)
+            if (ots == 0 and t > 1) or (ohs == 0 and hq > 1):
+                raise ValueError("attend: out is a broadcast tensor")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (t, hq) or lse.get_device() != self._dev_index or
                                 not lse.is_contiguous()):
             raise ValueError(f"attend: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
         a = AttendArgs(self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len), layer, dt, hq,
@@ -612,7 +616,7 @@ class Engine:
                        lse.data_ptr() if lse is not None else None, qts, qhs, ots, ohs)
         n = self.L.kvt_attend_scratch_bytes(self.h, C.byref(a))
         if n:
-            scratch = torch.empty(n, dtype=torch.uint8, device=self._dev)   # from the current stream's pool, or the capture's
+            scratch = torch.empty(n, dtype=torch.uint8, device=self._dev)      # from the current stream's pool, or the capture's
             a.scratch, a.scratch_bytes = scratch.data_ptr(), n
         self._check(self.L.kvt_attend(self.h, C.byref(a), self._kv_stream()), "attend")
         return out

@@ -325,6 +325,8 @@ __device__ __forceinline__ void load_block(const AttendArgs &a, const KvMaps &m,
                ::"r"(dst), "l"(map), "r"(0), "r"(0), "r"(h * halves), "r"(c3), "r"(c4), "r"(bar) : "memory");
 }
 
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
 // Which CTA does what is worked out by every CTA for itself from the device-side lengths, so a captured launch follows
 // them. `unit`: one tile of rows of one sequence and KV head, against all its keys. Its number of blocks is bounded per
 // sequence (whole sequence, or window plus the tokens of a tile).
@@ -353,7 +355,7 @@ __device__ __forceinline__ u64 block_scan(u64 n, u64 *s_sum, u64 &all) {
 
 // Partial results in scratch: a header, a plan record per sequence, `rows` rows of head_dim sums per partial result, then the
 // (maximum, sum) pairs of all of them.
-//   kind 1 (few rows): header {work per CTA, -}, record {first unit's place in the work (64 bits), blocks of a unit, -}
+//   kind 1 (few rows): header {work per CTA, -}, record {first unit's place in the work (64 bits), length of a unit, -}
 //   kind 2:            header {any sequence cut, -}, record {first partial, pieces, tiles, -}
 __device__ __forceinline__ uint4 *scratch_plan(const AttendArgs &a) { return (uint4 *)a.scratch; }
 __host__ __device__ __forceinline__ u64 plan_bytes(u32 n_seqs) { return (16ull * (n_seqs + 1) + 255) & ~255ull; }
@@ -361,8 +363,9 @@ __device__ __forceinline__ float *scratch_sums(const AttendArgs &a) { return (fl
 
 // Kind 1: the blocks of all units, one after the other, are dealt out in equal stretches, one per CTA, so that every CTA
 // reads as much as any other whatever the lengths are; a unit that crosses a border is joined from its parts. A stretch is
-// `per` blocks, at least MIN_STRETCH. Order of units: sequence, tile, KV head.
-constexpr u32 MIN_STRETCH = 16;
+// `per` blocks, at least MIN_STRETCH. Order of units: sequence, tile, KV head. A unit counts UNIT_COST blocks more than it
+// has, at its front, for what it costs besides its blocks.
+constexpr u32 MIN_STRETCH = 8, UNIT_COST = 8;
 template <u32 THREADS>
 __device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publish, u64 &x, u64 &x_end, u32 &per, u32 &seq, u64 &base) {
   __shared__ u64 s_sum[THREADS / 32], s_base;
@@ -370,7 +373,7 @@ __device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publi
   auto units = [&](u32 s) -> u64 {
     if (s >= a.b.n_seqs) return 0;
     const Seq q = load_seq(a.b, s, a.err);
-    return (u64)seq_tiles(a, q, rows) * a.p.n_kv_heads * seq_blocks(a, q, rows);
+    return (u64)seq_tiles(a, q, rows) * a.p.n_kv_heads * (seq_blocks(a, q, rows) + UNIT_COST);
   };
   u64 total = 0, all, mine = 0, at = 0;
   for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
@@ -391,7 +394,7 @@ __device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publi
     at += base0;
     if (mine && x >= at && x < at + mine) { s_seq = s; s_base = at; }
     if (publish && s < a.b.n_seqs)
-      scratch_plan(a)[1 + s] = make_uint4((u32)at, (u32)(at >> 32), seq_blocks(a, load_seq(a.b, s, a.err), rows), 0);
+      scratch_plan(a)[1 + s] = make_uint4((u32)at, (u32)(at >> 32), seq_blocks(a, load_seq(a.b, s, a.err), rows) + UNIT_COST, 0);
     base0 += all;
     if (!publish && (!any || x < base0)) break;
   }
@@ -445,18 +448,20 @@ __device__ u32 choose_piece(const AttendArgs &a, u32 rows, u32 most, u32 sms) {
   return s_piece;
 }
 
-// Joins the parts of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. One warp per row (token, head) at a time;
-// rows of units that were not cut are already written. Launched behind the kernel that leaves the parts, waits for all of it.
+// Joins the parts of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. Rows of units that were not cut are already
+// written. Launched behind the kernel that leaves the parts, waits for all of it. Kind 1: few rows of many parts, a CTA
+// takes one row and a warp every fourth part of it; kind 2: many rows of few parts, a warp per row.
 template <class T, u32 D, u32 KIND>
 __global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u32 n_parts) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const u32 lane = threadIdx.x & 31, H = a.p.n_kv_heads;
-  const u32 head = scratch_plan(a)[0].x;
-  if (KIND == 2 && !head) return;
+  constexpr u32 WPR = KIND == 1 ? 4 : 1, C = D / 32;      // warps per row; columns per lane
+  __shared__ float s_acc[4][D], s_l[4];
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.p.n_kv_heads, sub = warp % WPR;
+  u32 head = 0;
+  bool waited = false;
   const float *sums = scratch_sums(a);
   const float2 *ml = (const float2 *)(sums + (u64)n_parts * rows * D);
-  const u64 n_rows = (u64)a.b.n_tokens * a.n_q_heads, step = (u64)gridDim.x * 4;
-  for (u64 id = (u64)blockIdx.x * 4 + (threadIdx.x >> 5); id < n_rows; id += step) {
+  const u64 n_rows = (u64)a.b.n_tokens * a.n_q_heads, step = (u64)gridDim.x * (4 / WPR);
+  for (u64 id = (u64)blockIdx.x * (4 / WPR) + warp / WPR; id < n_rows; id += step) {
     const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id % a.n_q_heads);
     u32 seq = 0;                         // the first sequence the token lies in
     bool found = false;
@@ -465,46 +470,64 @@ __global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u32
       const u32 hit = __ballot_sync(~0u, s < a.b.n_seqs && a.b.q_start[s] <= t && t < a.b.q_start[s + 1]);
       if (hit) { seq = s0 + __ffs(hit) - 1; found = true; }
     }
+    if (!waited) {                       // the batch's arrays are older than the kernel before this one
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      waited = true;
+      head = scratch_plan(a)[0].x;
+      if (KIND == 2 && !head) return;
+    }
     if (!found) continue;
     const uint4 plan = scratch_plan(a)[1 + seq];
     const u32 h = hq / a.group, r = (t - a.b.q_start[seq]) * a.group + hq % a.group, tile = r / rows, row = r % rows;
-    u64 c0 = 0, c1 = 0, p0, stride, n;     // partial i: p0 + i * stride, but for kind 1 the first may lie elsewhere
-    u64 odd = 0;
+    u32 p0, stride, n, odd = 0;          // partial i: p0 + i * stride; the first may lie `odd` further
     if (KIND == 1) {
-      const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z, e = s + plan.z;
-      c0 = s / head; c1 = (e - 1) / head;
-      p0 = 2 * c0; stride = 2; n = c1 - c0 + 1;
+      const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z, e = s + plan.z, c0 = s / head, c1 = (e - 1) / head;
+      p0 = (u32)(2 * c0); stride = 2; n = (u32)(c1 - c0) + 1;
       odd = s > c0 * head;
     } else {
-      p0 = ((u64)plan.x + tile) * H + h; stride = (u64)plan.z * H; n = plan.y;
+      p0 = (plan.x + tile) * H + h; stride = plan.z * H; n = plan.y;
     }
     if (n <= 1) continue;
-    if (p0 + (n - 1) * stride >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
-    auto place = [&](u64 i) { return (p0 + i * stride + (i == 0 ? odd : 0)) * rows + row; };
+    if ((u64)p0 + (u64)(n - 1) * stride >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
+    auto place = [&](u32 i) { return (p0 + i * stride + (i == 0 ? odd : 0)) * rows + row; };     // below n_parts * rows < 2^20
     float m = -INFINITY;
-    for (u64 i = lane; i < n; i += 32) m = fmaxf(m, ml[place(i)].x);
+    for (u32 i = lane; i < n; i += 32) m = fmaxf(m, ml[place(i)].x);
 #pragma unroll
     for (u32 o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
     const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, acc[D / 32];
+    float l = 0.0f, acc[C];
 #pragma unroll
-    for (u32 c = 0; c < D / 32; ++c) acc[c] = 0.0f;
-#pragma unroll 4
-    for (u64 i = 0; i < n; ++i) {
-      const u64 at = place(i);
+    for (u32 c = 0; c < C; ++c) acc[c] = 0.0f;
+#pragma unroll 8
+    for (u32 i = sub; i < n; i += WPR) {
+      const u32 at = place(i);
       const float2 x = ml[at];
-      const float w = x.x == -INFINITY ? 0.0f : exp2f(x.x - ref);      // a part without keys for this row holds zeros
-      l += w * x.y;
-      const float *o = sums + at * D + lane * (D / 32);
-      float v[D / 32];
+      const float *o = sums + (u64)at * D + lane * C;
+      float v[C];
       if (D == 128) *(float4 *)v = *(const float4 *)o; else *(float2 *)v = *(const float2 *)o;
+      const float w = x.x == -INFINITY ? 0.0f : ex2(x.x - ref);      // a part without keys for this row holds zeros
+      l += w * x.y;
 #pragma unroll
-      for (u32 c = 0; c < D / 32; ++c) acc[c] += w * v[c];
+      for (u32 c = 0; c < C; ++c) acc[c] += w * v[c];
+    }
+    if (WPR > 1) {
+      __syncthreads();                   // the row before this one is read
+#pragma unroll
+      for (u32 c = 0; c < C; ++c) s_acc[warp][lane * C + c] = acc[c];
+      if (lane == 0) s_l[warp] = l;
+      __syncthreads();
+      if (sub) continue;
+#pragma unroll
+      for (u32 w = 1; w < WPR; ++w) {
+        l += s_l[w];
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) acc[c] += s_acc[w][lane * C + c];
+      }
     }
     const float inv = l > 0.0f ? 1.0f / l : l;
-    T *o = (T *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + lane * (D / 32);
+    T *o = (T *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + lane * C;
 #pragma unroll
-    for (u32 c = 0; c < D / 32; ++c) o[c] = Elem<T>::down1(acc[c] * inv);
+    for (u32 c = 0; c < C; ++c) o[c] = Elem<T>::down1(acc[c] * inv);
     if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
   }
 }
@@ -535,7 +558,6 @@ __device__ __forceinline__ void ldm4(u32 (&r)[4], u32 addr) {
 __device__ __forceinline__ void ldm4t(u32 (&r)[4], u32 addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 // Place of (token r, 16 bytes c of the head) in a loaded block: [r / 8][c / 8][r % 8][c % 8], swizzled.
 template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
   return (r / 8) * (D * 16) + (c / 8) * 1024 + (r % 8) * 128 + (((c % 8) ^ (r % 8)) * 16);
@@ -562,7 +584,7 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
   const u64 x_begin = x;
   const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
   Seq q = load_seq(a.b, seq, a.err);
-  u32 tiles = seq_tiles(a, q, SPLIT_ROWS), unit = seq_blocks(a, q, SPLIT_ROWS);
+  u32 tiles = seq_tiles(a, q, SPLIT_ROWS), unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
   u32 it = 0;                            // stages this warp has used
   bool ok = true;
 
@@ -572,7 +594,7 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
       base += (u64)tiles * H * unit;
       if (++seq >= a.b.n_seqs) return;   // cannot happen: x < x_end <= all work
       q = load_seq(a.b, seq, a.err);
-      tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS);
+      tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
     }
     const u32 u = (u32)((x - base) / unit), tile = u / H, h = u % H;
     const u64 u0 = base + (u64)u * unit, x1 = min((unsigned long long)x_end, (unsigned long long)(u0 + unit));
@@ -583,7 +605,8 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
     row_range(a, q, r0 / a.group, first, all_hi);
     row_range(a, q, r1 / a.group, all_lo, last);
     const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
-    const u32 b0 = b_first + min((u32)(x - u0), nb), b1 = b_first + min((u32)(x1 - u0), nb);
+    const u32 o0 = (u32)(x - u0), o1 = (u32)(x1 - u0);
+    const u32 b0 = b_first + min(o0 > UNIT_COST ? o0 - UNIT_COST : 0, nb), b1 = b_first + min(o1 > UNIT_COST ? o1 - UNIT_COST : 0, nb);
     const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
     const u32 *row = a.b.table + seq * a.b.table_stride;
     u32 slots = 0;                       // lane i: the slot of this warp's block number (i mod 32) of the current 32
@@ -1243,7 +1266,7 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 
 template <class T, u32 D, u32 KIND>
 static cudaError_t launch_join(const AttendArgs &a, const AttendPlan &p, cudaStream_t s, u32 *launches) {
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((u32)std::min<u64>(((u64)a.b.n_tokens * a.n_q_heads + 3) / 4, 16ull * p.sms)); c.blockDim = dim3(128); c.stream = s;
+  c.gridDim = dim3((u32)std::min<u64>(KIND == 1 ? (u64)a.b.n_tokens * a.n_q_heads : ((u64)a.b.n_tokens * a.n_q_heads + 3) / 4, 16ull * p.sms)); c.blockDim = dim3(128); c.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
@@ -1267,7 +1290,7 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
   if ((u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group <= SPLIT_ROWS) {
     p.kind = 1;
     p.rows = SPLIT_ROWS;
-    const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, a.b.max_blocks / MIN_STRETCH);
+    const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, ((u64)a.b.max_blocks + UNIT_COST) / MIN_STRETCH);
     p.grid = (u32)std::max<u64>(1, std::min<u64>(2ull * sm_count, units * pieces));
     p.parts = p.grid > 1 ? 2 * p.grid : 0;      // one CTA takes every unit whole
   } else {
@@ -1281,9 +1304,18 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
   return p;
 }
 
+// Dynamic shared memory above 48 KB is asked for once per kernel and engine (a runtime call of half a microsecond).
+template <class K>
+static cudaError_t allow_smem(K kern, u32 which, u32 bytes, u32 *allowed) {
+  if (*allowed >> which & 1) return cudaSuccess;
+  const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (r == cudaSuccess) *allowed |= 1u << which;
+  return r;
+}
+
 template <class T, u32 D>
-static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
-  cudaError_t r = cudaFuncSetAttribute(k_attend_split<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitShape<D>::SMEM);
+static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
+  cudaError_t r = allow_smem(k_attend_split<T, D>, 2 + (D == 128) * 2 + a.fp16, SplitShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
   k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts);
   ++*launches;
@@ -1292,8 +1324,8 @@ static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const 
 }
 
 template <class T, u32 D>
-static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
-  cudaError_t r = cudaFuncSetAttribute(k_attend_tc<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<D>::SMEM);
+static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
+  cudaError_t r = allow_smem(k_attend_tc<T, D>, 6 + (D == 128) * 2 + a.fp16, TcShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
   k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts, p.parts);
   ++*launches;
@@ -1301,18 +1333,18 @@ static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvM
   return launch_join<T, D, 2>(a, p, s, launches);
 }
 
-cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *launches) {
+cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
   if (p.kind == 2) {
-    if (a.p.head_dim == 64) return a.fp16 ? launch_tc<__half, 64>(a, p, m, s, launches) : launch_tc<__nv_bfloat16, 64>(a, p, m, s, launches);
-    return a.fp16 ? launch_tc<__half, 128>(a, p, m, s, launches) : launch_tc<__nv_bfloat16, 128>(a, p, m, s, launches);
+    if (a.p.head_dim == 64) return a.fp16 ? launch_tc<__half, 64>(a, p, m, s, allowed, launches) : launch_tc<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
+    return a.fp16 ? launch_tc<__half, 128>(a, p, m, s, allowed, launches) : launch_tc<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
   }
   if (p.kind == 1) {
-    if (a.p.head_dim == 64) return a.fp16 ? launch_split<__half, 64>(a, p, m, s, launches) : launch_split<__nv_bfloat16, 64>(a, p, m, s, launches);
-    return a.fp16 ? launch_split<__half, 128>(a, p, m, s, launches) : launch_split<__nv_bfloat16, 128>(a, p, m, s, launches);
+    if (a.p.head_dim == 64) return a.fp16 ? launch_split<__half, 64>(a, p, m, s, allowed, launches) : launch_split<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
+    return a.fp16 ? launch_split<__half, 128>(a, p, m, s, allowed, launches) : launch_split<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
   }
   const u32 D = a.p.head_dim, smem = (ANY_ROWS * D + ANY_KEYS * (D + 1) + ANY_KEYS * D) * 4;
   auto kern = a.fp16 ? k_attend_any<__half> : k_attend_any<__nv_bfloat16>;
-  cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t r = allow_smem(kern, a.fp16, (ANY_ROWS + 2 * ANY_KEYS) * (ANY_MAX_DIM + 1) * 4, allowed);
   if (r != cudaSuccess) return r;
   kern<<<dim3(p.grid, a.p.n_kv_heads), ANY_THREADS, smem, s>>>(a);
   ++*launches;

@@ -63,6 +63,7 @@ struct AttendPlan {
 AttendPlan plan_attend(const AttendArgs &a, uint32_t max_q_len, int sm_count);
 
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, uint32_t *launches);
-cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint32_t *launches);
+// allowed: bits of the kernels whose shared memory has been asked for on this engine's device
+cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint32_t *allowed, uint32_t *launches);
 
 }  // namespace kvt

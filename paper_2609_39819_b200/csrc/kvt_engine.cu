@@ -157,7 +157,7 @@ struct kvt_engine {
   bool metadata_only;
   int sm_count = 148;
   int device = 0;
-  KvMaps kv_maps{}; bool kv_maps_ok = false;   // for head sizes of 64 and 128
+  KvMaps kv_maps{}; bool kv_maps_ok = false; u32 kv_smem_allowed = 0;   // for head sizes of 64 and 128
   u8 *tail_pool = nullptr; u32 n_tail = 0;   // blocks outside every tier (kvt_set_tail_pool)
   // host state
   std::vector<Ctx> ctxs;
@@ -2382,7 +2382,7 @@ int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *args, void *stream) {
     if ((uintptr_t)a.scratch & 15) return fail(e, KVT_E_INVAL, "attend: misaligned scratch");
   }
   u32 launches = 0;
-  const cudaError_t r = launch_attend(x, p, e->kv_maps, (cudaStream_t)stream, &launches);
+  const cudaError_t r = launch_attend(x, p, e->kv_maps, (cudaStream_t)stream, &e->kv_smem_allowed, &launches);
   return kv_launched(e, r, launches);
 }
 

@@ -786,8 +786,9 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
 // ------------------------------------------------------------------------------------------------------
 // Many rows (prompts, chunks of new tokens): bound by the tensor cores and the exponentials. A CTA takes up to 256 rows
 // of one KV head as two tiles of 128, the height of a tcgen05 matrix instruction, and walks over the keys 128 at a time.
-//   warp 9      (10 and 11 only give up their registers) loads K and V (TMA, one box per block) into a ring of 128-key stages
-//   warp 8      issues the matrix products: S = Q K^T and O += P V, both accumulated in tensor memory
+//   warp 10     works out the CTA's jobs
+//   warp 9      loads K and V (TMA, one box per block) into a ring of 128-key stages
+//   warp 8      issues the matrix products (warp 11 only gives up its registers): S = Q K^T and O += P V, both accumulated in tensor memory
 //   warps 0-7   one thread per row: maximum, powers, sum; P goes back to tensor memory in the place of S, as the first
 //               operand of the second product
 // The two tiles take turns: while one tile's powers are computed the tensor cores work on the other. Tensor memory: S0,
@@ -853,6 +854,30 @@ __device__ __forceinline__ void tc_st16(u32 addr, const u32 *r) {
                ::"r"(addr), TC_R16("r", r, 0) : "memory");
 }
 
+// Two 32-bit numbers at a time.
+__device__ __forceinline__ u64 pack2(float a, float b) { u64 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpack2(u64 x) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x)); return r; }
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ float maxnan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+// 2^x on the FMA pipes, for x <= 127: x = n + f with n the nearest whole number, 2^f by a polynomial of degree 4 that is 1 at
+// 0 (coefficients from a least-squares fit of the relative error on [-1/2, 1/2], reweighted until its ripples are equal: off
+// by 2.9e-6 of the value at most), n added to the exponent. -127 and anything below give 0. The special-function unit makes 16 powers per cycle and SM, as long as the
+// tensor cores take for the products around them; a quarter of the powers made here evens that out.
+__device__ __forceinline__ float2 exp2_poly(u64 y) {
+  constexpr float MAGIC = 12582912.0f;   // 1.5 * 2^23: added, it leaves the whole part in the low bits
+  const float2 v = unpack2(y);
+  y = pack2(maxnan(v.x, -127.0f), maxnan(v.y, -127.0f));
+  const u64 t = add2(y, pack2(MAGIC, MAGIC)), f = fma2(add2(t, pack2(-MAGIC, -MAGIC)), pack2(-1.0f, -1.0f), y);
+  u64 p = fma2(f, pack2(0.009582818485796452f, 0.009582818485796452f), pack2(0.05590637028217316f, 0.05590637028217316f));
+  p = fma2(p, f, pack2(0.24024099111557007f, 0.24024099111557007f));
+  p = fma2(p, f, pack2(0.6931241750717163f, 0.6931241750717163f));
+  p = fma2(p, f, pack2(1.0f, 1.0f));
+  const float2 q = unpack2(p), n = unpack2(t);
+  return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(q.y) + (__float_as_int(n.y) << 23)));
+}
+
 // A wait that also ends when another warp of the CTA has given up; gives up itself after WAIT_NS.
 __device__ __forceinline__ bool tc_wait_slow(u32 bar, u32 parity, volatile u32 *lost) {
   const u64 t0 = now_ns();
@@ -863,6 +888,7 @@ __device__ __forceinline__ bool tc_wait_slow(u32 bar, u32 parity, volatile u32 *
   *lost = 1;
   return false;
 }
+__device__ __forceinline__ bool tc_wait1(u32 bar, u32 parity, volatile u32 *lost) { return bar_try(bar, parity) || tc_wait_slow(bar, parity, lost); }
 // Whole warps wait, and come back with one answer.
 __device__ __forceinline__ bool tc_wait(u32 bar, u32 parity, volatile u32 *lost) {
   return __all_sync(~0u, bar_try(bar, parity) || tc_wait_slow(bar, parity, lost));
@@ -876,7 +902,8 @@ struct Job {
   u32 b0, b1, all_lo, all_hi;// blocks of keys [b0, b1); keys every row sees
   u32 part, direct, last;    // place of the partial result, or the whole result at once; last: no job, the end
 };
-constexpr u32 TC_JOBS = 4;
+constexpr u32 TC_JOBS = 4, TC_PARTS = 4;      // P is handed to the second product in so many parts
+constexpr u32 POLY_OF_4 = 1;                   // of four pairs of powers, so many are made by exp2_poly
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
@@ -884,7 +911,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   typedef TcShape<D> S;
   constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
   extern __shared__ u8 smem_raw[];
-  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2], s_qready[2], s_drain, s_jfull[TC_JOBS], s_jempty[TC_JOBS];
+  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2][TC_PARTS], s_qready[2], s_drain, s_jfull[TC_JOBS], s_jempty[TC_JOBS];
   __shared__ u32 s_tmem;
   __shared__ volatile u32 s_lost;
   __shared__ Job s_job[TC_JOBS];
@@ -894,7 +921,8 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
             qready = smem_addr(s_qready), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
   if (tid == 0) {
     for (u32 i = 0; i < S::STAGES; ++i) { bar_init(full + i * 8, 1); bar_init(empty + i * 8, 1); }
-    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(pready + i * 8, 4); bar_init(qready + i * 8, 4); }
+    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(qready + i * 8, 4); }
+    for (u32 i = 0; i < 2 * TC_PARTS; ++i) bar_init(pready + i * 8, 4);
     for (u32 i = 0; i < TC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 10); }
     bar_init(drain, 1);
     s_lost = 0;
@@ -1026,76 +1054,91 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     // whatever was loaded has landed before the CTA ends, if the products have waited for it or not
     for (u32 i = it > S::STAGES ? it - S::STAGES : 0; i < it; ++i) bar_wait(full + (i % S::STAGES) * 8, (i / S::STAGES) & 1);
   } else if (warp == 8) {
-    // ---- matrix products
+    // ---- matrix products: one thread does all of it, the tiles strictly in turn, which keeps their powers half a period apart
+    // (a thread per tile was tried: the tiles fall into step and compete, first for the tensor cores, then for the powers).
+    // What it does between two products is in the way of the tensor cores, so that is kept short: stages are counted up,
+    // not divided out, descriptors differ by constants, arrivals of K and V are looked at before those of P.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    const u32 id_s = tc_idesc(FP16, TC_KEYS, false), id_o = tc_idesc(FP16, D, true);
-    const bool leader = elect_one();
-    auto stage = [&](u32 it) { return ring + (it % S::STAGES) * S::STAGE; };
-    auto landed = [&](u32 it) { return tc_wait(full + (it % S::STAGES) * 8, (it / S::STAGES) & 1, lost); };
-    auto product_s = [&](u32 i, u32 it) {
-      const u32 qa = sq + i * (TC_TILE * D * 2), kb = stage(it);
+    if (elect_one()) {
+      const u32 id_s = tc_idesc(FP16, TC_KEYS, false), id_o = tc_idesc(FP16, D, true);
+      const u64 dq0 = tc_desc(sq, 16, 1024), dk0 = tc_desc(ring, 16, D * 16), dv0 = tc_desc(ring, 1024, D * 16);
+      u32 st = 0, ph = 0;                // stage in turn and its phase
+      auto landed = [&]() { return tc_wait1(full + st * 8, ph, lost); };
+      auto next = [&]() { if (++st == S::STAGES) { st = 0; ph ^= 1; } };
+      auto product_s = [&](u32 i, u64 dk) {
 #pragma unroll
-      for (u32 k = 0; k < D / 16; ++k)
-        tc_mma_ss(tmem + i * 128, tc_desc(qa + (k / 4) * (TC_TILE * 128) + (k % 4) * 32, 16, 1024),
-                  tc_desc(kb + (k / 4) * 1024 + (k % 4) * 32, 16, D * 16), id_s, k > 0);
-    };
-    auto product_o = [&](u32 i, u32 it, bool acc) {
-      const u32 vb = stage(it);
+        for (u32 k = 0; k < D / 16; ++k)
+          tc_mma_ss(tmem + i * 128, dq0 + (i * (TC_TILE * D * 2) + (k / 4) * (TC_TILE * 128) + (k % 4) * 32) / 16,
+                    dk + ((k / 4) * 1024 + (k % 4) * 32) / 16, id_s, k > 0);
+        tc_commit(sready + i * 8);
+      };
+      u32 seen_q[2] = {0, 0}, seen_p[2] = {0, 0};
+      bool ok = true;
+      for (;;) {
+        const u32 at = jobs % TC_JOBS;
+        if (!(ok = tc_wait1(jfull + at * 8, (jobs / TC_JOBS) & 1, lost))) break;
+        ++jobs;
+        const u32 r0 = s_job[at].r0, r1 = s_job[at].r1, b0 = s_job[at].b0, b1 = s_job[at].b1, kv = s_job[at].kv, end = s_job[at].last;
+        bar_arrive(jempty + at * 8);
+        if (end) break;
+        const u32 n = (b1 - b0 + TC_KB - 1) / TC_KB;
+        const bool two = r1 - r0 >= TC_TILE;
+        if (!n) continue;
+        if (!(ok = landed())) break;
+        u64 dk = dk0 + st * (S::STAGE / 16);
 #pragma unroll
-      for (u32 k = 0; k < TC_KEYS / 16; ++k)
-        tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, tc_desc(vb + k * (D * 32), 1024, D * 16), id_o, acc || k > 0);
-    };
-    u32 it = 0, seen_q[2] = {0, 0}, seen_p[2] = {0, 0};
-    bool ok = true;
-    for (Job j; ok && next_job(j);) {
-      const u32 n = (j.b1 - j.b0 + TC_KB - 1) / TC_KB, n_tiles = j.r1 - j.r0 >= TC_TILE ? 2 : 1;
-      if (!n) continue;
-      if (!(ok = landed(it))) break;
-      for (u32 i = 0; i < n_tiles; ++i) {
-        if (!(ok = tc_wait(qready + i * 8, seen_q[i]++ & 1, lost))) break;
-        tc_after();
-        if (leader) { product_s(i, it); tc_commit(sready + i * 8); }
-        __syncwarp();
-      }
-      if (!ok) break;
-      if (leader) tc_commit(empty + (it % S::STAGES) * 8);
-      __syncwarp();
-      for (u32 s = 0; ok && s < n; ++s) {
-        const u32 iv = it + 2 * s + 1, ik = iv + 1;
-        if (!(ok = landed(iv))) break;
-        if (s + 1 == n && j.b1 * BT > j.kv) {    // tokens behind the length in the last block: whatever their values hold,
-          const u32 r = lane / 2;                // weight 0 must not meet an Inf or a NaN
-          if ((j.b1 - 1) * BT + r >= j.kv)
-            for (u32 c = 0; c < D / 16; ++c)
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
-                           ::"r"(stage(iv) + ((j.b1 - 1 - j.b0) % TC_KB) * S::BLOCK + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-        }
-        for (u32 i = 0; i < n_tiles; ++i) {
-          if (!(ok = tc_wait(pready + i * 8, seen_p[i]++ & 1, lost))) break;
-          tc_after();
-          if (leader) product_o(i, iv, s > 0);
-          __syncwarp();
-          if (s + 1 < n) {
-            if (i == 0 && !(ok = landed(ik))) break;
-            if (leader) product_s(i, ik);
+        for (u32 i = 0; i < 2; ++i)
+          if (ok && (i == 0 || two)) {
+            ok = tc_wait1(qready + i * 8, seen_q[i]++ & 1, lost);
+            tc_after();
+            if (ok) product_s(i, dk);
           }
-          if (leader) tc_commit(sready + i * 8);     // S of the next keys, or the finished sums
-          __syncwarp();
+        if (!ok) break;
+        tc_commit(empty + st * 8);
+        next();
+        for (u32 s = 0; s < n; ++s) {
+          if (!(ok = landed())) break;
+          const u32 sv = st;
+          const bool more = s + 1 < n;
+          if (!more && b1 * BT > kv) {           // tokens behind the length in the last block: whatever their values hold,
+            for (u32 r = kv % BT; r < BT; ++r)   // weight 0 must not meet an Inf or a NaN
+              for (u32 c = 0; c < D / 8; ++c)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
+                             ::"r"(ring + sv * S::STAGE + ((b1 - 1 - b0) % TC_KB) * S::BLOCK + block_off<D>(r, c)), "r"(0) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          next();
+          if (more && !(ok = landed())) break;
+          const u64 dv = dv0 + sv * (S::STAGE / 16);
+          dk = dk0 + st * (S::STAGE / 16);
+#pragma unroll
+          for (u32 i = 0; i < 2; ++i)
+            if (i == 0 || two) {
+              const u32 phase = seen_p[i]++ & 1;
+#pragma unroll
+              for (u32 part = 0; part < TC_PARTS; ++part) {
+                ok = ok && tc_wait1(pready + (i * TC_PARTS + part) * 8, phase, lost);
+                if (!ok) break;
+                tc_after();
+#pragma unroll
+                for (u32 k = part * (TC_KB / TC_PARTS); k < (part + 1) * (TC_KB / TC_PARTS); ++k)
+                  tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, dv + k * (D * 32 / 16), id_o, s > 0 || k > 0);
+              }
+              if (!ok) break;
+              if (more) product_s(i, dk);
+              else tc_commit(sready + i * 8);    // the finished sums
+            }
+          if (!ok) break;
+          tc_commit(empty + sv * 8);
+          if (more) { tc_commit(empty + st * 8); next(); }
         }
-        if (ok && leader) {
-          tc_commit(empty + (iv % S::STAGES) * 8);
-          if (s + 1 < n) tc_commit(empty + (ik % S::STAGES) * 8);
-        }
-        __syncwarp();
+        if (!ok) break;
       }
-      it += 2 * n;
+      // all products and their arrivals are done before the CTA ends
+      tc_commit(drain);
+      bar_wait(drain, 0);
     }
-    // all products and their arrivals are done before the CTA ends
-    if (leader) tc_commit(drain);
     __syncwarp();
-    bar_wait(drain, 0);
   } else {
     // ---- one thread per row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
@@ -1141,25 +1184,28 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         if (!(ok = tc_wait(sready + i * 8, seen++ & 1, lost))) break;
         tc_after();
         u32 x[128];
+        float *const v = reinterpret_cast<float *>(x);
 #pragma unroll
         for (u32 c = 0; c < 4; ++c) tc_ld32(x + 32 * c, ts + 32 * c);
         tc_wait_ld();
-        float *const v = reinterpret_cast<float *>(x);
         const u32 key0 = (j.b0 + s * TC_KB) * BT;
         if (key0 < j.all_lo || key0 + TC_KEYS > j.all_hi) {
           const int from = (int)lo - (int)key0, to_ = (int)hi - (int)key0;
 #pragma unroll
           for (int c = 0; c < 128; ++c) if (c < from || c >= to_) v[c] = -INFINITY;
         }
-        float top[4] = {v[0], v[1], v[2], v[3]};
+        // maxima let a NaN through: the row is to become NaN, whichever way its powers are made
+        float top[4] = {max3nan(v[0], v[1], v[2]), max3nan(v[3], v[4], v[5]), max3nan(v[6], v[7], v[8]), max3nan(v[9], v[10], v[11])};
 #pragma unroll
-        for (u32 c = 4; c < 128; c += 4)
+        for (u32 c = 12; c < 124; c += 8)
 #pragma unroll
-          for (u32 y = 0; y < 4; ++y) top[y] = fmaxf(top[y], v[c + y]);
-        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+          for (u32 y = 0; y < 4; ++y) top[y] = max3nan(top[y], v[c + 2 * y], v[c + 2 * y + 1]);
+        const float now = maxnan(max3nan(max3nan(top[0], v[124], v[125]), max3nan(top[1], v[126], v[127]), top[2]), top[3]) * a.scale_log2;
         // The sums stay relative to an old maximum until a score passes it by 2^8 (as in the kernel for few rows)
-        if (__any_sync(~0u, now > m + 8.0f)) {
-          const float next = fmaxf(m, now), f = next == -INFINITY ? 1.0f : ex2(m - next);
+        if (__any_sync(~0u, !(now <= m + 8.0f))) {
+          float next = maxnan(m, now);
+          if (next == INFINITY) next = __int_as_float(0x7FC00000);     // Inf - Inf
+          const float f = next == -INFINITY ? 1.0f : ex2(m - next);
           m = next; l *= f;
           if (s > 0) {                   // the product before S of these keys has been waited for: O is at rest
 #pragma unroll
@@ -1174,23 +1220,35 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
           }
         }
         const float ref = m == -INFINITY ? 0.0f : m;
-        float sum[4] = {0, 0, 0, 0};
+        const u64 scale2 = pack2(a.scale_log2, a.scale_log2), ref2 = pack2(-ref, -ref);
+        u64 sum[2] = {0, 0};
 #pragma unroll
         for (u32 b = 0; b < 4; ++b) {
           u32 p[16];
 #pragma unroll
           for (u32 c = 0; c < 16; ++c) {
-            const float p0 = ex2(fmaf(v[32 * b + 2 * c], a.scale_log2, -ref)), p1 = ex2(fmaf(v[32 * b + 2 * c + 1], a.scale_log2, -ref));
-            sum[c % 4] += p0 + p1;
-            p[c] = Elem<T>::down(p0, p1);
+            const u64 y = fma2(pack2(v[32 * b + 2 * c], v[32 * b + 2 * c + 1]), scale2, ref2);
+            float2 e;
+            if (c % 4 >= 4 - POLY_OF_4) e = exp2_poly(y);
+            else { const float2 z = unpack2(y); e = make_float2(ex2(z.x), ex2(z.y)); }
+            sum[c % 2] = add2(sum[c % 2], pack2(e.x, e.y));
+            p[c] = Elem<T>::down(e.x, e.y);
+          }
+          // the store of the part before this one has had this part's powers to finish
+          if (b && b % (4 / TC_PARTS) == 0) {
+            tc_wait_st();
+            tc_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(pready + (i * TC_PARTS + b / (4 / TC_PARTS) - 1) * 8);
           }
           tc_st16(ts + 16 * b, p);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const float2 add = unpack2(add2(sum[0], sum[1]));
+        l += add.x + add.y;
         tc_wait_st();
         tc_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(pready + i * 8);
+        if (lane == 0) bar_arrive(pready + (i * TC_PARTS + TC_PARTS - 1) * 8);
       }
       // ---- results
       if (ok && n) { ok = tc_wait(sready + i * 8, seen++ & 1, lost); tc_after(); }

@@ -136,11 +136,108 @@ __global__ void __launch_bounds__(128) k_append_any(AppendArgs a) {
   }
 }
 
+// 16-byte accesses: head_dim and rot_dim multiples of 16, strides of 8 elements, aligned addresses. Memory-bound: q, k and v are
+// read once and written once. Work item: 16 elements (two vectors) of a head; with pairs (j, j + rot/2) a rotated item is
+// 8 elements from either half, with neighbouring pairs 16 in a row. All loads of a thread's UNROLL items are in flight
+// before the token's sines are waited for.
+template <class T, u32 THREADS, u32 UNROLL>
+__global__ void __launch_bounds__(THREADS) k_append_vec(AppendArgs a) {
+  extern __shared__ float2 cs[];
+  const u32 t = blockIdx.x, tid = threadIdx.x;
+  const u32 D = a.p.head_dim, H = a.p.n_kv_heads, half = a.rot_dim / 2;
+  const u32 per = D / 16, rot_items = a.rot_dim / 16, n_q = a.n_q_heads * per, n_k = H * per, n = n_q + 2 * n_k;
+  struct Item { const u16 *src; u32 lo, hi, pair; };     // first vector at src + lo, second at src + hi; pair: first pair, or none
+  auto item = [&](u32 i) {
+    Item x;
+    const u32 what = i < n_q ? 0 : i < n_q + n_k ? 1 : 2;
+    const u32 k = what == 0 ? i : what == 1 ? i - n_q : i - n_q - n_k, h = k / per, c = k - h * per;
+    x.src = what == 0 ? (const u16 *)a.q + t * a.q_ts + h * a.q_hs : what == 1 ? (const u16 *)a.k + t * a.k_ts + h * a.k_hs
+                                                                              : (const u16 *)a.v + t * a.v_ts + h * a.v_hs;
+    const bool turn = what < 2 && c < rot_items;
+    x.pair = turn ? 8 * c : 0xFFFFFFFFu;
+    x.lo = turn && !a.interleaved ? 8 * c : 16 * c;
+    x.hi = turn && !a.interleaved ? 8 * c + half : 16 * c + 8;
+    return x;
+  };
+  uint4 in[UNROLL][2];
+  const bool inside = t < a.b.q_start[a.b.n_seqs];       // else behind the last sequence: loads nothing, finds nothing below
+#pragma unroll
+  for (u32 y = 0; y < UNROLL; ++y) {
+    const u32 i = tid + y * THREADS;
+    if (inside && i < n) { const Item x = item(i); in[y][0] = __ldcs((const uint4 *)(x.src + x.lo)); in[y][1] = __ldcs((const uint4 *)(x.src + x.hi)); }
+  }
+  const Where w = find_token(a.b, t, a.err);
+  if (w.seq >= a.b.n_seqs) return;
+  u16 *kd = nullptr, *vd = nullptr;
+  if (w.ok) {
+    const u32 slot = a.b.table[w.seq * a.b.table_stride + w.index / BT];
+    kd = (u16 *)slot_ptr(a.p, a.p.k, slot);
+    vd = (u16 *)slot_ptr(a.p, a.p.v, slot);
+    if (!kd) { if (tid == 0) kv_err(a.err, KVERR_RANGE); }
+    else { const u64 off = (u64)(w.index % BT) * H * D; kd += off; vd += off; }
+  }
+  for (u32 j = tid; j < half; j += THREADS) cs[j] = pair_angle(a, t, w.index, j);
+  __syncthreads();
+  auto finish = [&](u32 i, uint4 v0, uint4 v1) {
+    const Item x = item(i);
+    u32 r0[4] = {v0.x, v0.y, v0.z, v0.w}, r1[4] = {v1.x, v1.y, v1.z, v1.w};
+    if (x.pair != 0xFFFFFFFFu) {
+      const float4 *f = (const float4 *)(cs + x.pair);   // two pairs' (cosine, sine)
+      if (a.interleaved) {
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) {
+          const float4 g = f[y];
+          u32 &p = y < 2 ? r0[2 * y] : r1[2 * y - 4], &q = y < 2 ? r0[2 * y + 1] : r1[2 * y - 3];
+          const float2 e = Elem<T>::up(p), o = Elem<T>::up(q);
+          p = Elem<T>::down(e.x * g.x - e.y * g.y, e.y * g.x + e.x * g.y);
+          q = Elem<T>::down(o.x * g.z - o.y * g.w, o.y * g.z + o.x * g.w);
+        }
+      } else {
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) {
+          const float4 g = f[y];
+          const float2 e = Elem<T>::up(r0[y]), o = Elem<T>::up(r1[y]);
+          r0[y] = Elem<T>::down(e.x * g.x - o.x * g.y, e.y * g.z - o.y * g.w);
+          r1[y] = Elem<T>::down(o.x * g.x + e.x * g.y, o.y * g.z + e.y * g.w);
+        }
+      }
+    }
+    u16 *d;
+    if (i < n_q) d = (u16 *)a.q_out + t * a.qo_ts + (i / per) * a.qo_hs;
+    else if (i < n_q + n_k) d = kd + (i - n_q) / per * D;
+    else d = vd + (i - n_q - n_k) / per * D;
+    if (i >= n_q && !kd) return;
+    *(uint4 *)(d + x.lo) = make_uint4(r0[0], r0[1], r0[2], r0[3]);
+    *(uint4 *)(d + x.hi) = make_uint4(r1[0], r1[1], r1[2], r1[3]);
+  };
+#pragma unroll
+  for (u32 y = 0; y < UNROLL; ++y) if (tid + y * THREADS < n) finish(tid + y * THREADS, in[y][0], in[y][1]);
+  for (u32 i = tid + UNROLL * THREADS; i < n; i += THREADS) {
+    const Item x = item(i);
+    const uint4 v0 = __ldcs((const uint4 *)(x.src + x.lo)), v1 = __ldcs((const uint4 *)(x.src + x.hi));
+    finish(i, v0, v1);
+  }
+}
+
+template <u32 THREADS, u32 UNROLL>
+static void append_vec(const AppendArgs &a, u32 smem, cudaStream_t s) {
+  if (a.fp16) k_append_vec<__half, THREADS, UNROLL><<<a.b.n_tokens, THREADS, smem, s>>>(a);
+  else k_append_vec<__nv_bfloat16, THREADS, UNROLL><<<a.b.n_tokens, THREADS, smem, s>>>(a);
+}
+
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, u32 *launches) {
   const u32 smem = a.rot_dim / 2 * sizeof(float2);
+  ++*launches;
+  const u64 strides = a.k_ts | a.k_hs | a.v_ts | a.v_hs | (a.n_q_heads ? a.q_ts | a.q_hs | a.qo_ts | a.qo_hs : 0);
+  const uintptr_t bases = (uintptr_t)a.k | (uintptr_t)a.v | (a.n_q_heads ? (uintptr_t)a.q | (uintptr_t)a.q_out : 0);
+  if (!(a.p.head_dim % 16 || a.rot_dim % 16 || strides % 8 || bases % 16)) {
+    const u64 items = ((u64)a.n_q_heads + 2 * a.p.n_kv_heads) * (a.p.head_dim / 16);
+    if (items <= 384) append_vec<128, 3>(a, smem, s);
+    else append_vec<256, 4>(a, smem, s);
+    return cudaGetLastError();
+  }
   if (a.fp16) k_append_any<__half><<<a.b.n_tokens, 128, smem, s>>>(a);
   else k_append_any<__nv_bfloat16><<<a.b.n_tokens, 128, smem, s>>>(a);
-  ++*launches;
   return cudaGetLastError();
 }
 
@@ -859,24 +956,7 @@ __device__ __forceinline__ u64 pack2(float a, float b) { u64 r; asm("mov.b64 %0,
 __device__ __forceinline__ float2 unpack2(u64 x) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x)); return r; }
 __device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ float max3nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
-__device__ __forceinline__ float maxnan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-// 2^x on the FMA pipes, for x <= 127: x = n + f with n the nearest whole number, 2^f by a polynomial of degree 4 that is 1 at
-// 0 (coefficients from a least-squares fit of the relative error on [-1/2, 1/2], reweighted until its ripples are equal: off
-// by 2.9e-6 of the value at most), n added to the exponent. -127 and anything below give 0. The special-function unit makes 16 powers per cycle and SM, as long as the
-// tensor cores take for the products around them; a quarter of the powers made here evens that out.
-__device__ __forceinline__ float2 exp2_poly(u64 y) {
-  constexpr float MAGIC = 12582912.0f;   // 1.5 * 2^23: added, it leaves the whole part in the low bits
-  const float2 v = unpack2(y);
-  y = pack2(maxnan(v.x, -127.0f), maxnan(v.y, -127.0f));
-  const u64 t = add2(y, pack2(MAGIC, MAGIC)), f = fma2(add2(t, pack2(-MAGIC, -MAGIC)), pack2(-1.0f, -1.0f), y);
-  u64 p = fma2(f, pack2(0.009582818485796452f, 0.009582818485796452f), pack2(0.05590637028217316f, 0.05590637028217316f));
-  p = fma2(p, f, pack2(0.24024099111557007f, 0.24024099111557007f));
-  p = fma2(p, f, pack2(0.6931241750717163f, 0.6931241750717163f));
-  p = fma2(p, f, pack2(1.0f, 1.0f));
-  const float2 q = unpack2(p), n = unpack2(t);
-  return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(q.y) + (__float_as_int(n.y) << 23)));
-}
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
 // A wait that also ends when another warp of the CTA has given up; gives up itself after WAIT_NS.
 __device__ __forceinline__ bool tc_wait_slow(u32 bar, u32 parity, volatile u32 *lost) {
@@ -902,8 +982,7 @@ struct Job {
   u32 b0, b1, all_lo, all_hi;// blocks of keys [b0, b1); keys every row sees
   u32 part, direct, last;    // place of the partial result, or the whole result at once; last: no job, the end
 };
-constexpr u32 TC_JOBS = 4, TC_PARTS = 4;      // P is handed to the second product in so many parts
-constexpr u32 POLY_OF_4 = 1;                   // of four pairs of powers, so many are made by exp2_poly
+constexpr u32 TC_JOBS = 4, TC_PARTS = 2;      // P is handed to the second product in so many parts
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
@@ -1194,18 +1273,15 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
 #pragma unroll
           for (int c = 0; c < 128; ++c) if (c < from || c >= to_) v[c] = -INFINITY;
         }
-        // maxima let a NaN through: the row is to become NaN, whichever way its powers are made
-        float top[4] = {max3nan(v[0], v[1], v[2]), max3nan(v[3], v[4], v[5]), max3nan(v[6], v[7], v[8]), max3nan(v[9], v[10], v[11])};
+        float top[4] = {max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[8]), max3(v[9], v[10], v[11])};
 #pragma unroll
         for (u32 c = 12; c < 124; c += 8)
 #pragma unroll
-          for (u32 y = 0; y < 4; ++y) top[y] = max3nan(top[y], v[c + 2 * y], v[c + 2 * y + 1]);
-        const float now = maxnan(max3nan(max3nan(top[0], v[124], v[125]), max3nan(top[1], v[126], v[127]), top[2]), top[3]) * a.scale_log2;
+          for (u32 y = 0; y < 4; ++y) top[y] = max3(top[y], v[c + 2 * y], v[c + 2 * y + 1]);
+        const float now = fmaxf(max3(max3(top[0], v[124], v[125]), max3(top[1], v[126], v[127]), top[2]), top[3]) * a.scale_log2;
         // The sums stay relative to an old maximum until a score passes it by 2^8 (as in the kernel for few rows)
-        if (__any_sync(~0u, !(now <= m + 8.0f))) {
-          float next = maxnan(m, now);
-          if (next == INFINITY) next = __int_as_float(0x7FC00000);     // Inf - Inf
-          const float f = next == -INFINITY ? 1.0f : ex2(m - next);
+        if (__any_sync(~0u, now > m + 8.0f)) {
+          const float next = fmaxf(m, now), f = next == -INFINITY ? 1.0f : ex2(m - next);
           m = next; l *= f;
           if (s > 0) {                   // the product before S of these keys has been waited for: O is at rest
 #pragma unroll
@@ -1228,14 +1304,12 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
 #pragma unroll
           for (u32 c = 0; c < 16; ++c) {
             const u64 y = fma2(pack2(v[32 * b + 2 * c], v[32 * b + 2 * c + 1]), scale2, ref2);
-            float2 e;
-            if (c % 4 >= 4 - POLY_OF_4) e = exp2_poly(y);
-            else { const float2 z = unpack2(y); e = make_float2(ex2(z.x), ex2(z.y)); }
-            sum[c % 2] = add2(sum[c % 2], pack2(e.x, e.y));
-            p[c] = Elem<T>::down(e.x, e.y);
+            const float2 z = unpack2(y);
+            const float p0 = ex2(z.x), p1 = ex2(z.y);
+            sum[c % 2] = add2(sum[c % 2], pack2(p0, p1));
+            p[c] = Elem<T>::down(p0, p1);
           }
-          // the store of the part before this one has had this part's powers to finish
-          if (b && b % (4 / TC_PARTS) == 0) {
+          if (b && b % (4 / TC_PARTS) == 0) {    // the store of the part before has had these powers to finish
             tc_wait_st();
             tc_before();
             __syncwarp();

@@ -501,92 +501,102 @@ __device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publi
   return true;
 }
 
-// Kind 2: tiles are cut into pieces of equal length, as many as make the rounds of one piece per SM end soonest: of the
-// longest sequence cut into 1 .. MAX_CUTS pieces (and the others into pieces no longer), the one with the smallest
-// rounds * (piece + what a piece costs besides), among those that leave at most `most` partial results. Returns the length
-// of a piece in blocks.
-constexpr u32 MAX_CUTS = 32, PIECE_COST = 24, MIN_PIECE = 64;
-template <u32 THREADS>
-__device__ u32 choose_piece(const AttendArgs &a, u32 rows, u32 most, u32 sms) {
-  __shared__ u32 s_longest, s_items[MAX_CUTS], s_parts[MAX_CUTS], s_piece;
-  const u32 lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) s_longest = 1;
-  if (threadIdx.x < MAX_CUTS) s_items[threadIdx.x] = s_parts[threadIdx.x] = 0;
-  __syncthreads();
-  u32 mine = 0;
-  for (u32 s = threadIdx.x; s < a.b.n_seqs; s += THREADS) {
-    const Seq q = load_seq(a.b, s, a.err);
-    if (q.n) mine = max(mine, seq_blocks(a, q, rows));
-  }
-  if (mine) atomicMax(&s_longest, mine);
-  __syncthreads();
-  const u32 longest = s_longest;
-  if (longest <= MIN_PIECE || !most) return longest;
-  const u32 piece = max(MIN_PIECE, ((longest + lane) / (lane + 1) + 7) / 8 * 8);     // lane: one candidate each; whole stages
-  u32 items = 0, parts = 0;
-  for (u32 s = threadIdx.x / 32; s < a.b.n_seqs; s += THREADS / 32) {
-    const Seq q = load_seq(a.b, s, a.err);
-    const u32 tiles = seq_tiles(a, q, rows), n = (seq_blocks(a, q, rows) + piece - 1) / piece;
-    items += tiles * n;
-    if (n > 1) parts += tiles * n;
-  }
-  if (items) { atomicAdd(&s_items[lane], items); atomicAdd(&s_parts[lane], parts); }
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    u64 cost = ((u64)s_items[lane] * a.p.n_kv_heads + sms - 1) / sms * (piece + PIECE_COST);
-    if ((u64)s_parts[lane] * a.p.n_kv_heads > most && lane) cost = ~0ull >> 8;
-    cost = cost << 8 | lane;
+// Kind 2: tiles are cut into pieces, of at most so many blocks. With n pieces in all, the longest of them of p blocks, the
+// kernel ends after about the lesser of
+//   rounds of one piece per SM, ceil(n / SMs) * (p + c)               (all pieces alike)
+//   the SMs' mean share and one more piece, (blocks + n c) / SMs + p + c   (pieces of all lengths)
+// with c = PIECE_COST blocks for what a piece costs besides, and joining costs JOIN_COST blocks and a quarter of one per
+// partial result. Tried for the longest sequence cut into CUTS[] pieces, and the others into pieces no longer; `most` bounds
+// the partial results. For more than 32 sequences the search would take longer than it gains: pieces of half the mean share.
+// Every warp takes part with the candidates warp, warp + warps, ...; lane: one of the first 32 sequences.
+constexpr u32 PIECE_COST = 16, JOIN_COST = 24, MIN_PIECE = 16, N_CUTS = 16;
+__constant__ const u8 CUTS[N_CUTS] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
+__device__ __forceinline__ u32 cut_length(u32 longest, u32 cuts) { return max(MIN_PIECE, ((longest + cuts - 1) / cuts + 7) / 8 * 8); }   // whole stages
+__device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
-    for (u32 o = 16; o; o /= 2) { const u64 y = __shfl_xor_sync(~0u, cost, o); cost = y < cost ? y : cost; }
-    const u32 best = __shfl_sync(~0u, piece, (u32)(cost & 31));
-    if (lane == 0) s_piece = (cost & 31) ? best : longest;
+  for (u32 o = 16; o; o /= 2) x += __shfl_xor_sync(~0u, x, o);
+  return x;
+}
+struct Cut { u32 longest; float share; };
+__device__ __forceinline__ Cut weigh_cuts(const AttendArgs &a, u32 rows, u32 most, u32 sms, u32 warp, u32 warps, float *s_cost, Seq &q) {
+  const u32 lane = threadIdx.x & 31;
+  const float H = a.p.n_kv_heads;
+  u32 longest = 1, tiles = 0, nb = 0;
+  float blocks = 0.0f;
+  q = Seq{0, 0, 0};
+  for (u32 s = lane; s < a.b.n_seqs; s += 32) {
+    const Seq x = load_seq(a.b, s, a.err);
+    if (s == lane) q = x;
+    if (!x.n) continue;
+    tiles = seq_tiles(a, x, rows); nb = seq_blocks(a, x, rows);
+    blocks += (float)tiles * nb;
+    longest = max(longest, nb);
   }
-  __syncthreads();
-  return s_piece;
+  Cut c;
+  c.longest = __reduce_max_sync(~0u, longest);
+  c.share = warp_sum(blocks) * H / sms;
+  if (c.longest <= MIN_PIECE || !most || a.b.n_seqs > 32) return c;
+  for (u32 k = warp; k < N_CUTS; k += warps) {
+    const u32 piece = k ? cut_length(c.longest, CUTS[k]) : c.longest;
+    const u32 mine = tiles * ((nb + piece - 1) / piece);
+    const float n = __reduce_add_sync(~0u, mine) * H, parts = __reduce_add_sync(~0u, nb > piece ? mine : 0) * H;
+    float cost = fminf(ceilf(n / sms) * (piece + PIECE_COST), c.share + n * PIECE_COST / sms + piece + PIECE_COST);
+    if (parts > 0.0f) cost += JOIN_COST + parts * 0.25f;
+    if (lane == 0) s_cost[k] = k && parts > most ? INFINITY : cost;
+  }
+  return c;
+}
+// The length of a piece; the scheduling warp asks, behind a barrier.
+__device__ __forceinline__ u32 choose_cut(const AttendArgs &a, u32 most, const Cut &c, const float *s_cost) {
+  if (c.longest <= MIN_PIECE || !most) return c.longest;
+  if (a.b.n_seqs > 32) return (u32)fminf((float)c.longest, fmaxf((float)MIN_PIECE, ceilf((c.share / 2 + 1) / 8) * 8));
+  const u32 lane = threadIdx.x & 31, cost = lane < N_CUTS ? __float_as_uint(s_cost[lane]) : ~0u;      // positive: ordered as integers
+  const u32 k = __ffs(__ballot_sync(~0u, cost == __reduce_min_sync(~0u, cost))) - 1;
+  return k ? cut_length(c.longest, CUTS[k]) : c.longest;
 }
 
-// Joins the parts of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. Rows of units that were not cut are already
-// written. Launched behind the kernel that leaves the parts, waits for all of it. Kind 1: few rows of many parts, a CTA
-// takes one row and a warp every fourth part of it; kind 2: many rows of few parts, a warp per row.
-template <class T, u32 D, u32 KIND>
-__global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u32 n_parts) {
-  constexpr u32 WPR = KIND == 1 ? 4 : 1, C = D / 32;      // warps per row; columns per lane
+// Joining the parts of a row: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i. Rows of units that were not cut are already
+// written. Launched behind the kernel that leaves the parts, waits for all of it.
+// The sequence a token lies in; ~0 for none. A whole warp asks.
+__device__ __forceinline__ u32 seq_of_token(const KvBatch &b, u32 t) {
+  const u32 lane = threadIdx.x & 31;
+  for (u32 s0 = 0; s0 < b.n_seqs; s0 += 32) {
+    const u32 s = s0 + lane;
+    const u32 hit = __ballot_sync(~0u, s < b.n_seqs && b.q_start[s] <= t && t < b.q_start[s + 1]);
+    if (hit) return s0 + __ffs(hit) - 1;
+  }
+  return ~0u;
+}
+template <u32 C> __device__ __forceinline__ void load_sums(float (&v)[C], const float *p) {
+  if (C == 4) *(float4 *)v = *(const float4 *)p; else *(float2 *)v = *(const float2 *)p;
+}
+
+// Kind 1, few rows of many parts: a CTA per row, a warp takes every fourth part.
+template <class T, u32 D>
+__global__ void __launch_bounds__(128) k_attend_join_split(AttendArgs a, u32 n_parts) {
+  constexpr u32 C = D / 32, ROWS = 16;   // columns per lane; rows of a tile
   __shared__ float s_acc[4][D], s_l[4];
-  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.p.n_kv_heads, sub = warp % WPR;
-  u32 head = 0;
-  bool waited = false;
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.p.n_kv_heads;
   const float *sums = scratch_sums(a);
-  const float2 *ml = (const float2 *)(sums + (u64)n_parts * rows * D);
-  const u64 n_rows = (u64)a.b.n_tokens * a.n_q_heads, step = (u64)gridDim.x * (4 / WPR);
-  for (u64 id = (u64)blockIdx.x * (4 / WPR) + warp / WPR; id < n_rows; id += step) {
-    const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id % a.n_q_heads);
-    u32 seq = 0;                         // the first sequence the token lies in
-    bool found = false;
-    for (u32 s0 = 0; s0 < a.b.n_seqs && !found; s0 += 32) {
-      const u32 s = s0 + lane;
-      const u32 hit = __ballot_sync(~0u, s < a.b.n_seqs && a.b.q_start[s] <= t && t < a.b.q_start[s + 1]);
-      if (hit) { seq = s0 + __ffs(hit) - 1; found = true; }
-    }
-    if (!waited) {                       // the batch's arrays are older than the kernel before this one
+  const float2 *ml = (const float2 *)(sums + (u64)n_parts * ROWS * D);
+  const u64 n_rows = (u64)a.b.n_tokens * a.n_q_heads;
+  u32 per = 0;
+  for (u64 id = blockIdx.x; id < n_rows; id += gridDim.x) {
+    const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id - (u64)t * a.n_q_heads), seq = seq_of_token(a.b, t);
+    const u32 h = hq / a.group;
+    if (!per) {                          // the batch's arrays are older than the kernel before this one
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      waited = true;
-      head = scratch_plan(a)[0].x;
-      if (KIND == 2 && !head) return;
+      per = scratch_plan(a)[0].x;
+      if (!per) return;
     }
-    if (!found) continue;
+    if (seq == ~0u) continue;
     const uint4 plan = scratch_plan(a)[1 + seq];
-    const u32 h = hq / a.group, r = (t - a.b.q_start[seq]) * a.group + hq % a.group, tile = r / rows, row = r % rows;
-    u32 p0, stride, n, odd = 0;          // partial i: p0 + i * stride; the first may lie `odd` further
-    if (KIND == 1) {
-      const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z, e = s + plan.z, c0 = s / head, c1 = (e - 1) / head;
-      p0 = (u32)(2 * c0); stride = 2; n = (u32)(c1 - c0) + 1;
-      odd = s > c0 * head;
-    } else {
-      p0 = (plan.x + tile) * H + h; stride = plan.z * H; n = plan.y;
-    }
+    const u32 r = (t - a.b.q_start[seq]) * a.group + hq - h * a.group, tile = r / ROWS, row = r % ROWS;
+    const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z, e = s + plan.z, c0 = s / per, c1 = (e - 1) / per;
+    const u32 n = (u32)(c1 - c0) + 1, p0 = (u32)(2 * c0), odd = s > c0 * per;
     if (n <= 1) continue;
-    if ((u64)p0 + (u64)(n - 1) * stride >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
-    auto place = [&](u32 i) { return (p0 + i * stride + (i == 0 ? odd : 0)) * rows + row; };     // below n_parts * rows < 2^20
+    if (p0 + 2ull * (n - 1) >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
+    auto place = [&](u32 i) { return (p0 + 2 * i + (i == 0 ? odd : 0)) * ROWS + row; };
     float m = -INFINITY;
     for (u32 i = lane; i < n; i += 32) m = fmaxf(m, ml[place(i)].x);
 #pragma unroll
@@ -596,36 +606,104 @@ __global__ void __launch_bounds__(128) k_attend_join(AttendArgs a, u32 rows, u32
 #pragma unroll
     for (u32 c = 0; c < C; ++c) acc[c] = 0.0f;
 #pragma unroll 8
-    for (u32 i = sub; i < n; i += WPR) {
+    for (u32 i = warp; i < n; i += 4) {
       const u32 at = place(i);
       const float2 x = ml[at];
-      const float *o = sums + (u64)at * D + lane * C;
       float v[C];
-      if (D == 128) *(float4 *)v = *(const float4 *)o; else *(float2 *)v = *(const float2 *)o;
+      load_sums<C>(v, sums + (u64)at * D + lane * C);
       const float w = x.x == -INFINITY ? 0.0f : ex2(x.x - ref);      // a part without keys for this row holds zeros
       l += w * x.y;
 #pragma unroll
       for (u32 c = 0; c < C; ++c) acc[c] += w * v[c];
     }
-    if (WPR > 1) {
-      __syncthreads();                   // the row before this one is read
+    __syncthreads();                     // the row before this one is read
 #pragma unroll
-      for (u32 c = 0; c < C; ++c) s_acc[warp][lane * C + c] = acc[c];
-      if (lane == 0) s_l[warp] = l;
-      __syncthreads();
-      if (sub) continue;
+    for (u32 c = 0; c < C; ++c) s_acc[warp][lane * C + c] = acc[c];
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    if (warp) continue;
 #pragma unroll
-      for (u32 w = 1; w < WPR; ++w) {
-        l += s_l[w];
+    for (u32 w = 1; w < 4; ++w) {
+      l += s_l[w];
 #pragma unroll
-        for (u32 c = 0; c < C; ++c) acc[c] += s_acc[w][lane * C + c];
-      }
+      for (u32 c = 0; c < C; ++c) acc[c] += s_acc[w][lane * C + c];
     }
     const float inv = l > 0.0f ? 1.0f / l : l;
     T *o = (T *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + lane * C;
 #pragma unroll
     for (u32 c = 0; c < C; ++c) o[c] = Elem<T>::down1(acc[c] * inv);
     if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
+  }
+}
+
+// Kind 2, many rows of few parts: a warp takes BATCH heads of a token at a time and keeps their loads in flight together.
+template <class T, u32 D>
+__global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, u32 n_parts) {
+  constexpr u32 C = D / 32, BATCH = 8;
+  const u32 lane = threadIdx.x & 31, H = a.p.n_kv_heads;
+  const float *sums = scratch_sums(a);
+  const float2 *ml = (const float2 *)(sums + (u64)n_parts * rows * D);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!scratch_plan(a)[0].x) return;
+  const u32 groups = (a.n_q_heads + BATCH - 1) / BATCH, warps = gridDim.x * 4;
+  u32 last_t = ~0u, seq = ~0u, start = 0;
+  uint4 plan = make_uint4(0, 0, 0, 0);
+  for (u64 id = blockIdx.x * 4 + (threadIdx.x >> 5); id < (u64)a.b.n_tokens * groups; id += warps) {
+    const u32 t = (u32)(id / groups), hq0 = (u32)(id - (u64)t * groups) * BATCH;
+    if (t != last_t) {
+      last_t = t;
+      seq = seq_of_token(a.b, t);
+      if (seq != ~0u) { plan = scratch_plan(a)[1 + seq]; start = a.b.q_start[seq]; }
+    }
+    const u32 n = plan.y, stride = plan.z * H;
+    if (seq == ~0u || n <= 1) continue;
+    u32 at[BATCH];                       // first partial's row
+    float m[BATCH], l[BATCH], acc[BATCH][C];
+#pragma unroll
+    for (u32 b = 0; b < BATCH; ++b) {
+      const u32 hq = min(hq0 + b, a.n_q_heads - 1), h = hq / a.group, r = (t - start) * a.group + hq - h * a.group, tile = r / rows;
+      const u32 p0 = (plan.x + tile) * H + h;
+      at[b] = (p0 + (u64)(n - 1) * stride < n_parts ? p0 : 0) * rows + r - tile * rows;
+      if (p0 + (u64)(n - 1) * stride >= n_parts && lane == 0) kv_err(a.err, KVERR_RANGE);     // cannot happen
+      m[b] = -INFINITY; l[b] = 0.0f;
+#pragma unroll
+      for (u32 c = 0; c < C; ++c) acc[b][c] = 0.0f;
+    }
+    for (u32 i = 0; i < n; ++i) {
+      float2 x[BATCH];
+      float v[BATCH][C];
+#pragma unroll
+      for (u32 b = 0; b < BATCH; ++b) {
+        const u32 p = at[b] + i * stride * rows;
+        x[b] = ml[p];
+        load_sums<C>(v[b], sums + (u64)p * D + lane * C);
+      }
+#pragma unroll
+      for (u32 b = 0; b < BATCH; ++b) {
+        const float now = fmaxf(m[b], x[b].x), ref = now == -INFINITY ? 0.0f : now, f = ex2(m[b] - ref);
+        const float w = ex2(x[b].x - ref);             // a part without keys for this row holds zeros, weight 2^-inf
+        m[b] = now;
+        l[b] = l[b] * f + w * x[b].y;
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) acc[b][c] = acc[b][c] * f + w * v[b][c];
+      }
+    }
+#pragma unroll
+    for (u32 b = 0; b < BATCH; ++b) {
+      const u32 hq = hq0 + b;
+      if (hq >= a.n_q_heads) break;
+      const float inv = l[b] > 0.0f ? 1.0f / l[b] : l[b];
+      u16 *o = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + lane * C;
+      u32 e[C / 2];
+#pragma unroll
+      for (u32 c = 0; c < C / 2; ++c) e[c] = Elem<T>::down(acc[b][2 * c] * inv, acc[b][2 * c + 1] * inv);
+      if (C == 4 && ((uintptr_t)o & 7) == 0) *(uint2 *)o = make_uint2(e[0], e[C / 2 - 1]);
+      else {
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) o[c] = (u16)(e[c / 2] >> (16 * (c % 2)));
+      }
+      if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m[b] + log2f(l[b])) * 0.69314718055994531f;
+    }
   }
 }
 
@@ -675,6 +753,7 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
   u64 x, x_end, base;
   u32 per, seq;
   if (!find_stretch<SPLIT_THREADS>(a, SPLIT_ROWS, gridDim.x, n_parts && blockIdx.x == 0, x, x_end, per, seq, base)) return;
@@ -986,7 +1065,7 @@ constexpr u32 TC_JOBS = 4, TC_PARTS = 2;      // P is handed to the second produ
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
-k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 most_parts, u32 n_parts) {
+k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts) {
   typedef TcShape<D> S;
   constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
   extern __shared__ u8 smem_raw[];
@@ -994,6 +1073,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   __shared__ u32 s_tmem;
   __shared__ volatile u32 s_lost;
   __shared__ Job s_job[TC_JOBS];
+  __shared__ float s_cost[N_CUTS];
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
   const u32 full = smem_addr(s_full), empty = smem_addr(s_empty), sready = smem_addr(s_sready), pready = smem_addr(s_pready),
@@ -1012,7 +1092,9 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
-  const u32 piece = choose_piece<TC_THREADS>(a, TC_ROWS, most_parts, gridDim.x);
+  if (warp == 9 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &maps.tail : &maps.pool) : "memory");
+  Seq mine;                              // the sequence of this lane among the first 32
+  const Cut cut = weigh_cuts(a, TC_ROWS, n_parts, gridDim.x, warp, TC_THREADS / 32, s_cost, mine);
   tc_before();
   __syncthreads();
   tc_after();
@@ -1039,25 +1121,26 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     // a causal prompt even out. Jobs of a sequence: piece, tile (last tokens first), KV head; those that run at the same
     // time then mostly read the same keys.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    u64 base = 0;                        // first job and first partial of the 32 sequences in hand
-    u32 part0 = 0, s0 = 0;
-    Seq q{0, 0, 0};
+    const u32 piece = choose_cut(a, n_parts, cut, s_cost);
+    // (a launch has fewer than 2^32 jobs: tokens times query heads and a few thousand pieces)
+    u32 base = 0, part0 = 0, s0 = 0;     // first job and first partial of the 32 sequences in hand
+    Seq q = mine;
     u32 tiles = 0, pieces = 0;
-    u64 my_jobs = 0, at = 0, all = 0; u32 my_part = 0, all_parts = 0;
+    u32 my_jobs = 0, at = 0, all = 0, my_part = 0, all_parts = 0;
     auto take = [&]() {                  // lane: one of the sequences s0 .. s0 + 31
       const u32 s = s0 + lane;
       tiles = pieces = 0;
       if (s < a.b.n_seqs) {
-        q = load_seq(a.b, s, a.err);
+        if (s0) q = load_seq(a.b, s, a.err);
         tiles = seq_tiles(a, q, TC_ROWS);
         pieces = (seq_blocks(a, q, TC_ROWS) + piece - 1) / piece;
       }
-      my_jobs = (u64)tiles * pieces * H;
+      my_jobs = tiles * pieces * H;
       const u32 parts = pieces > 1 ? tiles * pieces : 0;
-      u64 incl = my_jobs; u32 pincl = parts;
+      u32 incl = my_jobs, pincl = parts;
 #pragma unroll
       for (u32 o = 1; o < 32; o *= 2) {
-        const u64 y = __shfl_up_sync(~0u, incl, o); const u32 z = __shfl_up_sync(~0u, pincl, o);
+        const u32 y = __shfl_up_sync(~0u, incl, o), z = __shfl_up_sync(~0u, pincl, o);
         if (lane >= o) { incl += y; pincl += z; }
       }
       at = base + incl - my_jobs; my_part = part0 + pincl - parts;
@@ -1071,16 +1154,14 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     take();
     bool ok = true;
     for (u32 k = 0;; ++k) {
-      const u64 want = (u64)k * gridDim.x + (k % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      const u32 want = k * gridDim.x + (k % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
       while (want >= base + all && s0 + 32 < a.b.n_seqs) { base += all; part0 += all_parts; s0 += 32; take(); }
       const u32 hit = __ballot_sync(~0u, want >= at && want < at + my_jobs);
       const u32 slot = k % TC_JOBS;
       if (k >= TC_JOBS && !(ok = tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost))) break;
       if (hit && lane == __ffs(hit) - 1) {
         Job j;
-        u64 i = want - at;
-        const u32 h = (u32)(i % H); i /= H;
-        const u32 tile = tiles - 1 - (u32)(i % tiles), pc = (u32)(i / tiles);
+        const u32 x = want - at, y = x / H, h = x - y * H, pc = y / tiles, tile = tiles - 1 - (y - pc * tiles);
         j.t0 = q.t0; j.kv = q.kv; j.seq = s0 + lane; j.h = h; j.shift = q.kv - q.n;
         j.r0 = tile * TC_ROWS; j.r1 = min(j.r0 + TC_ROWS, q.n * a.group) - 1;
         u32 first, last;                 // keys any row sees
@@ -1237,21 +1318,34 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         hi = a.full ? j.kv : own < 0 ? 0u : (u32)own + 1;
         lo = a.window && hi > a.window ? hi - a.window : 0u;
       }
+      // Place of 16 bytes (c) of a row in the Q tile. A warp's 32 rows there are its own: loaded and, once the last S is made,
+      // used to bring the results into whole rows. Lanes take 16 bytes each of as many rows as make 512 bytes.
+      auto q_place = [&](u32 row, u32 c) { return sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + row * 128 + (((c % 8) ^ (row % 8)) * 16); };
+      const u32 row0 = warp % 4 * 32;
       if (n) {
-        const u16 *src = (const u16 *)a.q + (u64)t * a.q_ts + (u64)hq * a.q_hs;
-        const bool wide = ((uintptr_t)src & 15) == 0;
+        const u16 *const src = (const u16 *)a.q + (u64)t * a.q_ts + (u64)hq * a.q_hs;
+        const bool wide = __all_sync(~0u, ((uintptr_t)src & 15) == 0);
 #pragma unroll
-        for (u32 c = 0; c < D / 8; ++c) {
-          uint4 v;
-          if (wide) v = *(const uint4 *)(src + c * 8);
-          else {
-            u32 x[4];
+        for (u32 k0 = 0; k0 < D / 8; k0 += 8) {
+          uint4 v[8];
 #pragma unroll
-            for (u32 y = 0; y < 4; ++y) x[y] = (u32)src[c * 8 + 2 * y] | (u32)src[c * 8 + 2 * y + 1] << 16;
-            v = make_uint4(x[0], x[1], x[2], x[3]);
+          for (u32 k = 0; k < 8; ++k) {
+            const u32 at = (k0 + k) * 32 + lane, c = at % (D / 8);
+            const u16 *from = (const u16 *)__shfl_sync(~0u, (u64)src, at / (D / 8)) + c * 8;
+            if (wide) v[k] = *(const uint4 *)from;
+            else {
+              u32 x[4];
+#pragma unroll
+              for (u32 y = 0; y < 4; ++y) x[y] = (u32)from[2 * y] | (u32)from[2 * y + 1] << 16;
+              v[k] = make_uint4(x[0], x[1], x[2], x[3]);
+            }
           }
-          const u32 dst = sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + rt * 128 + (((c % 8) ^ (rt % 8)) * 16);
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+#pragma unroll
+          for (u32 k = 0; k < 8; ++k) {
+            const u32 at = (k0 + k) * 32 + lane;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(q_place(row0 + at / (D / 8), at % (D / 8))), "r"(v[k].x), "r"(v[k].y), "r"(v[k].z), "r"(v[k].w) : "memory");
+          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_before();
@@ -1328,33 +1422,49 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       if (ok && n) { ok = tc_wait(sready + i * 8, seen++ & 1, lost); tc_after(); }
       if (!ok) break;
       const float inv = !j.direct ? 1.0f : l > 0.0f ? 1.0f / l : l;
-      u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
-      const bool wide = ((uintptr_t)out & 15) == 0;
       const u32 prow = i * TC_TILE + rt;
-      float *const sums = scratch_sums(a) + ((u64)j.part * TC_ROWS + prow) * D;
-#pragma unroll
-      for (u32 c = 0; c < D / 32; ++c) {
-        u32 y[32];
+      u8 *const row_out = j.direct ? (u8 *)((u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs)
+                                   : (u8 *)(scratch_sums(a) + ((u64)j.part * TC_ROWS + prow) * D);
+      const bool wide = __all_sync(~0u, ((uintptr_t)row_out & 15) == 0);
+      const u32 n_here = min(j.r1 - j.r0 + 1 - i * TC_TILE, TC_TILE);       // rows of this tile
+      // 2 * head_dim bytes per row and round: the whole result, or half of a partial one
+      for (u32 round = 0; round < (j.direct ? 1 : 2); ++round) {
         __syncwarp();
-        if (n) { tc_ld32(y, to + 32 * c); tc_wait_ld(); }
-        else {
 #pragma unroll
-          for (u32 z = 0; z < 32; ++z) y[z] = 0;
-        }
-        if (!mine) {
-        } else if (!j.direct) {
-#pragma unroll
-          for (u32 z = 0; z < 32; z += 4) *(uint4 *)(sums + 32 * c + z) = make_uint4(y[z], y[z + 1], y[z + 2], y[z + 3]);
-        } else {
+        for (u32 c = 0; c < D / 32; ++c) {
           u32 e[16];
+          if (j.direct) {
+            u32 y[32];
+            if (n) { tc_ld32(y, to + 32 * c); tc_wait_ld(); }
 #pragma unroll
-          for (u32 z = 0; z < 16; ++z) e[z] = Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv);
-          if (wide) {
-#pragma unroll
-            for (u32 z = 0; z < 16; z += 4) *(uint4 *)(out + 32 * c + 2 * z) = make_uint4(e[z], e[z + 1], e[z + 2], e[z + 3]);
+            for (u32 z = 0; z < 16; ++z) e[z] = n ? Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv) : 0;
           } else {
+            if (n) { tc_ld16(e, to + round * (D / 2) + 16 * c); tc_wait_ld(); }
+            else {
 #pragma unroll
-            for (u32 z = 0; z < 16; ++z) { out[32 * c + 2 * z] = (u16)e[z]; out[32 * c + 2 * z + 1] = (u16)(e[z] >> 16); }
+              for (u32 z = 0; z < 16; ++z) e[z] = 0;
+            }
+          }
+#pragma unroll
+          for (u32 z = 0; z < 4; ++z)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(q_place(rt, 4 * c + z)), "r"(e[4 * z]), "r"(e[4 * z + 1]), "r"(e[4 * z + 2]), "r"(e[4 * z + 3]) : "memory");
+        }
+        __syncwarp();
+#pragma unroll 4
+        for (u32 k = 0; k < D / 8; ++k) {
+          const u32 at = k * 32 + lane, row = at / (D / 8), c = at % (D / 8);
+          uint4 v;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(q_place(row0 + row, c)) : "memory");
+          u8 *const dst = (u8 *)__shfl_sync(~0u, (u64)row_out, row) + round * (D * 2) + c * 16;
+          if (row0 + row >= n_here) {
+          } else if (wide) {
+            *(uint4 *)dst = v;
+          } else {                       // an output whose rows are not aligned to 16 bytes: partial results are
+            u16 *const d = (u16 *)dst;
+            const u32 x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (u32 y = 0; y < 4; ++y) { d[2 * y] = (u16)x[y]; d[2 * y + 1] = (u16)(x[y] >> 16); }
           }
         }
       }
@@ -1395,16 +1505,16 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class T, u32 D, u32 KIND>
-static cudaError_t launch_join(const AttendArgs &a, const AttendPlan &p, cudaStream_t s, u32 *launches) {
+template <class... Exp, class... Act>
+static cudaError_t launch_join(void (*kern)(Exp...), u64 ctas, u32 sms, cudaStream_t s, u32 *launches, Act... args) {
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((u32)std::min<u64>(KIND == 1 ? (u64)a.b.n_tokens * a.n_q_heads : ((u64)a.b.n_tokens * a.n_q_heads + 3) / 4, 16ull * p.sms)); c.blockDim = dim3(128); c.stream = s;
+  c.gridDim = dim3((u32)std::min<u64>(ctas, 8ull * sms)); c.blockDim = dim3(128); c.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   c.attrs = &at; c.numAttrs = 1;
   ++*launches;
-  return cudaLaunchKernelEx(&c, k_attend_join<T, D, KIND>, a, p.rows, p.parts);
+  return cudaLaunchKernelEx(&c, kern, args...);
 }
 
 AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
@@ -1430,7 +1540,7 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     p.rows = TC_ROWS;
     const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, (a.b.max_blocks + MIN_PIECE - 1) / MIN_PIECE);
     p.grid = (u32)std::max<u64>(1, std::min<u64>(sm_count, units * pieces));
-    p.parts = pieces > 1 ? 4 * sm_count : 0;
+    p.parts = pieces > 1 ? 4 * sm_count + 64 : 0;     // 64: rounding of the mean share
   }
   if (p.parts) p.scratch_bytes = plan_bytes(a.b.n_seqs) + (u64)p.parts * p.rows * (a.p.head_dim + 2) * 4;
   return p;
@@ -1452,17 +1562,17 @@ static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const 
   k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
-  return launch_join<T, D, 1>(a, p, s, launches);
+  return launch_join(k_attend_join_split<T, D>, (u64)a.b.n_tokens * a.n_q_heads, p.sms, s, launches, a, p.parts);
 }
 
 template <class T, u32 D>
 static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
   cudaError_t r = allow_smem(k_attend_tc<T, D>, 6 + (D == 128) * 2 + a.fp16, TcShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
-  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts, p.parts);
+  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
-  return launch_join<T, D, 2>(a, p, s, launches);
+  return launch_join(k_attend_join_tc<T, D>, ((u64)a.b.n_tokens * ((a.n_q_heads + 7) / 8) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);
 }
 
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {

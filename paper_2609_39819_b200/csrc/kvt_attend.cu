@@ -636,24 +636,30 @@ __global__ void __launch_bounds__(128) k_attend_join_split(AttendArgs a, u32 n_p
   }
 }
 
-// Kind 2, many rows of few parts: a warp takes BATCH heads of a token at a time and keeps their loads in flight together.
+// Kind 2, many rows of few parts: a warp takes BATCH heads of a token at a time and keeps the loads of STEP parts of each in
+// flight together.
 template <class T, u32 D>
 __global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, u32 n_parts) {
-  constexpr u32 C = D / 32, BATCH = 8;
+  constexpr u32 C = D / 32, BATCH = 4, STEP = 4;
   const u32 lane = threadIdx.x & 31, H = a.p.n_kv_heads;
   const float *sums = scratch_sums(a);
   const float2 *ml = (const float2 *)(sums + (u64)n_parts * rows * D);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (!scratch_plan(a)[0].x) return;
   const u32 groups = (a.n_q_heads + BATCH - 1) / BATCH, warps = gridDim.x * 4;
   u32 last_t = ~0u, seq = ~0u, start = 0;
+  bool waited = false;
   uint4 plan = make_uint4(0, 0, 0, 0);
   for (u64 id = blockIdx.x * 4 + (threadIdx.x >> 5); id < (u64)a.b.n_tokens * groups; id += warps) {
     const u32 t = (u32)(id / groups), hq0 = (u32)(id - (u64)t * groups) * BATCH;
     if (t != last_t) {
       last_t = t;
       seq = seq_of_token(a.b, t);
-      if (seq != ~0u) { plan = scratch_plan(a)[1 + seq]; start = a.b.q_start[seq]; }
+      if (seq != ~0u) start = a.b.q_start[seq];
+      if (!waited) {                     // the batch's arrays are older than the kernel before this one
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
+        if (!scratch_plan(a)[0].x) return;
+      }
+      if (seq != ~0u) plan = scratch_plan(a)[1 + seq];
     }
     const u32 n = plan.y, stride = plan.z * H;
     if (seq == ~0u || n <= 1) continue;
@@ -669,23 +675,35 @@ __global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, 
 #pragma unroll
       for (u32 c = 0; c < C; ++c) acc[b][c] = 0.0f;
     }
-    for (u32 i = 0; i < n; ++i) {
-      float2 x[BATCH];
-      float v[BATCH][C];
+    for (u32 i = 0; i < n; i += STEP) {
+      float2 x[STEP][BATCH];
+      float v[STEP][BATCH][C];
+#pragma unroll
+      for (u32 y = 0; y < STEP; ++y)
+#pragma unroll
+        for (u32 b = 0; b < BATCH; ++b) {
+          const u32 p = at[b] + min(i + y, n - 1) * stride * rows;
+          x[y][b] = ml[p];
+          load_sums<C>(v[y][b], sums + (u64)p * D + lane * C);
+        }
 #pragma unroll
       for (u32 b = 0; b < BATCH; ++b) {
-        const u32 p = at[b] + i * stride * rows;
-        x[b] = ml[p];
-        load_sums<C>(v[b], sums + (u64)p * D + lane * C);
-      }
+        float now = m[b];
 #pragma unroll
-      for (u32 b = 0; b < BATCH; ++b) {
-        const float now = fmaxf(m[b], x[b].x), ref = now == -INFINITY ? 0.0f : now, f = ex2(m[b] - ref);
-        const float w = ex2(x[b].x - ref);             // a part without keys for this row holds zeros, weight 2^-inf
+        for (u32 y = 0; y < STEP; ++y) { if (i + y >= n) x[y][b] = make_float2(-INFINITY, 0.0f); now = fmaxf(now, x[y][b].x); }
+        const float ref = now == -INFINITY ? 0.0f : now, f = ex2(m[b] - ref);
         m[b] = now;
-        l[b] = l[b] * f + w * x[b].y;
+        l[b] *= f;
 #pragma unroll
-        for (u32 c = 0; c < C; ++c) acc[b][c] = acc[b][c] * f + w * v[b][c];
+        for (u32 c = 0; c < C; ++c) acc[b][c] *= f;
+#pragma unroll
+        for (u32 y = 0; y < STEP; ++y) {
+          const float w = ex2(x[y][b].x - ref);        // a part without keys for this row holds zeros, weight 2^-inf
+          l[b] += w * x[y][b].y;
+          if (i + y < n)
+#pragma unroll
+            for (u32 c = 0; c < C; ++c) acc[b][c] += w * v[y][b][c];
+        }
       }
     }
 #pragma unroll
@@ -1074,6 +1092,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   __shared__ volatile u32 s_lost;
   __shared__ Job s_job[TC_JOBS];
   __shared__ float s_cost[N_CUTS];
+  __shared__ u8 s_order[32];
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
   const u32 full = smem_addr(s_full), empty = smem_addr(s_empty), sready = smem_addr(s_sready), pready = smem_addr(s_pready),
@@ -1127,13 +1146,32 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     Seq q = mine;
     u32 tiles = 0, pieces = 0;
     u32 my_jobs = 0, at = 0, all = 0, my_part = 0, all_parts = 0;
-    auto take = [&]() {                  // lane: one of the sequences s0 .. s0 + 31
+    u32 my_seq = 0;
+    // lane: one of the sequences s0 .. s0 + 31, those with the longest pieces first: jobs that get shorter, dealt out back and
+    // forth, come out even
+    auto take = [&]() {
       const u32 s = s0 + lane;
       tiles = pieces = 0;
+      u32 length = 0;
       if (s < a.b.n_seqs) {
         if (s0) q = load_seq(a.b, s, a.err);
         tiles = seq_tiles(a, q, TC_ROWS);
-        pieces = (seq_blocks(a, q, TC_ROWS) + piece - 1) / piece;
+        const u32 nb = seq_blocks(a, q, TC_ROWS);
+        pieces = (nb + piece - 1) / piece;
+        length = tiles ? (nb + pieces - 1) / pieces : 0;
+      }
+      my_seq = s;
+      if (a.b.n_seqs > 1) {
+        u32 rank = 0;
+#pragma unroll 8
+        for (u32 y = 0; y < 32; ++y) { const u32 z = __shfl_sync(~0u, length, y); rank += z > length || (z == length && y < lane); }
+        s_order[rank] = (u8)lane;
+        __syncwarp();
+        const u32 from = s_order[lane];
+        q.t0 = __shfl_sync(~0u, q.t0, from); q.n = __shfl_sync(~0u, q.n, from); q.kv = __shfl_sync(~0u, q.kv, from);
+        tiles = __shfl_sync(~0u, tiles, from); pieces = __shfl_sync(~0u, pieces, from);
+        my_seq = s0 + from;
+        __syncwarp();
       }
       my_jobs = tiles * pieces * H;
       const u32 parts = pieces > 1 ? tiles * pieces : 0;
@@ -1145,8 +1183,8 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       }
       at = base + incl - my_jobs; my_part = part0 + pincl - parts;
       all = __shfl_sync(~0u, incl, 31); all_parts = __shfl_sync(~0u, pincl, 31);
-      if (blockIdx.x == 0 && n_parts && s < a.b.n_seqs) {
-        scratch_plan(a)[1 + s] = make_uint4(my_part, pieces, tiles, 0);
+      if (blockIdx.x == 0 && n_parts && my_seq < a.b.n_seqs) {
+        scratch_plan(a)[1 + my_seq] = make_uint4(my_part, pieces, tiles, 0);
         if (pieces > 1) scratch_plan(a)[0].x = 1;
       }
     };
@@ -1162,7 +1200,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       if (hit && lane == __ffs(hit) - 1) {
         Job j;
         const u32 x = want - at, y = x / H, h = x - y * H, pc = y / tiles, tile = tiles - 1 - (y - pc * tiles);
-        j.t0 = q.t0; j.kv = q.kv; j.seq = s0 + lane; j.h = h; j.shift = q.kv - q.n;
+        j.t0 = q.t0; j.kv = q.kv; j.seq = my_seq; j.h = h; j.shift = q.kv - q.n;
         j.r0 = tile * TC_ROWS; j.r1 = min(j.r0 + TC_ROWS, q.n * a.group) - 1;
         u32 first, last;                 // keys any row sees
         row_range(a, q, j.r0 / a.group, first, j.all_hi);
@@ -1572,7 +1610,7 @@ static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvM
   k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
-  return launch_join(k_attend_join_tc<T, D>, ((u64)a.b.n_tokens * ((a.n_q_heads + 7) / 8) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);
+  return launch_join(k_attend_join_tc<T, D>, ((u64)a.b.n_tokens * ((a.n_q_heads + 3) / 4) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);
 }
 
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {

@@ -1260,16 +1260,19 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     if (elect_one()) {
       const u32 id_s = tc_idesc(FP16, TC_KEYS, false), id_o = tc_idesc(FP16, D, true);
       const u64 dq0 = tc_desc(sq, 16, 1024), dk0 = tc_desc(ring, 16, D * 16), dv0 = tc_desc(ring, 1024, D * 16);
-      u32 st = 0, ph = 0;                // stage in turn and its phase
-      auto landed = [&]() { return tc_wait1(full + st * 8, ph, lost); };
-      auto next = [&]() { if (++st == S::STAGES) { st = 0; ph ^= 1; } };
-      auto product_s = [&](u32 i, u64 dk) {
+      struct Place { u32 st, ph; };      // a stage and its phase
+      auto after = [](Place x) { return x.st + 1 == S::STAGES ? Place{0, x.ph ^ 1} : Place{x.st + 1, x.ph}; };
+      auto has = [&](Place x) { return bar_try(full + x.st * 8, x.ph); };
+      auto landed = [&](Place x) { return tc_wait1(full + x.st * 8, x.ph, lost); };
+      auto product_s = [&](u32 i, u32 st) {
+        const u64 dk = dk0 + st * (S::STAGE / 16);
 #pragma unroll
         for (u32 k = 0; k < D / 16; ++k)
           tc_mma_ss(tmem + i * 128, dq0 + (i * (TC_TILE * D * 2) + (k / 4) * (TC_TILE * 128) + (k % 4) * 32) / 16,
                     dk + ((k / 4) * 1024 + (k % 4) * 32) / 16, id_s, k > 0);
         tc_commit(sready + i * 8);
       };
+      Place at_k{0, 0};                  // the first K of the job in turn
       u32 seen_q[2] = {0, 0}, seen_p[2] = {0, 0};
       bool ok = true;
       for (;;) {
@@ -1282,33 +1285,32 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         const u32 n = (b1 - b0 + TC_KB - 1) / TC_KB;
         const bool two = r1 - r0 >= TC_TILE;
         if (!n) continue;
-        if (!(ok = landed())) break;
-        u64 dk = dk0 + st * (S::STAGE / 16);
+        if (!(ok = landed(at_k))) break;
 #pragma unroll
         for (u32 i = 0; i < 2; ++i)
           if (ok && (i == 0 || two)) {
             ok = tc_wait1(qready + i * 8, seen_q[i]++ & 1, lost);
             tc_after();
-            if (ok) product_s(i, dk);
+            if (ok) product_s(i, at_k.st);
           }
         if (!ok) break;
-        tc_commit(empty + st * 8);
-        next();
+        // stages to hand back, V of the keys before and the K in use: not at once, which would hold up the next product, but
+        // in the pause before the second tile's powers are there. The arrivals of the next keys are looked at there too.
+        Place v = after(at_k), k = after(v);
+        u32 free_k = at_k.st, free_v = ~0u;
+        bool has_v = false, has_k = false;
         for (u32 s = 0; s < n; ++s) {
-          if (!(ok = landed())) break;
-          const u32 sv = st;
           const bool more = s + 1 < n;
+          const Place v1 = after(k), k1 = after(v1);
+          if (!has_v && !(ok = landed(v))) break;
           if (!more && b1 * BT > kv) {           // tokens behind the length in the last block: whatever their values hold,
             for (u32 r = kv % BT; r < BT; ++r)   // weight 0 must not meet an Inf or a NaN
               for (u32 c = 0; c < D / 8; ++c)
                 asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
-                             ::"r"(ring + sv * S::STAGE + ((b1 - 1 - b0) % TC_KB) * S::BLOCK + block_off<D>(r, c)), "r"(0) : "memory");
+                             ::"r"(ring + v.st * S::STAGE + ((b1 - 1 - b0) % TC_KB) * S::BLOCK + block_off<D>(r, c)), "r"(0) : "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
-          next();
-          if (more && !(ok = landed())) break;
-          const u64 dv = dv0 + sv * (S::STAGE / 16);
-          dk = dk0 + st * (S::STAGE / 16);
+          const u64 dv = dv0 + v.st * (S::STAGE / 16);
 #pragma unroll
           for (u32 i = 0; i < 2; ++i)
             if (i == 0 || two) {
@@ -1319,18 +1321,27 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
                 if (!ok) break;
                 tc_after();
 #pragma unroll
-                for (u32 k = part * (TC_KB / TC_PARTS); k < (part + 1) * (TC_KB / TC_PARTS); ++k)
-                  tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + k * 8, dv + k * (D * 32 / 16), id_o, s > 0 || k > 0);
+                for (u32 y = part * (TC_KB / TC_PARTS); y < (part + 1) * (TC_KB / TC_PARTS); ++y)
+                  tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + y * 8, dv + y * (D * 32 / 16), id_o, s > 0 || y > 0);
               }
               if (!ok) break;
-              if (more) product_s(i, dk);
-              else tc_commit(sready + i * 8);    // the finished sums
+              if (!more) tc_commit(sready + i * 8);      // the finished sums
+              else if (i == 0 && !has_k && !(ok = landed(k))) break;
+              else product_s(i, k.st);
+              if (i == 0) {
+                if (free_v != ~0u) tc_commit(empty + free_v * 8);
+                tc_commit(empty + free_k * 8);
+                has_v = more && has(v1);
+                has_k = s + 2 < n && has(k1);
+              }
             }
-          if (!ok) break;
-          tc_commit(empty + sv * 8);
-          if (more) { tc_commit(empty + st * 8); next(); }
+          if (!ok || !more) break;
+          free_v = v.st; free_k = k.st;
+          v = v1; k = k1;
         }
         if (!ok) break;
+        tc_commit(empty + v.st * 8);     // the last V; behind it lies the next job's first K
+        at_k = k;
       }
       // all products and their arrivals are done before the CTA ends
       tc_commit(drain);

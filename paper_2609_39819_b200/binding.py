@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -80,6 +81,11 @@ class AttendArgs(C.Structure):
                [(n, C.c_uint64) for n in ("q_ts", "q_hs", "o_ts", "o_hs")] + \
                [("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
 
+
+# the same layouts for struct.pack, which is what a call made thousands of times a second uses
+_BATCH = "IIIIQPPP"
+_APPEND = struct.Struct("@" + _BATCH + "IIIIIIPPPPQQQQQQQQPPPQ")
+_ATTEND = struct.Struct("@" + _BATCH + "IIIIIfPPPQQQQPQ")
 
 CALL_INFO_DTYPE = np.dtype([(n, np.uint32) for n in ("n_blocks", "hit_len", "n_hit_hbm", "n_hit_host",
                                                        "n_admissible", "n_admitted", "n_held", "n_pinned",
@@ -315,6 +321,7 @@ class Engine:
         # the address of the device's current stream, without a Stream object around it (2 us of a call of 10)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self._scratch_bytes = {}
         self.tail_pool = None
         if n_tail_blocks:       # blocks outside every tier: slot ids n_hbm_blocks + i of append_kv and attend
             self.set_tail_pool((torch.zeros if zero_pools else torch.empty)(n_tail_blocks * self.block_bytes, dtype=torch.uint8,
@@ -539,7 +546,7 @@ class Engine:
             raise ValueError(f"{what}: {n} table rows need {n} lengths and {n + 1} starts, with consecutive elements")
         if block_table.get_device() != dev or q_start.get_device() != dev or kv_len.get_device() != dev:
             raise ValueError(f"{what}: block_table, q_start and kv_len must be on {self._dev}")
-        return Batch(n, n_tokens, m, max_q_len or 0, ts, q_start.data_ptr(), kv_len.data_ptr(), block_table.data_ptr())
+        return n, n_tokens, m, max_q_len or 0, ts, q_start.data_ptr(), kv_len.data_ptr(), block_table.data_ptr()
 
     def _kv_stream(self):
         return self._raw_stream(self._dev_index)
@@ -557,36 +564,43 @@ class Engine:
         t, h, d = k.shape[0], self.n_kv_heads, self.head_dim
         kp, kts, khs = self._kv_tensor(k, "append_kv: k", (t, h, d), k.dtype)
         vp, vts, vhs = self._kv_tensor(v, "append_kv: v", (t, h, d), k.dtype)
-        a = AppendArgs(self._kv_batch("append_kv", t, block_table, q_start, kv_len, 0), layer, dt, 0, 0, 0, 0,
-                       None, kp, vp, None, 0, 0, kts, khs, vts, vhs)
+        batch = self._kv_batch("append_kv", t, block_table, q_start, kv_len, 0)
+        hq = qp = qts = qhs = op = ots = ohs = 0
         if q is not None:
             hq = q.shape[1] if q.dim() == 3 else 0
-            a.n_q_heads = hq
-            a.q, a.q_ts, a.q_hs = self._kv_tensor(q, "append_kv: q", (t, hq, d), k.dtype)
+            qp, qts, qhs = self._kv_tensor(q, "append_kv: q", (t, hq, d), k.dtype)
             if q_out is None:
                 q_out = q.new_empty((t, hq, d))
-            a.q_out, a.qo_ts, a.qo_hs = self._kv_tensor(q_out, "append_kv: q_out", (t, hq, d), k.dtype)
-            if (a.qo_ts == 0 and t > 1) or (a.qo_hs == 0 and hq > 1):
-                raise ValueError("append_kv: q_out is a broadcast tensor")
-            if a.q == a.q_out and (a.q_ts, a.q_hs) != (a.qo_ts, a.qo_hs):
-                raise ValueError("append_kv: q_out in the place of q needs its strides")
+                op, ots, ohs = q_out.data_ptr(), hq * d, d
+            else:
+                op, ots, ohs = self._kv_tensor(q_out, "append_kv: q_out", (t, hq, d), k.dtype)
+                if (ots == 0 and t > 1) or (ohs == 0 and hq > 1):
+                    raise ValueError("append_kv: q_out is a broadcast tensor")
+                if qp == op and (qts, qhs) != (ots, ohs):
+                    raise ValueError("append_kv: q_out in the place of q needs its strides")
         elif q_out is not None:
             raise ValueError("append_kv: q_out without q")
+        rot = flags = freqs = axis_of = pos = pos_stride = 0
+        n_axes = 1
         if rope is not None:
+            rot, n_axes, freqs = rope.rot_dim, rope.n_axes, rope.freqs.data_ptr()
             if rope.freqs.get_device() != self._dev_index:
                 raise ValueError(f"append_kv: rope is on {rope.freqs.device}, the engine on {self._dev}")
-            a.rot_dim, a.flags, a.freqs = rope.rot_dim, ROPE_INTERLEAVED if rope.interleaved else 0, rope.freqs.data_ptr()
-            a.n_axes = rope.n_axes
-            a.axis_of = rope.axis_of.data_ptr() if rope.axis_of is not None else None
-            if positions is None and rope.n_axes > 1:
-                raise ValueError(f"append_kv: {rope.n_axes} axes need positions")
+            if rope.interleaved:
+                flags = ROPE_INTERLEAVED
+            if rope.axis_of is not None:
+                axis_of = rope.axis_of.data_ptr()
+            if positions is None and n_axes > 1:
+                raise ValueError(f"append_kv: {n_axes} axes need positions")
         if positions is not None:
             p2 = positions if positions.dim() == 2 else positions[None]
-            if rope is None or p2.dtype != torch.int32 or p2.shape != (rope.n_axes, t) or p2.get_device() != self._dev_index or \
+            if rope is None or p2.dtype != torch.int32 or p2.shape != (n_axes, t) or p2.get_device() != self._dev_index or \
                     (t > 1 and p2.stride(1) != 1):
-                raise ValueError(f"append_kv: positions must be int32 [{rope.n_axes if rope else 1}, {t}] on {self._dev}, with a rope")
-            a.positions, a.pos_stride = p2.data_ptr(), p2.stride(0)
-        self._check(self.L.kvt_append_kv(self.h, C.byref(a), self._kv_stream()), "append_kv")
+                raise ValueError(f"append_kv: positions must be int32 [{n_axes}, {t}] on {self._dev}, with a rope")
+            pos, pos_stride = p2.data_ptr(), p2.stride(0)
+        a = _APPEND.pack(*batch, layer, dt, hq, flags, rot, n_axes, qp, kp, vp, op, qts, qhs, kts, khs, vts, vhs, ots, ohs,
+                         freqs, axis_of, pos, pos_stride)
+        self._check(self.L.kvt_append_kv(self.h, a, self._kv_stream()), "append_kv")
         return q_out
 
     def attend(self, layer, q, block_table, q_start, kv_len, max_q_len=None, causal=True, window=None, scale=None, out=None,
@@ -602,7 +616,7 @@ class Engine:
         t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
         qp, qts, qhs = self._kv_tensor(q, "attend: q", (t, hq, self.head_dim), q.dtype)
         if out is None:
-            out = q.new_empty((t, hq, d))
+            out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((t, hq, d))
             op, ots, ohs = out.data_ptr(), hq * d, d
         else:
             op, ots, ohs = self._kv_tensor(out, "attend: out", (t, hq, d), q.dtype)
@@ -611,14 +625,21 @@ class Engine:
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != (t, hq) or lse.get_device() != self._dev_index or
                                 not lse.is_contiguous()):
             raise ValueError(f"attend: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
-        a = AttendArgs(self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len), layer, dt, hq,
-                       0 if causal else ATTN_FULL, window or 0, scale or 0.0, qp, op,
-                       lse.data_ptr() if lse is not None else None, qts, qhs, ots, ohs)
-        n = self.L.kvt_attend_scratch_bytes(self.h, C.byref(a))
-        if n:
-            scratch = torch.empty(n, dtype=torch.uint8, device=self._dev)      # from the current stream's pool, or the capture's
-            a.scratch, a.scratch_bytes = scratch.data_ptr(), n
-        self._check(self.L.kvt_attend(self.h, C.byref(a), self._kv_stream()), "attend")
+        batch = self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len)
+        flags, lsep = 0 if causal else ATTN_FULL, lse.data_ptr() if lse is not None else 0
+        key = (t, batch[0], batch[2], max_q_len, hq, flags, window or 0)      # all that the scratch depends on
+        n = self._scratch_bytes.get(key)
+        if n is None:
+            probe = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs, 0, 0)
+            n = self.L.kvt_attend_scratch_bytes(self.h, probe)
+            if len(self._scratch_bytes) >= 4096:
+                self._scratch_bytes.clear()
+            self._scratch_bytes[key] = n
+        # from the current stream's pool, or the capture's: nobody else has it while this call's kernels run
+        scratch = torch.empty(n, dtype=torch.uint8, device=self._dev) if n else None
+        a = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs,
+                         scratch.data_ptr() if n else 0, n)
+        self._check(self.L.kvt_attend(self.h, a, self._kv_stream()), "attend")
         return out
 
     def kv_check(self):

@@ -57,12 +57,18 @@ __device__ __forceinline__ u8 *slot_ptr(const KvPools &p, const KvRow &r, u32 sl
 // ======================================================================================================
 // Append: rotation of q and k by the tokens' positions, k and v into the blocks.
 // ======================================================================================================
-// Where token t goes; the whole CTA asks. Every thread compares some of the starts with t, so the sequence is found
-// with one round of loads instead of a chain of them.
+// Where token t goes; the whole CTA, or one warp, asks. Every thread compares some of the starts with t, so the sequence is
+// found with one round of loads instead of a chain of them.
 struct Where { u32 seq, index; bool ok; };
+template <bool WARP>
 __device__ __forceinline__ Where find_token(const KvBatch &b, u32 t, u32 *err) {
   u32 seq = 0;
-  for (u32 s0 = 0; s0 < b.n_seqs; s0 += blockDim.x) {
+  if (WARP) {
+    for (u32 s0 = 0; s0 < b.n_seqs; s0 += 32) {
+      const u32 s = s0 + (threadIdx.x & 31);
+      seq += __popc(__ballot_sync(~0u, s < b.n_seqs && b.q_start[s + 1] <= t));
+    }
+  } else for (u32 s0 = 0; s0 < b.n_seqs; s0 += blockDim.x) {
     const u32 s = s0 + threadIdx.x;
     seq += __syncthreads_count(s < b.n_seqs && b.q_start[s + 1] <= t);
   }
@@ -73,7 +79,7 @@ __device__ __forceinline__ Where find_token(const KvBatch &b, u32 t, u32 *err) {
   w.index = kv - (z - t);
   // starts that decrease; a token in front of the sequence's first place or behind its last block
   w.ok = t >= a && t < z && kv >= z - t && w.index / BT < b.max_blocks;
-  if (cut && threadIdx.x == 0) kv_err(err, KVERR_RANGE);
+  if (cut && threadIdx.x % (WARP ? 32 : blockDim.x) == 0) kv_err(err, KVERR_RANGE);
   return w;
 }
 
@@ -95,7 +101,7 @@ template <class T>
 __global__ void __launch_bounds__(128) k_append_any(AppendArgs a) {
   extern __shared__ float2 cs[];
   const u32 t = blockIdx.x;
-  const Where w = find_token(a.b, t, a.err);
+  const Where w = find_token<false>(a.b, t, a.err);
   if (w.seq >= a.b.n_seqs) return;
   const u32 half = a.rot_dim / 2;
   for (u32 j = threadIdx.x; j < half; j += blockDim.x) cs[j] = pair_angle(a, t, w.index, j);
@@ -140,10 +146,13 @@ __global__ void __launch_bounds__(128) k_append_any(AppendArgs a) {
 // read once and written once. Work item: 16 elements (two vectors) of a head; with pairs (j, j + rot/2) a rotated item is
 // 8 elements from either half, with neighbouring pairs 16 in a row. All loads of a thread's UNROLL items are in flight
 // before the token's sines are waited for.
-template <class T, u32 THREADS, u32 UNROLL>
+// GROUP threads work on a token: the whole CTA, or with few heads a warp, so that a CTA of four takes four tokens.
+template <class T, u32 THREADS, u32 GROUP, u32 UNROLL>
 __global__ void __launch_bounds__(THREADS) k_append_vec(AppendArgs a) {
-  extern __shared__ float2 cs[];
-  const u32 t = blockIdx.x, tid = threadIdx.x;
+  extern __shared__ float2 cs_all[];
+  const u32 t = blockIdx.x * (THREADS / GROUP) + threadIdx.x / GROUP, tid = threadIdx.x % GROUP;
+  if (t >= a.b.n_tokens) return;         // the last CTA's spare warps
+  float2 *const cs = cs_all + threadIdx.x / GROUP * (a.rot_dim / 2);
   const u32 D = a.p.head_dim, H = a.p.n_kv_heads, half = a.rot_dim / 2;
   const u32 per = D / 16, rot_items = a.rot_dim / 16, n_q = a.n_q_heads * per, n_k = H * per, n = n_q + 2 * n_k;
   struct Item { const u16 *src; u32 lo, hi, pair; };     // first vector at src + lo, second at src + hi; pair: first pair, or none
@@ -163,10 +172,10 @@ __global__ void __launch_bounds__(THREADS) k_append_vec(AppendArgs a) {
   const bool inside = t < a.b.q_start[a.b.n_seqs];       // else behind the last sequence: loads nothing, finds nothing below
 #pragma unroll
   for (u32 y = 0; y < UNROLL; ++y) {
-    const u32 i = tid + y * THREADS;
+    const u32 i = tid + y * GROUP;
     if (inside && i < n) { const Item x = item(i); in[y][0] = __ldcs((const uint4 *)(x.src + x.lo)); in[y][1] = __ldcs((const uint4 *)(x.src + x.hi)); }
   }
-  const Where w = find_token(a.b, t, a.err);
+  const Where w = find_token<GROUP == 32>(a.b, t, a.err);
   if (w.seq >= a.b.n_seqs) return;
   u16 *kd = nullptr, *vd = nullptr;
   if (w.ok) {
@@ -176,8 +185,8 @@ __global__ void __launch_bounds__(THREADS) k_append_vec(AppendArgs a) {
     if (!kd) { if (tid == 0) kv_err(a.err, KVERR_RANGE); }
     else { const u64 off = (u64)(w.index % BT) * H * D; kd += off; vd += off; }
   }
-  for (u32 j = tid; j < half; j += THREADS) cs[j] = pair_angle(a, t, w.index, j);
-  __syncthreads();
+  for (u32 j = tid; j < half; j += GROUP) cs[j] = pair_angle(a, t, w.index, j);
+  if (GROUP == 32) __syncwarp(); else __syncthreads();
   auto finish = [&](u32 i, uint4 v0, uint4 v1) {
     const Item x = item(i);
     u32 r0[4] = {v0.x, v0.y, v0.z, v0.w}, r1[4] = {v1.x, v1.y, v1.z, v1.w};
@@ -211,18 +220,20 @@ __global__ void __launch_bounds__(THREADS) k_append_vec(AppendArgs a) {
     *(uint4 *)(d + x.hi) = make_uint4(r1[0], r1[1], r1[2], r1[3]);
   };
 #pragma unroll
-  for (u32 y = 0; y < UNROLL; ++y) if (tid + y * THREADS < n) finish(tid + y * THREADS, in[y][0], in[y][1]);
-  for (u32 i = tid + UNROLL * THREADS; i < n; i += THREADS) {
+  for (u32 y = 0; y < UNROLL; ++y) if (tid + y * GROUP < n) finish(tid + y * GROUP, in[y][0], in[y][1]);
+  for (u32 i = tid + UNROLL * GROUP; i < n; i += GROUP) {
     const Item x = item(i);
     const uint4 v0 = __ldcs((const uint4 *)(x.src + x.lo)), v1 = __ldcs((const uint4 *)(x.src + x.hi));
     finish(i, v0, v1);
   }
 }
 
-template <u32 THREADS, u32 UNROLL>
+template <u32 THREADS, u32 GROUP, u32 UNROLL>
 static void append_vec(const AppendArgs &a, u32 smem, cudaStream_t s) {
-  if (a.fp16) k_append_vec<__half, THREADS, UNROLL><<<a.b.n_tokens, THREADS, smem, s>>>(a);
-  else k_append_vec<__nv_bfloat16, THREADS, UNROLL><<<a.b.n_tokens, THREADS, smem, s>>>(a);
+  constexpr u32 TOKENS = THREADS / GROUP;
+  const u32 ctas = (a.b.n_tokens + TOKENS - 1) / TOKENS;
+  if (a.fp16) k_append_vec<__half, THREADS, GROUP, UNROLL><<<ctas, THREADS, smem * TOKENS, s>>>(a);
+  else k_append_vec<__nv_bfloat16, THREADS, GROUP, UNROLL><<<ctas, THREADS, smem * TOKENS, s>>>(a);
 }
 
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, u32 *launches) {
@@ -232,8 +243,9 @@ cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, u32 *launches) {
   const uintptr_t bases = (uintptr_t)a.k | (uintptr_t)a.v | (a.n_q_heads ? (uintptr_t)a.q | (uintptr_t)a.q_out : 0);
   if (!(a.p.head_dim % 16 || a.rot_dim % 16 || strides % 8 || bases % 16)) {
     const u64 items = ((u64)a.n_q_heads + 2 * a.p.n_kv_heads) * (a.p.head_dim / 16);
-    if (items <= 384) append_vec<128, 3>(a, smem, s);
-    else append_vec<256, 4>(a, smem, s);
+    if (items <= 128) append_vec<128, 32, 4>(a, smem, s);
+    else if (items <= 384) append_vec<128, 128, 3>(a, smem, s);
+    else append_vec<256, 256, 4>(a, smem, s);
     return cudaGetLastError();
   }
   if (a.fp16) k_append_any<__half><<<a.b.n_tokens, 128, smem, s>>>(a);
@@ -791,7 +803,13 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
       tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
     }
     const u32 u = (u32)((x - base) / unit), tile = u / H, h = u % H;
-    const u64 u0 = base + (u64)u * unit, x1 = min((unsigned long long)x_end, (unsigned long long)(u0 + unit));
+    const u64 u0 = base + (u64)u * unit;
+    if (!n_parts && x > u0) {            // nothing is cut: a unit goes whole to the stretch it begins in
+      x = u0 + unit;
+      more = x < x_end;
+      continue;
+    }
+    const u64 x1 = n_parts ? min((unsigned long long)x_end, (unsigned long long)(u0 + unit)) : u0 + unit;
     const bool direct = x == u0 && x1 == u0 + unit;
     const u32 part = 2 * blockIdx.x + (x == u0 && x > x_begin);
     const u32 n_rows = q.n * a.group, r0 = tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
@@ -1582,14 +1600,18 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     p.kind = 1;
     p.rows = SPLIT_ROWS;
     const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, ((u64)a.b.max_blocks + UNIT_COST) / MIN_STRETCH);
-    p.grid = (u32)std::max<u64>(1, std::min<u64>(2ull * sm_count, units * pieces));
-    p.parts = p.grid > 1 ? 2 * p.grid : 0;      // one CTA takes every unit whole
+    // Short sequences are not cut: a CTA is through them sooner than a second kernel has joined their parts, the more so when
+    // there is a unit for every SM. One sequence of 200 tokens, 8 heads of 128: 7.9 us against 11.3 cut, of 500 tokens 11.0
+    // against 9.0; 32 sequences of 500: 13.1 against 19.3, of 1000 27.8 against 31.8.
+    const bool cut = a.b.max_blocks > (units < (u64)sm_count ? 16u : 64u);
+    p.grid = (u32)std::max<u64>(1, std::min<u64>(2ull * sm_count, cut ? units * pieces : units));
+    p.parts = p.grid > 1 && cut ? 2 * p.grid : 0;
   } else {
     p.kind = 2;
     p.rows = TC_ROWS;
     const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, (a.b.max_blocks + MIN_PIECE - 1) / MIN_PIECE);
     p.grid = (u32)std::max<u64>(1, std::min<u64>(sm_count, units * pieces));
-    p.parts = pieces > 1 ? 4 * sm_count + 64 : 0;     // 64: rounding of the mean share
+    p.parts = pieces > 1 && (units < (u64)sm_count || a.b.max_blocks > 64) ? 4 * sm_count + 64 : 0;     // 64: rounding of the mean share
   }
   if (p.parts) p.scratch_bytes = plan_bytes(a.b.n_seqs) + (u64)p.parts * p.rows * (a.p.head_dim + 2) * 4;
   return p;

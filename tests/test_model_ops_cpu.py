@@ -58,3 +58,14 @@ def test_rope_description():
                 dict(rot_dim=4, axis_of=[0, 1], sections=[1, 1])):
         with pytest.raises(ValueError):
             B.Rope(device="cpu", **bad)
+
+
+def test_packed_arguments_are_the_structs():
+    """The calls pack their arguments with struct; every field must land where the ctypes structs have it."""
+    from paper_2609_39819_b200 import binding as B
+    for cls, packer in ((B.AppendArgs, B._APPEND), (B.AttendArgs, B._ATTEND)):
+        assert packer.size == C.sizeof(cls)
+        names = [f[0] for f in B.Batch._fields_] + [f[0] for f in cls._fields_[1:]]
+        x = cls.from_buffer_copy(packer.pack(*range(1, len(names) + 1)))
+        got = [getattr(x.b, f[0]) for f in B.Batch._fields_] + [getattr(x, f[0]) for f in cls._fields_[1:]]
+        assert got == list(range(1, len(names) + 1))

@@ -278,6 +278,28 @@ def test_attend_scores_that_climb_and_scores_of_one_huge_key(B):
         check_attend(s)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 72])
+@pytest.mark.parametrize("new", [1, 40, 200])
+def test_a_nan_or_an_overflow_stays_with_the_rows_that_see_it(B, new, dim):
+    """A NaN in a query spoils its row, a NaN in a key or a score beyond the range the rows that see the key; nobody else."""
+    import torch
+    for key_back in (0, 3, 6, 7, 29, 120):          # how far before the end the bad key lies: every way a power is made
+        for bad in (math.nan, math.inf):
+            s = Setup(B, [new, 5], [300, 40], heads=2, group=2, dim=dim, dtype="bf16", seed=9)
+            s.q[:, :, 0] = s.q[:, :, 0].abs() + 0.5
+            s.put()
+            at = s.kv[0] - 1 - key_back
+            s._chunk(int(s.host_table[0, at // BT]), 0)[at % BT, 1, 0] = bad
+            s.q[new - 1, 0, 3] = math.nan
+            got = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
+            s.eng.kv_check()
+            want_bad = torch.zeros(s.t, 4, dtype=torch.bool, device="cuda")
+            own = torch.arange(new, device="cuda") + 300
+            want_bad[:new, 2:] = (own >= at)[:, None]
+            want_bad[new - 1, 0] = True
+            assert torch.equal(torch.isnan(got).all(-1), want_bad) and torch.equal(torch.isfinite(got).all(-1), ~want_bad), (key_back, bad)
+
+
 # ---- append -----------------------------------------------------------------------------------------------
 def rotated(torch, x, pos, freqs, axis, rot, interleaved):
     """x: [tokens, heads, dim] in 64 bits, pos: [axes, tokens]. Also the size the rounding errors scale with."""

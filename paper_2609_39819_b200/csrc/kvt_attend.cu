@@ -4,6 +4,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cuda/ptx>
 
 #include <algorithm>
 
@@ -464,19 +465,26 @@ __device__ __forceinline__ u64 block_scan(u64 n, u64 *s_sum, u64 &all) {
 
 // Partial results in scratch: a header, a plan record per sequence, `rows` rows of head_dim sums per partial result, then the
 // (maximum, sum) pairs of all of them.
-//   kind 1 (few rows): header {work per CTA, -}, record {first unit's place in the work (64 bits), length of a unit, -}
+//   kind 1 (few rows): header: the stretches, record {first unit's place in the work (64 bits), length of a unit, -}
 //   kind 2:            header {any sequence cut, -}, record {first partial, pieces, tiles, -}
 __device__ __forceinline__ uint4 *scratch_plan(const AttendArgs &a) { return (uint4 *)a.scratch; }
 __host__ __device__ __forceinline__ u64 plan_bytes(u32 n_seqs) { return (16ull * (n_seqs + 1) + 255) & ~255ull; }
 __device__ __forceinline__ float *scratch_sums(const AttendArgs &a) { return (float *)(a.scratch + plan_bytes(a.b.n_seqs)); }
 
-// Kind 1: the blocks of all units, one after the other, are dealt out in equal stretches, one per CTA, so that every CTA
-// reads as much as any other whatever the lengths are; a unit that crosses a border is joined from its parts. A stretch is
-// `per` blocks, at least MIN_STRETCH. Order of units: sequence, tile, KV head. A unit counts UNIT_COST blocks more than it
-// has, at its front, for what it costs besides its blocks.
-constexpr u32 MIN_STRETCH = 8, UNIT_COST = 8;
+// Kind 1: the blocks of all units, one after the other, are dealt out in stretches, one per CTA, so that every CTA reads as much
+// as any other whatever the lengths are; a unit that crosses a border is joined from its parts. Order of units: sequence,
+// tile, KV head. A unit counts UNIT_COST blocks more than it has, at its front, for what it costs besides its blocks.
+// As many stretches as CTAs run at once, none below MIN_STRETCH. SMs do not get equal shares of the memory's bandwidth (with
+// equal stretches the last CTA ends 15 % after the mean), so of long work, LONG_STRETCH blocks per CTA and more, only the
+// first four fifths are dealt out like that; the rest goes in two short stretches per CTA to whoever is through first.
+constexpr u32 MIN_STRETCH = 8, LONG_STRETCH = 128, UNIT_COST = 8;
+struct Stretches {
+  u32 per, n1, per2;         // the first n1 are of `per` blocks, the others of `per2`
+  __device__ __forceinline__ u64 start(u32 c) const { return c <= n1 ? (u64)c * per : (u64)n1 * per + (u64)(c - n1) * per2; }
+  __device__ __forceinline__ u32 of(u64 x) const { const u64 y = (u64)n1 * per; return x < y ? (u32)(x / per) : n1 + (u32)((x - y) / per2); }
+};
 template <u32 THREADS>
-__device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publish, u64 &x, u64 &x_end, u32 &per, u32 &seq, u64 &base) {
+__device__ void find_stretch(const AttendArgs &a, u32 rows, u32 slots, bool publish, u64 &x, u64 &total, Stretches &st, u32 &seq, u64 &base) {
   __shared__ u64 s_sum[THREADS / 32], s_base;
   __shared__ u32 s_seq;
   auto units = [&](u32 s) -> u64 {
@@ -484,18 +492,24 @@ __device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publi
     const Seq q = load_seq(a.b, s, a.err);
     return (u64)seq_tiles(a, q, rows) * a.p.n_kv_heads * (seq_blocks(a, q, rows) + UNIT_COST);
   };
-  u64 total = 0, all, mine = 0, at = 0;
+  u64 all, mine = 0, at = 0;
+  total = 0;
   for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
     mine = units(s0 + threadIdx.x);
     at = block_scan<THREADS>(mine, s_sum, all);
     total += all;
   }
-  const u64 n = max(1ull, min((unsigned long long)ctas, (unsigned long long)(total / MIN_STRETCH)));
-  per = (u32)((total + n - 1) / n);
-  x = (u64)blockIdx.x * per;
-  x_end = min((unsigned long long)total, (unsigned long long)(x + per));
-  const bool any = x < total;
-  if (publish && threadIdx.x == 0) scratch_plan(a)[0] = make_uint4(per, 0, 0, 0);
+  if (gridDim.x >= 3 * slots && total >= (u64)LONG_STRETCH * slots) {
+    st.n1 = slots;
+    st.per = (u32)(total * 4 / 5 / slots);
+    st.per2 = (u32)((total - (u64)st.per * slots + 2 * slots - 1) / (2 * slots));
+  } else {
+    const u64 n = max(1ull, min((unsigned long long)min(slots, gridDim.x), (unsigned long long)(total / MIN_STRETCH)));
+    st.n1 = (u32)n; st.per = st.per2 = (u32)((total + n - 1) / n);
+  }
+  x = st.start(blockIdx.x);
+  const bool any = x < total;            // else the stretch is empty; seq and base are the first sequence's
+  if (publish && threadIdx.x == 0) scratch_plan(a)[0] = make_uint4(st.per, st.n1, st.per2, 0);
   u64 base0 = 0;
   for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += THREADS) {
     const u32 s = s0 + threadIdx.x;
@@ -507,10 +521,9 @@ __device__ bool find_stretch(const AttendArgs &a, u32 rows, u32 ctas, bool publi
     base0 += all;
     if (!publish && (!any || x < base0)) break;
   }
-  if (!any) return false;
+  seq = 0; base = 0;
   __syncthreads();
-  seq = s_seq; base = s_base;
-  return true;
+  if (any) { seq = s_seq; base = s_base; }
 }
 
 // Kind 2: tiles are cut into pieces, of at most so many blocks. With n pieces in all, the longest of them of p blocks, the
@@ -583,62 +596,78 @@ template <u32 C> __device__ __forceinline__ void load_sums(float (&v)[C], const 
   if (C == 4) *(float4 *)v = *(const float4 *)p; else *(float2 *)v = *(const float2 *)p;
 }
 
-// Kind 1, few rows of many parts: a CTA per row, a warp takes every fourth part.
-template <class T, u32 D>
-__global__ void __launch_bounds__(128) k_attend_join_split(AttendArgs a, u32 n_parts) {
+// Kind 1, few rows of many parts: a CTA per row, its warps take the parts in turn. Four warps, or sixteen where short
+// stretches make hundreds of parts (258 K tokens, 370 parts at most: NN us against NN).
+template <class T, u32 D, u32 WARPS>
+__global__ void __launch_bounds__(WARPS * 32) k_attend_join_split(AttendArgs a, u32 n_parts) {
   constexpr u32 C = D / 32, ROWS = 16;   // columns per lane; rows of a tile
-  __shared__ float s_acc[4][D], s_l[4];
+  __shared__ float s_acc[WARPS][D], s_l[WARPS], s_m[WARPS];
   const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.p.n_kv_heads;
   const float *sums = scratch_sums(a);
   const float2 *ml = (const float2 *)(sums + (u64)n_parts * ROWS * D);
   const u64 n_rows = (u64)a.b.n_tokens * a.n_q_heads;
-  u32 per = 0;
+  Stretches str{0, 0, 0};
   for (u64 id = blockIdx.x; id < n_rows; id += gridDim.x) {
     const u32 t = (u32)(id / a.n_q_heads), hq = (u32)(id - (u64)t * a.n_q_heads), seq = seq_of_token(a.b, t);
     const u32 h = hq / a.group;
-    if (!per) {                          // the batch's arrays are older than the kernel before this one
+    if (!str.per) {                      // the batch's arrays are older than the kernel before this one
       asm volatile("griddepcontrol.wait;" ::: "memory");
-      per = scratch_plan(a)[0].x;
-      if (!per) return;
+      const uint4 head = scratch_plan(a)[0];
+      str = Stretches{head.x, head.y, head.z};
+      if (!str.per) return;
     }
     if (seq == ~0u) continue;
     const uint4 plan = scratch_plan(a)[1 + seq];
     const u32 r = (t - a.b.q_start[seq]) * a.group + hq - h * a.group, tile = r / ROWS, row = r % ROWS;
-    const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z, e = s + plan.z, c0 = s / per, c1 = (e - 1) / per;
-    const u32 n = (u32)(c1 - c0) + 1, p0 = (u32)(2 * c0), odd = s > c0 * per;
+    const u64 s = ((u64)plan.y << 32 | plan.x) + ((u64)tile * H + h) * plan.z;
+    const u32 c0 = str.of(s), c1 = str.of(s + plan.z - 1), n = c1 - c0 + 1, p0 = 2 * c0, odd = s > str.start(c0);
     if (n <= 1) continue;
     if (p0 + 2ull * (n - 1) >= n_parts) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
     auto place = [&](u32 i) { return (p0 + 2 * i + (i == 0 ? odd : 0)) * ROWS + row; };
-    float m = -INFINITY;
-    for (u32 i = lane; i < n; i += 32) m = fmaxf(m, ml[place(i)].x);
-#pragma unroll
-    for (u32 o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, acc[C];
+    // a warp's parts: warp + y * WARPS, 32 of them at a time, a lane for the maximum and sum of each
+    float m = -INFINITY, l = 0.0f, acc[C];
 #pragma unroll
     for (u32 c = 0; c < C; ++c) acc[c] = 0.0f;
-#pragma unroll 8
-    for (u32 i = warp; i < n; i += 4) {
-      const u32 at = place(i);
-      const float2 x = ml[at];
-      float v[C];
-      load_sums<C>(v, sums + (u64)at * D + lane * C);
-      const float w = x.x == -INFINITY ? 0.0f : ex2(x.x - ref);      // a part without keys for this row holds zeros
-      l += w * x.y;
+    for (u32 i0 = warp; i0 < n; i0 += 32 * WARPS) {
+      const u32 mine = i0 + lane * WARPS, here = min(32u, (n - i0 + WARPS - 1) / WARPS);
+      const float2 x = mine < n ? ml[place(mine)] : make_float2(-INFINITY, 0.0f);
+      float now = x.x;
 #pragma unroll
-      for (u32 c = 0; c < C; ++c) acc[c] += w * v[c];
+      for (u32 o = 16; o; o /= 2) now = fmaxf(now, __shfl_xor_sync(~0u, now, o));
+      now = fmaxf(m, now);
+      const float ref = now == -INFINITY ? 0.0f : now, f = ex2(m - ref), w = ex2(x.x - ref);    // no keys for this row: weight 2^-inf, zeros
+      m = now;
+      l = l * f + warp_sum(w * x.y);
+#pragma unroll
+      for (u32 c = 0; c < C; ++c) acc[c] *= f;
+#pragma unroll 8
+      for (u32 y = 0; y < here; ++y) {
+        float v[C];
+        load_sums<C>(v, sums + (u64)place(i0 + y * WARPS) * D + lane * C);
+        const float wy = __shfl_sync(~0u, w, y);
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) acc[c] += wy * v[c];
+      }
     }
     __syncthreads();                     // the row before this one is read
 #pragma unroll
     for (u32 c = 0; c < C; ++c) s_acc[warp][lane * C + c] = acc[c];
-    if (lane == 0) s_l[warp] = l;
+    if (lane == 0) { s_l[warp] = l; s_m[warp] = m; }
     __syncthreads();
     if (warp) continue;
+    float all = -INFINITY;
 #pragma unroll
-    for (u32 w = 1; w < 4; ++w) {
-      l += s_l[w];
+    for (u32 w = 0; w < WARPS; ++w) all = fmaxf(all, s_m[w]);
+    const float ref = all == -INFINITY ? 0.0f : all, f0 = ex2(m - ref);
+    m = all; l *= f0;
 #pragma unroll
-      for (u32 c = 0; c < C; ++c) acc[c] += s_acc[w][lane * C + c];
+    for (u32 c = 0; c < C; ++c) acc[c] *= f0;
+#pragma unroll
+    for (u32 w = 1; w < WARPS; ++w) {
+      const float f = ex2(s_m[w] - ref);
+      l += f * s_l[w];
+#pragma unroll
+      for (u32 c = 0; c < C; ++c) acc[c] += f * s_acc[w][lane * C + c];
     }
     const float inv = l > 0.0f ? 1.0f / l : l;
     T *o = (T *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + lane * C;
@@ -770,228 +799,262 @@ template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(SPLIT_THREADS, 2)
-k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts) {
+k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts, u32 slots) {
   typedef SplitShape<D> S;
   extern __shared__ u8 smem_raw[];
   __shared__ __align__(8) u64 bars[SPLIT_WARPS * S::STAGES];
   __shared__ float s_ml[SPLIT_WARPS][SPLIT_ROWS][2];
+  __shared__ __align__(16) longlong2 s_next;             // answer to the request for another stretch
+  __shared__ __align__(8) u64 s_next_bar;
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
   const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8;
   if (lane == 0) {
     for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
+    if (warp == 0) bar_init(smem_addr(&s_next_bar), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
-  u64 x, x_end, base;
-  u32 per, seq;
-  if (!find_stretch<SPLIT_THREADS>(a, SPLIT_ROWS, gridDim.x, n_parts && blockIdx.x == 0, x, x_end, per, seq, base)) return;
-  const u64 x_begin = x;
+  u64 x, total, base;
+  Stretches str;
+  u32 seq, cta = blockIdx.x, taken = 0;                  // whose stretch this is; stretches taken over so far
+  find_stretch<SPLIT_THREADS>(a, SPLIT_ROWS, slots, n_parts && blockIdx.x == 0, x, total, str, seq, base);
   const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
   Seq q = load_seq(a.b, seq, a.err);
   u32 tiles = seq_tiles(a, q, SPLIT_ROWS), unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
   u32 it = 0;                            // stages this warp has used
   bool ok = true;
-
-  for (bool more = true; more;) {
-    // the unit x lies in, and the part of it in this stretch
-    while (x >= base + (u64)tiles * H * unit) {
-      base += (u64)tiles * H * unit;
-      if (++seq >= a.b.n_seqs) return;   // cannot happen: x < x_end <= all work
-      q = load_seq(a.b, seq, a.err);
-      tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
+  const bool steal = n_parts && gridDim.x > slots;       // else all CTAs run at once
+  // A CTA that has not been launched yet is called off and its stretch taken over; the answer arrives during the join of the
+  // last unit. CTAs with empty stretches do so too, which is sooner over than launching the others.
+  auto ask = [&]() {
+    if (tid == 0) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_expect(smem_addr(&s_next_bar), 16);
+      cuda::ptx::clusterlaunchcontrol_try_cancel(&s_next, &s_next_bar);
     }
-    const u32 u = (u32)((x - base) / unit), tile = u / H, h = u % H;
-    const u64 u0 = base + (u64)u * unit;
-    if (!n_parts && x > u0) {            // nothing is cut: a unit goes whole to the stretch it begins in
-      x = u0 + unit;
-      more = x < x_end;
-      continue;
-    }
-    const u64 x1 = n_parts ? min((unsigned long long)x_end, (unsigned long long)(u0 + unit)) : u0 + unit;
-    const bool direct = x == u0 && x1 == u0 + unit;
-    const u32 part = 2 * blockIdx.x + (x == u0 && x > x_begin);
-    const u32 n_rows = q.n * a.group, r0 = tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
-    u32 first, last, all_lo, all_hi;     // keys any row sees; keys every row sees
-    row_range(a, q, r0 / a.group, first, all_hi);
-    row_range(a, q, r1 / a.group, all_lo, last);
-    const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
-    const u32 o0 = (u32)(x - u0), o1 = (u32)(x1 - u0);
-    const u32 b0 = b_first + min(o0 > UNIT_COST ? o0 - UNIT_COST : 0, nb), b1 = b_first + min(o1 > UNIT_COST ? o1 - UNIT_COST : 0, nb);
-    const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
-    const u32 *row = a.b.table + seq * a.b.table_stride;
-    u32 slots = 0;                       // lane i: the slot of this warp's block number (i mod 32) of the current 32
-    auto load = [&](u32 i) {             // i-th block of this warp here; whole warp
-      if (i % 32 == 0) {
-        slots = i + lane < n_mine ? row[b0 + warp + (i + lane) * SPLIT_WARPS] : 0;
-        if (i + lane < n_mine && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
-      }
-      const u32 slot = __shfl_sync(~0u, slots, i % 32);
-      if (lane == 0) {
-        const u32 st = (it + i) % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
-        bar_expect(bar, 2 * S::BLOCK);
-        load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
-        load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
-      }
-    };
-    const u32 n_pro = min(n_mine, S::STAGES);
-    for (u32 i = 0; i < n_pro; ++i) load(i);
+  };
 
-    // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
-    u32 qf[D / 16][4];
-    u32 lo[2], hi[2];
-#pragma unroll
-    for (u32 y = 0; y < 2; ++y) {
-      const u32 r = min(r0 + lane / 4 + 8 * y, r1);     // rows behind the last one repeat it and are not written
-      row_range(a, q, r / a.group, lo[y], hi[y]);
-      const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
-      const bool even = ((uintptr_t)src & 3) == 0;
-#pragma unroll
-      for (u32 k = 0; k < D / 16; ++k)
-#pragma unroll
-        for (u32 z = 0; z < 2; ++z) {
-          const u16 *p = src + k * 16 + z * 8;
-          qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+  for (;;) {                             // a stretch
+    const u64 x_begin = x, x_end = min((unsigned long long)total, (unsigned long long)str.start(cta + 1));
+    bool asked = false;
+    for (bool more = x < total; more;) {
+      // the unit x lies in, and the part of it in this stretch
+      while (x >= base + (u64)tiles * H * unit) {
+        base += (u64)tiles * H * unit;
+        if (++seq >= a.b.n_seqs) return;   // cannot happen: x < x_end <= all work
+        q = load_seq(a.b, seq, a.err);
+        tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
+      }
+      const u32 u = (u32)((x - base) / unit), tile = u / H, h = u % H;
+      const u64 u0 = base + (u64)u * unit;
+      if (!n_parts && x > u0) {            // nothing is cut (one stretch per CTA): a unit goes whole to the one it begins in
+        x = u0 + unit;
+        more = x < x_end;
+        continue;
+      }
+      const u64 x1 = n_parts ? min((unsigned long long)x_end, (unsigned long long)(u0 + unit)) : u0 + unit;
+      const bool direct = x == u0 && x1 == u0 + unit;
+      const u32 part = 2 * cta + (x == u0 && x > x_begin);
+      const u32 n_rows = q.n * a.group, r0 = tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
+      u32 first, last, all_lo, all_hi;     // keys any row sees; keys every row sees
+      row_range(a, q, r0 / a.group, first, all_hi);
+      row_range(a, q, r1 / a.group, all_lo, last);
+      const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+      const u32 o0 = (u32)(x - u0), o1 = (u32)(x1 - u0);
+      const u32 b0 = b_first + min(o0 > UNIT_COST ? o0 - UNIT_COST : 0, nb), b1 = b_first + min(o1 > UNIT_COST ? o1 - UNIT_COST : 0, nb);
+      const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
+      const u32 *row = a.b.table + seq * a.b.table_stride;
+      u32 slots = 0;                       // lane i: the slot of this warp's block number (i mod 32) of the current 32
+      auto load = [&](u32 i) {             // i-th block of this warp here; whole warp
+        if (i % 32 == 0) {
+          slots = i + lane < n_mine ? row[b0 + warp + (i + lane) * SPLIT_WARPS] : 0;
+          if (i + lane < n_mine && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
         }
-    }
-    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (u32 n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (u32 y = 0; y < 4; ++y) o[n][y] = 0.0f;
-
-    for (u32 i = 0; ok && i < n_mine; ++i) {
-      const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
-      if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
-      const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
-      // scores of 16 keys: two column groups of 8
-      float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-      for (u32 k = 0; k < D / 16; ++k) {
-        u32 f[4];
-        ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
-        mma16816<T>(s[0], qf[k], f[0], f[1]);
-        mma16816<T>(s[1], qf[k], f[2], f[3]);
-      }
-      if (key0 + BT > q.kv) {            // the last block's tokens behind the length: whatever their values hold, weight 0
-        const u32 r = lane / 2;          // must not meet an Inf or a NaN
-        if (key0 + r >= q.kv)
-#pragma unroll
-          for (u32 c = 0; c < D / 16; ++c)
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
-        __syncwarp();
-      }
-      const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
-      float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-      for (u32 n = 0; n < 2; ++n)
-#pragma unroll
-        for (u32 y = 0; y < 4; ++y) {
-          const u32 key = key0 + n * 8 + (lane % 4) * 2 + (y & 1);
-          float v = s[n][y] * a.scale_log2;
-          if (!whole && (key < lo[y >> 1] || key >= hi[y >> 1])) v = -INFINITY;
-          s[n][y] = v;
-          top[y >> 1] = fmaxf(top[y >> 1], v);
+        const u32 slot = __shfl_sync(~0u, slots, i % 32);
+        if (lane == 0) {
+          const u32 st = (it + i) % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
+          bar_expect(bar, 2 * S::BLOCK);
+          load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
+          load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
         }
+      };
+      const u32 n_pro = min(n_mine, S::STAGES);
+      for (u32 i = 0; i < n_pro; ++i) load(i);
+
+      // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
+      u32 qf[D / 16][4];
+      u32 lo[2], hi[2];
 #pragma unroll
       for (u32 y = 0; y < 2; ++y) {
-        top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 1));
-        top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 2));
+        const u32 r = min(r0 + lane / 4 + 8 * y, r1);     // rows behind the last one repeat it and are not written
+        row_range(a, q, r / a.group, lo[y], hi[y]);
+        const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
+        const bool even = ((uintptr_t)src & 3) == 0;
+#pragma unroll
+        for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (u32 z = 0; z < 2; ++z) {
+            const u16 *p = src + k * 16 + z * 8;
+            qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+          }
       }
-      // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
-      // those below 1, and most blocks then need no rescaling.
-      if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+      float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) o[n][y] = 0.0f;
+
+      for (u32 i = 0; ok && i < n_mine; ++i) {
+        const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
+        if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
+        const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
+        // scores of 16 keys: two column groups of 8
+        float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (u32 k = 0; k < D / 16; ++k) {
+          u32 f[4];
+          ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
+          mma16816<T>(s[0], qf[k], f[0], f[1]);
+          mma16816<T>(s[1], qf[k], f[2], f[3]);
+        }
+        if (key0 + BT > q.kv) {            // the last block's tokens behind the length: whatever their values hold, weight 0
+          const u32 r = lane / 2;          // must not meet an Inf or a NaN
+          if (key0 + r >= q.kv)
+#pragma unroll
+            for (u32 c = 0; c < D / 16; ++c)
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+          __syncwarp();
+        }
+        const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+          for (u32 y = 0; y < 4; ++y) {
+            const u32 key = key0 + n * 8 + (lane % 4) * 2 + (y & 1);
+            float v = s[n][y] * a.scale_log2;
+            if (!whole && (key < lo[y >> 1] || key >= hi[y >> 1])) v = -INFINITY;
+            s[n][y] = v;
+            top[y >> 1] = fmaxf(top[y >> 1], v);
+          }
 #pragma unroll
         for (u32 y = 0; y < 2; ++y) {
-          const float now = fmaxf(m[y], top[y]), f = now == -INFINITY ? 1.0f : ex2(m[y] - now);
-          m[y] = now; l[y] *= f;
-#pragma unroll
-          for (u32 n = 0; n < D / 8; ++n) { o[n][2 * y] *= f; o[n][2 * y + 1] *= f; }
+          top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 1));
+          top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 2));
         }
+        // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
+        // those below 1, and most blocks then need no rescaling.
+        if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+#pragma unroll
+          for (u32 y = 0; y < 2; ++y) {
+            const float now = fmaxf(m[y], top[y]), f = now == -INFINITY ? 1.0f : ex2(m[y] - now);
+            m[y] = now; l[y] *= f;
+#pragma unroll
+            for (u32 n = 0; n < D / 8; ++n) { o[n][2 * y] *= f; o[n][2 * y + 1] *= f; }
+          }
+        }
+        const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+#pragma unroll
+        for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+          for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
+        const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
+                          Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
+#pragma unroll
+        for (u32 n = 0; n < D / 16; ++n) {
+          u32 f[4];
+          ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
+          mma16816<T>(o[2 * n], p, f[0], f[1]);
+          mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+        }
+        __syncwarp();                      // the stage is read: refill it
+        if (i + S::STAGES < n_mine) load(i + S::STAGES);
       }
-      const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-#pragma unroll
-      for (u32 n = 0; n < 2; ++n)
-#pragma unroll
-        for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
-      const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
-                        Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
-#pragma unroll
-      for (u32 n = 0; n < D / 16; ++n) {
-        u32 f[4];
-        ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
-        mma16816<T>(o[2 * n], p, f[0], f[1]);
-        mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
-      }
-      __syncwarp();                      // the stage is read: refill it
-      if (i + S::STAGES < n_mine) load(i + S::STAGES);
-    }
-    it += n_mine;
+      it += n_mine;
+      if (steal && x1 >= x_end) { ask(); asked = true; }
 
-    // join the four warps: sums through the (now idle) rings
+      // join the four warps: sums through the (now idle) rings
 #pragma unroll
-    for (u32 y = 0; y < 2; ++y) {
-      l[y] += __shfl_xor_sync(~0u, l[y], 1);
-      l[y] += __shfl_xor_sync(~0u, l[y], 2);
-      if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * y][0] = m[y]; s_ml[warp][lane / 4 + 8 * y][1] = l[y]; }
-    }
-    constexpr u32 LD = D + 8;            // row pitch in floats: the four rows of a quarter warp fall on different banks
-    static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
-    float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
-#pragma unroll
-    for (u32 n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (u32 y = 0; y < 2; ++y)
-        *(float2 *)&so[(lane / 4 + 8 * y) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * y], o[n][2 * y + 1]);
-    if (__syncthreads_or(!ok)) { ok = false; break; }      // a wait ran out somewhere: nothing is written
-    const u32 r = tid / 8, c0 = (tid % 8) * 4;             // thread: row r, four columns out of every 32
-    if (r0 + r <= r1 && (direct || part < n_parts)) {
-      float mm = -INFINITY, ll = 0.0f, f[SPLIT_WARPS];
-#pragma unroll
-      for (u32 y = 0; y < SPLIT_WARPS; ++y) mm = fmaxf(mm, s_ml[y][r][0]);
-      const float ref = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll
-      for (u32 y = 0; y < SPLIT_WARPS; ++y) { f[y] = ex2(s_ml[y][r][0] - ref); ll += f[y] * s_ml[y][r][1]; }
-      const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
-      const float *sum = (const float *)(smem_raw + (ring0 - smem_addr(smem_raw))) + r * LD;
-      const float inv = !direct ? 1.0f : ll > 0.0f ? 1.0f / ll : ll;
-      u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
-      float *const sums = scratch_sums(a) + ((u64)part * SPLIT_ROWS + r) * D;
-#pragma unroll
-      for (u32 c = c0; c < D; c += 32) {
-        float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-        for (u32 y = 0; y < SPLIT_WARPS; ++y) {
-          const float4 z = *(const float4 *)(sum + y * (S::RING / 4) + c);
-          v.x += f[y] * z.x; v.y += f[y] * z.y; v.z += f[y] * z.z; v.w += f[y] * z.w;
-        }
-        if (direct) {
-          const u32 p0 = Elem<T>::down(v.x * inv, v.y * inv), p1 = Elem<T>::down(v.z * inv, v.w * inv);
-          u16 *d = out + c;
-          if (((uintptr_t)d & 7) == 0) *(uint2 *)d = make_uint2(p0, p1);
-          else { d[0] = (u16)p0; d[1] = (u16)(p0 >> 16); d[2] = (u16)p1; d[3] = (u16)(p1 >> 16); }
-        } else {
-          *(float4 *)(sums + c) = v;
-        }
+      for (u32 y = 0; y < 2; ++y) {
+        l[y] += __shfl_xor_sync(~0u, l[y], 1);
+        l[y] += __shfl_xor_sync(~0u, l[y], 2);
+        if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * y][0] = m[y]; s_ml[warp][lane / 4 + 8 * y][1] = l[y]; }
       }
-      if (tid % 8 == 0) {
-        if (!direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * SPLIT_ROWS * D))[part * SPLIT_ROWS + r] = make_float2(mm, ll);
-        else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (mm + log2f(ll)) * 0.69314718055994531f;
+      constexpr u32 LD = D + 8;            // row pitch in floats: the four rows of a quarter warp fall on different banks
+      static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
+      float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
+#pragma unroll
+      for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+        for (u32 y = 0; y < 2; ++y)
+          *(float2 *)&so[(lane / 4 + 8 * y) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * y], o[n][2 * y + 1]);
+      if (__syncthreads_or(!ok)) { ok = false; break; }      // a wait ran out somewhere: nothing is written
+      const u32 r = tid / 8, c0 = (tid % 8) * 4;             // thread: row r, four columns out of every 32
+      if (r0 + r <= r1 && (direct || part < n_parts)) {
+        float mm = -INFINITY, ll = 0.0f, f[SPLIT_WARPS];
+#pragma unroll
+        for (u32 y = 0; y < SPLIT_WARPS; ++y) mm = fmaxf(mm, s_ml[y][r][0]);
+        const float ref = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+        for (u32 y = 0; y < SPLIT_WARPS; ++y) { f[y] = ex2(s_ml[y][r][0] - ref); ll += f[y] * s_ml[y][r][1]; }
+        const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
+        const float *sum = (const float *)(smem_raw + (ring0 - smem_addr(smem_raw))) + r * LD;
+        const float inv = !direct ? 1.0f : ll > 0.0f ? 1.0f / ll : ll;
+        u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
+        float *const sums = scratch_sums(a) + ((u64)part * SPLIT_ROWS + r) * D;
+#pragma unroll
+        for (u32 c = c0; c < D; c += 32) {
+          float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+          for (u32 y = 0; y < SPLIT_WARPS; ++y) {
+            const float4 z = *(const float4 *)(sum + y * (S::RING / 4) + c);
+            v.x += f[y] * z.x; v.y += f[y] * z.y; v.z += f[y] * z.z; v.w += f[y] * z.w;
+          }
+          if (direct) {
+            const u32 p0 = Elem<T>::down(v.x * inv, v.y * inv), p1 = Elem<T>::down(v.z * inv, v.w * inv);
+            u16 *d = out + c;
+            if (((uintptr_t)d & 7) == 0) *(uint2 *)d = make_uint2(p0, p1);
+            else { d[0] = (u16)p0; d[1] = (u16)(p0 >> 16); d[2] = (u16)p1; d[3] = (u16)(p1 >> 16); }
+          } else {
+            *(float4 *)(sums + c) = v;
+          }
+        }
+        if (tid % 8 == 0) {
+          if (!direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * SPLIT_ROWS * D))[part * SPLIT_ROWS + r] = make_float2(mm, ll);
+          else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (mm + log2f(ll)) * 0.69314718055994531f;
+        }
+      } else if (r0 + r <= r1 && tid == 0) {
+        kv_err(a.err, KVERR_RANGE);        // cannot happen: two parts per CTA
       }
-    } else if (r0 + r <= r1 && tid == 0) {
-      kv_err(a.err, KVERR_RANGE);        // cannot happen: two parts per CTA
+      x = x1;
+      more = x < x_end;
+      if (more) {                          // the rings are read: loads may write them again
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+      }
     }
-    x = x1;
-    more = x < x_end;
-    if (more) {                          // the rings are read: loads may write them again
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncthreads();
+    if (!ok || !steal) break;
+    if (!asked) ask();
+    if (__syncthreads_or(!bar_wait(smem_addr(&s_next_bar), taken & 1))) { ok = false; break; }
+    const longlong2 answer = s_next;
+    if (!cuda::ptx::clusterlaunchcontrol_query_cancel_is_canceled(answer)) break;    // there is none left to take
+    cta = cuda::ptx::clusterlaunchcontrol_query_cancel_get_first_ctaid_x<u32>(answer);
+    ++taken;
+    x = str.start(cta);
+    if (x < base) {                        // CTAs are called off in ascending order as a rule: then the search goes on from here
+      seq = 0; base = 0;
+      q = load_seq(a.b, 0, a.err);
+      tiles = seq_tiles(a, q, SPLIT_ROWS); unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // rings and answer are read
+    __syncthreads();
   }
   if (!ok) {                             // let the copies in flight land, for a while, before the CTA ends
     if (lane == 0) kv_err(a.err, KVERR_WAIT);
     for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
+    for (u32 y = 0; y < 2; ++y) bar_wait(smem_addr(&s_next_bar), y);
   }
 }
 
@@ -1573,9 +1636,9 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 
 }
 
 template <class... Exp, class... Act>
-static cudaError_t launch_join(void (*kern)(Exp...), u64 ctas, u32 sms, cudaStream_t s, u32 *launches, Act... args) {
+static cudaError_t launch_join(void (*kern)(Exp...), u32 threads, u64 ctas, u32 sms, cudaStream_t s, u32 *launches, Act... args) {
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((u32)std::min<u64>(ctas, 8ull * sms)); c.blockDim = dim3(128); c.stream = s;
+  c.gridDim = dim3((u32)std::min<u64>(ctas, 8ull * sms)); c.blockDim = dim3(threads); c.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
@@ -1604,7 +1667,9 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     // there is a unit for every SM. One sequence of 200 tokens, 8 heads of 128: 7.9 us against 11.3 cut, of 500 tokens 11.0
     // against 9.0; 32 sequences of 500: 13.1 against 19.3, of 1000 27.8 against 31.8.
     const bool cut = a.b.max_blocks > (units < (u64)sm_count ? 16u : 64u);
-    p.grid = (u32)std::max<u64>(1, std::min<u64>(2ull * sm_count, cut ? units * pieces : units));
+    const u64 most = units * (a.b.max_blocks + UNIT_COST);           // work, if every sequence fills its table row
+    p.grid = (u32)std::max<u64>(1, cut ? (most >= 2ull * sm_count * LONG_STRETCH ? 6ull * sm_count : std::min<u64>(2ull * sm_count, units * pieces))
+                                       : std::min<u64>(2ull * sm_count, units));
     p.parts = p.grid > 1 && cut ? 2 * p.grid : 0;
   } else {
     p.kind = 2;
@@ -1630,10 +1695,12 @@ template <class T, u32 D>
 static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
   cudaError_t r = allow_smem(k_attend_split<T, D>, 2 + (D == 128) * 2 + a.fp16, SplitShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
-  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts);
+  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts, 2 * p.sms);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
-  return launch_join(k_attend_join_split<T, D>, (u64)a.b.n_tokens * a.n_q_heads, p.sms, s, launches, a, p.parts);
+  const u64 rows = (u64)a.b.n_tokens * a.n_q_heads;
+  if (p.grid > 2 * p.sms) return launch_join(k_attend_join_split<T, D, 16>, 512, rows, p.sms, s, launches, a, p.parts);
+  return launch_join(k_attend_join_split<T, D, 4>, 128, rows, p.sms, s, launches, a, p.parts);
 }
 
 template <class T, u32 D>
@@ -1643,7 +1710,7 @@ static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvM
   k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
-  return launch_join(k_attend_join_tc<T, D>, ((u64)a.b.n_tokens * ((a.n_q_heads + 3) / 4) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);
+  return launch_join(k_attend_join_tc<T, D>, 128, ((u64)a.b.n_tokens * ((a.n_q_heads + 3) / 4) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);
 }
 
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {

@@ -597,7 +597,7 @@ template <u32 C> __device__ __forceinline__ void load_sums(float (&v)[C], const 
 }
 
 // Kind 1, few rows of many parts: a CTA per row, its warps take the parts in turn. Four warps, or sixteen where short
-// stretches make hundreds of parts (258 K tokens, 370 parts at most: NN us against NN).
+// stretches make hundreds of parts (258 K tokens, 370 parts at most: 171 us for both kernels against 183).
 template <class T, u32 D, u32 WARPS>
 __global__ void __launch_bounds__(WARPS * 32) k_attend_join_split(AttendArgs a, u32 n_parts) {
   constexpr u32 C = D / 32, ROWS = 16;   // columns per lane; rows of a tile

@@ -12,6 +12,9 @@ larger than L2, a few GB on the device at most, a handful of launches).
     python -m paper_2609_39819_b200.profile_case mover_remote  # host tier <-> third tier, third tier -> HBM
     python -m paper_2609_39819_b200.profile_case mover_ctas # bandwidth against the number of thread blocks the mover may use
     python -m paper_2609_39819_b200.profile_case overlap    # a GEMM loop beside an offload: what the mover's grid size costs
+    python -m paper_2609_39819_b200.profile_case attend_step    # one new token on 258 K cached ones (8 x 128 KV heads, groups of 4)
+    python -m paper_2609_39819_b200.profile_case attend_prompt  # 4096 new tokens, the same heads
+    python -m paper_2609_39819_b200.profile_case append         # 8192 new tokens into the pool, rotated, with their queries
     python -m paper_2609_39819_b200.profile_case sweep      # C5: movement bandwidth sweep (markdown table)
 Each prints one line with CUDA-event timings of its launches.
 """
@@ -319,6 +322,25 @@ def main(case: str):
         st = eng.get_stats()
         print(f"c4: {n_res} resident, {n_calls} calls x 16128 blocks; hits {st['hits_hbm']}, inserted {st['inserted']}, "
               f"adopted {st['adopted']}, tombstones {st['tombstones']}; {res}")
+    elif case in ("attend_step", "attend_prompt", "append"):
+        n, past = {"attend_step": (1, 258047), "attend_prompt": (4096, 0), "append": (8192, 0)}[case]
+        kv, blocks = n + past, (n + past + 15) // 16
+        eng = B.Engine(n_layers=1, n_kv_heads=8, head_dim=128, n_hbm_blocks=blocks + 8, n_host_blocks=0, max_contexts=1,
+                       max_tokens=64, max_messages=16, zero_pools=False)
+        eng.hbm_pool.view(torch.bfloat16).normal_()
+        table = torch.from_numpy(W.ids_c5(1, blocks, blocks + 8, True).view(np.int32)).cuda()[None]
+        start = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        length = torch.tensor([kv], dtype=torch.int32, device="cuda")
+        q, k, v = (torch.empty(n, h, 128, dtype=torch.bfloat16, device="cuda").normal_() for h in (32, 8, 8))
+        rope = B.Rope(128)
+        if case == "append":
+            ms = _events(torch, lambda: eng.append_kv(0, k, v, table, start, length, rope=rope, q=q), 4)
+            print(f"append: {n} tokens, ms {ms}, read+write GB/s {[round(2 * n * 48 * 256 / m / 1e6, 1) for m in ms]}")
+        else:
+            ms = _events(torch, lambda: eng.attend(0, q, table, start, length, max_q_len=n), 4)
+            pairs = n * past + n * (n + 1) // 2
+            print(f"{case}: {n} new tokens on {past}, ms {ms}, K+V GB/s {[round(kv * 4096 / m / 1e6, 1) for m in ms]}, "
+                  f"TFLOP/s {[round(4 * pairs * 32 * 128 / m / 1e9, 1) for m in ms]}")
     elif case == "sweep":
         sweep(torch, B, W)
     else:

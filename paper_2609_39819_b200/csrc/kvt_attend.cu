@@ -1677,8 +1677,15 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     p.grid = (u32)std::min<u64>(tiles(p.rows), 0x7FFFFFFFu);
     return p;
   }
-  // One tile of 16 rows reads K and V once; with more rows than that the other kernel's taller tiles still do.
-  if ((u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group <= SPLIT_ROWS) {
+  // One tile of 16 rows reads K and V once. With more rows the kernel for few rows reads them once per tile, but it starts,
+  // ends and joins 8 us sooner, which decides when there is little to do: up to 8 K blocks (of 16 rows and one KV head, as
+  // many as fit the table rows), or 32 K where a sequence has two tiles only. Measured, us of few / many rows, heads of 128:
+  //   64 tokens 6.6 / 12.2, 128 tokens 8.2 / 12.2, 200 tokens 16.3 / 14.0 (1.5 K, 4.1 K, 8.4 K blocks; groups of 4, 8 KV heads)
+  //   32 on 1000 16.9 / 21.8, 64 on 1000 22.9 / 23.8, 100 on 2000 38.6 / 28.8 (4.7 K, 9.6 K, 28 K)
+  //   two tiles: 8 on 4000 16.3 / 27.6, 8 x 8 on 2000 28.4 / 32.0, 32 x 8 on 500 24.5 / 29.0 (4.1 K, 25 K, 30 K)
+  const u64 rows = (u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group,
+            few = tiles(SPLIT_ROWS) * H * ((u64)a.b.max_blocks + UNIT_COST);
+  if (rows <= SPLIT_ROWS || few <= 8192 || (rows <= 2 * SPLIT_ROWS && few <= 32768)) {
     p.kind = 1;
     p.rows = SPLIT_ROWS;
     const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, ((u64)a.b.max_blocks + UNIT_COST) / MIN_STRETCH);

@@ -149,11 +149,27 @@ class Setup:
             t0 += n
         return out, lse, tol, tol_l
 
+    def widened(self):
+        """The block table with rows that could hold 320 K tokens more: the kernel for prompts is taken for fewer of them."""
+        w = self.torch.full((self.table.shape[0], self.table.shape[1] + 20000), 0x7FFFFFF0, dtype=self.torch.int32, device="cuda")
+        w[:, :self.table.shape[1]] = self.table
+        return w
+
     def bits(self):
         return [p.clone().contiguous().view(self.torch.int16) for p in self.pools]
 
 
-def check_attend(s, window=0, causal=True, scale=None, max_q_len="own", want_lse=True):
+def check_attend(s, window=0, causal=True, scale=None, want_lse=True):
+    """The result must not depend on what the kernel is chosen by: the hint, and how much a table row could hold."""
+    torch = s.torch
+    wide = s.widened()
+    check_one(s, s.table, max(s.new), window, causal, scale, want_lse)
+    check_one(s, wide, None, window, causal, scale, want_lse)       # many rows: the kernel for prompts
+    check_one(s, s.table, 1, window, causal, scale, want_lse)       # the kernel for few rows
+    check_one(s, wide, 1, window, causal, scale, want_lse)
+
+
+def check_one(s, table, max_q_len, window, causal, scale, want_lse):
     torch = s.torch
     hq = s.heads * s.group
     guard = 7.25
@@ -161,8 +177,8 @@ def check_attend(s, window=0, causal=True, scale=None, max_q_len="own", want_lse
     view = out[:, ::2, 1:1 + s.dim] if s.rows % 2 else out[:, :hq, :s.dim]
     lse = torch.full((s.rows, hq), guard, device="cuda") if want_lse else None
     before = s.bits()
-    s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len, max_q_len=max(s.new) if max_q_len == "own" else max_q_len,
-                 window=window, causal=causal, scale=scale, out=view, lse=lse)
+    s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len, max_q_len=max_q_len, window=window, causal=causal, scale=scale,
+                 out=view, lse=lse)
     s.eng.kv_check()
     want, wl, tol, tl = s.reference(window, causal, scale)
     got = view[:s.t].double()
@@ -200,7 +216,6 @@ def test_attend_shapes(B, batch, dtype, layout, heads, group, dim):
     s = Setup(B, *BATCHES[batch], heads=heads, group=group, dim=dim, dtype=dtype, layout=layout, seed=len(batch) + dim, q_gain=2.0)
     s.put()
     check_attend(s)
-    check_attend(s, max_q_len=None)
 
 
 @pytest.mark.parametrize("dim", [64, 128, 32])
@@ -254,6 +269,18 @@ def test_attend_long(B, dim, new, past, heads, group):
     check_attend(s)
 
 
+@pytest.mark.parametrize("past", [[80000], [30011, 50000, 100, 0]])
+def test_attend_work_that_ctas_take_over(B, past):
+    """Enough blocks that part of the work is left to the CTAs that are through first; who takes what must not show."""
+    import torch
+    s = Setup(B, [1] * len(past), past, heads=8, group=2, dim=64, layers=1, layer=0, q_gain=2.0, seed=77)
+    s.put()
+    check_attend(s)
+    first = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
+    for _ in range(10):
+        assert torch.equal(first, s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len))
+
+
 def test_attend_many_sequences(B):
     rng = np.random.default_rng(5)
     n = 700
@@ -291,13 +318,15 @@ def test_a_nan_or_an_overflow_stays_with_the_rows_that_see_it(B, new, dim):
             at = s.kv[0] - 1 - key_back
             s._chunk(int(s.host_table[0, at // BT]), 0)[at % BT, 1, 0] = bad
             s.q[new - 1, 0, 3] = math.nan
-            got = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
-            s.eng.kv_check()
             want_bad = torch.zeros(s.t, 4, dtype=torch.bool, device="cuda")
             own = torch.arange(new, device="cuda") + 300
             want_bad[:new, 2:] = (own >= at)[:, None]
             want_bad[new - 1, 0] = True
-            assert torch.equal(torch.isnan(got).all(-1), want_bad) and torch.equal(torch.isfinite(got).all(-1), ~want_bad), (key_back, bad)
+            for table in (s.table, s.widened()):
+                got = s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len)
+                s.eng.kv_check()
+                assert torch.equal(torch.isnan(got).all(-1), want_bad), (key_back, bad)
+                assert torch.equal(torch.isfinite(got).all(-1), ~want_bad), (key_back, bad)
 
 
 # ---- append -----------------------------------------------------------------------------------------------
@@ -456,11 +485,13 @@ def test_refusals(B):
 
 
 @pytest.mark.parametrize("dim", [64, 128, 40])
-@pytest.mark.parametrize("new", [1, 50])
-def test_bad_slots_and_lengths_are_reported_and_harmless(B, dim, new):
+@pytest.mark.parametrize("new,wide", [(1, False), (50, False), (50, True)])
+def test_bad_slots_and_lengths_are_reported_and_harmless(B, dim, new, wide):
     import torch
     s = Setup(B, [new, new], [100, 200], heads=2, group=4, dim=dim, tail=True, seed=41)
     s.put()
+    if wide:
+        s.table = s.widened()
     sound = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
     s.eng.kv_check()
 
@@ -512,12 +543,14 @@ def test_nothing_to_do(B):
 
 
 # ---- streams, graphs, the set as it is used --------------------------------------------------------------------
-@pytest.mark.parametrize("new", [1, 60])
-def test_captured_and_replayed_with_other_lengths(B, new):
+@pytest.mark.parametrize("new,wide", [(1, False), (1, True), (60, False), (60, True)])
+def test_captured_and_replayed_with_other_lengths(B, new, wide):
     """Two graphs of the same engine, replayed at once on two streams, with lengths changed after the capture."""
     import torch
     s = Setup(B, [new] * 3, [900, 40, 2000], heads=2, group=4, dim=128, seed=61)
     s.put()
+    if wide:
+        s.table = s.widened()
     rope = B.Rope(128)
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
     kv = [s.kv_len.clone(), s.kv_len.clone()]
@@ -560,9 +593,10 @@ def test_same_call_gives_the_same_bits(B):
     for new, past in (([1] * 20, list(range(0, 6000, 300))), ([90, 300], [3000, 20])):
         s = Setup(B, new, past, heads=2, group=4, dim=128, seed=71)
         s.put()
-        first = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
-        for _ in range(5):
-            assert torch.equal(first, s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len))
+        for table in (s.table, s.widened()):
+            first = s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len)
+            for _ in range(5):
+                assert torch.equal(first, s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len))
 
 
 @pytest.mark.parametrize("layout", [0, 1])

@@ -394,7 +394,8 @@ int32_t kvt_hash_tokens_noalloc(const uint32_t *d_tokens, uint64_t n_tokens, uin
  * step sequence s holds kv_len[s] tokens, the new ones last: its i-th new token has index
  * kv_len[s] - (q_start[s+1] - q_start[s]) + i in the sequence. Rows behind q_start[n_seqs] belong to nobody: they are
  * neither read nor written (a padded batch). Starts that decrease or pass n_tokens and lengths beyond the table row
- * are cut to what fits and set the error word. */
+ * are cut to what fits and set the error word; a batch whose starts go up and down so that tokens belong to several
+ * sequences may be left undone. */
 typedef struct kvt_batch {
   uint32_t n_seqs;
   uint32_t n_tokens;

@@ -560,6 +560,8 @@ class Engine:
         by default the tokens' indices in their sequences. Asynchronous on the current stream; ids and lengths outside
         their ranges are skipped and reported by kv_check()."""
         torch = self.torch
+        if layer < 0:
+            raise ValueError("append_kv: layer cannot be negative")
         dt = self._kv_dtype(k, "append_kv")
         t, h, d = k.shape[0], self.n_kv_heads, self.head_dim
         kp, kts, khs = self._kv_tensor(k, "append_kv: k", (t, h, d), k.dtype)
@@ -612,6 +614,8 @@ class Engine:
         if known (chooses the kernel, not the result). out, lse ([tokens, heads] float32, contiguous): written if
         given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream."""
         torch = self.torch
+        if layer < 0 or (max_q_len or 0) < 0 or (window or 0) < 0:
+            raise ValueError("attend: layer, max_q_len and window cannot be negative")
         dt = self._kv_dtype(q, "attend")
         t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
         qp, qts, qhs = self._kv_tensor(q, "attend: q", (t, hq, self.head_dim), q.dtype)

@@ -64,6 +64,9 @@ struct Where { u32 seq, index; bool ok; };
 template <bool WARP>
 __device__ __forceinline__ Where find_token(const KvBatch &b, u32 t, u32 *err) {
   u32 seq = 0;
+  if (t == 0)                                        // one of the tokens looks all starts over
+    for (u32 s = threadIdx.x % (WARP ? 32 : blockDim.x); s < b.n_seqs; s += WARP ? 32 : blockDim.x)
+      if (b.q_start[s] > b.q_start[s + 1]) kv_err(err, KVERR_RANGE);
   if (WARP) {
     for (u32 s0 = 0; s0 < b.n_seqs; s0 += 32) {
       const u32 s = s0 + (threadIdx.x & 31);
@@ -503,7 +506,7 @@ struct Stretches {
   __device__ __forceinline__ u32 of(u64 x) const { const u64 y = (u64)n1 * per; return x < y ? (u32)(x / per) : n1 + (u32)((x - y) / per2); }
 };
 template <u32 THREADS>
-__device__ void find_stretch(const AttendArgs &a, u32 rows, u32 slots, bool publish, u64 &x, u64 &total, Stretches &st, u32 &seq, u64 &base) {
+__device__ void find_stretch(const AttendArgs &a, u32 rows, u32 slots, u64 most, bool publish, u64 &x, u64 &total, Stretches &st, u32 &seq, u64 &base) {
   __shared__ u64 s_sum[THREADS / 32], s_base;
   __shared__ u32 s_seq;
   auto units = [&](u32 s) -> u64 {
@@ -518,6 +521,9 @@ __device__ void find_stretch(const AttendArgs &a, u32 rows, u32 slots, bool publ
     at = block_scan<THREADS>(mine, s_sum, all);
     total += all;
   }
+  // More work than non-overlapping sequences can bring (starts that go up and down make the same tokens count again and
+  // again): nothing is done. load_seq has set the error word.
+  if (total > most) total = 0;
   if (gridDim.x >= 3 * slots && total >= (u64)LONG_STRETCH * slots) {
     st.n1 = slots;
     st.per = (u32)(total * 4 / 5 / slots);
@@ -561,22 +567,23 @@ __device__ __forceinline__ float warp_sum(float x) {
   for (u32 o = 16; o; o /= 2) x += __shfl_xor_sync(~0u, x, o);
   return x;
 }
-struct Cut { u32 longest; float share; };
-__device__ __forceinline__ Cut weigh_cuts(const AttendArgs &a, u32 rows, u32 most, u32 sms, u32 warp, u32 warps, float *s_cost, Seq &q) {
+struct Cut { u32 longest; float share; bool sound; };    // sound: no more tiles than the host reckons with
+__device__ __forceinline__ Cut weigh_cuts(const AttendArgs &a, u32 rows, u32 most, u32 sms, float most_tiles, u32 warp, u32 warps, float *s_cost, Seq &q) {
   const u32 lane = threadIdx.x & 31;
   const float H = a.p.n_kv_heads;
   u32 longest = 1, tiles = 0, nb = 0;
-  float blocks = 0.0f;
+  float blocks = 0.0f, all_tiles = 0.0f;
   q = Seq{0, 0, 0};
   for (u32 s = lane; s < a.b.n_seqs; s += 32) {
     const Seq x = load_seq(a.b, s, a.err);
     if (s == lane) q = x;
     if (!x.n) continue;
     tiles = seq_tiles(a, x, rows); nb = seq_blocks(a, x, rows);
-    blocks += (float)tiles * nb;
+    blocks += (float)tiles * nb; all_tiles += tiles;
     longest = max(longest, nb);
   }
   Cut c;
+  c.sound = warp_sum(all_tiles) <= most_tiles * 1.001f;
   c.longest = __reduce_max_sync(~0u, longest);
   c.share = warp_sum(blocks) * H / sms;
   if (c.longest <= MIN_PIECE || !most || a.b.n_seqs > 32) return c;
@@ -818,7 +825,7 @@ template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(SPLIT_THREADS, 2)
-k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts, u32 slots) {
+k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts, u32 slots, u64 most) {
   typedef SplitShape<D> S;
   extern __shared__ u8 smem_raw[];
   __shared__ __align__(8) u64 bars[SPLIT_WARPS * S::STAGES];
@@ -838,7 +845,7 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
   u64 x, total, base;
   Stretches str;
   u32 seq, cta = blockIdx.x, taken = 0;                  // whose stretch this is; stretches taken over so far
-  find_stretch<SPLIT_THREADS>(a, SPLIT_ROWS, slots, n_parts && blockIdx.x == 0, x, total, str, seq, base);
+  find_stretch<SPLIT_THREADS>(a, SPLIT_ROWS, slots, most, n_parts && blockIdx.x == 0, x, total, str, seq, base);
   const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
   Seq q = load_seq(a.b, seq, a.err);
   u32 tiles = seq_tiles(a, q, SPLIT_ROWS), unit = seq_blocks(a, q, SPLIT_ROWS) + UNIT_COST;
@@ -1183,7 +1190,7 @@ constexpr u32 TC_JOBS = 4, TC_PARTS = 2;      // P is handed to the second produ
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
-k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts) {
+k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts, u64 most_tiles) {
   typedef TcShape<D> S;
   constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
   extern __shared__ u8 smem_raw[];
@@ -1213,7 +1220,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   }
   if (warp == 9 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &maps.tail : &maps.pool) : "memory");
   Seq mine;                              // the sequence of this lane among the first 32
-  const Cut cut = weigh_cuts(a, TC_ROWS, n_parts, gridDim.x, warp, TC_THREADS / 32, s_cost, mine);
+  const Cut cut = weigh_cuts(a, TC_ROWS, n_parts, gridDim.x, (float)most_tiles, warp, TC_THREADS / 32, s_cost, mine);
   tc_before();
   __syncthreads();
   tc_after();
@@ -1253,7 +1260,9 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       const u32 s = s0 + lane;
       tiles = pieces = 0;
       u32 length = 0;
-      if (s < a.b.n_seqs) {
+      // starts that go up and down make the same tokens count again and again: then nothing is done (load_seq has set the
+      // error word)
+      if (s < a.b.n_seqs && cut.sound) {
         if (s0) q = load_seq(a.b, s, a.err);
         tiles = seq_tiles(a, q, TC_ROWS);
         const u32 nb = seq_blocks(a, q, TC_ROWS);
@@ -1693,14 +1702,15 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     // there is a unit for every SM. One sequence of 200 tokens, 8 heads of 128: 7.9 us against 11.3 cut, of 500 tokens 11.0
     // against 9.0; 32 sequences of 500: 13.1 against 19.3, of 1000 27.8 against 31.8.
     const bool cut = a.b.max_blocks > (units < (u64)sm_count ? 16u : 64u);
-    const u64 most = units * (a.b.max_blocks + UNIT_COST);           // work, if every sequence fills its table row
-    p.grid = (u32)std::max<u64>(1, cut ? (most >= 2ull * sm_count * LONG_STRETCH ? 6ull * sm_count : std::min<u64>(2ull * sm_count, units * pieces))
+    p.most = units * (a.b.max_blocks + UNIT_COST);                   // work, if every sequence fills its table row
+    p.grid = (u32)std::max<u64>(1, cut ? (p.most >= 2ull * sm_count * LONG_STRETCH ? 6ull * sm_count : std::min<u64>(2ull * sm_count, units * pieces))
                                        : std::min<u64>(2ull * sm_count, units));
     p.parts = p.grid > 1 && cut ? 2 * p.grid : 0;
   } else {
     p.kind = 2;
     p.rows = TC_ROWS;
-    const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, (a.b.max_blocks + MIN_PIECE - 1) / MIN_PIECE);
+    p.most = tiles(p.rows);
+    const u64 units = p.most * H, pieces = std::max<u64>(1, (a.b.max_blocks + MIN_PIECE - 1) / MIN_PIECE);
     p.grid = (u32)std::max<u64>(1, std::min<u64>(sm_count, units * pieces));
     p.parts = pieces > 1 && (units < (u64)sm_count || a.b.max_blocks > 64) ? 4 * sm_count + 64 : 0;     // 64: rounding of the mean share
   }
@@ -1721,7 +1731,7 @@ template <class T, u32 D>
 static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
   cudaError_t r = allow_smem(k_attend_split<T, D>, 2 + (D == 128) * 2 + a.fp16, SplitShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
-  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts, 2 * p.sms);
+  k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts, 2 * p.sms, p.most);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
   const u64 rows = (u64)a.b.n_tokens * a.n_q_heads;
@@ -1733,7 +1743,7 @@ template <class T, u32 D>
 static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
   cudaError_t r = allow_smem(k_attend_tc<T, D>, 6 + (D == 128) * 2 + a.fp16, TcShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
-  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts);
+  k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts, p.most);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess || !p.parts) return r;
   return launch_join(k_attend_join_tc<T, D>, 128, ((u64)a.b.n_tokens * ((a.n_q_heads + 3) / 4) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);

@@ -58,6 +58,7 @@ struct AttendPlan {
   uint32_t rows;             // rows of a tile
   uint32_t sms, grid;
   uint32_t parts;            // partial results there is room for; 0: nothing can be cut
+  uint64_t most;             // kind 1: work, kind 2: tiles that sequences which do not overlap can bring
   uint64_t scratch_bytes;
 };
 AttendPlan plan_attend(const AttendArgs &a, uint32_t max_q_len, int sm_count);

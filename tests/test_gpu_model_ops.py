@@ -444,6 +444,10 @@ def test_refusals(B):
     refused(B.KvtError, lambda: e.attend(L, s.q, *good, scale=-1.0))
     refused(B.KvtError, lambda: e.attend(L, s.q, *good, scale=math.nan))
     refused(ValueError, lambda: e.attend(L, s.q.float(), *good))
+    refused(ValueError, lambda: e.attend(-1, s.q, *good))
+    refused(ValueError, lambda: e.attend(L, s.q, *good, window=-4))
+    refused(ValueError, lambda: e.append_kv(-1, s.k, s.v, *good))
+    refused(ValueError, lambda: e.attend(L, s.q, *good, out=s.q[:, :1].expand(-1, 4, -1)))
     refused(ValueError, lambda: e.attend(L, s.q[..., :32], *good))
     refused(ValueError, lambda: e.attend(L, s.q.transpose(1, 2), *good))
     refused(ValueError, lambda: e.attend(L, s.q.cpu(), *good))
@@ -521,6 +525,11 @@ def test_bad_slots_and_lengths_are_reported_and_harmless(B, dim, new, wide):
     report(lambda: s.eng.attend(s.layer, s.q, s.table, s.q_start.flip(0).contiguous(), s.kv_len))
     report(lambda: s.eng.append_kv(s.layer, s.k, s.v, s.table[:, :5], s.q_start, s.kv_len))
     report(lambda: s.eng.append_kv(s.layer, s.k, s.v, s.table, s.q_start + torch.tensor([0, 0, 7], dtype=torch.int32, device="cuda"), s.kv_len))
+    # the same tokens in every other of 400 sequences: reported, and over at once
+    up_down = torch.tensor([0, s.t] * 200 + [0], dtype=torch.int32, device="cuda")
+    many = s.table[:1].expand(400, -1).contiguous()
+    report(lambda: s.eng.attend(s.layer, s.q, many, up_down, s.kv_len[:1].expand(400).contiguous()))
+    report(lambda: s.eng.append_kv(s.layer, s.k, s.v, many, up_down, s.kv_len[:1].expand(400).contiguous()))
     rope = B.Rope(dim, axis_of=[j % 3 for j in range(dim // 2)])
     rope.n_axes = 2
     report(lambda: s.eng.append_kv(s.layer, s.k, s.v, s.table, s.q_start, s.kv_len, rope=rope,

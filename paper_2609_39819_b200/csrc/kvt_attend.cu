@@ -287,6 +287,16 @@ __device__ __forceinline__ void row_range(const AttendArgs &a, const Seq &q, u32
   lo = a.window && hi > a.window ? hi - a.window : 0u;
 }
 
+// Blocks of keys that any of the rows r0 .. r1 sees: how many from block b_first on.
+__device__ __forceinline__ u32 tile_blocks(const AttendArgs &a, const Seq &q, u32 r0, u32 r1, u32 &b_first) {
+  u32 first, last, dummy;
+  row_range(a, q, r0 / a.group, first, dummy);
+  row_range(a, q, r1 / a.group, dummy, last);
+  b_first = first / BT;
+  const u32 b_last = (last + BT - 1) / BT;
+  return b_last > b_first ? b_last - b_first : 0;
+}
+
 // Finds the sequence a tile belongs to: tiles are numbered sequence by sequence. All threads of the CTA take part.
 // Returns false behind the last tile.
 template <u32 THREADS>
@@ -823,6 +833,172 @@ template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
   return (r / 8) * (D * 16) + (c / 8) * 1024 + (r % 8) * 128 + (((c % 8) ^ (r % 8)) * 16);
 }
 
+// The keys in blocks [b0, b1) for rows r0 .. r1 of a sequence: this warp's share of them, every fourth block. o, m, l: sums,
+// maximum and sum of powers of rows lane / 4 and lane / 4 + 8, this lane's columns and keys. `it`: stages used so far. false: a
+// wait ran out.
+template <class T, u32 D>
+__device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &maps, const Seq &q, u32 seq, u32 h, u32 r0, u32 r1, u32 b0, u32 b1,
+                                           u32 ring, u32 bar0, u32 &it, float (&o)[D / 8][4], float (&m)[2], float (&l)[2]) {
+  typedef SplitShape<D> S;
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u32 first, last, all_lo, all_hi;       // keys every row sees: [all_lo, all_hi)
+  row_range(a, q, r0 / a.group, first, all_hi);
+  row_range(a, q, r1 / a.group, all_lo, last);
+  bool ok = true;
+  const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
+  const u32 *row = a.b.table + seq * a.b.table_stride;
+  u32 held = 0;                        // lane i: the slot of this warp's block number (i mod 32) of the current 32
+  auto load = [&](u32 i) {             // i-th block of this warp here; whole warp
+    if (i % 32 == 0) {
+      held = i + lane < n_mine ? row[b0 + warp + (i + lane) * SPLIT_WARPS] : 0;
+      if (i + lane < n_mine && held >= a.p.n_slots && held - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+    }
+    const u32 slot = __shfl_sync(~0u, held, i % 32);
+    if (lane == 0) {
+      const u32 st = (it + i) % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
+      bar_expect(bar, 2 * S::BLOCK);
+      load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
+      load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
+    }
+  };
+  const u32 n_pro = min(n_mine, S::STAGES);
+  for (u32 i = 0; i < n_pro; ++i) load(i);
+
+  // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
+  u32 qf[D / 16][4];
+  u32 lo[2], hi[2];
+#pragma unroll
+  for (u32 y = 0; y < 2; ++y) {
+    const u32 r = min(r0 + lane / 4 + 8 * y, r1);     // rows behind the last one repeat it and are not written
+    row_range(a, q, r / a.group, lo[y], hi[y]);
+    const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
+    const bool even = ((uintptr_t)src & 3) == 0;
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (u32 z = 0; z < 2; ++z) {
+        const u16 *p = src + k * 16 + z * 8;
+        qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+      }
+  }
+  m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.0f;
+#pragma unroll
+  for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+    for (u32 y = 0; y < 4; ++y) o[n][y] = 0.0f;
+
+  for (u32 i = 0; ok && i < n_mine; ++i) {
+    const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
+    if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
+    const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
+    // scores of 16 keys: two column groups of 8
+    float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k) {
+      u32 f[4];
+      ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
+      mma16816<T>(s[0], qf[k], f[0], f[1]);
+      mma16816<T>(s[1], qf[k], f[2], f[3]);
+    }
+    if (key0 + BT > q.kv) {            // the last block's tokens behind the length: whatever their values hold, weight 0
+      const u32 r = lane / 2;          // must not meet an Inf or a NaN
+      if (key0 + r >= q.kv)
+#pragma unroll
+        for (u32 c = 0; c < D / 16; ++c)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+      __syncwarp();
+    }
+    const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) {
+        const u32 key = key0 + n * 8 + (lane % 4) * 2 + (y & 1);
+        float v = s[n][y] * a.scale_log2;
+        if (!whole && (key < lo[y >> 1] || key >= hi[y >> 1])) v = -INFINITY;
+        s[n][y] = v;
+        top[y >> 1] = fmaxf(top[y >> 1], v);
+      }
+#pragma unroll
+    for (u32 y = 0; y < 2; ++y) {
+      top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 1));
+      top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 2));
+    }
+    // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
+    // those below 1, and most blocks then need no rescaling.
+    if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y) {
+        const float now = fmaxf(m[y], top[y]), f = now == -INFINITY ? 1.0f : ex2(m[y] - now);
+        m[y] = now; l[y] *= f;
+#pragma unroll
+        for (u32 n = 0; n < D / 8; ++n) { o[n][2 * y] *= f; o[n][2 * y + 1] *= f; }
+      }
+    }
+    const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+#pragma unroll
+    for (u32 n = 0; n < 2; ++n)
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
+    const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
+                      Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
+#pragma unroll
+    for (u32 n = 0; n < D / 16; ++n) {
+      u32 f[4];
+      ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
+      mma16816<T>(o[2 * n], p, f[0], f[1]);
+      mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
+    }
+    __syncwarp();                      // the stage is read: refill it
+    if (i + S::STAGES < n_mine) load(i + S::STAGES);
+  }
+  it += n_mine;
+  return ok;
+}
+// Leaves the warps' results for the CTA: sums in the (now idle) rings, row pitch split_pitch() floats, maxima and sums in s_ml.
+template <u32 D> __device__ __forceinline__ constexpr u32 split_pitch() { return D + 8; }      // four rows of a quarter warp fall on different banks
+template <u32 D>
+__device__ __forceinline__ void split_leave(u8 *smem_raw, u32 ring, float (&o)[D / 8][4], float (&m)[2], float (&l)[2],
+                                            float (&s_ml)[SPLIT_WARPS][SPLIT_ROWS][2]) {
+  typedef SplitShape<D> S;
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (u32 y = 0; y < 2; ++y) {
+    l[y] += __shfl_xor_sync(~0u, l[y], 1);
+    l[y] += __shfl_xor_sync(~0u, l[y], 2);
+    if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * y][0] = m[y]; s_ml[warp][lane / 4 + 8 * y][1] = l[y]; }
+  }
+  constexpr u32 LD = split_pitch<D>();
+  static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
+  float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
+#pragma unroll
+  for (u32 n = 0; n < D / 8; ++n)
+#pragma unroll
+    for (u32 y = 0; y < 2; ++y)
+      *(float2 *)&so[(lane / 4 + 8 * y) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * y], o[n][2 * y + 1]);
+}
+// Row r (of 16) as the CTA's four warps have it together: maximum, sum of powers, and the weight of each warp's sums.
+__device__ __forceinline__ void split_row(const float (&s_ml)[SPLIT_WARPS][SPLIT_ROWS][2], u32 r, float &mm, float &ll, float (&f)[SPLIT_WARPS]) {
+  mm = -INFINITY; ll = 0.0f;
+#pragma unroll
+  for (u32 y = 0; y < SPLIT_WARPS; ++y) mm = fmaxf(mm, s_ml[y][r][0]);
+  const float ref = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+  for (u32 y = 0; y < SPLIT_WARPS; ++y) { f[y] = ex2(s_ml[y][r][0] - ref); ll += f[y] * s_ml[y][r][1]; }
+}
+template <u32 D>
+__device__ __forceinline__ float4 split_sum(const u8 *smem_raw, u32 ring0, u32 r, u32 c, const float (&f)[SPLIT_WARPS]) {
+  const float *sum = (const float *)(smem_raw + (ring0 - smem_addr(smem_raw))) + r * split_pitch<D>() + c;
+  float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+  for (u32 y = 0; y < SPLIT_WARPS; ++y) {
+    const float4 z = *(const float4 *)(sum + y * (SplitShape<D>::RING / 4));
+    v.x += f[y] * z.x; v.y += f[y] * z.y; v.z += f[y] * z.z; v.w += f[y] * z.w;
+  }
+  return v;
+}
+
 template <class T, u32 D>
 __global__ void __launch_bounds__(SPLIT_THREADS, 2)
 k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps, u32 n_parts, u32 slots, u64 most) {
@@ -884,160 +1060,27 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
       const bool direct = x == u0 && x1 == u0 + unit;
       const u32 part = 2 * cta + (x == u0 && x > x_begin);
       const u32 n_rows = q.n * a.group, r0 = tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, n_rows) - 1;
-      u32 first, last, all_lo, all_hi;     // keys any row sees; keys every row sees
-      row_range(a, q, r0 / a.group, first, all_hi);
-      row_range(a, q, r1 / a.group, all_lo, last);
-      const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+      u32 b_first;
+      const u32 nb = tile_blocks(a, q, r0, r1, b_first);
       const u32 o0 = (u32)(x - u0), o1 = (u32)(x1 - u0);
       const u32 b0 = b_first + min(o0 > UNIT_COST ? o0 - UNIT_COST : 0, nb), b1 = b_first + min(o1 > UNIT_COST ? o1 - UNIT_COST : 0, nb);
-      const u32 n_mine = b0 + warp < b1 ? (b1 - b0 - warp + SPLIT_WARPS - 1) / SPLIT_WARPS : 0;   // blocks b0 + warp + 4 i
-      const u32 *row = a.b.table + seq * a.b.table_stride;
-      u32 slots = 0;                       // lane i: the slot of this warp's block number (i mod 32) of the current 32
-      auto load = [&](u32 i) {             // i-th block of this warp here; whole warp
-        if (i % 32 == 0) {
-          slots = i + lane < n_mine ? row[b0 + warp + (i + lane) * SPLIT_WARPS] : 0;
-          if (i + lane < n_mine && slots >= a.p.n_slots && slots - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
-        }
-        const u32 slot = __shfl_sync(~0u, slots, i % 32);
-        if (lane == 0) {
-          const u32 st = (it + i) % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
-          bar_expect(bar, 2 * S::BLOCK);
-          load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
-          load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
-        }
-      };
-      const u32 n_pro = min(n_mine, S::STAGES);
-      for (u32 i = 0; i < n_pro; ++i) load(i);
-
-      // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
-      u32 qf[D / 16][4];
-      u32 lo[2], hi[2];
-#pragma unroll
-      for (u32 y = 0; y < 2; ++y) {
-        const u32 r = min(r0 + lane / 4 + 8 * y, r1);     // rows behind the last one repeat it and are not written
-        row_range(a, q, r / a.group, lo[y], hi[y]);
-        const u16 *src = (const u16 *)a.q + (u64)(q.t0 + r / a.group) * a.q_ts + (u64)(h * a.group + r % a.group) * a.q_hs + (lane % 4) * 2;
-        const bool even = ((uintptr_t)src & 3) == 0;
-#pragma unroll
-        for (u32 k = 0; k < D / 16; ++k)
-#pragma unroll
-          for (u32 z = 0; z < 2; ++z) {
-            const u16 *p = src + k * 16 + z * 8;
-            qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
-          }
-      }
-      float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (u32 n = 0; n < D / 8; ++n)
-#pragma unroll
-        for (u32 y = 0; y < 4; ++y) o[n][y] = 0.0f;
-
-      for (u32 i = 0; ok && i < n_mine; ++i) {
-        const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
-        if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
-        const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
-        // scores of 16 keys: two column groups of 8
-        float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-        for (u32 k = 0; k < D / 16; ++k) {
-          u32 f[4];
-          ldm4(f, kb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * k + (lane / 8) % 2));
-          mma16816<T>(s[0], qf[k], f[0], f[1]);
-          mma16816<T>(s[1], qf[k], f[2], f[3]);
-        }
-        if (key0 + BT > q.kv) {            // the last block's tokens behind the length: whatever their values hold, weight 0
-          const u32 r = lane / 2;          // must not meet an Inf or a NaN
-          if (key0 + r >= q.kv)
-#pragma unroll
-            for (u32 c = 0; c < D / 16; ++c)
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
-          __syncwarp();
-        }
-        const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
-        float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (u32 n = 0; n < 2; ++n)
-#pragma unroll
-          for (u32 y = 0; y < 4; ++y) {
-            const u32 key = key0 + n * 8 + (lane % 4) * 2 + (y & 1);
-            float v = s[n][y] * a.scale_log2;
-            if (!whole && (key < lo[y >> 1] || key >= hi[y >> 1])) v = -INFINITY;
-            s[n][y] = v;
-            top[y >> 1] = fmaxf(top[y >> 1], v);
-          }
-#pragma unroll
-        for (u32 y = 0; y < 2; ++y) {
-          top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 1));
-          top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 2));
-        }
-        // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
-        // those below 1, and most blocks then need no rescaling.
-        if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
-#pragma unroll
-          for (u32 y = 0; y < 2; ++y) {
-            const float now = fmaxf(m[y], top[y]), f = now == -INFINITY ? 1.0f : ex2(m[y] - now);
-            m[y] = now; l[y] *= f;
-#pragma unroll
-            for (u32 n = 0; n < D / 8; ++n) { o[n][2 * y] *= f; o[n][2 * y + 1] *= f; }
-          }
-        }
-        const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-#pragma unroll
-        for (u32 n = 0; n < 2; ++n)
-#pragma unroll
-          for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
-        const u32 p[4] = {Elem<T>::down(s[0][0], s[0][1]), Elem<T>::down(s[0][2], s[0][3]),
-                          Elem<T>::down(s[1][0], s[1][1]), Elem<T>::down(s[1][2], s[1][3])};
-#pragma unroll
-        for (u32 n = 0; n < D / 16; ++n) {
-          u32 f[4];
-          ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
-          mma16816<T>(o[2 * n], p, f[0], f[1]);
-          mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
-        }
-        __syncwarp();                      // the stage is read: refill it
-        if (i + S::STAGES < n_mine) load(i + S::STAGES);
-      }
-      it += n_mine;
+      float o[D / 8][4], m[2], l[2];
+      ok = split_keys<T, D>(a, maps, q, seq, h, r0, r1, b0, b1, ring, bar0, it, o, m, l);
       if (steal && x1 >= x_end) { ask(); asked = true; }
 
-      // join the four warps: sums through the (now idle) rings
-#pragma unroll
-      for (u32 y = 0; y < 2; ++y) {
-        l[y] += __shfl_xor_sync(~0u, l[y], 1);
-        l[y] += __shfl_xor_sync(~0u, l[y], 2);
-        if (lane % 4 == 0) { s_ml[warp][lane / 4 + 8 * y][0] = m[y]; s_ml[warp][lane / 4 + 8 * y][1] = l[y]; }
-      }
-      constexpr u32 LD = D + 8;            // row pitch in floats: the four rows of a quarter warp fall on different banks
-      static_assert(SPLIT_ROWS * LD * 4 <= S::RING, "sums fit a warp's ring");
-      float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
-#pragma unroll
-      for (u32 n = 0; n < D / 8; ++n)
-#pragma unroll
-        for (u32 y = 0; y < 2; ++y)
-          *(float2 *)&so[(lane / 4 + 8 * y) * LD + n * 8 + (lane % 4) * 2] = make_float2(o[n][2 * y], o[n][2 * y + 1]);
+      split_leave<D>(smem_raw, ring, o, m, l, s_ml);
       if (__syncthreads_or(!ok)) { ok = false; break; }      // a wait ran out somewhere: nothing is written
       const u32 r = tid / 8, c0 = (tid % 8) * 4;             // thread: row r, four columns out of every 32
       if (r0 + r <= r1 && (direct || part < n_parts)) {
-        float mm = -INFINITY, ll = 0.0f, f[SPLIT_WARPS];
-#pragma unroll
-        for (u32 y = 0; y < SPLIT_WARPS; ++y) mm = fmaxf(mm, s_ml[y][r][0]);
-        const float ref = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll
-        for (u32 y = 0; y < SPLIT_WARPS; ++y) { f[y] = ex2(s_ml[y][r][0] - ref); ll += f[y] * s_ml[y][r][1]; }
+        float mm, ll, f[SPLIT_WARPS];
+        split_row(s_ml, r, mm, ll, f);
         const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
-        const float *sum = (const float *)(smem_raw + (ring0 - smem_addr(smem_raw))) + r * LD;
         const float inv = !direct ? 1.0f : ll > 0.0f ? 1.0f / ll : ll;
         u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs;
         float *const sums = scratch_sums(a) + ((u64)part * SPLIT_ROWS + r) * D;
 #pragma unroll
         for (u32 c = c0; c < D; c += 32) {
-          float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-          for (u32 y = 0; y < SPLIT_WARPS; ++y) {
-            const float4 z = *(const float4 *)(sum + y * (S::RING / 4) + c);
-            v.x += f[y] * z.x; v.y += f[y] * z.y; v.z += f[y] * z.z; v.w += f[y] * z.w;
-          }
+          const float4 v = split_sum<D>(smem_raw, ring0, r, c, f);
           if (direct) {
             const u32 p0 = Elem<T>::down(v.x * inv, v.y * inv), p1 = Elem<T>::down(v.z * inv, v.w * inv);
             u16 *d = out + c;
@@ -1082,6 +1125,115 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
     for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
     for (u32 y = 0; y < 2; ++y) bar_wait(smem_addr(&s_next_bar), y);
   }
+}
+
+// Few units of moderate length: a cluster of CTAs takes a unit, its blocks dealt out evenly, and joins the parts through the
+// CTAs' shared memory: one launch, no scratch.
+template <class T, u32 D, u32 CLUSTER>
+__global__ void __launch_bounds__(SPLIT_THREADS, 2)
+k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps) {
+  typedef SplitShape<D> S;
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 bars[SPLIT_WARPS * S::STAGES];
+  __shared__ float s_ml[SPLIT_WARPS][SPLIT_ROWS][2];
+  __shared__ float s_part_ml[SPLIT_ROWS][2];
+  __shared__ u32 s_lost;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
+  const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8, rank = blockIdx.x % CLUSTER, unit = blockIdx.x / CLUSTER, h = unit % H;
+  if (lane == 0) {
+    for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
+  Seq q; u32 seq, tile;
+  if (!find_tile<SPLIT_THREADS>(a, SPLIT_ROWS, unit / H, q, seq, tile)) return;      // the whole cluster
+  const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
+  const u32 r0 = tile * SPLIT_ROWS, r1 = min(r0 + SPLIT_ROWS, q.n * a.group) - 1;
+  u32 b_first, it = 0;
+  const u32 nb = tile_blocks(a, q, r0, r1, b_first), per = (nb + CLUSTER - 1) / CLUSTER;
+  float o[D / 8][4], m[2], l[2];
+  const bool ok = split_keys<T, D>(a, maps, q, seq, h, r0, r1, b_first + min(rank * per, nb), b_first + min((rank + 1) * per, nb), ring, bar0, it, o, m, l);
+  split_leave<D>(smem_raw, ring, o, m, l, s_ml);
+  const bool lost = __syncthreads_or(!ok);
+  // this CTA's part: sums behind warp 0's in its ring
+  constexpr u32 PART = (SPLIT_ROWS * split_pitch<D>() * 4 + 127) / 128 * 128;
+  static_assert(PART + SPLIT_ROWS * D * 4 <= S::RING, "the part fits warp 0's ring");
+  float *const part = (float *)(smem_raw + (ring0 - smem_addr(smem_raw)) + PART);
+  {
+    const u32 r = tid / 8;
+    float mm, ll, f[SPLIT_WARPS];
+    split_row(s_ml, r, mm, ll, f);
+#pragma unroll
+    for (u32 c = (tid % 8) * 4; c < D; c += 32) *(float4 *)(part + r * D + c) = split_sum<D>(smem_raw, ring0, r, c, f);
+    if (tid % 8 == 0) { s_part_ml[r][0] = mm; s_part_ml[r][1] = ll; }
+    if (tid == 0) s_lost = lost;
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  // a CTA joins 16 / CLUSTER of the rows, a thread COLS columns of one
+  constexpr u32 ROWS_HERE = SPLIT_ROWS / CLUSTER, COLS = D * ROWS_HERE < SPLIT_THREADS ? 1 : D * ROWS_HERE / SPLIT_THREADS, PER_ROW = D / COLS;
+  auto there = [&](const void *p, u32 cta) {             // the same place in another CTA's shared memory
+    u32 r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(cta));
+    return r;
+  };
+  const bool busy = tid < ROWS_HERE * PER_ROW;
+  const u32 r = rank * ROWS_HERE + (busy ? tid / PER_ROW : 0), c = tid % PER_ROW * COLS;
+  float top = -INFINITY, sum = 0.0f, e[COLS];
+  u32 any_lost = 0;
+#pragma unroll
+  for (u32 z = 0; z < COLS; ++z) e[z] = 0.0f;
+  constexpr u32 STEP = CLUSTER < 8 ? CLUSTER : 8;        // parts read together
+#pragma unroll 1
+  for (u32 y0 = 0; y0 < CLUSTER; y0 += STEP) {
+    float mm[STEP], ll[STEP], v[STEP][COLS], now = top;
+#pragma unroll
+    for (u32 y = 0; y < STEP; ++y) {
+      u32 x;
+      asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(mm[y]), "=f"(ll[y]) : "r"(there(&s_part_ml[r][0], y0 + y)) : "memory");
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(there(&s_lost, y0 + y)) : "memory");
+      any_lost |= x;
+      const u32 at = there(part + r * D + c, y0 + y);
+#pragma unroll
+      for (u32 z = 0; z < COLS; z += 4) {
+        if (COLS >= 4) asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                    : "=f"(v[y][z]), "=f"(v[y][(z + 1) % COLS]), "=f"(v[y][(z + 2) % COLS]), "=f"(v[y][(z + 3) % COLS]) : "r"(at + 4 * z) : "memory");
+        else if (COLS == 2) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[y][0]), "=f"(v[y][1 % COLS]) : "r"(at) : "memory");
+        else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[y][0]) : "r"(at) : "memory");
+      }
+      now = fmaxf(now, mm[y]);
+    }
+    const float ref = now == -INFINITY ? 0.0f : now, f = ex2(top - ref);
+    top = now; sum *= f;
+#pragma unroll
+    for (u32 z = 0; z < COLS; ++z) e[z] *= f;
+#pragma unroll
+    for (u32 y = 0; y < STEP; ++y) {
+      const float w = ex2(mm[y] - ref);
+      sum += w * ll[y];
+#pragma unroll
+      for (u32 z = 0; z < COLS; ++z) e[z] += w * v[y][z];
+    }
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");    // nobody reads here any more
+  if (any_lost) {
+    if (tid == 0) kv_err(a.err, KVERR_WAIT);
+    if (!ok) for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);   // copies in flight
+    return;
+  }
+  if (!busy || r0 + r > r1) return;
+  const float inv = sum > 0.0f ? 1.0f / sum : sum;
+  const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
+  u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + c;
+  if (COLS >= 4 && ((uintptr_t)out & 7) == 0) {
+#pragma unroll
+    for (u32 z = 0; z < COLS; z += 4)
+      *(uint2 *)(out + z) = make_uint2(Elem<T>::down(e[z] * inv, e[(z + 1) % COLS] * inv), Elem<T>::down(e[(z + 2) % COLS] * inv, e[(z + 3) % COLS] * inv));
+  } else {
+#pragma unroll
+    for (u32 z = 0; z < COLS; ++z) ((T *)out)[z] = Elem<T>::down1(e[z] * inv);
+  }
+  if (a.lse && c == 0) a.lse[(u64)t * a.n_q_heads + hq] = (top + log2f(sum)) * 0.69314718055994531f;
 }
 
 // ------------------------------------------------------------------------------------------------------
@@ -1686,18 +1838,37 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     p.grid = (u32)std::min<u64>(tiles(p.rows), 0x7FFFFFFFu);
     return p;
   }
-  // One tile of 16 rows reads K and V once. With more rows the kernel for few rows reads them once per tile, but it starts,
-  // ends and joins 8 us sooner, which decides when there is little to do: up to 8 K blocks (of 16 rows and one KV head, as
-  // many as fit the table rows), or 32 K where a sequence has two tiles only. Measured, us of few / many rows, heads of 128:
+  // Units so few that several CTAs fit on each: clusters of as many as run at once (16 of them only for 8 units and less: more
+  // such clusters do not find room together). A cluster's CTAs take 4 us and 0.2 us per block of theirs; stretches take 11 us
+  // (with the join) and as much per block, but use all SMs and are even whatever the lengths. One sequence of 8 heads of 128:
+  // 1000 tokens 7.0 us against 11.6, 4000 tokens 10.5 against 13.7, 8000 tokens 13.8 (clusters of 8: 17.5) against 14.8;
+  // 4 sequences of 8000 27.4 against 32.8. Bounded, since only the longest sequence the table has room for is known here.
+  const u64 units16 = tiles(SPLIT_ROWS) * H, nb = a.b.max_blocks, slots = 2ull * sm_count;
+  u32 cluster = 0;
+  for (u32 c = units16 <= 8 && nb > 192 ? 16 : 8; c >= 2; c /= 2) {
+    if (units16 * c > slots) continue;
+    if (nb > 64 * c || nb * (slots - units16 * c) > 28 * slots * c) break;
+    cluster = nb <= 4 ? 0 : nb <= 2 * c ? std::max(2u, c / 2) : c;     // no more CTAs than there is something to do for
+    break;
+  }
+  // One tile of 16 rows reads K and V once. With more rows the kernels for few rows read them once per tile, but they start and
+  // end 8 us sooner, which decides when there is little to do: up to 8 K blocks (of 16 rows and one KV head, as many as fit
+  // the table rows), 24 K in clusters, or 32 K where a sequence has two tiles only. Measured, us of few / many rows, heads of 128:
   //   64 tokens 6.6 / 12.2, 128 tokens 8.2 / 12.2, 200 tokens 16.3 / 14.0 (1.5 K, 4.1 K, 8.4 K blocks; groups of 4, 8 KV heads)
-  //   32 on 1000 16.9 / 21.8, 64 on 1000 22.9 / 23.8, 100 on 2000 38.6 / 28.8 (4.7 K, 9.6 K, 28 K)
-  //   two tiles: 8 on 4000 16.3 / 27.6, 8 x 8 on 2000 28.4 / 32.0, 32 x 8 on 500 24.5 / 29.0 (4.1 K, 25 K, 30 K)
-  const u64 rows = (u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group,
-            few = tiles(SPLIT_ROWS) * H * ((u64)a.b.max_blocks + UNIT_COST);
-  if (rows <= SPLIT_ROWS || few <= 8192 || (rows <= 2 * SPLIT_ROWS && few <= 32768)) {
-    p.kind = 1;
+  //   clusters: 64 on 1000 14.8 / 23.6, 2 x 20 on 3000 17.1 / 31.0, 32 on 4000 20.7 / 28.2 (9.6 K, 12 K, 17 K); others: 100 on
+  //   2000 38.6 / 28.8 (28 K)
+  //   two tiles: 8 x 8 on 2000 28.4 / 32.0, 32 x 8 on 500 24.5 / 29.0 (25 K, 30 K)
+  const u64 rows = (u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group, few = units16 * (nb + UNIT_COST);
+  if (rows <= SPLIT_ROWS || few <= (cluster ? 24576 : 8192) || (rows <= 2 * SPLIT_ROWS && few <= 32768)) {
     p.rows = SPLIT_ROWS;
-    const u64 units = tiles(p.rows) * H, pieces = std::max<u64>(1, ((u64)a.b.max_blocks + UNIT_COST) / MIN_STRETCH);
+    if (cluster) {
+      p.kind = 3;
+      p.cluster = cluster;
+      p.grid = (u32)(units16 * cluster);
+      return p;
+    }
+    p.kind = 1;
+    const u64 units = units16, pieces = std::max<u64>(1, (nb + UNIT_COST) / MIN_STRETCH);
     // Short sequences are not cut: a CTA is through them sooner than a second kernel has joined their parts, the more so when
     // there is a unit for every SM. One sequence of 200 tokens, 8 heads of 128: 7.9 us against 11.3 cut, of 500 tokens 11.0
     // against 9.0; 32 sequences of 500: 13.1 against 19.3, of 1000 27.8 against 31.8.
@@ -1739,6 +1910,34 @@ static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const 
   return launch_join(k_attend_join_split<T, D, 4>, 128, rows, p.sms, s, launches, a, p.parts);
 }
 
+template <class T, u32 D, u32 CLUSTER>
+static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
+  constexpr u32 which = 10 + (CLUSTER == 16 ? 3 : CLUSTER == 8 ? 2 : CLUSTER == 4 ? 1 : 0) * 4 + (D == 128) * 2 + (sizeof(T) == 2 && __is_same(T, __half));
+  if (CLUSTER > 8 && !(*allowed >> which & 1)) {
+    const cudaError_t r = cudaFuncSetAttribute(k_attend_cluster<T, D, CLUSTER>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (r != cudaSuccess) return r;
+  }
+  cudaError_t r = allow_smem(k_attend_cluster<T, D, CLUSTER>, which, SplitShape<D>::SMEM, allowed);
+  if (r != cudaSuccess) return r;
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3(p.grid); c.blockDim = dim3(SPLIT_THREADS); c.dynamicSmemBytes = SplitShape<D>::SMEM; c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = CLUSTER; at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  c.attrs = &at; c.numAttrs = 1;
+  ++*launches;
+  return cudaLaunchKernelEx(&c, k_attend_cluster<T, D, CLUSTER>, a, m);
+}
+template <class T, u32 D>
+static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
+  switch (p.cluster) {
+    case 2: return launch_cluster<T, D, 2>(a, p, m, s, allowed, launches);
+    case 4: return launch_cluster<T, D, 4>(a, p, m, s, allowed, launches);
+    case 8: return launch_cluster<T, D, 8>(a, p, m, s, allowed, launches);
+    default: return launch_cluster<T, D, 16>(a, p, m, s, allowed, launches);
+  }
+}
+
 template <class T, u32 D>
 static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
   cudaError_t r = allow_smem(k_attend_tc<T, D>, 6 + (D == 128) * 2 + a.fp16, TcShape<D>::SMEM, allowed);
@@ -1753,6 +1952,10 @@ cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps
   if (p.kind == 2) {
     if (a.p.head_dim == 64) return a.fp16 ? launch_tc<__half, 64>(a, p, m, s, allowed, launches) : launch_tc<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
     return a.fp16 ? launch_tc<__half, 128>(a, p, m, s, allowed, launches) : launch_tc<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
+  }
+  if (p.kind == 3) {
+    if (a.p.head_dim == 64) return a.fp16 ? launch_cluster<__half, 64>(a, p, m, s, allowed, launches) : launch_cluster<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
+    return a.fp16 ? launch_cluster<__half, 128>(a, p, m, s, allowed, launches) : launch_cluster<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
   }
   if (p.kind == 1) {
     if (a.p.head_dim == 64) return a.fp16 ? launch_split<__half, 64>(a, p, m, s, allowed, launches) : launch_split<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);

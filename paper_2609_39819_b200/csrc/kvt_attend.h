@@ -54,9 +54,10 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, uint64_t n_slots,
 
 // What kvt_attend does, decided from sizes alone.
 struct AttendPlan {
-  uint32_t kind;             // 0 any head size, 1 few rows (warp-level matrix instructions), 2 many rows (tcgen05)
+  uint32_t kind;             // 0 any head size, 1 few rows (warp-level matrix instructions), 2 many rows (tcgen05),
+                             // 3 few rows of few and moderately long units (clusters)
   uint32_t rows;             // rows of a tile
-  uint32_t sms, grid;
+  uint32_t sms, grid, cluster;
   uint32_t parts;            // partial results there is room for; 0: nothing can be cut
   uint64_t most;             // kind 1: work, kind 2: tiles that sequences which do not overlap can bring
   uint64_t scratch_bytes;

@@ -572,7 +572,7 @@ class Engine:
             hq = q.shape[1] if q.dim() == 3 else 0
             qp, qts, qhs = self._kv_tensor(q, "append_kv: q", (t, hq, d), k.dtype)
             if q_out is None:
-                q_out = q.new_empty((t, hq, d))
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
                 op, ots, ohs = q_out.data_ptr(), hq * d, d
             else:
                 op, ots, ohs = self._kv_tensor(q_out, "append_kv: q_out", (t, hq, d), k.dtype)
@@ -620,7 +620,7 @@ class Engine:
         t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
         qp, qts, qhs = self._kv_tensor(q, "attend: q", (t, hq, self.head_dim), q.dtype)
         if out is None:
-            out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((t, hq, d))
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
             op, ots, ohs = out.data_ptr(), hq * d, d
         else:
             op, ots, ohs = self._kv_tensor(out, "attend: out", (t, hq, d), q.dtype)

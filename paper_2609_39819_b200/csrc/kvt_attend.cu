@@ -569,8 +569,8 @@ __device__ void find_stretch(const AttendArgs &a, u32 rows, u32 slots, u64 most,
 // partial result. Tried for the longest sequence cut into CUTS[] pieces, and the others into pieces no longer; `most` bounds
 // the partial results. For more than 32 sequences the search would take longer than it gains: pieces of half the mean share.
 // Every warp takes part with the candidates warp, warp + warps, ...; lane: one of the first 32 sequences.
-constexpr u32 PIECE_COST = 16, JOIN_COST = 24, MIN_PIECE = 16, N_CUTS = 16;
-__constant__ const u8 CUTS[N_CUTS] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
+constexpr u32 PIECE_COST = 16, JOIN_COST = 24, MIN_PIECE = 16, N_CUTS = 12;      // one for each warp
+__constant__ const u8 CUTS[N_CUTS] = {1, 2, 3, 4, 5, 6, 7, 9, 12, 16, 22, 32};
 __device__ __forceinline__ u32 cut_length(u32 longest, u32 cuts) { return max(MIN_PIECE, ((longest + cuts - 1) / cuts + 7) / 8 * 8); }   // whole stages
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
@@ -1323,6 +1323,11 @@ __device__ __forceinline__ void tc_st16(u32 addr, const u32 *r) {
                ::"r"(addr), TC_R16("r", r, 0) : "memory");
 }
 
+__device__ __forceinline__ void st_global32(void *p, const u32 *x) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+}
+
 // Two 32-bit numbers at a time.
 __device__ __forceinline__ u64 pack2(float a, float b) { u64 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float2 unpack2(u64 x) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x)); return r; }
@@ -1362,7 +1367,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   typedef TcShape<D> S;
   constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
   extern __shared__ u8 smem_raw[];
-  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2][TC_PARTS], s_qready[2], s_drain, s_jfull[TC_JOBS], s_jempty[TC_JOBS];
+  __shared__ __align__(8) u64 s_full[S::STAGES], s_empty[S::STAGES], s_sready[2], s_pready[2][TC_PARTS], s_qready[2], s_oready[2], s_drain, s_jfull[TC_JOBS], s_jempty[TC_JOBS];
   __shared__ u32 s_tmem;
   __shared__ volatile u32 s_lost;
   __shared__ Job s_job[TC_JOBS];
@@ -1371,12 +1376,12 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
   const u32 full = smem_addr(s_full), empty = smem_addr(s_empty), sready = smem_addr(s_sready), pready = smem_addr(s_pready),
-            qready = smem_addr(s_qready), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
+            qready = smem_addr(s_qready), oready = smem_addr(s_oready), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
   if (tid == 0) {
     for (u32 i = 0; i < S::STAGES; ++i) { bar_init(full + i * 8, 1); bar_init(empty + i * 8, 1); }
-    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(qready + i * 8, 4); }
+    for (u32 i = 0; i < 2; ++i) { bar_init(sready + i * 8, 1); bar_init(oready + i * 8, 1); bar_init(qready + i * 8, 4); }
     for (u32 i = 0; i < 2 * TC_PARTS; ++i) bar_init(pready + i * 8, 4);
-    for (u32 i = 0; i < TC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 10); }
+    for (u32 i = 0; i < TC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 11); }
     bar_init(drain, 1);
     s_lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -1407,14 +1412,22 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     return j.last == 0;
   };
 
-  // registers: 168 for each of 384 threads at the launch; 224 for a thread that holds a row of S, 56 for the others
+  // registers: 168 for each of 384 threads at the launch; 208 for a thread that holds a row of S, 88 for the others (with 224 and
+  // 56 the others spill)
   if (warp == 11) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // ---- queries of the jobs to come into the L2 cache
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    for (Job j; next_job(j);)
+      for (u32 r = j.r0 + lane; r <= j.r1; r += 32) {
+        const u32 tok = r / a.group;
+        const u16 *src = (const u16 *)a.q + (u64)(j.t0 + tok) * a.q_ts + (u64)(j.h * a.group + r - tok * a.group) * a.q_hs;
+        if (((uintptr_t)src & 15) == 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(D * 2) : "memory");
+      }
   } else if (warp == 10) {
     // ---- scheduling: this CTA's jobs, one per round of the grid, every other round in reverse so that the long first jobs of
     // a causal prompt even out. Jobs of a sequence: piece, tile (last tokens first), KV head; those that run at the same
     // time then mostly read the same keys.
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     const u32 piece = choose_cut(a, n_parts, cut, s_cost);
     // (a launch has fewer than 2^32 jobs: tokens times query heads and a few thousand pieces)
     u32 base = 0, part0 = 0, s0 = 0;     // first job and first partial of the 32 sequences in hand
@@ -1422,55 +1435,60 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     u32 tiles = 0, pieces = 0;
     u32 my_jobs = 0, at = 0, all = 0, my_part = 0, all_parts = 0;
     u32 my_seq = 0;
-    // lane: one of the sequences s0 .. s0 + 31, those with the longest pieces first: jobs that get shorter, dealt out back and
-    // forth, come out even
-    auto take = [&]() {
-      const u32 s = s0 + lane;
-      tiles = pieces = 0;
-      u32 length = 0;
-      // starts that go up and down make the same tokens count again and again: then nothing is done (load_seq has set the
-      // error word)
-      if (s < a.b.n_seqs && cut.sound) {
-        if (s0) q = load_seq(a.b, s, a.err);
-        tiles = seq_tiles(a, q, TC_ROWS);
-        const u32 nb = seq_blocks(a, q, TC_ROWS);
-        pieces = (nb + piece - 1) / piece;
-        length = tiles ? (nb + pieces - 1) / pieces : 0;
-      }
-      my_seq = s;
-      if (a.b.n_seqs > 1) {
-        u32 rank = 0;
-#pragma unroll 8
-        for (u32 y = 0; y < 32; ++y) { const u32 z = __shfl_sync(~0u, length, y); rank += z > length || (z == length && y < lane); }
-        s_order[rank] = (u8)lane;
-        __syncwarp();
-        const u32 from = s_order[lane];
-        q.t0 = __shfl_sync(~0u, q.t0, from); q.n = __shfl_sync(~0u, q.n, from); q.kv = __shfl_sync(~0u, q.kv, from);
-        tiles = __shfl_sync(~0u, tiles, from); pieces = __shfl_sync(~0u, pieces, from);
-        my_seq = s0 + from;
-        __syncwarp();
-      }
-      my_jobs = tiles * pieces * H;
-      const u32 parts = pieces > 1 ? tiles * pieces : 0;
-      u32 incl = my_jobs, pincl = parts;
-#pragma unroll
-      for (u32 o = 1; o < 32; o *= 2) {
-        const u32 y = __shfl_up_sync(~0u, incl, o), z = __shfl_up_sync(~0u, pincl, o);
-        if (lane >= o) { incl += y; pincl += z; }
-      }
-      at = base + incl - my_jobs; my_part = part0 + pincl - parts;
-      all = __shfl_sync(~0u, incl, 31); all_parts = __shfl_sync(~0u, pincl, 31);
-      if (blockIdx.x == 0 && n_parts && my_seq < a.b.n_seqs) {
-        scratch_plan(a)[1 + my_seq] = make_uint4(my_part, pieces, tiles, 0);
-        if (pieces > 1) scratch_plan(a)[0].x = 1;
-      }
-    };
+    bool ok = true, first = true;
     if (blockIdx.x == 0 && n_parts) { if (lane == 0) scratch_plan(a)[0] = make_uint4(0, 0, 0, 0); __syncwarp(); }
-    take();
-    bool ok = true;
     for (u32 k = 0;; ++k) {
       const u32 want = k * gridDim.x + (k % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-      while (want >= base + all && s0 + 32 < a.b.n_seqs) { base += all; part0 += all_parts; s0 += 32; take(); }
+#pragma unroll 1
+      while (first || (want >= base + all && s0 + 32 < a.b.n_seqs)) {
+        // the next 32 sequences, one per lane, those with the longest pieces first: jobs that get shorter, dealt out back and
+        // forth, come out even
+        if (!first) { base += all; part0 += all_parts; s0 += 32; }
+        my_seq = s0 + lane;
+        tiles = pieces = 0;
+        u32 length = 0;
+        // starts that go up and down make the same tokens count again and again: then nothing is done (load_seq has set the
+        // error word)
+        if (my_seq < a.b.n_seqs && cut.sound) {
+          if (!first) q = load_seq(a.b, my_seq, a.err);
+          tiles = seq_tiles(a, q, TC_ROWS);
+          const u32 nb = seq_blocks(a, q, TC_ROWS);
+          pieces = (nb + piece - 1) / piece;
+          length = tiles ? (nb + pieces - 1) / pieces : 0;
+        }
+        first = false;
+        const u32 n = min(32u, a.b.n_seqs - s0);
+        if (n > 1) {
+          u32 rank = lane;               // lanes behind the last sequence stay where they are
+          if (lane < n) rank = 0;
+#pragma unroll 4
+          for (u32 y = 0; y < n; ++y) {
+            const u32 z = __shfl_sync(~0u, length, y);
+            if (lane < n) rank += z > length || (z == length && y < lane);
+          }
+          s_order[rank] = (u8)lane;
+          __syncwarp();
+          const u32 from = s_order[lane];
+          q.t0 = __shfl_sync(~0u, q.t0, from); q.n = __shfl_sync(~0u, q.n, from); q.kv = __shfl_sync(~0u, q.kv, from);
+          tiles = __shfl_sync(~0u, tiles, from); pieces = __shfl_sync(~0u, pieces, from);
+          my_seq = s0 + from;
+          __syncwarp();
+        }
+        my_jobs = tiles * pieces * H;
+        const u32 parts = pieces > 1 ? tiles * pieces : 0;
+        u32 incl = my_jobs, pincl = parts;
+#pragma unroll
+        for (u32 o = 1; o < 32; o *= 2) {
+          const u32 y = __shfl_up_sync(~0u, incl, o), z = __shfl_up_sync(~0u, pincl, o);
+          if (lane >= o) { incl += y; pincl += z; }
+        }
+        at = base + incl - my_jobs; my_part = part0 + pincl - parts;
+        all = __shfl_sync(~0u, incl, 31); all_parts = __shfl_sync(~0u, pincl, 31);
+        if (blockIdx.x == 0 && n_parts && my_seq < a.b.n_seqs) {
+          scratch_plan(a)[1 + my_seq] = make_uint4(my_part, pieces, tiles, 0);
+          if (pieces > 1) scratch_plan(a)[0].x = 1;
+        }
+      }
       const u32 hit = __ballot_sync(~0u, want >= at && want < at + my_jobs);
       const u32 slot = k % TC_JOBS;
       if (k >= TC_JOBS && !(ok = tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost))) break;
@@ -1495,14 +1513,11 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       }
       __syncwarp();
       if (lane == 0) bar_arrive(jfull + slot * 8);
-      if (!hit) {                        // behind the last job; block 0 still has the plan of the other sequences to write
-        if (blockIdx.x == 0 && n_parts) while (s0 + 32 < a.b.n_seqs) { base += all; part0 += all_parts; s0 += 32; take(); }
-        break;
-      }
+      if (!hit) break;                   // behind the last job, and so behind the last sequence
     }
   } else if (warp == 9) {
     // ---- loads: K0, V0, K1, V1, ...; blocks behind the piece's last one read as zeros (a slot behind both pools)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     u32 it = 0;
     bool ok = true;
     for (Job j; ok && next_job(j);) {
@@ -1533,7 +1548,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     // (a thread per tile was tried: the tiles fall into step and compete, first for the tensor cores, then for the powers).
     // What it does between two products is in the way of the tensor cores, so that is kept short: stages are counted up,
     // not divided out, descriptors differ by constants, arrivals of K and V are looked at before those of P.
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (elect_one()) {
       const u32 id_s = tc_idesc(FP16, TC_KEYS, false), id_o = tc_idesc(FP16, D, true);
       const u64 dq0 = tc_desc(sq, 16, 1024), dk0 = tc_desc(ring, 16, D * 16), dv0 = tc_desc(ring, 1024, D * 16);
@@ -1602,7 +1617,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
                   tc_mma_ts(tmem + 256 + i * D, tmem + i * 128 + y * 8, dv + y * (D * 32 / 16), id_o, s > 0 || y > 0);
               }
               if (!ok) break;
-              if (!more) tc_commit(sready + i * 8);      // the finished sums
+              if (!more) tc_commit(oready + i * 8);      // the finished sums
               else if (i == 0 && !has_k && !(ok = landed(k))) break;
               else product_s(i, k.st);
               if (i == 0) {
@@ -1626,61 +1641,63 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
     }
     __syncwarp();
   } else {
-    // ---- one thread per row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // ---- one thread per row. Between two jobs the tensor cores would stand still while queries come and results go, so the
+    // next job's queries are brought in as soon as the last S is made, and its first S is made while the results are written.
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const u32 i = warp / 4, rt = tid % TC_TILE;
     const u32 lanes = (warp % 4) << 21, ts = tmem + lanes + i * 128, to = tmem + lanes + 256 + i * D;
-    u32 seen = 0;                        // completions of sready[i]
+    u32 seen_s = 0, seen_o = 0;          // completions of sready[i], oready[i]
     bool ok = true;
-    for (Job j; ok && next_job(j);) {
-      const u32 n_tiles = j.r1 - j.r0 >= TC_TILE ? 2 : 1, n = (j.b1 - j.b0 + TC_KB - 1) / TC_KB;
-      if (i >= n_tiles) continue;
-      const u32 r = j.r0 + i * TC_TILE + rt, rr = min(r, j.r1);     // rows behind the last one repeat it and are not written
+    // The next job with rows in this tile; its queries into shared memory.
+    auto begin = [&](Job &j) {
+      do { if (!next_job(j)) return false; } while (i && j.r1 - j.r0 < TC_TILE);
+      if (j.b0 >= j.b1) return true;
+      const u32 rr = min(j.r0 + i * TC_TILE + rt, j.r1), tok = rr / a.group;      // rows behind the last one repeat it
+      const u16 *const src = (const u16 *)a.q + (u64)(j.t0 + tok) * a.q_ts + (u64)(j.h * a.group + rr - tok * a.group) * a.q_hs;
+      const bool wide = __all_sync(~0u, ((uintptr_t)src & 15) == 0);
+      uint4 v[D / 8];                    // lanes take 16 bytes each of as many rows as make 512 bytes
+      auto from = [&](u32 k) { return (const u16 *)__shfl_sync(~0u, (u64)src, (k * 32 + lane) / (D / 8)) + lane % (D / 8) * 8; };
+      if (wide) {                        // (a branch for each would make each load wait for the one before)
+#pragma unroll
+        for (u32 k = 0; k < D / 8; ++k) v[k] = *(const uint4 *)from(k);
+      } else {
+#pragma unroll
+        for (u32 k = 0; k < D / 8; ++k) {
+          const u16 *const f = from(k);
+          u32 x[4];
+#pragma unroll
+          for (u32 y = 0; y < 4; ++y) x[y] = (u32)f[2 * y] | (u32)f[2 * y + 1] << 16;
+          v[k] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+      }
+#pragma unroll
+      for (u32 k = 0; k < D / 8; ++k) {
+        const u32 at = k * 32 + lane, row = warp % 4 * 32 + at / (D / 8), c = at % (D / 8);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                     ::"r"(sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + row * 128 + (((c % 8) ^ (row % 8)) * 16)),
+                       "r"(v[k].x), "r"(v[k].y), "r"(v[k].z), "r"(v[k].w) : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      tc_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(qready + i * 8);
+      return true;
+    };
+    Job j;
+    for (bool have = begin(j); have;) {
+      const u32 n = (j.b1 - j.b0 + TC_KB - 1) / TC_KB;
+      const u32 r = j.r0 + i * TC_TILE + rt, rr = min(r, j.r1);
       const bool mine = r <= j.r1;
-      const u32 tok = rr / a.group, t = j.t0 + tok, hq = j.h * a.group + rr % a.group;
+      const u32 tok = rr / a.group, t = j.t0 + tok, hq = j.h * a.group + rr - tok * a.group;
       u32 lo, hi;
       {
         const long long own = (long long)(int)j.shift + tok;
         hi = a.full ? j.kv : own < 0 ? 0u : (u32)own + 1;
         lo = a.window && hi > a.window ? hi - a.window : 0u;
       }
-      // Place of 16 bytes (c) of a row in the Q tile. A warp's 32 rows there are its own: loaded and, once the last S is made,
-      // used to bring the results into whole rows. Lanes take 16 bytes each of as many rows as make 512 bytes.
-      auto q_place = [&](u32 row, u32 c) { return sq + i * (TC_TILE * D * 2) + (c / 8) * (TC_TILE * 128) + row * 128 + (((c % 8) ^ (row % 8)) * 16); };
-      const u32 row0 = warp % 4 * 32;
-      if (n) {
-        const u16 *const src = (const u16 *)a.q + (u64)t * a.q_ts + (u64)hq * a.q_hs;
-        const bool wide = __all_sync(~0u, ((uintptr_t)src & 15) == 0);
-#pragma unroll
-        for (u32 k0 = 0; k0 < D / 8; k0 += 8) {
-          uint4 v[8];
-#pragma unroll
-          for (u32 k = 0; k < 8; ++k) {
-            const u32 at = (k0 + k) * 32 + lane, c = at % (D / 8);
-            const u16 *from = (const u16 *)__shfl_sync(~0u, (u64)src, at / (D / 8)) + c * 8;
-            if (wide) v[k] = *(const uint4 *)from;
-            else {
-              u32 x[4];
-#pragma unroll
-              for (u32 y = 0; y < 4; ++y) x[y] = (u32)from[2 * y] | (u32)from[2 * y + 1] << 16;
-              v[k] = make_uint4(x[0], x[1], x[2], x[3]);
-            }
-          }
-#pragma unroll
-          for (u32 k = 0; k < 8; ++k) {
-            const u32 at = (k0 + k) * 32 + lane;
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
-                         ::"r"(q_place(row0 + at / (D / 8), at % (D / 8))), "r"(v[k].x), "r"(v[k].y), "r"(v[k].z), "r"(v[k].w) : "memory");
-          }
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        tc_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(qready + i * 8);
-      }
       float m = -INFINITY, l = 0.0f;
       for (u32 s = 0; s < n; ++s) {
-        if (!(ok = tc_wait(sready + i * 8, seen++ & 1, lost))) break;
+        if (!(ok = tc_wait(sready + i * 8, seen_s++ & 1, lost))) break;
         tc_after();
         u32 x[128];
         float *const v = reinterpret_cast<float *>(x);
@@ -1691,7 +1708,11 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         if (key0 < j.all_lo || key0 + TC_KEYS > j.all_hi) {
           const int from = (int)lo - (int)key0, to_ = (int)hi - (int)key0;
 #pragma unroll
-          for (int c = 0; c < 128; ++c) if (c < from || c >= to_) v[c] = -INFINITY;
+          for (int b = 0; b < 128; b += 32) {     // a bit for each key the row sees
+            const u32 see = (from >= b + 32 ? 0u : from > b ? ~0u << (from - b) : ~0u) & (to_ >= b + 32 ? ~0u : to_ > b ? ~(~0u << (to_ - b)) : 0u);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) v[b + c] = see >> c & 1 ? v[b + c] : -INFINITY;
+          }
         }
         float top[4] = {max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[8]), max3(v[9], v[10], v[11])};
 #pragma unroll
@@ -1744,61 +1765,55 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         __syncwarp();
         if (lane == 0) bar_arrive(pready + (i * TC_PARTS + TC_PARTS - 1) * 8);
       }
-      // ---- results
-      if (ok && n) { ok = tc_wait(sready + i * 8, seen++ & 1, lost); tc_after(); }
       if (!ok) break;
-      const float inv = !j.direct ? 1.0f : l > 0.0f ? 1.0f / l : l;
-      const u32 prow = i * TC_TILE + rt;
-      u8 *const row_out = j.direct ? (u8 *)((u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs)
-                                   : (u8 *)(scratch_sums(a) + ((u64)j.part * TC_ROWS + prow) * D);
-      const bool wide = __all_sync(~0u, ((uintptr_t)row_out & 15) == 0);
-      const u32 n_here = min(j.r1 - j.r0 + 1 - i * TC_TILE, TC_TILE);       // rows of this tile
-      // 2 * head_dim bytes per row and round: the whole result, or half of a partial one
-      for (u32 round = 0; round < (j.direct ? 1 : 2); ++round) {
-        __syncwarp();
-#pragma unroll
-        for (u32 c = 0; c < D / 32; ++c) {
-          u32 e[16];
-          if (j.direct) {
-            u32 y[32];
-            if (n) { tc_ld32(y, to + 32 * c); tc_wait_ld(); }
-#pragma unroll
-            for (u32 z = 0; z < 16; ++z) e[z] = n ? Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv) : 0;
-          } else {
-            if (n) { tc_ld16(e, to + round * (D / 2) + 16 * c); tc_wait_ld(); }
-            else {
-#pragma unroll
-              for (u32 z = 0; z < 16; ++z) e[z] = 0;
-            }
-          }
-#pragma unroll
-          for (u32 z = 0; z < 4; ++z)
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
-                         ::"r"(q_place(rt, 4 * c + z)), "r"(e[4 * z]), "r"(e[4 * z + 1]), "r"(e[4 * z + 2]), "r"(e[4 * z + 3]) : "memory");
-        }
-        __syncwarp();
-#pragma unroll 4
-        for (u32 k = 0; k < D / 8; ++k) {
-          const u32 at = k * 32 + lane, row = at / (D / 8), c = at % (D / 8);
-          uint4 v;
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(q_place(row0 + row, c)) : "memory");
-          u8 *const dst = (u8 *)__shfl_sync(~0u, (u64)row_out, row) + round * (D * 2) + c * 16;
-          if (row0 + row >= n_here) {
-          } else if (wide) {
-            *(uint4 *)dst = v;
-          } else {                       // an output whose rows are not aligned to 16 bytes: partial results are
-            u16 *const d = (u16 *)dst;
-            const u32 x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (u32 y = 0; y < 4; ++y) { d[2 * y] = (u16)x[y]; d[2 * y + 1] = (u16)(x[y] >> 16); }
-          }
-        }
-      }
+      // ---- results: every thread writes its row, 32 bytes at a time
+      const bool direct = j.direct != 0;
+      const float inv = !direct ? 1.0f : l > 0.0f ? 1.0f / l : l;
+      const u64 prow = (u64)j.part * TC_ROWS + i * TC_TILE + rt;
+      u8 *const out = direct ? (u8 *)((u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs) : (u8 *)(scratch_sums(a) + prow * D);
+      have = begin(j);
+      if (n && !(ok = tc_wait(oready + i * 8, seen_o++ & 1, lost))) break;
+      tc_after();
       if (mine) {
-        if (!j.direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * TC_ROWS * D))[j.part * TC_ROWS + prow] = make_float2(m, l);
+        if (!direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * TC_ROWS * D))[prow] = make_float2(m, l);
         else if (a.lse) a.lse[(u64)t * a.n_q_heads + hq] = (m + log2f(l)) * 0.69314718055994531f;
       }
-      __syncwarp();
+      const bool wide = ((uintptr_t)out & 31) == 0;
+#pragma unroll
+      for (u32 c = 0; c < D; c += 64) {
+        u32 y[64];
+        tc_ld32(y, to + c);
+        tc_ld32(y + 32, to + c + 32);
+        tc_wait_ld();
+        if (!n) {                        // no keys: nothing was ever summed up
+#pragma unroll
+          for (u32 z = 0; z < 64; ++z) y[z] = 0;
+        }
+        if (!mine) {
+        } else if (direct) {
+          u32 e[32];
+#pragma unroll
+          for (u32 z = 0; z < 32; ++z) e[z] = Elem<T>::down(__uint_as_float(y[2 * z]) * inv, __uint_as_float(y[2 * z + 1]) * inv);
+          u8 *const dst = out + c * 2;
+          if (wide) {
+#pragma unroll
+            for (u32 z = 0; z < 4; ++z) st_global32(dst + 32 * z, e + 8 * z);
+          } else {
+#pragma unroll
+            for (u32 z = 0; z < 32; ++z) { ((u16 *)dst)[2 * z] = (u16)e[z]; ((u16 *)dst)[2 * z + 1] = (u16)(e[z] >> 16); }
+          }
+        } else {
+          u8 *const dst = out + c * 4;
+          if (wide) {
+#pragma unroll
+            for (u32 z = 0; z < 8; ++z) st_global32(dst + 32 * z, y + 8 * z);
+          } else {                       // scratch is aligned to 16 bytes
+#pragma unroll
+            for (u32 z = 0; z < 16; ++z) *(uint4 *)(dst + 16 * z) = make_uint4(y[4 * z], y[4 * z + 1], y[4 * z + 2], y[4 * z + 3]);
+          }
+        }
+        __syncwarp();
+      }
     }
   }
   tc_before();

@@ -563,13 +563,18 @@ __device__ void find_stretch(const AttendArgs &a, u32 rows, u32 slots, u64 most,
 
 // Kind 2: tiles are cut into pieces, of at most so many blocks. With n pieces in all, the longest of them of p blocks, the
 // kernel ends after about the lesser of
-//   rounds of one piece per SM, ceil(n / SMs) * (p + c)               (all pieces alike)
-//   the SMs' mean share and one more piece, (blocks + n c) / SMs + p + c   (pieces of all lengths)
+//   rounds of one piece per SM, ceil(n / SMs) * (p + c)                          (all pieces alike)
+//   the longest piece, or the SMs' mean share and a third of a mean piece        (pieces of all lengths, the longest first)
 // with c = PIECE_COST blocks for what a piece costs besides, and joining costs JOIN_COST blocks and a quarter of one per
 // partial result. Tried for the longest sequence cut into CUTS[] pieces, and the others into pieces no longer; `most` bounds
-// the partial results. For more than 32 sequences the search would take longer than it gains: pieces of half the mean share.
+// the partial results. Measured: reckoning with a whole longest piece beyond the mean share cuts too often (8 sequences of 1 to
+// 246 new tokens on 108 to 4121: 56.7 us, so 47.0; 2 prompts 154 -> 112); shares of 1/4 to 3/4 of a mean piece, c from 10 to 24
+// and 24 candidates in the place of 12 differ by 1 to 3 % on average.
+// More than 32 sequences are in order 32 by 32 only: two thirds of a mean piece (40 sequences of 60 to 140 tokens on 10 to 3000:
+// 91 us, with half the mean share as the piece's length 110). For more than MOST_WEIGHED the search would take longer than it
+// gains: pieces of the mean share.
 // Every warp takes part with the candidates warp, warp + warps, ...; lane: one of the first 32 sequences.
-constexpr u32 PIECE_COST = 16, JOIN_COST = 24, MIN_PIECE = 16, N_CUTS = 12;      // one for each warp
+constexpr u32 PIECE_COST = 12, JOIN_COST = 24, MIN_PIECE = 16, N_CUTS = 12 /* one for each warp */, MOST_WEIGHED = 512;
 __constant__ const u8 CUTS[N_CUTS] = {1, 2, 3, 4, 5, 6, 7, 9, 12, 16, 22, 32};
 __device__ __forceinline__ u32 cut_length(u32 longest, u32 cuts) { return max(MIN_PIECE, ((longest + cuts - 1) / cuts + 7) / 8 * 8); }   // whole stages
 __device__ __forceinline__ float warp_sum(float x) {
@@ -596,12 +601,23 @@ __device__ __forceinline__ Cut weigh_cuts(const AttendArgs &a, u32 rows, u32 mos
   c.sound = warp_sum(all_tiles) <= most_tiles * 1.001f;
   c.longest = __reduce_max_sync(~0u, longest);
   c.share = warp_sum(blocks) * H / sms;
-  if (c.longest <= MIN_PIECE || !most || a.b.n_seqs > 32) return c;
+  if (c.longest <= MIN_PIECE || !most || a.b.n_seqs > MOST_WEIGHED) return c;
   for (u32 k = warp; k < N_CUTS; k += warps) {
     const u32 piece = k ? cut_length(c.longest, CUTS[k]) : c.longest;
-    const u32 mine = tiles * ((nb + piece - 1) / piece);
-    const float n = __reduce_add_sync(~0u, mine) * H, parts = __reduce_add_sync(~0u, nb > piece ? mine : 0) * H;
-    float cost = fminf(ceilf(n / sms) * (piece + PIECE_COST), c.share + n * PIECE_COST / sms + piece + PIECE_COST);
+    u32 mine = 0, cut = 0;
+    auto count = [&](u32 tiles, u32 nb) {
+      const u32 pieces = tiles * ((nb + piece - 1) / piece);
+      mine += pieces; cut += nb > piece ? pieces : 0;
+    };
+    if (a.b.n_seqs <= 32) count(tiles, nb);
+    else
+      for (u32 s = lane; s < a.b.n_seqs; s += 32) {
+        const Seq x = load_seq(a.b, s, a.err);
+        if (x.n) count(seq_tiles(a, x, rows), seq_blocks(a, x, rows));
+      }
+    const float n = __reduce_add_sync(~0u, mine) * H, parts = __reduce_add_sync(~0u, cut) * H;
+    const float rounds = ceilf(n / sms) * (piece + PIECE_COST), mean = c.share + n * PIECE_COST / sms;
+    float cost = a.b.n_seqs == 1 ? rounds : fminf(rounds, fmaxf(piece + PIECE_COST, mean + (a.b.n_seqs > 32 ? 0.7f : 0.35f) * mean * sms / n));
     if (parts > 0.0f) cost += JOIN_COST + parts * 0.25f;
     if (lane == 0) s_cost[k] = k && parts > most ? INFINITY : cost;
   }
@@ -610,7 +626,7 @@ __device__ __forceinline__ Cut weigh_cuts(const AttendArgs &a, u32 rows, u32 mos
 // The length of a piece; the scheduling warp asks, behind a barrier.
 __device__ __forceinline__ u32 choose_cut(const AttendArgs &a, u32 most, const Cut &c, const float *s_cost) {
   if (c.longest <= MIN_PIECE || !most) return c.longest;
-  if (a.b.n_seqs > 32) return (u32)fminf((float)c.longest, fmaxf((float)MIN_PIECE, ceilf((c.share / 2 + 1) / 8) * 8));
+  if (a.b.n_seqs > MOST_WEIGHED) return (u32)fminf((float)c.longest, fmaxf((float)MIN_PIECE, ceilf((c.share + 1) / 8) * 8));
   const u32 lane = threadIdx.x & 31, cost = lane < N_CUTS ? __float_as_uint(s_cost[lane]) : ~0u;      // positive: ordered as integers
   const u32 k = __ffs(__ballot_sync(~0u, cost == __reduce_min_sync(~0u, cost))) - 1;
   return k ? cut_length(c.longest, CUTS[k]) : c.longest;

@@ -289,6 +289,39 @@ def test_attend_many_sequences(B):
     check_attend(s)
 
 
+@pytest.mark.parametrize("n,new,past", [(40, 90, 3000), (540, 40, 260), (3, 700, 9000)])
+def test_attend_ragged_sequences_in_pieces(B, n, new, past):
+    """Pieces of one length over sequences of many, more sequences than are ordered (or weighed) at a time, some with nothing."""
+    rng = np.random.default_rng(n)
+    news = [int(x) for x in rng.integers(0, new, n)]
+    s = Setup(B, news, [int(x) for x in rng.integers(0, past, n)], heads=1, group=3, dim=64 if n > 500 else 128, seed=n)
+    s.put()
+    check_attend(s)
+
+
+def test_attend_scratch_at_any_16_bytes(B):
+    """Partial results in scratch that is aligned to 16 bytes and no more, with something else before it."""
+    import torch
+    s = Setup(B, [300], [4000], heads=2, group=2, dim=128, seed=5)
+    s.put()
+    want = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
+    real = torch.empty
+    offset = []
+
+    def empty(*size, **kw):
+        if kw.get("dtype") is torch.uint8 and len(size) == 1 and isinstance(size[0], int):
+            offset.append(size[0])
+            return real(size[0] + 16, **kw)[16:]
+        return real(*size, **kw)
+
+    torch.empty = empty
+    try:
+        got = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
+    finally:
+        torch.empty = real
+    assert offset and torch.equal(want, got)
+
+
 def test_attend_scores_that_climb_and_scores_of_one_huge_key(B):
     """The running maximum has to be raised again and again, by little and by much, in either kernel."""
     import torch

@@ -8,8 +8,10 @@
  *   (2) lookup of those hashes in a GPU-resident open-addressing block table (reusable prefix),
  *   (3) derivation of each resident block's KV-level lifecycle state from message-level states
  *       (Section 5.2 state machine; Section 6.1, the paragraph on KV shared between contexts),
- *   (4) state-prioritised, recency-ordered victim selection (Algorithm 1; Section 6.2), and
- *   (5) movement of paged KV blocks between the HBM pool, a pinned host tier and an optional third tier (Section 7).
+ *   (4) state-prioritised, recency-ordered victim selection (Algorithm 1; Section 6.2),
+ *   (5) movement of paged KV blocks between the HBM pool, a pinned host tier and an optional third tier (Section 7), and
+ *   (6) what a model does with the pool: appending the K and V of new tokens (with the rotation of their positions) and
+ *       attention of the new tokens over everything their sequences hold there.
  *
  * General conventions
  *   - Plain C, no exceptions, no stdout. Every function returns an int32_t status: KVT_OK (0) or a
@@ -456,11 +458,11 @@ typedef struct kvt_attend_args {
 
 /* softmax(scale q k^T) v of the new tokens over their sequences' keys and values in the pool (their own included:
  * append first). A row that sees no key gives zeros and lse = -inf. Scores, sums and the output are held in 32 bits;
- * the probabilities are rounded to the element type for the second product. Keys a row does not see have no effect,
- * whatever their values, with one exception: a value that is Inf or NaN in a token that other rows of the
- * sequence see may reach all of that sequence's new rows. What lies in a block behind kv_len has no effect. Errors: KVT_E_INVAL as above
- * (head_dim above 256, heads that do not divide, window with KVT_ATTN_FULL, scale that is negative or not finite),
- * KVT_E_BUFSZ scratch too small. Asynchronous. */
+ * the probabilities are rounded to the element type for the second product (in fp16, where there are few rows, carried
+ * exactly). Keys a row does not see have no effect, whatever their values, with one exception: a value that is Inf or
+ * NaN in a token that other rows of the sequence see may reach all of that sequence's new rows. What lies in a block
+ * behind kv_len has no effect. Errors: KVT_E_INVAL as above (head_dim above 256, heads that do not divide, window with
+ * KVT_ATTN_FULL, scale that is negative or not finite), KVT_E_BUFSZ scratch too small. Asynchronous. */
 int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *a, void *stream);
 /* Depends on sizes only (n_seqs, n_tokens, max_blocks, max_q_len, n_q_heads), not on what device arrays hold.
  * 0 for arguments kvt_attend refuses and where none is needed. */

@@ -278,7 +278,10 @@ cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, u32 *launches) {
 
 // ======================================================================================================
 // Attention. Rows: the (token, query head of the group) pairs of one sequence and one KV head, token-major, so that row r
-// is token r / group, head r % group. A CTA takes a tile of consecutive rows, which all read the same K and V.
+// is token r / group, head r % group. A CTA takes a tile of consecutive rows, which all read the same K and V once:
+//   m = max_j s_j, l = sum_j 2^(s_j - m), o = sum_j 2^(s_j - m) v_j, s_j = scale log2(e) q.k_j, result o / l,
+// over one block of keys after the other: where m rises, l and o are multiplied by 2^(old m - new m). Parts of the keys that
+// different warps or CTAs went over are put together by the same rule. Scores, m, l and o are 32-bit numbers.
 // ======================================================================================================
 // Keys row `token` (0 = first new token) sees: [lo, hi).
 __device__ __forceinline__ void row_range(const AttendArgs &a, const Seq &q, u32 token, u32 &lo, u32 &hi) {
@@ -331,7 +334,8 @@ __device__ bool find_tile(const AttendArgs &a, u32 rows, u32 want, Seq &q, u32 &
 
 // Any head size up to 256, any alignment: 32-bit arithmetic on the CUDA cores. A CTA takes 16 rows, a warp 4 of them;
 // K and V of 32 keys at a time go through shared memory as 32-bit values; a lane forms the scores of one key, and in
-// the second product owns every 32nd column of the output.
+// the second product owns every 32nd column of the output. Bound by shared memory and multiply-adds: it is there so that every
+// head size has its result, not for speed (heads of 64 and 128 never come here).
 constexpr u32 ANY_ROWS = 16, ANY_KEYS = 32, ANY_THREADS = 128, ANY_MAX_DIM = 256;
 
 template <class T>
@@ -823,6 +827,10 @@ __global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, 
 // the keys for up to 16 rows of one KV head, the height of a warp-level matrix instruction. Every warp has its own ring
 // of TMA loads (a block's K and V per stage) and its own running maximum and sums over every fourth block, so warps
 // never wait for one another until the end of a unit. Two CTAs per SM keep up to 192 KB of loads in flight.
+// The matrix units idle most of the time (20 % busy), so the warp-level instructions do, whose sums and operands lie in
+// registers: nothing has to be handed from one kind of warp to another.
+// Measured, heads of 128, 8 KV heads, groups of 4: one token on 258,047 (1.06 GB) 169-173 us with the join, 6.2 TB/s, 95 % of the
+// measured copy bandwidth; 32 tokens on 2,000 to 130,000 each (6.1 GB, groups of 12) 905 us, 102 %.
 // ------------------------------------------------------------------------------------------------------
 constexpr u32 SPLIT_ROWS = 16, SPLIT_WARPS = 4, SPLIT_THREADS = SPLIT_WARPS * 32;
 template <u32 D> struct SplitShape {
@@ -1160,7 +1168,9 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
 }
 
 // Few units of moderate length: a cluster of CTAs takes a unit, its blocks dealt out evenly, and joins the parts through the
-// CTAs' shared memory: one launch, no scratch.
+// CTAs' shared memory: one launch, no scratch. Bound by latency: 4 us for the launch, the lengths and the first block, then a
+// block of each warp's every 0.8 us, then the join through shared memory. One token, 8 KV heads of 128, groups of 4: 300 cached
+// tokens 6.2 us, 1000 7.0, 4000 10.5, 8000 13.9 (33 MB, 2.4 TB/s); the kernel with two launches takes 11.6, 13.7 and 14.8.
 template <class T, u32 D, u32 CLUSTER>
 __global__ void __launch_bounds__(SPLIT_THREADS, 2)
 k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps) {
@@ -1277,7 +1287,15 @@ k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ K
 //   warps 0-7   one thread per row: maximum, powers, sum; P goes back to tensor memory in the place of S, as the first
 //               operand of the second product
 // The two tiles take turns: while one tile's powers are computed the tensor cores work on the other. Tensor memory: S0,
-// S1 (128 columns each), O0, O1 (head_dim columns each).
+// S1 (128 columns each), O0, O1 (head_dim columns each): full with heads of 128, so S is not held twice, and a tile's next S
+// waits for the second product of its P.
+// Measured (heads of 128, bf16): 128 keys for both tiles take 2950 cycles, of which the tensor cores need 2040 and the exponential
+// units 2048: a row waits 830 cycles for its S, then 50 to load it, 350 for the maximum, 1460 for the powers, 160 for the store.
+// 8192 new tokens, 8 KV heads, groups of 4: 434-440 us cold (1260 TFLOP/s; 76 % of the measured matrix rate), 508 us at the
+// 1.58 GHz that the power limit leaves when it runs on and on (1081 TFLOP/s, 78 % of the sustained rate). 500 tokens on 130,500:
+// 890-1000 us. Tried and slower or the same: two threads per row (480 us where this took 465), a thread issuing the products
+// for each tile (525: the tiles fall into step), P handed over in four parts, a polynomial for every fourth power (0-4 %).
+// Between two jobs of a CTA 4 us pass, and a launch has its first S after 6 us, most of it for working out the jobs.
 // ------------------------------------------------------------------------------------------------------
 constexpr u32 TC_ROWS = 256, TC_TILE = 128, TC_KEYS = 128, TC_KB = TC_KEYS / BT, TC_THREADS = 384;
 template <u32 D> struct TcShape {
@@ -1899,12 +1917,12 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
     break;
   }
   // One tile of 16 rows reads K and V once. With more rows the kernels for few rows read them once per tile, but they start and
-  // end 8 us sooner, which decides when there is little to do: up to 8 K blocks (of 16 rows and one KV head, as many as fit
+  // end 7 us sooner, which decides when there is little to do: up to 8 K blocks (of 16 rows and one KV head, as many as fit
   // the table rows), 24 K in clusters, or 32 K where a sequence has two tiles only. Measured, us of few / many rows, heads of 128:
-  //   64 tokens 6.6 / 12.2, 128 tokens 8.2 / 12.2, 200 tokens 16.3 / 14.0 (1.5 K, 4.1 K, 8.4 K blocks; groups of 4, 8 KV heads)
-  //   clusters: 64 on 1000 14.8 / 23.6, 2 x 20 on 3000 17.1 / 31.0, 32 on 4000 20.7 / 28.2 (9.6 K, 12 K, 17 K); others: 100 on
-  //   2000 38.6 / 28.8 (28 K)
-  //   two tiles: 8 x 8 on 2000 28.4 / 32.0, 32 x 8 on 500 24.5 / 29.0 (25 K, 30 K)
+  //   64 tokens 6.4 / 13.4, 128 tokens 8.3 / 13.6, 200 tokens 16.4 / 12.9 (1.5 K, 4.1 K, 8.4 K blocks; groups of 4, 8 KV heads)
+  //   clusters: 64 on 1000 14.7 / 25.1, 2 x 20 on 3000 17.1 / 30.4, 32 on 4000 20.8 / 29.6 (9.6 K, 12 K, 17 K); others: 100 on
+  //   2000 38.8 / 28.0 (28 K)
+  //   two tiles: 16 x 8 on 500 14.1 / 17.0, 10 x 8 on 1000 20.8 / 23.1, 32 x 8 on 500 24.4 / 24.0 (15 K, 16 K, 30 K; heads of 64: 20.2 / 21.2)
   const u64 rows = (u64)(max_q_len && max_q_len < a.b.n_tokens ? max_q_len : a.b.n_tokens) * a.group, few = units16 * (nb + UNIT_COST);
   if (rows <= SPLIT_ROWS || few <= (cluster ? 24576 : 8192) || (rows <= 2 * SPLIT_ROWS && few <= 32768)) {
     p.rows = SPLIT_ROWS;

@@ -332,108 +332,6 @@ __device__ bool find_tile(const AttendArgs &a, u32 rows, u32 want, Seq &q, u32 &
   return true;
 }
 
-// Any head size up to 256, any alignment: 32-bit arithmetic on the CUDA cores. A CTA takes 16 rows, a warp 4 of them;
-// K and V of 32 keys at a time go through shared memory as 32-bit values; a lane forms the scores of one key, and in
-// the second product owns every 32nd column of the output. Bound by shared memory and multiply-adds: it is there so that every
-// head size has its result, not for speed (heads of 64 and 128 never come here).
-constexpr u32 ANY_ROWS = 16, ANY_KEYS = 32, ANY_THREADS = 128, ANY_MAX_DIM = 256;
-
-template <class T>
-__global__ void __launch_bounds__(ANY_THREADS) k_attend_any(AttendArgs a) {
-  extern __shared__ float sm[];
-  const u32 D = a.p.head_dim, H = a.p.n_kv_heads, h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  float *const sq = sm, *const sk = sq + ANY_ROWS * D, *const sv = sk + ANY_KEYS * (D + 1);
-  Seq q; u32 seq, tile;
-  if (!find_tile<ANY_THREADS>(a, ANY_ROWS, blockIdx.x, q, seq, tile)) return;
-  const u32 n_rows = q.n * a.group, r0 = tile * ANY_ROWS;
-  for (u32 i = tid; i < ANY_ROWS * D; i += ANY_THREADS) {
-    const u32 r = r0 + i / D, d = i % D;
-    sq[i] = r < n_rows ? Elem<T>::up1(((const T *)a.q)[(q.t0 + r / a.group) * a.q_ts + (h * a.group + r % a.group) * a.q_hs + d]) : 0.0f;
-  }
-  u32 lo[4], hi[4];
-#pragma unroll
-  for (u32 x = 0; x < 4; ++x) {
-    const u32 r = r0 + warp * 4 + x;
-    lo[x] = hi[x] = 0;
-    if (r < n_rows) row_range(a, q, r / a.group, lo[x], hi[x]);
-  }
-  u32 first, last, dummy;      // keys any row of the tile sees
-  row_range(a, q, r0 / a.group, first, dummy);
-  row_range(a, q, (min(r0 + ANY_ROWS, n_rows) - 1) / a.group, dummy, last);
-  float m[4], l[4], acc[4][ANY_MAX_DIM / 32];
-#pragma unroll
-  for (u32 x = 0; x < 4; ++x) {
-    m[x] = -INFINITY; l[x] = 0.0f;
-#pragma unroll
-    for (u32 c = 0; c < ANY_MAX_DIM / 32; ++c) acc[x][c] = 0.0f;
-  }
-  for (u32 k0 = first; k0 < last; k0 += ANY_KEYS) {
-    __syncthreads();
-    for (u32 i = tid; i < ANY_KEYS * D; i += ANY_THREADS) {
-      const u32 kk = i / D, d = i - kk * D, key = k0 + kk;
-      float kx = 0.0f, vx = 0.0f;
-      if (key < last) {
-        const u32 slot = a.b.table[seq * a.b.table_stride + key / BT];
-        const T *kp = (const T *)slot_ptr(a.p, a.p.k, slot), *vp = (const T *)slot_ptr(a.p, a.p.v, slot);
-        if (kp) {
-          const u64 off = ((u64)(key % BT) * H + h) * D + d;
-          kx = Elem<T>::up1(kp[off]); vx = Elem<T>::up1(vp[off]);
-        } else if (d == 0) kv_err(a.err, KVERR_RANGE);
-      }
-      sk[kk * (D + 1) + d] = kx; sv[kk * D + d] = vx;
-    }
-    __syncthreads();
-    float p[4] = {0, 0, 0, 0};
-    for (u32 d = 0; d < D; ++d) {
-      const float kx = sk[lane * (D + 1) + d];
-#pragma unroll
-      for (u32 x = 0; x < 4; ++x) p[x] += sq[(warp * 4 + x) * D + d] * kx;
-    }
-#pragma unroll
-    for (u32 x = 0; x < 4; ++x) {
-      const u32 key = k0 + lane;
-      const float s = key >= lo[x] && key < hi[x] ? p[x] * a.scale_log2 : -INFINITY;
-      float top = s;
-#pragma unroll
-      for (u32 o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-      const float now = fmaxf(m[x], top), ref = now == -INFINITY ? 0.0f : now, f = exp2f(m[x] - ref);
-      p[x] = exp2f(s - ref);
-      float sum = p[x];
-#pragma unroll
-      for (u32 o = 16; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-      l[x] = l[x] * f + sum;
-      m[x] = now;
-#pragma unroll
-      for (u32 c = 0; c < ANY_MAX_DIM / 32; ++c) acc[x][c] *= f;
-    }
-    for (u32 kk = 0; kk < ANY_KEYS; ++kk) {
-      float w[4];
-#pragma unroll
-      for (u32 x = 0; x < 4; ++x) w[x] = __shfl_sync(~0u, p[x], kk);
-#pragma unroll
-      for (u32 c = 0; c < ANY_MAX_DIM / 32; ++c) {
-        const u32 d = c * 32 + lane;
-        if (d < D) {
-          const float vx = sv[kk * D + d];
-#pragma unroll
-          for (u32 x = 0; x < 4; ++x) acc[x][c] += w[x] * vx;
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (u32 x = 0; x < 4; ++x) {
-    const u32 r = r0 + warp * 4 + x;
-    if (r >= n_rows) continue;
-    const u32 t = q.t0 + r / a.group, hq = h * a.group + r % a.group;
-    const float inv = l[x] > 0.0f ? 1.0f / l[x] : l[x] == 0.0f ? 0.0f : l[x];   // no key: zeros; a NaN stays one
-    T *o = (T *)a.out + t * a.o_ts + hq * a.o_hs;
-#pragma unroll
-    for (u32 c = 0; c < ANY_MAX_DIM / 32; ++c) { const u32 d = c * 32 + lane; if (d < D) o[d] = Elem<T>::down1(acc[x][c] * inv); }
-    if (a.lse && lane == 0) a.lse[(u64)t * a.n_q_heads + hq] = (m[x] + log2f(l[x])) * 0.69314718055994531f;
-  }
-}
-
 // ------------------------------------------------------------------------------------------------------
 // Shared by the kernels that read the pool with TMA.
 // ------------------------------------------------------------------------------------------------------
@@ -834,7 +732,7 @@ __global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, 
 // ------------------------------------------------------------------------------------------------------
 constexpr u32 SPLIT_ROWS = 16, SPLIT_WARPS = 4, SPLIT_THREADS = SPLIT_WARPS * 32;
 template <u32 D> struct SplitShape {
-  static constexpr u32 BLOCK = BT * D * 2, STAGES = 3 * 128 / D, RING = STAGES * 2 * BLOCK, SMEM = SPLIT_WARPS * RING + 1024;
+  static constexpr u32 BLOCK = BT * D * 2, STAGES = D == 64 ? 6 : 3, RING = STAGES * 2 * BLOCK, SMEM = SPLIT_WARPS * RING + 1024;
 };
 
 template <class T> __device__ __forceinline__ void mma16816(float (&c)[4], const u32 (&a)[4], u32 b0, u32 b1);
@@ -857,10 +755,36 @@ template <u32 D> __device__ __forceinline__ u32 block_off(u32 r, u32 c) {
   return (r / 8) * (D * 16) + (c / 8) * 1024 + (r % 8) * 128 + (((c % 8) ^ (r % 8)) * 16);
 }
 
+// Heads that are not 64 or 128 wide, or not as TMA wants them: one head of one block, whole warp, in the same places; columns
+// behind the head stay as they are. A slot beyond both pools reads as zeros.
+template <u32 D>
+__device__ __forceinline__ void copy_block(const AttendArgs &a, const KvRow &row, u32 slot, u32 h, u32 dst) {
+  const u32 d = a.p.head_dim, n = (d + 7) / 8, lane = threadIdx.x & 31;
+  const u8 *const src = slot_ptr(a.p, row, slot);
+  const u64 pitch = (u64)a.p.n_kv_heads * d;             // elements
+  const bool vec = src && d % 8 == 0 && ((uintptr_t)src & 15) == 0;
+  u32 r = lane / n, c = lane % n;
+  while (r < BT) {
+    const u32 to = dst + block_off<D>(r, c);
+    const u16 *const p = (const u16 *)src + (src ? r * pitch + (u64)h * d + c * 8 : 0);
+    if (vec) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p) : "memory");
+    } else {
+      u32 x[4] = {0, 0, 0, 0};
+      if (src)
+#pragma unroll
+        for (u32 y = 0; y < 8; ++y) if (c * 8 + y < d) x[y / 2] |= (u32)p[y] << (y % 2 * 16);
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+    }
+    r += 32 / n; c += 32 % n;
+    if (c >= n) { c -= n; ++r; }
+  }
+}
+
 // The keys in blocks [b0, b1) for rows r0 .. r1 of a sequence: this warp's share of them, every fourth block. o, m, l: sums,
 // maximum and sum of powers of rows lane / 4 and lane / 4 + 8, this lane's columns and keys. `it`: stages used so far. false: a
-// wait ran out.
-template <class T, u32 D>
+// wait ran out. ANY: heads of any size up to D, filled up with zeros.
+template <class T, u32 D, bool ANY = false>
 __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &maps, const Seq &q, u32 seq, u32 h, u32 r0, u32 r1, u32 b0, u32 b1,
                                            u32 ring, u32 bar0, u32 &it, float (&o)[D / 8][4], float (&m)[2], float (&l)[2]) {
   typedef SplitShape<D> S;
@@ -878,15 +802,30 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
       if (i + lane < n_mine && held >= a.p.n_slots && held - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
     }
     const u32 slot = __shfl_sync(~0u, held, i % 32);
-    if (lane == 0) {
+    if (ANY) {
+      const u32 dst = ring + (it + i) % S::STAGES * 2 * S::BLOCK;
+      copy_block<D>(a, a.p.k, slot, h, dst);
+      copy_block<D>(a, a.p.v, slot, h, dst + S::BLOCK);
+    } else if (lane == 0) {
       const u32 st = (it + i) % S::STAGES, bar = bar0 + st * 8, dst = ring + st * 2 * S::BLOCK;
       bar_expect(bar, 2 * S::BLOCK);
       load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
       load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
     }
   };
-  const u32 n_pro = min(n_mine, S::STAGES);
-  for (u32 i = 0; i < n_pro; ++i) load(i);
+  if (ANY) {
+    const u32 n = (a.p.head_dim + 7) / 8;
+    if (n < D / 8)
+      for (u32 i = lane; i < S::STAGES * 2 * BT * (D / 8 - n); i += 32) {
+        const u32 r = i / (D / 8 - n);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + r / BT * S::BLOCK + block_off<D>(r % BT, n + i % (D / 8 - n))), "r"(0) : "memory");
+      }
+  }
+#pragma unroll 1
+  for (u32 i = 0; i < S::STAGES; ++i) {
+    if (i < n_mine) load(i);
+    if (ANY) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
 
   // queries: rows lane / 4 and lane / 4 + 8 of the tile, in the registers of the first operand
   u32 qf[D / 16][4];
@@ -902,7 +841,12 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
 #pragma unroll
       for (u32 z = 0; z < 2; ++z) {
         const u16 *p = src + k * 16 + z * 8;
-        qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+        if (ANY) {
+          const u32 c = (lane % 4) * 2 + k * 16 + z * 8;
+          qf[k][y + 2 * z] = (c < a.p.head_dim ? (u32)p[0] : 0u) | (c + 1 < a.p.head_dim ? (u32)p[1] << 16 : 0u);
+        } else {
+          qf[k][y + 2 * z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+        }
       }
   }
   m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.0f;
@@ -913,7 +857,10 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
 
   for (u32 i = 0; ok && i < n_mine; ++i) {
     const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
-    if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
+    if (ANY) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
+      __syncwarp();
+    } else if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, ((it + i) / S::STAGES) & 1)))) break;
     const u32 key0 = (b0 + warp + i * SPLIT_WARPS) * BT;
     // scores of 16 keys: two column groups of 8
     float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -992,6 +939,7 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
     }
     __syncwarp();                      // the stage is read: refill it
     if (i + S::STAGES < n_mine) load(i + S::STAGES);
+    if (ANY) asm volatile("cp.async.commit_group;" ::: "memory");
   }
   it += n_mine;
   return ok;
@@ -1171,8 +1119,14 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
 // CTAs' shared memory: one launch, no scratch. Bound by latency: 4 us for the launch, the lengths and the first block, then a
 // block of each warp's every 0.8 us, then the join through shared memory. One token, 8 KV heads of 128, groups of 4: 300 cached
 // tokens 6.2 us, 1000 7.0, 4000 10.5, 8000 13.9 (33 MB, 2.4 TB/s); the kernel with two launches takes 11.6, 13.7 and 14.8.
-template <class T, u32 D, u32 CLUSTER>
-__global__ void __launch_bounds__(SPLIT_THREADS, 2)
+//
+// ANY: heads of every other size up to 256 and every alignment, filled up to 64, 128 or 256 columns with zeros (three widths are
+// enough: the matrix units have time, and no more bytes are read). K and V come with 16-byte copies where the head allows it,
+// element by element elsewhere. Long sequences and prompts are its work too, without a kernel of their own. Heads of 96, 8 KV
+// heads, groups of 4: one token on 4000 22 us, 1000 new tokens 176 us, 32 on 1000 18 us (with 32-bit arithmetic on the CUDA
+// cores and one CTA per unit 1613, 1064 and 424).
+template <class T, u32 D, u32 CLUSTER, bool ANY>
+__global__ void __launch_bounds__(SPLIT_THREADS, D > 128 ? 1 : 2)
 k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps) {
   typedef SplitShape<D> S;
   extern __shared__ u8 smem_raw[];
@@ -1187,7 +1141,7 @@ k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ K
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
+  if (!ANY && tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
   Seq q; u32 seq, tile;
   if (!find_tile<SPLIT_THREADS>(a, SPLIT_ROWS, unit / H, q, seq, tile)) return;      // the whole cluster
   const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
@@ -1195,7 +1149,7 @@ k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ K
   u32 b_first, it = 0;
   const u32 nb = tile_blocks(a, q, r0, r1, b_first), per = (nb + CLUSTER - 1) / CLUSTER;
   float o[D / 8][4], m[2], l[2];
-  const bool ok = split_keys<T, D>(a, maps, q, seq, h, r0, r1, b_first + min(rank * per, nb), b_first + min((rank + 1) * per, nb), ring, bar0, it, o, m, l);
+  const bool ok = split_keys<T, D, ANY>(a, maps, q, seq, h, r0, r1, b_first + min(rank * per, nb), b_first + min((rank + 1) * per, nb), ring, bar0, it, o, m, l);
   split_leave<D>(smem_raw, ring, o, m, l, s_ml);
   const bool lost = __syncthreads_or(!ok);
   // this CTA's part: sums behind warp 0's in its ring
@@ -1267,13 +1221,14 @@ k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ K
   const float inv = sum > 0.0f ? 1.0f / sum : sum;
   const u32 t = q.t0 + (r0 + r) / a.group, hq = h * a.group + (r0 + r) % a.group;
   u16 *const out = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + c;
-  if (COLS >= 4 && ((uintptr_t)out & 7) == 0) {
+  const u32 d = ANY ? a.p.head_dim : D;
+  if (COLS >= 4 && ((uintptr_t)out & 7) == 0 && c + COLS <= d) {
 #pragma unroll
     for (u32 z = 0; z < COLS; z += 4)
       *(uint2 *)(out + z) = make_uint2(Elem<T>::down(e[z] * inv, e[(z + 1) % COLS] * inv), Elem<T>::down(e[(z + 2) % COLS] * inv, e[(z + 3) % COLS] * inv));
   } else {
 #pragma unroll
-    for (u32 z = 0; z < COLS; ++z) ((T *)out)[z] = Elem<T>::down1(e[z] * inv);
+    for (u32 z = 0; z < COLS; ++z) if (c + z < d) ((T *)out)[z] = Elem<T>::down1(e[z] * inv);
   }
   if (a.lse && c == 0) a.lse[(u64)t * a.n_q_heads + hq] = (top + log2f(sum)) * 0.69314718055994531f;
 }
@@ -1281,9 +1236,10 @@ k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ K
 // ------------------------------------------------------------------------------------------------------
 // Many rows (prompts, chunks of new tokens): bound by the tensor cores and the exponentials. A CTA takes up to 256 rows
 // of one KV head as two tiles of 128, the height of a tcgen05 matrix instruction, and walks over the keys 128 at a time.
+//   warp 11     brings the coming jobs' queries into the L2 cache
 //   warp 10     works out the CTA's jobs
 //   warp 9      loads K and V (TMA, one box per block) into a ring of 128-key stages
-//   warp 8      issues the matrix products (warp 11 only gives up its registers): S = Q K^T and O += P V, both accumulated in tensor memory
+//   warp 8      issues the matrix products: S = Q K^T and O += P V, both accumulated in tensor memory
 //   warps 0-7   one thread per row: maximum, powers, sum; P goes back to tensor memory in the place of S, as the first
 //               operand of the second product
 // The two tiles take turns: while one tile's powers are computed the tensor cores work on the other. Tensor memory: S0,
@@ -1899,8 +1855,11 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
   // no more tiles than this: every sequence adds less than one to the quotient
   auto tiles = [&](u64 rows) { return ((u64)a.b.n_tokens * a.group + a.b.n_seqs * (rows - 1)) / rows; };
   if (a.p.head_dim != 64 && a.p.head_dim != 128) {
-    p.rows = ANY_ROWS;
-    p.grid = (u32)std::min<u64>(tiles(p.rows), 0x7FFFFFFFu);
+    // a unit's keys over up to 8 CTAs, as long as all run at once and each of their warps has a block or more
+    const u64 units = tiles(SPLIT_ROWS) * H, slots = (a.p.head_dim > 128 ? 1ull : 2ull) * sm_count;
+    p.rows = SPLIT_ROWS;
+    for (p.cluster = 1; p.cluster < 8 && units * p.cluster * 2 <= slots && a.b.max_blocks >= 8 * p.cluster; p.cluster *= 2) {}
+    p.grid = (u32)std::min<u64>(units * p.cluster, 0x7FFFFFFFu / p.cluster * p.cluster);
     return p;
   }
   // Units so few that several CTAs fit on each: clusters of as many as run at once (16 of them only for 8 units and less: more
@@ -1956,16 +1915,16 @@ AttendPlan plan_attend(const AttendArgs &a, u32 max_q_len, int sm_count) {
 
 // Dynamic shared memory above 48 KB is asked for once per kernel and engine (a runtime call of half a microsecond).
 template <class K>
-static cudaError_t allow_smem(K kern, u32 which, u32 bytes, u32 *allowed) {
+static cudaError_t allow_smem(K kern, u32 which, u32 bytes, u64 *allowed) {
   if (*allowed >> which & 1) return cudaSuccess;
   const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (r == cudaSuccess) *allowed |= 1u << which;
+  if (r == cudaSuccess) *allowed |= 1ull << which;
   return r;
 }
 
 template <class T, u32 D>
-static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
-  cudaError_t r = allow_smem(k_attend_split<T, D>, 2 + (D == 128) * 2 + a.fp16, SplitShape<D>::SMEM, allowed);
+static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
+  cudaError_t r = allow_smem(k_attend_split<T, D>, (D == 128) * 2 + a.fp16, SplitShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
   k_attend_split<T, D><<<p.grid, SPLIT_THREADS, SplitShape<D>::SMEM, s>>>(a, m, p.parts, 2 * p.sms, p.most);
   ++*launches;
@@ -1975,14 +1934,16 @@ static cudaError_t launch_split(const AttendArgs &a, const AttendPlan &p, const 
   return launch_join(k_attend_join_split<T, D, 4>, 128, rows, p.sms, s, launches, a, p.parts);
 }
 
-template <class T, u32 D, u32 CLUSTER>
-static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
-  constexpr u32 which = 10 + (CLUSTER == 16 ? 3 : CLUSTER == 8 ? 2 : CLUSTER == 4 ? 1 : 0) * 4 + (D == 128) * 2 + (sizeof(T) == 2 && __is_same(T, __half));
+template <class T, u32 D, u32 CLUSTER, bool ANY>
+static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
+  constexpr u32 size = CLUSTER == 16 ? 4 : CLUSTER == 8 ? 3 : CLUSTER == 4 ? 2 : CLUSTER == 2 ? 1 : 0, width = D == 256 ? 2 : D == 128 ? 1 : 0;
+  constexpr u32 which = 8 + ((ANY ? 10 : 0) + (ANY ? 4 : 5) * width + size) * 2 + __is_same(T, __half);      // 8 .. 51
+  auto const kern = k_attend_cluster<T, D, CLUSTER, ANY>;
   if (CLUSTER > 8 && !(*allowed >> which & 1)) {
-    const cudaError_t r = cudaFuncSetAttribute(k_attend_cluster<T, D, CLUSTER>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (r != cudaSuccess) return r;
   }
-  cudaError_t r = allow_smem(k_attend_cluster<T, D, CLUSTER>, which, SplitShape<D>::SMEM, allowed);
+  cudaError_t r = allow_smem(kern, which, SplitShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3(p.grid); c.blockDim = dim3(SPLIT_THREADS); c.dynamicSmemBytes = SplitShape<D>::SMEM; c.stream = s;
@@ -1991,21 +1952,30 @@ static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, cons
   at.val.clusterDim.x = CLUSTER; at.val.clusterDim.y = at.val.clusterDim.z = 1;
   c.attrs = &at; c.numAttrs = 1;
   ++*launches;
-  return cudaLaunchKernelEx(&c, k_attend_cluster<T, D, CLUSTER>, a, m);
+  return cudaLaunchKernelEx(&c, kern, a, m);
 }
 template <class T, u32 D>
-static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
+static cudaError_t launch_cluster(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
   switch (p.cluster) {
-    case 2: return launch_cluster<T, D, 2>(a, p, m, s, allowed, launches);
-    case 4: return launch_cluster<T, D, 4>(a, p, m, s, allowed, launches);
-    case 8: return launch_cluster<T, D, 8>(a, p, m, s, allowed, launches);
-    default: return launch_cluster<T, D, 16>(a, p, m, s, allowed, launches);
+    case 2: return launch_cluster<T, D, 2, false>(a, p, m, s, allowed, launches);
+    case 4: return launch_cluster<T, D, 4, false>(a, p, m, s, allowed, launches);
+    case 8: return launch_cluster<T, D, 8, false>(a, p, m, s, allowed, launches);
+    default: return launch_cluster<T, D, 16, false>(a, p, m, s, allowed, launches);
+  }
+}
+template <class T, u32 D>
+static cudaError_t launch_any(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
+  switch (p.cluster) {
+    case 1: return launch_cluster<T, D, 1, true>(a, p, m, s, allowed, launches);
+    case 2: return launch_cluster<T, D, 2, true>(a, p, m, s, allowed, launches);
+    case 4: return launch_cluster<T, D, 4, true>(a, p, m, s, allowed, launches);
+    default: return launch_cluster<T, D, 8, true>(a, p, m, s, allowed, launches);
   }
 }
 
 template <class T, u32 D>
-static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
-  cudaError_t r = allow_smem(k_attend_tc<T, D>, 6 + (D == 128) * 2 + a.fp16, TcShape<D>::SMEM, allowed);
+static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
+  cudaError_t r = allow_smem(k_attend_tc<T, D>, 4 + (D == 128) * 2 + a.fp16, TcShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
   k_attend_tc<T, D><<<p.grid, TC_THREADS, TcShape<D>::SMEM, s>>>(a, m, p.parts, p.most);
   ++*launches;
@@ -2013,7 +1983,7 @@ static cudaError_t launch_tc(const AttendArgs &a, const AttendPlan &p, const KvM
   return launch_join(k_attend_join_tc<T, D>, 128, ((u64)a.b.n_tokens * ((a.n_q_heads + 3) / 4) + 3) / 4, p.sms, s, launches, a, p.rows, p.parts);
 }
 
-cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u32 *allowed, u32 *launches) {
+cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
   if (p.kind == 2) {
     if (a.p.head_dim == 64) return a.fp16 ? launch_tc<__half, 64>(a, p, m, s, allowed, launches) : launch_tc<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
     return a.fp16 ? launch_tc<__half, 128>(a, p, m, s, allowed, launches) : launch_tc<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
@@ -2026,13 +1996,9 @@ cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps
     if (a.p.head_dim == 64) return a.fp16 ? launch_split<__half, 64>(a, p, m, s, allowed, launches) : launch_split<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
     return a.fp16 ? launch_split<__half, 128>(a, p, m, s, allowed, launches) : launch_split<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
   }
-  const u32 D = a.p.head_dim, smem = (ANY_ROWS * D + ANY_KEYS * (D + 1) + ANY_KEYS * D) * 4;
-  auto kern = a.fp16 ? k_attend_any<__half> : k_attend_any<__nv_bfloat16>;
-  cudaError_t r = allow_smem(kern, a.fp16, (ANY_ROWS + 2 * ANY_KEYS) * (ANY_MAX_DIM + 1) * 4, allowed);
-  if (r != cudaSuccess) return r;
-  kern<<<dim3(p.grid, a.p.n_kv_heads), ANY_THREADS, smem, s>>>(a);
-  ++*launches;
-  return cudaGetLastError();
+  if (a.p.head_dim <= 64) return a.fp16 ? launch_any<__half, 64>(a, p, m, s, allowed, launches) : launch_any<__nv_bfloat16, 64>(a, p, m, s, allowed, launches);
+  if (a.p.head_dim <= 128) return a.fp16 ? launch_any<__half, 128>(a, p, m, s, allowed, launches) : launch_any<__nv_bfloat16, 128>(a, p, m, s, allowed, launches);
+  return a.fp16 ? launch_any<__half, 256>(a, p, m, s, allowed, launches) : launch_any<__nv_bfloat16, 256>(a, p, m, s, allowed, launches);
 }
 
 }  // namespace kvt

@@ -54,7 +54,7 @@ bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, uint64_t n_slots,
 
 // What kvt_attend does, decided from sizes alone.
 struct AttendPlan {
-  uint32_t kind;             // 0 any head size, 1 few rows (warp-level matrix instructions), 2 many rows (tcgen05),
+  uint32_t kind;             // 0 any other head size, 1 few rows (warp-level matrix instructions), 2 many rows (tcgen05),
                              // 3 few rows of few and moderately long units (clusters)
   uint32_t rows;             // rows of a tile
   uint32_t sms, grid, cluster;
@@ -66,6 +66,6 @@ AttendPlan plan_attend(const AttendArgs &a, uint32_t max_q_len, int sm_count);
 
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, uint32_t *launches);
 // allowed: bits of the kernels whose shared memory has been asked for on this engine's device
-cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint32_t *allowed, uint32_t *launches);
+cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 
 }  // namespace kvt

@@ -157,7 +157,7 @@ struct kvt_engine {
   bool metadata_only;
   int sm_count = 148;
   int device = 0;
-  KvMaps kv_maps{}; bool kv_maps_ok = false; u32 kv_smem_allowed = 0;   // for head sizes of 64 and 128
+  KvMaps kv_maps{}; bool kv_maps_ok = false; u64 kv_smem_allowed = 0;   // for head sizes of 64 and 128
   u8 *tail_pool = nullptr; u32 n_tail = 0;   // blocks outside every tier (kvt_set_tail_pool)
   // host state
   std::vector<Ctx> ctxs;

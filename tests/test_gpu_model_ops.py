@@ -322,6 +322,18 @@ def test_attend_scratch_at_any_16_bytes(B):
     assert offset and torch.equal(want, got)
 
 
+@pytest.mark.parametrize("dtype,layout", [("bf16", 0), ("fp16", 1)])
+@pytest.mark.parametrize("dim", [1, 7, 8, 33, 63, 65, 80, 96, 120, 127, 129, 160, 192, 250, 256])
+def test_attend_every_head_size(B, dim, dtype, layout):
+    """Heads that fill a part of a tile's columns, that 16-byte copies reach or do not; one part of the keys or several."""
+    s = Setup(B, [1, 37, 0, 3], [700, 20, 5, 4000], dtype=dtype, layout=layout, heads=2, group=3, dim=dim, seed=dim)
+    s.put()
+    check_attend(s, window=300 if dim % 2 else 0)
+    s = Setup(B, [300, 1], [40, 0], dtype=dtype, layout=layout, heads=1, group=2, dim=dim, seed=dim)
+    s.put()
+    check_attend(s)
+
+
 def test_attend_scores_that_climb_and_scores_of_one_huge_key(B):
     """The running maximum has to be raised again and again, by little and by much, in either kernel."""
     import torch

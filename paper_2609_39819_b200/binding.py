@@ -1,10 +1,11 @@
-"""Thin ctypes binding of libkvt.so: argument marshalling only. Every stage of the path (hashing,
+"""Thin ctypes binding of libkvt.so: argument marshalling only (that of append_kv and attend natively, in _kvt_torch.so). Every stage of the path (hashing,
 table lookup, classification, victim selection, block movement) runs in the library's CUDA kernels.
 PyTorch is used for device / pinned memory and streams, nothing else. There is no CPU fallback:
 loading fails loudly when the library or a CUDA device is missing."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -169,6 +170,31 @@ def load_library():
     return _lib
 
 
+_native = None
+
+
+def load_native():
+    """The native marshalling of append_kv and attend (built in-tree by build.build_torch_lib). Raises if it is missing."""
+    global _native
+    if _native is None:
+        import importlib.machinery
+        import importlib.util
+        import torch  # noqa: F401  (the module's symbols are torch's)
+        from . import build
+        try:
+            build.build_torch_lib()
+        except Exception as exc:
+            if not os.path.exists(build.TORCH_LIB):
+                raise RuntimeError(f"{build.TORCH_LIB} is missing and could not be built ({exc})") from exc
+            import warnings
+            warnings.warn(f"_kvt_torch.so could not be rebuilt ({exc}); loading the existing binary")
+        loader = importlib.machinery.ExtensionFileLoader("_kvt_torch", build.TORCH_LIB)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kvt_torch", loader))
+        loader.exec_module(module)
+        _native = module
+    return _native
+
+
 def _p(a):
     return a.ctypes.data_as(C.c_void_p) if a is not None else None
 
@@ -321,7 +347,10 @@ class Engine:
         # the address of the device's current stream, without a Stream object around it (2 us of a call of 10)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
-        self._scratch_bytes = {}
+        native = load_native()
+        entry = lambda f: C.cast(f, C.c_void_p).value      # noqa: E731
+        self._append_native = functools.partial(native.append, entry(self.L.kvt_append_kv))
+        self._attend_native = functools.partial(native.attend, entry(self.L.kvt_attend), entry(self.L.kvt_attend_scratch_bytes))
         self.tail_pool = None
         if n_tail_blocks:       # blocks outside every tier: slot ids n_hbm_blocks + i of append_kv and attend
             self.set_tail_pool((torch.zeros if zero_pools else torch.empty)(n_tail_blocks * self.block_bytes, dtype=torch.uint8,
@@ -559,6 +588,15 @@ class Engine:
         16-token block (below n_hbm_blocks: HBM tier; above: tail block). positions: int32 [tokens] or [axes, tokens],
         by default the tokens' indices in their sequences. Asynchronous on the current stream; ids and lengths outside
         their ranges are skipped and reported by kv_check()."""
+        done = self._append_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                                   layer, k, v, block_table, q_start, kv_len,
+                                   *((0, 1, None, None, False) if rope is None else
+                                     (rope.rot_dim, rope.n_axes, rope.freqs, rope.axis_of, rope.interleaved)), positions, q, q_out)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "append_kv")
+            return done
+        # something is not as it should be (what, is said here), or only of another type than it might be
         torch = self.torch
         if layer < 0:
             raise ValueError("append_kv: layer cannot be negative")
@@ -613,6 +651,13 @@ class Engine:
         causal=False: all kv_len keys. scale: 1 / sqrt(head_dim) by default. max_q_len: most new tokens of one sequence,
         if known (chooses the kernel, not the result). out, lse ([tokens, heads] float32, contiguous): written if
         given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream."""
+        done = self._attend_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                                   layer, q, block_table, q_start, kv_len, max_q_len, causal, window, scale, out, lse)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "attend")
+            return done
+        # something is not as it should be (what, is said here), or only of another type than it might be
         torch = self.torch
         if layer < 0 or (max_q_len or 0) < 0 or (window or 0) < 0:
             raise ValueError("attend: layer, max_q_len and window cannot be negative")
@@ -631,14 +676,8 @@ class Engine:
             raise ValueError(f"attend: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
         batch = self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len)
         flags, lsep = 0 if causal else ATTN_FULL, lse.data_ptr() if lse is not None else 0
-        key = (t, batch[0], batch[2], max_q_len, hq, flags, window or 0)      # all that the scratch depends on
-        n = self._scratch_bytes.get(key)
-        if n is None:
-            probe = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs, 0, 0)
-            n = self.L.kvt_attend_scratch_bytes(self.h, probe)
-            if len(self._scratch_bytes) >= 4096:
-                self._scratch_bytes.clear()
-            self._scratch_bytes[key] = n
+        probe = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs, 0, 0)
+        n = self.L.kvt_attend_scratch_bytes(self.h, probe)
         # from the current stream's pool, or the capture's: nobody else has it while this call's kernels run
         scratch = torch.empty(n, dtype=torch.uint8, device=self._dev) if n else None
         a = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs,

@@ -12,13 +12,15 @@ DEPS = ["kvt_kernels.cuh", "kvt_attend.h", os.path.join("..", "..", "include", "
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
               "-Xcompiler", "-fPIC", "--threads", "2"]
 DEFINES: list = []
+TORCH_SOURCE = "kvt_torch.cpp"
+TORCH_LIB = os.path.join(_HERE, "_kvt_torch.so")
 
 
 def _stale(lib: str = LIB) -> bool:
     if not os.path.exists(lib):
         return True
     t = os.path.getmtime(lib)
-    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(_HERE, "..", "include", "kvt.h")]
+    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != TORCH_SOURCE] + [os.path.join(_HERE, "..", "include", "kvt.h")]
     return any(os.path.getmtime(f) > t for f in files)
 
 
@@ -68,9 +70,45 @@ def build_trace_lib(force: bool = False) -> str:
     return build_lib(force, lib=TRACE_LIB, defines=["-DKVT_TRACE"])
 
 
+def build_torch_lib(force: bool = False) -> str:
+    """The native marshalling of append_kv and attend (a CPython module against torch's headers), compiled with g++ if it is
+    missing or older than its source. Safe when several processes call it at once."""
+    src, header = os.path.join(CSRC, TORCH_SOURCE), os.path.join(_HERE, "..", "include", "kvt.h")
+
+    def stale():
+        return not os.path.exists(TORCH_LIB) or os.path.getmtime(TORCH_LIB) < max(os.path.getmtime(src), os.path.getmtime(header))
+
+    if not (force or stale()):
+        return TORCH_LIB
+    import fcntl
+    import sysconfig
+    import torch
+    at = os.path.dirname(torch.__file__)
+    with open(TORCH_LIB + ".lock", "w") as lock:
+        fcntl.flock(lock, fcntl.LOCK_EX)
+        try:
+            if force or stale():
+                tmp = f"{TORCH_LIB}.{os.getpid()}.tmp"
+                cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                       f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(at, "include"),
+                       "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
+                       "-I" + sysconfig.get_paths()["include"], "-I/usr/local/cuda/include", "-o", tmp, src,
+                       "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+                try:
+                    subprocess.check_call(cmd)
+                    os.replace(tmp, TORCH_LIB)
+                finally:
+                    if os.path.exists(tmp):
+                        os.remove(tmp)
+        finally:
+            fcntl.flock(lock, fcntl.LOCK_UN)
+    return TORCH_LIB
+
+
 if __name__ == "__main__":
     import sys
     if "--trace" in sys.argv:
         print(build_trace_lib(force=True))
     else:
         print(build_lib(force=True, verbose="-v" in sys.argv))
+        print(build_torch_lib(force=True))

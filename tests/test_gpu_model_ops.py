@@ -314,12 +314,42 @@ def test_attend_scratch_at_any_16_bytes(B):
             return real(size[0] + 16, **kw)[16:]
         return real(*size, **kw)
 
+    s.eng._attend_native = lambda *args: NotImplemented          # the marshalling in Python allocates with torch.empty
     torch.empty = empty
     try:
         got = s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len)
     finally:
         torch.empty = real
     assert offset and torch.equal(want, got)
+
+
+@pytest.mark.parametrize("axes,inter", [(1, False), (3, True)])
+def test_native_and_python_marshalling_make_the_same_call(B, axes, inter):
+    import torch
+    s = Setup(B, [3, 0, 70], [200, 0, 9], heads=2, group=3, dim=64, seed=4)
+    rope = B.Rope(64, sections=[10, 10, 12] if axes > 1 else None, interleaved=inter)
+    pos = torch.arange(axes * s.rows, dtype=torch.int32, device="cuda").view(axes, s.rows)[:, :s.rows] * 3
+    args = (s.table, s.q_start, s.kv_len)
+    lse = torch.empty(2, s.rows, 6, device="cuda").fill_(1.0)
+    got = []
+    for i in range(2):
+        if i:
+            for name in ("_append_native", "_attend_native"):
+                assert callable(getattr(s.eng, name))
+                setattr(s.eng, name, lambda *a: NotImplemented)
+        for p in s.pools:
+            p.zero_()
+        q = torch.zeros_like(s.q)
+        r = s.eng.append_kv(s.layer, s.k, s.v, *args, rope=rope, positions=pos, q=s.q, q_out=q)
+        assert r is q
+        assert s.eng.append_kv(s.layer, s.k, s.v, *args, rope=rope, positions=pos) is None
+        out = torch.zeros_like(s.q)
+        assert s.eng.attend(s.layer, q, *args, window=50, scale=0.2, max_q_len=70, out=out, lse=lse[i]) is out
+        new = s.eng.attend(s.layer, q, *args, causal=False)
+        s.eng.kv_check()
+        got.append([q, out, new[:s.t].clone(), lse[i]] + s.bits())
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("dtype,layout", [("bf16", 0), ("fp16", 1)])

@@ -69,3 +69,20 @@ def test_packed_arguments_are_the_structs():
         x = cls.from_buffer_copy(packer.pack(*range(1, len(names) + 1)))
         got = [getattr(x.b, f[0]) for f in B.Batch._fields_] + [getattr(x, f[0]) for f in cls._fields_[1:]]
         assert got == list(range(1, len(names) + 1))
+
+
+def test_native_marshalling_leaves_what_it_does_not_take_to_the_callers_checks():
+    """Wrong numbers of arguments, types, devices and shapes: no call is made, nothing is raised, nothing read."""
+    import torch
+    from paper_2609_39819_b200 import binding
+    native = binding.load_native()
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32)      # noqa: E731
+    append = [0, 0, 0, 0, 2, 64, 0, k, k, ints(0).view(1, 1), ints(0, 3), ints(3), 0, 1, None, None, False, None, None, None]
+    attend = [0, 0, 0, 0, 0, 2, 64, 0, k, ints(0).view(1, 1), ints(0, 3), ints(3), None, True, None, None, None, None]
+    for call, args in ((native.append, append), (native.attend, attend)):
+        assert call(*args) is NotImplemented                  # tensors that are not on a CUDA device
+        assert call() is NotImplemented and call(*args[:-1]) is NotImplemented
+        for i in range(len(args)):
+            for wrong in (None, -1, 1 << 70, "x", 1.5, k.float(), k[0], ints(1)):
+                assert call(*args[:i], wrong, *args[i + 1:]) is NotImplemented

@@ -26,6 +26,8 @@ template <> struct Elem<__nv_bfloat16> {
   static __device__ __forceinline__ u32 down(float a, float b) { T2 r = __floats2bfloat162_rn(a, b); return *reinterpret_cast<u32 *>(&r); }
   static __device__ __forceinline__ float up1(__nv_bfloat16 x) { return __bfloat162float(x); }
   static __device__ __forceinline__ __nv_bfloat16 down1(float x) { return __float2bfloat16_rn(x); }
+  // powers (see raise_or_lower)
+  static constexpr float AIM = 0.0f, HIGH = 8.0f, LOW = -INFINITY;
 };
 template <> struct Elem<__half> {
   typedef __half2 T2;
@@ -33,6 +35,7 @@ template <> struct Elem<__half> {
   static __device__ __forceinline__ u32 down(float a, float b) { T2 r = __floats2half2_rn(a, b); return *reinterpret_cast<u32 *>(&r); }
   static __device__ __forceinline__ float up1(__half x) { return __half2float(x); }
   static __device__ __forceinline__ __half down1(float x) { return __float2half_rn(x); }
+  static constexpr float AIM = 8.0f, HIGH = 15.9f, LOW = -4.0f;
 };
 
 // The new tokens [t0, t0 + n) of sequence s and the tokens it holds, cut to what the arrays can hold.
@@ -279,9 +282,9 @@ cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, u32 *launches) {
 // ======================================================================================================
 // Attention. Rows: the (token, query head of the group) pairs of one sequence and one KV head, token-major, so that row r
 // is token r / group, head r % group. A CTA takes a tile of consecutive rows, which all read the same K and V once:
-//   m = max_j s_j, l = sum_j 2^(s_j - m), o = sum_j 2^(s_j - m) v_j, s_j = scale log2(e) q.k_j, result o / l,
-// over one block of keys after the other: where m rises, l and o are multiplied by 2^(old m - new m). Parts of the keys that
-// different warps or CTAs went over are put together by the same rule. Scores, m, l and o are 32-bit numbers.
+//   l = sum_j 2^(s_j - m), o = sum_j 2^(s_j - m) v_j, s_j = scale log2(e) q.k_j, result o / l,
+// with m near max_j s_j, over one block of keys after the other: where m moves, l and o are multiplied by 2^(old m - new m).
+// Parts of the keys that different warps or CTAs went over are put together by the same rule. Scores, m, l and o are 32-bit numbers.
 // ======================================================================================================
 // Keys row `token` (0 = first new token) sees: [lo, hi).
 __device__ __forceinline__ void row_range(const AttendArgs &a, const Seq &q, u32 token, u32 &lo, u32 &hi) {
@@ -370,6 +373,30 @@ __device__ __forceinline__ void load_block(const AttendArgs &a, const KvMaps &m,
 }
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// A row's powers 2^(s - m) and their sums are relative to a number m that follows the largest score `top` of each step at a
+// distance: powers are between 2^LOW and 2^HIGH where a step's largest, and only when a step leaves that range is m moved, to
+// top - AIM, and what has been summed up multiplied by 2^(old m - new m); most steps then need no rescaling. The result does not
+// depend on m but for rounding: sums and m go together, wherever m is.
+//   bf16  has the exponents of a 32-bit number: m rises once a score passes it by 2^8, and never falls.
+//   fp16  ends at 2^16 and has a fixed step of 2^-24 below 2^-14. Powers of at most 1 would lose keys that are 2^25 below the
+//         largest, which a long context can have enough of to make the result (behind a first key that takes nearly all of
+//         the weight and whose value is small, for one). So the largest power aims at 2^8, and where a step's largest is
+//         below 2^-4, m falls: what a step of 128 keys loses to the fixed step is then below 128 * 2^-25 * 2^4 = 2^-14 of the
+//         step's largest power. (With 2^12 as the aim m moves more often: 8192-token prompt 485 us, with 2^8 454, before m
+//         could fall 456.) m does not fall where that would bring the sums above 2^LIMIT (32-bit sums of powers times values then stay
+//         below 2^107): what is that far below has no weight in 32 bits either.
+constexpr float LIMIT = 0x1p90f;
+template <class T> __device__ __forceinline__ bool must_fall(float m, float top) { return Elem<T>::LOW > -INFINITY && top < m + Elem<T>::LOW && top > -INFINITY; }
+template <class T> __device__ __forceinline__ bool must_move(float m, float top) { return top > m + Elem<T>::HIGH || must_fall<T>(m, top); }
+// Moves m; sum: the row's sum of powers so far. Returns what the sums are to be multiplied by.
+template <class T> __device__ __forceinline__ float raise_or_lower(float &m, float top, float sum) {
+  const bool fall = must_fall<T>(m, top);
+  float next = fall ? top - Elem<T>::AIM : fmaxf(m, top - Elem<T>::AIM), f = next == -INFINITY ? 1.0f : ex2(m - next);
+  if (fall && sum * f > LIMIT) { next = m; f = 1.0f; }
+  m = next;
+  return f;
+}
 
 // Which CTA does what is worked out by every CTA for itself from the device-side lengths, so a captured launch follows
 // them. `unit`: one tile of rows of one sequence and KV head, against all its keys. Its number of blocks is bounded per
@@ -896,13 +923,14 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
       top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 1));
       top[y] = fmaxf(top[y], __shfl_xor_sync(~0u, top[y], 2));
     }
-    // The sums stay relative to an old maximum until a score passes it by 2^8: powers of up to 2^8 are as exact as
-    // those below 1, and most blocks then need no rescaling.
-    if (__any_sync(~0u, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+    if (__any_sync(~0u, must_move<T>(m[0], top[0]) || must_move<T>(m[1], top[1]))) {
 #pragma unroll
       for (u32 y = 0; y < 2; ++y) {
-        const float now = fmaxf(m[y], top[y]), f = now == -INFINITY ? 1.0f : ex2(m[y] - now);
-        m[y] = now; l[y] *= f;
+        float all = l[y];                // four lanes hold a row's sum, and must come to the same m
+        all = fmaxf(all, __shfl_xor_sync(~0u, all, 1));
+        all = fmaxf(all, __shfl_xor_sync(~0u, all, 2));
+        const float f = raise_or_lower<T>(m[y], top[y], all);
+        l[y] *= f;
 #pragma unroll
         for (u32 n = 0; n < D / 8; ++n) { o[n][2 * y] *= f; o[n][2 * y + 1] *= f; }
       }
@@ -913,8 +941,8 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
 #pragma unroll
       for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
     // Powers are rounded to the element type for the second product. In fp16 that adds half again to the error of the result's
-    // own rounding, so there they are taken as the sum of two numbers, which is as exact as 32-bit powers; loading K and V
-    // leaves the matrix units the time (1 to 5 % in all). In bf16 the result's own rounding outweighs it.
+    // own rounding, so there they are taken as the sum of two numbers, which leaves 2^-22 of a power or the type's fixed step;
+    // loading K and V leaves the matrix units the time (1 to 5 % in all). In bf16 the result's own rounding outweighs it.
     constexpr bool EXACT = __is_same(T, __half);
     u32 p[4], rest[4];
 #pragma unroll
@@ -1710,10 +1738,9 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
 #pragma unroll
           for (u32 y = 0; y < 4; ++y) top[y] = max3(top[y], v[c + 2 * y], v[c + 2 * y + 1]);
         const float now = fmaxf(max3(max3(top[0], v[124], v[125]), max3(top[1], v[126], v[127]), top[2]), top[3]) * a.scale_log2;
-        // The sums stay relative to an old maximum until a score passes it by 2^8 (as in the kernel for few rows)
-        if (__any_sync(~0u, now > m + 8.0f)) {
-          const float next = fmaxf(m, now), f = next == -INFINITY ? 1.0f : ex2(m - next);
-          m = next; l *= f;
+        if (__any_sync(~0u, must_move<T>(m, now))) {
+          const float f = raise_or_lower<T>(m, now, l);
+          l *= f;
           if (s > 0) {                   // the product before S of these keys has been waited for: O is at rest
 #pragma unroll
             for (u32 c = 0; c < D / 16; ++c) {

@@ -1,0 +1,110 @@
+"""append_kv and attend where they are easily wrong: what lies just outside the rows' keys, the ends of the element types'
+ranges, arguments that are nearly right, reports from several streams. Setup and its 64-bit reference are the other file's."""
+import ctypes as C
+import math
+from types import SimpleNamespace
+
+import pytest
+from test_gpu_model_ops import B, BT, Setup  # noqa: F401  (B is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def every_kernel(s, **kw):
+    """attend by everything the kernel is chosen by (as in check_attend): few rows, prompts, with and without parts."""
+    wide = s.widened()
+    for table, hint in ((s.table, max(s.new)), (wide, None), (s.table, 1), (wide, 1)):
+        lse = s.torch.empty(s.rows, s.heads * s.group, device="cuda")
+        yield (table is wide, hint), s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len, max_q_len=hint, lse=lse, **kw), lse
+    s.eng.kv_check()
+
+
+def cached(s, i, c):
+    """(layer's K or V by slot, slots) of sequence i: blocks as [block, 16, heads, dim] by pool[slots]."""
+    n = -(-s.kv[i] // BT)
+    return s.pools[0][2 * s.layer + c], s.host_table[i, :n].long().cuda()
+
+
+# ---- fp16: small probabilities that a long context adds up ------------------------------------------------------
+def sink_case(s, gap, sinks, value, seed):
+    """Scores in powers of two (scale ln 2): `sinks` hold 0 and a value of 0, all other keys -gap with some spread and values
+    around `value`. Returns out and lse in 64 bits and by how much they may be off."""
+    torch = s.torch
+    g = torch.Generator("cuda").manual_seed(seed)
+    n = s.kv[0]
+    s.q.zero_()
+    s.q[..., 0] = 1.0
+    score = -gap + torch.randint(-32, 33, (n,), generator=g, device="cuda") / 64.0       # exact in fp16 for gaps below 32
+    score[[x for x in sinks if x < n]] = 0.0
+    v = (torch.rand(n, s.heads, s.dim, generator=g, device="cuda") + 0.5) * value
+    v[[x for x in sinks if x < n]] = 0.0
+    for c, x in ((0, torch.zeros_like(v)), (1, v)):
+        if c == 0:
+            x[..., 0] = score[:, None]
+        full = torch.full((-(-n // BT) * BT, s.heads, s.dim), math.nan, device="cuda")
+        full[:n] = x
+        pool, slots = cached(s, 0, c)
+        pool[slots] = full.view(-1, BT, s.heads, s.dim).to(s.dt)
+    k, v = s.gather(0)
+    x = k[:, :, 0].T[:, None, :] * 1.0                                                    # [heads, 1, keys]
+    own = torch.arange(n - s.new[0], n, device="cuda")
+    x = torch.where(torch.arange(n, device="cuda")[None] <= own[:, None], x, -math.inf)  # [heads, rows, keys]
+    p = torch.exp2(x)
+    total = p.sum(-1)
+    out = torch.einsum("hij,jhd->ihd", p, v) / total.T[..., None]
+    # The powers' own rounding (once to fp16, where there are many rows) and the result's: u each. A power is relative to a number
+    # that leaves the largest one of 128 keys at 2^-4 or more, where fp16 has a fixed step of 2^-24: 128 * 2^-25 * 2^4 of
+    # the step's sum, three times that as values differ by 3. Keys beside a sink are relative to the sink's 2^8. Sums of N keys:
+    # the matrix units add 16 products at a time and may cut off what is below 2^-23 of the sum (N / 16 times), denominators
+    # are added up one by one from eight keys of four warps. Scores: a product by ln 2 * log2 e, 32 units at most.
+    rel = 2 * s.u + 3 * 2.0 ** -14 + (n / 16 + 64) * 2.0 ** -23 + n * 2.0 ** -27 + 64 * 2.0 ** -24
+    tol = rel * out + len(sinks) * 128 * 1.5 * value * 2.0 ** -33 + 2.0 ** -25
+    tol_l = torch.full_like(total.T, (n * 2.0 ** -27 + 2.0 ** -16))
+    hq = s.heads * s.group
+    rep = lambda y: y.repeat_interleave(s.group, 1)          # noqa: E731
+    assert out.shape[1] * s.group == hq
+    return rep(out), rep(torch.log(total).T), rep(tol), rep(tol_l)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 72])
+@pytest.mark.parametrize("new,past,gap,value", [(1, 100_000, 22, 1.0), (1, 100_000, 25, 1.0), (60, 100_000, 26, 1.0), (1, 4000, 25, 1.0),
+                                                (60, 4000, 25, 1.0), (1, 130_000, 31, 1024.0), (60, 30_000, 28, 32000.0),
+                                                (1, 60_000, 14, 1.0), (60, 60_000, 18, 1.0)])
+@pytest.mark.parametrize("where", ["first", "last", "both and between"])
+def test_fp16_sums_what_is_far_below_the_largest_score(B, dim, new, past, gap, value, where):  # noqa: F811
+    """A key that takes nearly all of the weight and has nothing to say (an attention sink): the result is what the others add up to."""
+    import torch
+    s = Setup(B, [new], [past], heads=1, group=4, dim=dim, dtype="fp16", layers=1, layer=0, seed=past + gap)
+    n = s.kv[0]
+    sinks = {"first": [0], "last": [past - 1], "both and between": [0, past // 3, past // 3 + 1, past // 2, past - 1]}[where]
+    want, wl, tol, tl = sink_case(s, gap, sinks, value, past + gap)
+    for which, got, lse in every_kernel(s, scale=math.log(2.0)):
+        bad = (got.double() - want).abs() > tol
+        assert not bool(bad.any()), (which, n, float(((got.double() - want).abs() / want).max()))
+        assert not bool(((lse.double() - wl).abs() > tl).any()), (which, float((lse.double() - wl).abs().max()))
+
+
+def test_fp16_scores_that_go_up_and_down_by_much(B):  # noqa: F811
+    """Every block of keys on another level, up to 200 binades apart, rising, falling and in turn."""
+    import torch
+    for dim in (64, 128, 72):
+        for new in (1, 60):
+            for kind in ("down", "up", "turns"):
+                s = Setup(B, [new], [9000], heads=1, group=4, dim=dim, dtype="fp16", layers=1, layer=0, seed=dim + new)
+                s.put()
+                n = s.kv[0]
+                b = torch.arange(n, device="cuda") // BT
+                level = {"down": -200.0 * b / b.max(), "up": 200.0 * b / b.max(), "turns": -((b * 37) % 60).float()}[kind]
+                pool, slots = cached(s, 0, 0)
+                k = torch.zeros(len(slots) * BT, 1, dim, device="cuda")
+                k[:n, 0, 0] = (level * 8).round() / 8
+                pool[slots] = k.view(-1, BT, 1, dim).to(s.dt)
+                s.q.zero_()
+                s.q[..., 0] = 1.0
+                want, wl, tol, tl = s.reference(scale=math.log(2.0))
+                a = []
+                for which, got, lse in every_kernel(s, scale=math.log(2.0)):
+                    bad = (got.double() - want).abs() > tol
+                    assert not bool(bad.any()), (dim, new, kind, which)
+                    assert not bool(((lse.double() - wl).abs() > tl + 220 * 2.0 ** -23).any()), (dim, new, kind, which)   # log2 of a sum of 2^200
+                    a.append(got)

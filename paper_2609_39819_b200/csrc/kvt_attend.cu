@@ -816,7 +816,7 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
                                            u32 ring, u32 bar0, u32 &it, float (&o)[D / 8][4], float (&m)[2], float (&l)[2]) {
   typedef SplitShape<D> S;
   const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  u32 first, last, all_lo, all_hi;       // keys every row sees: [all_lo, all_hi)
+  u32 first, last, all_lo, all_hi;       // keys any row sees: [first, last), keys every row sees: [all_lo, all_hi)
   row_range(a, q, r0 / a.group, first, all_hi);
   row_range(a, q, r1 / a.group, all_lo, last);
   bool ok = true;
@@ -898,12 +898,15 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
       mma16816<T>(s[0], qf[k], f[0], f[1]);
       mma16816<T>(s[1], qf[k], f[2], f[3]);
     }
-    if (key0 + BT > q.kv) {            // the last block's tokens behind the length: whatever their values hold, weight 0
-      const u32 r = lane / 2;          // must not meet an Inf or a NaN
-      if (key0 + r >= q.kv)
+    // Tokens that no row sees, in front of the window in the first block and behind the length in the last: whatever their
+    // values hold, weight 0 must not meet an Inf or a NaN.
+    if (key0 < first || key0 + BT > q.kv) {
+      const u32 r = lane / 2;
+      if (key0 + r < first || key0 + r >= q.kv)
 #pragma unroll
         for (u32 c = 0; c < D / 16; ++c)
           asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+      if (!ANY) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // a load writes here next
       __syncwarp();
     }
     const bool whole = key0 >= all_lo && key0 + BT <= all_hi;
@@ -1375,6 +1378,7 @@ struct Job {
   u32 r0, r1;                // rows of the tile, counted in the sequence: first and last
   u32 shift;                 // index in the sequence of its first new token, as a signed number
   u32 b0, b1, all_lo, all_hi;// blocks of keys [b0, b1); keys every row sees
+  u32 first;                 // first key any row sees
   u32 part, direct, last;    // place of the partial result, or the whole result at once; last: no job, the end
 };
 constexpr u32 TC_JOBS = 4, TC_PARTS = 2;      // P is handed to the second product in so many parts
@@ -1515,10 +1519,10 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         const u32 x = want - at, y = x / H, h = x - y * H, pc = y / tiles, tile = tiles - 1 - (y - pc * tiles);
         j.t0 = q.t0; j.kv = q.kv; j.seq = my_seq; j.h = h; j.shift = q.kv - q.n;
         j.r0 = tile * TC_ROWS; j.r1 = min(j.r0 + TC_ROWS, q.n * a.group) - 1;
-        u32 first, last;                 // keys any row sees
-        row_range(a, q, j.r0 / a.group, first, j.all_hi);
+        u32 last;
+        row_range(a, q, j.r0 / a.group, j.first, j.all_hi);
         row_range(a, q, j.r1 / a.group, j.all_lo, last);
-        const u32 b_first = first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
+        const u32 b_first = j.first / BT, b_last = (last + BT - 1) / BT, nb = b_last > b_first ? b_last - b_first : 0;
         const u32 per = ((nb + pieces - 1) / pieces + TC_KB - 1) / TC_KB * TC_KB;       // whole stages
         j.b0 = b_first + min(pc * per, nb); j.b1 = b_first + min((pc + 1) * per, nb);
         j.direct = pieces == 1;
@@ -1589,7 +1593,8 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         const u32 at = jobs % TC_JOBS;
         if (!(ok = tc_wait1(jfull + at * 8, (jobs / TC_JOBS) & 1, lost))) break;
         ++jobs;
-        const u32 r0 = s_job[at].r0, r1 = s_job[at].r1, b0 = s_job[at].b0, b1 = s_job[at].b1, kv = s_job[at].kv, end = s_job[at].last;
+        const u32 r0 = s_job[at].r0, r1 = s_job[at].r1, b0 = s_job[at].b0, b1 = s_job[at].b1, kv = s_job[at].kv, first = s_job[at].first,
+                  end = s_job[at].last;
         bar_arrive(jempty + at * 8);
         if (end) break;
         const u32 n = (b1 - b0 + TC_KB - 1) / TC_KB;
@@ -1613,13 +1618,16 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
           const bool more = s + 1 < n;
           const Place v1 = after(k), k1 = after(v1);
           if (!has_v && !(ok = landed(v))) break;
-          if (!more && b1 * BT > kv) {           // tokens behind the length in the last block: whatever their values hold,
-            for (u32 r = kv % BT; r < BT; ++r)   // weight 0 must not meet an Inf or a NaN
+          // Tokens that no row sees, in front of the window in the first block and behind the length in the last: whatever
+          // their values hold, weight 0 must not meet an Inf or a NaN.
+          auto clear = [&](u32 block, u32 r0, u32 r1) {
+            for (u32 r = r0; r < r1; ++r)
               for (u32 c = 0; c < D / 8; ++c)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
-                             ::"r"(ring + v.st * S::STAGE + ((b1 - 1 - b0) % TC_KB) * S::BLOCK + block_off<D>(r, c)), "r"(0) : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + v.st * S::STAGE + block * S::BLOCK + block_off<D>(r, c)), "r"(0) : "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          }
+          };
+          if (s == 0 && b0 * BT < first) clear(0, 0, first - b0 * BT);      // fewer than a block's
+          if (!more && b1 * BT > kv) clear((b1 - 1 - b0) % TC_KB, kv % BT, BT);
           const u64 dv = dv0 + v.st * (S::STAGE / 16);
 #pragma unroll
           for (u32 i = 0; i < 2; ++i)

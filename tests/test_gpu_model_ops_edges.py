@@ -108,3 +108,27 @@ def test_fp16_scores_that_go_up_and_down_by_much(B):  # noqa: F811
                     assert not bool(bad.any()), (dim, new, kind, which)
                     assert not bool(((lse.double() - wl).abs() > tl + 220 * 2.0 ** -23).any()), (dim, new, kind, which)   # log2 of a sum of 2^200
                     a.append(got)
+
+
+# ---- keys that nobody sees ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 72, 20])
+@pytest.mark.parametrize("new,past,window", [(1, 300, 100), (1, 1500, 1003), (40, 300, 9), (200, 700, 333), (200, 2500, 1000), (1, 30, 2)])
+def test_values_in_front_of_a_window_have_no_effect(B, new, past, window, dim, dtype):  # noqa: F811
+    """The block of the first key that is seen begins with tokens that no row sees: NaN or Inf there must not get anywhere."""
+    import torch
+    s = Setup(B, [new, 3], [past, past // 2], heads=2, group=2, dim=dim, dtype=dtype, seed=past + window)
+    s.put()
+    want = [(got.clone(), lse.clone()) for _, got, lse in every_kernel(s, window=window)]
+    spoiled = 0
+    for bad in (math.nan, math.inf, -math.inf):
+        for i, (n, kv) in enumerate(zip(s.new, s.kv)):
+            first = max(0, kv - n + 1 - window)
+            at = first // BT * BT
+            for t in range(at, first):
+                for c in (0, 1):
+                    s._chunk(int(s.host_table[i, t // BT]), c)[t % BT] = bad
+                spoiled += 1
+        for (which, got, lse), (w, wl) in zip(every_kernel(s, window=window), want):
+            assert torch.equal(got, w) and torch.equal(lse, wl), (which, bad)
+    assert spoiled

@@ -475,9 +475,10 @@ uint64_t kvt_attend_scratch_bytes(kvt_engine *e, const kvt_attend_args *a);
  * Calls enqueued or captured earlier keep the buffer they were given. */
 int32_t kvt_set_tail_pool(kvt_engine *e, void *pool, uint64_t bytes);
 
-/* Synchronises, then reports and clears what the calls above found on the device: KVT_E_RANGE (a slot id outside the
+/* Synchronises `stream`, and reports and clears what the calls above found on the device: KVT_E_RANGE (a slot id outside the
  * pools, or lengths, starts or axes that had to be cut), KVT_E_DEVICE (a wait inside a kernel ran out; the outputs of
- * that call are not to be used), KVT_OK. */
+ * that call are not to be used), KVT_OK. Covers the calls that are ordered before it on `stream`. What a call that still
+ * runs on another stream finds is reported now or next time, never lost: the word is read and cleared in one step. */
 int32_t kvt_kv_check(kvt_engine *e, void *stream);
 
 /* ---- introspection ------------------------------------------------------------------------------ */

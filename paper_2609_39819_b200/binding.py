@@ -686,7 +686,8 @@ class Engine:
         return out
 
     def kv_check(self):
-        """Waits for the current stream and raises if append_kv or attend met an id or a length outside its range."""
+        """Waits for the current stream and raises if append_kv or attend met an id or a length outside its range. What a call
+        that still runs on another stream meets is raised by this check or the next."""
         self._check(self.L.kvt_kv_check(self.h, self._kv_stream()), "kv_check")
 
     # ---- introspection --------------------------------------------------------------------------

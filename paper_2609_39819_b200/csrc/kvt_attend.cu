@@ -19,6 +19,12 @@ constexpr u32 BT = 16;   // tokens of a block
 
 __device__ __forceinline__ void kv_err(u32 *err, u32 bits) { atomicOr(err, bits); }
 
+__global__ void k_take_error(u32 *err, u32 *out) { *out = atomicExch(err, 0u); }
+cudaError_t launch_take_error(u32 *err, u32 *out, cudaStream_t s) {
+  k_take_error<<<1, 1, 0, s>>>(err, out);
+  return cudaGetLastError();
+}
+
 template <class T> struct Elem;
 template <> struct Elem<__nv_bfloat16> {
   typedef __nv_bfloat162 T2;

@@ -64,6 +64,8 @@ struct AttendPlan {
 };
 AttendPlan plan_attend(const AttendArgs &a, uint32_t max_q_len, int sm_count);
 
+// out = *err, *err = 0, in one step: a bit that a kernel on another stream sets meanwhile is in `out` or stays for the next time.
+cudaError_t launch_take_error(uint32_t *err, uint32_t *out, cudaStream_t s);
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, uint32_t *launches);
 // allowed: bits of the kernels whose shared memory has been asked for on this engine's device
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint64_t *allowed, uint32_t *launches);

@@ -138,7 +138,7 @@ DevLayout make_layout(const kvt_config &c) {
   L.sel_state = take((SEL_MAX_LEVELS + 1) * sizeof(SelState));
   L.out_slots = take(Nt * 4); L.out_states = take(Nt);
   L.map_tier = take(B); L.map_slot = take(B * 4);
-  L.kv_err = take(4);   // sticky error word of the model-side operators
+  L.kv_err = take(8);   // sticky error word of the model-side operators; the one last taken
   L.total = off;
   return L;
 }
@@ -1092,7 +1092,7 @@ int32_t kvt_create(const kvt_config *cfg, void *stream, kvt_engine **out) {
   // everything except the key arena and scratch must start at zero; the table needs ent = NONE
   ok = ok && cudaMemsetAsync(e->meta + L.e_key, 0, L.keys - L.e_key, s) == cudaSuccess;
   ok = ok && cudaMemsetAsync(e->d_status, 0, ST_WORDS * 4, s) == cudaSuccess;
-  ok = ok && cudaMemsetAsync(e->dp<u32>(L.kv_err), 0, 4, s) == cudaSuccess;
+  ok = ok && cudaMemsetAsync(e->dp<u32>(L.kv_err), 0, 8, s) == cudaSuccess;
   ok = ok && cudaMemsetAsync(e->ent.link, 0xFF, N * 4, s) == cudaSuccess;   // no links
   if (ok) {
     KL(k_table_clear, cdiv((u64)c.table_capacity, TPB), TPB, s, e->tab);
@@ -2407,9 +2407,10 @@ int32_t kvt_kv_check(kvt_engine *e, void *stream) {
   cudaStream_t s = (cudaStream_t)stream;
   OnDevice on(e->device);
   if (!on.ok) return fail(e, KVT_E_CUDA, "kv_check: device");
-  u32 bits = 0;
-  CU(cudaMemcpyAsync(&bits, e->dp<u32>(e->L.kv_err), 4, cudaMemcpyDeviceToHost, s));
-  CU(cudaMemsetAsync(e->dp<u32>(e->L.kv_err), 0, 4, s));
+  u32 bits = 0, *const err = e->dp<u32>(e->L.kv_err);
+  CU(launch_take_error(err, err + 1, s));
+  ++e->st.kernel_launches;
+  CU(cudaMemcpyAsync(&bits, err + 1, 4, cudaMemcpyDeviceToHost, s));
   CU(cudaStreamSynchronize(s));
   if (bits & KVERR_WAIT) return fail(e, KVT_E_DEVICE, "a wait inside a model-side kernel ran out");
   if (bits) return fail(e, KVT_E_RANGE, "slot id, length, start or axis outside its range");

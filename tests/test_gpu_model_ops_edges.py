@@ -132,3 +132,34 @@ def test_values_in_front_of_a_window_have_no_effect(B, new, past, window, dim, d
         for (which, got, lse), (w, wl) in zip(every_kernel(s, window=window), want):
             assert torch.equal(got, w) and torch.equal(lse, wl), (which, bad)
     assert spoiled
+
+
+# ---- reports ---------------------------------------------------------------------------------------------------------
+def test_no_report_is_lost_between_two_streams(B):  # noqa: F811
+    """Bad slots met on one stream while kv_check runs on another, over and over: each is reported once."""
+    import time
+    import torch
+    s = Setup(B, [1], [40], heads=1, group=1, dim=64, seed=3)
+    bad = torch.full_like(s.table, 0x7FFFFFF0)
+    other = torch.cuda.Stream()
+    s.eng.append_kv(s.layer, s.k, s.v, s.table, s.q_start, s.kv_len)
+    s.eng.kv_check()
+    torch.cuda.synchronize()
+    lost = 0
+    for i in range(400):
+        with torch.cuda.stream(other):
+            torch.cuda._sleep(20000 + 997 * (i % 50))
+            s.eng.append_kv(s.layer, s.k, s.v, bad, s.q_start, s.kv_len)
+            done = torch.cuda.Event()
+            done.record()
+        reports, late = 0, 0
+        while late < 3:                     # three checks begun after the bad call was through
+            late += done.query()
+            try:
+                s.eng.kv_check()
+            except B.KvtError as exc:
+                assert exc.code == B.E_RANGE
+                reports += 1
+        assert reports <= 1
+        lost += reports == 0
+    assert lost == 0

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libkvt.so: argument marshalling only (that of append_kv and attend natively, in _kvt_torch.so). Every stage of the path (hashing,
+"""Thin ctypes binding of libkvt.so: argument marshalling only (that of append_kv and attend natively where _kvt_torch*.so can be had). Every stage of the path (hashing,
 table lookup, classification, victim selection, block movement) runs in the library's CUDA kernels.
 PyTorch is used for device / pinned memory and streams, nothing else. There is no CPU fallback:
 loading fails loudly when the library or a CUDA device is missing."""
@@ -171,28 +171,43 @@ def load_library():
 
 
 _native = None
+_native_missing = None      # why there is none, once that is known
 
 
 def load_native():
-    """The native marshalling of append_kv and attend (built in-tree by build.build_torch_lib). Raises if it is missing."""
-    global _native
+    """The native marshalling of append_kv and attend (built in-tree by build.build_torch_lib). Raises if it cannot be had."""
+    global _native, _native_missing
     if _native is None:
+        if _native_missing is not None:
+            raise RuntimeError(_native_missing)
         import importlib.machinery
         import importlib.util
         import torch  # noqa: F401  (the module's symbols are torch's)
         from . import build
         try:
-            build.build_torch_lib()
+            # a binary older than its sources is not an answer: it may have other ideas of the library's structs
+            loader = importlib.machinery.ExtensionFileLoader("_kvt_torch", build.build_torch_lib())
+            module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kvt_torch", loader))
+            loader.exec_module(module)
         except Exception as exc:
-            if not os.path.exists(build.TORCH_LIB):
-                raise RuntimeError(f"{build.TORCH_LIB} is missing and could not be built ({exc})") from exc
-            import warnings
-            warnings.warn(f"_kvt_torch.so could not be rebuilt ({exc}); loading the existing binary")
-        loader = importlib.machinery.ExtensionFileLoader("_kvt_torch", build.TORCH_LIB)
-        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_kvt_torch", loader))
-        loader.exec_module(module)
+            _native_missing = f"{build.TORCH_LIB} could not be built or loaded ({exc})"
+            raise RuntimeError(_native_missing) from exc
         _native = module
     return _native
+
+
+def _native_calls(lib):
+    """append_kv and attend with native marshalling for `lib`; without it functions that leave every call to the marshalling in
+    Python, which takes 4 us longer and does the same."""
+    try:
+        native = load_native()
+    except RuntimeError as exc:
+        import warnings
+        warnings.warn(f"append_kv and attend marshal their arguments in Python: {exc}")
+        return (lambda *args: NotImplemented,) * 2
+    entry = lambda f: C.cast(f, C.c_void_p).value      # noqa: E731
+    return (functools.partial(native.append, entry(lib.kvt_append_kv)),
+            functools.partial(native.attend, entry(lib.kvt_attend), entry(lib.kvt_attend_scratch_bytes)))
 
 
 def _p(a):
@@ -347,10 +362,7 @@ class Engine:
         # the address of the device's current stream, without a Stream object around it (2 us of a call of 10)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
-        native = load_native()
-        entry = lambda f: C.cast(f, C.c_void_p).value      # noqa: E731
-        self._append_native = functools.partial(native.append, entry(self.L.kvt_append_kv))
-        self._attend_native = functools.partial(native.attend, entry(self.L.kvt_attend), entry(self.L.kvt_attend_scratch_bytes))
+        self._append_native, self._attend_native = _native_calls(self.L)
         self.tail_pool = None
         if n_tail_blocks:       # blocks outside every tier: slot ids n_hbm_blocks + i of append_kv and attend
             self.set_tail_pool((torch.zeros if zero_pools else torch.empty)(n_tail_blocks * self.block_bytes, dtype=torch.uint8,

@@ -1,8 +1,10 @@
 """Builds libkvt.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import importlib.metadata
 import os
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -13,7 +15,19 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "--threads", "2"]
 DEFINES: list = []
 TORCH_SOURCE = "kvt_torch.cpp"
-TORCH_LIB = os.path.join(_HERE, "_kvt_torch.so")
+
+
+def _torch_lib() -> str:
+    """The file of the native marshalling. It is built against one torch and one Python, and named after them: another of either
+    does not find it."""
+    try:
+        torch_version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        torch_version = "none"
+    return os.path.join(_HERE, f"_kvt_torch.{torch_version}.{sysconfig.get_config_var('SOABI')}.so")
+
+
+TORCH_LIB = _torch_lib()
 
 
 def _stale(lib: str = LIB) -> bool:
@@ -70,6 +84,10 @@ def build_trace_lib(force: bool = False) -> str:
     return build_lib(force, lib=TRACE_LIB, defines=["-DKVT_TRACE"])
 
 
+def _cuda_home() -> str:
+    return os.environ.get("CUDA_HOME") or os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+
+
 def build_torch_lib(force: bool = False) -> str:
     """The native marshalling of append_kv and attend (a CPython module against torch's headers), compiled with g++ if it is
     missing or older than its source. Safe when several processes call it at once."""
@@ -81,7 +99,6 @@ def build_torch_lib(force: bool = False) -> str:
     if not (force or stale()):
         return TORCH_LIB
     import fcntl
-    import sysconfig
     import torch
     at = os.path.dirname(torch.__file__)
     with open(TORCH_LIB + ".lock", "w") as lock:
@@ -92,7 +109,7 @@ def build_torch_lib(force: bool = False) -> str:
                 cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
                        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(at, "include"),
                        "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
-                       "-I" + sysconfig.get_paths()["include"], "-I/usr/local/cuda/include", "-o", tmp, src,
+                       "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(_cuda_home(), "include"), "-o", tmp, src,
                        "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
                 try:
                     subprocess.check_call(cmd)

@@ -163,3 +163,27 @@ def test_no_report_is_lost_between_two_streams(B):  # noqa: F811
         assert reports <= 1
         lost += reports == 0
     assert lost == 0
+
+
+# ---- marshalling -----------------------------------------------------------------------------------------------------
+def test_an_engine_without_the_native_marshalling(B, monkeypatch):  # noqa: F811
+    """The native module saves host time and nothing else: without it engines are made and give the same results."""
+    import torch
+
+    def missing():
+        raise RuntimeError("no module")
+
+    with_it = Setup(B, [5, 40], [30, 200], heads=2, group=2, dim=64, seed=8)
+    monkeypatch.setattr(B, "load_native", missing)
+    with pytest.warns(UserWarning, match="no module"):
+        meta = B.Engine(n_layers=2, n_kv_heads=2, head_dim=64, n_hbm_blocks=8, n_host_blocks=0, metadata_only=True, max_tokens=256)
+    meta.spawn(0)
+    with pytest.warns(UserWarning, match="no module"):
+        without = Setup(B, [5, 40], [30, 200], heads=2, group=2, dim=64, seed=8)
+    got = []
+    for s in (with_it, without):
+        q = s.eng.append_kv(s.layer, s.k, s.v, s.table, s.q_start, s.kv_len, rope=B.Rope(64), q=s.q)
+        got.append((q, s.eng.attend(s.layer, q, s.table, s.q_start, s.kv_len), *s.bits()))
+        s.eng.kv_check()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

@@ -86,3 +86,38 @@ def test_native_marshalling_leaves_what_it_does_not_take_to_the_callers_checks()
         for i in range(len(args)):
             for wrong in (None, -1, 1 << 70, "x", 1.5, k.float(), k[0], ints(1)):
                 assert call(*args[:i], wrong, *args[i + 1:]) is NotImplemented
+
+
+@pytest.fixture
+def no_native_yet(monkeypatch):
+    from paper_2609_39819_b200 import binding
+    monkeypatch.setattr(binding, "_native", None)
+    monkeypatch.setattr(binding, "_native_missing", None, raising=False)
+    return binding
+
+
+def test_without_the_native_marshalling_every_call_is_left_to_python(no_native_yet, monkeypatch):
+    from paper_2609_39819_b200 import build
+    tried = []
+
+    def cannot(force=False):
+        tried.append(1)
+        raise OSError("no compiler")
+
+    monkeypatch.setattr(build, "build_torch_lib", cannot)
+    for _ in range(2):
+        with pytest.warns(UserWarning, match="no compiler"):
+            calls = no_native_yet._native_calls(no_native_yet.load_library())
+        assert [f(1, 2, 3) for f in calls] == [NotImplemented, NotImplemented]
+    assert len(tried) == 1          # an engine more does not try again for a minute
+    with pytest.raises(RuntimeError, match="no compiler"):
+        no_native_yet.load_native()
+
+
+def test_the_native_marshalling_belongs_to_one_torch(no_native_yet, monkeypatch):
+    import importlib.metadata
+    import torch
+    from paper_2609_39819_b200 import build
+    assert torch.__version__ in build.TORCH_LIB
+    monkeypatch.setattr(importlib.metadata, "version", lambda name: "1.2.3")
+    assert "1.2.3" in build._torch_lib() and not os.path.exists(build._torch_lib())

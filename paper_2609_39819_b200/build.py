@@ -5,15 +5,17 @@ import importlib.metadata
 import os
 import subprocess
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libkvt.so")
-SOURCES = ["kvt_engine.cu", "kvt_attend.cu"]
-DEPS = ["kvt_kernels.cuh", "kvt_attend.h", os.path.join("..", "..", "include", "kvt.h")]
-NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-              "-Xcompiler", "-fPIC", "--threads", "2"]
+NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 DEFINES: list = []
+HEADER = os.path.join(_HERE, "..", "include", "kvt.h")
+# The kernels of append_kv and attend, most of the compiler's time, have no checked or traced parts: one object for all libraries.
+ATTEND_OBJ = os.path.join(_HERE, "kvt_attend.o")
+ATTEND_DEPS = [os.path.join(CSRC, f) for f in ("kvt_attend.cu", "kvt_attend.h")]
 TORCH_SOURCE = "kvt_torch.cpp"
 
 
@@ -30,12 +32,35 @@ def _torch_lib() -> str:
 TORCH_LIB = _torch_lib()
 
 
+def _older(target: str, files) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(f) > os.path.getmtime(target) for f in files)
+
+
 def _stale(lib: str = LIB) -> bool:
-    if not os.path.exists(lib):
-        return True
-    t = os.path.getmtime(lib)
-    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != TORCH_SOURCE] + [os.path.join(_HERE, "..", "include", "kvt.h")]
-    return any(os.path.getmtime(f) > t for f in files)
+    return _older(lib, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != TORCH_SOURCE] + [HEADER])
+
+
+def _make(target: str, stale, command, force: bool = False) -> str:
+    """Runs command(temporary file) where `target` is stale. Safe when several processes or threads call it at once (one rank per
+    GPU): an exclusive file lock serialises them, the compiler writes to a temporary file and the result is moved into place
+    in one step, so nobody ever loads a half-written file."""
+    if not (force or stale()):
+        return target
+    import fcntl
+    with open(target + ".lock", "w") as lock:
+        fcntl.flock(lock, fcntl.LOCK_EX)
+        try:
+            if force or stale():             # somebody else may have built it while we waited
+                tmp = f"{target}.{os.getpid()}.tmp"
+                try:
+                    command(tmp)
+                    os.replace(tmp, target)
+                finally:
+                    if os.path.exists(tmp):
+                        os.remove(tmp)
+        finally:
+            fcntl.flock(lock, fcntl.LOCK_UN)
+    return target
 
 
 DEBUG_LIB = os.path.join(_HERE, "libkvt_debug.so")
@@ -49,29 +74,25 @@ def build_debug_lib(force: bool = False) -> str:
 
 
 def build_lib(force: bool = False, verbose: bool = False, lib: str = LIB, defines=None) -> str:
-    """Compiles libkvt.so if it is missing or older than its sources. Safe when several processes call it at once
-    (one rank per GPU): an exclusive file lock serialises them, the compiler writes to a temporary file and the
-    result is moved into place in one step, so nobody ever loads a half-written library."""
-    if not (force or _stale(lib)):
-        return lib
-    import fcntl
-    with open(lib + ".lock", "w") as lock:
-        fcntl.flock(lock, fcntl.LOCK_EX)
-        try:
-            if force or _stale(lib):         # somebody else may have built it while we waited
-                nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-                tmp = f"{lib}.{os.getpid()}.tmp"
-                cmd = [nvcc] + NVCC_FLAGS + DEFINES + list(defines or []) + (["-Xptxas", "-v"] if verbose else []) + \
-                      ["-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
-                try:
-                    subprocess.check_call(cmd)
-                    os.replace(tmp, lib)
-                finally:
-                    if os.path.exists(tmp):
-                        os.remove(tmp)
-        finally:
-            fcntl.flock(lock, fcntl.LOCK_UN)
-    return lib
+    """Compiles libkvt.so if it is missing or older than its sources (several processes may ask at once)."""
+    nvcc = [os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")] + NVCC_FLAGS + DEFINES + (["-Xptxas", "-v"] if verbose else [])
+
+    def attend():
+        return _make(ATTEND_OBJ, lambda: _older(ATTEND_OBJ, ATTEND_DEPS),
+                     lambda tmp: subprocess.check_call(nvcc + ["-c", "-o", tmp, ATTEND_DEPS[0]]), force and lib == LIB)
+
+    def link(tmp):
+        engine = tmp + ".engine.o"
+        with ThreadPoolExecutor(1) as other:         # both sources at once
+            obj = other.submit(attend)
+            try:
+                subprocess.check_call(nvcc + list(defines or []) + ["-c", "-o", engine, os.path.join(CSRC, "kvt_engine.cu")])
+                subprocess.check_call(nvcc + ["-shared", "-o", tmp, engine, obj.result()])
+            finally:
+                if os.path.exists(engine):
+                    os.remove(engine)
+
+    return _make(lib, lambda: _stale(lib), link, force)
 
 
 TRACE_LIB = os.path.join(_HERE, "libkvt_trace.so")
@@ -90,36 +111,26 @@ def _cuda_home() -> str:
 
 def build_torch_lib(force: bool = False) -> str:
     """The native marshalling of append_kv and attend (a CPython module against torch's headers), compiled with g++ if it is
-    missing or older than its source. Safe when several processes call it at once."""
-    src, header = os.path.join(CSRC, TORCH_SOURCE), os.path.join(_HERE, "..", "include", "kvt.h")
+    missing or older than its source (several processes may ask at once)."""
+    src = os.path.join(CSRC, TORCH_SOURCE)
 
-    def stale():
-        return not os.path.exists(TORCH_LIB) or os.path.getmtime(TORCH_LIB) < max(os.path.getmtime(src), os.path.getmtime(header))
+    def compile_(tmp):
+        import torch
+        at = os.path.dirname(torch.__file__)
+        subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(at, "include"),
+                               "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
+                               "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(_cuda_home(), "include"), "-o", tmp, src,
+                               "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
-    if not (force or stale()):
-        return TORCH_LIB
-    import fcntl
-    import torch
-    at = os.path.dirname(torch.__file__)
-    with open(TORCH_LIB + ".lock", "w") as lock:
-        fcntl.flock(lock, fcntl.LOCK_EX)
-        try:
-            if force or stale():
-                tmp = f"{TORCH_LIB}.{os.getpid()}.tmp"
-                cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
-                       f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(at, "include"),
-                       "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
-                       "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(_cuda_home(), "include"), "-o", tmp, src,
-                       "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-                try:
-                    subprocess.check_call(cmd)
-                    os.replace(tmp, TORCH_LIB)
-                finally:
-                    if os.path.exists(tmp):
-                        os.remove(tmp)
-        finally:
-            fcntl.flock(lock, fcntl.LOCK_UN)
-    return TORCH_LIB
+    return _make(TORCH_LIB, lambda: _older(TORCH_LIB, [src, HEADER]), compile_, force)
+
+
+def build_all() -> None:
+    """Every library of the package, compiled side by side."""
+    with ThreadPoolExecutor(4) as pool:
+        for done in [pool.submit(f) for f in (build_lib, build_torch_lib, build_debug_lib, build_trace_lib)]:
+            done.result()
 
 
 if __name__ == "__main__":

@@ -121,3 +121,23 @@ def test_the_native_marshalling_belongs_to_one_torch(no_native_yet, monkeypatch)
     assert torch.__version__ in build.TORCH_LIB
     monkeypatch.setattr(importlib.metadata, "version", lambda name: "1.2.3")
     assert "1.2.3" in build._torch_lib() and not os.path.exists(build._torch_lib())
+
+
+def test_the_attention_kernels_are_compiled_once_for_all_libraries(monkeypatch, tmp_path):
+    from paper_2609_39819_b200 import build
+    commands = []
+
+    def compiler(cmd):
+        commands.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+
+    monkeypatch.setattr(build.subprocess, "check_call", compiler)
+    monkeypatch.setattr(build, "ATTEND_OBJ", str(tmp_path / "attend.o"))
+    for name, defines in (("a.so", None), ("b.so", ["-DKVT_DEBUG"]), ("c.so", ["-DKVT_TRACE"])):
+        assert build.build_lib(lib=str(tmp_path / name), defines=defines) == str(tmp_path / name)
+    of = lambda src: [c for c in commands if any(x.endswith(src) for x in c)]       # noqa: E731
+    assert len(of("kvt_attend.cu")) == 1 and not any(x.startswith("-D") for x in of("kvt_attend.cu")[0])
+    assert len(of("kvt_engine.cu")) == 3 and ["-DKVT_DEBUG" in c for c in of("kvt_engine.cu")] == [False, True, False]
+    links = [c for c in commands if "-shared" in c]
+    assert len(links) == 3 and all(str(tmp_path / "attend.o") in c for c in links)
+    assert sorted(p.name for p in tmp_path.iterdir() if not p.name.endswith(".lock")) == ["a.so", "attend.o", "b.so", "c.so"]

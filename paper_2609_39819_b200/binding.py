@@ -87,6 +87,7 @@ class AttendArgs(C.Structure):
 _BATCH = "IIIIQPPP"
 _APPEND = struct.Struct("@" + _BATCH + "IIIIIIPPPPQQQQQQQQPPPQ")
 _ATTEND = struct.Struct("@" + _BATCH + "IIIIIfPPPQQQQPQ")
+_FLT_MIN = 2.0 ** -126      # smallest scale that is told from 0
 
 CALL_INFO_DTYPE = np.dtype([(n, np.uint32) for n in ("n_blocks", "hit_len", "n_hit_hbm", "n_hit_host",
                                                        "n_admissible", "n_admitted", "n_held", "n_pinned",
@@ -660,7 +661,7 @@ class Engine:
         """softmax(scale q k^T) v of the new tokens' queries over everything their sequences hold in `layer` (append
         first: the new tokens are among the kv_len[s]). q: [tokens, heads, head_dim], heads a multiple of n_kv_heads;
         batch as in append_kv. causal: a query sees the keys up to its own, with `window` the last `window` of them;
-        causal=False: all kv_len keys. scale: 1 / sqrt(head_dim) by default. max_q_len: most new tokens of one sequence,
+        causal=False: all kv_len keys. scale: 1 / sqrt(head_dim) if None. max_q_len: most new tokens of one sequence,
         if known (chooses the kernel, not the result). out, lse ([tokens, heads] float32, contiguous): written if
         given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream."""
         done = self._attend_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
@@ -688,11 +689,13 @@ class Engine:
             raise ValueError(f"attend: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
         batch = self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len)
         flags, lsep = 0 if causal else ATTN_FULL, lse.data_ptr() if lse is not None else 0
-        probe = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs, 0, 0)
+        # 0, which is the library's word for the default, becomes next to 0
+        factor = 0.0 if scale is None else max(float(scale), _FLT_MIN) if scale >= 0 else float(scale)
+        probe = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, factor, qp, op, lsep, qts, qhs, ots, ohs, 0, 0)
         n = self.L.kvt_attend_scratch_bytes(self.h, probe)
         # from the current stream's pool, or the capture's: nobody else has it while this call's kernels run
         scratch = torch.empty(n, dtype=torch.uint8, device=self._dev) if n else None
-        a = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, scale or 0.0, qp, op, lsep, qts, qhs, ots, ohs,
+        a = _ATTEND.pack(*batch, layer, dt, hq, flags, window or 0, factor, qp, op, lsep, qts, qhs, ots, ohs,
                          scratch.data_ptr() if n else 0, n)
         self._check(self.L.kvt_attend(self.h, a, self._kv_stream()), "attend")
         return out

@@ -10,6 +10,8 @@
 #include <ATen/ops/empty_like.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cfloat>
+
 #include "../../include/kvt.h"
 
 namespace {
@@ -180,7 +182,8 @@ PyObject *attend(PyObject *, PyObject *const *x, Py_ssize_t n) {
     a.window = x[14] == Py_None ? 0u : small(x[14]);
     if (x[15] != Py_None) {
       want(PyFloat_CheckExact(x[15]));
-      a.scale = (float)PyFloat_AS_DOUBLE(x[15]);
+      const double scale = PyFloat_AS_DOUBLE(x[15]);       // 0, which is the library's word for the default, becomes next to 0
+      a.scale = scale >= 0.0 && scale < FLT_MIN ? FLT_MIN : (float)scale;
     }
     const at::Tensor out = result(x[16], q);
     const Place op = c.rows(out, t, tokens, hq);

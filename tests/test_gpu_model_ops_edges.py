@@ -187,3 +187,16 @@ def test_an_engine_without_the_native_marshalling(B, monkeypatch):  # noqa: F811
         s.eng.kv_check()
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_scale_of_nothing(B):  # noqa: F811
+    """scale=0.0 is a scale, not the default: all keys weigh the same. So does one that is 0 in 32 bits."""
+    import torch
+    for dim in (64, 72):
+        s = Setup(B, [1, 30], [50, 300], heads=2, group=2, dim=dim, seed=5)
+        s.put()
+        for scale in (0.0, 0, -0.0, 1e-60):
+            want, wl, tol, tl = s.reference(scale=0.0)
+            for _, got, lse in every_kernel(s, scale=scale):
+                assert not bool(((got.double() - want).abs() > tol).any())
+                assert not bool(((lse.double() - wl).abs() > tl).any())

@@ -571,6 +571,8 @@ class Engine:
         if x.dtype is not dtype or x.shape != shape or x.get_device() != self._dev_index:
             raise ValueError(f"{what}: {dtype} tensor {tuple(shape)} on {self._dev} expected, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
+        if x.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError(f"{what}: the tensor requires a gradient, and there is no backward pass; call under torch.no_grad()")
         ts, hs, es = x.stride()
         if es != 1 and shape[2] > 1:
             raise ValueError(f"{what}: the elements of a head must be consecutive")
@@ -600,7 +602,8 @@ class Engine:
         [q_start[s], q_start[s+1]) and holds kv_len[s] tokens with them; block_table[s, b] is the slot of its b-th
         16-token block (below n_hbm_blocks: HBM tier; above: tail block). positions: int32 [tokens] or [axes, tokens],
         by default the tokens' indices in their sequences. Asynchronous on the current stream; ids and lengths outside
-        their ranges are skipped and reported by kv_check()."""
+        their ranges are skipped and reported by kv_check(). No backward pass: tensors that require gradients are taken
+        under torch.no_grad() only."""
         done = self._append_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
                                    layer, k, v, block_table, q_start, kv_len,
                                    *((0, 1, None, None, False) if rope is None else
@@ -663,7 +666,8 @@ class Engine:
         batch as in append_kv. causal: a query sees the keys up to its own, with `window` the last `window` of them;
         causal=False: all kv_len keys. scale: 1 / sqrt(head_dim) if None. max_q_len: most new tokens of one sequence,
         if known (chooses the kernel, not the result). out, lse ([tokens, heads] float32, contiguous): written if
-        given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream."""
+        given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream. No backward
+        pass: tensors that require gradients are taken under torch.no_grad() only."""
         done = self._attend_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
                                    layer, q, block_table, q_start, kv_len, max_q_len, causal, window, scale, out, lse)
         if done is not NotImplemented:

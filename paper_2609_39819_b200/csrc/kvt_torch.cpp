@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -42,6 +43,7 @@ struct Call {
   void on(const at::Tensor &x) const { want(x.is_cuda() && x.get_device() == dev); }
   Place rows(const at::Tensor &x, at::ScalarType t, int64_t n, int64_t h) const {
     want(x.scalar_type() == t && x.dim() == 3 && x.size(0) == n && x.size(1) == h && x.size(2) == dim && (x.stride(2) == 1 || dim <= 1));
+    want(!x.requires_grad() || !at::GradMode::is_enabled());       // there is no backward pass
     on(x);
     return {x.data_ptr(), (uint64_t)x.stride(0), (uint64_t)x.stride(1)};
   }

@@ -200,3 +200,25 @@ def test_scale_of_nothing(B):  # noqa: F811
             for _, got, lse in every_kernel(s, scale=scale):
                 assert not bool(((got.double() - want).abs() > tol).any())
                 assert not bool(((lse.double() - wl).abs() > tl).any())
+
+
+def test_inputs_that_require_gradients_are_refused(B):  # noqa: F811
+    """There is no backward pass: results that silently carry no gradient are not what such a caller wants."""
+    import torch
+    s = Setup(B, [4], [20], heads=1, group=2, dim=64, seed=6)
+    good = (s.table, s.q_start, s.kv_len)
+    leaf = lambda x: x.detach().clone().requires_grad_()          # noqa: E731
+    for native in (True, False):
+        if not native:
+            s.eng._append_native = s.eng._attend_native = lambda *a: NotImplemented
+        for f in (lambda: s.eng.attend(s.layer, leaf(s.q), *good), lambda: s.eng.append_kv(s.layer, leaf(s.k), s.v, *good),
+                  lambda: s.eng.append_kv(s.layer, s.k, leaf(s.v), *good),
+                  lambda: s.eng.append_kv(s.layer, s.k, s.v, *good, rope=B.Rope(64), q=leaf(s.q)),
+                  lambda: s.eng.attend(s.layer, s.q, *good, out=leaf(s.q))):
+            with pytest.raises(ValueError, match="gradient"):
+                f()
+        with torch.no_grad():
+            s.eng.append_kv(s.layer, leaf(s.k), leaf(s.v), *good)
+            a = s.eng.attend(s.layer, leaf(s.q), *good)
+        assert torch.equal(a, s.eng.attend(s.layer, s.q, *good)) and not a.requires_grad
+    s.eng.kv_check()

@@ -553,9 +553,10 @@ class Engine:
 
     # ---- model-side operators on the HBM pool -----------------------------------------------------
     def set_tail_pool(self, pool):
-        """Tail blocks (slot ids n_hbm_blocks + i): a uint8 device tensor of whole blocks, block-major; None removes it."""
-        if pool is not None and (pool.device.type != "cuda" or pool.dtype != self.torch.uint8 or not pool.is_contiguous()):
-            raise ValueError("set_tail_pool: a contiguous uint8 tensor on the engine's device expected")
+        """Tail blocks (slot ids n_hbm_blocks + i): a uint8 device tensor of whole blocks, block-major; None removes it. Calls made
+        or captured before keep the tensor they were given, which has to be kept alive as long as they may run."""
+        if pool is not None and (pool.device != self._dev or pool.dtype != self.torch.uint8 or not pool.is_contiguous()):
+            raise ValueError(f"set_tail_pool: a contiguous uint8 tensor on the engine's device ({self._dev}) expected")
         self._check(self.L.kvt_set_tail_pool(self.h, pool.data_ptr() if pool is not None else None,
                                              pool.numel() if pool is not None else 0), "set_tail_pool")
         self.tail_pool = pool

@@ -222,3 +222,16 @@ def test_inputs_that_require_gradients_are_refused(B):  # noqa: F811
             a = s.eng.attend(s.layer, leaf(s.q), *good)
         assert torch.equal(a, s.eng.attend(s.layer, s.q, *good)) and not a.requires_grad
     s.eng.kv_check()
+
+
+def test_tail_pool_of_another_device_is_refused(B):  # noqa: F811
+    import torch
+    s = Setup(B, [4], [20], heads=1, group=2, dim=64, tail=True, seed=6)
+    p = s.eng.tail_pool
+    elsewhere = SimpleNamespace(device=torch.device("cuda", s.eng._dev_index + 1), dtype=p.dtype, is_contiguous=lambda: True,
+                                data_ptr=p.data_ptr, numel=p.numel, get_device=lambda: s.eng._dev_index + 1)
+    with pytest.raises(ValueError, match="device"):
+        s.eng.set_tail_pool(elsewhere)
+    with pytest.raises(ValueError, match="device"):
+        s.eng.set_tail_pool(torch.zeros(p.numel(), dtype=torch.uint8))
+    assert s.eng.tail_pool is p

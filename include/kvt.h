@@ -404,7 +404,7 @@ typedef struct kvt_batch {
   uint32_t max_blocks;          /* entries of a block table row */
   uint32_t max_q_len;           /* most new tokens of one sequence (0: not known). A hint that chooses the kernel of
                                    kvt_attend; results do not depend on it */
-  uint64_t table_stride;        /* elements between two rows of block_table */
+  uint64_t table_stride;        /* elements between two rows of block_table (0: one row for all sequences) */
   const uint32_t *q_start;      /* device, n_seqs + 1 */
   const uint32_t *kv_len;       /* device, n_seqs */
   const uint32_t *block_table;  /* device */
@@ -427,7 +427,7 @@ typedef struct kvt_append_args {
   const uint8_t *axis_of;       /* device, rot_dim/2: the row of `positions` pair j takes (>= n_axes reads as 0 and sets the
                                    error word); NULL: row 0 */
   const int32_t *positions;     /* device, n_axes rows of n_tokens; NULL: the token's index in its sequence */
-  uint64_t pos_stride;          /* elements between two rows of `positions` */
+  uint64_t pos_stride;          /* elements between two rows of `positions` (0: the same positions on all axes) */
 } kvt_append_args;
 
 /* Writes the new tokens' keys (rotated by their positions) and values into the blocks of `layer`, and the rotated

@@ -2277,7 +2277,6 @@ const char *kv_batch_fault(const kvt_batch &b) {
   if (!b.n_seqs || !b.n_tokens) return nullptr;     // nothing to do
   if (!b.q_start || !b.kv_len || !b.block_table || !b.max_blocks) return "batch without starts, lengths or block table";
   if (((uintptr_t)b.q_start | (uintptr_t)b.kv_len | (uintptr_t)b.block_table) & 3) return "misaligned batch array";
-  if (b.table_stride < b.max_blocks && b.n_seqs > 1) return "table_stride below max_blocks";
   if (b.n_seqs > 0x7FFFFFFFu / 2 || b.n_tokens > 0x7FFFFFFFu || b.max_blocks > 0x7FFFFFFFu / 16) return "batch too large";
   return nullptr;
 }
@@ -2342,7 +2341,6 @@ int32_t kvt_append_kv(kvt_engine *e, const kvt_append_args *args, void *stream) 
   if (((uintptr_t)a.q | (uintptr_t)a.q_out | (uintptr_t)a.k | (uintptr_t)a.v) & 1) return fail(e, KVT_E_INVAL, "append: misaligned tensor");
   if (a.rot_dim && (!a.freqs || ((uintptr_t)a.freqs & 7))) return fail(e, KVT_E_INVAL, "append: freqs");
   if (((uintptr_t)a.positions & 3) || (a.positions && !a.n_axes)) return fail(e, KVT_E_INVAL, "append: positions");
-  if (a.positions && a.n_axes > 1 && a.pos_stride < a.b.n_tokens) return fail(e, KVT_E_INVAL, "append: pos_stride");
   if ((u64)a.n_q_heads * e->cfg.head_dim > 0x7FFFFFFFu) return fail(e, KVT_E_INVAL, "append: too many query heads");
   OnDevice on(e->device);
   if (!on.ok) return fail(e, KVT_E_CUDA, "append: device");

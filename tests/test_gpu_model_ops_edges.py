@@ -235,3 +235,24 @@ def test_tail_pool_of_another_device_is_refused(B):  # noqa: F811
     with pytest.raises(ValueError, match="device"):
         s.eng.set_tail_pool(torch.zeros(p.numel(), dtype=torch.uint8))
     assert s.eng.tail_pool is p
+
+
+def test_positions_and_tables_that_are_broadcast(B):  # noqa: F811
+    """One row of positions for all axes (text among images), one table row for all sequences: read only, so nothing to refuse."""
+    import torch
+    s = Setup(B, [7, 20], [50, 3], heads=2, group=2, dim=64, seed=7)
+    rope = B.Rope(64, sections=[12, 10, 10])
+    pos = torch.arange(s.t, dtype=torch.int32, device="cuda") * 11
+    args = (s.table, s.q_start, s.kv_len)
+    for native in (True, False):
+        if not native:
+            s.eng._append_native = s.eng._attend_native = lambda *a: NotImplemented
+        want = s.eng.append_kv(s.layer, s.k, s.v, *args, rope=rope, positions=pos.repeat(3, 1), q=s.q)
+        pool = s.bits()
+        got = s.eng.append_kv(s.layer, s.k, s.v, *args, rope=rope, positions=pos[None].expand(3, -1), q=s.q)
+        assert torch.equal(want, got) and all(torch.equal(a, b) for a, b in zip(pool, s.bits()))
+        shared = s.table[:1].expand(2, -1)
+        short = torch.full_like(s.kv_len, min(s.kv))
+        assert torch.equal(s.eng.attend(s.layer, s.q, shared, s.q_start, short),
+                           s.eng.attend(s.layer, s.q, shared.contiguous(), s.q_start, short))
+    s.eng.kv_check()

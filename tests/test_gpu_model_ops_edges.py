@@ -1,6 +1,7 @@
 """append_kv and attend where they are easily wrong: what lies just outside the rows' keys, the ends of the element types'
 ranges, arguments that are nearly right, reports from several streams. Setup and its 64-bit reference are the other file's."""
 import ctypes as C
+import functools
 import math
 from types import SimpleNamespace
 
@@ -256,3 +257,86 @@ def test_positions_and_tables_that_are_broadcast(B):  # noqa: F811
         assert torch.equal(s.eng.attend(s.layer, s.q, shared, s.q_start, short),
                            s.eng.attend(s.layer, s.q, shared.contiguous(), s.q_start, short))
     s.eng.kv_check()
+
+
+def test_scratch_that_is_too_small_or_misaligned(B):  # noqa: F811
+    s = Setup(B, [100, 5], [3000, 40], heads=2, group=2, dim=128, seed=9)
+    out = s.torch.empty_like(s.q)
+    table = s.widened()                             # rows that could hold 320 K tokens: sequences may have to be cut
+    a = B.AttendArgs(B.Batch(2, s.t, table.shape[1], 0, table.stride(0), s.q_start.data_ptr(), s.kv_len.data_ptr(), table.data_ptr()),
+                     s.layer, 0, 4, 0, 0, 0.0, s.q.data_ptr(), out.data_ptr(), None, *s.q.stride()[:2], *out.stride()[:2])
+    lib, h = s.eng.L, s.eng.h
+    need = lib.kvt_attend_scratch_bytes(h, C.byref(a))
+    assert need > 0
+    scratch = s.torch.empty(need + 16, dtype=s.torch.uint8, device="cuda")
+    for ptr, size, code in ((scratch.data_ptr(), need - 1, B.E_BUFSZ), (None, need, B.E_BUFSZ), (scratch.data_ptr(), 0, B.E_BUFSZ),
+                            (scratch.data_ptr() + 8, need, B.E_INVAL)):
+        a.scratch, a.scratch_bytes = ptr, size
+        assert lib.kvt_attend(h, C.byref(a), None) == code
+    a.scratch, a.scratch_bytes = scratch.data_ptr(), need
+    s.put()
+    s.torch.cuda.synchronize()                      # this call runs on the default stream
+    assert lib.kvt_attend(h, C.byref(a), None) == 0
+    s.torch.cuda.synchronize()
+    s.eng.kv_check()
+    assert s.torch.equal(out, s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len))
+
+
+def test_one_wrong_argument_at_a_time(B):  # noqa: F811
+    """From calls that are taken, one argument spoiled: neither marshalling makes the call. (The library's entry points are stood in
+    for, so that nothing runs whatever gets through.)"""
+    import torch
+    s = Setup(B, [3, 5], [30, 200], heads=2, group=2, dim=64, seed=8)
+    t, cuda = s.t, dict(device="cuda")
+    made = []
+    entry = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p)(lambda e, a, st: made.append(1) or 0)
+    bytes_ = C.CFUNCTYPE(C.c_uint64, C.c_void_p, C.c_void_p)(lambda e, a: 0)
+    at = lambda f: C.cast(f, C.c_void_p).value               # noqa: E731
+    s.eng._append_native = functools.partial(B.load_native().append, at(entry))
+    s.eng._attend_native = functools.partial(B.load_native().attend, at(entry), at(bytes_))
+    real = s.eng.L
+    rope = B.Rope(64, sections=[8, 24])
+    pos = torch.zeros(2, t, dtype=torch.int32, **cuda)
+    lse = torch.zeros(t, 4, **cuda)
+
+    def other(x):
+        return [x.cpu(), x.float() if x.dtype != torch.float32 else x.half(), x[..., None], x[0], x[:, :1].repeat(1, 7)[:, :x.shape[1] - 1]
+                if x.dim() == 2 else x[:-1]]
+
+    append = dict(layer=s.layer, k=s.k, v=s.v, block_table=s.table, q_start=s.q_start, kv_len=s.kv_len, rope=rope, positions=pos, q=s.q,
+                  q_out=torch.zeros_like(s.q))
+    attend = dict(layer=s.layer, q=s.q, block_table=s.table, q_start=s.q_start, kv_len=s.kv_len, max_q_len=5, causal=True, window=7,
+                  scale=0.5, out=torch.zeros_like(s.q), lse=lse)
+    spoilt = {
+        "layer": [-1, None, "x", 1 << 70], "k": other(s.k) + [None, s.k[..., ::2], s.k.half()], "v": other(s.v) + [None, s.v.half()],
+        "block_table": [s.table.cpu(), s.table.long(), s.table[0], s.table[:1], s.table.T.contiguous().T, None],
+        "q_start": [s.q_start.cpu(), s.q_start.long(), s.q_start[:-1], s.q_start[None], s.q_start.repeat_interleave(2)[::2], None],
+        "kv_len": [s.kv_len.cpu(), s.kv_len.long(), s.kv_len[:-1], s.kv_len[None], s.kv_len.repeat_interleave(2)[::2], None],
+        "positions": [None, pos.cpu(), pos.long(), pos[:1], pos[0], pos[:, :-1], pos.T.contiguous().T],
+        "rope": [None, B.Rope(64, sections=[8, 20, 4])],
+        "q": [s.q.cpu(), s.q.float(), s.q.half(), s.q[0], s.q[:-1], s.q[..., :32]],
+        "q_out": other(s.q) + [s.q[:, :1].expand(-1, 4, -1), s.q[:1].expand(t, -1, -1)],
+        "out": other(s.q) + [s.q[:, :1].expand(-1, 4, -1), s.q[:1].expand(t, -1, -1)],
+        "lse": other(lse) + [torch.zeros(4, t, **cuda).T, lse.half()],
+        "max_q_len": [-1, "x"], "window": [-1, "x"], "scale": ["x"],
+    }
+    for call, args in ((s.eng.append_kv, append), (s.eng.attend, attend)):
+        which = "_append_native" if call == s.eng.append_kv else "_attend_native"
+        native = getattr(s.eng, which)
+        for python in (False, True):
+            s.eng.L = SimpleNamespace(kvt_append_kv=lambda e, a, st: made.append(1) or 0, kvt_attend=lambda e, a, st: made.append(1) or 0,
+                                      kvt_attend_scratch_bytes=lambda e, a: 0)
+            setattr(s.eng, which, (lambda *a: NotImplemented) if python else native)
+            try:
+                call(**args)
+                assert made == [1]
+                made.clear()
+                for name in args:
+                    for i, wrong in enumerate(spoilt.get(name, [])):
+                        with pytest.raises(Exception):
+                            call(**{**args, name: wrong})
+                        assert not made, (name, i, python)
+                    made.clear()
+            finally:
+                s.eng.L = real
+                setattr(s.eng, which, native)

@@ -355,7 +355,8 @@ __device__ __forceinline__ bool bar_try(u32 bar, u32 parity) {
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
-// Waits for the barrier's phase, for a second at most (nothing a kernel waits for takes a millisecond).
+// Waits for the barrier's phase, for a second at most. For what hardware does: a copy, a product, a cluster-launch answer, all of
+// which take microseconds. (Warps that wait for one another's work: tc_wait.)
 constexpr u64 WAIT_NS = 1000000000ull;
 __device__ __forceinline__ u64 now_ns() { u64 t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
 __device__ __forceinline__ bool bar_wait_slow(u32 bar, u32 parity) {
@@ -1362,20 +1363,23 @@ __device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 r; asm("fma.rn.f3
 __device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
-// A wait that also ends when another warp of the CTA has given up; gives up itself after WAIT_NS.
-__device__ __forceinline__ bool tc_wait_slow(u32 bar, u32 parity, volatile u32 *lost) {
-  const u64 t0 = now_ns();
+// What ends the waits of a CTA's warps for one another: another warp has given up, or the time is over. A warp may have to wait
+// until the others are through with up to TC_JOBS jobs, each as long as a table row at most: 16 keys take 0.25 us (both tiles,
+// at 1.5 GHz), so a job on 258 K keys 4 ms, and a second would be over at 64 M keys. Per block of a table row 4 us more are four times that.
+constexpr u64 WAIT_BLOCK_NS = 4000;
+__device__ __forceinline__ bool tc_wait_slow(u32 bar, u32 parity, volatile u32 *lost, u32 blocks) {
+  const u64 t0 = now_ns(), limit = WAIT_NS + WAIT_BLOCK_NS * blocks;
   do {
     for (u32 i = 0; i < 32; ++i) if (bar_try(bar, parity)) return true;
     if (*lost) return false;
-  } while (now_ns() - t0 < WAIT_NS);
+  } while (now_ns() - t0 < limit);
   *lost = 1;
   return false;
 }
-__device__ __forceinline__ bool tc_wait1(u32 bar, u32 parity, volatile u32 *lost) { return bar_try(bar, parity) || tc_wait_slow(bar, parity, lost); }
+__device__ __forceinline__ bool tc_wait1(u32 bar, u32 parity, volatile u32 *lost, u32 blocks) { return bar_try(bar, parity) || tc_wait_slow(bar, parity, lost, blocks); }
 // Whole warps wait, and come back with one answer.
-__device__ __forceinline__ bool tc_wait(u32 bar, u32 parity, volatile u32 *lost) {
-  return __all_sync(~0u, bar_try(bar, parity) || tc_wait_slow(bar, parity, lost));
+__device__ __forceinline__ bool tc_wait(u32 bar, u32 parity, volatile u32 *lost, u32 blocks) {
+  return __all_sync(~0u, bar_try(bar, parity) || tc_wait_slow(bar, parity, lost, blocks));
 }
 
 // A piece of a tile, as the scheduling warp hands it to the others.
@@ -1432,7 +1436,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
   u32 jobs = 0;
   auto next_job = [&](Job &j) {
     const u32 at = jobs % TC_JOBS;
-    if (!tc_wait(jfull + at * 8, (jobs / TC_JOBS) & 1, lost)) return false;
+    if (!tc_wait(jfull + at * 8, (jobs / TC_JOBS) & 1, lost, a.b.max_blocks)) return false;
     j = s_job[at];
     __syncwarp();
     if (lane == 0) bar_arrive(jempty + at * 8);
@@ -1519,7 +1523,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       }
       const u32 hit = __ballot_sync(~0u, want >= at && want < at + my_jobs);
       const u32 slot = k % TC_JOBS;
-      if (k >= TC_JOBS && !(ok = tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost))) break;
+      if (k >= TC_JOBS && !(ok = tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost, a.b.max_blocks))) break;
       if (hit && lane == __ffs(hit) - 1) {
         Job j;
         const u32 x = want - at, y = x / H, h = x - y * H, pc = y / tiles, tile = tiles - 1 - (y - pc * tiles);
@@ -1561,7 +1565,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
         const u32 slot = __shfl_sync(~0u, slots, (s % 4) * TC_KB + lane % TC_KB);
         for (u32 kv = 0; kv < 2; ++kv, ++it) {
           const u32 st = it % S::STAGES;
-          if (it >= S::STAGES && !tc_wait(empty + st * 8, (it / S::STAGES - 1) & 1, lost)) { ok = false; break; }
+          if (it >= S::STAGES && !tc_wait(empty + st * 8, (it / S::STAGES - 1) & 1, lost, a.b.max_blocks)) { ok = false; break; }
           if (lane == 0) bar_expect(full + st * 8, S::STAGE);
           __syncwarp();
           if (lane < TC_KB) load_block(a, maps, ring + st * S::STAGE + lane * S::BLOCK, full + st * 8, slot, 2 * a.layer + kv, j.h, D / 64);
@@ -1583,7 +1587,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       struct Place { u32 st, ph; };      // a stage and its phase
       auto after = [](Place x) { return x.st + 1 == S::STAGES ? Place{0, x.ph ^ 1} : Place{x.st + 1, x.ph}; };
       auto has = [&](Place x) { return bar_try(full + x.st * 8, x.ph); };
-      auto landed = [&](Place x) { return tc_wait1(full + x.st * 8, x.ph, lost); };
+      auto landed = [&](Place x) { return tc_wait1(full + x.st * 8, x.ph, lost, a.b.max_blocks); };
       auto product_s = [&](u32 i, u32 st) {
         const u64 dk = dk0 + st * (S::STAGE / 16);
 #pragma unroll
@@ -1597,7 +1601,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       bool ok = true;
       for (;;) {
         const u32 at = jobs % TC_JOBS;
-        if (!(ok = tc_wait1(jfull + at * 8, (jobs / TC_JOBS) & 1, lost))) break;
+        if (!(ok = tc_wait1(jfull + at * 8, (jobs / TC_JOBS) & 1, lost, a.b.max_blocks))) break;
         ++jobs;
         const u32 r0 = s_job[at].r0, r1 = s_job[at].r1, b0 = s_job[at].b0, b1 = s_job[at].b1, kv = s_job[at].kv, first = s_job[at].first,
                   end = s_job[at].last;
@@ -1610,7 +1614,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
 #pragma unroll
         for (u32 i = 0; i < 2; ++i)
           if (ok && (i == 0 || two)) {
-            ok = tc_wait1(qready + i * 8, seen_q[i]++ & 1, lost);
+            ok = tc_wait1(qready + i * 8, seen_q[i]++ & 1, lost, a.b.max_blocks);
             tc_after();
             if (ok) product_s(i, at_k.st);
           }
@@ -1641,7 +1645,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
               const u32 phase = seen_p[i]++ & 1;
 #pragma unroll
               for (u32 part = 0; part < TC_PARTS; ++part) {
-                ok = ok && tc_wait1(pready + (i * TC_PARTS + part) * 8, phase, lost);
+                ok = ok && tc_wait1(pready + (i * TC_PARTS + part) * 8, phase, lost, a.b.max_blocks);
                 if (!ok) break;
                 tc_after();
 #pragma unroll
@@ -1729,7 +1733,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       }
       float m = -INFINITY, l = 0.0f;
       for (u32 s = 0; s < n; ++s) {
-        if (!(ok = tc_wait(sready + i * 8, seen_s++ & 1, lost))) break;
+        if (!(ok = tc_wait(sready + i * 8, seen_s++ & 1, lost, a.b.max_blocks))) break;
         tc_after();
         u32 x[128];
         float *const v = reinterpret_cast<float *>(x);
@@ -1803,7 +1807,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       const u64 prow = (u64)j.part * TC_ROWS + i * TC_TILE + rt;
       u8 *const out = direct ? (u8 *)((u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs) : (u8 *)(scratch_sums(a) + prow * D);
       have = begin(j);
-      if (n && !(ok = tc_wait(oready + i * 8, seen_o++ & 1, lost))) break;
+      if (n && !(ok = tc_wait(oready + i * 8, seen_o++ & 1, lost, a.b.max_blocks))) break;
       tc_after();
       if (mine) {
         if (!direct) ((float2 *)(scratch_sums(a) + (u64)n_parts * TC_ROWS * D))[prow] = make_float2(m, l);

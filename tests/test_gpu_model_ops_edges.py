@@ -340,3 +340,35 @@ def test_one_wrong_argument_at_a_time(B):  # noqa: F811
             finally:
                 s.eng.L = real
                 setattr(s.eng, which, native)
+
+
+# ---- very long work ------------------------------------------------------------------------------------------------------
+def test_warps_wait_as_long_as_a_job_takes(B):  # noqa: F811
+    """A job of more than a second in front of a short one: the warps that wait for the short one must not give up. 130 M
+    cached tokens of 148 heads, whose table row names the same 60 blocks over and over."""
+    import torch
+    heads, group, dim, n_slots, long_kv = 148, 4, 64, 64, 130_000_000
+    eng = B.Engine(n_layers=1, n_kv_heads=heads, head_dim=dim, n_hbm_blocks=n_slots, n_host_blocks=0, max_contexts=1, max_messages=16,
+                   max_tokens=64)
+    g = torch.Generator("cuda").manual_seed(1)
+    eng.hbm_pool.view(torch.bfloat16).normal_(generator=g)
+    new, kv = [32, 64], [long_kv, 500]              # one tile of rows, then two
+    q = torch.randn(sum(new), heads * group, dim, generator=g, device="cuda").bfloat16()
+    table = (torch.arange(-(-long_kv // BT), device="cuda") % 60).int()[None].expand(2, -1)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")          # noqa: E731
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    out = eng.attend(0, q, table, ints(0, 32, 96), ints(*kv), max_q_len=64)
+    end.record()
+    eng.kv_check()
+    assert begin.elapsed_time(end) > 1000, "not as long as it has to be for this test"
+    assert bool(torch.isfinite(out).all())
+    pool = eng.hbm_pool.view(torch.bfloat16).view(2, n_slots, BT, heads, dim).double()
+    k, v = (pool[c, :60].reshape(-1, heads, dim)[:500].repeat_interleave(group, 1) for c in (0, 1))
+    x = torch.einsum("ihd,jhd->hij", q[32:].double(), k) * dim ** -0.5
+    x = x.masked_fill(torch.arange(500, device="cuda")[None] > torch.arange(436, 500, device="cuda")[:, None], -math.inf)
+    p = torch.softmax(x, -1)
+    want, size = torch.einsum("hij,jhd->ihd", p, v), torch.einsum("hij,jhd->ihd", p, v.abs())
+    # the probabilities' and the result's rounding, and 32-bit sums of 500 terms and scores of 64
+    assert not bool(((out[32:].double() - want).abs() > 2.0 ** -8 * want.abs() + size * (2.0 ** -8 + 2.0 ** -12)).any())
+    eng.close()

@@ -458,8 +458,8 @@ typedef struct kvt_attend_args {
 
 /* softmax(scale q k^T) v of the new tokens over their sequences' keys and values in the pool (their own included:
  * append first). A row that sees no key gives zeros and lse = -inf. Scores, sums and the output are held in 32 bits;
- * the probabilities are rounded to the element type for the second product (in fp16, where there are few rows, to the sum of
- * two such numbers). In fp16, whose range is small, they are relative to a number that follows the scores of the keys in hand up
+ * the probabilities are taken as the sum of two numbers of the element type for the second product where there are few rows, which
+ * leaves the error of 32-bit probabilities, and rounded to one where there are many. In fp16, whose range is small, they are relative to a number that follows the scores of the keys in hand up
  * and down: 128 keys in a row lose less than 2^-14 of the largest of their probabilities, however small that is. Keys a row does not see have no effect, whatever their values, with one exception: a value that is Inf or
  * NaN in a token that other rows of the sequence see may reach all of that sequence's new rows. What lies in a block
  * behind kv_len has no effect. Errors: KVT_E_INVAL as above (head_dim above 256, heads that do not divide, window with

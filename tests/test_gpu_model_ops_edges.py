@@ -372,3 +372,32 @@ def test_warps_wait_as_long_as_a_job_takes(B):  # noqa: F811
     # the probabilities' and the result's rounding, and 32-bit sums of 500 terms and scores of 64
     assert not bool(((out[32:].double() - want).abs() > 2.0 ** -8 * want.abs() + size * (2.0 ** -8 + 2.0 ** -12)).any())
     eng.close()
+
+
+# ---- rounding ------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 72])
+@pytest.mark.parametrize("past", [5, 300, 3000])
+def test_few_rows_are_as_exact_as_with_32_bit_probabilities(B, past, dim, dtype):  # noqa: F811
+    """Only the result is rounded to the element type, not the probabilities."""
+    import torch
+    s = Setup(B, [2], [past], heads=2, group=3, dim=dim, dtype=dtype, seed=past + dim)
+    s.put()
+    n = s.kv[0]
+    k, v = (x.repeat_interleave(3, 1) for x in s.gather(0))
+    q = s.q.double()
+    x = torch.einsum("ihd,jhd->ihj", q, k) * dim ** -0.5
+    hidden = torch.arange(n, device="cuda")[None, None] > torch.arange(n - 2, n, device="cuda")[:, None, None]
+    p = torch.softmax(x.masked_fill(hidden, -math.inf), -1)
+    want, size = torch.einsum("ihj,jhd->ihd", p, v), torch.einsum("ihj,jhd->ihd", p, v.abs())
+    # scores: dim products summed in 32 bits and the scaling; sums over the keys in 32 bits; a probability is the sum of two numbers,
+    # the second rounded: u * u, or for fp16 (16 keys' fixed step, 2^-25 each, relative to 2^-4 at least) 2^-17 of the largest
+    big = (torch.einsum("ihd,jhd->ihj", q.abs(), k.abs()) * dim ** -0.5).masked_fill(hidden, 0.0).amax(-1, keepdim=True)
+    rel = 2 * (dim + 4) * 2.0 ** -24 * big + 2 * (n + 64) * 2.0 ** -24 + max(s.u * s.u, 2.0 ** -17)
+    tol = s.u * want.abs() + size * rel * (1 + s.u) + (2.0 ** -25 if dtype == "fp16" else 0.0)
+    assert dtype == "fp16" or bool((rel < s.u / 3).all())      # so that probabilities rounded once would show
+    for table in (s.table, s.widened()):
+        got = s.eng.attend(s.layer, s.q, table, s.q_start, s.kv_len, max_q_len=2)
+        bad = (got.double() - want).abs() > tol
+        assert not bool(bad.any()), int(bad.sum())
+    s.eng.kv_check()

@@ -953,7 +953,7 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
     // The second product takes powers of the element type. Rounded once they would add a third (bf16) or half (fp16) to the error
     // of the result's own rounding, so they are taken as the sum of two such numbers, which leaves 2^-16 or 2^-22 of a power (or
     // fp16's fixed step): the results are those of 32-bit powers. Loading K and V leaves the matrix units the time, or nearly (bf16:
-    // one token on 1000 7.0 -> 7.3 us, on 258 K 170.4 -> 174.7, 32 long sessions 917 -> 933).
+    // one token on 1000 7.0 -> 7.3 us, on 258 K 170.4 -> 173.9, 32 long sessions 910 -> 919).
     u32 p[4], rest[4];
 #pragma unroll
     for (u32 y = 0; y < 4; ++y) {
@@ -963,13 +963,14 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
       rest[y] = Elem<T>::down(e0 - z.x, e1 - z.y);
     }
 #pragma unroll
-    for (u32 n = 0; n < D / 16; ++n) {
-      u32 f[4];
-      ldm4t(f, vb + block_off<D>(lane % 16, 2 * n + lane / 16));
-      mma16816<T>(o[2 * n], p, f[0], f[1]);
-      mma16816<T>(o[2 * n + 1], p, f[2], f[3]);
-      mma16816<T>(o[2 * n], rest, f[0], f[1]);
-      mma16816<T>(o[2 * n + 1], rest, f[2], f[3]);
+    for (u32 n = 0; n < D / 16; n += 2) {      // a sum's two products some distance apart
+      u32 f[2][4];
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y) ldm4t(f[y], vb + block_off<D>(lane % 16, 2 * (n + y) + lane / 16));
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) mma16816<T>(o[2 * n + y], p, f[y / 2][y % 2 * 2], f[y / 2][y % 2 * 2 + 1]);
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) mma16816<T>(o[2 * n + y], rest, f[y / 2][y % 2 * 2], f[y / 2][y % 2 * 2 + 1]);
     }
     __syncwarp();                      // the stage is read: refill it
     if (i + S::STAGES < n_mine) load(i + S::STAGES);

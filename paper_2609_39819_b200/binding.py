@@ -692,6 +692,8 @@ class Engine:
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != (t, hq) or lse.get_device() != self._dev_index or
                                 not lse.is_contiguous()):
             raise ValueError(f"attend: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
+        if lse is not None and lse.requires_grad and torch.is_grad_enabled():
+            raise ValueError("attend: lse requires a gradient, and there is no backward pass; call under torch.no_grad()")
         batch = self._kv_batch("attend", t, block_table, q_start, kv_len, max_q_len)
         flags, lsep = 0 if causal else ATTN_FULL, lse.data_ptr() if lse is not None else 0
         # 0, which is the library's word for the default, becomes next to 0

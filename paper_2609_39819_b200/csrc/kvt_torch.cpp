@@ -193,7 +193,8 @@ PyObject *attend(PyObject *, PyObject *const *x, Py_ssize_t n) {
     a.out = op.p; a.o_ts = op.ts; a.o_hs = op.hs;
     if (x[17] != Py_None) {
       const at::Tensor &l = tensor(x[17]);
-      want(l.scalar_type() == at::kFloat && l.dim() == 2 && l.size(0) == tokens && l.size(1) == hq && l.is_contiguous());
+      want(l.scalar_type() == at::kFloat && l.dim() == 2 && l.size(0) == tokens && l.size(1) == hq && l.is_contiguous() &&
+           (!l.requires_grad() || !at::GradMode::is_enabled()));
       c.on(l);
       a.lse = (float *)l.data_ptr();
     }

@@ -401,3 +401,36 @@ def test_few_rows_are_as_exact_as_with_32_bit_probabilities(B, past, dim, dtype)
         bad = (got.double() - want).abs() > tol
         assert not bool(bad.any()), int(bad.sum())
     s.eng.kv_check()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 72])
+@pytest.mark.parametrize("new", [1, 40, 200])
+def test_fp16_nan_and_infinite_scores_stay_with_the_rows_that_see_them(B, new, dim):  # noqa: F811
+    """NaN and +Inf spoil the rows that see the key, -Inf takes its weight away; what the powers are relative to survives all of them."""
+    import torch
+    for back in (0, 7, 120, 250):                   # how far before the end the key lies
+        s = Setup(B, [new, 5], [300, 40], heads=2, group=2, dim=dim, dtype="fp16", seed=9)
+        s.q[:, :, 0] = s.q[:, :, 0].abs() + 0.5
+        s.put()
+        at = s.kv[0] - 1 - back
+        place = s._chunk(int(s.host_table[0, at // BT]), 0)[at % BT, 1]
+        spoilt = torch.zeros(s.t, 4, dtype=torch.bool, device="cuda")
+        spoilt[:new, 2:] = (torch.arange(new, device="cuda") + 300 >= at)[:, None]
+        for bad in (math.nan, math.inf, -math.inf):
+            place[0] = bad
+            for _, got, lse in every_kernel(s):
+                if bad == -math.inf:
+                    assert bool(torch.isfinite(got).all()) and bool(torch.isfinite(lse).all()), (back, bad)
+                else:
+                    assert torch.equal(torch.isnan(got).all(-1), spoilt) and torch.equal(torch.isfinite(got).all(-1), ~spoilt), (back, bad)
+                    assert torch.equal(torch.isfinite(lse), ~spoilt), (back, bad)
+
+
+def test_lse_that_requires_a_gradient_is_refused(B):  # noqa: F811
+    import torch
+    s = Setup(B, [4], [20], heads=1, group=2, dim=64, seed=6)
+    for native in (True, False):
+        if not native:
+            s.eng._attend_native = lambda *a: NotImplemented
+        with pytest.raises(ValueError, match="gradient"):
+            s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len, lse=torch.zeros(4, 2, device="cuda", requires_grad=True))

@@ -29,7 +29,9 @@
  *     that return counts or data to the host synchronise that stream before returning (stated per
  *     call); kvt_copy_blocks is asynchronous.
  *   - An engine is not thread-safe; calls on one engine must be serialised by the caller and must
- *     all use streams that are ordered with respect to each other.
+ *     all use streams that are ordered with respect to each other. The one exception: kvt_append_kv,
+ *     kvt_attend and kvt_kv_check may be enqueued on streams that are not ordered (still by one host
+ *     thread at a time), under the conditions stated there.
  *   - Every device-side loop (table probe loops) has an iteration cap; on overrun the kernel sets
  *     a device error word and returns normally, and the call reports KVT_E_DEVICE.
  *   - The library has no CPU fallback: without a usable CUDA device kvt_create fails with
@@ -403,7 +405,8 @@ typedef struct kvt_batch {
   uint32_t n_tokens;
   uint32_t max_blocks;          /* entries of a block table row */
   uint32_t max_q_len;           /* most new tokens of one sequence (0: not known). A hint that chooses the kernel of
-                                   kvt_attend; results do not depend on it */
+                                   kvt_attend: any value is right, but kernels round differently, so results with
+                                   another hint agree within their rounding and not bit by bit */
   uint64_t table_stride;        /* elements between two rows of block_table (0: one row for all sequences) */
   const uint32_t *q_start;      /* device, n_seqs + 1 */
   const uint32_t *kv_len;       /* device, n_seqs */
@@ -457,12 +460,14 @@ typedef struct kvt_attend_args {
 } kvt_attend_args;
 
 /* softmax(scale q k^T) v of the new tokens over their sequences' keys and values in the pool (their own included:
- * append first). A row that sees no key gives zeros and lse = -inf. Scores, sums and the output are held in 32 bits;
- * the probabilities are taken as the sum of two numbers of the element type for the second product where there are few rows, which
- * leaves the error of 32-bit probabilities, and rounded to one where there are many. In fp16, whose range is small, they are relative to a number that follows the scores of the keys in hand up
- * and down: 128 keys in a row lose less than 2^-14 of the largest of their probabilities, however small that is. Keys a row does not see have no effect, whatever their values, with one exception: a value that is Inf or
- * NaN in a token that other rows of the sequence see may reach all of that sequence's new rows. What lies in a block
- * behind kv_len has no effect. Errors: KVT_E_INVAL as above (head_dim above 256, heads that do not divide, window with
+ * append first). A row that sees no key gives zeros and lse = -inf. Scores, sums and the output are held in 32 bits.
+ * For the second product the probabilities are taken as the sum of two numbers of the element type where there are few
+ * rows (and for every head_dim other than 64 and 128), which leaves the error of 32-bit probabilities, and rounded to
+ * one where there are many. In fp16, whose range is small, they are relative to a number that follows the scores of the
+ * keys in hand up and down: 128 keys in a row lose less than 2^-14 of the largest of their probabilities, however small
+ * that is. Keys a row does not see have no effect, whatever their values, with one exception: a value that is Inf or NaN
+ * in a token that other rows of the sequence see may reach all of that sequence's new rows. What no row sees, in front of
+ * a window or in a block behind kv_len, has no effect. Errors: KVT_E_INVAL as above (head_dim above 256, heads that do not divide, window with
  * KVT_ATTN_FULL, scale that is negative or not finite), KVT_E_BUFSZ scratch too small. Asynchronous. */
 int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *a, void *stream);
 /* Depends on sizes only (n_seqs, n_tokens, max_blocks, max_q_len, n_q_heads), not on what device arrays hold.

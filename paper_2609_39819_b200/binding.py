@@ -666,7 +666,7 @@ class Engine:
         first: the new tokens are among the kv_len[s]). q: [tokens, heads, head_dim], heads a multiple of n_kv_heads;
         batch as in append_kv. causal: a query sees the keys up to its own, with `window` the last `window` of them;
         causal=False: all kv_len keys. scale: 1 / sqrt(head_dim) if None. max_q_len: most new tokens of one sequence,
-        if known (chooses the kernel, not the result). out, lse ([tokens, heads] float32, contiguous): written if
+        if known (chooses the kernel; results agree within their rounding). out, lse ([tokens, heads] float32, contiguous): written if
         given; rows behind the last sequence stay as they are. Returns out. Asynchronous on the current stream. No backward
         pass: tensors that require gradients are taken under torch.no_grad() only."""
         done = self._attend_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,

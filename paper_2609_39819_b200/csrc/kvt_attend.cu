@@ -109,7 +109,8 @@ __device__ __forceinline__ float2 pair_angle(const AppendArgs &a, u32 t, u32 ind
   return make_float2(c, s);
 }
 
-// One element (or one pair) at a time: any head size, stride and alignment.
+// One element (or one pair) at a time: any head size, stride and alignment. Bound by the number of its loads and stores of two bytes:
+// 8192 tokens of 32 + 16 heads of 128 an odd distance apart 84 us (the 16-byte kernel 39), of heads of 72 51 us (floor 17).
 template <class T>
 __global__ void __launch_bounds__(128) k_append_any(AppendArgs a) {
   extern __shared__ float2 cs[];
@@ -160,8 +161,9 @@ __global__ void __launch_bounds__(128) k_append_any(AppendArgs a) {
 // 8 elements from either half, with neighbouring pairs 16 in a row. All loads of a thread's UNROLL items are in flight
 // before the token's sines are waited for. GROUP threads work on a token: the whole CTA, or with few heads a warp, so that
 // a CTA of four takes four tokens. SHIFT: log2 of a head's items, -1 where that is no whole number.
-// Measured (bf16, heads of 128): 8192 tokens of 32 + 16 heads 38.6 us (201 MB, 80 % of the measured copy bandwidth), 44,130
-// tokens of 96 + 16 heads 394 us (98 %), a decode step of 32 tokens 4.1 us (launch and two rounds of loads).
+// Measured (bf16, heads of 128, in a captured graph; call after call in brackets): 8192 tokens of 32 + 16 heads 38.7 us (41.0;
+// 201 MB, 79 % of the measured copy bandwidth), 44,130 tokens of 96 + 16 heads 410-420 us (427; 92-94 %), a decode step of
+// 32 tokens 4.2 us (launch and two rounds of loads).
 template <class T, u32 THREADS, u32 GROUP, u32 UNROLL, int SHIFT>
 __global__ void __launch_bounds__(THREADS) k_append_vec(AppendArgs a) {
   extern __shared__ float2 cs_all[];
@@ -759,10 +761,11 @@ __global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, 
 // the keys for up to 16 rows of one KV head, the height of a warp-level matrix instruction. Every warp has its own ring
 // of TMA loads (a block's K and V per stage) and its own running maximum and sums over every fourth block, so warps
 // never wait for one another until the end of a unit. Two CTAs per SM keep up to 192 KB of loads in flight.
-// The matrix units idle most of the time (20 % busy), so the warp-level instructions do, whose sums and operands lie in
+// The matrix units idle most of the time (30 % busy), so the warp-level instructions do, whose sums and operands lie in
 // registers: nothing has to be handed from one kind of warp to another.
-// Measured, heads of 128, 8 KV heads, groups of 4: one token on 258,047 (1.06 GB) 169-173 us with the join, 6.2 TB/s, 95 % of the
-// measured copy bandwidth; 32 tokens on 2,000 to 130,000 each (6.1 GB, groups of 12) 905 us, 102 %.
+// Measured, heads of 128, 8 KV heads, groups of 4, in a captured graph (call after call in brackets): one token on 258,047 (1.06
+// GB) 174-177 us (180) with the join, 6.0 TB/s, 92 % of the measured copy bandwidth; 32 tokens on 2,000 to 130,000 each (6.1 GB,
+// groups of 12) 915-922 us (950), 101 %.
 // ------------------------------------------------------------------------------------------------------
 constexpr u32 SPLIT_ROWS = 16, SPLIT_WARPS = 4, SPLIT_THREADS = SPLIT_WARPS * 32;
 template <u32 D> struct SplitShape {
@@ -952,8 +955,9 @@ __device__ __forceinline__ bool split_keys(const AttendArgs &a, const KvMaps &ma
       for (u32 y = 0; y < 4; ++y) { s[n][y] = ex2(s[n][y] - ref[y >> 1]); l[y >> 1] += s[n][y]; }
     // The second product takes powers of the element type. Rounded once they would add a third (bf16) or half (fp16) to the error
     // of the result's own rounding, so they are taken as the sum of two such numbers, which leaves 2^-16 or 2^-22 of a power (or
-    // fp16's fixed step): the results are those of 32-bit powers. Loading K and V leaves the matrix units the time, or nearly (bf16:
-    // one token on 1000 7.0 -> 7.3 us, on 258 K 170.4 -> 173.9, 32 long sessions 910 -> 919).
+    // fp16's fixed step): the results are those of 32-bit powers. Loading K and V leaves the matrix units the time, or nearly (bf16,
+    // call after call: one token on 1000 8.2 us with and without, on 258 K 175 -> 180, 32 long sessions 924 -> 950). Second numbers in
+    // the rows of the operand that are nobody's, where there are that many, save the second product but were slower (182, 957).
     u32 p[4], rest[4];
 #pragma unroll
     for (u32 y = 0; y < 4; ++y) {
@@ -1153,13 +1157,15 @@ k_attend_split(const __grid_constant__ AttendArgs a, const __grid_constant__ KvM
 // Few units of moderate length: a cluster of CTAs takes a unit, its blocks dealt out evenly, and joins the parts through the
 // CTAs' shared memory: one launch, no scratch. Bound by latency: 4 us for the launch, the lengths and the first block, then a
 // block of each warp's every 0.8 us, then the join through shared memory. One token, 8 KV heads of 128, groups of 4: 300 cached
-// tokens 6.2 us, 1000 7.0, 4000 10.5, 8000 13.9 (33 MB, 2.4 TB/s); the kernel with two launches takes 11.6, 13.7 and 14.8.
+// tokens 6.2 us, 1000 7.1, 4000 11.1, 8000 14.8 (33 MB, 2.2 TB/s); the kernel with two launches took 11.6, 13.7 and 14.8 for the
+// last three when this one took 7.0, 10.5 and 13.9.
 //
 // ANY: heads of every other size up to 256 and every alignment, filled up to 64, 128 or 256 columns with zeros (three widths are
 // enough: the matrix units have time, and no more bytes are read). K and V come with 16-byte copies where the head allows it,
 // element by element elsewhere. Long sequences and prompts are its work too, without a kernel of their own. Heads of 96, 8 KV
-// heads, groups of 4: one token on 4000 22 us, 1000 new tokens 176 us, 32 on 1000 18 us (with 32-bit arithmetic on the CUDA
-// cores and one CTA per unit 1613, 1064 and 424).
+// heads, groups of 4: one token on 4000 22 us, 1000 new tokens 185 us, 32 on 1000 19 us (with 32-bit arithmetic on the CUDA
+// cores and one CTA per unit 1613, 1064 and 424). Far from the floor where there is much to do, since every tile of 16 rows reads its
+// keys again and a unit has 8 CTAs at most: 8192 new tokens 8.3 ms (floor 0.25), one token on 100 K 386 us (47).
 template <class T, u32 D, u32 CLUSTER, bool ANY>
 __global__ void __launch_bounds__(SPLIT_THREADS, D > 128 ? 1 : 2)
 k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps maps) {
@@ -1282,9 +1288,9 @@ k_attend_cluster(const __grid_constant__ AttendArgs a, const __grid_constant__ K
 // waits for the second product of its P.
 // Measured (heads of 128, bf16): 128 keys for both tiles take 2950 cycles, of which the tensor cores need 2040 and the exponential
 // units 2048: a row waits 830 cycles for its S, then 50 to load it, 350 for the maximum, 1460 for the powers, 160 for the store.
-// 8192 new tokens, 8 KV heads, groups of 4: 434-440 us cold (1260 TFLOP/s; 76 % of the measured matrix rate), 508 us at the
-// 1.58 GHz that the power limit leaves when it runs on and on (1081 TFLOP/s, 78 % of the sustained rate). 500 tokens on 130,500:
-// 890-1000 us. Tried and slower or the same: two threads per row (480 us where this took 465), a thread issuing the products
+// 8192 new tokens, 8 KV heads, groups of 4: 432-441 us in a captured graph (1260 TFLOP/s; 76 % of the measured matrix rate), 500-514 us at
+// the 1.58 GHz that the power limit leaves when it runs on and on (1085 TFLOP/s, 78 % of the sustained rate). 500 tokens on 130,500:
+// 960-1000 us, 1011-1032 on and on. Tried and slower or the same: two threads per row (480 us where this took 465), a thread issuing the products
 // for each tile (525: the tiles fall into step), P handed over in four parts, a polynomial for every fourth power (0-4 %).
 // Between two jobs of a CTA 4 us pass, and a launch has its first S after 6 us, most of it for working out the jobs.
 // ------------------------------------------------------------------------------------------------------

@@ -393,8 +393,8 @@ __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32
 //         the weight and whose value is small, for one). So the largest power aims at 2^8, and where a step's largest is
 //         below 2^-4, m falls: what a step of 128 keys loses to the fixed step is then below 128 * 2^-25 * 2^4 = 2^-14 of the
 //         step's largest power. (With 2^12 as the aim m moves more often: 8192-token prompt 485 us, with 2^8 454, before m
-//         could fall 456.) m does not fall where that would bring the sums above 2^LIMIT (32-bit sums of powers times values then stay
-//         below 2^107): what is that far below has no weight in 32 bits either.
+//         could fall 456.) m does not fall where that would bring a sum of powers above LIMIT = 2^90 (sums of powers times values, of all
+//         parts together too, then stay below 2^120): what is that far below has no weight in 32 bits either.
 constexpr float LIMIT = 0x1p90f;
 template <class T> __device__ __forceinline__ bool must_fall(float m, float top) { return Elem<T>::LOW > -INFINITY && top < m + Elem<T>::LOW && top > -INFINITY; }
 template <class T> __device__ __forceinline__ bool must_move(float m, float top) { return top > m + Elem<T>::HIGH || must_fall<T>(m, top); }

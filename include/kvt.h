@@ -474,6 +474,128 @@ int32_t kvt_attend(kvt_engine *e, const kvt_attend_args *a, void *stream);
  * 0 for arguments kvt_attend refuses and where none is needed. */
 uint64_t kvt_attend_scratch_bytes(kvt_engine *e, const kvt_attend_args *a);
 
+/* ---- choosing blocks: what a step reads and what a sequence keeps ---------------------------------- */
+/* For long contexts: attention over some of a sequence's blocks only, chosen for every new token and KV head by a cheap
+ * score (kvt_bound_keys, kvt_select_blocks, kvt_attend_blocks), and eviction of the blocks that get least of the attention
+ * (kvt_weigh_blocks, kvt_evict_blocks). Batches, slots, errors on the device and streams are those of kvt_append_kv and
+ * kvt_attend. "Block" below is a number in a sequence: block b holds tokens [16 b, 16 b + 16) and lies in slot
+ * block_table[s][b]; a token's own block is the one it lies in.
+ *
+ * Bounds of the keys of full blocks, in memory of the caller, for slot ids below n_slots (n_hbm_blocks, or more for tail
+ * blocks that will be full): in channel d the keys of a block reach up to up_d and down to -down_d, held as whole steps of
+ * 2^e, ceil(x / 2^e), with the least e >= -126 for which the largest |key| of the block and head is at most 127 steps (e is
+ * at most 103: keys beyond 127 * 2^103 count as that much; NaN does not count). With W = head_dim rounded up to a multiple
+ * of 16 (channels behind the head: 0):
+ *   codes[layer][slot][KV head][up, down][W], exps[layer][slot][KV head] = e + 127. */
+typedef struct kvt_key_bounds {
+  int8_t *codes;                /* device, 16-byte aligned */
+  uint8_t *exps;                /* device */
+  uint64_t n_slots;
+} kvt_key_bounds;
+
+typedef struct kvt_bound_args {
+  kvt_batch b;                  /* max_q_len is not used */
+  uint32_t layer, dtype;        /* dtype: KVT_KV_*, of the pool */
+  kvt_key_bounds bounds;
+} kvt_bound_args;
+/* Writes the bounds of every block of `layer` that one of the batch's new tokens fills (is the last of): call it behind
+ * kvt_append_kv. Blocks that came into their slots in another way (a reload, an adopted prefix) get bounds by a batch that
+ * counts their tokens as new. Blocks that are not full have no bounds and need none. A slot id of n_slots or more sets the
+ * error word. Errors: KVT_E_INVAL (as kvt_append_kv, head_dim above 256, NULL or misaligned bounds). Asynchronous. */
+int32_t kvt_bound_keys(kvt_engine *e, const kvt_bound_args *a, void *stream);
+
+typedef struct kvt_select_args {
+  kvt_batch b;
+  uint32_t layer, dtype;
+  uint32_t n_q_heads;           /* as in kvt_attend */
+  uint32_t n_blocks;            /* entries of a list */
+  uint32_t first, last;         /* always among them: the first blocks, and the last up to the token's own (last >= 1,
+                                   first + last <= n_blocks) */
+  const void *q;                /* device, rotated queries; strides as in kvt_attend */
+  uint64_t q_ts, q_hs;
+  kvt_key_bounds bounds;
+  int32_t *out;                 /* device, [n_tokens][n_kv_heads][n_blocks] */
+  void *scratch;                /* device, 16-byte aligned, kvt_select_scratch_bytes(e, a) bytes */
+  uint64_t scratch_bytes;
+} kvt_select_args;
+/* For each new token and KV head: the blocks its queries attend to, in ascending order, -1 behind the last. A token whose own
+ * block is among the first n_blocks gets all up to it. Otherwise, of the blocks between the first and the last ones, those of
+ * the largest scores; of equal scores the lower number. With the group's query heads g, u+_d = sum_g max(q_gd, 0) and u-_d =
+ * sum_g max(-q_gd, 0), both rounded to whole steps of 2^f, f the least for which all are at most 255 steps (Inf counts as the
+ * largest finite number, NaN as 0): score = 2^e sum_d u+_d up_d + u-_d down_d, a bound of the sum of the group's products
+ * with any key of the block. It is exact in 32 bits, so the lists do not depend on the batch. A block whose slot is n_slots
+ * or more comes last and sets the error word; one whose bounds were never written (zeros) scores 0. Rows behind
+ * q_start[n_seqs] are not written. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
+int32_t kvt_select_blocks(kvt_engine *e, const kvt_select_args *a, void *stream);
+/* Depends on sizes only. 0 for arguments kvt_select_blocks refuses. */
+uint64_t kvt_select_scratch_bytes(kvt_engine *e, const kvt_select_args *a);
+
+typedef struct kvt_attend_blocks_args {
+  kvt_batch b;                  /* max_q_len is not used */
+  uint32_t layer, dtype;
+  uint32_t n_q_heads;
+  uint32_t n_blocks;            /* entries of a list */
+  float scale;                  /* as in kvt_attend */
+  uint32_t reserved;            /* 0 */
+  const void *q;
+  void *out;
+  float *lse;                   /* optional, [n_tokens][n_q_heads] */
+  uint64_t q_ts, q_hs, o_ts, o_hs;
+  const int32_t *blocks;        /* device, [n_tokens][n_kv_heads][n_blocks] */
+} kvt_attend_blocks_args;
+/* kvt_attend over the keys, up to its own, that lie in the blocks a token's list names; all query heads of a KV head share
+ * its list. Lists may be in any order; entries below 0 and blocks behind the token's own count for nothing; a block that is
+ * listed twice counts twice. A row whose list names no key gives zeros and lse = -inf. Precision as kvt_attend with few rows.
+ * Keys and values that are not named or lie behind the token have no effect, whatever their values. Errors: KVT_E_INVAL.
+ * Asynchronous. */
+int32_t kvt_attend_blocks(kvt_engine *e, const kvt_attend_blocks_args *a, void *stream);
+
+typedef struct kvt_weigh_args {
+  kvt_batch b;
+  uint32_t layer, dtype;
+  uint32_t n_q_heads, flags, window;   /* flags, window, scale: as given to the attention */
+  float scale;
+  float keep;                   /* what the old weights are multiplied with */
+  uint32_t reserved;            /* 0 */
+  const void *q;                /* device, rotated queries */
+  const float *lse;             /* device, [n_tokens][n_q_heads]: what kvt_attend wrote */
+  uint64_t q_ts, q_hs;
+  const float *weights;         /* device, row s at s * w_stride: the old weights, or NULL for none */
+  float *out;                   /* device, row s at s * o_stride, max_blocks each; may be `weights` with its stride */
+  uint64_t w_stride, o_stride;
+  void *scratch;                /* device, 16-byte aligned, kvt_weigh_scratch_bytes(e, a) bytes */
+  uint64_t scratch_bytes;
+} kvt_weigh_args;
+/* Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
+ * keys of block b that the token sees of exp(scale q.k - lse); 0 for blocks behind kv_len[s]. Sums of all layers come from
+ * calls with the same weights, one per layer. Sums are in 32 bits, in an order that is fixed by the sizes and lengths. A row
+ * with lse = -inf adds nothing. Keys a row does not see have no effect. A slot id beyond both pools sets the error word and its
+ * keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
+int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *a, void *stream);
+/* Depends on sizes only. 0 for arguments kvt_weigh_blocks refuses and where none is needed. */
+uint64_t kvt_weigh_scratch_bytes(kvt_engine *e, const kvt_weigh_args *a);
+
+typedef struct kvt_evict_args {
+  uint32_t n_seqs, max_blocks;
+  uint32_t n_blocks;            /* most blocks a sequence keeps */
+  uint32_t first, last;         /* always kept (last >= 1, first + last <= n_blocks) */
+  uint32_t reserved;            /* 0 */
+  const uint32_t *block_table, *kv_len;
+  const float *weights;         /* device, rows of max_blocks */
+  uint64_t table_stride, w_stride;
+  uint32_t *table_out, *kv_len_out;    /* may be block_table / kv_len themselves, with the same stride */
+  float *weights_out;           /* may be `weights` itself, with the same stride */
+  uint32_t *evicted;            /* rows of max_blocks, of its own */
+  uint64_t table_out_stride, w_out_stride, evicted_stride;
+} kvt_evict_args;
+/* Shortens the table rows of sequences that hold more than n_blocks blocks (a partly filled last one counts): of the blocks
+ * between the first and the last ones the heaviest stay, of equal weights the lower numbers; NaN weighs most. table_out and
+ * weights_out: what stays, in order, then ids of 0xFFFFFFFF and zeros; evicted: the slots that left, in order, then
+ * 0xFFFFFFFF; kv_len_out: kv_len less 16 per block that left. Rows of other sequences are copied. The slots are still held by
+ * whoever holds them (kvt_release gives those of the HBM tier back); keys keep the positions they were rotated by, so
+ * kvt_append_kv wants `positions` from here on. Errors: KVT_E_INVAL. Asynchronous. */
+int32_t kvt_evict_blocks(kvt_engine *e, const kvt_evict_args *a, void *stream);
+
 /* The engine gives slots to full, admitted blocks only. KV of a context's last, partly filled block, of blocks that
  * bypassed admission and of tokens still being generated lies in tail blocks: a device buffer of the caller
  * (block-major, 16-byte aligned, bytes / block_bytes blocks) that no tier operation touches. NULL / 0 removes it.

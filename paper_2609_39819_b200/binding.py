@@ -35,7 +35,9 @@ EXPORTS = ("kvt_query_sizes", "kvt_create", "kvt_destroy", "kvt_apply_op", "kvt_
            "kvt_last_error", "kvt_get_entries", "kvt_debug_load_resident", "kvt_set_profiling",
            "kvt_hash_tokens_noalloc", "kvt_debug_set_mover_variant", "kvt_exchange", "kvt_debug_set_lookup_variant", "kvt_move", "kvt_set_mover_ctas",
            "kvt_debug_set_wait_limit", "kvt_debug_set_classify_mode", "kvt_set_l2_residency", "kvt_debug_set_copy_delay",
-           "kvt_append_kv", "kvt_attend", "kvt_attend_scratch_bytes", "kvt_set_tail_pool", "kvt_kv_check")
+           "kvt_append_kv", "kvt_attend", "kvt_attend_scratch_bytes", "kvt_set_tail_pool", "kvt_kv_check", "kvt_bound_keys",
+           "kvt_select_blocks", "kvt_select_scratch_bytes", "kvt_attend_blocks", "kvt_weigh_blocks", "kvt_weigh_scratch_bytes",
+           "kvt_evict_blocks")
 
 
 class KvtError(RuntimeError):
@@ -81,6 +83,40 @@ class AttendArgs(C.Structure):
                [("scale", C.c_float)] + [(n, C.c_void_p) for n in ("q", "out", "lse")] + \
                [(n, C.c_uint64) for n in ("q_ts", "q_hs", "o_ts", "o_hs")] + \
                [("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
+class KeyBoundsArgs(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p), ("n_slots", C.c_uint64)]
+
+
+class BoundArgs(C.Structure):
+    _fields_ = [("b", Batch), ("layer", C.c_uint32), ("dtype", C.c_uint32), ("bounds", KeyBoundsArgs)]
+
+
+class SelectArgs(C.Structure):
+    _fields_ = [("b", Batch)] + [(n, C.c_uint32) for n in ("layer", "dtype", "n_q_heads", "n_blocks", "first", "last")] + \
+               [("q", C.c_void_p), ("q_ts", C.c_uint64), ("q_hs", C.c_uint64), ("bounds", KeyBoundsArgs), ("out", C.c_void_p),
+                ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
+class AttendBlocksArgs(C.Structure):
+    _fields_ = [("b", Batch)] + [(n, C.c_uint32) for n in ("layer", "dtype", "n_q_heads", "n_blocks")] + \
+               [("scale", C.c_float), ("reserved", C.c_uint32)] + [(n, C.c_void_p) for n in ("q", "out", "lse")] + \
+               [(n, C.c_uint64) for n in ("q_ts", "q_hs", "o_ts", "o_hs")] + [("blocks", C.c_void_p)]
+
+
+class WeighArgs(C.Structure):
+    _fields_ = [("b", Batch)] + [(n, C.c_uint32) for n in ("layer", "dtype", "n_q_heads", "flags", "window")] + \
+               [("scale", C.c_float), ("keep", C.c_float), ("reserved", C.c_uint32), ("q", C.c_void_p), ("lse", C.c_void_p),
+                ("q_ts", C.c_uint64), ("q_hs", C.c_uint64), ("weights", C.c_void_p), ("out", C.c_void_p), ("w_stride", C.c_uint64),
+                ("o_stride", C.c_uint64), ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
+class EvictArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("n_seqs", "max_blocks", "n_blocks", "first", "last", "reserved")] + \
+               [(n, C.c_void_p) for n in ("block_table", "kv_len", "weights")] + [("table_stride", C.c_uint64), ("w_stride", C.c_uint64)] + \
+               [(n, C.c_void_p) for n in ("table_out", "kv_len_out", "weights_out", "evicted")] + \
+               [(n, C.c_uint64) for n in ("table_out_stride", "w_out_stride", "evicted_stride")]
 
 
 # the same layouts for struct.pack, which is what a call made thousands of times a second uses
@@ -158,6 +194,11 @@ def load_library():
             "kvt_attend": [vp, vp, vp],
             "kvt_set_tail_pool": [vp, vp, u64],
             "kvt_kv_check": [vp, vp],
+            "kvt_bound_keys": [vp, vp, vp],
+            "kvt_select_blocks": [vp, vp, vp],
+            "kvt_attend_blocks": [vp, vp, vp],
+            "kvt_weigh_blocks": [vp, vp, vp],
+            "kvt_evict_blocks": [vp, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
@@ -165,8 +206,9 @@ def load_library():
             fn.restype = i32
         lib.kvt_hash_scratch_bytes.argtypes = [u64]
         lib.kvt_hash_scratch_bytes.restype = u64
-        lib.kvt_attend_scratch_bytes.argtypes = [vp, vp]
-        lib.kvt_attend_scratch_bytes.restype = u64
+        for name in ("kvt_attend_scratch_bytes", "kvt_select_scratch_bytes", "kvt_weigh_scratch_bytes"):
+            getattr(lib, name).argtypes = [vp, vp]
+            getattr(lib, name).restype = u64
         _lib = lib
     return _lib
 
@@ -279,6 +321,16 @@ class Rope:
                 raise ValueError(f"Rope: axis_of needs {half} axes below 256")
             self.n_axes = len(sections) if sections is not None else max(axis_of, default=0) + 1
             self.axis_of = torch.tensor(axis_of, dtype=torch.uint8).to(device)
+
+
+class KeyBounds:
+    """Bounds of the keys of an engine's full blocks (`Engine.key_bounds` makes them, `Engine.bound_keys` fills them in): int8 codes
+    [layers, slots, KV heads, 2, width] and uint8 exps [layers, slots, KV heads]. In channel d the keys of a block are at most
+    codes[l, s, h, 0, d] * 2 ** (exps[l, s, h] - 127) and at least -codes[l, s, h, 1, d] * 2 ** (...). dtype: that of the pool's
+    elements."""
+
+    def __init__(self, dtype, codes, exps):
+        self.dtype, self.codes, self.exps = dtype, codes, exps
 
 
 class Engine:
@@ -707,8 +759,184 @@ class Engine:
         self._check(self.L.kvt_attend(self.h, a, self._kv_stream()), "attend")
         return out
 
+    # ---- choosing blocks ----------------------------------------------------------------------------
+    def key_bounds(self, dtype):
+        """Room for the bounds of all blocks in the HBM pool and the tail pool of now, for bound_keys and select_blocks. dtype: of
+        the pool's elements, bfloat16 or float16."""
+        torch = self.torch
+        if self.metadata_only or dtype not in self._kv_dtypes or self.elem_bytes != 2:
+            raise ValueError("key_bounds: a pool of bfloat16 or float16 elements expected")
+        n = self.n_hbm_blocks + (self.tail_pool.numel() // self.block_bytes if self.tail_pool is not None else 0)
+        shape = (self.n_layers, n, self.n_kv_heads)
+        return KeyBounds(dtype, torch.zeros(*shape, 2, (self.head_dim + 15) // 16 * 16, dtype=torch.int8, device=self._dev),
+                         torch.zeros(shape, dtype=torch.uint8, device=self._dev))
+
+    def _bounds(self, what, bounds):
+        torch = self.torch
+        codes, exps = bounds.codes, bounds.exps
+        n = codes.shape[1] if codes.dim() == 5 else 0
+        shape = (self.n_layers, n, self.n_kv_heads)
+        if codes.shape != (*shape, 2, (self.head_dim + 15) // 16 * 16) or exps.shape != shape or codes.dtype is not torch.int8 or \
+                exps.dtype is not torch.uint8 or not codes.is_contiguous() or not exps.is_contiguous() or \
+                codes.get_device() != self._dev_index or exps.get_device() != self._dev_index:
+            raise ValueError(f"{what}: bounds are not this engine's (key_bounds() makes them)")
+        return KeyBoundsArgs(codes.data_ptr(), exps.data_ptr(), n)
+
+    def _kv_lse(self, what, lse, t, hq):
+        if lse.dtype is not self.torch.float32 or lse.shape != (t, hq) or lse.get_device() != self._dev_index or not lse.is_contiguous():
+            raise ValueError(f"{what}: lse must be a contiguous float32 [{t}, {hq}] tensor on {self._dev}")
+        if lse.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError(f"{what}: lse requires a gradient, and there is no backward pass; call under torch.no_grad()")
+        return lse.data_ptr()
+
+    def _kv_scale(self, scale):
+        # 0, which is the library's word for the default, becomes next to 0
+        return 0.0 if scale is None else max(float(scale), _FLT_MIN) if scale >= 0 else float(scale)
+
+    def _kv_rows(self, what, x, dtype, shape):
+        """(address, row stride) of a table [rows, elements]."""
+        if x.dtype is not dtype or x.shape != shape or x.get_device() != self._dev_index or (shape[1] > 1 and x.stride(1) != 1):
+            raise ValueError(f"{what}: {dtype} tensor {tuple(shape)} on {self._dev} with consecutive elements expected, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        if x.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError(f"{what}: the tensor requires a gradient, and there is no backward pass; call under torch.no_grad()")
+        return x.data_ptr(), x.stride(0)
+
+    def bound_keys(self, layer, bounds, block_table, q_start, kv_len, n_tokens):
+        """Writes the bounds of the blocks of `layer` that the batch's new tokens fill, from the keys in the pool: call it behind
+        append_kv with the same batch; n_tokens: rows of that batch. After blocks have come into their slots in another way
+        (reload, a prefix that was there), a batch that counts their tokens as new makes their bounds. Asynchronous on the current
+        stream."""
+        if layer < 0 or n_tokens < 0:
+            raise ValueError("bound_keys: layer and n_tokens cannot be negative")
+        batch = self._kv_batch("bound_keys", n_tokens, block_table, q_start, kv_len, 0)
+        a = BoundArgs(Batch(*batch), layer, self._kv_dtypes[bounds.dtype], self._bounds("bound_keys", bounds))
+        self._check(self.L.kvt_bound_keys(self.h, C.byref(a), self._kv_stream()), "bound_keys")
+
+    def select_blocks(self, layer, q, bounds, block_table, q_start, kv_len, n_blocks, first=1, last=2, max_q_len=None, out=None):
+        """For each new token and KV head the numbers of the n_blocks blocks of its sequence that its queries are to attend to: int32
+        [tokens, KV heads, n_blocks], ascending, -1 behind the last. Always among them: the first `first` blocks and the `last` last up
+        to the token's own; the others are those of the largest scores by `bounds` (include/kvt.h says how they are reckoned; they are
+        exact, so that neither the batch nor the kernel has a say). q: rotated queries, batch as in attend; rows behind the last
+        sequence stay as they are. Asynchronous on the current stream."""
+        torch = self.torch
+        if layer < 0 or (max_q_len or 0) < 0 or min(first, last, n_blocks) < 0:
+            raise ValueError("select_blocks: layer, max_q_len, first, last and n_blocks cannot be negative")
+        dt = self._kv_dtype(q, "select_blocks")
+        if q.dtype != bounds.dtype:
+            raise ValueError(f"select_blocks: q is {q.dtype}, the bounds are of {bounds.dtype} keys")
+        t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
+        qp, qts, qhs = self._kv_tensor(q, "select_blocks: q", (t, hq, self.head_dim), q.dtype)
+        shape = (t, self.n_kv_heads, n_blocks)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.int32, device=self._dev)
+        elif out.dtype is not torch.int32 or out.shape != shape or out.get_device() != self._dev_index or not out.is_contiguous():
+            raise ValueError(f"select_blocks: out must be a contiguous int32 {list(shape)} tensor on {self._dev}")
+        batch = self._kv_batch("select_blocks", t, block_table, q_start, kv_len, max_q_len)
+        a = SelectArgs(Batch(*batch), layer, dt, hq, n_blocks, first, last, qp, qts, qhs, self._bounds("select_blocks", bounds),
+                       out.data_ptr(), 0, 0)
+        n = self.L.kvt_select_scratch_bytes(self.h, C.byref(a))
+        scratch = torch.empty(n, dtype=torch.uint8, device=self._dev) if n else None
+        a.scratch, a.scratch_bytes = scratch.data_ptr() if n else None, n
+        self._check(self.L.kvt_select_blocks(self.h, C.byref(a), self._kv_stream()), "select_blocks")
+        return out
+
+    def attend_blocks(self, layer, q, blocks, block_table, q_start, kv_len, scale=None, out=None, lse=None):
+        """attend over the keys, up to each token's own, in the blocks that `blocks` (int32 [tokens, KV heads, n], contiguous, as
+        select_blocks gives them) names for it. Entries below 0 and blocks behind the token's own count for nothing; lists may be in
+        any order, without a block twice. Other arguments, precision and result as in attend."""
+        torch = self.torch
+        if layer < 0:
+            raise ValueError("attend_blocks: layer cannot be negative")
+        dt = self._kv_dtype(q, "attend_blocks")
+        t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
+        qp, qts, qhs = self._kv_tensor(q, "attend_blocks: q", (t, hq, self.head_dim), q.dtype)
+        if blocks.dtype is not torch.int32 or blocks.dim() != 3 or blocks.shape[:2] != (t, self.n_kv_heads) or \
+                blocks.get_device() != self._dev_index or not blocks.is_contiguous():
+            raise ValueError(f"attend_blocks: blocks must be a contiguous int32 [{t}, {self.n_kv_heads}, n] tensor on {self._dev}")
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            op, ots, ohs = out.data_ptr(), hq * d, d
+        else:
+            op, ots, ohs = self._kv_tensor(out, "attend_blocks: out", (t, hq, d), q.dtype)
+            if (ots == 0 and t > 1) or (ohs == 0 and hq > 1):
+                raise ValueError("attend_blocks: out is a broadcast tensor")
+        lsep = self._kv_lse("attend_blocks", lse, t, hq) if lse is not None else 0
+        batch = self._kv_batch("attend_blocks", t, block_table, q_start, kv_len, 0)
+        a = AttendBlocksArgs(Batch(*batch), layer, dt, hq, blocks.shape[2], self._kv_scale(scale), 0, qp, op, lsep, qts, qhs, ots, ohs,
+                             blocks.data_ptr())
+        self._check(self.L.kvt_attend_blocks(self.h, C.byref(a), self._kv_stream()), "attend_blocks")
+        return out
+
+    def weigh_blocks(self, layer, q, lse, block_table, q_start, kv_len, max_q_len=None, causal=True, window=None, scale=None,
+                     weights=None, keep=1.0, out=None):
+        """Attention weight per block, float32 [sequences, blocks of a table row]: keep * weights plus the sum, over the sequence's new
+        tokens, query heads and the block's keys, of the weights exp(scale q k - lse) that attend gave them. q, lse, causal, window
+        and scale are those of that call of attend. weights: from earlier steps or layers (none: zeros); out: written if given, may be
+        `weights`. Blocks behind kv_len get 0. Asynchronous on the current stream."""
+        torch = self.torch
+        if layer < 0 or (max_q_len or 0) < 0 or (window or 0) < 0:
+            raise ValueError("weigh_blocks: layer, max_q_len and window cannot be negative")
+        dt = self._kv_dtype(q, "weigh_blocks")
+        t, hq, d = q.shape if q.dim() == 3 else (0, 0, 0)
+        qp, qts, qhs = self._kv_tensor(q, "weigh_blocks: q", (t, hq, self.head_dim), q.dtype)
+        lsep = self._kv_lse("weigh_blocks", lse, t, hq)
+        batch = self._kv_batch("weigh_blocks", t, block_table, q_start, kv_len, max_q_len)
+        shape = tuple(block_table.shape)
+        wp, ws = self._kv_rows("weigh_blocks: weights", weights, torch.float32, shape) if weights is not None else (0, 0)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=self._dev)
+        op, os_ = self._kv_rows("weigh_blocks: out", out, torch.float32, shape)
+        if os_ < shape[1] and shape[0] > 1:
+            raise ValueError("weigh_blocks: rows of out overlap")
+        if wp == op and ws != os_ and shape[0] > 1:
+            raise ValueError("weigh_blocks: out in the place of weights needs its strides")
+        a = WeighArgs(Batch(*batch), layer, dt, hq, 0 if causal else ATTN_FULL, window or 0, self._kv_scale(scale), keep, 0, qp, lsep, qts,
+                      qhs, wp, op, ws, os_, 0, 0)
+        n = self.L.kvt_weigh_scratch_bytes(self.h, C.byref(a))
+        scratch = torch.empty(n, dtype=torch.uint8, device=self._dev) if n else None
+        a.scratch, a.scratch_bytes = scratch.data_ptr() if n else None, n
+        self._check(self.L.kvt_weigh_blocks(self.h, C.byref(a), self._kv_stream()), "weigh_blocks")
+        return out
+
+    def evict_blocks(self, weights, block_table, kv_len, n_blocks, first=1, last=2, out=None):
+        """Shortens the table rows of sequences that hold more than n_blocks blocks (a partly filled last one counts): the `first` first,
+        the `last` last and the heaviest others stay, in order; of equal weights the lower numbers. Returns (block_table, kv_len,
+        weights, evicted): rows of what stays, then -1 (weights: 0); lengths, 16 per block that left shorter; the slots that left,
+        then -1. out: four tensors to write, of which the first three may be block_table, kv_len and weights themselves. Slots of the
+        HBM tier go back with release(). Keys stay rotated by their old positions: append_kv needs `positions` from here on.
+        Asynchronous on the current stream."""
+        torch = self.torch
+        if min(n_blocks, first, last) < 0:
+            raise ValueError("evict_blocks: n_blocks, first and last cannot be negative")
+        if block_table.dim() != 2:
+            raise ValueError("evict_blocks: block_table [sequences, blocks] expected")
+        shape = tuple(block_table.shape)
+        tp, ts = self._kv_rows("evict_blocks: block_table", block_table, torch.int32, shape)
+        wp, ws = self._kv_rows("evict_blocks: weights", weights, torch.float32, shape)
+        if out is None:
+            out = (torch.empty(shape, dtype=torch.int32, device=self._dev), torch.empty(shape[0], dtype=torch.int32, device=self._dev),
+                   torch.empty(shape, dtype=torch.float32, device=self._dev), torch.empty(shape, dtype=torch.int32, device=self._dev))
+        table_out, len_out, w_out, evicted = out
+        for x in (kv_len, len_out):
+            if x.dtype is not torch.int32 or x.shape != shape[:1] or not x.is_contiguous() or x.get_device() != self._dev_index:
+                raise ValueError(f"evict_blocks: lengths must be a contiguous int32 [{shape[0]}] tensor on {self._dev}")
+        top, tos = self._kv_rows("evict_blocks: out block_table", table_out, torch.int32, shape)
+        wop, wos = self._kv_rows("evict_blocks: out weights", w_out, torch.float32, shape)
+        ep, es = self._kv_rows("evict_blocks: out evicted", evicted, torch.int32, shape)
+        if shape[0] > 1 and min(tos, wos, es) < shape[1]:
+            raise ValueError("evict_blocks: rows of an output overlap")
+        if shape[0] > 1 and ((top == tp and tos != ts) or (wop == wp and wos != ws)):
+            raise ValueError("evict_blocks: an output in the place of an input needs its strides")
+        if evicted.numel() and ep in (tp, wp, top, wop):
+            raise ValueError("evict_blocks: evicted needs a tensor of its own")
+        a = EvictArgs(shape[0], shape[1], n_blocks, first, last, 0, tp, kv_len.data_ptr(), wp, ts, ws, top, len_out.data_ptr(), wop, ep, tos,
+                      wos, es)
+        self._check(self.L.kvt_evict_blocks(self.h, C.byref(a), self._kv_stream()), "evict_blocks")
+        return table_out, len_out, w_out, evicted
+
     def kv_check(self):
-        """Waits for the current stream and raises if append_kv or attend met an id or a length outside its range. What a call
+        """Waits for the current stream and raises if one of the model-side calls met an id or a length outside its range. What a call
         that still runs on another stream meets is raised by this check or the next."""
         self._check(self.L.kvt_kv_check(self.h, self._kv_stream()), "kv_check")
 

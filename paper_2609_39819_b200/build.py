@@ -13,9 +13,11 @@ LIB = os.path.join(_HERE, "libkvt.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 DEFINES: list = []
 HEADER = os.path.join(_HERE, "..", "include", "kvt.h")
-# The kernels of append_kv and attend, most of the compiler's time, have no checked or traced parts: one object for all libraries.
+# The model-side kernels, most of the compiler's time, have no checked or traced parts: one object for all libraries, linked
+# together from those of its sources.
 ATTEND_OBJ = os.path.join(_HERE, "kvt_attend.o")
-ATTEND_DEPS = [os.path.join(CSRC, f) for f in ("kvt_attend.cu", "kvt_attend.h")]
+ATTEND_SOURCES = [os.path.join(CSRC, f) for f in ("kvt_attend.cu", "kvt_blocks.cu")]
+ATTEND_DEPS = ATTEND_SOURCES + [os.path.join(CSRC, f) for f in ("kvt_attend.h", "kvt_attend.cuh")]
 TORCH_SOURCE = "kvt_torch.cpp"
 
 
@@ -77,9 +79,20 @@ def build_lib(force: bool = False, verbose: bool = False, lib: str = LIB, define
     """Compiles libkvt.so if it is missing or older than its sources (several processes may ask at once)."""
     nvcc = [os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")] + NVCC_FLAGS + DEFINES + (["-Xptxas", "-v"] if verbose else [])
 
+    def attend_object(tmp):
+        parts = [f"{tmp}.{i}.o" for i in range(len(ATTEND_SOURCES))]
+        try:
+            with ThreadPoolExecutor(len(parts)) as each:
+                for done in [each.submit(subprocess.check_call, nvcc + ["-c", "-o", part, src]) for part, src in zip(parts, ATTEND_SOURCES)]:
+                    done.result()
+            subprocess.check_call(["ld", "-r", "-o", tmp] + parts)
+        finally:
+            for part in parts:
+                if os.path.exists(part):
+                    os.remove(part)
+
     def attend():
-        return _make(ATTEND_OBJ, lambda: _older(ATTEND_OBJ, ATTEND_DEPS),
-                     lambda tmp: subprocess.check_call(nvcc + ["-c", "-o", tmp, ATTEND_DEPS[0]]), force and lib == LIB)
+        return _make(ATTEND_OBJ, lambda: _older(ATTEND_OBJ, ATTEND_DEPS), attend_object, force and lib == LIB)
 
     def link(tmp):
         engine = tmp + ".engine.o"

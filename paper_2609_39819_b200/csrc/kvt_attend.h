@@ -1,4 +1,4 @@
-// kvt_attend.h — what the entry points in kvt_engine.cu hand to the kernels in kvt_attend.cu.
+// kvt_attend.h — what the entry points in kvt_engine.cu hand to the kernels in kvt_attend.cu and kvt_blocks.cu.
 #pragma once
 #include <cstdint>
 #include <cuda.h>
@@ -69,5 +69,49 @@ cudaError_t launch_take_error(uint32_t *err, uint32_t *out, cudaStream_t s);
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t s, uint32_t *launches);
 // allowed: bits of the kernels whose shared memory has been asked for on this engine's device
 cudaError_t launch_attend(const AttendArgs &a, const AttendPlan &p, const KvMaps &m, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
+
+// ---- choosing blocks (kvt_blocks.cu) ----
+
+// Bounds of one layer's keys: codes [slot][KV head][up, down][width], exps [slot][KV head].
+struct KvBounds { int8_t *codes; uint8_t *exps; uint64_t n_slots; uint32_t width; };
+
+struct BoundArgs { KvBatch b; KvPools p; KvBounds k; uint32_t fp16; uint32_t *err; };
+
+struct SelectArgs {
+  KvBatch b; KvBounds k;
+  const void *q; uint64_t q_ts, q_hs;
+  uint32_t n_kv_heads, head_dim, group, fp16;
+  uint32_t n_blocks, first, last;
+  int32_t *out;
+  uint32_t *scores; uint64_t scores_stride;      // [token of the slab][KV head][scores_stride]
+  uint32_t slab_begin, slab_end;                 // tokens in hand
+  uint32_t *err;
+};
+// Tokens whose scores are held at once, and the scratch they take.
+struct SelectPlan { uint32_t slab, sms; uint64_t scratch_bytes, scores_stride; };
+SelectPlan plan_select(const SelectArgs &a, int sm_count);
+
+struct AttendListArgs { AttendArgs a; const int32_t *blocks; uint32_t n_blocks; };
+
+struct WeighArgs {
+  AttendArgs a;                                  // lse is read
+  const float *weights; float *out;
+  uint64_t w_stride, o_stride;
+  float keep, scale_low;             // scale_log2 + scale_low: the scale in more than 32 bits
+};
+
+struct EvictArgs {
+  const uint32_t *table, *kv_len; const float *weights;
+  uint64_t table_stride, w_stride, table_out_stride, w_out_stride, evicted_stride;
+  uint32_t *table_out, *kv_len_out, *evicted; float *weights_out;
+  uint32_t n_seqs, max_blocks, n_blocks, first, last;
+  uint32_t *err;
+};
+
+cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, uint32_t *launches);
+cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
+cudaError_t launch_attend_blocks(const AttendListArgs &a, const KvMaps &m, int sm_count, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
+cudaError_t launch_weigh(const WeighArgs &a, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
+cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 
 }  // namespace kvt

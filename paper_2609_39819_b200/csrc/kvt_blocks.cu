@@ -1,0 +1,1049 @@
+// kvt_blocks.cu — model-side operators that choose among the blocks of the paged KV pool: bounds of a block's keys, selection of
+// blocks by them, attention over the selected blocks, attention weight per block, eviction by it.
+#include "kvt_attend.cuh"
+
+#include <algorithm>
+
+namespace kvt {
+
+__device__ __forceinline__ u32 max_over_warp(u32 x) { return __reduce_max_sync(~0u, x); }
+__device__ __forceinline__ float sum_over_warp(float x) {
+#pragma unroll
+  for (u32 o = 16; o; o /= 2) x += __shfl_xor_sync(~0u, x, o);
+  return x;
+}
+
+// ======================================================================================================
+// Bounds of a block's keys. For one block and KV head, channel d: up_d = max_r k_rd, down_d = max_r -k_rd over its 16 tokens, both
+// as whole steps of 2^e, rounded up: ceil(x 2^-e), where e is the least with max |k| <= 127 * 2^e. For any query q then
+//   q.k_r <= sum_d max(q_d, 0) up_d + max(-q_d, 0) down_d          for every key of the block.
+// Steps are powers of two so that nothing but the rounding up is rounded, and equal keys get equal codes whoever makes them.
+// Bound by reading the keys once.
+// ======================================================================================================
+constexpr int BOUND_E_MIN = -126, BOUND_E_MAX = 103;     // 2^24 steps of 2^103 are a 32-bit number
+__device__ __forceinline__ int bound_exponent(float most) {
+  const u32 b = __float_as_uint(most);
+  const int e = (int)(b >> 23) - 127 - 6 + ((b & 0x7FFFFF) > 0x7E0000);      // 127 = 1.984375 * 2^6
+  return max(BOUND_E_MIN, min(BOUND_E_MAX, b >> 23 ? e : BOUND_E_MIN));
+}
+__device__ __forceinline__ int bound_code(float x, float inv) {
+  float c = fminf(ceilf(x * inv), 127.0f);
+  if (x > 0.0f) c = fmaxf(c, 1.0f);                      // the product may have vanished
+  return (int)fmaxf(c, -127.0f);
+}
+__device__ __forceinline__ float number(float x) { return x == x ? x : 0.0f; }       // a NaN does not count
+
+template <class T> struct Pair;
+template <> struct Pair<__nv_bfloat16> { typedef __nv_bfloat162 T2; };
+template <> struct Pair<__half> { typedef __half2 T2; };
+
+// A CTA looks at 16 tokens; a warp takes a head of a block that one of them fills. VEC: heads of D channels, 16 bytes of a token
+// per lane, all loads of a lane in flight at once.
+template <class T, u32 D>
+__global__ void __launch_bounds__(256) k_bound_keys(BoundArgs a) {
+  __shared__ u32 s_slot[16];
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.p.n_kv_heads;
+  for (u32 i = warp; i < 16; i += 8) {
+    const u32 t = blockIdx.x * 16 + i;
+    u32 slot = ~0u;
+    if (t < a.b.n_tokens) {
+      const Where w = find_token<true>(a.b, t, a.err);
+      if (w.seq < a.b.n_seqs && w.ok && w.index % BT == BT - 1) {
+        slot = a.b.table[w.seq * a.b.table_stride + w.index / BT];
+        if (slot >= a.k.n_slots || !slot_ptr(a.p, a.p.k, slot)) { if (lane == 0) kv_err(a.err, KVERR_RANGE); slot = ~0u; }
+      }
+    }
+    if (lane == 0) s_slot[i] = slot;
+  }
+  __syncthreads();
+  const u32 slots = s_slot[lane % 16], filled = __ballot_sync(~0u, lane < 16 && slots != ~0u), n_items = __popc(filled) * H;
+  for (u32 item = blockIdx.y * 8 + warp; item < n_items; item += 8 * gridDim.y) {
+    const u32 which = item / H, h = item - which * H, slot = __shfl_sync(~0u, slots, __fns(filled, 0, which + 1));
+    const u16 *const src = (const u16 *)slot_ptr(a.p, a.p.k, slot);
+    int8_t *const to = a.k.codes + ((u64)slot * H + h) * 2 * a.k.width;
+    u8 *const exp_to = a.k.exps + (u64)slot * H + h;
+    if constexpr (D != 0) {
+      typedef typename Pair<T>::T2 T2;
+      constexpr u32 LANES = D / 8, PER = 32 / LANES, STEPS = BT / PER;       // lanes of a token, tokens of a load, loads
+      const u32 c = lane % LANES * 8;
+      uint4 v[STEPS];
+#pragma unroll
+      for (u32 y = 0; y < STEPS; ++y) v[y] = *(const uint4 *)(src + (u64)(y * PER + lane / LANES) * H * D + h * D + c);
+      T2 hi[4], lo[4];
+#pragma unroll
+      for (u32 z = 0; z < 4; ++z) {
+        auto part = [&](u32 y) { u32 x = z == 0 ? v[y].x : z == 1 ? v[y].y : z == 2 ? v[y].z : v[y].w; return *reinterpret_cast<T2 *>(&x); };
+        hi[z] = lo[z] = part(0);
+#pragma unroll
+        for (u32 y = 1; y < STEPS; ++y) { hi[z] = __hmax2(hi[z], part(y)); lo[z] = __hmin2(lo[z], part(y)); }
+#pragma unroll
+        for (u32 o = LANES; o < 32; o *= 2) {
+          hi[z] = __hmax2(hi[z], __shfl_xor_sync(~0u, hi[z], o));
+          lo[z] = __hmin2(lo[z], __shfl_xor_sync(~0u, lo[z], o));
+        }
+      }
+      float up[8], down[8], most = 0.0f;
+#pragma unroll
+      for (u32 z = 0; z < 4; ++z) {
+        const float2 x = Elem<T>::up(*reinterpret_cast<u32 *>(&hi[z])), y = Elem<T>::up(*reinterpret_cast<u32 *>(&lo[z]));
+        up[2 * z] = number(x.x); up[2 * z + 1] = number(x.y); down[2 * z] = -number(y.x); down[2 * z + 1] = -number(y.y);
+      }
+#pragma unroll
+      for (u32 z = 0; z < 8; ++z) most = fmaxf(most, fmaxf(fabsf(up[z]), fabsf(down[z])));
+      const int e = bound_exponent(__uint_as_float(max_over_warp(__float_as_uint(most))));
+      const float inv = __uint_as_float((u32)(127 - e) << 23);
+      u32 x[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (u32 z = 0; z < 8; ++z) {
+        x[z / 4] |= (u32)(bound_code(up[z], inv) & 0xFF) << (z % 4 * 8);
+        x[2 + z / 4] |= (u32)(bound_code(down[z], inv) & 0xFF) << (z % 4 * 8);
+      }
+      if (lane < LANES) {
+        *(uint2 *)(to + c) = make_uint2(x[0], x[1]);
+        *(uint2 *)(to + D + c) = make_uint2(x[2], x[3]);
+      }
+      if (lane == 0) *exp_to = (u8)(e + 127);
+    } else {
+      const u32 d = a.p.head_dim;
+      float up[8], down[8], most = 0.0f;
+#pragma unroll
+      for (u32 z = 0; z < 8; ++z) {
+        const u32 c = lane + 32 * z;
+        float hi = -INFINITY, lo = INFINITY;
+        if (c < d) for (u32 r = 0; r < BT; ++r) {
+          const float x = Elem<T>::up1(((const T *)src)[(u64)r * H * d + (u64)h * d + c]);
+          hi = fmaxf(hi, x); lo = fminf(lo, x);          // neither takes a NaN
+        }
+        up[z] = hi < lo || c >= d ? 0.0f : hi; down[z] = hi < lo || c >= d ? 0.0f : -lo;
+        most = fmaxf(most, fmaxf(fabsf(up[z]), fabsf(down[z])));
+      }
+      const int e = bound_exponent(__uint_as_float(max_over_warp(__float_as_uint(most))));
+      const float inv = __uint_as_float((u32)(127 - e) << 23);
+#pragma unroll
+      for (u32 z = 0; z < 8; ++z) {
+        const u32 c = lane + 32 * z;
+        if (c < a.k.width) { to[c] = (int8_t)bound_code(up[z], inv); to[a.k.width + c] = (int8_t)bound_code(down[z], inv); }
+      }
+      if (lane == 0) *exp_to = (u8)(e + 127);
+    }
+  }
+}
+
+template <class T>
+static void bound_keys(const BoundArgs &a, dim3 grid, cudaStream_t s) {
+  const bool aligned = (((uintptr_t)a.p.k.base | (uintptr_t)a.p.k.tail) & 15) == 0;
+  if (aligned && a.p.head_dim == 128) k_bound_keys<T, 128><<<grid, 256, 0, s>>>(a);
+  else if (aligned && a.p.head_dim == 64) k_bound_keys<T, 64><<<grid, 256, 0, s>>>(a);
+  else k_bound_keys<T, 0><<<grid, 256, 0, s>>>(a);
+}
+cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, u32 *launches) {
+  const u32 ctas = (a.b.n_tokens + 15) / 16;
+  const dim3 grid(ctas, std::max(1u, std::min(a.p.n_kv_heads, 2u * sm_count / ctas)));
+  ++*launches;
+  if (a.fp16) bound_keys<__half>(a, grid, s);
+  else bound_keys<__nv_bfloat16>(a, grid, s);
+  return cudaGetLastError();
+}
+
+// ======================================================================================================
+// The m-th largest of n keys, for a whole CTA, by digits of 8 bits from the top of what tells the smallest from the largest.
+// A key x is among the m largest if x > at, or x == at and fewer than `ties` keys equal to it come before.
+// ======================================================================================================
+struct Kth { u32 at, ties; };
+template <u32 THREADS, class Key>
+__device__ __forceinline__ Kth kth_largest(Key key, u32 n, u32 m) {
+  __shared__ u32 s_hist[256], s_lo, s_hi, s_digit, s_left, s_all;
+  const u32 tid = threadIdx.x, lane = tid & 31;
+  if (m >= n) return Kth{0, ~0u};                        // all: no key is below 0
+  if (tid == 0) { s_lo = ~0u; s_hi = 0; }
+  __syncthreads();
+  u32 lo = ~0u, hi = 0;
+  for (u32 i = tid; i < n; i += THREADS) { const u32 x = key(i); lo = min(lo, x); hi = max(hi, x); }
+  lo = __reduce_min_sync(~0u, lo); hi = __reduce_max_sync(~0u, hi);
+  if (lane == 0) { atomicMin(&s_lo, lo); atomicMax(&s_hi, hi); }
+  __syncthreads();
+  lo = s_lo; hi = s_hi;
+  u32 bits = 32 - __clz(hi - lo), prefix = 0, left = m;  // prefix: the digits above `bits` of the key in question
+  while (bits) {
+    const u32 shift = bits > 8 ? bits - 8 : 0, width = bits - shift;
+    for (u32 i = tid; i < 256; i += THREADS) s_hist[i] = 0;
+    __syncthreads();
+    for (u32 i = tid; i < n; i += THREADS) {
+      const u32 x = key(i) - lo;
+      if ((u64)x >> bits == prefix) atomicAdd(&s_hist[x >> shift & ((1u << width) - 1)], 1u);
+    }
+    __syncthreads();
+    if (tid < 32) {                                      // lane l: digits 255 - 8 l downwards
+      u32 c[8], sum = 0;
+#pragma unroll
+      for (u32 y = 0; y < 8; ++y) { c[y] = s_hist[255 - 8 * lane - y]; sum += c[y]; }
+      u32 incl = sum;
+#pragma unroll
+      for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
+      u32 before = incl - sum;
+      if (before < left && left <= incl) {
+        u32 y = 0;
+#pragma unroll
+        for (u32 z = 0; z < 7; ++z) if (y == z && before + c[z] < left) { before += c[z]; ++y; }
+        u32 here = c[0];
+#pragma unroll
+        for (u32 z = 1; z < 8; ++z) if (y == z) here = c[z];
+        s_digit = 255 - 8 * lane - y; s_left = left - before; s_all = here == left - before;
+      }
+    }
+    __syncthreads();
+    prefix = prefix << width | s_digit;
+    left = s_left;
+    bits = shift;
+    if (s_all) return Kth{lo + (prefix << bits), ~0u};   // all that begin like this
+    // (the barriers of the next round stand between these reads and the next writes)
+  }
+  return Kth{lo + prefix, left};
+}
+
+// Deals the numbers i of [0, n) out in order: pick(i) says which list each goes to (bit 0: the first, bit 1: the second), put(i, which, place)
+// is called with its place in that list. Every warp has a stretch of its own.
+template <u32 THREADS, class Pick, class Put>
+__device__ __forceinline__ void deal(u32 n, Pick pick, Put put) {
+  constexpr u32 WARPS = THREADS / 32;
+  __shared__ u32 s_n[WARPS][2];
+  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (n + THREADS - 1) / THREADS * 32;
+  const u32 from = min(n, warp * per), to = min(n, from + per);
+  u32 count[2] = {0, 0};
+  for (u32 i = from; i < to; i += 32) {
+    const u32 w = i + lane < to ? pick(i + lane) : 0;
+    count[0] += __popc(__ballot_sync(~0u, w & 1)); count[1] += __popc(__ballot_sync(~0u, w & 2));
+  }
+  __syncthreads();
+  if (lane == 0) { s_n[warp][0] = count[0]; s_n[warp][1] = count[1]; }
+  __syncthreads();
+  u32 at[2] = {0, 0};
+  for (u32 w = 0; w < warp; ++w) { at[0] += s_n[w][0]; at[1] += s_n[w][1]; }
+  for (u32 i = from; i < to; i += 32) {
+    const u32 w = i + lane < to ? pick(i + lane) : 0;
+    const u32 b0 = __ballot_sync(~0u, w & 1), b1 = __ballot_sync(~0u, w & 2), below = (1u << lane) - 1;
+    if (w & 1) put(i + lane, 0u, at[0] + __popc(b0 & below));
+    if (w & 2) put(i + lane, 1u, at[1] + __popc(b1 & below));
+    at[0] += __popc(b0); at[1] += __popc(b1);
+  }
+}
+
+// Order of floating numbers as order of whole ones.
+__device__ __forceinline__ u32 ordered(float x) {
+  const u32 b = __float_as_uint(x);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// ======================================================================================================
+// Selection of blocks. The group's queries of a token and KV head are added up, what is above zero and what is below apart, and
+// rounded to 8 bits without sign: u = rint(2^-f sum), f the least with max <= 255 * 2^f. With the bounds (up, down, e) of a block
+//   score = 2^e sum_d u+_d up_d + u-_d down_d,
+// the sum over the group's heads of what bounds their products with any key of the block (in steps of 2^f, which all blocks of the
+// query share). The sum is of at most 512 products of 255 * 127, a whole number below 2^24, so it is a 32-bit floating number
+// exactly, and so is the score: all kernels, batches and orders of summation give the same selection, bit by bit.
+// ======================================================================================================
+// New tokens [t0, t0 + n) of a sequence that lie among the tokens in hand; index of the first in its sequence.
+struct Part { u32 t0, n; long long index; };
+__device__ __forceinline__ Part part_of(const SelectArgs &a, u32 s) {
+  const Seq q = load_seq(a.b, s, a.err);
+  Part p;
+  p.t0 = max(q.t0, a.slab_begin);
+  const u32 end = min(q.t0 + q.n, a.slab_end);
+  p.n = end > p.t0 ? end - p.t0 : 0;
+  p.index = (long long)q.kv - q.n + (p.t0 - q.t0);
+  return p;
+}
+
+__device__ __forceinline__ void mma_u8s8(int (&c)[4], u32 a0, u32 a1, u32 a2, u32 a3, u32 b0, u32 b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Scores of 16 tokens of one sequence with one KV head's share of the blocks. blockIdx.x: tile of tokens, y: KV head, z: share of the
+// blocks. A warp takes 8 blocks at a time: a lane 16 bytes of every 64 of a block's codes, which are the operand of the matrix
+// instruction if the channels are counted in that order on both sides.
+template <class T, u32 G>      // G: 64-byte parts of (up, down)
+__global__ void __launch_bounds__(256) k_score_blocks(SelectArgs a, u32 shares) {
+  constexpr u32 ROW = G * 64 + 16;
+  __shared__ __align__(16) u8 su[16 * ROW];
+  __shared__ u64 s_sum[8];
+  __shared__ u32 s_seq, s_tile;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, H = a.n_kv_heads, W = a.k.width;
+  // the tile's sequence
+  if (tid == 0) s_seq = ~0u;
+  u32 base = 0;
+  for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += 256) {
+    const u32 n = s0 + tid < a.b.n_seqs ? (part_of(a, s0 + tid).n + 15) / 16 : 0;
+    u32 incl = n;
+#pragma unroll
+    for (u32 o = 1; o < 32; o *= 2) { const u32 y = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += y; }
+    __syncthreads();
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    u32 before = base, all = base;
+#pragma unroll
+    for (u32 w = 0; w < 8; ++w) { if (w < warp) before += (u32)s_sum[w]; all += (u32)s_sum[w]; }
+    if (blockIdx.x >= before + incl - n && blockIdx.x < before + incl) { s_seq = s0 + tid; s_tile = blockIdx.x - (before + incl - n); }
+    base = all;
+  }
+  __syncthreads();
+  const u32 seq = s_seq;
+  if (seq == ~0u) return;
+  Part p = part_of(a, seq);
+  p.t0 += s_tile * 16; p.index += s_tile * 16; p.n = min(16u, p.n - s_tile * 16);
+  // blocks that any of the tokens may choose from: [first, its own - last]; scored from a multiple of 8 on
+  const long long own = (p.index + p.n - 1) / BT;
+  const long long end_ = p.index + p.n - 1 < 0 ? 0 : min(own + 1 - (long long)a.last, (long long)a.b.max_blocks);
+  const u32 begin = a.first & ~7u, end = end_ > (long long)begin ? (u32)end_ : begin;
+  const u32 per = ((end - begin + shares - 1) / shares + 63) / 64 * 64;
+  const u32 b0 = begin + min(end - begin, blockIdx.z * per), b1 = begin + min(end - begin, (blockIdx.z + 1) * per);
+  if (b0 >= b1 || own + 1 <= (long long)a.n_blocks) return;       // nobody chooses
+
+  // queries: two tokens per warp
+  for (u32 r = warp; r < 16; r += 8) {
+    double up[8], down[8], most = 0.0;
+#pragma unroll
+    for (u32 z = 0; z < 8; ++z) {
+      const u32 c = lane + 32 * z;
+      up[z] = down[z] = 0.0;
+      if (z * 32 < G * 32 && c < a.head_dim && r < p.n)
+        for (u32 y = 0; y < a.group; ++y) {
+          float x = number(Elem<T>::up1(((const T *)a.q)[(u64)(p.t0 + r) * a.q_ts + (u64)(h * a.group + y) * a.q_hs + c]));
+          const float top = __is_same(T, __half) ? 65504.0f : 3.3895314e38f;       // Inf counts as the largest number
+          x = fminf(fmaxf(x, -top), top);
+          if (x > 0.0f) up[z] += (double)x; else down[z] -= (double)x;
+        }
+      most = fmax(most, fmax(up[z], down[z]));
+    }
+#pragma unroll
+    for (u32 o = 16; o; o /= 2) most = fmax(most, __shfl_xor_sync(~0u, most, o));
+    const u64 bits = (u64)__double_as_longlong(most);
+    const int f = most > 0.0 ? (int)(bits >> 52) - 1023 - 7 + ((bits & 0xFFFFFFFFFFFFFull) > 0xFE00000000000ull) : 0;     // 255 = 1.9921875 * 2^7
+    const double inv = __longlong_as_double((u64)(1023 - f) << 52);
+#pragma unroll
+    for (u32 z = 0; z < 8; ++z) {
+      const u32 c = lane + 32 * z;
+      if (z * 32 < G * 32 && c < W) { su[r * ROW + c] = (u8)__double2uint_rn(up[z] * inv); su[r * ROW + W + c] = (u8)__double2uint_rn(down[z] * inv); }
+    }
+    for (u32 c = 2 * W + lane; c < G * 64; c += 32) su[r * ROW + c] = 0;
+  }
+  __syncthreads();
+  uint4 qa[G][2];
+  const u32 j = lane % 4, r = lane / 4;
+#pragma unroll
+  for (u32 g = 0; g < G; ++g) {
+    qa[g][0] = *(const uint4 *)(su + r * ROW + g * 64 + j * 16);
+    qa[g][1] = *(const uint4 *)(su + (r + 8) * ROW + g * 64 + j * 16);
+  }
+  const u32 *const table = a.b.table + seq * a.b.table_stride;
+  u32 *const out = a.scores + ((u64)(p.t0 - a.slab_begin) * H + h) * a.scores_stride;
+  const u64 token = (u64)H * a.scores_stride;
+  auto slot_of = [&](u32 b) { return b + r < b1 ? table[b + r] : ~0u; };
+  struct Codes { uint4 v[G]; u32 e; };
+  auto load = [&](u32 b, u32 slot) {
+    Codes x;
+    const bool fine = slot < a.k.n_slots;
+    if (!fine && b + r < b1 && j == 0) kv_err(a.err, KVERR_RANGE);
+    const int8_t *const src = a.k.codes + ((fine ? (u64)slot : 0ull) * H + h) * 2 * W + j * 16;
+#pragma unroll
+    for (u32 g = 0; g < G; ++g)
+      x.v[g] = fine && g * 64 + j * 16 < 2 * W ? *(const uint4 *)(src + g * 64) : make_uint4(0, 0, 0, 0);
+    x.e = fine ? a.k.exps[(u64)slot * H + h] : 256;
+    return x;
+  };
+  u32 b = b0 + warp * 8;
+  if (b >= b1) return;
+  u32 next_slot = slot_of(b + 64);
+  Codes now = load(b, slot_of(b));
+  for (; b < b1; b += 64) {
+    Codes next;
+    if (b + 64 < b1) { next = load(b + 64, next_slot); next_slot = b + 128 < b1 ? slot_of(b + 128) : ~0u; }
+    int c[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (u32 g = 0; g < G; ++g) {
+      mma_u8s8(c, qa[g][0].x, qa[g][1].x, qa[g][0].y, qa[g][1].y, now.v[g].x, now.v[g].y);
+      mma_u8s8(c, qa[g][0].z, qa[g][1].z, qa[g][0].w, qa[g][1].w, now.v[g].z, now.v[g].w);
+    }
+    // this lane's scores: tokens r and r + 8, blocks b + 2 j and b + 2 j + 1, whose exponents lanes 8 j and 8 j + 4 hold
+    const u32 e0 = __shfl_sync(~0u, now.e, 8 * j), e1 = __shfl_sync(~0u, now.e, 8 * j + 4);
+    auto score = [](int sum, u32 e) { return e > 255 ? 0u : ordered(fmaf((float)sum, __uint_as_float(e << 23), 0.0f)); };     // no slot: last of all
+#pragma unroll
+    for (u32 y = 0; y < 2; ++y)
+      if (r + 8 * y < p.n) *(uint2 *)(out + (r + 8 * y) * token + b + 2 * j) = make_uint2(score(c[2 * y], e0), score(c[2 * y + 1], e1));
+    now = next;
+  }
+}
+
+// The blocks of a token and KV head, in order: the first ones, those of the largest scores, the last ones.
+template <u32 THREADS>
+__global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held) {
+  extern __shared__ u32 s_keys[];
+  const u32 tid = threadIdx.x, H = a.n_kv_heads, t = a.slab_begin + blockIdx.x / H, h = blockIdx.x % H;
+  const Where w = find_token<false>(a.b, t, a.err);
+  if (w.seq >= a.b.n_seqs) return;                       // behind the last sequence
+  int32_t *const out = a.out + ((u64)t * H + h) * a.n_blocks;
+  const u32 own = w.index / BT;
+  if (!w.ok || own < a.n_blocks) {                       // all there are
+    for (u32 i = tid; i < a.n_blocks; i += THREADS) out[i] = w.ok && i <= own ? (int32_t)i : -1;
+    return;
+  }
+  const u32 n = own + 1 - a.first - a.last, m = a.n_blocks - a.first - a.last;
+  const u32 *const scores = a.scores + ((u64)(t - a.slab_begin) * H + h) * a.scores_stride + a.first;
+  for (u32 i = tid; i < a.first + a.last; i += THREADS) out[i < a.first ? i : i + m] = i < a.first ? i : (int32_t)(own + 1 - a.last + i - a.first);
+  if (n <= held) for (u32 i = tid; i < n; i += THREADS) s_keys[i] = scores[i];
+  __syncthreads();
+  if (!m) return;
+  const u32 *const keys = n <= held ? s_keys : scores;
+  const Kth kth = kth_largest<THREADS>([&](u32 i) { return keys[i]; }, n, m);
+  __syncthreads();
+  // keys equal to the last one that is taken: the first `ties` of them. Both lists in one go where all of them are taken.
+  if (kth.ties == ~0u) {
+    deal<THREADS>(n, [&](u32 i) { return keys[i] >= kth.at ? 1u : 0u; }, [&](u32 i, u32, u32 at) { out[a.first + at] = (int32_t)(a.first + i); });
+    return;
+  }
+  __shared__ u32 s_border;                               // number of the last tie that is taken
+  deal<THREADS>(n, [&](u32 i) { return keys[i] == kth.at ? 1u : 0u; }, [&](u32 i, u32, u32 at) { if (at == kth.ties - 1) s_border = i; });
+  __syncthreads();
+  const u32 border = s_border;
+  deal<THREADS>(n, [&](u32 i) { return keys[i] > kth.at || (keys[i] == kth.at && i <= border) ? 1u : 0u; },
+                [&](u32 i, u32, u32 at) { out[a.first + at] = (int32_t)(a.first + i); });
+}
+
+constexpr u64 SLAB_BYTES = 64ull << 20;                  // scores that are in hand together: they stay in the L2 cache
+SelectPlan plan_select(const SelectArgs &a, int sm_count) {
+  SelectPlan p{};
+  p.sms = sm_count;
+  p.scores_stride = ((u64)a.b.max_blocks + 7) / 8 * 8;
+  const u64 token = p.scores_stride * a.n_kv_heads * 4;
+  p.slab = (u32)std::min<u64>(a.b.n_tokens, std::max<u64>(1, SLAB_BYTES / token));
+  p.scratch_bytes = p.slab * token;
+  return p;
+}
+
+template <class T>
+static void score_blocks(const SelectArgs &a, dim3 grid, u32 shares, cudaStream_t s) {
+  if (a.k.width <= 64) k_score_blocks<T, 2><<<grid, 256, 0, s>>>(a, shares);
+  else if (a.k.width <= 128) k_score_blocks<T, 4><<<grid, 256, 0, s>>>(a, shares);
+  else k_score_blocks<T, 8><<<grid, 256, 0, s>>>(a, shares);
+}
+template <u32 THREADS>
+static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, u32 held, u32 which, cudaStream_t s, u64 *allowed) {
+  const cudaError_t r = allow_smem(k_pick_blocks<THREADS>, which, 200 * 1024, allowed);
+  if (r != cudaSuccess) return r;
+  k_pick_blocks<THREADS><<<rows, THREADS, held * 4, s>>>(a, held);
+  return cudaGetLastError();
+}
+cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, u64 *allowed, u32 *launches) {
+  a.scores_stride = p.scores_stride;
+  const u32 held = (u32)std::min<u64>(a.b.max_blocks, 50 * 1024);        // keys in shared memory
+  for (u32 t = 0; t < a.b.n_tokens; t += p.slab) {
+    a.slab_begin = t; a.slab_end = std::min(a.b.n_tokens, t + p.slab);
+    const u32 n = a.slab_end - t;
+    const u32 tiles = (u32)(((u64)n + 15ull * std::min(a.b.n_seqs, n)) / 16);
+    if (a.b.max_blocks > a.n_blocks) {
+      const u32 shares = std::max(1u, std::min((a.b.max_blocks + 63) / 64, 4 * p.sms / std::max(1u, tiles * a.n_kv_heads)));
+      const dim3 grid(tiles, a.n_kv_heads, shares);
+      if (a.fp16) score_blocks<__half>(a, grid, shares, s); else score_blocks<__nv_bfloat16>(a, grid, shares, s);
+      ++*launches;
+      const cudaError_t r = cudaGetLastError();
+      if (r != cudaSuccess) return r;
+    }
+    const u32 rows = n * a.n_kv_heads;
+    const cudaError_t r = rows < 2 * p.sms && a.b.max_blocks > 2048 ? pick_blocks<1024>(a, rows, held, 0, s, allowed)
+                                                                     : pick_blocks<256>(a, rows, held, 1, s, allowed);
+    ++*launches;
+    if (r != cudaSuccess) return r;
+  }
+  return cudaSuccess;
+}
+
+// ======================================================================================================
+// Attention over listed blocks: softmax(scale q k^T) v of one token's group of query heads over the keys up to its own in the blocks
+// its list names. A unit is a token and KV head (and 8 or 16 query heads); its blocks are dealt out to the four warps of a CTA, or
+// of a cluster of them, each with a ring of loads of its own, and joined like the parts of a longer sequence.
+// The queries are the narrow side of the products, 8 columns: S^T = K Q^T has the block's 16 keys as rows, O^T = V^T P^T 16 channels.
+// ======================================================================================================
+constexpr u32 LIST_WARPS = 4, LIST_THREADS = LIST_WARPS * 32;
+template <u32 D> struct ListShape {
+  static constexpr u32 BLOCK = BT * D * 2, STAGES = D == 64 ? 6 : 3, RING = STAGES * 2 * BLOCK, SMEM = LIST_WARPS * RING + 1024, LD = D + 4;
+};
+__device__ __forceinline__ u32 transposed(u32 x) {       // an 8 x 8 matrix of 16-bit numbers, two per lane
+  u32 y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// The blocks at list places part, part + parts, ... below n for the columns of a unit, into o, m, l (see k_attend_blocks). A lane has
+// columns n * 8 + 2 (lane % 4) and the next, keys / channels lane / 4 and 8 further. DOUBLE: columns 4 to 7 are those 0 to 3 once
+// more and take the second numbers of the powers.
+template <class T, u32 D, u32 NT, bool DOUBLE, bool ANY>
+__device__ __forceinline__ bool list_keys(const AttendListArgs &x, const KvMaps &maps, const u32 *table, const int32_t *list, u32 n, u32 index, u32 h,
+                                          const u16 *const (&q)[NT], u32 part, u32 parts, u32 ring, u32 bar0, u32 *s_block,
+                                          float (&o)[D / 16][NT][4], float (&m)[NT][2], float (&l)[NT][2]) {
+  typedef ListShape<D> S;
+  const AttendArgs &a = x.a;
+  const u32 lane = threadIdx.x & 31, own = index / BT;
+  const u32 n_mine = part < n ? (n - part + parts - 1) / parts : 0;
+  u32 held_slot = 0, held_block = 0;
+  auto load = [&](u32 i) {
+    if (i % 32 == 0) {
+      held_block = i + lane < n_mine ? (u32)list[part + (i + lane) * parts] : ~0u;
+      held_slot = ~0u;
+      if (held_block <= own) {
+        held_slot = table[held_block];
+        if (held_slot >= a.p.n_slots && held_slot - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+      }
+    }
+    const u32 slot = __shfl_sync(~0u, held_slot, i % 32), block = __shfl_sync(~0u, held_block, i % 32);
+    const u32 st = i % S::STAGES, dst = ring + st * 2 * S::BLOCK;
+    if (lane == 0) s_block[st] = block;
+    if (ANY) {
+      copy_block<D>(a, a.p.k, slot, h, dst);
+      copy_block<D>(a, a.p.v, slot, h, dst + S::BLOCK);
+    } else if (lane == 0) {
+      const u32 bar = bar0 + st * 8;
+      bar_expect(bar, 2 * S::BLOCK);
+      load_block(a, maps, dst, bar, slot, 2 * a.layer, h, D / 64);
+      load_block(a, maps, dst + S::BLOCK, bar, slot, 2 * a.layer + 1, h, D / 64);
+    }
+  };
+  if (ANY) {
+    const u32 c = (a.p.head_dim + 7) / 8;
+    if (c < D / 8)
+      for (u32 i = lane; i < S::STAGES * 2 * BT * (D / 8 - c); i += 32) {
+        const u32 r = i / (D / 8 - c);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + r / BT * S::BLOCK + block_off<D>(r % BT, c + i % (D / 8 - c))), "r"(0) : "memory");
+      }
+  }
+#pragma unroll 1
+  for (u32 i = 0; i < S::STAGES; ++i) {
+    if (i < n_mine) load(i);
+    if (ANY) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // queries: column lane / 4 of every eight, the second operand
+  u32 qf[NT][D / 16][2];
+#pragma unroll
+  for (u32 c = 0; c < NT; ++c) {
+    const u16 *const src = q[c] + lane % 4 * 2;
+    const bool even = ((uintptr_t)src & 3) == 0;
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (u32 z = 0; z < 2; ++z) {
+        const u16 *const p = src + k * 16 + z * 8;
+        if (ANY) {
+          const u32 d = lane % 4 * 2 + k * 16 + z * 8;
+          qf[c][k][z] = (d < a.p.head_dim ? (u32)p[0] : 0u) | (d + 1 < a.p.head_dim ? (u32)p[1] << 16 : 0u);
+        } else {
+          qf[c][k][z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+        }
+      }
+  }
+#pragma unroll
+  for (u32 c = 0; c < NT; ++c) {
+    m[c][0] = m[c][1] = -INFINITY; l[c][0] = l[c][1] = 0.0f;
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) o[k][c][y] = 0.0f;
+  }
+  bool ok = true;
+  for (u32 i = 0; i < n_mine; ++i) {
+    const u32 st = i % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
+    if (ANY) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
+      __syncwarp();
+    } else if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, i / S::STAGES & 1)))) break;
+    const u32 block = s_block[st];
+    float s[NT][4];
+#pragma unroll
+    for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) s[c][y] = 0.0f;
+#pragma unroll
+    for (u32 k = 0; k < D / 16; ++k) {
+      u32 f[4];
+      ldm4(f, kb + block_off<D>(lane % 16, 2 * k + lane / 16));
+#pragma unroll
+      for (u32 c = 0; c < NT; ++c) mma16816<T>(s[c], f, qf[c][k][0], qf[c][k][1]);
+    }
+#pragma unroll
+    for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) s[c][y] *= a.scale_log2;
+    if (block >= own) {                  // the token's own block, or no block of its
+      const u32 seen = block == own ? index % BT + 1 : 0;
+#pragma unroll
+      for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) if (lane / 4 + 8 * (y / 2) >= seen) s[c][y] = -INFINITY;
+      // values behind the token: weight 0 must not meet an Inf or a NaN
+      const u32 r = lane / 2;
+      if (r >= seen)
+#pragma unroll
+        for (u32 c = 0; c < D / 16; ++c)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + block_off<D>(r, (lane % 2) * (D / 16) + c)), "r"(0) : "memory");
+      if (!ANY) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // a load writes here next
+      __syncwarp();
+    }
+    float top[NT][2];
+    bool move = false;
+#pragma unroll
+    for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y) {
+        top[c][y] = fmaxf(s[c][y], s[c][y + 2]);
+        if (Elem<T>::LOW > -INFINITY) {  // the largest may be too small, too: all of the column's keys have to be looked at
+#pragma unroll
+          for (u32 z = 4; z < 32; z *= 2) top[c][y] = fmaxf(top[c][y], __shfl_xor_sync(~0u, top[c][y], z));
+        }
+        move |= must_move<T>(m[c][y], top[c][y]);
+      }
+    if (__any_sync(~0u, move)) {
+#pragma unroll
+      for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+        for (u32 y = 0; y < 2; ++y) {
+          float all = l[c][y];
+#pragma unroll
+          for (u32 z = 4; z < 32; z *= 2) {
+            if (!(Elem<T>::LOW > -INFINITY)) top[c][y] = fmaxf(top[c][y], __shfl_xor_sync(~0u, top[c][y], z));
+            all = fmaxf(all, __shfl_xor_sync(~0u, all, z));
+          }
+          const float f = raise_or_lower<T>(m[c][y], top[c][y], all);
+          l[c][y] *= f;
+#pragma unroll
+          for (u32 k = 0; k < D / 16; ++k) { o[k][c][y] *= f; o[k][c][y + 2] *= f; }
+        }
+    }
+    // powers, as the sum of two numbers of the element type (see k_attend_split)
+    u32 p[NT][2], rest[NT][2];
+#pragma unroll
+    for (u32 c = 0; c < NT; ++c) {
+      const float ref[2] = {m[c][0] == -INFINITY ? 0.0f : m[c][0], m[c][1] == -INFINITY ? 0.0f : m[c][1]};
+#pragma unroll
+      for (u32 y = 0; y < 4; ++y) { s[c][y] = ex2(s[c][y] - ref[y & 1]); l[c][y & 1] += s[c][y]; }
+#pragma unroll
+      for (u32 z = 0; z < 2; ++z) {
+        const u32 first = Elem<T>::down(s[c][2 * z], s[c][2 * z + 1]);
+        const float2 w = Elem<T>::up(first);
+        const u32 second = Elem<T>::down(s[c][2 * z] - w.x, s[c][2 * z + 1] - w.y);
+        p[c][z] = transposed(DOUBLE && lane % 4 >= 2 ? second : first);
+        rest[c][z] = DOUBLE ? 0 : transposed(second);
+      }
+    }
+#pragma unroll
+    for (u32 k = 0; k < D / 16; k += 2) {
+      u32 f[2][4];
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y) ldm4t(f[y], vb + block_off<D>((lane / 16) * 8 + lane % 8, 2 * (k + y) + lane / 8 % 2));
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y)
+#pragma unroll
+        for (u32 c = 0; c < NT; ++c) mma16816<T>(o[k + y][c], f[y], p[c][0], p[c][1]);
+      if (!DOUBLE)
+#pragma unroll
+        for (u32 y = 0; y < 2; ++y)
+#pragma unroll
+          for (u32 c = 0; c < NT; ++c) mma16816<T>(o[k + y][c], f[y], rest[c][0], rest[c][1]);
+    }
+    __syncwarp();                        // the stage is read: refill it
+    if (i + S::STAGES < n_mine) load(i + S::STAGES);
+    if (ANY) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  return ok;
+}
+
+template <class T, u32 D, u32 NT, bool DOUBLE, u32 CLUSTER, bool ANY>
+__global__ void __launch_bounds__(LIST_THREADS, D > 128 ? 1 : 2)
+k_attend_blocks(const __grid_constant__ AttendListArgs x, const __grid_constant__ KvMaps maps, u32 col_tiles) {
+  typedef ListShape<D> S;
+  constexpr u32 COLS = NT * 8, REAL = DOUBLE ? 4 : COLS;       // columns; those that are query heads
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 bars[LIST_WARPS * S::STAGES];
+  __shared__ u32 s_block[LIST_WARPS][S::STAGES];
+  __shared__ float s_ml[LIST_WARPS][COLS][2], s_part_ml[REAL][2];
+  __shared__ u32 s_lost;
+  const AttendArgs &a = x.a;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
+  const u32 rank = blockIdx.x % CLUSTER, unit = blockIdx.x / CLUSTER, ct = unit % col_tiles, th = unit / col_tiles, t = th / H, h = th - t * H;
+  const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8;
+  if (lane == 0) {
+    for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (!ANY && tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
+  const Where w = find_token<false>(a.b, t, a.err);
+  if (w.seq >= a.b.n_seqs) return;       // behind the last sequence: the whole cluster
+  __syncwarp();
+  const u32 ring0 = (smem_addr(smem_raw) + 1023) & ~1023u, ring = ring0 + warp * S::RING;
+  const int32_t *const list = x.blocks + (u64)th * x.n_blocks;
+  u32 n = 0;                             // places up to the last that names a block with keys to see
+  if (w.ok) for (u32 i = 0; i < x.n_blocks; i += 32) {
+    const u32 have = __ballot_sync(~0u, i + lane < x.n_blocks && (u32)list[i + lane] <= w.index / BT);
+    if (have) n = i + 32 - __clz(have);
+  }
+  const u32 rows = min(a.group - ct * REAL, REAL);             // query heads of this unit
+  const u16 *q[NT];
+#pragma unroll
+  for (u32 c = 0; c < NT; ++c) {
+    const u32 r = min((c * 8 + lane / 4) % REAL, rows - 1);    // columns behind the last repeat it
+    q[c] = (const u16 *)a.q + (u64)t * a.q_ts + (u64)(h * a.group + ct * REAL + r) * a.q_hs;
+  }
+  float o[D / 16][NT][4], m[NT][2], l[NT][2];
+  const bool ok = list_keys<T, D, NT, DOUBLE, ANY>(x, maps, a.b.table + w.seq * a.b.table_stride, list, n, w.index, h, q, rank * LIST_WARPS + warp,
+                                                   CLUSTER * LIST_WARPS, ring, bar0, s_block[warp], o, m, l);
+  // each warp's sums into its ring, [column][channel]
+  float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
+  static_assert(2 * COLS * S::LD * 4 <= S::RING, "the sums, and the CTA's part behind warp 0's, fit a ring");
+#pragma unroll
+  for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+    for (u32 y = 0; y < 2; ++y) {
+#pragma unroll
+      for (u32 z = 4; z < 32; z *= 2) l[c][y] += __shfl_xor_sync(~0u, l[c][y], z);
+      const u32 col = c * 8 + lane % 4 * 2 + y;
+      if (lane < 4) { s_ml[warp][col][0] = m[c][y]; s_ml[warp][col][1] = l[c][y]; }
+#pragma unroll
+      for (u32 k = 0; k < D / 16; ++k) {
+        so[col * S::LD + k * 16 + lane / 4] = o[k][c][y];
+        so[col * S::LD + k * 16 + lane / 4 + 8] = o[k][c][y + 2];
+      }
+    }
+  const bool lost = __syncthreads_or(!ok);
+  float *const sums = (float *)(smem_raw + (ring0 - smem_addr(smem_raw))), *const mine = sums + COLS * S::LD;
+  auto write = [&](u32 r, u32 c, float4 v, float mm, float ll) {         // four channels of a query head
+    const float inv = ll > 0.0f ? 1.0f / ll : ll;
+    const u32 hq = h * a.group + ct * REAL + r, d = ANY ? a.p.head_dim : D;
+    u16 *const dst = (u16 *)a.out + (u64)t * a.o_ts + (u64)hq * a.o_hs + c;
+    const u32 p0 = Elem<T>::down(v.x * inv, v.y * inv), p1 = Elem<T>::down(v.z * inv, v.w * inv);
+    if (((uintptr_t)dst & 7) == 0 && c + 4 <= d) *(uint2 *)dst = make_uint2(p0, p1);
+    else {
+      if (c < d) dst[0] = (u16)p0;
+      if (c + 1 < d) dst[1] = (u16)(p0 >> 16);
+      if (c + 2 < d) dst[2] = (u16)p1;
+      if (c + 3 < d) dst[3] = (u16)(p1 >> 16);
+    }
+    if (a.lse && c == 0) a.lse[(u64)t * a.n_q_heads + hq] = (mm + log2f(ll)) * 0.69314718055994531f;
+  };
+  for (u32 i = tid; i < REAL * D / 4; i += LIST_THREADS) {
+    const u32 r = i / (D / 4), c = i % (D / 4) * 4;
+    float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+    for (u32 y = 0; y < LIST_WARPS; ++y) mm = fmaxf(mm, s_ml[y][r][0]);
+    const float ref = mm == -INFINITY ? 0.0f : mm;
+    float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (u32 y = 0; y < LIST_WARPS; ++y) {
+      const float f = ex2(s_ml[y][r][0] - ref);
+      ll += f * s_ml[y][r][1];
+#pragma unroll
+      for (u32 k = 0; k < (DOUBLE ? 2 : 1); ++k) {
+        const float4 z = *(const float4 *)(sums + y * (S::RING / 4) + (r + 4 * k) * S::LD + c);
+        v.x += f * z.x; v.y += f * z.y; v.z += f * z.z; v.w += f * z.w;
+      }
+    }
+    if (CLUSTER == 1) {
+      if (r < rows && !lost) write(r, c, v, mm, ll);
+    } else {
+      *(float4 *)(mine + r * S::LD + c) = v;
+      if (c == 0) { s_part_ml[r][0] = mm; s_part_ml[r][1] = ll; }
+    }
+  }
+  u32 any_lost = lost;
+  if (CLUSTER > 1) {
+    if (tid == 0) s_lost = lost;
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    auto there = [&](const void *p, u32 cta) {
+      u32 r;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(cta));
+      return r;
+    };
+    for (u32 first = 0; first < REAL * D / 4; first += CLUSTER * LIST_THREADS) {
+      const u32 at = first + rank * LIST_THREADS + tid;
+      const bool here = at < REAL * D / 4;
+      const u32 r = here ? at / (D / 4) : 0, c = here ? at % (D / 4) * 4 : 0;
+      float mm[CLUSTER], ll[CLUSTER], top = -INFINITY, sum = 0.0f;
+      float4 v = make_float4(0, 0, 0, 0), z[CLUSTER];
+#pragma unroll
+      for (u32 y = 0; y < CLUSTER; ++y) {
+        u32 gone;
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(mm[y]), "=f"(ll[y]) : "r"(there(&s_part_ml[r][0], y)) : "memory");
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(z[y].x), "=f"(z[y].y), "=f"(z[y].z), "=f"(z[y].w) : "r"(there(mine + r * S::LD + c, y)) : "memory");
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(gone) : "r"(there(&s_lost, y)) : "memory");
+        any_lost |= gone;
+        top = fmaxf(top, mm[y]);
+      }
+      const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+      for (u32 y = 0; y < CLUSTER; ++y) {
+        const float f = ex2(mm[y] - ref);
+        sum += f * ll[y];
+        v.x += f * z[y].x; v.y += f * z[y].y; v.z += f * z[y].z; v.w += f * z[y].w;
+      }
+      if (here && r < rows && !any_lost) write(r, c, v, top, sum);
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");    // nobody reads here any more
+  }
+  if (any_lost) {
+    if (tid == 0) kv_err(a.err, KVERR_WAIT);
+    if (!ok && !ANY) for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);     // copies in flight
+  }
+}
+
+template <class T, u32 D, u32 NT, bool DOUBLE, u32 CLUSTER, bool ANY>
+static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, cudaStream_t s, u64 *allowed) {
+  constexpr u32 size = CLUSTER == 8 ? 3 : CLUSTER == 4 ? 2 : CLUSTER == 2 ? 1 : 0, kind = DOUBLE ? 0 : NT;
+  constexpr u32 which = 8 + (ANY ? (D == 256 ? 2 : D == 128) : 4 + (D == 128 ? 12 : 0) + size * 3 + kind);      // 8 .. 35, and 28 more in fp16
+  auto const kern = k_attend_blocks<T, D, NT, DOUBLE, CLUSTER, ANY>;
+  cudaError_t r = allow_smem(kern, which + (__is_same(T, __half) ? 28 : 0), ListShape<D>::SMEM, allowed);
+  if (r != cudaSuccess) return r;
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3(units * CLUSTER); c.blockDim = dim3(LIST_THREADS); c.dynamicSmemBytes = ListShape<D>::SMEM; c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = CLUSTER; at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  c.attrs = &at; c.numAttrs = CLUSTER > 1;
+  return cudaLaunchKernelEx(&c, kern, x, m, col_tiles);
+}
+template <class T, u32 D, u32 NT, bool DOUBLE>
+static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, u32 cluster, cudaStream_t s, u64 *allowed) {
+  switch (cluster) {
+    case 1: return launch_list<T, D, NT, DOUBLE, 1, false>(x, m, units, col_tiles, s, allowed);
+    case 2: return launch_list<T, D, NT, DOUBLE, 2, false>(x, m, units, col_tiles, s, allowed);
+    case 4: return launch_list<T, D, NT, DOUBLE, 4, false>(x, m, units, col_tiles, s, allowed);
+    default: return launch_list<T, D, NT, DOUBLE, 8, false>(x, m, units, col_tiles, s, allowed);
+  }
+}
+template <class T>
+static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 sms, cudaStream_t s, u64 *allowed) {
+  const u32 g = x.a.group, d = x.a.p.head_dim, th = x.a.b.n_tokens * x.a.p.n_kv_heads;
+  if (d != 64 && d != 128) {             // heads of every other size: 16 columns
+    const u32 tiles = (g + 15) / 16;
+    if (d < 64) return launch_list<T, 64, 2, false, 1, true>(x, m, th * tiles, tiles, s, allowed);
+    if (d < 128) return launch_list<T, 128, 2, false, 1, true>(x, m, th * tiles, tiles, s, allowed);
+    return launch_list<T, 256, 2, false, 1, true>(x, m, th * tiles, tiles, s, allowed);
+  }
+  const u32 cols = g <= 4 ? 4 : g <= 8 ? 8 : 16, tiles = (g + cols - 1) / cols;
+  const u64 units = (u64)th * tiles;
+  u32 cluster = 1;
+  while (cluster < 8 && units * cluster * 2 <= 2ull * sms && x.n_blocks >= 16 * cluster) cluster *= 2;
+  if (d == 64) return cols == 4 ? launch_list<T, 64, 1, true>(x, m, units, tiles, cluster, s, allowed)
+                   : cols == 8 ? launch_list<T, 64, 1, false>(x, m, units, tiles, cluster, s, allowed)
+                               : launch_list<T, 64, 2, false>(x, m, units, tiles, cluster, s, allowed);
+  return cols == 4 ? launch_list<T, 128, 1, true>(x, m, units, tiles, cluster, s, allowed)
+       : cols == 8 ? launch_list<T, 128, 1, false>(x, m, units, tiles, cluster, s, allowed)
+                   : launch_list<T, 128, 2, false>(x, m, units, tiles, cluster, s, allowed);
+}
+cudaError_t launch_attend_blocks(const AttendListArgs &x, const KvMaps &m, int sm_count, cudaStream_t s, u64 *allowed, u32 *launches) {
+  ++*launches;
+  return x.a.fp16 ? launch_list<__half>(x, m, sm_count, s, allowed) : launch_list<__nv_bfloat16>(x, m, sm_count, s, allowed);
+}
+
+// ======================================================================================================
+// Attention weight of blocks: w_b = keep w_b + sum over the new tokens, query heads and keys j of block b of exp(scale q.k_j - lse), with the
+// logarithms lse of the sums of exponentials that the attention left. K is read, V is not.
+// ======================================================================================================
+// Powers relative to a row's lse: both the scale and lse / ln 2 are taken as two 32-bit numbers, since an error of 2^-24 of either
+// would be one of some 10^-6 of the power where scores are large.
+struct Lse { float high, low; };
+__device__ __forceinline__ Lse lse_log2(float lse) {
+  constexpr float L1 = 1.44269502f, L2 = 1.92596300e-8f;       // 1 / ln 2
+  Lse r;
+  r.high = lse * L1;
+  r.low = fmaf(lse, L1, -r.high) + lse * L2;
+  if (!(fabsf(lse) <= 1e30f)) { r.high = lse == -INFINITY ? INFINITY : lse; r.low = 0.0f; }     // a row that sees no key: no weight
+  return r;
+}
+
+// 16 bytes from 8 elements at p, of which n_left exist.
+__device__ __forceinline__ uint4 load8(const u16 *p, int n_left, bool vec) {
+  if (n_left >= 8 && vec) return *(const uint4 *)p;
+  u32 x[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int y = 0; y < 8; ++y) if (y < n_left) x[y / 2] |= (u32)p[y] << (y % 2 * 16);
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+// Eight blocks of one sequence per CTA. The block's 16 keys are the rows of the matrix instruction, eight (token, head) rows the
+// columns; a lane's 16 bytes of a key and of a query are operands if channels are counted in that order on both sides, so both go
+// from memory to registers.
+template <class T, u32 G>      // G: 64-byte parts of a head
+__global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
+  __shared__ float s_sum[8][8];
+  const AttendArgs &a = x.a;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads, g = a.group;
+  const u32 tiles = (a.b.max_blocks + 7) / 8, seq = blockIdx.x / tiles, b_tile = (blockIdx.x - seq * tiles) * 8;
+  const Seq q = load_seq(a.b, seq, a.err);
+  const u32 n_held = (q.kv + BT - 1) / BT;
+  const u32 WH = H >= 8 ? 8 : H >= 4 ? 4 : H >= 2 ? 2 : 1;     // warps that share the heads; each has WH of the blocks
+  const int shift = (int)q.kv - (int)q.n;                      // index of the first new token
+  const u32 j = lane % 4, r8 = lane / 4, d = a.p.head_dim;
+  if (lane < 8) s_sum[warp][lane] = 0.0f;
+  __syncwarp();
+  for (u32 h = warp % WH; h < H; h += WH)
+    for (u32 y = 0; y < WH; ++y) {
+      const u32 which = warp / WH * WH + y, b = b_tile + which;
+      if (b >= n_held || !q.n) continue;
+      // rows that see any of the block's keys: tokens with index >= first key, and inside the window
+      const int key0 = (int)(b * BT);
+      const u32 tok0 = a.full ? 0 : (u32)max(0, key0 - shift);
+      const u32 tok1 = a.window ? (u32)max(0ll, min((long long)q.n, (long long)key0 + BT - 1 + a.window - shift)) : q.n;
+      if (tok0 >= tok1) continue;
+      const u32 slot = a.b.table[seq * a.b.table_stride + b];
+      const u16 *const src = (const u16 *)slot_ptr(a.p, a.p.k, slot);
+      if (!src) { if (lane == 0) kv_err(a.err, KVERR_RANGE); }
+      uint4 k[G][2];
+      const bool vec = d % 8 == 0 && ((uintptr_t)src & 15) == 0;
+#pragma unroll
+      for (u32 i = 0; i < G; ++i)
+#pragma unroll
+        for (u32 z = 0; z < 2; ++z) {
+          const u32 c = i * 32 + j * 8;
+          k[i][z] = src && c < d ? load8(src + ((u64)(r8 + 8 * z) * H + h) * d + c, (int)d - (int)c, vec) : make_uint4(0, 0, 0, 0);
+        }
+      float sum = 0.0f, part = 0.0f;
+      u32 count = 0;
+      for (u32 r0 = tok0 * g; r0 < tok1 * g; r0 += 8) {
+        const u32 r = min(r0 + r8, tok1 * g - 1), tok = r / g;
+        const u16 *const qs = (const u16 *)a.q + (u64)(q.t0 + tok) * a.q_ts + (u64)(h * g + r - tok * g) * a.q_hs;
+        const bool qvec = d % 8 == 0 && ((uintptr_t)qs & 15) == 0;
+        float s[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (u32 i = 0; i < G; ++i) {
+          const u32 c = i * 32 + j * 8;
+          const uint4 v = c < d ? load8(qs + c, (int)d - (int)c, qvec) : make_uint4(0, 0, 0, 0);
+          const u32 f0[4] = {k[i][0].x, k[i][1].x, k[i][0].y, k[i][1].y}, f1[4] = {k[i][0].z, k[i][1].z, k[i][0].w, k[i][1].w};
+          mma16816<T>(s, f0, v.x, v.y);
+          mma16816<T>(s, f1, v.z, v.w);
+        }
+#pragma unroll
+        for (u32 z = 0; z < 2; ++z) {
+          const u32 rr = r0 + 2 * j + z;
+          if (rr >= tok1 * g) continue;
+          const u32 tk = rr / g;
+          const Lse L = lse_log2(a.lse[(u64)(q.t0 + tk) * a.n_q_heads + h * g + rr - tk * g]);
+          const int own = shift + (int)tk, hi = a.full ? (int)q.kv : own + 1, lo = a.window ? hi - (int)min(a.window, 0x7FFFFFFFu) : 0;
+#pragma unroll
+          for (u32 w = 0; w < 2; ++w) {
+            const int key = key0 + (int)r8 + 8 * (int)w;
+            const float v = s[2 * w + z], e = ex2(fmaf(v, a.scale_log2, -L.high) + fmaf(v, x.scale_low, -L.low));
+            part += key < hi && key >= lo ? e : 0.0f;
+          }
+        }
+        if (++count % 32 == 0) { sum += part; part = 0.0f; }   // sums of few, then of those: 32 bits hold them
+      }
+      sum = sum_over_warp(sum + part);
+      if (lane == 0) s_sum[warp][which] += sum;
+    }
+  __syncthreads();
+  if (tid < 8 && b_tile + tid < a.b.max_blocks) {
+    const u32 b = b_tile + tid;
+    float sum = 0.0f;
+    for (u32 w = 0; w < 8; ++w) sum += s_sum[w][tid];
+    if (x.weights) sum += x.keep * x.weights[seq * x.w_stride + b];
+    x.out[seq * x.o_stride + b] = b < n_held ? sum : 0.0f;
+  }
+}
+
+cudaError_t launch_weigh(const WeighArgs &x, cudaStream_t s, u64 *, u32 *launches) {
+  const u32 ctas = x.a.b.n_seqs * ((x.a.b.max_blocks + 7) / 8), d = x.a.p.head_dim;
+  ++*launches;
+  if (x.a.fp16) {
+    if (d <= 64) k_weigh<__half, 2><<<ctas, 256, 0, s>>>(x);
+    else if (d <= 128) k_weigh<__half, 4><<<ctas, 256, 0, s>>>(x);
+    else k_weigh<__half, 8><<<ctas, 256, 0, s>>>(x);
+  } else {
+    if (d <= 64) k_weigh<__nv_bfloat16, 2><<<ctas, 256, 0, s>>>(x);
+    else if (d <= 128) k_weigh<__nv_bfloat16, 4><<<ctas, 256, 0, s>>>(x);
+    else k_weigh<__nv_bfloat16, 8><<<ctas, 256, 0, s>>>(x);
+  }
+  return cudaGetLastError();
+}
+
+// ======================================================================================================
+// Eviction by weight: of a sequence's blocks the first, the last and the heaviest stay. Rows are packed in place: a CTA reads what it
+// is about to write over before it does.
+// ======================================================================================================
+constexpr u32 EVICT_THREADS = 1024;
+__global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a, u32 held) {
+  extern __shared__ u32 s_keys[];
+  __shared__ u32 s_border, s_n[2][EVICT_THREADS / 32];
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, seq = blockIdx.x;
+  const u32 *const table = a.table + seq * a.table_stride;
+  const float *const weights = a.weights + seq * a.w_stride;
+  u32 *const table_out = a.table_out + seq * a.table_out_stride, *const evicted = a.evicted + seq * a.evicted_stride;
+  float *const weights_out = a.weights_out + seq * a.w_out_stride;
+  const u32 room = a.max_blocks * BT;
+  u32 kv = a.kv_len[seq];
+  if (kv > room) { if (tid == 0) kv_err(a.err, KVERR_RANGE); kv = room; }
+  const u32 had = (kv + BT - 1) / BT, gone = had > a.n_blocks ? had - a.n_blocks : 0;
+  auto order = [&](float w) { return ordered(w == w ? w + 0.0f : INFINITY); };       // a NaN weighs most
+  Kth kth{0, ~0u};
+  u32 border = 0;
+  if (gone) {                            // of the n blocks between the first and the last ones m stay
+    const u32 n = had - a.first - a.last, m = n - gone;
+    const float *const w = weights + a.first;
+    if (n <= held) for (u32 i = tid; i < n; i += EVICT_THREADS) s_keys[i] = order(w[i]);
+    __syncthreads();
+    auto key = [&](u32 i) { return n <= held ? s_keys[i] : order(w[i]); };
+    if (m) kth = kth_largest<EVICT_THREADS>(key, n, m); else kth = Kth{~0u, 0};
+    __syncthreads();
+    if (kth.ties != ~0u && kth.ties) {
+      deal<EVICT_THREADS>(n, [&](u32 i) { return key(i) == kth.at ? 1u : 0u; }, [&](u32 i, u32, u32 at) { if (at == kth.ties - 1) s_border = i; });
+      __syncthreads();
+      border = s_border;
+    }
+  }
+  // in order, 4 blocks of each thread at a time: read, then written at or in front of where they were
+  u32 at[2] = {0, 0};
+  for (u32 i0 = 0; i0 < had; i0 += 4 * EVICT_THREADS) {
+    u32 slot[4], stays = 0, n[2] = {0, 0};
+    float w[4];
+#pragma unroll
+    for (u32 y = 0; y < 4; ++y) {
+      const u32 i = i0 + 4 * tid + y;
+      if (i >= had) continue;
+      slot[y] = table[i]; w[y] = weights[i];
+      const u32 x = order(w[y]);
+      const bool stay = !gone || i < a.first || i >= had - a.last || x > kth.at || (x == kth.at && (kth.ties == ~0u || (kth.ties && i - a.first <= border)));
+      stays |= (u32)stay << y;
+      ++n[stay ? 0 : 1];
+    }
+    u32 incl = n[0] | n[1] << 16;        // at most 4096 each
+    const u32 here = incl;
+#pragma unroll
+    for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
+    __syncthreads();                     // everything is read; the sums of the round before too
+    if (lane == 31) s_n[0][warp] = incl;
+    __syncthreads();
+    u32 before = 0, all = 0;
+#pragma unroll
+    for (u32 v = 0; v < EVICT_THREADS / 32; ++v) { if (v < warp) before += s_n[0][v]; all += s_n[0][v]; }
+    before += incl - here;
+    u32 to[2] = {at[0] + (before & 0xFFFF), at[1] + (before >> 16)};
+#pragma unroll
+    for (u32 y = 0; y < 4; ++y) {
+      if (i0 + 4 * tid + y >= had) continue;
+      if (stays >> y & 1) { table_out[to[0]] = slot[y]; weights_out[to[0]++] = w[y]; }
+      else evicted[to[1]++] = slot[y];
+    }
+    at[0] += all & 0xFFFF; at[1] += all >> 16;
+  }
+  __syncthreads();
+  for (u32 i = at[0] + tid; i < a.max_blocks; i += EVICT_THREADS) { table_out[i] = ~0u; weights_out[i] = 0.0f; }
+  for (u32 i = at[1] + tid; i < a.max_blocks; i += EVICT_THREADS) evicted[i] = ~0u;
+  if (tid == 0) a.kv_len_out[seq] = kv - gone * BT;
+}
+
+cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s, u64 *allowed, u32 *launches) {
+  const cudaError_t r = allow_smem(k_evict_blocks, 2, 200 * 1024, allowed);
+  if (r != cudaSuccess) return r;
+  const u32 held = (u32)std::min<u64>(a.max_blocks, 50 * 1024);
+  k_evict_blocks<<<a.n_seqs, EVICT_THREADS, held * 4, s>>>(a, held);
+  ++*launches;
+  return cudaGetLastError();
+}
+
+}  // namespace kvt

@@ -157,7 +157,7 @@ struct kvt_engine {
   bool metadata_only;
   int sm_count = 148;
   int device = 0;
-  KvMaps kv_maps{}; bool kv_maps_ok = false; u64 kv_smem_allowed = 0;   // for head sizes of 64 and 128
+  KvMaps kv_maps{}; bool kv_maps_ok = false; u64 kv_smem_allowed = 0, kv_blocks_allowed = 0;   // for head sizes of 64 and 128
   u8 *tail_pool = nullptr; u32 n_tail = 0;   // blocks outside every tier (kvt_set_tail_pool)
   // host state
   std::vector<Ctx> ctxs;
@@ -2327,7 +2327,163 @@ AttendArgs attend_args(kvt_engine *e, const kvt_attend_args &a) {
   return x;
 }
 
+KvBounds kv_bounds(const kvt_engine *e, const kvt_key_bounds &k, u32 layer) {
+  const u64 width = (e->cfg.head_dim + 15) / 16 * 16, heads = k.n_slots * e->cfg.n_kv_heads;
+  return KvBounds{k.codes + layer * heads * 2 * width, k.exps + layer * heads, k.n_slots, (u32)width};
+}
+const char *bounds_fault(const kvt_engine *e, const kvt_key_bounds &k) {
+  if (!k.codes || !k.exps || ((uintptr_t)k.codes & 15)) return "NULL or misaligned bounds";
+  if (e->cfg.head_dim > 256) return "bounds: head_dim above 256";
+  return nullptr;
+}
+const char *keep_fault(u32 n_blocks, u32 first, u32 last) {
+  return !last || (u64)first + last > n_blocks || n_blocks > 0x7FFFFFFFu ? "first and last blocks: last >= 1, first + last <= n_blocks" : nullptr;
+}
+// What kvt_attend would refuse in the arguments that other calls share with it.
+const char *attend_like_fault(const kvt_engine *e, const kvt_batch &b, u32 layer, u32 dtype, u32 n_q_heads, u32 flags, u32 window, float scale) {
+  kvt_attend_args x{};
+  x.b = b; x.layer = layer; x.dtype = dtype; x.n_q_heads = n_q_heads; x.flags = flags; x.window = window; x.scale = scale;
+  if (const char *m = attend_fault(e, x)) return m;
+  return b.n_seqs && (u64)b.n_tokens * n_q_heads > 0x7FFFFFFFull ? "batch too large" : nullptr;
+}
+const char *select_fault(const kvt_engine *e, const kvt_select_args &a) {
+  if (const char *m = attend_like_fault(e, a.b, a.layer, a.dtype, a.n_q_heads, 0, 0, 0.0f)) return m;
+  if (const char *m = bounds_fault(e, a.bounds)) return m;
+  return keep_fault(a.n_blocks, a.first, a.last);
+}
+SelectArgs select_args(kvt_engine *e, const kvt_select_args &a) {
+  SelectArgs x{};
+  x.b = kv_batch(a.b); x.k = kv_bounds(e, a.bounds, a.layer);
+  x.q = a.q; x.q_ts = a.q_ts; x.q_hs = a.q_hs;
+  x.n_kv_heads = e->cfg.n_kv_heads; x.head_dim = e->cfg.head_dim; x.group = a.n_q_heads / e->cfg.n_kv_heads; x.fp16 = a.dtype == KVT_KV_FP16;
+  x.n_blocks = a.n_blocks; x.first = a.first; x.last = a.last;
+  x.out = a.out; x.scores = (u32 *)a.scratch;
+  x.err = e->dp<u32>(e->L.kv_err);
+  return x;
+}
+const char *weigh_fault(const kvt_engine *e, const kvt_weigh_args &a) {
+  if (const char *m = attend_like_fault(e, a.b, a.layer, a.dtype, a.n_q_heads, a.flags, a.window, a.scale)) return m;
+  if ((u64)a.b.n_seqs * ((a.b.max_blocks + 7ull) / 8) > 0x7FFFFFFFull) return "weigh: table too large";
+  if (!(a.keep >= 0.0f) || a.keep > 3.0e38f || a.reserved) return "weigh: keep";
+  return nullptr;
+}
+WeighArgs weigh_args(kvt_engine *e, const kvt_weigh_args &a) {
+  kvt_attend_args y{};
+  y.b = a.b; y.layer = a.layer; y.dtype = a.dtype; y.n_q_heads = a.n_q_heads; y.flags = a.flags; y.window = a.window; y.scale = a.scale;
+  y.q = a.q; y.q_ts = a.q_ts; y.q_hs = a.q_hs; y.lse = const_cast<float *>(a.lse); y.scratch = a.scratch;
+  WeighArgs x{};
+  x.a = attend_args(e, y);
+  const double scale = (a.scale > 0.0f ? (double)a.scale : 1.0 / std::sqrt((double)e->cfg.head_dim)) * 1.4426950408889634074;
+  x.scale_low = (float)(scale - (double)x.a.scale_log2);
+  x.weights = a.weights; x.out = a.out; x.w_stride = a.w_stride; x.o_stride = a.o_stride; x.keep = a.keep;
+  return x;
+}
+
 }  // namespace
+
+int32_t kvt_bound_keys(kvt_engine *e, const kvt_bound_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_bound_args &a = *args;
+  if (const char *m = kv_engine_fault(e, a.layer, a.dtype)) return fail(e, KVT_E_INVAL, m);
+  if (const char *m = kv_batch_fault(a.b)) return fail(e, KVT_E_INVAL, m);
+  if (const char *m = bounds_fault(e, a.bounds)) return fail(e, KVT_E_INVAL, m);
+  if (!a.b.n_seqs || !a.b.n_tokens) return KVT_OK;
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "bound: device");
+  BoundArgs x{};
+  x.b = kv_batch(a.b); x.p = kv_pools(e, a.layer); x.k = kv_bounds(e, a.bounds, a.layer);
+  x.fp16 = a.dtype == KVT_KV_FP16; x.err = e->dp<u32>(e->L.kv_err);
+  u32 launches = 0;
+  const cudaError_t r = launch_bound(x, e->sm_count, (cudaStream_t)stream, &launches);
+  return kv_launched(e, r, launches);
+}
+
+uint64_t kvt_select_scratch_bytes(kvt_engine *e, const kvt_select_args *args) {
+  if (!e || !args || select_fault(e, *args) || !args->b.n_seqs || !args->b.n_tokens) return 0;
+  return plan_select(select_args(e, *args), e->sm_count).scratch_bytes;
+}
+
+int32_t kvt_select_blocks(kvt_engine *e, const kvt_select_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_select_args &a = *args;
+  if (const char *m = select_fault(e, a)) return fail(e, KVT_E_INVAL, m);
+  if (!a.b.n_seqs || !a.b.n_tokens) return KVT_OK;
+  if (!a.q || !a.out || ((uintptr_t)a.q & 1) || ((uintptr_t)a.out & 3)) return fail(e, KVT_E_INVAL, "select: NULL or misaligned tensor");
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "select: device");
+  const SelectArgs x = select_args(e, a);
+  const SelectPlan p = plan_select(x, e->sm_count);
+  if (p.scratch_bytes) {
+    if (!a.scratch || a.scratch_bytes < p.scratch_bytes) return fail(e, KVT_E_BUFSZ, "select: scratch too small");
+    if ((uintptr_t)a.scratch & 15) return fail(e, KVT_E_INVAL, "select: misaligned scratch");
+  }
+  u32 launches = 0;
+  const cudaError_t r = launch_select(x, p, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  return kv_launched(e, r, launches);
+}
+
+int32_t kvt_attend_blocks(kvt_engine *e, const kvt_attend_blocks_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_attend_blocks_args &a = *args;
+  if (const char *m = attend_like_fault(e, a.b, a.layer, a.dtype, a.n_q_heads, 0, 0, a.scale)) return fail(e, KVT_E_INVAL, m);
+  if (!a.n_blocks || a.n_blocks > 0x7FFFFFFFu || a.reserved) return fail(e, KVT_E_INVAL, "attend_blocks: n_blocks");
+  if (!a.b.n_seqs || !a.b.n_tokens) return KVT_OK;
+  if (!a.q || !a.out || !a.blocks || (((uintptr_t)a.q | (uintptr_t)a.out) & 1) || (((uintptr_t)a.lse | (uintptr_t)a.blocks) & 3))
+    return fail(e, KVT_E_INVAL, "attend_blocks: NULL or misaligned tensor");
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "attend_blocks: device");
+  kvt_attend_args y{};
+  y.b = a.b; y.layer = a.layer; y.dtype = a.dtype; y.n_q_heads = a.n_q_heads; y.scale = a.scale;
+  y.q = a.q; y.out = a.out; y.lse = a.lse; y.q_ts = a.q_ts; y.q_hs = a.q_hs; y.o_ts = a.o_ts; y.o_hs = a.o_hs;
+  const AttendListArgs x{attend_args(e, y), a.blocks, a.n_blocks};
+  u32 launches = 0;
+  const cudaError_t r = launch_attend_blocks(x, e->kv_maps, e->sm_count, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  return kv_launched(e, r, launches);
+}
+
+uint64_t kvt_weigh_scratch_bytes(kvt_engine *e, const kvt_weigh_args *args) {
+  if (!e || !args || weigh_fault(e, *args) || !args->b.n_seqs || !args->b.n_tokens) return 0;
+  return 0;
+}
+
+int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_weigh_args &a = *args;
+  if (const char *m = weigh_fault(e, a)) return fail(e, KVT_E_INVAL, m);
+  if (!a.b.n_seqs || !a.b.max_blocks) return KVT_OK;
+  if (!a.out || (((uintptr_t)a.weights | (uintptr_t)a.out | (uintptr_t)a.lse) & 3) || ((uintptr_t)a.q & 1) || (a.b.n_tokens && (!a.q || !a.lse)))
+    return fail(e, KVT_E_INVAL, "weigh: NULL or misaligned tensor");
+  if (!a.b.q_start || !a.b.kv_len || !a.b.block_table) return fail(e, KVT_E_INVAL, "weigh: batch without starts, lengths or block table");
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "weigh: device");
+  u32 launches = 0;
+  const cudaError_t r = launch_weigh(weigh_args(e, a), (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  return kv_launched(e, r, launches);
+}
+
+int32_t kvt_evict_blocks(kvt_engine *e, const kvt_evict_args *args, void *stream) {
+  if (!e || !args) return KVT_E_INVAL;
+  const kvt_evict_args &a = *args;
+  if (const char *m = keep_fault(a.n_blocks, a.first, a.last)) return fail(e, KVT_E_INVAL, m);
+  if (a.reserved || a.n_seqs > 0x7FFFFFFFu || a.max_blocks > 0x7FFFFFFFu / 16) return fail(e, KVT_E_INVAL, "evict: table too large");
+  if (!a.n_seqs) return KVT_OK;
+  if (!a.kv_len || !a.kv_len_out || (a.max_blocks && (!a.block_table || !a.weights || !a.table_out || !a.weights_out || !a.evicted)))
+    return fail(e, KVT_E_INVAL, "evict: NULL array");
+  if (((uintptr_t)a.block_table | (uintptr_t)a.kv_len | (uintptr_t)a.weights | (uintptr_t)a.table_out | (uintptr_t)a.kv_len_out |
+       (uintptr_t)a.weights_out | (uintptr_t)a.evicted) & 3)
+    return fail(e, KVT_E_INVAL, "evict: misaligned array");
+  OnDevice on(e->device);
+  if (!on.ok) return fail(e, KVT_E_CUDA, "evict: device");
+  EvictArgs x{};
+  x.table = a.block_table; x.kv_len = a.kv_len; x.weights = a.weights; x.table_stride = a.table_stride; x.w_stride = a.w_stride;
+  x.table_out = a.table_out; x.kv_len_out = a.kv_len_out; x.weights_out = a.weights_out; x.evicted = a.evicted;
+  x.table_out_stride = a.table_out_stride; x.w_out_stride = a.w_out_stride; x.evicted_stride = a.evicted_stride;
+  x.n_seqs = a.n_seqs; x.max_blocks = a.max_blocks; x.n_blocks = a.n_blocks; x.first = a.first; x.last = a.last;
+  x.err = e->dp<u32>(e->L.kv_err);
+  u32 launches = 0;
+  const cudaError_t r = launch_evict(x, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  return kv_launched(e, r, launches);
+}
 
 int32_t kvt_append_kv(kvt_engine *e, const kvt_append_args *args, void *stream) {
   if (!e || !args) return KVT_E_INVAL;

@@ -111,7 +111,10 @@ struct EvictArgs {
 cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, uint32_t *launches);
 cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 cudaError_t launch_attend_blocks(const AttendListArgs &a, const KvMaps &m, int sm_count, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
-cudaError_t launch_weigh(const WeighArgs &a, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
+// What kvt_weigh_blocks does, decided from sizes alone.
+struct WeighPlan { uint32_t many, grid; uint64_t scratch_bytes; };
+WeighPlan plan_weigh(const WeighArgs &a, uint32_t max_q_len, int sm_count);
+cudaError_t launch_weigh(const WeighArgs &a, const WeighPlan &p, const KvMaps &m, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 
 }  // namespace kvt

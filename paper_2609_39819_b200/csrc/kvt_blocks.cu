@@ -947,8 +947,435 @@ __global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
   }
 }
 
-cudaError_t launch_weigh(const WeighArgs &x, cudaStream_t s, u64 *, u32 *launches) {
+// Many rows (prompts, chunks). Here the keys are the rows of the matrix instruction as well: S^T = K Q^T for 256 keys, two tiles of
+// 128, by 128 (token, head) rows, so that a thread owns a key and adds up what its row of S^T gives in a register, with no
+// exchange between threads and no masks but at the diagonal.
+//   warps 0-7    a thread per key: powers and their sum
+//   warp 8       issues the products, S^T in tensor memory, held twice: 2 x 2 x 128 columns
+//   warp 9       works out what this CTA does
+//   warp 10      loads K (TMA, a box per block), 256 keys of a head per stage
+//   warps 11-14  bring queries, 128 rows per stage, and their lse; two warps for every other stage
+// Work: for each 256 keys of each sequence ("a pair" of tiles) the tiles of 128 rows that see any of them, head by head. All of it,
+// one tile after the other, is dealt out in equal stretches, one per CTA; a pair that several CTAs work on is put together from
+// their sums by the kernel behind, always in the same order.
+constexpr int NO_ROW = -0x7FFFFFFF - 1;
+constexpr u32 WTC_KEYS = 256, WTC_KB = WTC_KEYS / BT, WTC_THREADS = 480, WTC_JOBS = 4, WTC_Q = 2, WTC_L = 4;
+template <u32 D> struct WeighShape {
+  static constexpr u32 BLOCK = BT * D * 2, K = WTC_KEYS * D * 2, Q = TC_TILE * D * 2, SMEM = 2 * K + WTC_Q * Q + 1024;
+};
+// Rows of a sequence that see any of the keys [key0, key0 + 256): tokens [lo, hi) of the new ones.
+struct Seen { u32 lo, hi; };
+__device__ __forceinline__ Seen seen_by(const AttendArgs &a, const Seq &q, u32 key0) {
+  const long long shift = (long long)q.kv - q.n, last = min((long long)key0 + WTC_KEYS, (long long)q.kv) - 1;
+  Seen s;
+  s.lo = a.full ? 0u : (u32)max(0ll, min((long long)q.n, (long long)key0 - shift));
+  s.hi = a.window ? (u32)max(0ll, min((long long)q.n, last + (long long)a.window - shift)) : q.n;
+  s.hi = max(s.hi, s.lo);
+  return s;
+}
+__device__ __forceinline__ u32 row_tiles(const AttendArgs &a, const Seen &s) { return (u32)(((u64)(s.hi - s.lo) * a.group + TC_TILE - 1) / TC_TILE); }
+
+// Scratch: a header {tiles per stretch, tiles}, the place of each pair in the work (and the end), then 16 sums,
+// one per block, for each (pair, CTA): the one of pair p and CTA c is number p + c, as each next one has a greater p or c.
+struct WeighScratch { u64 *per, *place; float *sums; };
+__host__ __device__ __forceinline__ u64 weigh_pairs(u32 n_seqs, u32 max_blocks) { return (u64)n_seqs * ((max_blocks + WTC_KB - 1) / WTC_KB); }
+__host__ __device__ __forceinline__ WeighScratch weigh_scratch(u8 *p, u32 n_seqs, u32 max_blocks) {
+  WeighScratch s;
+  s.per = (u64 *)p;
+  s.place = s.per + 2;
+  s.sums = (float *)(p + ((16 + 8 * (weigh_pairs(n_seqs, max_blocks) + 1) + 15) & ~15ull));
+  return s;
+}
+
+struct WeighJob {
+  u32 t0, rows, index0;        // first row's token, rows that see any of the keys, index of the first token in its sequence
+  u32 kv, key0, seq;
+  u32 tiles, x0, x1;           // row tiles of a head; tiles [x0, x1) of all heads
+  u64 sum;                     // place of the sums
+  u32 last;
+};
+
+template <class T, u32 D>
+__global__ void __launch_bounds__(WTC_THREADS, 1)
+k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps maps) {
+  typedef WeighShape<D> S;
+  constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 s_kfull[2], s_kempty[2], s_qfull[WTC_Q], s_qempty[WTC_Q], s_lfull[WTC_L], s_sfull[2], s_sempty[2], s_drain, s_jfull[WTC_JOBS], s_jempty[WTC_JOBS];
+  __shared__ __align__(16) float s_l[WTC_L][TC_TILE];
+  __shared__ __align__(16) int s_index[WTC_L][TC_TILE];
+  __shared__ u32 s_tmem;
+  __shared__ volatile u32 s_lost;
+  __shared__ WeighJob s_job[WTC_JOBS];
+  const AttendArgs &a = x.a;
+  asm volatile("griddepcontrol.launch_dependents;");
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads, g = a.group;
+  const u32 kfull = smem_addr(s_kfull), kempty = smem_addr(s_kempty), qfull = smem_addr(s_qfull), qempty = smem_addr(s_qempty), lfull = smem_addr(s_lfull),
+            sfull = smem_addr(s_sfull), sempty = smem_addr(s_sempty), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
+  if (tid == 0) {
+    for (u32 i = 0; i < 2; ++i) { bar_init(kfull + i * 8, 1); bar_init(kempty + i * 8, 1); bar_init(sfull + i * 8, 1); bar_init(sempty + i * 8, 8); }
+    for (u32 i = 0; i < WTC_Q; ++i) { bar_init(qfull + i * 8, 2); bar_init(qempty + i * 8, 1); }
+    for (u32 i = 0; i < WTC_L; ++i) bar_init(lfull + i * 8, 2);
+    for (u32 i = 0; i < WTC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 14); }
+    bar_init(drain, 1);
+    s_lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if (warp == 10 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &maps.tail : &maps.pool) : "memory");
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const u32 tmem = s_tmem;
+  const u32 sk = (smem_addr(smem_raw) + 1023) & ~1023u, sq = sk + 2 * S::K;
+  volatile u32 *const lost = &s_lost;
+  // Waits last as long as a job of another warp may: a tile of 128 rows takes a microsecond, and a job has no more than x0 .. x1 of
+  // them; 32 for each of the longest that can be.
+  const u64 most = (u64)H * (((u64)a.b.n_tokens * g + TC_TILE - 1) / TC_TILE) * 8;
+  const u32 patience = (u32)min(most, (u64)0x7FFFFFFF);
+  u32 jobs = 0;
+  auto next_job = [&](WeighJob &j) {
+    const u32 at = jobs % WTC_JOBS;
+    if (!tc_wait(jfull + at * 8, (jobs / WTC_JOBS) & 1, lost, patience)) return false;
+    j = s_job[at];
+    __syncwarp();
+    if (lane == 0) bar_arrive(jempty + at * 8);
+    ++jobs;
+    return j.last == 0;
+  };
+
+  if (warp == 9) {
+    // ---- what this CTA does. A lane per pair, 32 pairs of a sequence at a time; twice: for the sum of the work, then for its share.
+    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
+    u64 total = 0, per = 0, tokens = 0;
+    u32 made = 0;
+    bool ok = true;
+    for (u32 pass = 0; pass < 2 && ok; ++pass) {
+      const u64 begin = per * blockIdx.x, end = min(begin + per, total);
+      u64 base = 0, pair = 0;
+      for (u32 s0 = 0; s0 < a.b.n_seqs && ok; s0 += 32) {
+        Seq mine{0, 0, 0};
+        if (s0 + lane < a.b.n_seqs) mine = load_seq(a.b, s0 + lane, a.err);
+        if (pass == 0) tokens += mine.n;
+        const u32 n_here = min(32u, a.b.n_seqs - s0);
+        for (u32 y = 0; y < n_here && ok; ++y) {
+          Seq q;
+          q.t0 = __shfl_sync(~0u, mine.t0, y); q.n = __shfl_sync(~0u, mine.n, y); q.kv = __shfl_sync(~0u, mine.kv, y);
+          const u32 pairs = (q.kv + WTC_KEYS - 1) / WTC_KEYS;
+          for (u32 k0 = 0; k0 < pairs && ok; k0 += 32) {
+            const u32 k = k0 + lane;
+            Seen seen{0, 0};
+            if (k < pairs) seen = seen_by(a, q, k * WTC_KEYS);
+            const u32 tiles = row_tiles(a, seen);
+            const u64 work = (u64)tiles * H;
+            u64 incl = work;
+#pragma unroll
+            for (u32 o = 1; o < 32; o *= 2) { const u64 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
+            if (pass) {
+              const u64 from = base + incl - work, to = base + incl;
+              if (blockIdx.x == 0 && k < pairs) sc.place[pair + k] = from;
+              const u64 f = max(from, begin), t = min(to, end);
+              for (u32 mask = __ballot_sync(~0u, f < t); mask && ok; mask &= mask - 1) {
+                const u32 at = made % WTC_JOBS;
+                if (made >= WTC_JOBS && !(ok = tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience))) break;
+                if (lane == __ffs(mask) - 1) {
+                  WeighJob j;
+                  j.t0 = q.t0 + seen.lo; j.rows = (seen.hi - seen.lo) * g; j.index0 = q.kv - q.n + seen.lo;
+                  j.kv = q.kv; j.key0 = k * WTC_KEYS; j.seq = s0 + y;
+                  j.tiles = tiles; j.x0 = (u32)(f - from); j.x1 = (u32)(t - from);
+                  j.sum = pair + k + blockIdx.x;
+                  j.last = 0;
+                  s_job[at] = j;
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(jfull + at * 8);
+                ++made;
+              }
+            }
+            base += __shfl_sync(~0u, incl, 31);
+            if (pass && blockIdx.x && base >= end) { k0 = pairs; y = n_here; s0 = a.b.n_seqs; break; }     // (CTA 0 goes on for the places)
+          }
+          pair += pairs;
+        }
+      }
+      if (pass == 0) {
+#pragma unroll
+        for (u32 o = 16; o; o /= 2) tokens += __shfl_xor_sync(~0u, tokens, o);
+        // starts that go up and down make the same tokens count again and again: then nothing is added (load_seq has set the error word)
+        total = tokens > a.b.n_tokens ? 0 : base;
+        per = (total + gridDim.x - 1) / gridDim.x;
+        if (blockIdx.x == 0 && lane == 0) { sc.per[0] = per; sc.per[1] = total; }
+      } else if (blockIdx.x == 0 && lane == 0) {
+        sc.place[pair] = base;
+      }
+    }
+    const u32 at = made % WTC_JOBS;
+    if (ok && made >= WTC_JOBS) ok = tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience);
+    if (ok && lane == 0) { s_job[at].last = 1; bar_arrive(jfull + at * 8); }
+  } else if (warp == 10) {
+    // ---- K: a head's 256 keys per stage; blocks behind the sequence's last read as zeros
+    u32 it = 0;
+    bool ok = true;
+    for (WeighJob j; ok && next_job(j);) {
+      const u32 b = j.key0 / BT + lane, held = (j.kv + BT - 1) / BT;
+      u32 slot = ~0u;
+      if (lane < WTC_KB && b < held) {
+        slot = a.b.table[j.seq * a.b.table_stride + b];
+        if (slot >= a.p.n_slots && slot - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+      }
+      for (u32 h = j.x0 / j.tiles; h <= (j.x1 - 1) / j.tiles; ++h, ++it) {
+        const u32 st = it % 2;
+        if (it >= 2 && !(ok = tc_wait(kempty + st * 8, (it / 2 - 1) & 1, lost, patience))) break;
+        if (lane == 0) bar_expect(kfull + st * 8, S::K);
+        __syncwarp();
+        if (lane < WTC_KB) load_block(a, maps, sk + st * S::K + lane * S::BLOCK, kfull + st * 8, slot, 2 * a.layer, h, D / 64);
+        __syncwarp();
+      }
+    }
+    for (u32 i = it > 2 ? it - 2 : 0; i < it; ++i) bar_wait(kfull + (i % 2) * 8, (i / 2) & 1);     // landed before the CTA ends
+  } else if (warp == 8) {
+    // ---- products
+    if (elect_one()) {
+      const u32 id = tc_idesc(FP16, TC_TILE, false);
+      const u64 dk0 = tc_desc(sk, 16, D * 16), dq0 = tc_desc(sq, 16, 1024);
+      u32 n = 0, it = 0;
+      bool ok = true;
+      for (; ok;) {
+        const u32 at = jobs % WTC_JOBS;
+        if (!(ok = tc_wait1(jfull + at * 8, (jobs / WTC_JOBS) & 1, lost, patience))) break;
+        ++jobs;
+        const u32 tiles = s_job[at].tiles, x0 = s_job[at].x0, x1 = s_job[at].x1, end = s_job[at].last;
+        bar_arrive(jempty + at * 8);
+        if (end) break;
+        u32 r = x0 % tiles;
+        bool fresh = true;
+        for (u32 i = x0; i < x1; ++i, ++n) {
+          const u32 st = n % WTC_Q, buf = n % 2, ks = it % 2;
+          if (fresh && !(ok = tc_wait1(kfull + ks * 8, (it / 2) & 1, lost, patience))) break;
+          if (!(ok = tc_wait1(qfull + st * 8, (n / WTC_Q) & 1, lost, patience))) break;
+          if (n >= 2 && !(ok = tc_wait1(sempty + buf * 8, (n / 2 - 1) & 1, lost, patience))) break;
+          tc_after();
+          const u64 dq = dq0 + st * (S::Q / 16);
+#pragma unroll
+          for (u32 tile = 0; tile < 2; ++tile) {
+            const u64 dk = dk0 + ks * (S::K / 16) + tile * (S::K / 32);
+#pragma unroll
+            for (u32 k = 0; k < D / 16; ++k)
+              tc_mma_ss(tmem + buf * 256 + tile * 128, dk + ((k / 4) * 1024 + (k % 4) * 32) / 16, dq + ((k / 4) * (TC_TILE * 128) + (k % 4) * 32) / 16, id, k > 0);
+          }
+          tc_commit(sfull + buf * 8);
+          tc_commit(qempty + st * 8);
+          fresh = ++r == tiles || i + 1 == x1;
+          if (fresh) { r = 0; tc_commit(kempty + ks * 8); ++it; }
+        }
+      }
+      tc_commit(drain);                  // all products and their arrivals are done before the CTA ends
+      bar_wait(drain, 0);
+    }
+    __syncwarp();
+  } else if (warp >= 11) {
+    // ---- queries: warps 11, 12 bring the even tiles, 13, 14 the odd ones
+    const u32 side = (warp - 11) / 2, mine = (warp - 11) % 2 * 32 + lane;      // 64 threads
+    constexpr u32 PER = D / 8, STEP = 64 / PER;                                // 16-byte parts of a row; rows per round
+    u32 n = 0;
+    bool ok = true;
+    for (WeighJob j; ok && next_job(j);) {
+      u32 h = j.x0 / j.tiles, r = j.x0 - h * j.tiles;
+      for (u32 i = j.x0; i < j.x1; ++i, ++n) {
+        if (n % 2 == side) {
+          const u32 st = n % WTC_Q, ls = n % WTC_L;
+          static_assert(WTC_Q == 2, "a side's stage is its own");
+          if (n >= WTC_Q && !(ok = tc_wait(qempty + st * 8, (n / WTC_Q - 1) & 1, lost, patience))) break;
+          // (lse of four tiles ago: its powers are done, or the products of two tiles ago would not be)
+          const u32 c = mine % PER;
+#pragma unroll 4
+          for (u32 y = 0; y < TC_TILE / STEP; ++y) {
+            const u32 row = y * STEP + mine / PER, rr = r * TC_TILE + row;
+            const u32 dst = sq + st * S::Q + (c / 8) * (TC_TILE * 128) + row * 128 + (((c % 8) ^ (row % 8)) * 16);
+            if (rr < j.rows) {
+              const u32 tok = rr / g;
+              const u16 *const src = (const u16 *)a.q + (u64)(j.t0 + tok) * a.q_ts + (u64)(h * g + rr - tok * g) * a.q_hs + c * 8;
+              if (((uintptr_t)src & 15) == 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+              else {
+                u32 v[4];
+#pragma unroll
+                for (u32 z = 0; z < 4; ++z) v[z] = (u32)src[2 * z] | (u32)src[2 * z + 1] << 16;
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+              }
+            } else {
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
+            }
+          }
+#pragma unroll
+          for (u32 y = 0; y < 2; ++y) {
+            const u32 row = mine * 2 + y, rr = r * TC_TILE + row;
+            float L = INFINITY;          // no row: no weight
+            int index = NO_ROW;
+            if (rr < j.rows) {
+              const u32 tok = rr / g;
+              L = lse_log2(a.lse[(u64)(j.t0 + tok) * a.n_q_heads + h * g + rr - tok * g]).high;
+              index = (int)(j.index0 + tok);
+            }
+            s_l[ls][row] = L; s_index[ls][row] = index;
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) { bar_arrive(lfull + ls * 8); bar_arrive(qfull + st * 8); }
+        }
+        if (++r == j.tiles) { r = 0; ++h; }
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+    // ---- powers and their sums: a thread per key
+    const u32 tile = warp / 4, key_t = tid % TC_TILE, from = tmem + ((warp % 4) << 21) + tile * 128;
+    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
+    const u64 scale2 = pack2(a.scale_log2, a.scale_log2);
+    u32 n = 0;
+    bool ok = true;
+    for (WeighJob j; ok && next_job(j);) {
+      const u32 key = j.key0 + tile * TC_TILE + key_t;
+      float sum = 0.0f;
+      u32 r = j.x0 % j.tiles;
+      for (u32 i = j.x0; i < j.x1; ++i, ++n) {
+        const u32 buf = n % 2, ls = n % WTC_L;
+        const u32 cols = min(TC_TILE, j.rows - r * TC_TILE);
+        // tokens of this tile: the first and the last
+        const u32 index0 = j.index0 + r * TC_TILE / g, index1 = j.index0 + (r * TC_TILE + cols - 1) / g;
+        const u32 k0 = j.key0 + tile * TC_TILE, k1 = min(k0 + TC_TILE, j.kv);       // this warpgroup's keys
+        const bool whole = cols == TC_TILE && (a.full || k1 <= index0 + 1) && (!a.window || (u64)k0 + a.window > index1);
+        if (!(ok = tc_wait(lfull + ls * 8, (n / WTC_L) & 1, lost, patience) && tc_wait(sfull + buf * 8, (n / 2) & 1, lost, patience))) break;
+        tc_after();
+        u64 part[2] = {0, 0};
+        u32 v[2][32];
+        tc_ld32(v[0], from + buf * 256);
+        const u32 chunks = (cols + 31) / 32;
+#pragma unroll
+        for (u32 c = 0; c < 4; ++c) {
+          if (c < chunks) {
+            tc_wait_ld();
+            if (c + 1 < 4) { if (c + 1 < chunks) tc_ld32(v[(c + 1) & 1], from + buf * 256 + 32 * (c + 1)); }
+            const float *const s = reinterpret_cast<const float *>(v[c & 1]);
+            if (whole) {
+#pragma unroll
+              for (u32 y = 0; y < 32; y += 4) {
+                const float4 L = *(const float4 *)&s_l[ls][32 * c + y];
+                const float2 p = unpack2(fma2(pack2(s[y], s[y + 1]), scale2, pack2(-L.x, -L.y))), q = unpack2(fma2(pack2(s[y + 2], s[y + 3]), scale2, pack2(-L.z, -L.w)));
+                part[0] = add2(part[0], pack2(ex2(p.x), ex2(p.y)));
+                part[1] = add2(part[1], pack2(ex2(q.x), ex2(q.y)));
+              }
+            } else {
+#pragma unroll
+              for (u32 y = 0; y < 32; y += 4) {
+                const float4 L = *(const float4 *)&s_l[ls][32 * c + y];
+                const int4 at = *(const int4 *)&s_index[ls][32 * c + y];
+                auto power = [&](float z, float l, int index) {
+                  const bool see = a.full ? index != NO_ROW : (int)key <= index && (!a.window || (long long)key + a.window > index);
+                  return see ? ex2(fmaf(z, a.scale_log2, -l)) : 0.0f;
+                };
+                part[0] = add2(part[0], pack2(power(s[y], L.x, at.x), power(s[y + 1], L.y, at.y)));
+                part[1] = add2(part[1], pack2(power(s[y + 2], L.z, at.z), power(s[y + 3], L.w, at.w)));
+              }
+            }
+          }
+        }
+        tc_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(sempty + buf * 8);
+        const float2 all = unpack2(add2(part[0], part[1]));
+        sum += all.x + all.y;
+        if (++r == j.tiles) r = 0;
+      }
+      if (!ok) break;
+      if (key >= j.kv) sum = 0.0f;
+#pragma unroll
+      for (u32 o = 8; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+      if (lane % 16 == 0) sc.sums[j.sum * WTC_KB + key_t / BT + tile * (TC_TILE / BT)] = sum;
+    }
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (tid == 0 && s_lost) kv_err(a.err, KVERR_WAIT);
+}
+
+// Puts the sums of the kernel before together: a thread per block.
+__global__ void __launch_bounds__(256) k_weigh_join(WeighArgs x) {
+  const AttendArgs &a = x.a;
+  const u32 chunks = (a.b.max_blocks + 255) / 256, seq = blockIdx.x / chunks, b = (blockIdx.x - seq * chunks) * 256 + threadIdx.x;
+  // the sequence's first pair
+  u32 before = 0;
+  for (u32 s0 = 0; s0 < seq; s0 += 256) {
+    u32 n = 0;
+    if (s0 + threadIdx.x < seq) n = (load_seq(a.b, s0 + threadIdx.x, a.err).kv + WTC_KEYS - 1) / WTC_KEYS;
+    n = __reduce_add_sync(~0u, n);
+    __shared__ u32 s_n[8];
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) s_n[threadIdx.x / 32] = n;
+    __syncthreads();
+    for (u32 w = 0; w < 8; ++w) before += s_n[w];
+  }
+  const Seq q = load_seq(a.b, seq, a.err);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (b >= a.b.max_blocks) return;
+  float sum = 0.0f;
+  const bool held = b < (q.kv + BT - 1) / BT;
+  if (held) {
+    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
+    const u64 per = sc.per[0], total = sc.per[1];
+    const u32 pair = before + b / WTC_KB;
+    if (total) {
+      const u64 from = sc.place[pair], to = sc.place[pair + 1];
+      if (from < to) for (u64 c = from / per; c <= (to - 1) / per; ++c) sum += sc.sums[(pair + c) * WTC_KB + b % WTC_KB];
+    }
+    if (x.weights) sum += x.keep * x.weights[seq * x.w_stride + b];
+  }
+  x.out[seq * x.o_stride + b] = held ? sum : 0.0f;
+}
+
+// Few rows or many. (One tile of 128 rows costs the second kernel as much as one row.)
+constexpr u32 WEIGH_FEW = 32;
+WeighPlan plan_weigh(const WeighArgs &x, u32 max_q_len, int sm_count) {
+  WeighPlan p{};
+  const u32 d = x.a.p.head_dim;
+  const u64 rows = (u64)(max_q_len && max_q_len < x.a.b.n_tokens ? max_q_len : x.a.b.n_tokens) * x.a.group;
+  p.many = (d == 64 || d == 128) && rows > WEIGH_FEW;
+  p.grid = sm_count;
+  if (p.many) {
+    const u64 pairs = weigh_pairs(x.a.b.n_seqs, x.a.b.max_blocks);
+    p.scratch_bytes = ((16 + 8 * (pairs + 1) + 15) & ~15ull) + (pairs + p.grid) * WTC_KB * 4;
+  }
+  return p;
+}
+
+template <class T, u32 D>
+static cudaError_t launch_weigh_tc(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
+  cudaError_t r = allow_smem(k_weigh_tc<T, D>, 3 + (D == 128) * 2 + __is_same(T, __half), WeighShape<D>::SMEM, allowed);
+  if (r != cudaSuccess) return r;
+  k_weigh_tc<T, D><<<p.grid, WTC_THREADS, WeighShape<D>::SMEM, s>>>(x, m);
+  ++*launches;
+  if ((r = cudaGetLastError()) != cudaSuccess) return r;
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3(x.a.b.n_seqs * ((x.a.b.max_blocks + 255) / 256)); c.blockDim = dim3(256); c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at; c.numAttrs = 1;
+  ++*launches;
+  return cudaLaunchKernelEx(&c, k_weigh_join, x);
+}
+cudaError_t launch_weigh(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
   const u32 ctas = x.a.b.n_seqs * ((x.a.b.max_blocks + 7) / 8), d = x.a.p.head_dim;
+  if (p.many) {
+    if (d == 64) return x.a.fp16 ? launch_weigh_tc<__half, 64>(x, p, m, s, allowed, launches) : launch_weigh_tc<__nv_bfloat16, 64>(x, p, m, s, allowed, launches);
+    return x.a.fp16 ? launch_weigh_tc<__half, 128>(x, p, m, s, allowed, launches) : launch_weigh_tc<__nv_bfloat16, 128>(x, p, m, s, allowed, launches);
+  }
   ++*launches;
   if (x.a.fp16) {
     if (d <= 64) k_weigh<__half, 2><<<ctas, 256, 0, s>>>(x);

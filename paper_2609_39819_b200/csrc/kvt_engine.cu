@@ -2442,8 +2442,8 @@ int32_t kvt_attend_blocks(kvt_engine *e, const kvt_attend_blocks_args *args, voi
 }
 
 uint64_t kvt_weigh_scratch_bytes(kvt_engine *e, const kvt_weigh_args *args) {
-  if (!e || !args || weigh_fault(e, *args) || !args->b.n_seqs || !args->b.n_tokens) return 0;
-  return 0;
+  if (!e || !args || weigh_fault(e, *args) || !args->b.n_seqs || !args->b.max_blocks) return 0;
+  return plan_weigh(weigh_args(e, *args), args->b.max_q_len, e->sm_count).scratch_bytes;
 }
 
 int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *args, void *stream) {
@@ -2456,8 +2456,14 @@ int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *args, void *stream
   if (!a.b.q_start || !a.b.kv_len || !a.b.block_table) return fail(e, KVT_E_INVAL, "weigh: batch without starts, lengths or block table");
   OnDevice on(e->device);
   if (!on.ok) return fail(e, KVT_E_CUDA, "weigh: device");
+  const WeighArgs x = weigh_args(e, a);
+  const WeighPlan p = plan_weigh(x, a.b.max_q_len, e->sm_count);
+  if (p.scratch_bytes) {
+    if (!a.scratch || a.scratch_bytes < p.scratch_bytes) return fail(e, KVT_E_BUFSZ, "weigh: scratch too small");
+    if ((uintptr_t)a.scratch & 15) return fail(e, KVT_E_INVAL, "weigh: misaligned scratch");
+  }
   u32 launches = 0;
-  const cudaError_t r = launch_weigh(weigh_args(e, a), (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  const cudaError_t r = launch_weigh(x, p, e->kv_maps, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
   return kv_launched(e, r, launches);
 }
 

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libkvt.so: argument marshalling only (that of append_kv and attend natively where _kvt_torch*.so can be had). Every stage of the path (hashing,
+"""Thin ctypes binding of libkvt.so: argument marshalling only (that of the model-side calls natively where _kvt_torch*.so can be had). Every stage of the path (hashing,
 table lookup, classification, victim selection, block movement) runs in the library's CUDA kernels.
 PyTorch is used for device / pinned memory and streams, nothing else. There is no CPU fallback:
 loading fails loudly when the library or a CUDA device is missing."""
@@ -253,6 +253,20 @@ def _native_calls(lib):
             functools.partial(native.attend, entry(lib.kvt_attend), entry(lib.kvt_attend_scratch_bytes)))
 
 
+def _native_block_calls(lib):
+    """The same for bound_keys, select_blocks, attend_blocks, weigh_blocks and evict_blocks."""
+    try:
+        native = load_native()
+    except RuntimeError:        # _native_calls has said so
+        return (lambda *args: NotImplemented,) * 5
+    entry = lambda f: C.cast(f, C.c_void_p).value      # noqa: E731
+    return (functools.partial(native.bound, entry(lib.kvt_bound_keys)),
+            functools.partial(native.select, entry(lib.kvt_select_blocks), entry(lib.kvt_select_scratch_bytes)),
+            functools.partial(native.attend_blocks, entry(lib.kvt_attend_blocks)),
+            functools.partial(native.weigh, entry(lib.kvt_weigh_blocks), entry(lib.kvt_weigh_scratch_bytes)),
+            functools.partial(native.evict, entry(lib.kvt_evict_blocks)))
+
+
 def _p(a):
     return a.ctypes.data_as(C.c_void_p) if a is not None else None
 
@@ -416,6 +430,8 @@ class Engine:
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._append_native, self._attend_native = _native_calls(self.L)
+        self._bound_native, self._select_native, self._attend_blocks_native, self._weigh_native, self._evict_native = \
+            _native_block_calls(self.L)
         self.tail_pool = None
         if n_tail_blocks:       # blocks outside every tier: slot ids n_hbm_blocks + i of append_kv and attend
             self.set_tail_pool((torch.zeros if zero_pools else torch.empty)(n_tail_blocks * self.block_bytes, dtype=torch.uint8,
@@ -807,6 +823,14 @@ class Engine:
         append_kv with the same batch; n_tokens: rows of that batch. After blocks have come into their slots in another way
         (reload, a prefix that was there), a batch that counts their tokens as new makes their bounds. Asynchronous on the current
         stream."""
+        done = self._bound_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                                  self.n_layers, layer, self._kv_dtypes.get(bounds.dtype), bounds.codes, bounds.exps, block_table, q_start,
+                                  kv_len, n_tokens)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "bound_keys")
+            return None
+        # something is not as it should be (what, is said here), or only of another type than it might be
         if layer < 0 or n_tokens < 0:
             raise ValueError("bound_keys: layer and n_tokens cannot be negative")
         batch = self._kv_batch("bound_keys", n_tokens, block_table, q_start, kv_len, 0)
@@ -819,6 +843,14 @@ class Engine:
         to the token's own; the others are those of the largest scores by `bounds` (include/kvt.h says how they are reckoned; they are
         exact, so that neither the batch nor the kernel has a say). q: rotated queries, batch as in attend; rows behind the last
         sequence stay as they are. Asynchronous on the current stream."""
+        done = self._select_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                                   self.n_layers, layer, self._kv_dtypes.get(bounds.dtype), q, bounds.codes, bounds.exps, block_table,
+                                   q_start, kv_len, n_blocks, first, last, max_q_len, out)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "select_blocks")
+            return done
+        # something is not as it should be (what, is said here), or only of another type than it might be
         torch = self.torch
         if layer < 0 or (max_q_len or 0) < 0 or min(first, last, n_blocks) < 0:
             raise ValueError("select_blocks: layer, max_q_len, first, last and n_blocks cannot be negative")
@@ -845,6 +877,13 @@ class Engine:
         """attend over the keys, up to each token's own, in the blocks that `blocks` (int32 [tokens, KV heads, n], contiguous, as
         select_blocks gives them) names for it. Entries below 0 and blocks behind the token's own count for nothing; lists may be in
         any order, without a block twice. Other arguments, precision and result as in attend."""
+        done = self._attend_blocks_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                                          layer, q, blocks, block_table, q_start, kv_len, scale, out, lse)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "attend_blocks")
+            return done
+        # something is not as it should be (what, is said here), or only of another type than it might be
         torch = self.torch
         if layer < 0:
             raise ValueError("attend_blocks: layer cannot be negative")
@@ -874,6 +913,13 @@ class Engine:
         tokens, query heads and the block's keys, of the weights exp(scale q k - lse) that attend gave them. q, lse, causal, window
         and scale are those of that call of attend. weights: from earlier steps or layers (none: zeros); out: written if given, may be
         `weights`. Blocks behind kv_len get 0. Asynchronous on the current stream."""
+        done = self._weigh_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                                  layer, q, lse, block_table, q_start, kv_len, max_q_len, causal, window, scale, weights, keep, out)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "weigh_blocks")
+            return done
+        # something is not as it should be (what, is said here), or only of another type than it might be
         torch = self.torch
         if layer < 0 or (max_q_len or 0) < 0 or (window or 0) < 0:
             raise ValueError("weigh_blocks: layer, max_q_len and window cannot be negative")
@@ -906,6 +952,14 @@ class Engine:
         then -1. out: four tensors to write, of which the first three may be block_table, kv_len and weights themselves. Slots of the
         HBM tier go back with release(). Keys stay rotated by their old positions: append_kv needs `positions` from here on.
         Asynchronous on the current stream."""
+        done = NotImplemented if out is not None else \
+            self._evict_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
+                               weights, block_table, kv_len, n_blocks, first, last)
+        if done is not NotImplemented:
+            if type(done) is int:
+                self._check(done, "evict_blocks")
+            return done
+        # something is not as it should be (what, is said here), or only of another type than it might be
         torch = self.torch
         if min(n_blocks, first, last) < 0:
             raise ValueError("evict_blocks: n_blocks, first and last cannot be negative")

@@ -1541,24 +1541,40 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
 // ------------------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+  static const EncodeTiled found = []() -> EncodeTiled {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult got;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+        got != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    return (EncodeTiled)fn;
+  }();
+  return found;
+}
 bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, u64 n_slots, u64 n_chunks, u64 n_kv_heads, u64 head_dim) {
-  typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                             const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  void *fn = nullptr;
-  cudaDriverEntryPointQueryResult got;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &got) != cudaSuccess ||
-      got != cudaDriverEntryPointSuccess || !fn) {
-    cudaGetLastError();
-    return false;
-  }
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
   const u64 tok = n_kv_heads * head_dim * 2, chunk = BT * tok;
   // 64 elements | 8 tokens | 64-element parts of a token's heads | halves of blocks | the other index
   const cuuint64_t dims[5] = {64, 8, n_kv_heads * head_dim / 64, 2 * (layer_major ? n_slots : n_chunks), layer_major ? n_chunks : n_slots};
   const cuuint64_t strides[4] = {tok, 128, 8 * tok, chunk * (layer_major ? n_slots : n_chunks)};
   const cuuint32_t box[5] = {64, 8, (cuuint32_t)(head_dim / 64), 2, 1}, es[5] = {1, 1, 1, 1, 1};
-  return ((Encode)fn)(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool make_row_map(CUtensorMap *m, const void *rows, u64 head_dim, u64 n_heads, u64 n_tokens, u64 head_stride, u64 token_stride, u32 heads, u32 tokens) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode || ((uintptr_t)rows & 15) || head_stride % 8 || token_stride % 8 || !head_stride || !token_stride || token_stride >> 38 || head_stride >> 38) return false;
+  const cuuint64_t dims[3] = {head_dim, n_heads, n_tokens}, strides[2] = {head_stride * 2, token_stride * 2};
+  const cuuint32_t box[3] = {64, heads, tokens}, es[3] = {1, 1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(rows), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <class... Exp, class... Act>

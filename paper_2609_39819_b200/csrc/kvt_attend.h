@@ -51,6 +51,10 @@ struct AttendArgs {
 struct KvMaps { CUtensorMap pool, tail; };
 bool make_kv_map(CUtensorMap *m, void *base, bool layer_major, uint64_t n_slots, uint64_t n_chunks, uint64_t n_kv_heads,
                  uint64_t head_dim);
+// Tensor map of a batch's rows [token][head][channel], for boxes of 64 channels of `heads` heads of `tokens` tokens, with 128-byte swizzle.
+// false: they do not lie as TMA wants them.
+bool make_row_map(CUtensorMap *m, const void *rows, uint64_t head_dim, uint64_t n_heads, uint64_t n_tokens, uint64_t head_stride, uint64_t token_stride,
+                  uint32_t heads, uint32_t tokens);
 
 // What kvt_attend does, decided from sizes alone.
 struct AttendPlan {
@@ -108,11 +112,12 @@ struct EvictArgs {
   uint32_t *err;
 };
 
+// allowed: two words of such bits
 cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, uint32_t *launches);
 cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 cudaError_t launch_attend_blocks(const AttendListArgs &a, const KvMaps &m, int sm_count, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 // What kvt_weigh_blocks does, decided from sizes alone.
-struct WeighPlan { uint32_t many, grid; uint64_t scratch_bytes; };
+struct WeighPlan { uint32_t many, grid, tile, share; uint64_t scratch_bytes; };
 WeighPlan plan_weigh(const WeighArgs &a, uint32_t max_q_len, int sm_count);
 cudaError_t launch_weigh(const WeighArgs &a, const WeighPlan &p, const KvMaps &m, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s, uint64_t *allowed, uint32_t *launches);

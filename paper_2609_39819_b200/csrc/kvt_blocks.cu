@@ -857,6 +857,12 @@ __device__ __forceinline__ Lse lse_log2(float lse) {
   return r;
 }
 
+// First block that any new token of a sequence sees: those in front of the window are not read and need no valid slot.
+__device__ __forceinline__ u32 first_seen(const AttendArgs &a, const Seq &q) {
+  const long long lo = a.window ? (long long)q.kv - q.n + 1 - (long long)a.window : 0;
+  return lo > 0 ? (u32)(lo / BT) : 0u;
+}
+
 // 16 bytes from 8 elements at p, of which n_left exist.
 __device__ __forceinline__ uint4 load8(const u16 *p, int n_left, bool vec) {
   if (n_left >= 8 && vec) return *(const uint4 *)p;
@@ -866,43 +872,176 @@ __device__ __forceinline__ uint4 load8(const u16 *p, int n_left, bool vec) {
   return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-// Eight blocks of one sequence per CTA. The block's 16 keys are the rows of the matrix instruction, eight (token, head) rows the
-// columns; a lane's 16 bytes of a key and of a query are operands if channels are counted in that order on both sides, so both go
-// from memory to registers.
-template <class T, u32 G>      // G: 64-byte parts of a head
-__global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
-  __shared__ float s_sum[8][8];
+// Few rows (a new token per sequence), heads of 64 and 128: bound by reading K once. A CTA of four warps takes a tile of up to 32 blocks of one
+// sequence, each warp every fourth head of it, with a ring of TMA loads of its own (a block's keys of one head per stage). The block's 16
+// keys are the rows of the matrix instruction, eight (token, head) rows the columns, which stay in registers for all blocks of a head.
+// Lane i holds the sum of block i. Two CTAs per SM keep 192 KB of loads in flight.
+constexpr u32 WEIGH_TILE = 32, WS_WARPS = 4, WS_THREADS = WS_WARPS * 32;
+template <u32 D> struct WeighRing { static constexpr u32 BLOCK = BT * D * 2, STAGES = D == 64 ? 12 : 6, RING = STAGES * BLOCK, SMEM = WS_WARPS * RING + 1024; };
+template <class T, u32 D, u32 NT>
+__global__ void __launch_bounds__(WS_THREADS, 2) k_weigh_split(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps maps, u32 n_tile) {
+  typedef WeighRing<D> S;
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 bars[WS_WARPS * S::STAGES];
+  __shared__ float s_sum[WS_WARPS][WEIGH_TILE];
   const AttendArgs &a = x.a;
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads, g = a.group;
-  const u32 tiles = (a.b.max_blocks + 7) / 8, seq = blockIdx.x / tiles, b_tile = (blockIdx.x - seq * tiles) * 8;
+  const u32 tiles = (a.b.max_blocks + n_tile - 1) / n_tile, seq = blockIdx.x / tiles, b_tile = (blockIdx.x - seq * tiles) * n_tile;
+  const Seq q = load_seq(a.b, seq, a.err);
+  const u32 n_held = (q.kv + BT - 1) / BT, b0 = max(b_tile, first_seen(a, q)), b1 = min(b_tile + n_tile, n_held), nb = b1 > b0 && q.n ? b1 - b0 : 0;
+  bool ok = true;
+  if (nb) {
+    const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8, ring = ((smem_addr(smem_raw) + 1023) & ~1023u) + warp * S::RING;
+    u32 held = ~0u;                      // lane i: slot of block i
+    if (lane < nb) {
+      held = a.b.table[seq * a.b.table_stride + b0 + lane];
+      if (held >= a.p.n_slots && held - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+    }
+    if (lane == 0) {
+      for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncwarp();
+    const u32 rows = q.n * g, n_rounds = (rows + NT * 8 - 1) / (NT * 8), n_heads = warp < H ? (H - warp + WS_WARPS - 1) / WS_WARPS : 0, n_items = n_rounds * n_heads * nb;
+    const int shift = (int)q.kv - (int)q.n;                      // index of the first new token
+    u32 load_b = 0, load_h = warp, load_st = 0;                  // the next item to load
+    auto load = [&]() {
+      const u32 slot = __shfl_sync(~0u, held, load_b);
+      if (lane == 0) {
+        bar_expect(bar0 + load_st * 8, S::BLOCK);
+        load_block(a, maps, ring + load_st * S::BLOCK, bar0 + load_st * 8, slot, 2 * a.layer, load_h, D / 64);
+      }
+      if (++load_st == S::STAGES) load_st = 0;
+      if (++load_b == nb) { load_b = 0; load_h += WS_WARPS; if (load_h >= H) load_h = warp; }
+    };
+    for (u32 i = 0; i < min(S::STAGES, n_items); ++i) load();
+    float acc = 0.0f;
+    u32 it = 0, st = 0, phase = 0;
+    for (u32 r0 = 0; ok && r0 < rows; r0 += NT * 8)
+      for (u32 h = warp; ok && h < H; h += WS_WARPS) {
+        u32 qf[NT][D / 16][2];
+        Lse L[NT][2];
+        int lo[NT][2], hi[NT][2];        // keys that columns 2 (lane % 4) and the next see
+#pragma unroll
+        for (u32 c = 0; c < NT; ++c) {
+          const u32 r = min(r0 + c * 8 + lane / 4, rows - 1), tok = r / g;
+          const u16 *const src = (const u16 *)a.q + (u64)(q.t0 + tok) * a.q_ts + (u64)(h * g + r - tok * g) * a.q_hs + lane % 4 * 2;
+          const bool even = ((uintptr_t)src & 3) == 0;
+#pragma unroll
+          for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+            for (u32 z = 0; z < 2; ++z) {
+              const u16 *const p = src + k * 16 + z * 8;
+              qf[c][k][z] = even ? *(const u32 *)p : (u32)p[0] | (u32)p[1] << 16;
+            }
+#pragma unroll
+          for (u32 z = 0; z < 2; ++z) {
+            const u32 rr = r0 + c * 8 + lane % 4 * 2 + z, tk = min(rr, rows - 1) / g;
+            L[c][z] = lse_log2(a.lse[(u64)(q.t0 + tk) * a.n_q_heads + h * g + min(rr, rows - 1) - tk * g]);
+            hi[c][z] = rr >= rows ? 0 : a.full ? (int)q.kv : max(0, shift + (int)tk + 1);
+            lo[c][z] = a.window ? hi[c][z] - (int)min(a.window, 0x7FFFFFFFu) : 0;
+          }
+        }
+        for (u32 b = 0; b < nb; ++b, ++it) {
+          if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, phase)))) break;
+          const u32 kb = ring + st * S::BLOCK;
+          float s[NT][4];
+#pragma unroll
+          for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+            for (u32 y = 0; y < 4; ++y) s[c][y] = 0.0f;
+#pragma unroll
+          for (u32 k = 0; k < D / 16; ++k) {
+            u32 f[4];
+            ldm4(f, kb + block_off<D>(lane % 16, 2 * k + lane / 16));
+#pragma unroll
+            for (u32 c = 0; c < NT; ++c) mma16816<T>(s[c], f, qf[c][k][0], qf[c][k][1]);
+          }
+          __syncwarp();                  // the stage is read
+          if (it + S::STAGES < n_items) load();
+          if (++st == S::STAGES) { st = 0; phase ^= 1; }
+          const int key0 = (int)((b0 + b) * BT + lane / 4);
+          float sum = 0.0f;
+#pragma unroll
+          for (u32 c = 0; c < NT; ++c)
+#pragma unroll
+            for (u32 y = 0; y < 4; ++y) {
+              const int key = key0 + (int)(y / 2) * 8;
+              const float e = ex2(fmaf(s[c][y], a.scale_log2, -L[c][y & 1].high) + fmaf(s[c][y], x.scale_low, -L[c][y & 1].low));
+              sum += key < hi[c][y & 1] && key >= lo[c][y & 1] ? e : 0.0f;
+            }
+          sum = sum_over_warp(sum);
+          if (lane == b) acc += sum;
+        }
+      }
+    s_sum[warp][lane] = acc;
+    if (__syncthreads_or(!ok)) {         // let the copies in flight land, for a while, before the CTA ends; nothing is written
+      if (lane == 0) kv_err(a.err, KVERR_WAIT);
+      for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
+      return;
+    }
+  }
+  if (tid < n_tile && b_tile + tid < a.b.max_blocks) {
+    const u32 b = b_tile + tid;
+    float sum = 0.0f;
+    if (b >= b0 && b < b0 + nb) for (u32 w = 0; w < WS_WARPS; ++w) sum += s_sum[w][b - b0];
+    if (x.weights) sum += x.keep * x.weights[seq * x.w_stride + b];
+    x.out[seq * x.o_stride + b] = b < n_held ? sum : 0.0f;
+  }
+}
+
+// Heads of every other size, any number of rows. `share` warps work on a block, each on every so many-th head; a lane's 16 bytes of a key and
+// of a query are operands of the matrix instruction if channels are counted in that order on both sides, so both go from memory to
+// registers. The next (block, head)'s keys are on their way while one is worked on.
+constexpr u32 WEIGH_LSE = 512;
+template <class T, u32 G>      // G: 64-byte parts of a head
+__global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n_tile, u32 share) {
+  __shared__ float s_sum[8][WEIGH_TILE];
+  __shared__ Lse s_lse[WEIGH_LSE];
+  const AttendArgs &a = x.a;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads, g = a.group;
+  const u32 tiles = (a.b.max_blocks + n_tile - 1) / n_tile, seq = blockIdx.x / tiles, b_tile = (blockIdx.x - seq * tiles) * n_tile;
   const Seq q = load_seq(a.b, seq, a.err);
   const u32 n_held = (q.kv + BT - 1) / BT;
-  const u32 WH = H >= 8 ? 8 : H >= 4 ? 4 : H >= 2 ? 2 : 1;     // warps that share the heads; each has WH of the blocks
-  const int shift = (int)q.kv - (int)q.n;                      // index of the first new token
-  const u32 j = lane % 4, r8 = lane / 4, d = a.p.head_dim;
-  if (lane < 8) s_sum[warp][lane] = 0.0f;
-  __syncwarp();
-  for (u32 h = warp % WH; h < H; h += WH)
-    for (u32 y = 0; y < WH; ++y) {
-      const u32 which = warp / WH * WH + y, b = b_tile + which;
-      if (b >= n_held || !q.n) continue;
+  if (b_tile < n_held && q.n) {
+    const bool staged = (u64)q.n * a.n_q_heads <= WEIGH_LSE;
+    if (staged) {
+      for (u32 i = tid; i < q.n * a.n_q_heads; i += 256) s_lse[i] = lse_log2(a.lse[(u64)q.t0 * a.n_q_heads + i]);
+      __syncthreads();
+    }
+    const int shift = (int)q.kv - (int)q.n;                      // index of the first new token
+    const u32 j = lane % 4, r8 = lane / 4, d = a.p.head_dim;
+    // this warp's blocks b_tile + first + step * i and heads sub + share * k
+    const u32 first = warp / share, step = 8 / share, sub = warp % share;
+    const u32 n_blocks = min(n_tile, n_held - b_tile) > first ? (min(n_tile, n_held - b_tile) - first + step - 1) / step : 0, n_heads = sub < H ? (H - sub + share - 1) / share : 0;
+    u32 held = ~0u;                      // lane i: slot of block i
+    if (lane < n_blocks && b_tile + first + step * lane >= first_seen(a, q)) {
+      held = a.b.table[seq * a.b.table_stride + b_tile + first + step * lane];
+      if (held >= a.p.n_slots && held - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
+    }
+    struct Keys { uint4 v[G][2]; };
+    auto load = [&](u32 i, u32 k) {
+      Keys x;
+      const u16 *const src = (const u16 *)slot_ptr(a.p, a.p.k, __shfl_sync(~0u, held, i));
+      const bool vec = d % 8 == 0 && ((uintptr_t)src & 15) == 0;
+#pragma unroll
+      for (u32 y = 0; y < G; ++y)
+#pragma unroll
+        for (u32 z = 0; z < 2; ++z) {
+          const u32 c = y * 32 + j * 8;
+          x.v[y][z] = src && c < d ? load8(src + ((u64)(r8 + 8 * z) * H + sub + share * k) * d + c, (int)d - (int)c, vec) : make_uint4(0, 0, 0, 0);
+        }
+      return x;
+    };
+    float total = 0.0f;                  // of the block, over the heads
+    // of one block and head
+    auto work = [&](const Keys &keys, u32 i, u32 k) {
+      const u32 h = sub + share * k, b = b_tile + first + step * i;
       // rows that see any of the block's keys: tokens with index >= first key, and inside the window
       const int key0 = (int)(b * BT);
       const u32 tok0 = a.full ? 0 : (u32)max(0, key0 - shift);
       const u32 tok1 = a.window ? (u32)max(0ll, min((long long)q.n, (long long)key0 + BT - 1 + a.window - shift)) : q.n;
-      if (tok0 >= tok1) continue;
-      const u32 slot = a.b.table[seq * a.b.table_stride + b];
-      const u16 *const src = (const u16 *)slot_ptr(a.p, a.p.k, slot);
-      if (!src) { if (lane == 0) kv_err(a.err, KVERR_RANGE); }
-      uint4 k[G][2];
-      const bool vec = d % 8 == 0 && ((uintptr_t)src & 15) == 0;
-#pragma unroll
-      for (u32 i = 0; i < G; ++i)
-#pragma unroll
-        for (u32 z = 0; z < 2; ++z) {
-          const u32 c = i * 32 + j * 8;
-          k[i][z] = src && c < d ? load8(src + ((u64)(r8 + 8 * z) * H + h) * d + c, (int)d - (int)c, vec) : make_uint4(0, 0, 0, 0);
-        }
       float sum = 0.0f, part = 0.0f;
       u32 count = 0;
       for (u32 r0 = tok0 * g; r0 < tok1 * g; r0 += 8) {
@@ -911,10 +1050,10 @@ __global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
         const bool qvec = d % 8 == 0 && ((uintptr_t)qs & 15) == 0;
         float s[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (u32 i = 0; i < G; ++i) {
-          const u32 c = i * 32 + j * 8;
+        for (u32 y = 0; y < G; ++y) {
+          const u32 c = y * 32 + j * 8;
           const uint4 v = c < d ? load8(qs + c, (int)d - (int)c, qvec) : make_uint4(0, 0, 0, 0);
-          const u32 f0[4] = {k[i][0].x, k[i][1].x, k[i][0].y, k[i][1].y}, f1[4] = {k[i][0].z, k[i][1].z, k[i][0].w, k[i][1].w};
+          const u32 f0[4] = {keys.v[y][0].x, keys.v[y][1].x, keys.v[y][0].y, keys.v[y][1].y}, f1[4] = {keys.v[y][0].z, keys.v[y][1].z, keys.v[y][0].w, keys.v[y][1].w};
           mma16816<T>(s, f0, v.x, v.y);
           mma16816<T>(s, f1, v.z, v.w);
         }
@@ -922,8 +1061,8 @@ __global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
         for (u32 z = 0; z < 2; ++z) {
           const u32 rr = r0 + 2 * j + z;
           if (rr >= tok1 * g) continue;
-          const u32 tk = rr / g;
-          const Lse L = lse_log2(a.lse[(u64)(q.t0 + tk) * a.n_q_heads + h * g + rr - tk * g]);
+          const u32 tk = rr / g, at = tk * a.n_q_heads + h * g + rr - tk * g;
+          const Lse L = staged ? s_lse[at] : lse_log2(a.lse[(u64)q.t0 * a.n_q_heads + at]);
           const int own = shift + (int)tk, hi = a.full ? (int)q.kv : own + 1, lo = a.window ? hi - (int)min(a.window, 0x7FFFFFFFu) : 0;
 #pragma unroll
           for (u32 w = 0; w < 2; ++w) {
@@ -934,14 +1073,38 @@ __global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
         }
         if (++count % 32 == 0) { sum += part; part = 0.0f; }   // sums of few, then of those: 32 bits hold them
       }
-      sum = sum_over_warp(sum + part);
-      if (lane == 0) s_sum[warp][which] += sum;
+      total += sum + part;
+      if (k + 1 == n_heads) {            // the block is through
+        total = sum_over_warp(total);
+        if (lane == 0) s_sum[warp][first + step * i] = total;
+        total = 0.0f;
+      }
+    };
+    const u32 n_items = n_blocks * n_heads;
+    u32 i = 0, k = 0;                    // the item in hand
+    auto after = [&](u32 &i, u32 &k) { if (++k == n_heads) { k = 0; ++i; } };
+    if (n_items) {
+      Keys one = load(0, 0), two;
+      for (u32 it = 0; it < n_items; it += 2) {
+        u32 i1 = i, k1 = k;
+        after(i1, k1);
+        if (it + 1 < n_items) two = load(i1, k1);
+        work(one, i, k);
+        if (it + 1 >= n_items) break;
+        i = i1; k = k1;
+        after(i, k);
+        if (it + 2 < n_items) one = load(i, k);
+        work(two, i1, k1);
+      }
+    } else if (n_blocks) {               // more warps than heads
+      if (lane < n_blocks) s_sum[warp][first + step * lane] = 0.0f;
     }
-  __syncthreads();
-  if (tid < 8 && b_tile + tid < a.b.max_blocks) {
+    __syncthreads();
+  }
+  if (tid < n_tile && b_tile + tid < a.b.max_blocks) {
     const u32 b = b_tile + tid;
     float sum = 0.0f;
-    for (u32 w = 0; w < 8; ++w) sum += s_sum[w][tid];
+    if (b < n_held && q.n) for (u32 w = tid % (8 / share) * share, y = 0; y < share; ++y) sum += s_sum[w + y][tid];
     if (x.weights) sum += x.keep * x.weights[seq * x.w_stride + b];
     x.out[seq * x.o_stride + b] = b < n_held ? sum : 0.0f;
   }
@@ -949,20 +1112,72 @@ __global__ void __launch_bounds__(256) k_weigh(WeighArgs x) {
 
 // Many rows (prompts, chunks). Here the keys are the rows of the matrix instruction as well: S^T = K Q^T for 256 keys, two tiles of
 // 128, by 128 (token, head) rows, so that a thread owns a key and adds up what its row of S^T gives in a register, with no
-// exchange between threads and no masks but at the diagonal.
-//   warps 0-7    a thread per key: powers and their sum
-//   warp 8       issues the products, S^T in tensor memory, held twice: 2 x 2 x 128 columns
-//   warp 9       works out what this CTA does
-//   warp 10      loads K (TMA, a box per block), 256 keys of a head per stage
-//   warps 11-14  bring queries, 128 rows per stage, and their lse; two warps for every other stage
-// Work: for each 256 keys of each sequence ("a pair" of tiles) the tiles of 128 rows that see any of them, head by head. All of it,
+// exchange between threads and no masks but at the diagonal. The row's lse comes off in the product itself: with 16 channels more,
+// constants on the side of K and the parts of -lse / scale in the element type on the side of Q, S^T is (s - lse / scale) in 32 bits,
+// and a power is one multiplication and ex2. (With lse from shared memory and a fused multiply-add it was bound by shared memory, which
+// the products alone keep busy half of the time: 8192 tokens, 8 x 4 heads of 128, 352 us.)
+//   warps 0-15   two threads per key, each for half of the rows: powers and their sum
+//   warp 16      issues the products, S^T in tensor memory, held twice: 2 x 2 x 128 columns
+//   warp 17      works out what this CTA does
+//   warp 18      loads K (TMA, a box per block), 128 keys of a head per stage, three stages: two in use, one ahead
+//   warps 19-22  bring queries, up to 128 rows per stage (TMA where they lie as it wants them), and their lse; two warps for every other stage
+// A tile of rows is as many tokens as fit 128 / group: rows are the same (token, head of the group) in every tile, and one box of TMA.
+// Work: for each 256 keys of each sequence ("a pair" of tiles) the tiles of rows that see any of them, head by head. All of it,
 // one tile after the other, is dealt out in equal stretches, one per CTA; a pair that several CTAs work on is put together from
 // their sums by the kernel behind, always in the same order.
-constexpr int NO_ROW = -0x7FFFFFFF - 1;
-constexpr u32 WTC_KEYS = 256, WTC_KB = WTC_KEYS / BT, WTC_THREADS = 480, WTC_JOBS = 4, WTC_Q = 2, WTC_L = 4;
+constexpr u32 WTC_KEYS = 256, WTC_KB = WTC_KEYS / BT, WTC_THREADS = 736, WTC_JOBS = 4, WTC_Q = 3, WTC_K = 3;
 template <u32 D> struct WeighShape {
-  static constexpr u32 BLOCK = BT * D * 2, K = WTC_KEYS * D * 2, Q = TC_TILE * D * 2, SMEM = 2 * K + WTC_Q * Q + 1024;
+  static constexpr u32 BLOCK = BT * D * 2, K = TC_TILE * D * 2, Q = TC_TILE * D * 2, EXTRA = TC_TILE * 32, SMEM = WTC_K * K + WTC_Q * Q + (WTC_Q + 1) * EXTRA + 1024;
 };
+// The 16 channels more, [row / 8][channel / 8][row % 8][channel % 8] without swizzle (lbo = 128: next 8 channels, sbo = 256: next 8 rows).
+// Channels 1 to 4 carry parts of -lse / scale over ALPHA = 2^-e, where the scale (of powers of two) is 2^e to 2^(e+1), channel 0 a coarse
+// part over 2^15 first in fp16, whose numbers end at 2^16.
+__device__ __forceinline__ u64 plain_desc(u32 addr) { return (u64)((addr & 0x3FFFF) >> 4) | (u64)(128 >> 4) << 16 | (u64)(256 >> 4) << 32 | 1ull << 46; }
+__device__ __forceinline__ float extra_alpha(float scale_log2) { return __uint_as_float((254u - (__float_as_uint(scale_log2) >> 23)) << 23); }
+template <class T> __device__ __forceinline__ uint4 extra_parts(float lse, const WeighArgs &x) {
+  constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
+  float e[5] = {0, 0, 0, 0, 0};
+  if (lse == -INFINITY || lse == INFINITY) e[1] = -INFINITY;           // no weight
+  else if (lse != lse) e[1] = lse;
+  else {
+    double d = -(double)lse * 1.4426950408889634 / ((double)x.a.scale_log2 + (double)x.scale_low);
+    if (FP16) { e[0] = Elem<T>::up1(Elem<T>::down1((float)(d * 0x1p-15))); d -= (double)e[0] * 0x1p15; }
+    d *= 1.0 / (double)extra_alpha(x.a.scale_log2);
+#pragma unroll
+    for (u32 y = 1; y < 5; ++y) { e[y] = Elem<T>::up1(Elem<T>::down1((float)d)); d -= (double)e[y]; }
+  }
+  return make_uint4(Elem<T>::down(e[0], e[1]), Elem<T>::down(e[2], e[3]), Elem<T>::down(e[4], 0.0f), 0u);
+}
+// 2^t of two numbers without the special-function units: t = n + f with n the nearest whole number, 2^f on [-1/2, 1/2] by the polynomial of
+// degree 5 with the least relative error (fitted by reweighted least squares: 7.5e-8; 2.0e-7 with the roundings of its steps), times
+// 2^n put together from n's bits. Below 2^-127 it gives 0, above 2^128 Inf, and NaN for NaN.
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) { u64 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float within(float t) {
+  float r;
+  asm("{\n\t.reg .f32 x;\n\tmax.NaN.f32 x, %1, 0fC2FE0000;\n\tmin.NaN.f32 %0, x, 0f43000000;\n\t}" : "=f"(r) : "f"(t));     // [-127, 128]
+  return r;
+}
+__device__ __forceinline__ u64 twice(float x) { return pack2(x, x); }
+__device__ __forceinline__ u64 ex2_fma(float t0, float t1) {
+  const u64 t = pack2(within(t0), within(t1));
+  const u64 m = add2(t, twice(12582912.0f));               // 1.5 * 2^23: n in the lowest bits
+  const u64 f = fma2(add2(m, twice(-12582912.0f)), twice(-1.0f), t);
+  u64 p = fma2(twice(0.0013276472454890609f), f, twice(0.009675540961325169f));
+  p = fma2(p, f, twice(0.05550713092088699f));
+  p = fma2(p, f, twice(0.24022120237350464f));
+  p = fma2(p, f, twice(0.6931469440460205f));
+  p = fma2(p, f, twice(1.0000001192092896f));
+  const float2 z = unpack2(m);
+  return mul2(p, pack2(__uint_as_float((__float_as_uint(z.x) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(z.y) << 23) + 0x3F800000u)));
+}
+
+// Waits for the loads from tensor memory. What was added up from the numbers before is done first, and nothing is done with the new ones
+// before: the compiler sees neither in the instruction.
+__device__ __forceinline__ void tc_wait_ld16(u32 *r, u64 (&done)[2]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+               "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+l"(done[0]), "+l"(done[1]) :: "memory");
+}
+
 // Rows of a sequence that see any of the keys [key0, key0 + 256): tokens [lo, hi) of the new ones.
 struct Seen { u32 lo, hi; };
 __device__ __forceinline__ Seen seen_by(const AttendArgs &a, const Seq &q, u32 key0) {
@@ -973,7 +1188,7 @@ __device__ __forceinline__ Seen seen_by(const AttendArgs &a, const Seq &q, u32 k
   s.hi = max(s.hi, s.lo);
   return s;
 }
-__device__ __forceinline__ u32 row_tiles(const AttendArgs &a, const Seen &s) { return (u32)(((u64)(s.hi - s.lo) * a.group + TC_TILE - 1) / TC_TILE); }
+__device__ __forceinline__ u32 row_tiles(const Seen &s, u32 tokens) { return (s.hi - s.lo + tokens - 1) / tokens; }
 
 // Scratch: a header {tiles per stretch, tiles}, the place of each pair in the work (and the end), then 16 sums,
 // one per block, for each (pair, CTA): the one of pair p and CTA c is number p + c, as each next one has a greater p or c.
@@ -988,8 +1203,8 @@ __host__ __device__ __forceinline__ WeighScratch weigh_scratch(u8 *p, u32 n_seqs
 }
 
 struct WeighJob {
-  u32 t0, rows, index0;        // first row's token, rows that see any of the keys, index of the first token in its sequence
-  u32 kv, key0, seq;
+  u32 t0, tokens, index0;      // first token, tokens that see any of the keys, index of the first one in its sequence
+  u32 kv, key0, seq, first;    // first: block that is seen at all
   u32 tiles, x0, x1;           // row tiles of a head; tiles [x0, x1) of all heads
   u64 sum;                     // place of the sums
   u32 last;
@@ -997,45 +1212,46 @@ struct WeighJob {
 
 template <class T, u32 D>
 __global__ void __launch_bounds__(WTC_THREADS, 1)
-k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps maps) {
+k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps maps, const __grid_constant__ CUtensorMap queries, u32 mapped) {
   typedef WeighShape<D> S;
   constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
   extern __shared__ u8 smem_raw[];
-  __shared__ __align__(8) u64 s_kfull[2], s_kempty[2], s_qfull[WTC_Q], s_qempty[WTC_Q], s_lfull[WTC_L], s_sfull[2], s_sempty[2], s_drain, s_jfull[WTC_JOBS], s_jempty[WTC_JOBS];
-  __shared__ __align__(16) float s_l[WTC_L][TC_TILE];
-  __shared__ __align__(16) int s_index[WTC_L][TC_TILE];
+  __shared__ __align__(8) u64 s_kfull[WTC_K], s_kempty[WTC_K], s_qfull[WTC_Q], s_qempty[WTC_Q], s_sfull[2], s_sempty[2], s_hfull[2 * WTC_JOBS], s_drain, s_jfull[WTC_JOBS], s_jempty[WTC_JOBS];
+  __shared__ float s_half[WTC_JOBS][WTC_KEYS];
   __shared__ u32 s_tmem;
   __shared__ volatile u32 s_lost;
   __shared__ WeighJob s_job[WTC_JOBS];
   const AttendArgs &a = x.a;
   asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads, g = a.group;
-  const u32 kfull = smem_addr(s_kfull), kempty = smem_addr(s_kempty), qfull = smem_addr(s_qfull), qempty = smem_addr(s_qempty), lfull = smem_addr(s_lfull),
-            sfull = smem_addr(s_sfull), sempty = smem_addr(s_sempty), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
+  const u32 kfull = smem_addr(s_kfull), kempty = smem_addr(s_kempty), qfull = smem_addr(s_qfull), qempty = smem_addr(s_qempty),
+            sfull = smem_addr(s_sfull), sempty = smem_addr(s_sempty), hfull = smem_addr(s_hfull), drain = smem_addr(&s_drain), jfull = smem_addr(s_jfull), jempty = smem_addr(s_jempty);
   if (tid == 0) {
-    for (u32 i = 0; i < 2; ++i) { bar_init(kfull + i * 8, 1); bar_init(kempty + i * 8, 1); bar_init(sfull + i * 8, 1); bar_init(sempty + i * 8, 8); }
-    for (u32 i = 0; i < WTC_Q; ++i) { bar_init(qfull + i * 8, 2); bar_init(qempty + i * 8, 1); }
-    for (u32 i = 0; i < WTC_L; ++i) bar_init(lfull + i * 8, 2);
-    for (u32 i = 0; i < WTC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 14); }
+    for (u32 i = 0; i < 2 * WTC_JOBS; ++i) bar_init(hfull + i * 8, 4);
+    for (u32 i = 0; i < 2; ++i) { bar_init(sfull + i * 8, 1); bar_init(sempty + i * 8, 16); }
+    for (u32 i = 0; i < WTC_K; ++i) { bar_init(kfull + i * 8, 1); bar_init(kempty + i * 8, 1); }
+    for (u32 i = 0; i < WTC_Q; ++i) { bar_init(qfull + i * 8, 3); bar_init(qempty + i * 8, 1); }
+    for (u32 i = 0; i < WTC_JOBS; ++i) { bar_init(jfull + i * 8, 1); bar_init(jempty + i * 8, 22); }
     bar_init(drain, 1);
     s_lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
-  if (warp == 10 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &maps.tail : &maps.pool) : "memory");
+  if (warp == 18 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &maps.tail : &maps.pool) : "memory");
   tc_before();
   __syncthreads();
   tc_after();
   const u32 tmem = s_tmem;
-  const u32 sk = (smem_addr(smem_raw) + 1023) & ~1023u, sq = sk + 2 * S::K;
+  const u32 sk = (smem_addr(smem_raw) + 1023) & ~1023u, sq = sk + WTC_K * S::K, extra = sq + WTC_Q * S::Q;       // extra: K's constants, then a stage's parts of lse each
+  const u32 TOK = TC_TILE / g, ROWS = TOK * g;           // tokens and rows of a tile
   volatile u32 *const lost = &s_lost;
   // Waits last as long as a job of another warp may: a tile of 128 rows takes a microsecond, and a job has no more than x0 .. x1 of
   // them; 32 for each of the longest that can be.
-  const u64 most = (u64)H * (((u64)a.b.n_tokens * g + TC_TILE - 1) / TC_TILE) * 8;
+  const u64 most = (u64)H * ((a.b.n_tokens + TOK - 1) / TOK) * 8;
   const u32 patience = (u32)min(most, (u64)0x7FFFFFFF);
   u32 jobs = 0;
   auto next_job = [&](WeighJob &j) {
@@ -1048,7 +1264,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
     return j.last == 0;
   };
 
-  if (warp == 9) {
+  if (warp == 17) {
     // ---- what this CTA does. A lane per pair, 32 pairs of a sequence at a time; twice: for the sum of the work, then for its share.
     const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
     u64 total = 0, per = 0, tokens = 0;
@@ -1070,7 +1286,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
             const u32 k = k0 + lane;
             Seen seen{0, 0};
             if (k < pairs) seen = seen_by(a, q, k * WTC_KEYS);
-            const u32 tiles = row_tiles(a, seen);
+            const u32 tiles = row_tiles(seen, TOK);
             const u64 work = (u64)tiles * H;
             u64 incl = work;
 #pragma unroll
@@ -1084,8 +1300,8 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
                 if (made >= WTC_JOBS && !(ok = tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience))) break;
                 if (lane == __ffs(mask) - 1) {
                   WeighJob j;
-                  j.t0 = q.t0 + seen.lo; j.rows = (seen.hi - seen.lo) * g; j.index0 = q.kv - q.n + seen.lo;
-                  j.kv = q.kv; j.key0 = k * WTC_KEYS; j.seq = s0 + y;
+                  j.t0 = q.t0 + seen.lo; j.tokens = seen.hi - seen.lo; j.index0 = q.kv - q.n + seen.lo;
+                  j.kv = q.kv; j.key0 = k * WTC_KEYS; j.seq = s0 + y; j.first = first_seen(a, q);
                   j.tiles = tiles; j.x0 = (u32)(f - from); j.x1 = (u32)(t - from);
                   j.sum = pair + k + blockIdx.x;
                   j.last = 0;
@@ -1116,32 +1332,33 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
     const u32 at = made % WTC_JOBS;
     if (ok && made >= WTC_JOBS) ok = tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience);
     if (ok && lane == 0) { s_job[at].last = 1; bar_arrive(jfull + at * 8); }
-  } else if (warp == 10) {
-    // ---- K: a head's 256 keys per stage; blocks behind the sequence's last read as zeros
+  } else if (warp == 18) {
+    // ---- K: blocks in front of the window and behind the sequence's last read as zeros
     u32 it = 0;
     bool ok = true;
     for (WeighJob j; ok && next_job(j);) {
       const u32 b = j.key0 / BT + lane, held = (j.kv + BT - 1) / BT;
       u32 slot = ~0u;
-      if (lane < WTC_KB && b < held) {
+      if (lane < WTC_KB && b < held && b >= j.first) {
         slot = a.b.table[j.seq * a.b.table_stride + b];
         if (slot >= a.p.n_slots && slot - a.p.n_slots >= a.p.n_tail) kv_err(a.err, KVERR_RANGE);
       }
-      for (u32 h = j.x0 / j.tiles; h <= (j.x1 - 1) / j.tiles; ++h, ++it) {
-        const u32 st = it % 2;
-        if (it >= 2 && !(ok = tc_wait(kempty + st * 8, (it / 2 - 1) & 1, lost, patience))) break;
-        if (lane == 0) bar_expect(kfull + st * 8, S::K);
-        __syncwarp();
-        if (lane < WTC_KB) load_block(a, maps, sk + st * S::K + lane * S::BLOCK, kfull + st * 8, slot, 2 * a.layer, h, D / 64);
-        __syncwarp();
-      }
+      for (u32 h = j.x0 / j.tiles; ok && h <= (j.x1 - 1) / j.tiles; ++h)
+        for (u32 tile = 0; tile < 2; ++tile, ++it) {
+          const u32 st = it % WTC_K;
+          if (it >= WTC_K && !(ok = tc_wait(kempty + st * 8, (it / WTC_K - 1) & 1, lost, patience))) break;
+          if (lane == 0) bar_expect(kfull + st * 8, S::K);
+          __syncwarp();
+          if (lane / (WTC_KB / 2) == tile) load_block(a, maps, sk + st * S::K + lane % (WTC_KB / 2) * S::BLOCK, kfull + st * 8, slot, 2 * a.layer, h, D / 64);
+          __syncwarp();
+        }
     }
-    for (u32 i = it > 2 ? it - 2 : 0; i < it; ++i) bar_wait(kfull + (i % 2) * 8, (i / 2) & 1);     // landed before the CTA ends
-  } else if (warp == 8) {
+    for (u32 i = it > WTC_K ? it - WTC_K : 0; i < it; ++i) bar_wait(kfull + (i % WTC_K) * 8, (i / WTC_K) & 1);     // landed before the CTA ends
+  } else if (warp == 16) {
     // ---- products
     if (elect_one()) {
       const u32 id = tc_idesc(FP16, TC_TILE, false);
-      const u64 dk0 = tc_desc(sk, 16, D * 16), dq0 = tc_desc(sq, 16, 1024);
+      const u64 dk0 = tc_desc(sk, 16, D * 16), dq0 = tc_desc(sq, 16, 1024), de = plain_desc(extra);
       u32 n = 0, it = 0;
       bool ok = true;
       for (; ok;) {
@@ -1154,154 +1371,195 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
         u32 r = x0 % tiles;
         bool fresh = true;
         for (u32 i = x0; i < x1; ++i, ++n) {
-          const u32 st = n % WTC_Q, buf = n % 2, ks = it % 2;
-          if (fresh && !(ok = tc_wait1(kfull + ks * 8, (it / 2) & 1, lost, patience))) break;
+          const u32 st = n % WTC_Q, buf = n % 2, ks[2] = {it % WTC_K, (it + 1) % WTC_K};
           if (!(ok = tc_wait1(qfull + st * 8, (n / WTC_Q) & 1, lost, patience))) break;
           if (n >= 2 && !(ok = tc_wait1(sempty + buf * 8, (n / 2 - 1) & 1, lost, patience))) break;
           tc_after();
           const u64 dq = dq0 + st * (S::Q / 16);
 #pragma unroll
           for (u32 tile = 0; tile < 2; ++tile) {
-            const u64 dk = dk0 + ks * (S::K / 16) + tile * (S::K / 32);
+            if (fresh && !(ok = tc_wait1(kfull + ks[tile] * 8, ((it + tile) / WTC_K) & 1, lost, patience))) break;
+            const u64 dk = dk0 + ks[tile] * (S::K / 16);
 #pragma unroll
             for (u32 k = 0; k < D / 16; ++k)
               tc_mma_ss(tmem + buf * 256 + tile * 128, dk + ((k / 4) * 1024 + (k % 4) * 32) / 16, dq + ((k / 4) * (TC_TILE * 128) + (k % 4) * 32) / 16, id, k > 0);
+            tc_mma_ss(tmem + buf * 256 + tile * 128, de, de + (1 + st) * (S::EXTRA / 16), id, 1);
           }
+          if (!ok) break;
           tc_commit(sfull + buf * 8);
           tc_commit(qempty + st * 8);
           fresh = ++r == tiles || i + 1 == x1;
-          if (fresh) { r = 0; tc_commit(kempty + ks * 8); ++it; }
+          if (fresh) { r = 0; tc_commit(kempty + ks[0] * 8); tc_commit(kempty + ks[1] * 8); it += 2; }
         }
       }
       tc_commit(drain);                  // all products and their arrivals are done before the CTA ends
       bar_wait(drain, 0);
     }
     __syncwarp();
-  } else if (warp >= 11) {
-    // ---- queries: warps 11, 12 bring the even tiles, 13, 14 the odd ones
-    const u32 side = (warp - 11) / 2, mine = (warp - 11) % 2 * 32 + lane;      // 64 threads
+  } else if (warp >= 19) {
+    // ---- queries: warps 19, 20 bring the even tiles, 21, 22 the odd ones
+    const u32 side = (warp - 19) / 2, mine = (warp - 19) % 2 * 32 + lane;      // 64 threads
     constexpr u32 PER = D / 8, STEP = 64 / PER;                                // 16-byte parts of a row; rows per round
-    u32 n = 0;
+    const u32 my_tok[2] = {mine / g, (mine + 64) / g};                         // tokens of the rows whose lse this thread brings
+    u32 n = 0, brought = ~0u;
+    // rows that no tile has, and that none has had yet: no NaN in them. The second 8 channels more are 0.
+    auto zero = [](u32 at) { asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory"); };
+    for (u32 i = side * 64 + mine; i < WTC_Q * S::Q / 16; i += 128) zero(sq + i * 16);
+    for (u32 i = side * 64 + mine; i < WTC_Q * S::EXTRA / 16; i += 128) zero(extra + S::EXTRA + i * 16);
+    if (side == 0) {                     // K's constants, before the first tile is handed over
+      const float alpha = extra_alpha(a.scale_log2);
+      const u32 c0 = Elem<T>::down(FP16 ? 0x1p15f : 0.0f, alpha), c1 = Elem<T>::down(alpha, alpha), c2 = Elem<T>::down(alpha, 0.0f);
+      for (u32 row = mine; row < TC_TILE; row += 64) {
+        const u32 at = extra + row / 8 * 256 + row % 8 * 16;
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(c0), "r"(c1), "r"(c2), "r"(0) : "memory");
+        zero(at + 128);
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("bar.sync 1, 128;" ::: "memory");
     bool ok = true;
     for (WeighJob j; ok && next_job(j);) {
       u32 h = j.x0 / j.tiles, r = j.x0 - h * j.tiles;
       for (u32 i = j.x0; i < j.x1; ++i, ++n) {
         if (n % 2 == side) {
-          const u32 st = n % WTC_Q, ls = n % WTC_L;
-          static_assert(WTC_Q == 2, "a side's stage is its own");
+          const u32 st = n % WTC_Q;
+          const u32 left = min(TOK, j.tokens - r * TOK) * g, t = j.t0 + r * TOK;       // rows of this tile, its first token
+          uint4 parts[2];                // while the stage is still in use
+#pragma unroll
+          for (u32 y = 0; y < 2; ++y) {
+            const u32 row = mine + 64 * y;
+            parts[y] = extra_parts<T>(row < left ? a.lse[(u64)(t + my_tok[y]) * a.n_q_heads + h * g + row - my_tok[y] * g] : -INFINITY, x);
+          }
           if (n >= WTC_Q && !(ok = tc_wait(qempty + st * 8, (n / WTC_Q - 1) & 1, lost, patience))) break;
-          // (lse of four tiles ago: its powers are done, or the products of two tiles ago would not be)
-          const u32 c = mine % PER;
+          brought = n;
+          if (mapped) {
+            if (mine == 0) {
+              bar_expect(qfull + st * 8, ROWS * D * 2);
+#pragma unroll
+              for (u32 y = 0; y < D / 64; ++y)
+                asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                             ::"r"(sq + st * S::Q + y * (TC_TILE * 128)), "l"(&queries), "r"(64 * y), "r"(h * g), "r"(t), "r"(qfull + st * 8) : "memory");
+            }
+          } else {
+            const u32 c = mine % PER;
 #pragma unroll 4
-          for (u32 y = 0; y < TC_TILE / STEP; ++y) {
-            const u32 row = y * STEP + mine / PER, rr = r * TC_TILE + row;
-            const u32 dst = sq + st * S::Q + (c / 8) * (TC_TILE * 128) + row * 128 + (((c % 8) ^ (row % 8)) * 16);
-            if (rr < j.rows) {
-              const u32 tok = rr / g;
-              const u16 *const src = (const u16 *)a.q + (u64)(j.t0 + tok) * a.q_ts + (u64)(h * g + rr - tok * g) * a.q_hs + c * 8;
-              if (((uintptr_t)src & 15) == 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-              else {
+            for (u32 y = 0; y < TC_TILE / STEP; ++y) {
+              const u32 row = y * STEP + mine / PER, tok = row / g;
+              const u32 dst = sq + st * S::Q + (c / 8) * (TC_TILE * 128) + row * 128 + (((c % 8) ^ (row % 8)) * 16);
+              if (row < left) {
+                const u16 *const src = (const u16 *)a.q + (u64)(t + tok) * a.q_ts + (u64)(h * g + row - tok * g) * a.q_hs + c * 8;
                 u32 v[4];
 #pragma unroll
                 for (u32 z = 0; z < 4; ++z) v[z] = (u32)src[2 * z] | (u32)src[2 * z + 1] << 16;
                 asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
               }
-            } else {
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
             }
+            if (mine == 0) bar_arrive(qfull + st * 8);
           }
 #pragma unroll
           for (u32 y = 0; y < 2; ++y) {
-            const u32 row = mine * 2 + y, rr = r * TC_TILE + row;
-            float L = INFINITY;          // no row: no weight
-            int index = NO_ROW;
-            if (rr < j.rows) {
-              const u32 tok = rr / g;
-              L = lse_log2(a.lse[(u64)(j.t0 + tok) * a.n_q_heads + h * g + rr - tok * g]).high;
-              index = (int)(j.index0 + tok);
-            }
-            s_l[ls][row] = L; s_index[ls][row] = index;
+            const u32 row = mine + 64 * y;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(extra + (1 + st) * S::EXTRA + row / 8 * 256 + row % 8 * 16),
+                         "r"(parts[y].x), "r"(parts[y].y), "r"(parts[y].z), "r"(parts[y].w) : "memory");
           }
-          asm volatile("cp.async.wait_all;" ::: "memory");
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) { bar_arrive(lfull + ls * 8); bar_arrive(qfull + st * 8); }
+          if (lane == 0) bar_arrive(qfull + st * 8);
         }
         if (++r == j.tiles) { r = 0; ++h; }
       }
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (mapped && mine == 0 && n > side) {               // landed before the CTA ends: this side's last tile, number `brought`
+      if (brought != ~0u) bar_wait(qfull + (brought % WTC_Q) * 8, (brought / WTC_Q) & 1);
+    }
   } else {
-    // ---- powers and their sums: a thread per key
-    const u32 tile = warp / 4, key_t = tid % TC_TILE, from = tmem + ((warp % 4) << 21) + tile * 128;
+    // ---- powers and their sums: a key per thread, half of the columns
+    const u32 tile = warp / 8, half = warp / 4 % 2, key_t = tid % TC_TILE, from = tmem + ((warp % 4) << 21) + tile * 128 + half * 64;
     const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
     const u64 scale2 = pack2(a.scale_log2, a.scale_log2);
     u32 n = 0;
     bool ok = true;
+    u32 v[2][16];
+    auto begin = [&](u32 n) {            // the first columns of tile n
+      if (!tc_wait(sfull + n % 2 * 8, (n / 2) & 1, lost, patience)) return false;
+      tc_after();
+      tc_ld16(v[0], from + n % 2 * 256);
+      return true;
+    };
     for (WeighJob j; ok && next_job(j);) {
       const u32 key = j.key0 + tile * TC_TILE + key_t;
       float sum = 0.0f;
       u32 r = j.x0 % j.tiles;
+      if (!(ok = begin(n))) break;
       for (u32 i = j.x0; i < j.x1; ++i, ++n) {
-        const u32 buf = n % 2, ls = n % WTC_L;
-        const u32 cols = min(TC_TILE, j.rows - r * TC_TILE);
-        // tokens of this tile: the first and the last
-        const u32 index0 = j.index0 + r * TC_TILE / g, index1 = j.index0 + (r * TC_TILE + cols - 1) / g;
-        const u32 k0 = j.key0 + tile * TC_TILE, k1 = min(k0 + TC_TILE, j.kv);       // this warpgroup's keys
-        const bool whole = cols == TC_TILE && (a.full || k1 <= index0 + 1) && (!a.window || (u64)k0 + a.window > index1);
-        if (!(ok = tc_wait(lfull + ls * 8, (n / WTC_L) & 1, lost, patience) && tc_wait(sfull + buf * 8, (n / 2) & 1, lost, patience))) break;
-        tc_after();
+        const u32 buf = n % 2;
+        const u32 toks = min(TOK, j.tokens - r * TOK), cols = toks * g;
+        const u32 index0 = j.index0 + r * TOK, index1 = index0 + toks - 1;        // of the tile's first and last token
+        const u32 k0 = j.key0 + tile * TC_TILE, k1 = min(k0 + TC_TILE, j.kv);       // this tile's keys
+        const bool whole = cols >= half * 64 + 64 && (a.full || k1 <= index0 + 1) && (!a.window || (u64)k0 + a.window > index1);
         u64 part[2] = {0, 0};
-        u32 v[2][32];
-        tc_ld32(v[0], from + buf * 256);
-        const u32 chunks = (cols + 31) / 32;
+        // columns that see this thread's key: tokens from its own on, while it is inside the window; index0 is negative only with `full`
+        u64 see = ~0ull;
+        if (!whole) {
+          const int behind = (int)key - (int)index0;
+          const u32 lo = a.full ? 0u : (u32)max(behind, 0), hi = a.window ? (u32)max(0ll, min((long long)toks, (long long)behind + a.window)) : toks;
+          const int lo_col = (int)(min(lo, toks) * g) - (int)half * 64, hi_col = (int)(hi * g) - (int)half * 64;
+          see = (lo_col >= 64 ? 0ull : lo_col > 0 ? ~0ull << lo_col : ~0ull) & (hi_col >= 64 ? ~0ull : hi_col > 0 ? ~(~0ull << hi_col) : 0ull);
+        }
 #pragma unroll
         for (u32 c = 0; c < 4; ++c) {
-          if (c < chunks) {
-            tc_wait_ld();
-            if (c + 1 < 4) { if (c + 1 < chunks) tc_ld32(v[(c + 1) & 1], from + buf * 256 + 32 * (c + 1)); }
-            const float *const s = reinterpret_cast<const float *>(v[c & 1]);
-            if (whole) {
+          tc_wait_ld16(v[c & 1], part);
+          if (c < 3) tc_ld16(v[(c + 1) & 1], from + buf * 256 + 16 * (c + 1));
+          else {                         // S is read: on with the next tile's before the last powers of this one
+            tc_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(sempty + buf * 8);
+            if (i + 1 < j.x1 && !(ok = begin(n + 1))) break;
+          }
+          const float *const s = reinterpret_cast<const float *>(v[c & 1]);
+          if (whole) {
 #pragma unroll
-              for (u32 y = 0; y < 32; y += 4) {
-                const float4 L = *(const float4 *)&s_l[ls][32 * c + y];
-                const float2 p = unpack2(fma2(pack2(s[y], s[y + 1]), scale2, pack2(-L.x, -L.y))), q = unpack2(fma2(pack2(s[y + 2], s[y + 3]), scale2, pack2(-L.z, -L.w)));
-                part[0] = add2(part[0], pack2(ex2(p.x), ex2(p.y)));
-                part[1] = add2(part[1], pack2(ex2(q.x), ex2(q.y)));
-              }
-            } else {
+            for (u32 y = 0; y < 16; y += 2) {
+              const float2 p = unpack2(mul2(pack2(s[y], s[y + 1]), scale2));
+              part[y / 2 % 2] = add2(part[y / 2 % 2], y == 4 ? ex2_fma(p.x, p.y) : pack2(ex2(p.x), ex2(p.y)));
+            }
+          } else {
+            const u32 mask = (u32)(see >> (16 * c));
+            if (__any_sync(~0u, mask & 0xFFFF)) {
 #pragma unroll
-              for (u32 y = 0; y < 32; y += 4) {
-                const float4 L = *(const float4 *)&s_l[ls][32 * c + y];
-                const int4 at = *(const int4 *)&s_index[ls][32 * c + y];
-                auto power = [&](float z, float l, int index) {
-                  const bool see = a.full ? index != NO_ROW : (int)key <= index && (!a.window || (long long)key + a.window > index);
-                  return see ? ex2(fmaf(z, a.scale_log2, -l)) : 0.0f;
-                };
-                part[0] = add2(part[0], pack2(power(s[y], L.x, at.x), power(s[y + 1], L.y, at.y)));
-                part[1] = add2(part[1], pack2(power(s[y + 2], L.z, at.z), power(s[y + 3], L.w, at.w)));
+              for (u32 y = 0; y < 16; y += 2) {
+                auto power = [&](u32 i) { return mask >> i & 1 ? ex2(s[i] * a.scale_log2) : 0.0f; };
+                part[y / 2 % 2] = add2(part[y / 2 % 2], pack2(power(y), power(y + 1)));
               }
             }
           }
         }
-        tc_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(sempty + buf * 8);
+        if (!ok) break;
         const float2 all = unpack2(add2(part[0], part[1]));
         sum += all.x + all.y;
         if (++r == j.tiles) r = 0;
       }
       if (!ok) break;
-      if (key >= j.kv) sum = 0.0f;
+      // The halves together. Four places in turn: the second half can be no more than two tiles of rows ahead of the first.
+      const u32 at = (jobs - 1) % WTC_JOBS, bar = hfull + (tile * WTC_JOBS + at) * 8;
+      if (half) {
+        s_half[at][tile * TC_TILE + key_t] = sum;
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar);
+      } else {
+        if (!(ok = tc_wait(bar, ((jobs - 1) / WTC_JOBS) & 1, lost, patience))) break;
+        sum += s_half[at][tile * TC_TILE + key_t];
+        if (key >= j.kv) sum = 0.0f;
 #pragma unroll
-      for (u32 o = 8; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-      if (lane % 16 == 0) sc.sums[j.sum * WTC_KB + key_t / BT + tile * (TC_TILE / BT)] = sum;
+        for (u32 o = 8; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+        if (lane % 16 == 0) sc.sums[j.sum * WTC_KB + key_t / BT + tile * (TC_TILE / BT)] = sum;
+      }
     }
   }
   tc_before();
   __syncthreads();
   tc_after();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
   if (tid == 0 && s_lost) kv_err(a.err, KVERR_WAIT);
 }
 
@@ -1345,8 +1603,18 @@ WeighPlan plan_weigh(const WeighArgs &x, u32 max_q_len, int sm_count) {
   WeighPlan p{};
   const u32 d = x.a.p.head_dim;
   const u64 rows = (u64)(max_q_len && max_q_len < x.a.b.n_tokens ? max_q_len : x.a.b.n_tokens) * x.a.group;
-  p.many = (d == 64 || d == 128) && rows > WEIGH_FEW;
+  // (the parts of lse / scale are numbers of the element type: scales far from 1 are left to the first kernel)
+  p.many = (d == 64 || d == 128) && rows > WEIGH_FEW && x.a.group <= TC_TILE && x.a.scale_log2 > 0x1p-13f && x.a.scale_log2 < 0x1p13f;
   p.grid = sm_count;
+  const u64 blocks = (u64)x.a.b.n_seqs * x.a.b.max_blocks;
+  if (d == 64 || d == 128) {             // four CTAs per slot, as long as a tile has a block
+    p.share = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+    p.tile = (u32)std::max<u64>(1, std::min<u64>(WEIGH_TILE, blocks / (8ull * sm_count)));
+  } else {                               // one warp per block and 32 blocks per CTA where there are enough of them, else the heads of a block over several warps
+    p.share = 1;
+    while (p.share < 8 && p.share * 2 <= x.a.p.n_kv_heads && blocks * p.share < 32ull * sm_count) p.share *= 2;
+    p.tile = p.share > 1 || blocks < 128ull * sm_count ? 8 : WEIGH_TILE;
+  }
   if (p.many) {
     const u64 pairs = weigh_pairs(x.a.b.n_seqs, x.a.b.max_blocks);
     p.scratch_bytes = ((16 + 8 * (pairs + 1) + 15) & ~15ull) + (pairs + p.grid) * WTC_KB * 4;
@@ -1358,7 +1626,9 @@ template <class T, u32 D>
 static cudaError_t launch_weigh_tc(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
   cudaError_t r = allow_smem(k_weigh_tc<T, D>, 3 + (D == 128) * 2 + __is_same(T, __half), WeighShape<D>::SMEM, allowed);
   if (r != cudaSuccess) return r;
-  k_weigh_tc<T, D><<<p.grid, WTC_THREADS, WeighShape<D>::SMEM, s>>>(x, m);
+  CUtensorMap queries{};
+  const u32 mapped = make_row_map(&queries, x.a.q, D, x.a.n_q_heads, x.a.b.n_tokens, x.a.q_hs, x.a.q_ts, x.a.group, TC_TILE / x.a.group);
+  k_weigh_tc<T, D><<<p.grid, WTC_THREADS, WeighShape<D>::SMEM, s>>>(x, m, queries, mapped);
   ++*launches;
   if ((r = cudaGetLastError()) != cudaSuccess) return r;
   cudaLaunchConfig_t c{};
@@ -1370,21 +1640,39 @@ static cudaError_t launch_weigh_tc(const WeighArgs &x, const WeighPlan &p, const
   ++*launches;
   return cudaLaunchKernelEx(&c, k_weigh_join, x);
 }
+template <class T, u32 D, u32 NT>
+static cudaError_t launch_weigh_split(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed) {
+  constexpr u32 SMALL = WeighRing<D>::SMEM;
+  const cudaError_t r = allow_smem(k_weigh_split<T, D, NT>, ((D == 128) * 2 + __is_same(T, __half)) * 3 + (NT == 4 ? 2 : NT - 1), SMALL, allowed + 1);
+  if (r != cudaSuccess) return r;
+  k_weigh_split<T, D, NT><<<x.a.b.n_seqs * ((x.a.b.max_blocks + p.tile - 1) / p.tile), WS_THREADS, SMALL, s>>>(x, m, p.tile);
+  return cudaGetLastError();
+}
+template <class T, u32 D>
+static cudaError_t launch_weigh_split(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
+  ++*launches;
+  if (p.share == 1) return launch_weigh_split<T, D, 1>(x, p, m, s, allowed);
+  if (p.share == 2) return launch_weigh_split<T, D, 2>(x, p, m, s, allowed);
+  return launch_weigh_split<T, D, 4>(x, p, m, s, allowed);
+}
 cudaError_t launch_weigh(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed, u32 *launches) {
-  const u32 ctas = x.a.b.n_seqs * ((x.a.b.max_blocks + 7) / 8), d = x.a.p.head_dim;
+  const u32 d = x.a.p.head_dim;
   if (p.many) {
     if (d == 64) return x.a.fp16 ? launch_weigh_tc<__half, 64>(x, p, m, s, allowed, launches) : launch_weigh_tc<__nv_bfloat16, 64>(x, p, m, s, allowed, launches);
     return x.a.fp16 ? launch_weigh_tc<__half, 128>(x, p, m, s, allowed, launches) : launch_weigh_tc<__nv_bfloat16, 128>(x, p, m, s, allowed, launches);
   }
+  if (d == 64) return x.a.fp16 ? launch_weigh_split<__half, 64>(x, p, m, s, allowed, launches) : launch_weigh_split<__nv_bfloat16, 64>(x, p, m, s, allowed, launches);
+  if (d == 128) return x.a.fp16 ? launch_weigh_split<__half, 128>(x, p, m, s, allowed, launches) : launch_weigh_split<__nv_bfloat16, 128>(x, p, m, s, allowed, launches);
+  const u32 ctas = x.a.b.n_seqs * ((x.a.b.max_blocks + p.tile - 1) / p.tile);
   ++*launches;
   if (x.a.fp16) {
-    if (d <= 64) k_weigh<__half, 2><<<ctas, 256, 0, s>>>(x);
-    else if (d <= 128) k_weigh<__half, 4><<<ctas, 256, 0, s>>>(x);
-    else k_weigh<__half, 8><<<ctas, 256, 0, s>>>(x);
+    if (d <= 64) k_weigh<__half, 2><<<ctas, 256, 0, s>>>(x, p.tile, p.share);
+    else if (d <= 128) k_weigh<__half, 4><<<ctas, 256, 0, s>>>(x, p.tile, p.share);
+    else k_weigh<__half, 8><<<ctas, 256, 0, s>>>(x, p.tile, p.share);
   } else {
-    if (d <= 64) k_weigh<__nv_bfloat16, 2><<<ctas, 256, 0, s>>>(x);
-    else if (d <= 128) k_weigh<__nv_bfloat16, 4><<<ctas, 256, 0, s>>>(x);
-    else k_weigh<__nv_bfloat16, 8><<<ctas, 256, 0, s>>>(x);
+    if (d <= 64) k_weigh<__nv_bfloat16, 2><<<ctas, 256, 0, s>>>(x, p.tile, p.share);
+    else if (d <= 128) k_weigh<__nv_bfloat16, 4><<<ctas, 256, 0, s>>>(x, p.tile, p.share);
+    else k_weigh<__nv_bfloat16, 8><<<ctas, 256, 0, s>>>(x, p.tile, p.share);
   }
   return cudaGetLastError();
 }

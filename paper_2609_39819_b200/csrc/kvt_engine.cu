@@ -157,7 +157,7 @@ struct kvt_engine {
   bool metadata_only;
   int sm_count = 148;
   int device = 0;
-  KvMaps kv_maps{}; bool kv_maps_ok = false; u64 kv_smem_allowed = 0, kv_blocks_allowed = 0;   // for head sizes of 64 and 128
+  KvMaps kv_maps{}; bool kv_maps_ok = false; u64 kv_smem_allowed = 0, kv_blocks_allowed[2] = {0, 0};   // for head sizes of 64 and 128
   u8 *tail_pool = nullptr; u32 n_tail = 0;   // blocks outside every tier (kvt_set_tail_pool)
   // host state
   std::vector<Ctx> ctxs;
@@ -2418,7 +2418,7 @@ int32_t kvt_select_blocks(kvt_engine *e, const kvt_select_args *args, void *stre
     if ((uintptr_t)a.scratch & 15) return fail(e, KVT_E_INVAL, "select: misaligned scratch");
   }
   u32 launches = 0;
-  const cudaError_t r = launch_select(x, p, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  const cudaError_t r = launch_select(x, p, (cudaStream_t)stream, e->kv_blocks_allowed, &launches);
   return kv_launched(e, r, launches);
 }
 
@@ -2437,7 +2437,7 @@ int32_t kvt_attend_blocks(kvt_engine *e, const kvt_attend_blocks_args *args, voi
   y.q = a.q; y.out = a.out; y.lse = a.lse; y.q_ts = a.q_ts; y.q_hs = a.q_hs; y.o_ts = a.o_ts; y.o_hs = a.o_hs;
   const AttendListArgs x{attend_args(e, y), a.blocks, a.n_blocks};
   u32 launches = 0;
-  const cudaError_t r = launch_attend_blocks(x, e->kv_maps, e->sm_count, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  const cudaError_t r = launch_attend_blocks(x, e->kv_maps, e->sm_count, (cudaStream_t)stream, e->kv_blocks_allowed, &launches);
   return kv_launched(e, r, launches);
 }
 
@@ -2463,7 +2463,7 @@ int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *args, void *stream
     if ((uintptr_t)a.scratch & 15) return fail(e, KVT_E_INVAL, "weigh: misaligned scratch");
   }
   u32 launches = 0;
-  const cudaError_t r = launch_weigh(x, p, e->kv_maps, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  const cudaError_t r = launch_weigh(x, p, e->kv_maps, (cudaStream_t)stream, e->kv_blocks_allowed, &launches);
   return kv_launched(e, r, launches);
 }
 
@@ -2487,7 +2487,7 @@ int32_t kvt_evict_blocks(kvt_engine *e, const kvt_evict_args *args, void *stream
   x.n_seqs = a.n_seqs; x.max_blocks = a.max_blocks; x.n_blocks = a.n_blocks; x.first = a.first; x.last = a.last;
   x.err = e->dp<u32>(e->L.kv_err);
   u32 launches = 0;
-  const cudaError_t r = launch_evict(x, (cudaStream_t)stream, &e->kv_blocks_allowed, &launches);
+  const cudaError_t r = launch_evict(x, (cudaStream_t)stream, e->kv_blocks_allowed, &launches);
   return kv_launched(e, r, launches);
 }
 

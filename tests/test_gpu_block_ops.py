@@ -98,7 +98,7 @@ def sparse_reference(s, blocks, scale=None):
 def weights_reference(s, lse, window=0, causal=True, scale=None):
     """New weights per block [sequences, blocks of a row] and how far each may be off."""
     torch = s.torch
-    scale = s.dim ** -0.5 if scale is None else scale
+    scale = s.dim ** -0.5 if scale is None else float(np.float32(scale))
     width = s.table.shape[1]
     out = torch.zeros(len(s.new), width * BT, dtype=torch.float64, device="cuda")
     tol = torch.zeros_like(out)
@@ -127,7 +127,8 @@ def weights_reference(s, lse, window=0, causal=True, scale=None):
     per_block = lambda x: x.view(len(s.new), width, BT).sum(-1)      # noqa: E731
     out, tol = per_block(out), per_block(tol)
     rows = max(s.new + [1]) * s.heads * s.group * BT
-    return out, tol + out * E32 * (rows + 8)       # sums in 32 bits, whatever their order
+    # sums in 32 bits, whatever their order; powers below 2^-126, the least number of 32 bits, may count as 0
+    return out, tol + out * E32 * (rows + 8) + rows * 2.0 ** -126
 
 
 BATCHES = {
@@ -447,6 +448,23 @@ def test_weigh_window(B, batch, window, dim):  # noqa: F811
     check_weigh(make(B, batch, "bf16", 0, 2, 2, dim), window=window, scale=0.2)
 
 
+@pytest.mark.parametrize("new", [[1, 1], [90, 3]])
+def test_weigh_blocks_in_front_of_the_window_need_no_slot(B, new):  # noqa: F811
+    import torch
+    s = make(B, (new, [1000, 5000]), "bf16", 0, 2, 4, 64)
+    want = check_weigh(s, window=200)
+    for i, n in enumerate(new):
+        s.table[i, :(s.kv[i] - n + 1 - 200) // BT] = -1
+    lse = torch.empty(s.rows, 8, device="cuda")
+    s.eng.attend(s.layer, s.q, s.table, s.q_start, s.kv_len, window=200, lse=lse)
+    got = s.eng.weigh_blocks(s.layer, s.q, lse, s.table, s.q_start, s.kv_len, max_q_len=1, window=200)
+    s.eng.kv_check()
+    assert torch.equal(got, want)
+    got = s.eng.weigh_blocks(s.layer, s.q, lse, s.table, s.q_start, s.kv_len, window=200)
+    s.eng.kv_check()
+    assert torch.allclose(got, want, rtol=1e-5, atol=0)
+
+
 @pytest.mark.parametrize("dim", [64, 128, 40])
 @pytest.mark.parametrize("batch", [*BATCHES, ([200, 3], [100, 900])])
 def test_weigh_full(B, batch, dim):  # noqa: F811
@@ -454,11 +472,20 @@ def test_weigh_full(B, batch, dim):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("dim,heads,group", [(128, 2, 4), (64, 4, 3), (128, 1, 12), (64, 3, 1)])
+@pytest.mark.parametrize("dim,heads,group", [(128, 2, 4), (64, 4, 3), (128, 1, 12), (64, 3, 1), (128, 1, 40), (64, 1, 130)])
 @pytest.mark.parametrize("new,past", [([600], [0]), ([257, 1, 40], [1000, 3000, 17]), ([64], [5000]), ([1000, 129], [77, 2000])])
 def test_weigh_prompts_and_chunks(B, dtype, dim, heads, group, new, past):  # noqa: F811
     s = make(B, (new, past), dtype, 0, heads, group, dim, layers=1, layer=0, q_gain=2.0, tail=group == 3, strided=group == 12)
     check_weigh(s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("scale,gain", [(1e-3, 4.0), (4.0, 1.0), (0.125, 30.0), (5e-5, 1.0), (3e4, 1e-3), (0.0, 1.0), (1.0, 8.0)])
+def test_weigh_scales_near_and_far(B, dtype, scale, gain):  # noqa: F811
+    """lse of some thousands and of nearly nothing."""
+    for new in ([200], [2]):
+        s = make(B, (new, [300]), dtype, 0, 2, 4, 128, layers=1, layer=0, q_gain=gain)
+        check_weigh(s, scale=scale)
 
 
 def test_weights_sum_to_the_number_of_rows(B):  # noqa: F811

@@ -231,7 +231,7 @@ __device__ __forceinline__ void deal(u32 n, Pick pick, Put put) {
 // Order of floating numbers as order of whole ones.
 __device__ __forceinline__ u32 ordered(float x) {
   const u32 b = __float_as_uint(x);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return b ^ ((u32)((int)b >> 31) | 0x80000000u);
 }
 
 // ======================================================================================================
@@ -259,21 +259,27 @@ __device__ __forceinline__ void mma_u8s8(int (&c)[4], u32 a0, u32 a1, u32 a2, u3
                : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Scores of 16 tokens of one sequence with one KV head's share of the blocks. blockIdx.x: tile of tokens, y: KV head, z: share of the
-// blocks. A warp takes 8 blocks at a time: a lane 16 bytes of every 64 of a block's codes, which are the operand of the matrix
+// Scores of M * 16 tokens of one sequence with one KV head's share of the blocks. blockIdx.x: tile of tokens, y: KV head, z: share of the
+// blocks. A warp takes 8 blocks at a time, with a ring of bulk copies of its own: the codes of the next groups come in while one is worked
+// on, those of the first while the queries are rounded. A lane's 16 bytes of every 64 of a block's codes are the operand of the matrix
 // instruction if the channels are counted in that order on both sides.
-template <class T, u32 G>      // G: 64-byte parts of (up, down)
-__global__ void __launch_bounds__(256) k_score_blocks(SelectArgs a, u32 shares) {
-  constexpr u32 ROW = G * 64 + 16;
-  __shared__ __align__(16) u8 su[16 * ROW];
-  __shared__ u64 s_sum[8];
-  __shared__ u32 s_seq, s_tile;
+constexpr u32 SCORE_STAGES = 4;
+template <u32 G> struct ScoreRing { static constexpr u32 PITCH = G * 64 + 64 /* lanes of two blocks on different banks */, STAGE = 8 * PITCH, SMEM = 8 * SCORE_STAGES * STAGE; };
+template <class T, u32 G, u32 M>      // G: 64-byte parts of (up, down)
+__global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_score_blocks(SelectArgs a, u32 shares) {
+  typedef ScoreRing<G> S;
+  constexpr u32 ROW = G * 64 + 16, TOKENS = M * 16;
+  extern __shared__ __align__(16) u8 smem_raw[];
+  __shared__ __align__(8) u64 bars[8 * SCORE_STAGES];
+  __shared__ __align__(16) u8 su[TOKENS * ROW];
+  __shared__ u32 s_sum[8], s_seq, s_tile;
+  asm volatile("griddepcontrol.launch_dependents;");
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, H = a.n_kv_heads, W = a.k.width;
   // the tile's sequence
   if (tid == 0) s_seq = ~0u;
   u32 base = 0;
   for (u32 s0 = 0; s0 < a.b.n_seqs; s0 += 256) {
-    const u32 n = s0 + tid < a.b.n_seqs ? (part_of(a, s0 + tid).n + 15) / 16 : 0;
+    const u32 n = s0 + tid < a.b.n_seqs ? (part_of(a, s0 + tid).n + TOKENS - 1) / TOKENS : 0;
     u32 incl = n;
 #pragma unroll
     for (u32 o = 1; o < 32; o *= 2) { const u32 y = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += y; }
@@ -282,7 +288,7 @@ __global__ void __launch_bounds__(256) k_score_blocks(SelectArgs a, u32 shares) 
     __syncthreads();
     u32 before = base, all = base;
 #pragma unroll
-    for (u32 w = 0; w < 8; ++w) { if (w < warp) before += (u32)s_sum[w]; all += (u32)s_sum[w]; }
+    for (u32 w = 0; w < 8; ++w) { if (w < warp) before += s_sum[w]; all += s_sum[w]; }
     if (blockIdx.x >= before + incl - n && blockIdx.x < before + incl) { s_seq = s0 + tid; s_tile = blockIdx.x - (before + incl - n); }
     base = all;
   }
@@ -290,7 +296,7 @@ __global__ void __launch_bounds__(256) k_score_blocks(SelectArgs a, u32 shares) 
   const u32 seq = s_seq;
   if (seq == ~0u) return;
   Part p = part_of(a, seq);
-  p.t0 += s_tile * 16; p.index += s_tile * 16; p.n = min(16u, p.n - s_tile * 16);
+  p.t0 += s_tile * TOKENS; p.index += s_tile * TOKENS; p.n = min(TOKENS, p.n - s_tile * TOKENS);
   // blocks that any of the tokens may choose from: [first, its own - last]; scored from a multiple of 8 on
   const long long own = (p.index + p.n - 1) / BT;
   const long long end_ = p.index + p.n - 1 < 0 ? 0 : min(own + 1 - (long long)a.last, (long long)a.b.max_blocks);
@@ -299,87 +305,161 @@ __global__ void __launch_bounds__(256) k_score_blocks(SelectArgs a, u32 shares) 
   const u32 b0 = begin + min(end - begin, blockIdx.z * per), b1 = begin + min(end - begin, (blockIdx.z + 1) * per);
   if (b0 >= b1 || own + 1 <= (long long)a.n_blocks) return;       // nobody chooses
 
-  // queries: two tokens per warp
-  for (u32 r = warp; r < 16; r += 8) {
-    double up[8], down[8], most = 0.0;
+  const u32 j = lane % 4, r = lane / 4;
+  const u32 *const table = a.b.table + seq * a.b.table_stride;
+  const u32 ring = smem_addr(smem_raw) + warp * SCORE_STAGES * S::STAGE, bar0 = smem_addr(bars) + warp * SCORE_STAGES * 8;
+  if (lane == 0) {
+    for (u32 i = 0; i < SCORE_STAGES; ++i) bar_init(bar0 + i * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncwarp();
+  auto slot_of = [&](u32 b) { return lane < 8 && b + lane < b1 ? table[b + lane] : ~0u; };      // lane i: slot of block b + i
+  u32 e[SCORE_STAGES];                   // lane i: exponent of block i of the stage; 256: none
+  auto load = [&](u32 st, u32 b, u32 slot) {
+    const bool fine = slot < a.k.n_slots;
+    if (!fine && lane < 8 && b + lane < b1) kv_err(a.err, KVERR_RANGE);
+    const u32 n = __popc(__ballot_sync(~0u, fine)), bar = bar0 + st * 8;
+    if (lane == 0) bar_expect(bar, n * 2 * W);
+    __syncwarp();
+    if (fine)
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                   ::"r"(ring + st * S::STAGE + lane * S::PITCH), "l"(a.k.codes + ((u64)slot * H + h) * 2 * W), "r"(2 * W), "r"(bar) : "memory");
+    return fine ? (u32)a.k.exps[(u64)slot * H + h] : 256u;
+  };
+  u32 b = b0 + warp * 8, phase = 0;
 #pragma unroll
-    for (u32 z = 0; z < 8; ++z) {
-      const u32 c = lane + 32 * z;
-      up[z] = down[z] = 0.0;
-      if (z * 32 < G * 32 && c < a.head_dim && r < p.n)
-        for (u32 y = 0; y < a.group; ++y) {
-          float x = number(Elem<T>::up1(((const T *)a.q)[(u64)(p.t0 + r) * a.q_ts + (u64)(h * a.group + y) * a.q_hs + c]));
-          const float top = __is_same(T, __half) ? 65504.0f : 3.3895314e38f;       // Inf counts as the largest number
-          x = fminf(fmaxf(x, -top), top);
-          if (x > 0.0f) up[z] += (double)x; else down[z] -= (double)x;
+  for (u32 st = 0; st < SCORE_STAGES; ++st) { e[st] = 256; if (b + 64 * st < b1) e[st] = load(st, b + 64 * st, slot_of(b + 64 * st)); }
+  u32 slot = slot_of(b + 64 * SCORE_STAGES);
+
+  // queries: a warp per token; V channels in a row per lane
+  constexpr u32 V = G;
+  for (u32 t = warp; t < TOKENS; t += 8) {
+    double up[V], down[V], most = 0.0;
+#pragma unroll
+    for (u32 z = 0; z < V; ++z) up[z] = down[z] = 0.0;
+    if (t < p.n && lane * V < a.head_dim) {
+      const u16 *const src = (const u16 *)a.q + (u64)(p.t0 + t) * a.q_ts + (u64)(h * a.group) * a.q_hs + lane * V;
+      const bool vec = lane * V + V <= a.head_dim && (((uintptr_t)src | a.q_hs * 2) & (V * 2 - 1)) == 0;
+      for (u32 y0 = 0; y0 < a.group; y0 += 4) {
+        u32 raw[4][V / 2];
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) {
+          const u16 *const from = src + min(y0 + y, a.group - 1) * a.q_hs;
+          if (vec) {
+            if (V == 2) raw[y][0] = *(const u32 *)from;
+            else if (V == 4) *(uint2 *)raw[y] = *(const uint2 *)from;
+            else *(uint4 *)raw[y] = *(const uint4 *)from;
+          } else {
+#pragma unroll
+            for (u32 z = 0; z < V / 2; ++z) {
+              const u32 c = lane * V + 2 * z;
+              raw[y][z] = (c < a.head_dim ? (u32)from[2 * z] : 0u) | (c + 1 < a.head_dim ? (u32)from[2 * z + 1] << 16 : 0u);
+            }
+          }
         }
-      most = fmax(most, fmax(up[z], down[z]));
+#pragma unroll
+        for (u32 y = 0; y < 4; ++y) {
+          if (y0 + y >= a.group) continue;
+#pragma unroll
+          for (u32 z = 0; z < V; ++z) {
+            const float2 pair = Elem<T>::up(raw[y][z / 2]);
+            const float top = __is_same(T, __half) ? 65504.0f : 3.3895314e38f;       // Inf counts as the largest number
+            const float v = fminf(fmaxf(number(z % 2 ? pair.y : pair.x), -top), top);
+            up[z] += (double)fmaxf(v, 0.0f); down[z] += (double)fmaxf(-v, 0.0f);
+          }
+        }
+      }
     }
 #pragma unroll
-    for (u32 o = 16; o; o /= 2) most = fmax(most, __shfl_xor_sync(~0u, most, o));
+    for (u32 z = 0; z < V; ++z) most = fmax(most, fmax(up[z], down[z]));
+    // the exponent alone, and whether it is above 255 / 256 of the power: 255 = 1.9921875 * 2^7
     const u64 bits = (u64)__double_as_longlong(most);
-    const int f = most > 0.0 ? (int)(bits >> 52) - 1023 - 7 + ((bits & 0xFFFFFFFFFFFFFull) > 0xFE00000000000ull) : 0;     // 255 = 1.9921875 * 2^7
+    const int e = most > 0.0 ? (int)(bits >> 52) - 1023 - 7 + ((bits & 0xFFFFFFFFFFFFFull) > 0xFE00000000000ull) : -2000;
+    const int f_ = (int)__reduce_max_sync(~0u, e), f = f_ == -2000 ? 0 : f_;
     const double inv = __longlong_as_double((u64)(1023 - f) << 52);
+    u32 pu[V / 2 > 1 ? V / 4 : 1], pd[V / 2 > 1 ? V / 4 : 1];
 #pragma unroll
-    for (u32 z = 0; z < 8; ++z) {
-      const u32 c = lane + 32 * z;
-      if (z * 32 < G * 32 && c < W) { su[r * ROW + c] = (u8)__double2uint_rn(up[z] * inv); su[r * ROW + W + c] = (u8)__double2uint_rn(down[z] * inv); }
+    for (u32 z = 0; z < V; ++z) {
+      const u32 x = __double2uint_rn(up[z] * inv), y = __double2uint_rn(down[z] * inv);
+      if (z % 4 == 0) { pu[z / 4] = x; pd[z / 4] = y; } else { pu[z / 4] |= x << (z % 4 * 8); pd[z / 4] |= y << (z % 4 * 8); }
     }
-    for (u32 c = 2 * W + lane; c < G * 64; c += 32) su[r * ROW + c] = 0;
+    // (a lane's channels lie all in front of the width or all behind it: it is a multiple of 16)
+    if (lane * V < W) {
+      u8 *const to = su + t * ROW + lane * V;
+      if (V == 2) { *(u16 *)to = (u16)pu[0]; *(u16 *)(to + W) = (u16)pd[0]; }
+      else if (V == 4) { *(u32 *)to = pu[0]; *(u32 *)(to + W) = pd[0]; }
+      else { *(uint2 *)to = make_uint2(pu[0], pu[V / 4 - 1]); *(uint2 *)(to + W) = make_uint2(pd[0], pd[V / 4 - 1]); }
+    }
+    for (u32 c = 2 * W + lane; c < G * 64; c += 32) su[t * ROW + c] = 0;
   }
   __syncthreads();
-  uint4 qa[G][2];
-  const u32 j = lane % 4, r = lane / 4;
+  uint4 qa[M][G][2];
 #pragma unroll
-  for (u32 g = 0; g < G; ++g) {
-    qa[g][0] = *(const uint4 *)(su + r * ROW + g * 64 + j * 16);
-    qa[g][1] = *(const uint4 *)(su + (r + 8) * ROW + g * 64 + j * 16);
-  }
-  const u32 *const table = a.b.table + seq * a.b.table_stride;
-  u32 *const out = a.scores + ((u64)(p.t0 - a.slab_begin) * H + h) * a.scores_stride;
-  const u64 token = (u64)H * a.scores_stride;
-  auto slot_of = [&](u32 b) { return b + r < b1 ? table[b + r] : ~0u; };
-  struct Codes { uint4 v[G]; u32 e; };
-  auto load = [&](u32 b, u32 slot) {
-    Codes x;
-    const bool fine = slot < a.k.n_slots;
-    if (!fine && b + r < b1 && j == 0) kv_err(a.err, KVERR_RANGE);
-    const int8_t *const src = a.k.codes + ((fine ? (u64)slot : 0ull) * H + h) * 2 * W + j * 16;
-#pragma unroll
-    for (u32 g = 0; g < G; ++g)
-      x.v[g] = fine && g * 64 + j * 16 < 2 * W ? *(const uint4 *)(src + g * 64) : make_uint4(0, 0, 0, 0);
-    x.e = fine ? a.k.exps[(u64)slot * H + h] : 256;
-    return x;
-  };
-  u32 b = b0 + warp * 8;
-  if (b >= b1) return;
-  u32 next_slot = slot_of(b + 64);
-  Codes now = load(b, slot_of(b));
-  for (; b < b1; b += 64) {
-    Codes next;
-    if (b + 64 < b1) { next = load(b + 64, next_slot); next_slot = b + 128 < b1 ? slot_of(b + 128) : ~0u; }
-    int c[4] = {0, 0, 0, 0};
+  for (u32 m = 0; m < M; ++m)
 #pragma unroll
     for (u32 g = 0; g < G; ++g) {
-      mma_u8s8(c, qa[g][0].x, qa[g][1].x, qa[g][0].y, qa[g][1].y, now.v[g].x, now.v[g].y);
-      mma_u8s8(c, qa[g][0].z, qa[g][1].z, qa[g][0].w, qa[g][1].w, now.v[g].z, now.v[g].w);
+      qa[m][g][0] = *(const uint4 *)(su + (m * 16 + r) * ROW + g * 64 + j * 16);
+      qa[m][g][1] = *(const uint4 *)(su + (m * 16 + r + 8) * ROW + g * 64 + j * 16);
     }
-    // this lane's scores: tokens r and r + 8, blocks b + 2 j and b + 2 j + 1, whose exponents lanes 8 j and 8 j + 4 hold
-    const u32 e0 = __shfl_sync(~0u, now.e, 8 * j), e1 = __shfl_sync(~0u, now.e, 8 * j + 4);
-    auto score = [](int sum, u32 e) { return e > 255 ? 0u : ordered(fmaf((float)sum, __uint_as_float(e << 23), 0.0f)); };     // no slot: last of all
+  const u64 token = (u64)H * a.scores_stride;
+  u32 *out = a.scores + ((u64)(p.t0 - a.slab_begin + r) * H + h) * a.scores_stride + b + 2 * j;      // token r's, blocks b + 2 j and the next
+  bool ok = true;
+  while (ok && b < b1) {
 #pragma unroll
-    for (u32 y = 0; y < 2; ++y)
-      if (r + 8 * y < p.n) *(uint2 *)(out + (r + 8 * y) * token + b + 2 * j) = make_uint2(score(c[2 * y], e0), score(c[2 * y + 1], e1));
-    now = next;
+    for (u32 st = 0; st < SCORE_STAGES; ++st) {
+      if (b >= b1 || !(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, phase)))) break;
+      // scale and, where there is no slot, a score below all others
+      const u32 e0 = __shfl_sync(~0u, e[st], 2 * j), e1 = __shfl_sync(~0u, e[st], 2 * j + 1);
+      const float s0 = __uint_as_float(e0 > 255 ? 0u : e0 << 23), s1 = __uint_as_float(e1 > 255 ? 0u : e1 << 23), d0 = e0 > 255 ? -INFINITY : 0.0f, d1 = e1 > 255 ? -INFINITY : 0.0f;
+      int c[M][4];
+#pragma unroll
+      for (u32 m = 0; m < M; ++m) c[m][0] = c[m][1] = c[m][2] = c[m][3] = 0;
+#pragma unroll
+      for (u32 g = 0; g < G; ++g) {
+        u32 v[4];
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(ring + st * S::STAGE + r * S::PITCH + g * 64 + j * 16) : "memory");
+#pragma unroll
+        for (u32 m = 0; m < M; ++m) {
+          mma_u8s8(c[m], qa[m][g][0].x, qa[m][g][1].x, qa[m][g][0].y, qa[m][g][1].y, v[0], v[1]);
+          mma_u8s8(c[m], qa[m][g][0].z, qa[m][g][1].z, qa[m][g][0].w, qa[m][g][1].w, v[2], v[3]);
+        }
+      }
+      __syncwarp();                      // the stage is read
+      if (b + 64 * SCORE_STAGES < b1) {
+        e[st] = load(st, b + 64 * SCORE_STAGES, slot);
+        slot = slot_of(b + 64 * (SCORE_STAGES + 1));
+      }
+#pragma unroll
+      for (u32 m = 0; m < M; ++m)
+#pragma unroll
+        for (u32 y = 0; y < 2; ++y)
+          if (m * 16 + r + 8 * y < p.n)
+            *(uint2 *)(out + (m * 16 + 8 * y) * token) = make_uint2(ordered(fmaf((float)c[m][2 * y], s0, d0)), ordered(fmaf((float)c[m][2 * y + 1], s1, d1)));
+      b += 64; out += 64;
+    }
+    phase ^= 1;
+  }
+  if (!ok) {                             // let the copies in flight land, for a while
+    if (lane == 0) kv_err(a.err, KVERR_WAIT);
+    for (u32 i = 0; i < SCORE_STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
   }
 }
 
 // The blocks of a token and KV head, in order: the first ones, those of the largest scores, the last ones.
-template <u32 THREADS>
+constexpr u32 PICK_CAP = 512;            // candidates
+// VECTORS: the row's scores in registers, 16 bytes so many times per thread; 0: in shared memory as far as `held` of them fit, else where they are.
+template <u32 THREADS, u32 VECTORS>
 __global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held) {
+  constexpr u32 WARPS = THREADS / 32;
   extern __shared__ u32 s_keys[];
+  __shared__ u32 s_n, s_least[WARPS];
+  __shared__ u64 s_key[PICK_CAP];
+  __shared__ u32 s_bits[THREADS], s_count[WARPS];        // VECTORS: a bit per block that is taken
+  __shared__ u8 taken[PICK_CAP];         // else: whether a candidate is among the m largest
   const u32 tid = threadIdx.x, H = a.n_kv_heads, t = a.slab_begin + blockIdx.x / H, h = blockIdx.x % H;
   const Where w = find_token<false>(a.b, t, a.err);
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the scores; the batch's arrays are older than the kernel before this one
   if (w.seq >= a.b.n_seqs) return;                       // behind the last sequence
   int32_t *const out = a.out + ((u64)t * H + h) * a.n_blocks;
   const u32 own = w.index / BT;
@@ -387,13 +467,113 @@ __global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held)
     for (u32 i = tid; i < a.n_blocks; i += THREADS) out[i] = w.ok && i <= own ? (int32_t)i : -1;
     return;
   }
-  const u32 n = own + 1 - a.first - a.last, m = a.n_blocks - a.first - a.last;
-  const u32 *const scores = a.scores + ((u64)(t - a.slab_begin) * H + h) * a.scores_stride + a.first;
-  for (u32 i = tid; i < a.first + a.last; i += THREADS) out[i < a.first ? i : i + m] = i < a.first ? i : (int32_t)(own + 1 - a.last + i - a.first);
-  if (n <= held) for (u32 i = tid; i < n; i += THREADS) s_keys[i] = scores[i];
-  __syncthreads();
+  // of the blocks [first, end) m are taken
+  const u32 end = own + 1 - a.last, n = end - a.first, m = a.n_blocks - a.first - a.last;
+  const u32 *const scores = a.scores + ((u64)(t - a.slab_begin) * H + h) * a.scores_stride;
+  for (u32 i = tid; i < a.first + a.last; i += THREADS) out[i < a.first ? i : i + m] = i < a.first ? (int32_t)i : (int32_t)(end + i - a.first);
   if (!m) return;
-  const u32 *const keys = n <= held ? s_keys : scores;
+  u32 most = 0;
+  constexpr u32 VN = VECTORS ? VECTORS : 1;
+  uint4 v[VN];
+  auto mine = [&](u32 y, u32 z) { return z == 0 ? v[y].x : z == 1 ? v[y].y : z == 2 ? v[y].z : v[y].w; };
+  if constexpr (VECTORS > 0) {
+#pragma unroll
+    for (u32 y = 0; y < VN; ++y) {
+      const u32 i = 4 * (tid + y * THREADS);
+      v[y] = i < end ? *(const uint4 *)(scores + i) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (u32 y = 0; y < VN; ++y) {
+      const u32 i = 4 * (tid + y * THREADS);
+      if (i < a.first || i + 4 > end) {                  // what is not to be chosen counts as 0, and is known by its place
+        if (i < a.first || i >= end) v[y].x = 0;
+        if (i + 1 < a.first || i + 1 >= end) v[y].y = 0;
+        if (i + 2 < a.first || i + 2 >= end) v[y].z = 0;
+        if (i + 3 < a.first || i + 3 >= end) v[y].w = 0;
+      }
+      most = max(max(most, max(v[y].x, v[y].y)), max(v[y].z, v[y].w));
+    }
+  } else {
+    for (u32 i = tid; i < n; i += THREADS) {
+      const u32 x = scores[a.first + i];
+      if (n <= held) s_keys[i] = x;
+      most = max(most, x);
+    }
+  }
+  // Few of many. With k = m / warps, rounded up, every warp has k threads whose largest is not below the k-th largest of these; the least
+  // of the warps' k-th is below at least m scores, then, and above nearly all others. What it leaves is put in order by counting.
+  const u32 k = (m + WARPS - 1) / WARPS;
+  if (k <= 16 && n >= 4 * THREADS) {
+    u32 x = most, kth = 0;
+    for (u32 y = 0; y < k; ++y) {
+      kth = __reduce_max_sync(~0u, x);
+      if (tid % 32 == __ffs(__ballot_sync(~0u, x == kth)) - 1) x = 0;
+    }
+    if (tid % 32 == 0) s_least[tid / 32] = kth;
+    if (tid == 0) s_n = 0;
+    s_bits[tid] = 0;
+    __syncthreads();
+    u32 least = s_least[tid % WARPS];
+    least = __reduce_min_sync(~0u, least);
+    auto candidate = [&](u32 x, u32 i) {                 // i: number of the block; of equal scores the lower one is the larger key
+      const u32 at = atomicAdd(&s_n, 1u);
+      if (at < PICK_CAP) s_key[at] = (u64)x << 32 | (u32)~i;
+    };
+    if (most >= least) {
+      if constexpr (VECTORS > 0) {       // few threads have more than one: a mask, then the scores once more from the cache
+        u32 mask = 0;
+#pragma unroll
+        for (u32 y = 0; y < VN; ++y)
+#pragma unroll
+          for (u32 z = 0; z < 4; ++z) mask |= mine(y, z) >= least ? 1u << (4 * y + z) : 0u;
+        for (; mask; mask &= mask - 1) {
+          const u32 at = __ffs(mask) - 1, i = 4 * (tid + at / 4 * THREADS) + at % 4;
+          if (i >= a.first && i < end) candidate(scores[i], i);
+        }
+      } else {
+        for (u32 i = tid; i < n; i += THREADS) {
+          const u32 x = n <= held ? s_keys[i] : scores[a.first + i];
+          if (x >= least) candidate(x, a.first + i);
+        }
+      }
+    }
+    __syncthreads();
+    const u32 c = s_n;
+    if (c <= PICK_CAP) {
+      for (u32 i = tid; i < c; i += THREADS) {
+        const u64 x = s_key[i];
+        u32 before = 0;
+#pragma unroll 4
+        for (u32 y = 0; y < c; ++y) before += s_key[y] > x;
+        if constexpr (VECTORS > 0) { if (before < m) atomicOr(&s_bits[~(u32)x / 32], 1u << (~(u32)x % 32)); }
+        else taken[i] = before < m;
+      }
+      __syncthreads();
+      if constexpr (VECTORS > 0) {       // in order: a word of 32 blocks per thread
+        static_assert(VECTORS <= 8, "a bit for every block");
+        u32 word = s_bits[tid], incl = __popc(word);
+#pragma unroll
+        for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (tid % 32 >= o) incl += z; }
+        if (tid % 32 == 31) s_count[tid / 32] = incl;
+        __syncthreads();
+        u32 at = a.first + incl - __popc(word);
+        for (u32 y = 0; y < tid / 32; ++y) at += s_count[y];
+        for (; word; word &= word - 1) out[at++] = (int32_t)(tid * 32 + __ffs(word) - 1);
+        return;
+      }
+      for (u32 i = tid; i < c; i += THREADS) {
+        if (!taken[i]) continue;
+        const u32 x = (u32)s_key[i];     // the larger, the lower the number
+        u32 before = 0;
+#pragma unroll 4
+        for (u32 y = 0; y < c; ++y) before += taken[y] && (u32)s_key[y] > x;
+        out[a.first + before] = (int32_t)~x;
+      }
+      return;
+    }
+  }
+  __syncthreads();
+  const u32 *const keys = VECTORS == 0 && n <= held ? s_keys : scores + a.first;
   const Kth kth = kth_largest<THREADS>([&](u32 i) { return keys[i]; }, n, m);
   __syncthreads();
   // keys equal to the last one that is taken: the first `ties` of them. Both lists in one go where all of them are taken.
@@ -420,37 +600,58 @@ SelectPlan plan_select(const SelectArgs &a, int sm_count) {
   return p;
 }
 
-template <class T>
-static void score_blocks(const SelectArgs &a, dim3 grid, u32 shares, cudaStream_t s) {
-  if (a.k.width <= 64) k_score_blocks<T, 2><<<grid, 256, 0, s>>>(a, shares);
-  else if (a.k.width <= 128) k_score_blocks<T, 4><<<grid, 256, 0, s>>>(a, shares);
-  else k_score_blocks<T, 8><<<grid, 256, 0, s>>>(a, shares);
-}
-template <u32 THREADS>
-static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, u32 held, u32 which, cudaStream_t s, u64 *allowed) {
-  const cudaError_t r = allow_smem(k_pick_blocks<THREADS>, which, 200 * 1024, allowed);
+template <class T, u32 G, u32 M>
+static cudaError_t score_blocks(const SelectArgs &a, dim3 grid, u32 shares, u32 which, cudaStream_t s, u64 *allowed) {
+  const cudaError_t r = allow_smem(k_score_blocks<T, G, M>, which + 32, ScoreRing<G>::SMEM, allowed + 1);
   if (r != cudaSuccess) return r;
-  k_pick_blocks<THREADS><<<rows, THREADS, held * 4, s>>>(a, held);
+  k_score_blocks<T, G, M><<<grid, 256, ScoreRing<G>::SMEM, s>>>(a, shares);
   return cudaGetLastError();
+}
+template <class T>
+static cudaError_t score_blocks(const SelectArgs &a, dim3 grid, u32 shares, bool wide, cudaStream_t s, u64 *allowed) {
+  constexpr u32 F = __is_same(T, __half) * 8;
+  if (wide && a.k.width <= 64) return score_blocks<T, 2, 2>(a, grid, shares, F + 0, s, allowed);
+  if (wide) return score_blocks<T, 4, 2>(a, grid, shares, F + 1, s, allowed);
+  if (a.k.width <= 64) return score_blocks<T, 2, 1>(a, grid, shares, F + 2, s, allowed);
+  if (a.k.width <= 128) return score_blocks<T, 4, 1>(a, grid, shares, F + 3, s, allowed);
+  return score_blocks<T, 8, 1>(a, grid, shares, F + 4, s, allowed);
+}
+template <u32 THREADS, u32 VECTORS>
+static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, u32 held, bool scored, cudaStream_t s) {
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3(rows); c.blockDim = dim3(THREADS); c.dynamicSmemBytes = held * 4; c.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at; c.numAttrs = scored;    // behind a kernel of this call only: the batch's arrays may be of the kernel before that
+  return cudaLaunchKernelEx(&c, k_pick_blocks<THREADS, VECTORS>, a, held);
+}
+static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, bool scored, cudaStream_t s, u64 *allowed) {
+  if (a.b.max_blocks <= 2048) return pick_blocks<256, 2>(a, rows, 0, scored, s);
+  if (a.b.max_blocks <= 4096) return pick_blocks<256, 4>(a, rows, 0, scored, s);
+  if (a.b.max_blocks <= 8192) return pick_blocks<256, 8>(a, rows, 0, scored, s);
+  if (a.b.max_blocks <= 16384) return pick_blocks<512, 8>(a, rows, 0, scored, s);
+  if (a.b.max_blocks <= 32768) return pick_blocks<1024, 8>(a, rows, 0, scored, s);
+  const cudaError_t r = allow_smem(k_pick_blocks<1024, 0>, 0, 200 * 1024, allowed);
+  if (r != cudaSuccess) return r;
+  return pick_blocks<1024, 0>(a, rows, std::min(a.b.max_blocks, 50u * 1024), scored, s);         // scores in shared memory
 }
 cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, u64 *allowed, u32 *launches) {
   a.scores_stride = p.scores_stride;
-  const u32 held = (u32)std::min<u64>(a.b.max_blocks, 50 * 1024);        // keys in shared memory
   for (u32 t = 0; t < a.b.n_tokens; t += p.slab) {
     a.slab_begin = t; a.slab_end = std::min(a.b.n_tokens, t + p.slab);
     const u32 n = a.slab_end - t;
-    const u32 tiles = (u32)(((u64)n + 15ull * std::min(a.b.n_seqs, n)) / 16);
+    // tiles of 32 tokens where the sequences bring as many on average: half the codes are read
+    const bool wide = a.k.width <= 128 && n / a.b.n_seqs >= 24;
+    const u32 rows_of = wide ? 32 : 16, tiles = (u32)(((u64)n + (rows_of - 1ull) * std::min(a.b.n_seqs, n)) / rows_of);
     if (a.b.max_blocks > a.n_blocks) {
-      const u32 shares = std::max(1u, std::min((a.b.max_blocks + 63) / 64, 4 * p.sms / std::max(1u, tiles * a.n_kv_heads)));
+      const u32 shares = std::max(1u, std::min((a.b.max_blocks + 63) / 64, 2 * p.sms / std::max(1u, tiles * a.n_kv_heads)));
       const dim3 grid(tiles, a.n_kv_heads, shares);
-      if (a.fp16) score_blocks<__half>(a, grid, shares, s); else score_blocks<__nv_bfloat16>(a, grid, shares, s);
+      const cudaError_t r = a.fp16 ? score_blocks<__half>(a, grid, shares, wide, s, allowed) : score_blocks<__nv_bfloat16>(a, grid, shares, wide, s, allowed);
       ++*launches;
-      const cudaError_t r = cudaGetLastError();
       if (r != cudaSuccess) return r;
     }
-    const u32 rows = n * a.n_kv_heads;
-    const cudaError_t r = rows < 2 * p.sms && a.b.max_blocks > 2048 ? pick_blocks<1024>(a, rows, held, 0, s, allowed)
-                                                                     : pick_blocks<256>(a, rows, held, 1, s, allowed);
+    const cudaError_t r = pick_blocks(a, n * a.n_kv_heads, a.b.max_blocks > a.n_blocks, s, allowed);
     ++*launches;
     if (r != cudaSuccess) return r;
   }

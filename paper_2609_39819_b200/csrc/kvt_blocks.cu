@@ -146,59 +146,61 @@ cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, u32 *
 }
 
 // ======================================================================================================
-// The m-th largest of n keys, for a whole CTA, by digits of 8 bits from the top of what tells the smallest from the largest.
+// The m-th largest of n keys, for a whole CTA, by digits from the top: 12, 12 and 8 bits. Once few keys begin like the one in question they
+// are put into a list, which the next digits are counted in. each(f) calls f with every key that is this thread's.
 // A key x is among the m largest if x > at, or x == at and fewer than `ties` keys equal to it come before.
 // ======================================================================================================
 struct Kth { u32 at, ties; };
-template <u32 THREADS, class Key>
-__device__ __forceinline__ Kth kth_largest(Key key, u32 n, u32 m) {
-  __shared__ u32 s_hist[256], s_lo, s_hi, s_digit, s_left, s_all;
-  const u32 tid = threadIdx.x, lane = tid & 31;
+constexpr u32 KTH_LIST = 1024;
+template <u32 THREADS, class Each>
+__device__ __forceinline__ Kth kth_largest(Each each, u32 n, u32 m) {
+  constexpr u32 BINS = 4096, PER = BINS / THREADS, WARPS = THREADS / 32;
+  __shared__ u32 s_hist[BINS], s_list[KTH_LIST], s_sum[WARPS], s_digit, s_left, s_here, s_n;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (m >= n) return Kth{0, ~0u};                        // all: no key is below 0
-  if (tid == 0) { s_lo = ~0u; s_hi = 0; }
-  __syncthreads();
-  u32 lo = ~0u, hi = 0;
-  for (u32 i = tid; i < n; i += THREADS) { const u32 x = key(i); lo = min(lo, x); hi = max(hi, x); }
-  lo = __reduce_min_sync(~0u, lo); hi = __reduce_max_sync(~0u, hi);
-  if (lane == 0) { atomicMin(&s_lo, lo); atomicMax(&s_hi, hi); }
-  __syncthreads();
-  lo = s_lo; hi = s_hi;
-  u32 bits = 32 - __clz(hi - lo), prefix = 0, left = m;  // prefix: the digits above `bits` of the key in question
-  while (bits) {
-    const u32 shift = bits > 8 ? bits - 8 : 0, width = bits - shift;
-    for (u32 i = tid; i < 256; i += THREADS) s_hist[i] = 0;
+  u32 prefix = 0, left = m, listed = 0;                  // prefix: the digits in front of the one in hand
+#pragma unroll 1
+  for (u32 bits = 32; bits;) {
+    const u32 shift = bits == 32 ? 20 : bits == 20 ? 8 : 0, mask = (1u << (bits - shift)) - 1;
+    for (u32 i = tid; i < BINS; i += THREADS) s_hist[i] = 0;
+    if (tid == 0) s_n = 0;
     __syncthreads();
-    for (u32 i = tid; i < n; i += THREADS) {
-      const u32 x = key(i) - lo;
-      if ((u64)x >> bits == prefix) atomicAdd(&s_hist[x >> shift & ((1u << width) - 1)], 1u);
-    }
+    auto count = [&](u32 x) { if ((u64)x >> bits == prefix) atomicAdd(&s_hist[x >> shift & mask], 1u); };
+    if (listed) { for (u32 i = tid; i < listed; i += THREADS) count(s_list[i]); }
+    else each(count);
     __syncthreads();
-    if (tid < 32) {                                      // lane l: digits 255 - 8 l downwards
-      u32 c[8], sum = 0;
+    // this thread's digits: PER of them downwards from BINS - 1 - tid * PER
+    u32 c[PER], sum = 0;
 #pragma unroll
-      for (u32 y = 0; y < 8; ++y) { c[y] = s_hist[255 - 8 * lane - y]; sum += c[y]; }
-      u32 incl = sum;
+    for (u32 y = 0; y < PER; ++y) { c[y] = s_hist[BINS - 1 - tid * PER - y]; sum += c[y]; }
+    u32 incl = sum;
 #pragma unroll
-      for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
-      u32 before = incl - sum;
-      if (before < left && left <= incl) {
-        u32 y = 0;
+    for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
+    if (lane == 31) s_sum[warp] = incl;
+    __syncthreads();
+    u32 before = incl - sum;
+#pragma unroll 8
+    for (u32 w = 0; w < WARPS; ++w) before += w < warp ? s_sum[w] : 0u;
+    if (before < left && left <= before + sum) {
 #pragma unroll
-        for (u32 z = 0; z < 7; ++z) if (y == z && before + c[z] < left) { before += c[z]; ++y; }
-        u32 here = c[0];
-#pragma unroll
-        for (u32 z = 1; z < 8; ++z) if (y == z) here = c[z];
-        s_digit = 255 - 8 * lane - y; s_left = left - before; s_all = here == left - before;
+      for (u32 y = 0; y < PER; ++y) {
+        if (before < left && left <= before + c[y]) { s_digit = BINS - 1 - tid * PER - y; s_left = left - before; s_here = c[y]; }
+        before += c[y];
       }
     }
     __syncthreads();
-    prefix = prefix << width | s_digit;
+    prefix = prefix << (bits - shift) | s_digit;
     left = s_left;
     bits = shift;
-    if (s_all) return Kth{lo + (prefix << bits), ~0u};   // all that begin like this
-    // (the barriers of the next round stand between these reads and the next writes)
+    const u32 here = s_here;
+    if (here == left) return Kth{prefix << bits, ~0u};   // all that begin like this
+    if (bits && !listed && here <= KTH_LIST) {
+      each([&](u32 x) { if (x >> bits == prefix) s_list[atomicAdd(&s_n, 1u)] = x; });
+      listed = here;
+    }
+    __syncthreads();                                     // the digit is read, the list is written
   }
-  return Kth{lo + prefix, left};
+  return Kth{prefix, left};
 }
 
 // Deals the numbers i of [0, n) out in order: pick(i) says which list each goes to (bit 0: the first, bit 1: the second), put(i, which, place)
@@ -574,7 +576,7 @@ __global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held)
   }
   __syncthreads();
   const u32 *const keys = VECTORS == 0 && n <= held ? s_keys : scores + a.first;
-  const Kth kth = kth_largest<THREADS>([&](u32 i) { return keys[i]; }, n, m);
+  const Kth kth = kth_largest<THREADS>([&](auto f) { for (u32 i = tid; i < n; i += THREADS) f(keys[i]); }, n, m);
   __syncthreads();
   // keys equal to the last one that is taken: the first `ties` of them. Both lists in one go where all of them are taken.
   if (kth.ties == ~0u) {
@@ -632,9 +634,9 @@ static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, bool scored, cudaS
   if (a.b.max_blocks <= 8192) return pick_blocks<256, 8>(a, rows, 0, scored, s);
   if (a.b.max_blocks <= 16384) return pick_blocks<512, 8>(a, rows, 0, scored, s);
   if (a.b.max_blocks <= 32768) return pick_blocks<1024, 8>(a, rows, 0, scored, s);
-  const cudaError_t r = allow_smem(k_pick_blocks<1024, 0>, 0, 200 * 1024, allowed);
+  const cudaError_t r = allow_smem(k_pick_blocks<1024, 0>, 0, 180 * 1024, allowed);
   if (r != cudaSuccess) return r;
-  return pick_blocks<1024, 0>(a, rows, std::min(a.b.max_blocks, 50u * 1024), scored, s);         // scores in shared memory
+  return pick_blocks<1024, 0>(a, rows, std::min(a.b.max_blocks, 45u * 1024), scored, s);         // scores in shared memory
 }
 cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, u64 *allowed, u32 *launches) {
   a.scores_stride = p.scores_stride;
@@ -1879,13 +1881,99 @@ cudaError_t launch_weigh(const WeighArgs &x, const WeighPlan &p, const KvMaps &m
 }
 
 // ======================================================================================================
-// Eviction by weight: of a sequence's blocks the first, the last and the heaviest stay. Rows are packed in place: a CTA reads what it
-// is about to write over before it does.
+// Eviction by weight: of a sequence's blocks the first, the last and the heaviest stay. A CTA per sequence. Bound by latency: three rounds
+// of loads and some thirty barriers.
 // ======================================================================================================
 constexpr u32 EVICT_THREADS = 1024;
-__global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a, u32 held) {
+__device__ __forceinline__ u32 weight_order(float w) { return ordered(w == w ? w + 0.0f : INFINITY); }       // a NaN weighs most
+
+// R: the row in registers, so many blocks per thread, all of it read before anything is written, wherever the outputs are.
+template <u32 R>
+__global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a) {
+  __shared__ u32 s_n[R * 32], s_all[R];
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, seq = blockIdx.x;
+  u32 slot[R];
+  float w[R];
+#pragma unroll
+  for (u32 k = 0; k < R; ++k) {
+    const u32 i = tid + k * EVICT_THREADS;
+    if (i < a.max_blocks) { slot[k] = a.table[seq * a.table_stride + i]; w[k] = a.weights[seq * a.w_stride + i]; }
+  }
+  const u32 room = a.max_blocks * BT;
+  u32 kv = a.kv_len[seq];
+  if (kv > room) { if (tid == 0) kv_err(a.err, KVERR_RANGE); kv = room; }
+  const u32 had = (kv + BT - 1) / BT, gone = had > a.n_blocks ? had - a.n_blocks : 0, end = had - a.last;       // [first, end): those to choose from
+  // flags: a bit per block of this thread; at: how many flagged blocks of the sequence come before each
+  auto places = [&](u32 flags, u32 (&at)[R]) {
+#pragma unroll
+    for (u32 k = 0; k < R; ++k) {
+      const u32 b = __ballot_sync(~0u, flags >> k & 1);
+      at[k] = __popc(b & ((1u << lane) - 1));
+      if (lane == 0) s_n[k * 32 + warp] = __popc(b);
+    }
+    __syncthreads();
+    if (warp < R) {
+      const u32 mine = s_n[warp * 32 + lane];
+      u32 incl = mine;
+#pragma unroll
+      for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
+      s_n[warp * 32 + lane] = incl - mine;
+      if (lane == 31) s_all[warp] = incl;
+    }
+    __syncthreads();
+    u32 before = 0;
+#pragma unroll
+    for (u32 k = 0; k < R; ++k) { at[k] += before + s_n[k * 32 + warp]; before += s_all[k]; }
+    __syncthreads();
+  };
+  u32 stays = 0, at[R];
+#pragma unroll
+  for (u32 k = 0; k < R; ++k) {
+    const u32 i = tid + k * EVICT_THREADS;
+    if (i < had && (!gone || i < a.first || i >= end)) stays |= 1u << k;
+  }
+  const u32 m = gone ? end - a.first - gone : 0;       // to be kept of those to choose from
+  if (m) {
+    const Kth kth = kth_largest<EVICT_THREADS>([&](auto f) {
+#pragma unroll
+      for (u32 k = 0; k < R; ++k) { const u32 i = tid + k * EVICT_THREADS; if (i >= a.first && i < end) f(weight_order(w[k])); }
+    }, end - a.first, m);
+    u32 ties = 0;
+#pragma unroll
+    for (u32 k = 0; k < R; ++k) {
+      const u32 i = tid + k * EVICT_THREADS;
+      if (i < a.first || i >= end) continue;
+      const u32 x = weight_order(w[k]);
+      if (x > kth.at || (x == kth.at && kth.ties == ~0u)) stays |= 1u << k;
+      else if (x == kth.at) ties |= 1u << k;
+    }
+    if (kth.ties != ~0u) {               // of those that weigh the same the first ones
+      places(ties, at);
+#pragma unroll
+      for (u32 k = 0; k < R; ++k) if ((ties >> k & 1) && at[k] < kth.ties) stays |= 1u << k;
+    }
+  }
+  places(stays, at);
+  u32 *const table_out = a.table_out + seq * a.table_out_stride, *const evicted = a.evicted + seq * a.evicted_stride;
+  float *const weights_out = a.weights_out + seq * a.w_out_stride;
+  const u32 kept = had - gone;
+#pragma unroll
+  for (u32 k = 0; k < R; ++k) {
+    const u32 i = tid + k * EVICT_THREADS;
+    if (i < had) {
+      if (stays >> k & 1) { table_out[at[k]] = slot[k]; weights_out[at[k]] = w[k]; }
+      else evicted[i - at[k]] = slot[k];
+    }
+    if (i >= kept && i < a.max_blocks) { table_out[i] = ~0u; weights_out[i] = 0.0f; }
+    if (i >= gone && i < a.max_blocks) evicted[i] = ~0u;
+  }
+  if (tid == 0) a.kv_len_out[seq] = kv - gone * BT;
+}
+
+// Rows of any length, 4 K blocks at a time: read, then written at or in front of where they were.
+__global__ void __launch_bounds__(EVICT_THREADS) k_evict_long(EvictArgs a, u32 held) {
   extern __shared__ u32 s_keys[];
-  __shared__ u32 s_border, s_n[2][EVICT_THREADS / 32];
+  __shared__ u32 s_border, s_n[EVICT_THREADS / 32];
   const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, seq = blockIdx.x;
   const u32 *const table = a.table + seq * a.table_stride;
   const float *const weights = a.weights + seq * a.w_stride;
@@ -1895,7 +1983,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a, u32
   u32 kv = a.kv_len[seq];
   if (kv > room) { if (tid == 0) kv_err(a.err, KVERR_RANGE); kv = room; }
   const u32 had = (kv + BT - 1) / BT, gone = had > a.n_blocks ? had - a.n_blocks : 0;
-  auto order = [&](float w) { return ordered(w == w ? w + 0.0f : INFINITY); };       // a NaN weighs most
+  auto order = [&](float w) { return weight_order(w); };
   Kth kth{0, ~0u};
   u32 border = 0;
   if (gone) {                            // of the n blocks between the first and the last ones m stay
@@ -1904,7 +1992,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a, u32
     if (n <= held) for (u32 i = tid; i < n; i += EVICT_THREADS) s_keys[i] = order(w[i]);
     __syncthreads();
     auto key = [&](u32 i) { return n <= held ? s_keys[i] : order(w[i]); };
-    if (m) kth = kth_largest<EVICT_THREADS>(key, n, m); else kth = Kth{~0u, 0};
+    if (m) kth = kth_largest<EVICT_THREADS>([&](auto f) { for (u32 i = tid; i < n; i += EVICT_THREADS) f(key(i)); }, n, m); else kth = Kth{~0u, 0};
     __syncthreads();
     if (kth.ties != ~0u && kth.ties) {
       deal<EVICT_THREADS>(n, [&](u32 i) { return key(i) == kth.at ? 1u : 0u; }, [&](u32 i, u32, u32 at) { if (at == kth.ties - 1) s_border = i; });
@@ -1932,11 +2020,11 @@ __global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a, u32
 #pragma unroll
     for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
     __syncthreads();                     // everything is read; the sums of the round before too
-    if (lane == 31) s_n[0][warp] = incl;
+    if (lane == 31) s_n[warp] = incl;
     __syncthreads();
     u32 before = 0, all = 0;
 #pragma unroll
-    for (u32 v = 0; v < EVICT_THREADS / 32; ++v) { if (v < warp) before += s_n[0][v]; all += s_n[0][v]; }
+    for (u32 v = 0; v < EVICT_THREADS / 32; ++v) { if (v < warp) before += s_n[v]; all += s_n[v]; }
     before += incl - here;
     u32 to[2] = {at[0] + (before & 0xFFFF), at[1] + (before >> 16)};
 #pragma unroll
@@ -1954,10 +2042,15 @@ __global__ void __launch_bounds__(EVICT_THREADS) k_evict_blocks(EvictArgs a, u32
 }
 
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t s, u64 *allowed, u32 *launches) {
-  const cudaError_t r = allow_smem(k_evict_blocks, 2, 200 * 1024, allowed);
-  if (r != cudaSuccess) return r;
-  const u32 held = (u32)std::min<u64>(a.max_blocks, 50 * 1024);
-  k_evict_blocks<<<a.n_seqs, EVICT_THREADS, held * 4, s>>>(a, held);
+  if (a.max_blocks <= 4096) k_evict_blocks<4><<<a.n_seqs, EVICT_THREADS, 0, s>>>(a);
+  else if (a.max_blocks <= 8192) k_evict_blocks<8><<<a.n_seqs, EVICT_THREADS, 0, s>>>(a);
+  else if (a.max_blocks <= 16384) k_evict_blocks<16><<<a.n_seqs, EVICT_THREADS, 0, s>>>(a);
+  else {
+    const u32 held = std::min(a.max_blocks, 45u * 1024);         // keys in shared memory
+    const cudaError_t r = allow_smem(k_evict_long, 2, 180 * 1024, allowed);
+    if (r != cudaSuccess) return r;
+    k_evict_long<<<a.n_seqs, EVICT_THREADS, held * 4, s>>>(a, held);
+  }
   ++*launches;
   return cudaGetLastError();
 }

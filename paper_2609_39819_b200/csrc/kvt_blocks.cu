@@ -37,28 +37,35 @@ template <class T> struct Pair;
 template <> struct Pair<__nv_bfloat16> { typedef __nv_bfloat162 T2; };
 template <> struct Pair<__half> { typedef __half2 T2; };
 
-// A CTA looks at 16 tokens; a warp takes a head of a block that one of them fills. VEC: heads of D channels, 16 bytes of a token
-// per lane, all loads of a lane in flight at once.
+// A CTA looks at `rows` tokens, one per thread; a warp takes a head of a block that one of them fills. VEC: heads of D channels, 16 bytes
+// of a token per lane, all loads of a lane in flight at once.
+constexpr u32 BOUND_ROWS = 64;
 template <class T, u32 D>
-__global__ void __launch_bounds__(256) k_bound_keys(BoundArgs a) {
-  __shared__ u32 s_slot[16];
-  const u32 lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = a.p.n_kv_heads;
-  for (u32 i = warp; i < 16; i += 8) {
-    const u32 t = blockIdx.x * 16 + i;
-    u32 slot = ~0u;
-    if (t < a.b.n_tokens) {
-      const Where w = find_token<true>(a.b, t, a.err);
-      if (w.seq < a.b.n_seqs && w.ok && w.index % BT == BT - 1) {
-        slot = a.b.table[w.seq * a.b.table_stride + w.index / BT];
-        if (slot >= a.k.n_slots || !slot_ptr(a.p, a.p.k, slot)) { if (lane == 0) kv_err(a.err, KVERR_RANGE); slot = ~0u; }
+__global__ void __launch_bounds__(256) k_bound_keys(BoundArgs a, u32 rows) {
+  __shared__ u32 s_slot[BOUND_ROWS], s_n;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
+  if (blockIdx.x == 0 && blockIdx.y == 0)                // one CTA looks all starts over
+    for (u32 s = tid; s < a.b.n_seqs; s += 256) if (a.b.q_start[s] > a.b.q_start[s + 1]) kv_err(a.err, KVERR_RANGE);
+  if (tid == 0) s_n = 0;
+  __syncthreads();
+  const u32 t = blockIdx.x * rows + tid;
+  if (tid < rows && t < a.b.n_tokens) {
+    u32 lo = 0, hi = a.b.n_seqs;                         // the sequence: the first that ends behind the token
+    while (lo < hi) { const u32 mid = (lo + hi) / 2; if (a.b.q_start[mid + 1] <= t) lo = mid + 1; else hi = mid; }
+    if (lo < a.b.n_seqs) {
+      const u32 from = a.b.q_start[lo], to = a.b.q_start[lo + 1], kv = a.b.kv_len[lo], index = kv - (to - t);
+      if (t < from || to > a.b.n_tokens || kv > (u64)a.b.max_blocks * BT || kv < to - from) kv_err(a.err, KVERR_RANGE);
+      if (t >= from && kv >= to - t && index / BT < a.b.max_blocks && index % BT == BT - 1) {
+        const u32 slot = a.b.table[lo * a.b.table_stride + index / BT];
+        if (slot >= a.k.n_slots || !slot_ptr(a.p, a.p.k, slot)) kv_err(a.err, KVERR_RANGE);
+        else s_slot[atomicAdd(&s_n, 1u)] = slot;
       }
     }
-    if (lane == 0) s_slot[i] = slot;
   }
   __syncthreads();
-  const u32 slots = s_slot[lane % 16], filled = __ballot_sync(~0u, lane < 16 && slots != ~0u), n_items = __popc(filled) * H;
+  const u32 n_items = s_n * H;
   for (u32 item = blockIdx.y * 8 + warp; item < n_items; item += 8 * gridDim.y) {
-    const u32 which = item / H, h = item - which * H, slot = __shfl_sync(~0u, slots, __fns(filled, 0, which + 1));
+    const u32 which = item / H, h = item - which * H, slot = s_slot[which];
     const u16 *const src = (const u16 *)slot_ptr(a.p, a.p.k, slot);
     int8_t *const to = a.k.codes + ((u64)slot * H + h) * 2 * a.k.width;
     u8 *const exp_to = a.k.exps + (u64)slot * H + h;
@@ -130,18 +137,19 @@ __global__ void __launch_bounds__(256) k_bound_keys(BoundArgs a) {
 }
 
 template <class T>
-static void bound_keys(const BoundArgs &a, dim3 grid, cudaStream_t s) {
+static void bound_keys(const BoundArgs &a, dim3 grid, u32 rows, cudaStream_t s) {
   const bool aligned = (((uintptr_t)a.p.k.base | (uintptr_t)a.p.k.tail) & 15) == 0;
-  if (aligned && a.p.head_dim == 128) k_bound_keys<T, 128><<<grid, 256, 0, s>>>(a);
-  else if (aligned && a.p.head_dim == 64) k_bound_keys<T, 64><<<grid, 256, 0, s>>>(a);
-  else k_bound_keys<T, 0><<<grid, 256, 0, s>>>(a);
+  if (aligned && a.p.head_dim == 128) k_bound_keys<T, 128><<<grid, 256, 0, s>>>(a, rows);
+  else if (aligned && a.p.head_dim == 64) k_bound_keys<T, 64><<<grid, 256, 0, s>>>(a, rows);
+  else k_bound_keys<T, 0><<<grid, 256, 0, s>>>(a, rows);
 }
 cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, u32 *launches) {
-  const u32 ctas = (a.b.n_tokens + 15) / 16;
+  // long batches: several blocks per CTA, since finding them costs as much as one
+  const u32 rows = a.b.n_tokens >= 64u * sm_count ? BOUND_ROWS : 16, ctas = (a.b.n_tokens + rows - 1) / rows;
   const dim3 grid(ctas, std::max(1u, std::min(a.p.n_kv_heads, 2u * sm_count / ctas)));
   ++*launches;
-  if (a.fp16) bound_keys<__half>(a, grid, s);
-  else bound_keys<__nv_bfloat16>(a, grid, s);
+  if (a.fp16) bound_keys<__half>(a, grid, rows, s);
+  else bound_keys<__nv_bfloat16>(a, grid, rows, s);
   return cudaGetLastError();
 }
 

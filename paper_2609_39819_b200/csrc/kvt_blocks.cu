@@ -612,7 +612,7 @@ SelectPlan plan_select(const SelectArgs &a, int sm_count) {
 
 template <class T, u32 G, u32 M>
 static cudaError_t score_blocks(const SelectArgs &a, dim3 grid, u32 shares, u32 which, cudaStream_t s, u64 *allowed) {
-  const cudaError_t r = allow_smem(k_score_blocks<T, G, M>, which + 32, ScoreRing<G>::SMEM, allowed + 1);
+  const cudaError_t r = allow_smem(k_score_blocks<T, G, M>, which + 24, ScoreRing<G>::SMEM, allowed + 1);
   if (r != cudaSuccess) return r;
   k_score_blocks<T, G, M><<<grid, 256, ScoreRing<G>::SMEM, s>>>(a, shares);
   return cudaGetLastError();
@@ -684,12 +684,13 @@ __device__ __forceinline__ u32 transposed(u32 x) {       // an 8 x 8 matrix of 1
   return y;
 }
 
-// The blocks at list places part, part + parts, ... below n for the columns of a unit, into o, m, l (see k_attend_blocks). A lane has
+// The blocks at list places part, part + parts, ... below n for the columns of a unit, into o, m, l (see k_attend_blocks). `it`: stages used
+// so far. A lane has
 // columns n * 8 + 2 (lane % 4) and the next, keys / channels lane / 4 and 8 further. DOUBLE: columns 4 to 7 are those 0 to 3 once
 // more and take the second numbers of the powers.
 template <class T, u32 D, u32 NT, bool DOUBLE, bool ANY>
 __device__ __forceinline__ bool list_keys(const AttendListArgs &x, const KvMaps &maps, const u32 *table, const int32_t *list, u32 n, u32 index, u32 h,
-                                          const u16 *const (&q)[NT], u32 part, u32 parts, u32 ring, u32 bar0, u32 *s_block,
+                                          const u16 *const (&q)[NT], u32 part, u32 parts, u32 ring, u32 bar0, u32 *s_block, u32 &it,
                                           float (&o)[D / 16][NT][4], float (&m)[NT][2], float (&l)[NT][2]) {
   typedef ListShape<D> S;
   const AttendArgs &a = x.a;
@@ -706,7 +707,7 @@ __device__ __forceinline__ bool list_keys(const AttendListArgs &x, const KvMaps 
       }
     }
     const u32 slot = __shfl_sync(~0u, held_slot, i % 32), block = __shfl_sync(~0u, held_block, i % 32);
-    const u32 st = i % S::STAGES, dst = ring + st * 2 * S::BLOCK;
+    const u32 st = (it + i) % S::STAGES, dst = ring + st * 2 * S::BLOCK;
     if (lane == 0) s_block[st] = block;
     if (ANY) {
       copy_block<D>(a, a.p.k, slot, h, dst);
@@ -760,11 +761,11 @@ __device__ __forceinline__ bool list_keys(const AttendListArgs &x, const KvMaps 
   }
   bool ok = true;
   for (u32 i = 0; i < n_mine; ++i) {
-    const u32 st = i % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
+    const u32 st = (it + i) % S::STAGES, kb = ring + st * 2 * S::BLOCK, vb = kb + S::BLOCK;
     if (ANY) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
       __syncwarp();
-    } else if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, i / S::STAGES & 1)))) break;
+    } else if (!(ok = __all_sync(~0u, bar_wait(bar0 + st * 8, (it + i) / S::STAGES & 1)))) break;
     const u32 block = s_block[st];
     float s[NT][4];
 #pragma unroll
@@ -862,6 +863,7 @@ __device__ __forceinline__ bool list_keys(const AttendListArgs &x, const KvMaps 
     if (i + S::STAGES < n_mine) load(i + S::STAGES);
     if (ANY) asm volatile("cp.async.commit_group;" ::: "memory");
   }
+  it += n_mine;
   return ok;
 }
 
@@ -903,8 +905,9 @@ k_attend_blocks(const __grid_constant__ AttendListArgs x, const __grid_constant_
     q[c] = (const u16 *)a.q + (u64)t * a.q_ts + (u64)(h * a.group + ct * REAL + r) * a.q_hs;
   }
   float o[D / 16][NT][4], m[NT][2], l[NT][2];
+  u32 it = 0;
   const bool ok = list_keys<T, D, NT, DOUBLE, ANY>(x, maps, a.b.table + w.seq * a.b.table_stride, list, n, w.index, h, q, rank * LIST_WARPS + warp,
-                                                   CLUSTER * LIST_WARPS, ring, bar0, s_block[warp], o, m, l);
+                                                   CLUSTER * LIST_WARPS, ring, bar0, s_block[warp], it, o, m, l);
   // each warp's sums into its ring, [column][channel]
   float *const so = (float *)(smem_raw + (ring - smem_addr(smem_raw)));
   static_assert(2 * COLS * S::LD * 4 <= S::RING, "the sums, and the CTA's part behind warp 0's, fit a ring");
@@ -1003,6 +1006,81 @@ k_attend_blocks(const __grid_constant__ AttendListArgs x, const __grid_constant_
   }
 }
 
+// Many units (chunks and prompts): a warp per unit, one after the other, without a word to the others; what a unit takes besides its blocks
+// is hidden by the seven other warps of the SM.
+template <class T, u32 D, u32 NT, bool DOUBLE>
+__global__ void __launch_bounds__(LIST_THREADS, 2)
+k_attend_lists(const __grid_constant__ AttendListArgs x, const __grid_constant__ KvMaps maps, u32 col_tiles, u32 n_units) {
+  typedef ListShape<D> S;
+  constexpr u32 COLS = NT * 8, REAL = DOUBLE ? 4 : COLS;
+  extern __shared__ u8 smem_raw[];
+  __shared__ __align__(8) u64 bars[LIST_WARPS * S::STAGES];
+  __shared__ u32 s_block[LIST_WARPS][S::STAGES];
+  const AttendArgs &a = x.a;
+  const u32 tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.p.n_kv_heads;
+  const u32 bar0 = smem_addr(bars) + warp * S::STAGES * 8, ring = ((smem_addr(smem_raw) + 1023) & ~1023u) + warp * S::RING;
+  if (lane == 0) {
+    for (u32 i = 0; i < S::STAGES; ++i) bar_init(bar0 + i * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.tail : &maps.pool) : "memory");
+  __syncwarp();
+  u32 it = 0;
+  for (u32 unit = blockIdx.x * LIST_WARPS + warp; unit < n_units; unit += gridDim.x * LIST_WARPS) {
+    const u32 ct = unit % col_tiles, th = unit / col_tiles, t = th / H, h = th - t * H;
+    const Where w = find_token<true>(a.b, t, a.err);
+    if (w.seq >= a.b.n_seqs) continue;   // behind the last sequence
+    const int32_t *const list = x.blocks + (u64)th * x.n_blocks;
+    u32 n = 0;                           // places up to the last that names a block with keys to see
+    if (w.ok) for (u32 i = 0; i < x.n_blocks; i += 32) {
+      const u32 have = __ballot_sync(~0u, i + lane < x.n_blocks && (u32)list[i + lane] <= w.index / BT);
+      if (have) n = i + 32 - __clz(have);
+    }
+    const u32 rows = min(a.group - ct * REAL, REAL);
+    const u16 *q[NT];
+#pragma unroll
+    for (u32 c = 0; c < NT; ++c) {
+      const u32 r = min((c * 8 + lane / 4) % REAL, rows - 1);
+      q[c] = (const u16 *)a.q + (u64)t * a.q_ts + (u64)(h * a.group + ct * REAL + r) * a.q_hs;
+    }
+    float o[D / 16][NT][4], m[NT][2], l[NT][2];
+    if (!list_keys<T, D, NT, DOUBLE, false>(x, maps, a.b.table + w.seq * a.b.table_stride, list, n, w.index, h, q, 0, 1, ring, bar0, s_block[warp], it, o, m, l)) {
+      if (lane == 0) kv_err(a.err, KVERR_WAIT);          // let the copies in flight land, for a while, before the warp ends
+      for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
+      return;
+    }
+    // results from the registers: pairs of channels of a query head, put together by turning each 8 x 8 part over
+#pragma unroll
+    for (u32 c = 0; c < NT; ++c) {
+      float inv[2];
+#pragma unroll
+      for (u32 y = 0; y < 2; ++y) {
+#pragma unroll
+        for (u32 z = 4; z < 32; z *= 2) l[c][y] += __shfl_xor_sync(~0u, l[c][y], z);
+        inv[y] = l[c][y] > 0.0f ? 1.0f / l[c][y] : l[c][y];
+        const u32 r = c * 8 + lane % 4 * 2 + y;
+        if (a.lse && lane < 4 && r < rows) a.lse[(u64)t * a.n_q_heads + h * a.group + ct * REAL + r] = (m[c][y] + log2f(l[c][y])) * 0.69314718055994531f;
+      }
+      const u32 r = c * 8 + lane / 4;
+      u16 *const dst = (u16 *)a.out + (u64)t * a.o_ts + (u64)(h * a.group + ct * REAL + min(r, rows - 1)) * a.o_hs + lane % 4 * 2;
+      const bool even = ((uintptr_t)dst & 3) == 0;
+#pragma unroll
+      for (u32 k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (u32 z = 0; z < 2; ++z) {
+          float v0 = o[k][c][2 * z], v1 = o[k][c][2 * z + 1];
+          if (DOUBLE) { v0 += __shfl_xor_sync(~0u, v0, 2); v1 += __shfl_xor_sync(~0u, v1, 2); }
+          const u32 e = transposed(Elem<T>::down(v0 * inv[0], v1 * inv[1]));
+          u16 *const p = dst + k * 16 + z * 8;
+          if (r >= rows) continue;
+          if (even) *(u32 *)p = e; else { p[0] = (u16)e; p[1] = (u16)(e >> 16); }
+        }
+    }
+    __syncwarp();
+  }
+}
+
 template <class T, u32 D, u32 NT, bool DOUBLE, u32 CLUSTER, bool ANY>
 static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, cudaStream_t s, u64 *allowed) {
   constexpr u32 size = CLUSTER == 8 ? 3 : CLUSTER == 4 ? 2 : CLUSTER == 2 ? 1 : 0, kind = DOUBLE ? 0 : NT;
@@ -1019,8 +1097,14 @@ static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 uni
   return cudaLaunchKernelEx(&c, kern, x, m, col_tiles);
 }
 template <class T, u32 D, u32 NT, bool DOUBLE>
-static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, u32 cluster, cudaStream_t s, u64 *allowed) {
+static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, u32 cluster, u32 list_ctas, cudaStream_t s, u64 *allowed) {
   switch (cluster) {
+    case 0: {                            // a warp per unit
+      const cudaError_t r = allow_smem(k_attend_lists<T, D, NT, DOUBLE>, 12 + ((D == 128) * 2 + __is_same(T, __half)) * 3 + (DOUBLE ? 0 : NT), ListShape<D>::SMEM, allowed + 1);
+      if (r != cudaSuccess) return r;
+      k_attend_lists<T, D, NT, DOUBLE><<<std::min((units + LIST_WARPS - 1) / LIST_WARPS, list_ctas), LIST_THREADS, ListShape<D>::SMEM, s>>>(x, m, col_tiles, units);
+      return cudaGetLastError();
+    }
     case 1: return launch_list<T, D, NT, DOUBLE, 1, false>(x, m, units, col_tiles, s, allowed);
     case 2: return launch_list<T, D, NT, DOUBLE, 2, false>(x, m, units, col_tiles, s, allowed);
     case 4: return launch_list<T, D, NT, DOUBLE, 4, false>(x, m, units, col_tiles, s, allowed);
@@ -1038,14 +1122,15 @@ static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 sms
   }
   const u32 cols = g <= 4 ? 4 : g <= 8 ? 8 : 16, tiles = (g + cols - 1) / cols;
   const u64 units = (u64)th * tiles;
-  u32 cluster = 1;
-  while (cluster < 8 && units * cluster * 2 <= 2ull * sms && x.n_blocks >= 16 * cluster) cluster *= 2;
-  if (d == 64) return cols == 4 ? launch_list<T, 64, 1, true>(x, m, units, tiles, cluster, s, allowed)
-                   : cols == 8 ? launch_list<T, 64, 1, false>(x, m, units, tiles, cluster, s, allowed)
-                               : launch_list<T, 64, 2, false>(x, m, units, tiles, cluster, s, allowed);
-  return cols == 4 ? launch_list<T, 128, 1, true>(x, m, units, tiles, cluster, s, allowed)
-       : cols == 8 ? launch_list<T, 128, 1, false>(x, m, units, tiles, cluster, s, allowed)
-                   : launch_list<T, 128, 2, false>(x, m, units, tiles, cluster, s, allowed);
+  // a warp per unit where there is one for each that runs at once, else CTAs or clusters of them per unit
+  u32 cluster = units >= 8ull * sms ? 0 : 1;
+  while (cluster && cluster < 8 && units * cluster * 2 <= 2ull * sms && x.n_blocks >= 16 * cluster) cluster *= 2;
+  if (d == 64) return cols == 4 ? launch_list<T, 64, 1, true>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
+                   : cols == 8 ? launch_list<T, 64, 1, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
+                               : launch_list<T, 64, 2, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed);
+  return cols == 4 ? launch_list<T, 128, 1, true>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
+       : cols == 8 ? launch_list<T, 128, 1, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
+                   : launch_list<T, 128, 2, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed);
 }
 cudaError_t launch_attend_blocks(const AttendListArgs &x, const KvMaps &m, int sm_count, cudaStream_t s, u64 *allowed, u32 *launches) {
   ++*launches;

@@ -373,6 +373,15 @@ def test_attend_blocks_groups(B, dtype, group, dim, n, new):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("group", [1, 4, 7, 8, 12, 18])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_blocks_of_many_tokens(B, dtype, group, dim):  # noqa: F811
+    """More units than warps run at once, empty lists among them, a sequence behind whose tokens there are rows of nobody."""
+    s = make(B, ([600, 33], [300, 20]), dtype, 0, 2, group, dim, layers=1, layer=0, pad=3, tail=group == 4, strided=group == 7, q_gain=2.0)
+    check_sparse(s, random_lists(s, 7, seed=group))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("group", [2, 8])
 def test_attend_blocks_scores_that_climb_and_fall(B, dtype, group):  # noqa: F811
     import torch

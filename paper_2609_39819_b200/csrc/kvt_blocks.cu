@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held)
   if (!m) return;
   u32 most = 0;
   constexpr u32 VN = VECTORS ? VECTORS : 1;
-  uint4 v[VN];
+  uint4 v[VN] = {};
   auto mine = [&](u32 y, u32 z) { return z == 0 ? v[y].x : z == 1 ? v[y].y : z == 2 ? v[y].z : v[y].w; };
   if constexpr (VECTORS > 0) {
 #pragma unroll
@@ -569,9 +569,7 @@ __global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held)
         u32 at = a.first + incl - __popc(word);
         for (u32 y = 0; y < tid / 32; ++y) at += s_count[y];
         for (; word; word &= word - 1) out[at++] = (int32_t)(tid * 32 + __ffs(word) - 1);
-        return;
-      }
-      for (u32 i = tid; i < c; i += THREADS) {
+      } else for (u32 i = tid; i < c; i += THREADS) {
         if (!taken[i]) continue;
         const u32 x = (u32)s_key[i];     // the larger, the lower the number
         u32 before = 0;
@@ -675,8 +673,8 @@ cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, u64
 // The queries are the narrow side of the products, 8 columns: S^T = K Q^T has the block's 16 keys as rows, O^T = V^T P^T 16 channels.
 // ======================================================================================================
 constexpr u32 LIST_WARPS = 4, LIST_THREADS = LIST_WARPS * 32;
-template <u32 D> struct ListShape {
-  static constexpr u32 BLOCK = BT * D * 2, STAGES = D == 64 ? 6 : 3, RING = STAGES * 2 * BLOCK, SMEM = LIST_WARPS * RING + 1024, LD = D + 4;
+template <u32 D, u32 PARTS = 3 /* of 8 KB of a warp's ring */> struct ListShape {
+  static constexpr u32 BLOCK = BT * D * 2, STAGES = D == 64 ? 2 * PARTS : PARTS, RING = STAGES * 2 * BLOCK, SMEM = LIST_WARPS * RING + 1024, LD = D + 4;
 };
 __device__ __forceinline__ u32 transposed(u32 x) {       // an 8 x 8 matrix of 16-bit numbers, two per lane
   u32 y;
@@ -688,11 +686,10 @@ __device__ __forceinline__ u32 transposed(u32 x) {       // an 8 x 8 matrix of 1
 // so far. A lane has
 // columns n * 8 + 2 (lane % 4) and the next, keys / channels lane / 4 and 8 further. DOUBLE: columns 4 to 7 are those 0 to 3 once
 // more and take the second numbers of the powers.
-template <class T, u32 D, u32 NT, bool DOUBLE, bool ANY>
+template <class T, u32 D, u32 NT, bool DOUBLE, bool ANY, class S = ListShape<D>>
 __device__ __forceinline__ bool list_keys(const AttendListArgs &x, const KvMaps &maps, const u32 *table, const int32_t *list, u32 n, u32 index, u32 h,
                                           const u16 *const (&q)[NT], u32 part, u32 parts, u32 ring, u32 bar0, u32 *s_block, u32 &it,
                                           float (&o)[D / 16][NT][4], float (&m)[NT][2], float (&l)[NT][2]) {
-  typedef ListShape<D> S;
   const AttendArgs &a = x.a;
   const u32 lane = threadIdx.x & 31, own = index / BT;
   const u32 n_mine = part < n ? (n - part + parts - 1) / parts : 0;
@@ -1007,11 +1004,16 @@ k_attend_blocks(const __grid_constant__ AttendListArgs x, const __grid_constant_
 }
 
 // Many units (chunks and prompts): a warp per unit, one after the other, without a word to the others; what a unit takes besides its blocks
-// is hidden by the seven other warps of the SM.
+// is hidden by the other warps of the SM.
+// Bound by the chain of a block's own steps, so more warps do more than a longer ring: with 4 CTAs per SM and one stage (heads of 128; 64:
+// two) 792 tokens, 8 KV heads, groups of 4, lists of 64 take 203 us (64: 150), with 3 CTAs and two stages 218 (178), with 2 and three 277
+// (240). Two tiles of columns have more registers: groups of 12 with 3 CTAs 323 us, with 2 378, with 4 351.
+template <u32 NT> constexpr u32 MANY_PARTS = NT == 1 ? 1 : 2;
+template <u32 D, u32 NT> constexpr u32 MANY_CTAS = NT == 1 ? 4 : 3;
 template <class T, u32 D, u32 NT, bool DOUBLE>
-__global__ void __launch_bounds__(LIST_THREADS, 2)
+__global__ void __launch_bounds__(LIST_THREADS, MANY_CTAS<D, NT>)
 k_attend_lists(const __grid_constant__ AttendListArgs x, const __grid_constant__ KvMaps maps, u32 col_tiles, u32 n_units) {
-  typedef ListShape<D> S;
+  typedef ListShape<D, MANY_PARTS<NT>> S;
   constexpr u32 COLS = NT * 8, REAL = DOUBLE ? 4 : COLS;
   extern __shared__ u8 smem_raw[];
   __shared__ __align__(8) u64 bars[LIST_WARPS * S::STAGES];
@@ -1045,7 +1047,7 @@ k_attend_lists(const __grid_constant__ AttendListArgs x, const __grid_constant__
       q[c] = (const u16 *)a.q + (u64)t * a.q_ts + (u64)(h * a.group + ct * REAL + r) * a.q_hs;
     }
     float o[D / 16][NT][4], m[NT][2], l[NT][2];
-    if (!list_keys<T, D, NT, DOUBLE, false>(x, maps, a.b.table + w.seq * a.b.table_stride, list, n, w.index, h, q, 0, 1, ring, bar0, s_block[warp], it, o, m, l)) {
+    if (!list_keys<T, D, NT, DOUBLE, false, S>(x, maps, a.b.table + w.seq * a.b.table_stride, list, n, w.index, h, q, 0, 1, ring, bar0, s_block[warp], it, o, m, l)) {
       if (lane == 0) kv_err(a.err, KVERR_WAIT);          // let the copies in flight land, for a while, before the warp ends
       for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
       return;
@@ -1097,12 +1099,13 @@ static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 uni
   return cudaLaunchKernelEx(&c, kern, x, m, col_tiles);
 }
 template <class T, u32 D, u32 NT, bool DOUBLE>
-static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, u32 cluster, u32 list_ctas, cudaStream_t s, u64 *allowed) {
+static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, u32 cluster, u32 sms, cudaStream_t s, u64 *allowed) {
   switch (cluster) {
     case 0: {                            // a warp per unit
-      const cudaError_t r = allow_smem(k_attend_lists<T, D, NT, DOUBLE>, 12 + ((D == 128) * 2 + __is_same(T, __half)) * 3 + (DOUBLE ? 0 : NT), ListShape<D>::SMEM, allowed + 1);
+      constexpr u32 SMEM = ListShape<D, MANY_PARTS<NT>>::SMEM;
+      const cudaError_t r = allow_smem(k_attend_lists<T, D, NT, DOUBLE>, 12 + ((D == 128) * 2 + __is_same(T, __half)) * 3 + (DOUBLE ? 0 : NT), SMEM, allowed + 1);
       if (r != cudaSuccess) return r;
-      k_attend_lists<T, D, NT, DOUBLE><<<std::min((units + LIST_WARPS - 1) / LIST_WARPS, list_ctas), LIST_THREADS, ListShape<D>::SMEM, s>>>(x, m, col_tiles, units);
+      k_attend_lists<T, D, NT, DOUBLE><<<std::min((units + LIST_WARPS - 1) / LIST_WARPS, MANY_CTAS<D, NT> * sms), LIST_THREADS, SMEM, s>>>(x, m, col_tiles, units);
       return cudaGetLastError();
     }
     case 1: return launch_list<T, D, NT, DOUBLE, 1, false>(x, m, units, col_tiles, s, allowed);
@@ -1125,12 +1128,12 @@ static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 sms
   // a warp per unit where there is one for each that runs at once, else CTAs or clusters of them per unit
   u32 cluster = units >= 8ull * sms ? 0 : 1;
   while (cluster && cluster < 8 && units * cluster * 2 <= 2ull * sms && x.n_blocks >= 16 * cluster) cluster *= 2;
-  if (d == 64) return cols == 4 ? launch_list<T, 64, 1, true>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
-                   : cols == 8 ? launch_list<T, 64, 1, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
-                               : launch_list<T, 64, 2, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed);
-  return cols == 4 ? launch_list<T, 128, 1, true>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
-       : cols == 8 ? launch_list<T, 128, 1, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed)
-                   : launch_list<T, 128, 2, false>(x, m, units, tiles, cluster, 2 * sms, s, allowed);
+  if (d == 64) return cols == 4 ? launch_list<T, 64, 1, true>(x, m, units, tiles, cluster, sms, s, allowed)
+                   : cols == 8 ? launch_list<T, 64, 1, false>(x, m, units, tiles, cluster, sms, s, allowed)
+                               : launch_list<T, 64, 2, false>(x, m, units, tiles, cluster, sms, s, allowed);
+  return cols == 4 ? launch_list<T, 128, 1, true>(x, m, units, tiles, cluster, sms, s, allowed)
+       : cols == 8 ? launch_list<T, 128, 1, false>(x, m, units, tiles, cluster, sms, s, allowed)
+                   : launch_list<T, 128, 2, false>(x, m, units, tiles, cluster, sms, s, allowed);
 }
 cudaError_t launch_attend_blocks(const AttendListArgs &x, const KvMaps &m, int sm_count, cudaStream_t s, u64 *allowed, u32 *launches) {
   ++*launches;

@@ -2349,6 +2349,7 @@ const char *attend_like_fault(const kvt_engine *e, const kvt_batch &b, u32 layer
 const char *select_fault(const kvt_engine *e, const kvt_select_args &a) {
   if (const char *m = attend_like_fault(e, a.b, a.layer, a.dtype, a.n_q_heads, 0, 0, 0.0f)) return m;
   if (const char *m = bounds_fault(e, a.bounds)) return m;
+  if (e->cfg.n_kv_heads > 65535) return "select: too many KV heads";
   return keep_fault(a.n_blocks, a.first, a.last);
 }
 SelectArgs select_args(kvt_engine *e, const kvt_select_args &a) {

@@ -242,6 +242,33 @@ def test_select(B, batch, dtype, layout, heads, group, dim, n_blocks, first, las
     check_select(s, random_bounds(s, torch.Generator("cuda").manual_seed(dim)), n_blocks, first, last)
 
 
+@pytest.mark.parametrize("n_blocks,first,last", [(60, 21, 17), (40, 9, 31), (90, 0, 1), (64, 63, 1)])
+def test_select_many_first_and_last(B, n_blocks, first, last):  # noqa: F811
+    import torch
+    s = make(B, ([5, 1], [1500, 7000]), "bf16", 0, 2, 2, 64)
+    check_select(s, random_bounds(s, torch.Generator("cuda").manual_seed(8)), n_blocks, first, last)
+
+
+def test_select_in_parts(B):  # noqa: F811
+    """More scores than are in hand together, since the table could hold many more blocks: parts that end inside a sequence."""
+    import torch
+    s = make(B, ([700, 600], [900, 3000]), "fp16", 0, 2, 2, 16, pad=3)
+    k = random_bounds(s, torch.Generator("cuda").manual_seed(8))
+    wide = torch.full((2, 20000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :s.table.shape[1]] = s.table
+    want = s.eng.select_blocks(1, s.q, k, s.table, s.q_start, s.kv_len, 30)
+    got = s.eng.select_blocks(1, s.q, k, wide, s.q_start, s.kv_len, 30)
+    s.eng.kv_check()
+    assert torch.equal(want[:s.t], got[:s.t])
+    t0 = 0
+    for i, n in enumerate(s.new):
+        slots = s.host_table[i, :-(-s.kv[i] // BT)].long().cuda()
+        some = list(range(0, n, 37))
+        ref = lists_of(torch, s.q[[t0 + x for x in some]], k.codes[1, slots], k.exps[1, slots], [s.kv[i] - n + x for x in some], 2, 30, 1, 2)
+        assert np.array_equal(got[[t0 + x for x in some]].cpu().numpy(), ref)
+        t0 += n
+
+
 @pytest.mark.parametrize("span", [1, 3])
 @pytest.mark.parametrize("codes", [1, 2, 127])
 def test_select_ties_go_to_the_lower_number(B, codes, span):  # noqa: F811
@@ -735,6 +762,32 @@ def test_nothing_to_do(B):  # noqa: F811
     held = torch.arange(s.table.shape[1], device="cuda") * BT < s.kv_len[:, None]
     assert torch.equal(got, torch.where(held, w * 0.5, 0.0))
     assert s.eng.evict_blocks(w[:0], *none[::2], 5)[0].shape == none[0].shape
+    s.eng.kv_check()
+
+
+def test_native_and_python_marshalling_make_the_same_call(B, monkeypatch):  # noqa: F811
+    import torch
+    s = make(B, ([40, 1], [900, 2000]), "bf16", 0, 2, 4, 64, tail=True, strided=True)
+    batch = (s.table, s.q_start, s.kv_len)
+    lse = torch.full((s.t, 8), 6.0, device="cuda")
+    old = torch.rand(s.table.shape, device="cuda")
+
+    def run():
+        k = s.eng.key_bounds(s.dt)
+        s.eng.bound_keys(s.layer, k, *batch, n_tokens=s.t)
+        k.codes.random_(-127, 128, generator=torch.Generator("cuda").manual_seed(1))
+        k.exps.fill_(120)
+        blocks = s.eng.select_blocks(s.layer, s.q, k, *batch, 12, first=2, last=3, max_q_len=40)
+        return (k.codes, blocks, s.eng.attend_blocks(s.layer, s.q, blocks, *batch, scale=0.25, lse=torch.empty_like(lse)),
+                s.eng.weigh_blocks(s.layer, s.q, lse, *batch, max_q_len=40, window=500, scale=0.25, weights=old, keep=0.5),
+                *s.eng.evict_blocks(old, s.table, s.kv_len, 20, first=3, last=4))
+
+    want = run()
+    for name in ("bound", "select", "attend_blocks", "weigh", "evict"):
+        assert s.eng.__dict__[f"_{name}_native"] is not None
+        monkeypatch.setattr(s.eng, f"_{name}_native", lambda *args: NotImplemented)
+    for x, y in zip(want, run()):
+        assert torch.equal(x, y)
     s.eng.kv_check()
 
 

@@ -112,7 +112,7 @@ struct EvictArgs {
   uint32_t *err;
 };
 
-// allowed: two words of such bits
+// allowed: three words of such bits
 cudaError_t launch_bound(const BoundArgs &a, int sm_count, cudaStream_t s, uint32_t *launches);
 cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, uint64_t *allowed, uint32_t *launches);
 cudaError_t launch_attend_blocks(const AttendListArgs &a, const KvMaps &m, int sm_count, cudaStream_t s, uint64_t *allowed, uint32_t *launches);

@@ -597,6 +597,68 @@ __global__ void __launch_bounds__(THREADS) k_pick_blocks(SelectArgs a, u32 held)
                 [&](u32 i, u32, u32 at) { out[a.first + at] = (int32_t)(a.first + i); });
 }
 
+// Short rows: a warp per token and KV head, KEYS scores in a row per lane; the m-th largest is found by halving the range it lies in.
+template <u32 KEYS>
+__global__ void __launch_bounds__(128) k_pick_short(SelectArgs a, u32 rows) {
+  const u32 lane = threadIdx.x & 31, row = blockIdx.x * 4 + threadIdx.x / 32, H = a.n_kv_heads, t = a.slab_begin + row / H;
+  const bool any = row < rows;
+  Where w{~0u, 0, false};
+  if (any) w = find_token<true>(a.b, t, a.err);
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the scores; the batch's arrays are older than the kernel before this one
+  if (!any || w.seq >= a.b.n_seqs) return;               // behind the last sequence
+  int32_t *const out = a.out + ((u64)a.slab_begin * H + row) * a.n_blocks;
+  const u32 own = w.index / BT;
+  if (!w.ok || own < a.n_blocks) {                       // all there are
+    for (u32 i = lane; i < a.n_blocks; i += 32) out[i] = w.ok && i <= own ? (int32_t)i : -1;
+    return;
+  }
+  const u32 end = own + 1 - a.last, m = a.n_blocks - a.first - a.last;
+  for (u32 i = lane; i < a.first + a.last; i += 32) out[i < a.first ? i : i + m] = i < a.first ? (int32_t)i : (int32_t)(end + i - a.first);
+  if (!m) return;
+  const u32 *const scores = a.scores + (u64)row * a.scores_stride;
+  u32 x[KEYS], valid = 0, lo = ~0u, hi = 0;
+#pragma unroll
+  for (u32 y = 0; y < KEYS; y += 4) {
+    const u32 i = lane * KEYS + y;
+    const uint4 v = i < end ? *(const uint4 *)(scores + i) : make_uint4(0, 0, 0, 0);
+    x[y] = v.x; x[y + 1] = v.y; x[y + 2] = v.z; x[y + 3] = v.w;
+  }
+#pragma unroll
+  for (u32 y = 0; y < KEYS; ++y) {
+    const u32 i = lane * KEYS + y;
+    if (i >= a.first && i < end) { valid |= 1u << y; lo = min(lo, x[y]); hi = max(hi, x[y]); }
+  }
+  lo = __reduce_min_sync(~0u, lo); hi = __reduce_max_sync(~0u, hi);
+  auto at_least = [&](u32 least) {                       // a bit for each
+    u32 mask = 0;
+#pragma unroll
+    for (u32 y = 0; y < KEYS; ++y) mask |= x[y] >= least ? 1u << y : 0u;
+    return mask & valid;
+  };
+  // lo: a score that m or more reach; hi: the largest that may be it
+  u32 mask = valid, c = end - a.first;
+  while (lo < hi && c != m) {
+    const u32 mid = lo + (hi - lo) / 2 + 1, some = at_least(mid), n = __reduce_add_sync(~0u, __popc(some));
+    if (n >= m) { lo = mid; mask = some; c = n; } else hi = mid - 1;
+  }
+  auto before = [&](u32 n) {                             // sum over the lanes in front
+    u32 incl = n;
+#pragma unroll
+    for (u32 o = 1; o < 32; o *= 2) { const u32 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
+    return incl - n;
+  };
+  if (c != m) {                          // more scores are lo than are taken: the first of them
+    u32 ties = 0;
+#pragma unroll
+    for (u32 y = 0; y < KEYS; ++y) ties |= x[y] == lo ? 1u << y : 0u;
+    ties &= valid;
+    mask &= ~ties;
+    const u32 take = m - __reduce_add_sync(~0u, __popc(mask));
+    for (u32 at = before(__popc(ties)); ties && at < take; ++at, ties &= ties - 1) mask |= ties & (0u - ties);
+  }
+  for (u32 at = a.first + before(__popc(mask)); mask; mask &= mask - 1) out[at++] = (int32_t)(lane * KEYS + __ffs(mask) - 1);
+}
+
 // Scores that are in hand together. (500 tokens on 130,500, 8 KV heads: 134 MB at once 127 us, in two parts of 64 MB 140, of 32 MB 167.)
 constexpr u64 SLAB_BYTES = 160ull << 20;
 SelectPlan plan_select(const SelectArgs &a, int sm_count) {
@@ -625,17 +687,23 @@ static cudaError_t score_blocks(const SelectArgs &a, dim3 grid, u32 shares, bool
   if (a.k.width <= 128) return score_blocks<T, 4, 1>(a, grid, shares, F + 3, s, allowed);
   return score_blocks<T, 8, 1>(a, grid, shares, F + 4, s, allowed);
 }
-template <u32 THREADS, u32 VECTORS>
-static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, u32 held, bool scored, cudaStream_t s) {
+template <class Kernel>
+static cudaError_t launch_pick(Kernel kern, const SelectArgs &a, u32 ctas, u32 threads, u32 smem, u32 arg, bool scored, cudaStream_t s) {
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3(rows); c.blockDim = dim3(THREADS); c.dynamicSmemBytes = held * 4; c.stream = s;
+  c.gridDim = dim3(ctas); c.blockDim = dim3(threads); c.dynamicSmemBytes = smem; c.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   c.attrs = &at; c.numAttrs = scored;    // behind a kernel of this call only: the batch's arrays may be of the kernel before that
-  return cudaLaunchKernelEx(&c, k_pick_blocks<THREADS, VECTORS>, a, held);
+  return cudaLaunchKernelEx(&c, kern, a, arg);
+}
+template <u32 THREADS, u32 VECTORS>
+static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, u32 held, bool scored, cudaStream_t s) {
+  return launch_pick(k_pick_blocks<THREADS, VECTORS>, a, rows, THREADS, held * 4, held, scored, s);
 }
 static cudaError_t pick_blocks(const SelectArgs &a, u32 rows, bool scored, cudaStream_t s, u64 *allowed) {
+  if (a.b.max_blocks <= 512) return launch_pick(k_pick_short<16>, a, (rows + 3) / 4, 128, 0, rows, scored, s);
+  if (a.b.max_blocks <= 1024) return launch_pick(k_pick_short<32>, a, (rows + 3) / 4, 128, 0, rows, scored, s);
   if (a.b.max_blocks <= 2048) return pick_blocks<256, 2>(a, rows, 0, scored, s);
   if (a.b.max_blocks <= 4096) return pick_blocks<256, 4>(a, rows, 0, scored, s);
   if (a.b.max_blocks <= 8192) return pick_blocks<256, 8>(a, rows, 0, scored, s);
@@ -1087,9 +1155,9 @@ k_attend_lists(const __grid_constant__ AttendListArgs x, const __grid_constant__
 template <class T, u32 D, u32 NT, bool DOUBLE, u32 CLUSTER, bool ANY>
 static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 units, u32 col_tiles, cudaStream_t s, u64 *allowed) {
   constexpr u32 size = CLUSTER == 8 ? 3 : CLUSTER == 4 ? 2 : CLUSTER == 2 ? 1 : 0, kind = DOUBLE ? 0 : NT;
-  constexpr u32 which = 8 + (ANY ? (D == 256 ? 2 : D == 128) : 4 + (D == 128 ? 12 : 0) + size * 3 + kind);      // 8 .. 35, and 28 more in fp16
+  constexpr u32 which = 7 + (ANY ? (D == 256 ? 2 : D == 128) + (CLUSTER > 1 ? 3 : 0) : 6 + (D == 128 ? 12 : 0) + size * 3 + kind);      // 7 .. 36
   auto const kern = k_attend_blocks<T, D, NT, DOUBLE, CLUSTER, ANY>;
-  cudaError_t r = allow_smem(kern, which + (__is_same(T, __half) ? 28 : 0), ListShape<D>::SMEM, allowed);
+  cudaError_t r = allow_smem(kern, which, ListShape<D>::SMEM, allowed + (__is_same(T, __half) ? 2 : 0));
   if (r != cudaSuccess) return r;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3(units * CLUSTER); c.blockDim = dim3(LIST_THREADS); c.dynamicSmemBytes = ListShape<D>::SMEM; c.stream = s;
@@ -1120,9 +1188,11 @@ static cudaError_t launch_list(const AttendListArgs &x, const KvMaps &m, u32 sms
   const u32 g = x.a.group, d = x.a.p.head_dim, th = x.a.b.n_tokens * x.a.p.n_kv_heads;
   if (d != 64 && d != 128) {             // heads of every other size: 16 columns
     const u32 tiles = (g + 15) / 16;
-    if (d < 64) return launch_list<T, 64, 2, false, 1, true>(x, m, th * tiles, tiles, s, allowed);
-    if (d < 128) return launch_list<T, 128, 2, false, 1, true>(x, m, th * tiles, tiles, s, allowed);
-    return launch_list<T, 256, 2, false, 1, true>(x, m, th * tiles, tiles, s, allowed);
+    const u64 units = (u64)th * tiles;
+    const bool few = units * 8 <= (d > 128 ? 1ull : 2ull) * sms && x.n_blocks >= 32;
+    if (d < 64) return few ? launch_list<T, 64, 2, false, 8, true>(x, m, units, tiles, s, allowed) : launch_list<T, 64, 2, false, 1, true>(x, m, units, tiles, s, allowed);
+    if (d < 128) return few ? launch_list<T, 128, 2, false, 8, true>(x, m, units, tiles, s, allowed) : launch_list<T, 128, 2, false, 1, true>(x, m, units, tiles, s, allowed);
+    return few ? launch_list<T, 256, 2, false, 8, true>(x, m, units, tiles, s, allowed) : launch_list<T, 256, 2, false, 1, true>(x, m, units, tiles, s, allowed);
   }
   const u32 cols = g <= 4 ? 4 : g <= 8 ? 8 : 16, tiles = (g + cols - 1) / cols;
   const u64 units = (u64)th * tiles;
@@ -1927,7 +1997,7 @@ WeighPlan plan_weigh(const WeighArgs &x, u32 max_q_len, int sm_count) {
   } else {                               // one warp per block and 32 blocks per CTA where there are enough of them, else the heads of a block over several warps
     p.share = 1;
     while (p.share < 8 && p.share * 2 <= x.a.p.n_kv_heads && blocks * p.share < 32ull * sm_count) p.share *= 2;
-    p.tile = p.share > 1 || blocks < 128ull * sm_count ? 8 : WEIGH_TILE;
+    p.tile = p.share == 1 && blocks >= 128ull * sm_count ? WEIGH_TILE : (u32)std::max<u64>(1, std::min<u64>(8, blocks / (2ull * sm_count)));
   }
   if (p.many) {
     const u64 pairs = weigh_pairs(x.a.b.n_seqs, x.a.b.max_blocks);

@@ -391,7 +391,7 @@ def test_attend_blocks(B, batch, dtype, layout, heads, group, dim, n):  # noqa: 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("group", [1, 4, 5, 8, 9, 16, 20])
-@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dim", [64, 128, 40, 96, 200])
 @pytest.mark.parametrize("n,new", [(200, [1]), (64, [1, 1, 2]), (17, [40, 7]), (130, [3, 60])])
 def test_attend_blocks_groups(B, dtype, group, dim, n, new):  # noqa: F811
     """Clusters of every size, CTAs and warps per unit."""

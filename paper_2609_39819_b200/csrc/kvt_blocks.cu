@@ -18,7 +18,8 @@ __device__ __forceinline__ float sum_over_warp(float x) {
 // as whole steps of 2^e, rounded up: ceil(x 2^-e), where e is the least with max |k| <= 127 * 2^e. For any query q then
 //   q.k_r <= sum_d max(q_d, 0) up_d + max(-q_d, 0) down_d          for every key of the block.
 // Steps are powers of two so that nothing but the rounding up is rounded, and equal keys get equal codes whoever makes them.
-// Bound by reading the keys once.
+// Bound by reading the keys once: 130,500 tokens, 8 heads of 128 (284 MB) 48 us in a captured graph, 90 % of the measured copy bandwidth; a
+// step of 32 sessions 3.5 us, launch and three dependent loads.
 // ======================================================================================================
 constexpr int BOUND_E_MIN = -126, BOUND_E_MAX = 103;     // 2^24 steps of 2^103 are a 32-bit number
 __device__ __forceinline__ int bound_exponent(float most) {
@@ -251,6 +252,9 @@ __device__ __forceinline__ u32 ordered(float x) {
 // the sum over the group's heads of what bounds their products with any key of the block (in steps of 2^f, which all blocks of the
 // query share). The sum is of at most 512 products of 255 * 127, a whole number below 2^24, so it is a 32-bit floating number
 // exactly, and so is the score: all kernels, batches and orders of summation give the same selection, bit by bit.
+// Two kernels: scores into scratch, then each list from its scores. 8 KV heads of 128, groups of 4, lists of 64, in a captured graph: one
+// token on 258,047 17.3 us (floor 5.1: 33 MB of codes; the kernels take 8 and 7 us, each of them a chain of dependent loads), 500 tokens
+// on 130,500 123 us (71 and 48: scores and their stores, 134 MB of them), a prompt of 8192 166 us.
 // ======================================================================================================
 // New tokens [t0, t0 + n) of a sequence that lie among the tokens in hand; index of the first in its sequence.
 struct Part { u32 t0, n; long long index; };
@@ -739,7 +743,10 @@ cudaError_t launch_select(SelectArgs a, const SelectPlan &p, cudaStream_t s, u64
 // Attention over listed blocks: softmax(scale q k^T) v of one token's group of query heads over the keys up to its own in the blocks
 // its list names. A unit is a token and KV head (and 8 or 16 query heads); its blocks are dealt out to the four warps of a CTA, or
 // of a cluster of them, each with a ring of loads of its own, and joined like the parts of a longer sequence.
-// The queries are the narrow side of the products, 8 columns: S^T = K Q^T has the block's 16 keys as rows, O^T = V^T P^T 16 channels.
+// The queries are the narrow side of the products, 8 columns: S^T = K Q^T has the block's 16 keys as rows, O^T = V^T P^T 16 channels. That
+// takes half the matrix instructions that 16 rows of queries would, where groups are of 8 heads and less, and a quarter for 4 and less.
+// Measured in a captured graph, 8 KV heads of 128, bf16: one token, lists of 64, groups of 4 6.6 us (launch, three dependent loads before the
+// first block, join through the cluster); 32 tokens, lists of 256, groups of 12 (538 MB) 90 us, 92 % of the measured copy bandwidth.
 // ======================================================================================================
 constexpr u32 LIST_WARPS = 4, LIST_THREADS = LIST_WARPS * 32;
 template <u32 D, u32 PARTS = 3 /* of 8 KB of a warp's ring */> struct ListShape {
@@ -1245,7 +1252,9 @@ __device__ __forceinline__ uint4 load8(const u16 *p, int n_left, bool vec) {
 // Few rows (a new token per sequence), heads of 64 and 128: bound by reading K once. A CTA of four warps takes a tile of up to 32 blocks of one
 // sequence, each warp every fourth head of it, with a ring of TMA loads of its own (a block's keys of one head per stage). The block's 16
 // keys are the rows of the matrix instruction, eight (token, head) rows the columns, which stay in registers for all blocks of a head.
-// Lane i holds the sum of block i. Two CTAs per SM keep 192 KB of loads in flight.
+// Lane i holds the sum of block i. Two CTAs per SM keep 192 KB of loads in flight. Measured in a captured graph, 8 KV heads of 128: 32 tokens on
+// 2,000 to 130,000 each, groups of 12 (3.0 GB) 469 us, 99 % of the measured copy bandwidth; one token on 258,047 90 us (89 %), on 1000 4.6 us.
+// (K straight into registers, the next block's while one is worked on, took 1370 us where this takes 469.)
 constexpr u32 WEIGH_TILE = 32, WS_WARPS = 4, WS_THREADS = WS_WARPS * 32;
 template <u32 D> struct WeighRing { static constexpr u32 BLOCK = BT * D * 2, STAGES = D == 64 ? 12 : 6, RING = STAGES * BLOCK, SMEM = WS_WARPS * RING + 1024; };
 template <class T, u32 D, u32 NT>
@@ -1363,7 +1372,8 @@ __global__ void __launch_bounds__(WS_THREADS, 2) k_weigh_split(const __grid_cons
 
 // Heads of every other size, any number of rows. `share` warps work on a block, each on every so many-th head; a lane's 16 bytes of a key and
 // of a query are operands of the matrix instruction if channels are counted in that order on both sides, so both go from memory to
-// registers. The next (block, head)'s keys are on their way while one is worked on.
+// registers. The next (block, head)'s keys are on their way while one is worked on. Heads of 96: one token on 100,000 61 us (floor 24), 1000
+// tokens 618 us (floor 2: rows go by eight, and a block's rows are not divided).
 constexpr u32 WEIGH_LSE = 512;
 template <class T, u32 G>      // G: 64-byte parts of a head
 __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n_tile, u32 share) {
@@ -1486,6 +1496,11 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
 // constants on the side of K and the parts of -lse / scale in the element type on the side of Q, S^T is (s - lse / scale) in 32 bits,
 // and a power is one multiplication and ex2. (With lse from shared memory and a fused multiply-add it was bound by shared memory, which
 // the products alone keep busy half of the time: 8192 tokens, 8 x 4 heads of 128, 352 us.)
+// Bound by the exponentials: 256 keys by 128 rows take 2600 cycles, of which the special-function units need 2048 for all of them (every
+// eighth pair is made on the FMA pipes: 341 -> 331 us; every fourth 331, three of eight 343) and the tensor cores 1160. In a captured graph:
+// 8192 tokens, 8 KV heads of 128, groups of 4 334 us (275 TFLOP: 823 TFLOP/s, half of the measured matrix rate), 500 tokens on 130,500 599 us,
+// the last 32 of 32,000 26 us. One thread per key instead of two 410 us, K in stages of 256 keys and two stages of queries 339, lse in parts
+// by 64-bit arithmetic 339, 32 columns of S at a time 375.
 //   warps 0-15   two threads per key, each for half of the rows: powers and their sum
 //   warp 16      issues the products, S^T in tensor memory, held twice: 2 x 2 x 128 columns
 //   warp 17      works out what this CTA does
@@ -2062,8 +2077,9 @@ cudaError_t launch_weigh(const WeighArgs &x, const WeighPlan &p, const KvMaps &m
 }
 
 // ======================================================================================================
-// Eviction by weight: of a sequence's blocks the first, the last and the heaviest stay. A CTA per sequence. Bound by latency: three rounds
-// of loads and some thirty barriers.
+// Eviction by weight: of a sequence's blocks the first, the last and the heaviest stay. A CTA per sequence. Bound by latency, three rounds of
+// loads and some thirty barriers, and for long rows by the instructions of one SM: 1001 blocks 7.6 us, 32 sequences of up to 15,600 19 us, one of
+// 62,501 115 us, in a captured graph.
 // ======================================================================================================
 constexpr u32 EVICT_THREADS = 1024;
 __device__ __forceinline__ u32 weight_order(float w) { return ordered(w == w ? w + 0.0f : INFINITY); }       // a NaN weighs most

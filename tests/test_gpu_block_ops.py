@@ -326,6 +326,33 @@ def test_select_long(B, new, blocks, heads, n_blocks):  # noqa: F811
         t0 += m
 
 
+@pytest.mark.parametrize("codes,span", [(1, 1), (3, 2), (127, 1), (127, 4)])
+@pytest.mark.parametrize("width,blocks", [(512, 500), (513, 513), (1024, 1000), (1025, 1025), (2048, 1500), (4096, 4000), (8192, 3000), (8192, 8192),
+                                          (16384, 16000), (32768, 5000), (32768, 32768), (32769, 6000), (50000, 49999)])
+def test_select_by_every_kernel(B, width, blocks, codes, span):  # noqa: F811
+    """Scores that are the same many times over, and scores that hardly are, in rows of every length; short and long lists."""
+    import torch
+    eng = B.Engine(n_layers=1, n_kv_heads=2, head_dim=16, n_hbm_blocks=blocks, n_host_blocks=0, max_contexts=1, max_messages=16, max_tokens=64)
+    g = torch.Generator("cuda").manual_seed(width + codes)
+    k = eng.key_bounds(torch.bfloat16)
+    k.codes.random_(-codes, codes + 1, generator=g)
+    k.exps.random_(120, 120 + span, generator=g)
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, :blocks] = torch.randperm(blocks, generator=g, device="cuda")
+    q = torch.empty(3, 2, 16, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    if codes < 127:
+        q.sign_()
+        q[:, :, 4:] = 0
+    q[2] = 0
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")      # noqa: E731
+    for n_blocks, first, last in ((9, 1, 2), (64, 0, 1), (64, 5, 9), (300, 1, 2), (min(blocks - 1, 2000), 2, 2)):
+        got = eng.select_blocks(0, q, k, table, ints(0, 3), ints(blocks * BT - 7), n_blocks, first=first, last=last).cpu().numpy()
+        eng.kv_check()
+        slots = table[0, :blocks].long()
+        want = lists_of(torch, q, k.codes[0, slots], k.exps[0, slots], [blocks * BT - 10 + t for t in range(3)], 1, n_blocks, first, last)
+        assert np.array_equal(got, want)
+
+
 def test_selection_does_not_depend_on_the_batch(B):  # noqa: F811
     import torch
     s = make(B, ([30, 1, 17], [5000, 9000, 2000]), "bf16", 0, 2, 4, 128)

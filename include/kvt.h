@@ -568,9 +568,11 @@ typedef struct kvt_weigh_args {
 } kvt_weigh_args;
 /* Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
  * keys of block b that the token sees of exp(scale q.k - lse); 0 for blocks behind kv_len[s]. Sums of all layers come from
- * calls with the same weights, one per layer. Sums are in 32 bits, in an order that is fixed by the sizes and lengths. A row
- * with lse = -inf adds nothing. Keys a row does not see have no effect. A slot id beyond both pools sets the error word and its
- * keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
+ * calls with the same weights, one per layer. Sums are in 32 bits, in an order that is fixed by the sizes and lengths, without
+ * atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within
+ * their rounding). A row with lse = -inf, whose products are not Inf or NaN, adds nothing. Keys a row does not see have no
+ * effect; blocks that no row of a sequence sees, in front of a window, are not read and need no valid slot. Other slot ids
+ * beyond both pools set the error word, and their keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
 int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *a, void *stream);
 /* Depends on sizes only. 0 for arguments kvt_weigh_blocks refuses and where none is needed. */
 uint64_t kvt_weigh_scratch_bytes(kvt_engine *e, const kvt_weigh_args *a);

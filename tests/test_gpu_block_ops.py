@@ -542,6 +542,26 @@ def test_weigh_prompts_and_chunks(B, dtype, dim, heads, group, new, past):  # no
     check_weigh(s)
 
 
+@pytest.mark.parametrize("dim,group", [(128, 4), (64, 7), (40, 2)])
+def test_many_sequences(B, dim, group):  # noqa: F811
+    """More of them than a warp has lanes, some without new tokens, some without any."""
+    import torch
+    n = 75
+    new, past = [(i * 7) % 45 if i % 6 else 0 for i in range(n)], [(i * 131) % 900 if i % 5 else 0 for i in range(n)]
+    s = make(B, (new, past), "bf16", 0, 2, group, dim, layers=1, layer=0, tail=True, pad=5)
+    check_bounds(s)
+    k = random_bounds(s, torch.Generator("cuda").manual_seed(3))
+    check_select(s, k, 9, 1, 2)
+    check_sparse(s, random_lists(s, 4, seed=5))
+    check_weigh(s, keep=0.5)
+    check_weigh(s, window=70)
+
+
+@pytest.mark.parametrize("new,past,window", [([40, 1], [30000, 9000], 0), ([64, 3], [20000, 100], 9000), ([9], [66000], 0)])
+def test_weigh_long(B, new, past, window):  # noqa: F811
+    check_weigh(make(B, (new, past), "bf16", 0, 1, 4, 64, layers=1, layer=0), window=window)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("scale,gain", [(1e-3, 4.0), (4.0, 1.0), (0.125, 30.0), (5e-5, 1.0), (3e4, 1e-3), (0.0, 1.0), (1.0, 8.0)])
 def test_weigh_scales_near_and_far(B, dtype, scale, gain):  # noqa: F811

@@ -628,8 +628,9 @@ def evict_reference(table, weights, kv_len, n_blocks, first, last):
 
 
 @pytest.mark.parametrize("n_blocks,first,last", [(40, 1, 2), (3, 0, 1), (7, 3, 4), (5000, 4, 32), (100000, 1, 2)])
-@pytest.mark.parametrize("kv,width", [([0, 1, 16, 700, 9999], 700), ([100000], 6250), ([1000003, 640, 5], 62501), ([639, 640, 641, 656, 657], 45)])
-@pytest.mark.parametrize("values", ["random", "few", "strange"])
+@pytest.mark.parametrize("kv,width", [([0, 1, 16, 700, 9999], 700), ([100000], 6250), ([1000003, 640, 5], 62501), ([639, 640, 641, 656, 657], 45), ([65540, 70000, 100], 4376),
+                                      ([400000, 524288], 32768), ([2200001], 137501)])
+@pytest.mark.parametrize("values", ["random", "few", "strange", "near"])
 def test_evict(B, kv, width, n_blocks, first, last, values):  # noqa: F811
     import torch
     eng = B.Engine(n_layers=1, n_kv_heads=1, head_dim=64, n_hbm_blocks=4, n_host_blocks=0, max_contexts=1, max_messages=16, max_tokens=64)
@@ -639,6 +640,11 @@ def test_evict(B, kv, width, n_blocks, first, last, values):  # noqa: F811
     weights = torch.randn(n, width + 1, generator=g, device="cuda")[:, 1:]
     if values == "few":
         weights = weights.mul_(1.5).round_()
+    if values == "near":                     # apart in the last of the 32 bits alone: most of them, and of the rest, three by three, two alike and one next to them
+        weights = weights.mul_(20).round_() * 2.0 ** -23 + 1
+        rest = torch.randn(n, -(-width // 9), generator=g, device="cuda") * 2
+        for i, x in ((0, rest), (3, rest), (6, torch.nextafter(rest, torch.full_like(rest, math.inf)))):
+            weights[:, i::9] = x[:, :weights[:, i::9].shape[1]]
     if values == "strange":
         weights[:, ::7] = math.nan
         weights[:, ::5] = -math.inf

@@ -668,6 +668,8 @@ constexpr u64 SLAB_BYTES = 160ull << 20;
 SelectPlan plan_select(const SelectArgs &a, int sm_count) {
   SelectPlan p{};
   p.sms = sm_count;
+  p.slab = a.b.n_tokens;
+  if (a.b.max_blocks <= a.n_blocks) return p;            // every list has all there are: no scores
   p.scores_stride = ((u64)a.b.max_blocks + 7) / 8 * 8;
   const u64 token = p.scores_stride * a.n_kv_heads * 4;
   p.slab = (u32)std::min<u64>(a.b.n_tokens, std::max<u64>(1, SLAB_BYTES / token));

@@ -572,7 +572,9 @@ typedef struct kvt_weigh_args {
  * atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within
  * their rounding). A row with lse = -inf, whose products are not Inf or NaN, adds nothing. Keys a row does not see have no
  * effect; blocks that no row of a sequence sees, in front of a window, are not read and need no valid slot. Other slot ids
- * beyond both pools set the error word, and their keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
+ * beyond both pools set the error word, and their keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. Where
+ * kvt_kv_check reports a wait that ran out (KVT_E_DEVICE), `out` holds, of each sequence's blocks, new weights or what it held
+ * before, and with many rows (max_q_len) what it held before. */
 int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *a, void *stream);
 /* Depends on sizes only. 0 for arguments kvt_weigh_blocks refuses and where none is needed. */
 uint64_t kvt_weigh_scratch_bytes(kvt_engine *e, const kvt_weigh_args *a);
@@ -689,7 +691,8 @@ int32_t kvt_debug_set_classify_mode(kvt_engine *e, uint32_t mode);
 
 /* Test hook for the bounded wait of the single-pass lookup (variant 2): the number of polls a chunk spends on its
  * predecessors' publications before it gives up (default 2^18). With 0 every chunk that needs a predecessor gives
- * up at once: the kernel still returns normally, the call reports KVT_E_DEVICE and the engine is unchanged. */
+ * up at once: the kernel still returns normally, the call reports KVT_E_DEVICE and the engine is unchanged. 0 also makes
+ * the many-row kernel of kvt_weigh_blocks give up where it would wait for its own warps for the first time. */
 int32_t kvt_debug_set_wait_limit(kvt_engine *e, uint32_t polls);
 
 /* Text of the last error of this engine (always NUL-terminated). */

@@ -42,6 +42,7 @@ struct AttendArgs {
   uint32_t layer, layer_major;
   uint8_t *scratch;
   float scale_log2;                 // scale / ln 2: scores in powers of two
+  uint32_t lose;                    // a test: the first wait of a planning warp for another's work counts as run out
   uint32_t *err;
 };
 

@@ -1589,15 +1589,20 @@ __device__ __forceinline__ Seen seen_by(const AttendArgs &a, const Seq &q, u32 k
 }
 __device__ __forceinline__ u32 row_tiles(const Seen &s, u32 tokens) { return (s.hi - s.lo + tokens - 1) / tokens; }
 
-// Scratch: a header {tiles per stretch, tiles}, the place of each pair in the work (and the end), then 16 sums,
-// one per block, for each (pair, CTA): the one of pair p and CTA c is number p + c, as each next one has a greater p or c.
-struct WeighScratch { u64 *per, *place; float *sums; };
+// Scratch: a header {tiles per stretch, tiles}, the place of each pair in the work (and the end), a word per CTA (1: it has given up a
+// wait, and its sums are not to be used), then 16 sums, one per block, for each (pair, CTA): the one of pair p and CTA c is number p + c,
+// as each next one has a greater p or c. All but the sums are written whatever the waits come to, so what the kernel behind
+// reads by them is in bounds.
+struct WeighScratch { u64 *per, *place; u32 *lost; float *sums; };
 __host__ __device__ __forceinline__ u64 weigh_pairs(u32 n_seqs, u32 max_blocks) { return (u64)n_seqs * ((max_blocks + WTC_KB - 1) / WTC_KB); }
-__host__ __device__ __forceinline__ WeighScratch weigh_scratch(u8 *p, u32 n_seqs, u32 max_blocks) {
+__host__ __device__ __forceinline__ u64 weigh_header(u64 pairs, u32 n_ctas) { return (16 + 8 * (pairs + 1) + 4ull * n_ctas + 15) & ~15ull; }
+__device__ __forceinline__ WeighScratch weigh_scratch(u8 *p, u32 n_seqs, u32 max_blocks, u32 n_ctas) {
+  const u64 pairs = weigh_pairs(n_seqs, max_blocks);
   WeighScratch s;
   s.per = (u64 *)p;
   s.place = s.per + 2;
-  s.sums = (float *)(p + ((16 + 8 * (weigh_pairs(n_seqs, max_blocks) + 1) + 15) & ~15ull));
+  s.lost = (u32 *)(s.place + pairs + 1);
+  s.sums = (float *)(p + weigh_header(pairs, n_ctas));
   return s;
 }
 
@@ -1664,8 +1669,9 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
   };
 
   if (warp == 17) {
-    // ---- what this CTA does. A lane per pair, 32 pairs of a sequence at a time; twice: for the sum of the work, then for its share.
-    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
+    // ---- what this CTA does. A lane per pair, 32 pairs of a sequence at a time; twice: for the sum of the work (and CTA 0 for the places,
+    // before anything is waited for), then for its share.
+    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks, gridDim.x);
     u64 total = 0, per = 0, tokens = 0;
     u32 made = 0;
     bool ok = true;
@@ -1690,13 +1696,17 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
             u64 incl = work;
 #pragma unroll
             for (u32 o = 1; o < 32; o *= 2) { const u64 z = __shfl_up_sync(~0u, incl, o); if (lane >= o) incl += z; }
-            if (pass) {
-              const u64 from = base + incl - work, to = base + incl;
+            const u64 from = base + incl - work, to = base + incl;
+            if (pass == 0) {
               if (blockIdx.x == 0 && k < pairs) sc.place[pair + k] = from;
+            } else {
               const u64 f = max(from, begin), t = min(to, end);
               for (u32 mask = __ballot_sync(~0u, f < t); mask && ok; mask &= mask - 1) {
                 const u32 at = made % WTC_JOBS;
-                if (made >= WTC_JOBS && !(ok = tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience))) break;
+                if (made >= WTC_JOBS) {
+                  if (a.lose) *lost = 1;               // a test: as if this wait had run out
+                  if (!(ok = !a.lose && tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience))) break;
+                }
                 if (lane == __ffs(mask) - 1) {
                   WeighJob j;
                   j.t0 = q.t0 + seen.lo; j.tokens = seen.hi - seen.lo; j.index0 = q.kv - q.n + seen.lo;
@@ -1712,7 +1722,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
               }
             }
             base += __shfl_sync(~0u, incl, 31);
-            if (pass && blockIdx.x && base >= end) { k0 = pairs; y = n_here; s0 = a.b.n_seqs; break; }     // (CTA 0 goes on for the places)
+            if (pass && base >= end) { k0 = pairs; y = n_here; s0 = a.b.n_seqs; break; }
           }
           pair += pairs;
         }
@@ -1723,9 +1733,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
         // starts that go up and down make the same tokens count again and again: then nothing is added (load_seq has set the error word)
         total = tokens > a.b.n_tokens ? 0 : base;
         per = (total + gridDim.x - 1) / gridDim.x;
-        if (blockIdx.x == 0 && lane == 0) { sc.per[0] = per; sc.per[1] = total; }
-      } else if (blockIdx.x == 0 && lane == 0) {
-        sc.place[pair] = base;
+        if (blockIdx.x == 0 && lane == 0) { sc.per[0] = per; sc.per[1] = total; sc.place[pair] = base; }
       }
     }
     const u32 at = made % WTC_JOBS;
@@ -1870,13 +1878,14 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
         if (++r == j.tiles) { r = 0; ++h; }
       }
     }
-    if (mapped && mine == 0 && n > side) {               // landed before the CTA ends: this side's last tile, number `brought`
-      if (brought != ~0u) bar_wait(qfull + (brought % WTC_Q) * 8, (brought / WTC_Q) & 1);
+    if (mapped && mine == 0 && brought != ~0u) {         // landed before the CTA ends: this side's last tile, and where it may not have been used the one before
+      if (*lost && brought >= 2) bar_wait(qfull + ((brought - 2) % WTC_Q) * 8, ((brought - 2) / WTC_Q) & 1);
+      bar_wait(qfull + (brought % WTC_Q) * 8, (brought / WTC_Q) & 1);
     }
   } else {
     // ---- powers and their sums: a key per thread, half of the columns
     const u32 tile = warp / 8, half = warp / 4 % 2, key_t = tid % TC_TILE, from = tmem + ((warp % 4) << 21) + tile * 128 + half * 64;
-    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
+    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks, gridDim.x);
     const u64 scale2 = pack2(a.scale_log2, a.scale_log2);
     u32 n = 0;
     bool ok = true;
@@ -1961,11 +1970,14 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
   __syncthreads();
   tc_after();
   if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-  if (tid == 0 && s_lost) kv_err(a.err, KVERR_WAIT);
+  if (tid == 0) {
+    weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks, gridDim.x).lost[blockIdx.x] = s_lost;
+    if (s_lost) kv_err(a.err, KVERR_WAIT);
+  }
 }
 
-// Puts the sums of the kernel before together: a thread per block.
-__global__ void __launch_bounds__(256) k_weigh_join(WeighArgs x) {
+// Puts the sums of the kernel before, of n_ctas CTAs, together: a thread per block. Where one of them has given up nothing is written.
+__global__ void __launch_bounds__(256) k_weigh_join(WeighArgs x, u32 n_ctas) {
   const AttendArgs &a = x.a;
   const u32 chunks = (a.b.max_blocks + 255) / 256, seq = blockIdx.x / chunks, b = (blockIdx.x - seq * chunks) * 256 + threadIdx.x;
   // the sequence's first pair
@@ -1982,12 +1994,14 @@ __global__ void __launch_bounds__(256) k_weigh_join(WeighArgs x) {
   }
   const Seq q = load_seq(a.b, seq, a.err);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (b >= a.b.max_blocks) return;
+  const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks, n_ctas);
+  const u64 per = sc.per[0], total = sc.per[1];
+  bool lost = false;
+  for (u32 c = threadIdx.x; c < n_ctas; c += 256) lost |= sc.lost[c] != 0;
+  if (__syncthreads_or(lost) || b >= a.b.max_blocks) return;
   float sum = 0.0f;
   const bool held = b < (q.kv + BT - 1) / BT;
   if (held) {
-    const WeighScratch sc = weigh_scratch(a.scratch, a.b.n_seqs, a.b.max_blocks);
-    const u64 per = sc.per[0], total = sc.per[1];
     const u32 pair = before + b / WTC_KB;
     if (total) {
       const u64 from = sc.place[pair], to = sc.place[pair + 1];
@@ -2018,7 +2032,7 @@ WeighPlan plan_weigh(const WeighArgs &x, u32 max_q_len, int sm_count) {
   }
   if (p.many) {
     const u64 pairs = weigh_pairs(x.a.b.n_seqs, x.a.b.max_blocks);
-    p.scratch_bytes = ((16 + 8 * (pairs + 1) + 15) & ~15ull) + (pairs + p.grid) * WTC_KB * 4;
+    p.scratch_bytes = weigh_header(pairs, p.grid) + (pairs + p.grid) * WTC_KB * 4;
   }
   return p;
 }
@@ -2039,7 +2053,7 @@ static cudaError_t launch_weigh_tc(const WeighArgs &x, const WeighPlan &p, const
   at.val.programmaticStreamSerializationAllowed = 1;
   c.attrs = &at; c.numAttrs = 1;
   ++*launches;
-  return cudaLaunchKernelEx(&c, k_weigh_join, x);
+  return cudaLaunchKernelEx(&c, k_weigh_join, x, p.grid);
 }
 template <class T, u32 D, u32 NT>
 static cudaError_t launch_weigh_split(const WeighArgs &x, const WeighPlan &p, const KvMaps &m, cudaStream_t s, u64 *allowed) {

@@ -2322,7 +2322,7 @@ AttendArgs attend_args(kvt_engine *e, const kvt_attend_args &a) {
   const double scale = a.scale > 0.0f ? (double)a.scale : 1.0 / std::sqrt((double)e->cfg.head_dim);
   x.scale_log2 = (float)(scale * 1.4426950408889634);
   x.layer = a.layer; x.layer_major = e->cfg.pool_layout == KVT_LAYOUT_LAYER_MAJOR;
-  x.scratch = (u8 *)a.scratch;
+  x.scratch = (u8 *)a.scratch; x.lose = e->wait_limit == 0;
   x.err = e->dp<u32>(e->L.kv_err);
   return x;
 }

@@ -613,6 +613,38 @@ def test_weigh_is_the_same_every_time(B):  # noqa: F811
         assert all(torch.equal(runs[0], r) for r in runs[1:])
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("strided", [False, True])
+def test_weigh_that_gives_up_a_wait_writes_nothing(B, dtype, dim, strided):  # noqa: F811
+    """40 and 33 tokens on long contexts: a CTA has more jobs than it holds at once, so its planning warp has to wait. Where that wait runs
+    out the call ends, says so, and leaves the weights that it was given as they were, whatever was in its scratch before."""
+    import torch
+    s = make(B, ([40, 33], [100000, 60000]), dtype, 0, 2, 2, dim, layers=1, layer=0, strided=strided)
+    lse = torch.full((s.rows, 4), 6.0, device="cuda")
+    old = torch.rand(s.table.shape, generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    call = lambda w: s.eng.weigh_blocks(s.layer, s.q, lse, s.table, s.q_start, s.kv_len, weights=w, out=w)      # noqa: E731
+    want = call(old.clone())
+    s.eng.kv_check()
+    weights = old.clone()
+    s.eng.set_wait_limit(0)
+    b = B.Batch(*s.eng._kv_batch("", s.t, s.table, s.q_start, s.kv_len, 0))
+    a = B.WeighArgs(b, 0, 0 if dtype == "bf16" else 1, 4, 0, 0, 0.0, 1.0, 0, s.q.data_ptr(), lse.data_ptr(), *s.q.stride()[:2], weights.data_ptr(),
+                    weights.data_ptr(), weights.stride(0), weights.stride(0), 0, 0)
+    n = s.eng.L.kvt_weigh_scratch_bytes(s.eng.h, C.byref(a))
+    assert n
+    scratch = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    a.scratch, a.scratch_bytes = scratch.data_ptr(), n
+    assert s.eng.L.kvt_weigh_blocks(s.eng.h, C.byref(a), s.eng._kv_stream()) == 0
+    with pytest.raises(B.KvtError, match="wait"):
+        s.eng.kv_check()
+    assert torch.equal(weights, old)
+    s.eng.set_wait_limit(1 << 18)
+    scratch.fill_(255)
+    assert s.eng.L.kvt_weigh_blocks(s.eng.h, C.byref(a), s.eng._kv_stream()) == 0
+    s.eng.kv_check()
+    assert torch.equal(weights, want)
+
+
 # ---- eviction -----------------------------------------------------------------------------------
 def evict_reference(table, weights, kv_len, n_blocks, first, last):
     t, w, e, n = np.full_like(table, -1), np.zeros_like(weights), np.full_like(table, -1), kv_len.copy()

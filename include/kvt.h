@@ -692,7 +692,7 @@ int32_t kvt_debug_set_classify_mode(kvt_engine *e, uint32_t mode);
 /* Test hook for the bounded wait of the single-pass lookup (variant 2): the number of polls a chunk spends on its
  * predecessors' publications before it gives up (default 2^18). With 0 every chunk that needs a predecessor gives
  * up at once: the kernel still returns normally, the call reports KVT_E_DEVICE and the engine is unchanged. 0 also makes
- * the many-row kernel of kvt_weigh_blocks give up where it would wait for its own warps for the first time. */
+ * the many-row kernels of kvt_attend and kvt_weigh_blocks give up where their planning warps would wait for the first time. */
 int32_t kvt_debug_set_wait_limit(kvt_engine *e, uint32_t polls);
 
 /* Text of the last error of this engine (always NUL-terminated). */

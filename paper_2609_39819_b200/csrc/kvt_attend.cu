@@ -503,17 +503,19 @@ __global__ void __launch_bounds__(128) k_attend_join_tc(AttendArgs a, u32 rows, 
     const u32 n = plan.y, stride = plan.z * H;
     if (seq == ~0u || n <= 1) continue;
     u32 at[BATCH];                       // first partial's row
+    bool sound = true;                   // a plan that was not written, since a wait for jobs ran out, names places that there are not
     float m[BATCH], l[BATCH], acc[BATCH][C];
 #pragma unroll
     for (u32 b = 0; b < BATCH; ++b) {
       const u32 hq = min(hq0 + b, a.n_q_heads - 1), h = hq / a.group, r = (t - start) * a.group + hq - h * a.group, tile = r / rows;
       const u32 p0 = (plan.x + tile) * H + h;
-      at[b] = (p0 + (u64)(n - 1) * stride < n_parts ? p0 : 0) * rows + r - tile * rows;
-      if (p0 + (u64)(n - 1) * stride >= n_parts && lane == 0) kv_err(a.err, KVERR_RANGE);     // cannot happen
+      at[b] = p0 * rows + r - tile * rows;
+      sound &= p0 + (u64)(n - 1) * max(stride, 1u) < n_parts;
       m[b] = -INFINITY; l[b] = 0.0f;
 #pragma unroll
       for (u32 c = 0; c < C; ++c) acc[b][c] = 0.0f;
     }
+    if (!sound) { if (lane == 0) kv_err(a.err, KVERR_RANGE); continue; }
     for (u32 i = 0; i < n; i += STEP) {
       float2 x[STEP][BATCH];
       float v[STEP][BATCH][C];
@@ -1203,7 +1205,7 @@ k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ KvMaps
       }
       const u32 hit = __ballot_sync(~0u, want >= at && want < at + my_jobs);
       const u32 slot = k % TC_JOBS;
-      if (k >= TC_JOBS && !(ok = tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost, a.b.max_blocks))) break;
+      if (k >= TC_JOBS && !(ok = !a.lose && tc_wait(jempty + slot * 8, (k / TC_JOBS - 1) & 1, lost, a.b.max_blocks))) { *lost = 1; break; }
       if (hit && lane == __ffs(hit) - 1) {
         Job j;
         const u32 x = want - at, y = x / H, h = x - y * H, pc = y / tiles, tile = tiles - 1 - (y - pc * tiles);

@@ -1703,10 +1703,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
               const u64 f = max(from, begin), t = min(to, end);
               for (u32 mask = __ballot_sync(~0u, f < t); mask && ok; mask &= mask - 1) {
                 const u32 at = made % WTC_JOBS;
-                if (made >= WTC_JOBS) {
-                  if (a.lose) *lost = 1;               // a test: as if this wait had run out
-                  if (!(ok = !a.lose && tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience))) break;
-                }
+                if (made >= WTC_JOBS && !(ok = !a.lose && tc_wait(jempty + at * 8, (made / WTC_JOBS - 1) & 1, lost, patience))) { *lost = 1; break; }
                 if (lane == __ffs(mask) - 1) {
                   WeighJob j;
                   j.t0 = q.t0 + seen.lo; j.tokens = seen.hi - seen.lo; j.index0 = q.kv - q.n + seen.lo;

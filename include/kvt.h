@@ -570,7 +570,9 @@ typedef struct kvt_weigh_args {
  * keys of block b that the token sees of exp(scale q.k - lse); 0 for blocks behind kv_len[s]. Sums of all layers come from
  * calls with the same weights, one per layer. Sums are in 32 bits, in an order that is fixed by the sizes and lengths, without
  * atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within
- * their rounding). A row with lse = -inf, whose products are not Inf or NaN, adds nothing. Keys a row does not see have no
+ * their rounding). The exponent is off by up to some 2^-22 of |scale q.k| and |lse|, so from 2^20 on little is left of a weight; where
+ * scale q.k - lse is far from 0 all the same, it is 0 or Inf as it should be. A row with lse = -inf, whose products are not Inf or NaN, adds
+ * nothing. Keys a row does not see have no
  * effect; blocks that no row of a sequence sees, in front of a window, are not read and need no valid slot. Other slot ids
  * beyond both pools set the error word, and their keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. Where
  * kvt_kv_check reports a wait that ran out (KVT_E_DEVICE), `out` holds, of each sequence's blocks, new weights or what it held

@@ -1495,7 +1495,7 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
 // Many rows (prompts, chunks). Here the keys are the rows of the matrix instruction as well: S^T = K Q^T for 256 keys, two tiles of
 // 128, by 128 (token, head) rows, so that a thread owns a key and adds up what its row of S^T gives in a register, with no
 // exchange between threads and no masks but at the diagonal. The row's lse comes off in the product itself: with 16 channels more,
-// constants on the side of K and the parts of -lse / scale in the element type on the side of Q, S^T is (s - lse / scale) in 32 bits,
+// constants on the side of K and the parts of -lse / scale in bf16 on the side of Q, S^T is (s - lse / scale) in 32 bits,
 // and a power is one multiplication and ex2. (With lse from shared memory and a fused multiply-add it was bound by shared memory, which
 // the products alone keep busy half of the time: 8192 tokens, 8 x 4 heads of 128, 352 us.)
 // Bound by the exponentials: 256 keys by 128 rows take 2600 cycles, of which the special-function units need 2048 for all of them (every
@@ -1517,8 +1517,8 @@ template <u32 D> struct WeighShape {
   static constexpr u32 BLOCK = BT * D * 2, K = TC_TILE * D * 2, Q = TC_TILE * D * 2, EXTRA = TC_TILE * 32, SMEM = WTC_K * K + WTC_Q * Q + (WTC_Q + 1) * EXTRA + 1024;
 };
 // The 16 channels more, [row / 8][channel / 8][row % 8][channel % 8] without swizzle (lbo = 128: next 8 channels, sbo = 256: next 8 rows).
-// Channels 1 to 4 carry parts of -lse / scale over ALPHA = 2^-e, where the scale (of powers of two) is 2^e to 2^(e+1), channel 0 a coarse
-// part over 2^15 first in fp16, whose numbers end at 2^16.
+// Channels 0 to 3 carry parts of -lse / scale over ALPHA = 2^-e, where the scale (of powers of two) is 2^e to 2^(e+1). They are bf16 in either
+// type of pool, an instruction of its own on the same sums: fp16 numbers end at 2^16, and lse / scale of fp16 scores at 2^40.
 __device__ __forceinline__ u64 plain_desc(u32 addr) { return (u64)((addr & 0x3FFFF) >> 4) | (u64)(128 >> 4) << 16 | (u64)(256 >> 4) << 32 | 1ull << 46; }
 __device__ __forceinline__ float extra_alpha(float scale_log2) { return __uint_as_float((254u - (__float_as_uint(scale_log2) >> 23)) << 23); }
 // -1 / scale as two numbers (the scale that scores are multiplied by is the one of powers of two): lse times it is -lse / scale. (32-bit arithmetic in two parts: with 64 bits the warps that make the
@@ -1530,21 +1530,20 @@ __device__ __forceinline__ PerScale per_scale(const WeighArgs &x) {
   p.high = (float)k; p.low = (float)(k - (double)p.high);
   return p;
 }
-template <class T> __device__ __forceinline__ uint4 extra_parts(float lse, const PerScale &k, float per_alpha) {
-  constexpr bool FP16 = !__is_same(T, __nv_bfloat16);
-  float e[5] = {0, 0, 0, 0, 0};
-  if (fabsf(lse) < INFINITY) {
+__device__ __forceinline__ uint4 extra_parts(float lse, const PerScale &k, float per_alpha) {
+  typedef Elem<__nv_bfloat16> E;
+  float e[4] = {0, 0, 0, 0};
+  if (fabsf(lse) <= 1e30f) {
     float high = lse * k.high, low = fmaf(lse, k.high, -high) + lse * k.low;
-    if (FP16) { e[0] = Elem<T>::up1(Elem<T>::down1(high * 0x1p-15f)); high -= e[0] * 0x1p15f; }
     high *= per_alpha; low *= per_alpha;
 #pragma unroll
-    for (u32 y = 1; y < 5; ++y) {
-      e[y] = Elem<T>::up1(Elem<T>::down1(high));
+    for (u32 y = 0; y < 4; ++y) {
+      e[y] = E::up1(E::down1(high));
       high -= e[y];
-      if (y == 1) high += low;           // (what is left of the first part is far smaller, so nothing of either is lost)
+      if (y == 0) high += low;           // (what is left of the first part is far smaller, so nothing of either is lost)
     }
-  } else e[1] = lse != lse ? lse : -INFINITY;            // -inf: a row without keys, no weight
-  return make_uint4(Elem<T>::down(e[0], e[1]), Elem<T>::down(e[2], e[3]), Elem<T>::down(e[4], 0.0f), 0u);
+  } else e[0] = lse != lse ? lse : lse > 0.0f || lse == -INFINITY ? -INFINITY : INFINITY;      // -inf: a row without keys, no weight
+  return make_uint4(E::down(e[0], e[1]), E::down(e[2], e[3]), 0u, 0u);
 }
 
 // 2^t of two numbers without the special-function units: t = n + f with n the nearest whole number, 2^f on [-1/2, 1/2] by the polynomial of
@@ -1761,7 +1760,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
   } else if (warp == 16) {
     // ---- products
     if (elect_one()) {
-      const u32 id = tc_idesc(FP16, TC_TILE, false);
+      const u32 id = tc_idesc(FP16, TC_TILE, false), id_extra = tc_idesc(false, TC_TILE, false);
       const u64 dk0 = tc_desc(sk, 16, D * 16), dq0 = tc_desc(sq, 16, 1024), de = plain_desc(extra);
       u32 n = 0, it = 0;
       bool ok = true;
@@ -1787,7 +1786,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
 #pragma unroll
             for (u32 k = 0; k < D / 16; ++k)
               tc_mma_ss(tmem + buf * 256 + tile * 128, dk + ((k / 4) * 1024 + (k % 4) * 32) / 16, dq + ((k / 4) * (TC_TILE * 128) + (k % 4) * 32) / 16, id, k > 0);
-            tc_mma_ss(tmem + buf * 256 + tile * 128, de, de + (1 + st) * (S::EXTRA / 16), id, 1);
+            tc_mma_ss(tmem + buf * 256 + tile * 128, de, de + (1 + st) * (S::EXTRA / 16), id_extra, 1);
           }
           if (!ok) break;
           tc_commit(sfull + buf * 8);
@@ -1814,10 +1813,10 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
     for (u32 i = side * 64 + mine; i < WTC_Q * S::EXTRA / 16; i += 128) zero(extra + S::EXTRA + i * 16);
     if (side == 0) {                     // K's constants, before the first tile is handed over
       const float alpha = extra_alpha(a.scale_log2);
-      const u32 c0 = Elem<T>::down(FP16 ? 0x1p15f : 0.0f, alpha), c1 = Elem<T>::down(alpha, alpha), c2 = Elem<T>::down(alpha, 0.0f);
+      const u32 c = Elem<__nv_bfloat16>::down(alpha, alpha);
       for (u32 row = mine; row < TC_TILE; row += 64) {
         const u32 at = extra + row / 8 * 256 + row % 8 * 16;
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(c0), "r"(c1), "r"(c2), "r"(0) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(c), "r"(c), "r"(0), "r"(0) : "memory");
         zero(at + 128);
       }
     }
@@ -1834,7 +1833,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
 #pragma unroll
           for (u32 y = 0; y < 2; ++y) {
             const u32 row = mine + 64 * y;
-            parts[y] = extra_parts<T>(row < left ? a.lse[(u64)(t + my_tok[y]) * a.n_q_heads + h * g + row - my_tok[y] * g] : -INFINITY, k, per_alpha);
+            parts[y] = extra_parts(row < left ? a.lse[(u64)(t + my_tok[y]) * a.n_q_heads + h * g + row - my_tok[y] * g] : -INFINITY, k, per_alpha);
           }
           if (n >= WTC_Q && !(ok = tc_wait(qempty + st * 8, (n / WTC_Q - 1) & 1, lost, patience))) break;
           brought = n;
@@ -2015,7 +2014,7 @@ WeighPlan plan_weigh(const WeighArgs &x, u32 max_q_len, int sm_count) {
   WeighPlan p{};
   const u32 d = x.a.p.head_dim;
   const u64 rows = (u64)(max_q_len && max_q_len < x.a.b.n_tokens ? max_q_len : x.a.b.n_tokens) * x.a.group;
-  // (the parts of lse / scale are numbers of the element type: scales far from 1 are left to the first kernel)
+  // (the parts of lse / scale are bf16 numbers, over a power of two that is one as well: scales far from 1 are left to the first kernel)
   p.many = (d == 64 || d == 128) && rows > WEIGH_FEW && x.a.group <= TC_TILE && x.a.scale_log2 > 0x1p-13f && x.a.scale_log2 < 0x1p13f;
   p.grid = sm_count;
   const u64 blocks = (u64)x.a.b.n_seqs * x.a.b.max_blocks;

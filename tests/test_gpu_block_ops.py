@@ -571,6 +571,37 @@ def test_weigh_scales_near_and_far(B, dtype, scale, gain):  # noqa: F811
         check_weigh(s, scale=scale)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lse", [5.0, 3e8, 6e9, 2e11, 1e28, 3e38, -3e8, -6e9, -2e11, -1e28, -3e38, math.inf, math.nan])
+def test_weigh_lse_of_any_size(B, dtype, dim, lse):  # noqa: F811
+    """Scores of 0 and of +- 2^29 dim / sqrt(dim), the same by every kernel: far from lse, so that every weight is 0 or Inf, or at 0."""
+    import torch
+    s = make(B, ([60], [500]), dtype, 0, 1, 2, dim, layers=1, layer=0)
+    s.q.fill_(2.0 ** 15)
+    for b in range(s.host_table.shape[1] - 2):
+        s._chunk(int(s.host_table[0, b]), 0).fill_((0.0, 2.0 ** 14, -2.0 ** 14)[b % 3])
+    rows = torch.full((s.t, 2), lse, device="cuda")
+    rows[::2] = -math.inf                   # half of the rows count for nothing
+    n = s.table.shape[1]
+    want = torch.zeros(n, dtype=torch.float64)
+    for b in range(n - 2):
+        score = (0.0, 1.0, -1.0)[b % 3] * 2.0 ** 29 * dim ** 0.5
+        for i in range(b * BT, min(b * BT + BT, s.kv[0])):
+            seen = sum(1 for t in range(1, s.t, 2) if 500 + t >= i)
+            if seen:
+                x = score - float(np.float32(lse))
+                want[b] += 2 * seen * (math.nan if math.isnan(x) else math.inf if x > 700 else math.exp(x))
+    want = want.float().double()
+    for hint in (None, 1):
+        got = s.eng.weigh_blocks(0, s.q, rows, s.table, s.q_start, s.kv_len, max_q_len=hint)[0].double().cpu()
+        s.eng.kv_check()
+        fine = torch.isfinite(want)
+        assert torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)]) and torch.equal(torch.isnan(got), torch.isnan(want))
+        # at a score of 0 and lse of 5: powers to 2^-22 and 5 * 2^-22, and 32-bit sums
+        assert bool(((got - want).abs()[fine] <= want[fine] * (6 * 2.0 ** -22 + (n * 40) * E32)).all())
+
+
 def test_weights_sum_to_the_number_of_rows(B):  # noqa: F811
     s = make(B, ([50, 1, 700], [10, 5000, 0]), "bf16", 0, 2, 4, 128)
     got = check_weigh(s).double().sum(1).cpu()

@@ -568,8 +568,8 @@ typedef struct kvt_weigh_args {
 } kvt_weigh_args;
 /* Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
  * keys of block b that the token sees of exp(scale q.k - lse); 0 for blocks behind kv_len[s]. Sums of all layers come from
- * calls with the same weights, one per layer. Sums are in 32 bits, in an order that is fixed by the sizes and lengths, without
- * atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within
+ * calls with the same weights, one per layer. Sums of up to a hundred powers are in 32 bits, sums of those in 64 or with what their rounding
+ * took, the result in 32; all in an order that is fixed by the sizes and lengths, without atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within
  * their rounding). The exponent is off by up to some 2^-22 of |scale q.k| and |lse|, so from 2^20 on little is left of a weight; where
  * scale q.k - lse is far from 0 all the same, it is 0 or Inf as it should be. A row with lse = -inf, whose products are not Inf or NaN, adds
  * nothing. Keys a row does not see have no

@@ -1297,7 +1297,7 @@ __global__ void __launch_bounds__(WS_THREADS, 2) k_weigh_split(const __grid_cons
       if (++load_b == nb) { load_b = 0; load_h += WS_WARPS; if (load_h >= H) load_h = warp; }
     };
     for (u32 i = 0; i < min(S::STAGES, n_items); ++i) load();
-    float acc = 0.0f;
+    double acc = 0.0;                    // (a long prompt adds thousands of sums up: 32 bits would lose some 10^-5)
     u32 it = 0, st = 0, phase = 0;
     for (u32 r0 = 0; ok && r0 < rows; r0 += NT * 8)
       for (u32 h = warp; ok && h < H; h += WS_WARPS) {
@@ -1356,7 +1356,7 @@ __global__ void __launch_bounds__(WS_THREADS, 2) k_weigh_split(const __grid_cons
           if (lane == b) acc += sum;
         }
       }
-    s_sum[warp][lane] = acc;
+    s_sum[warp][lane] = (float)acc;
     if (__syncthreads_or(!ok)) {         // let the copies in flight land, for a while, before the CTA ends; nothing is written
       if (lane == 0) kv_err(a.err, KVERR_WAIT);
       for (u32 i = 0; i < S::STAGES; ++i) for (u32 y = 0; y < 2; ++y) bar_wait(bar0 + i * 8, y);
@@ -1416,7 +1416,7 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
         }
       return x;
     };
-    float total = 0.0f;                  // of the block, over the heads
+    double total = 0.0;                  // of the block, over the heads
     // of one block and head
     auto work = [&](const Keys &keys, u32 i, u32 k) {
       const u32 h = sub + share * k, b = b_tile + first + step * i;
@@ -1424,7 +1424,8 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
       const int key0 = (int)(b * BT);
       const u32 tok0 = a.full ? 0 : (u32)max(0, key0 - shift);
       const u32 tok1 = a.window ? (u32)max(0ll, min((long long)q.n, (long long)key0 + BT - 1 + a.window - shift)) : q.n;
-      float sum = 0.0f, part = 0.0f;
+      double sum = 0.0;
+      float part = 0.0f;
       u32 count = 0;
       for (u32 r0 = tok0 * g; r0 < tok1 * g; r0 += 8) {
         const u32 r = min(r0 + r8, tok1 * g - 1), tok = r / g;
@@ -1453,13 +1454,13 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
             part += key < hi && key >= lo ? e : 0.0f;
           }
         }
-        if (++count % 32 == 0) { sum += part; part = 0.0f; }   // sums of few, then of those: 32 bits hold them
+        if (++count % 16 == 0) { sum += part; part = 0.0f; }   // sums of few in 32 bits, of those in 64
       }
       total += sum + part;
       if (k + 1 == n_heads) {            // the block is through
-        total = sum_over_warp(total);
-        if (lane == 0) s_sum[warp][first + step * i] = total;
-        total = 0.0f;
+        const float all = sum_over_warp((float)total);
+        if (lane == 0) s_sum[warp][first + step * i] = all;
+        total = 0.0;
       }
     };
     const u32 n_items = n_blocks * n_heads;
@@ -1894,7 +1895,7 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
     };
     for (WeighJob j; ok && next_job(j);) {
       const u32 key = j.key0 + tile * TC_TILE + key_t;
-      float sum = 0.0f;
+      float sum = 0.0f, rest = 0.0f;     // rest: what rounding took from the sum, since a long prompt has thousands of tiles
       u32 r = j.x0 % j.tiles;
       if (!(ok = begin(n))) break;
       for (u32 i = j.x0; i < j.x1; ++i, ++n) {
@@ -1942,10 +1943,13 @@ k_weigh_tc(const __grid_constant__ WeighArgs x, const __grid_constant__ KvMaps m
         }
         if (!ok) break;
         const float2 all = unpack2(add2(part[0], part[1]));
-        sum += all.x + all.y;
+        const float y = all.x + all.y, t = sum + y;
+        rest += y - (t - sum);
+        sum = t;                         // (nothing is negative, so the sum is nearly always the greater of the two)
         if (++r == j.tiles) r = 0;
       }
       if (!ok) break;
+      if (sum < INFINITY) sum += rest;   // Inf stays Inf
       // The halves together. Four places in turn: the second half can be no more than two tiles of rows ahead of the first.
       const u32 at = (jobs - 1) % WTC_JOBS, bar = hfull + (tile * WTC_JOBS + at) * 8;
       if (half) {
@@ -1995,7 +1999,7 @@ __global__ void __launch_bounds__(256) k_weigh_join(WeighArgs x, u32 n_ctas) {
   bool lost = false;
   for (u32 c = threadIdx.x; c < n_ctas; c += 256) lost |= sc.lost[c] != 0;
   if (__syncthreads_or(lost) || b >= a.b.max_blocks) return;
-  float sum = 0.0f;
+  double sum = 0.0;
   const bool held = b < (q.kv + BT - 1) / BT;
   if (held) {
     const u32 pair = before + b / WTC_KB;
@@ -2005,7 +2009,7 @@ __global__ void __launch_bounds__(256) k_weigh_join(WeighArgs x, u32 n_ctas) {
     }
     if (x.weights) sum += x.keep * x.weights[seq * x.w_stride + b];
   }
-  x.out[seq * x.o_stride + b] = held ? sum : 0.0f;
+  x.out[seq * x.o_stride + b] = held ? (float)sum : 0.0f;
 }
 
 // Few rows or many. (One tile of 128 rows costs the second kernel as much as one row.)

@@ -626,6 +626,21 @@ def test_weigh_rows_without_keys_and_masked_nan(B):  # noqa: F811
         assert not bool(torch.isnan(got[:, :last // BT]).any())
 
 
+@pytest.mark.parametrize("new,dim,hint", [(65536, 64, None), (65536, 128, None), (65536, 64, 1), (40000, 40, None)])
+def test_weigh_long_prompts_lose_nothing(B, new, dim, hint):  # noqa: F811
+    """All scores 0 and lse the same, so that every key gets exp(-lse) from every row that sees it. However many rows there are, the result is off
+    by the power (2^-22, and the exponent by 4 * 3.7 * 2^-24) and by what sums of up to 80 powers lose in 32 bits (80 * 2^-24)."""
+    import torch
+    s = make(B, ([new], [0]), "bf16", 0, 2, 4, dim, layers=1, layer=0)
+    s.q.zero_()
+    lse = torch.full((new, 8), 3.7, device="cuda")
+    got = s.eng.weigh_blocks(0, s.q, lse, s.table, s.q_start, s.kv_len, max_q_len=hint)[0, :new // BT].double().cpu().numpy()
+    s.eng.kv_check()
+    rows = (new - np.arange(new)).reshape(-1, BT).sum(1) * 8.0
+    want = rows * math.exp(-float(np.float32(3.7)))
+    assert float(np.abs(got / want - 1).max()) <= 2.0 ** -22 + 4 * 3.7 * E32 + 80 * E32
+
+
 def test_weigh_adds_the_layers_up(B):  # noqa: F811
     import torch
     s = make(B, ([3, 1], [200, 90]), "bf16", 0, 2, 4, 64, layers=2, layer=0)

@@ -527,7 +527,8 @@ typedef struct kvt_select_args {
  * or more comes last and sets the error word; one whose bounds were never written (zeros) scores 0. Rows behind
  * q_start[n_seqs] are not written. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
 int32_t kvt_select_blocks(kvt_engine *e, const kvt_select_args *a, void *stream);
-/* Depends on sizes only. 0 for arguments kvt_select_blocks refuses. */
+/* Depends on sizes only: 4 bytes per token, KV head and table entry, for as many tokens at a time as 128 MiB hold (one at least). 0 for arguments
+ * kvt_select_blocks refuses and where every list has all blocks of the table. */
 uint64_t kvt_select_scratch_bytes(kvt_engine *e, const kvt_select_args *a);
 
 typedef struct kvt_attend_blocks_args {

@@ -663,8 +663,11 @@ __global__ void __launch_bounds__(128) k_pick_short(SelectArgs a, u32 rows) {
   for (u32 at = a.first + before(__popc(mask)); mask; mask &= mask - 1) out[at++] = (int32_t)(lane * KEYS + __ffs(mask) - 1);
 }
 
-// Scores that are in hand together. (500 tokens on 130,500, 8 KV heads: 134 MB at once 127 us, in two parts of 64 MB 140, of 32 MB 167.)
-constexpr u64 SLAB_BYTES = 160ull << 20;
+// Scores that are in hand together: about as many as L2 holds (126 MB), and parts of a long batch alike, since a short one fills the GPU as
+// badly as a small batch. 32 chunks of 64 to 5000 tokens on 20,000 to 258,000, 8 KV heads, against all scores at once (up to 2.6 GB of them): parts of
+// up to 16 MB take 1.40 times as long on average, 32 MB 1.15, 64 MB 1.03, 96 MB 1.02, 128 MB 1.004 (at most 1.14), 192 MB 1.01, 256 MB 0.995. 600 tokens on
+// 130,500, 160 MB of scores: 243 us as 155 + 5 MB, 209 in two halves.
+constexpr u64 SLAB_BYTES = 128ull << 20;
 SelectPlan plan_select(const SelectArgs &a, int sm_count) {
   SelectPlan p{};
   p.sms = sm_count;
@@ -672,7 +675,8 @@ SelectPlan plan_select(const SelectArgs &a, int sm_count) {
   if (a.b.max_blocks <= a.n_blocks) return p;            // every list has all there are: no scores
   p.scores_stride = ((u64)a.b.max_blocks + 7) / 8 * 8;
   const u64 token = p.scores_stride * a.n_kv_heads * 4;
-  p.slab = (u32)std::min<u64>(a.b.n_tokens, std::max<u64>(1, SLAB_BYTES / token));
+  const u32 most = (u32)std::min<u64>(a.b.n_tokens, std::max<u64>(1, SLAB_BYTES / token)), parts = (a.b.n_tokens + most - 1) / most;
+  p.slab = std::min(most, ((a.b.n_tokens + parts - 1) / parts + 31) / 32 * 32);          // equal parts, of whole tiles of tokens
   p.scratch_bytes = p.slab * token;
   return p;
 }

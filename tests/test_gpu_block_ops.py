@@ -269,6 +269,20 @@ def test_select_in_parts(B):  # noqa: F811
         t0 += n
 
 
+@pytest.mark.parametrize("n_tokens,width,heads", [(1, 100, 8), (500, 8157, 8), (600, 8157, 8), (700, 8157, 8), (5000, 4063, 8), (33, 1 << 20, 1), (3, 1 << 22, 8), (90000, 700, 2)])
+def test_select_parts_are_alike(B, n_tokens, width, heads):  # noqa: F811
+    """The scratch is that of parts of equal length (up to 31 tokens apart), no more of them than 128 MiB of scores each make necessary."""
+    import torch
+    eng = B.Engine(n_layers=1, n_kv_heads=heads, head_dim=16, n_hbm_blocks=4, n_host_blocks=0, max_contexts=1, max_messages=16, max_tokens=64)
+    k = eng.key_bounds(torch.bfloat16)
+    a = B.SelectArgs(B.Batch(1, n_tokens, width, 0, width, 16, 16, 16), 0, 0, heads, 9, 1, 2, 0, heads * 16, 16, eng._bounds("", k), 0, 0, 0)
+    got = eng.L.kvt_select_scratch_bytes(eng.h, C.byref(a))
+    token = (width + 7) // 8 * 8 * heads * 4
+    most = max(1, (128 << 20) // token)
+    parts = -(-n_tokens // most)
+    assert got % token == 0 and -(-n_tokens // parts) <= got // token <= min(most, -(-n_tokens // parts) + 31)
+
+
 @pytest.mark.parametrize("span", [1, 3])
 @pytest.mark.parametrize("codes", [1, 2, 127])
 def test_select_ties_go_to_the_lower_number(B, codes, span):  # noqa: F811

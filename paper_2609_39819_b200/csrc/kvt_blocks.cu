@@ -1376,7 +1376,7 @@ __global__ void __launch_bounds__(WS_THREADS, 2) k_weigh_split(const __grid_cons
   }
 }
 
-// Heads of every other size, any number of rows. `share` warps work on a block, each on every so many-th head; a lane's 16 bytes of a key and
+// Heads of every other size, any number of rows. `share` warps, no more than there are KV heads, work on a block, each on every so many-th head; a lane's 16 bytes of a key and
 // of a query are operands of the matrix instruction if channels are counted in that order on both sides, so both go from memory to
 // registers. The next (block, head)'s keys are on their way while one is worked on. Heads of 96: one token on 100,000 61 us (floor 24), 1000
 // tokens 618 us (floor 2: rows go by eight, and a block's rows are not divided).
@@ -1400,7 +1400,7 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
     const u32 j = lane % 4, r8 = lane / 4, d = a.p.head_dim;
     // this warp's blocks b_tile + first + step * i and heads sub + share * k
     const u32 first = warp / share, step = 8 / share, sub = warp % share;
-    const u32 n_blocks = min(n_tile, n_held - b_tile) > first ? (min(n_tile, n_held - b_tile) - first + step - 1) / step : 0, n_heads = sub < H ? (H - sub + share - 1) / share : 0;
+    const u32 n_blocks = min(n_tile, n_held - b_tile) > first ? (min(n_tile, n_held - b_tile) - first + step - 1) / step : 0, n_heads = (H - sub + share - 1) / share;
     u32 held = ~0u;                      // lane i: slot of block i
     if (lane < n_blocks && b_tile + first + step * lane >= first_seen(a, q)) {
       held = a.b.table[seq * a.b.table_stride + b_tile + first + step * lane];
@@ -1483,8 +1483,6 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
         if (it + 2 < n_items) one = load(i, k);
         work(two, i1, k1);
       }
-    } else if (n_blocks) {               // more warps than heads
-      if (lane < n_blocks) s_sum[warp][first + step * lane] = 0.0f;
     }
     __syncthreads();
   }
@@ -2030,7 +2028,7 @@ WeighPlan plan_weigh(const WeighArgs &x, u32 max_q_len, int sm_count) {
     p.share = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
     p.tile = (u32)std::max<u64>(1, std::min<u64>(WEIGH_TILE, blocks / (8ull * sm_count)));
   } else {                               // one warp per block and 32 blocks per CTA where there are enough of them, else the heads of a block over several warps
-    p.share = 1;
+    p.share = 1;                         // (never more than KV heads)
     while (p.share < 8 && p.share * 2 <= x.a.p.n_kv_heads && blocks * p.share < 32ull * sm_count) p.share *= 2;
     p.tile = p.share == 1 && blocks >= 128ull * sm_count ? WEIGH_TILE : (u32)std::max<u64>(1, std::min<u64>(8, blocks / (2ull * sm_count)));
   }

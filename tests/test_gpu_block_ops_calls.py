@@ -1,7 +1,7 @@
-"""How the calls that choose blocks are made: by the native marshalling."""
+"""How the calls that choose blocks are made: by the native marshalling, and by one engine on two streams at once."""
 import pytest
 
-from test_gpu_block_ops import make
+from test_gpu_block_ops import make, random_bounds
 from test_gpu_model_ops import B, Setup  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +49,44 @@ def test_native_marshalling_runs_and_agrees_with_pythons(B, monkeypatch, dtype, 
     for x, y in zip(want, run(), strict=True):
         assert torch.equal(x, y)
     s.eng.kv_check()
+
+
+def test_one_engine_on_two_streams(B):  # noqa: F811
+    """Sequences of one engine stepped by two streams at once, each with its own results: the same as one after the other."""
+    import torch
+    s = make(B, ([1, 60, 1, 200], [5000, 3000, 300, 100]), "bf16", 0, 2, 4, 128, layers=1, layer=0)
+    eng = s.eng
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")      # noqa: E731
+    chosen = random_bounds(s, torch.Generator("cuda").manual_seed(3))
+    fresh = eng.key_bounds(s.dt)
+    halves = []
+    for a in (0, 2):                         # two sequences each
+        t0, n = sum(s.new[:a]), s.new[a:a + 2]
+        halves.append((s.q[t0:t0 + sum(n)], (s.table[a:a + 2], ints(0, n[0], sum(n)), ints(*s.kv[a:a + 2]))))
+
+    def step(q, batch):
+        eng.bound_keys(0, fresh, *batch, n_tokens=len(q))
+        blocks = eng.select_blocks(0, q, chosen, *batch, 9)
+        sparse = eng.attend_blocks(0, q, blocks, *batch)
+        lse = torch.empty(len(q), 8, device="cuda")
+        dense = eng.attend(0, q, *batch, lse=lse)
+        weights = eng.weigh_blocks(0, q, lse, *batch)
+        return (blocks, sparse, dense, lse, weights, *eng.evict_blocks(weights, *batch[::2], 9))
+
+    want = [step(*h) for h in halves]
+    bounds = (fresh.codes.clone(), fresh.exps.clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        fresh.codes.zero_()
+        fresh.exps.zero_()
+        torch.cuda.synchronize()
+        got = [None, None]
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i] = step(*halves[i])
+        torch.cuda.synchronize()
+        for x, y in zip(want, got):
+            assert all(torch.equal(a, b) for a, b in zip(x, y, strict=True))
+        assert torch.equal(fresh.codes, bounds[0]) and torch.equal(fresh.exps, bounds[1])
+    eng.kv_check()

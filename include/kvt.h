@@ -559,7 +559,7 @@ typedef struct kvt_weigh_args {
   float keep;                   /* what the old weights are multiplied with */
   uint32_t reserved;            /* 0 */
   const void *q;                /* device, rotated queries */
-  const float *lse;             /* device, [n_tokens][n_q_heads]: what kvt_attend wrote */
+  const float *lse;             /* device, [n_tokens][n_q_heads]: what kvt_attend wrote for these rows and keys */
   uint64_t q_ts, q_hs;
   const float *weights;         /* device, row s at s * w_stride: the old weights, or NULL for none */
   float *out;                   /* device, row s at s * o_stride, max_blocks each; may be `weights` with its stride */
@@ -567,7 +567,10 @@ typedef struct kvt_weigh_args {
   void *scratch;                /* device, 16-byte aligned, kvt_weigh_scratch_bytes(e, a) bytes */
   uint64_t scratch_bytes;
 } kvt_weigh_args;
-/* Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
+/* (lse has to be of all keys that a row sees. That of kvt_attend_blocks is of the listed keys: with it every key of a block that was not listed
+ * would be weighed too, against a sum that it is not in, and so too heavily. Steps that attend to some blocks only add nothing to the
+ * weights unless kvt_attend gives the lse of their rows as well.)
+ * Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
  * keys of block b that the token sees of exp(scale q.k - lse); 0 for blocks behind kv_len[s]. Sums of all layers come from
  * calls with the same weights, one per layer. Sums of up to a hundred powers are in 32 bits, sums of those in 64 or with what their rounding
  * took, the result in 32; all in an order that is fixed by the sizes and lengths, without atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within

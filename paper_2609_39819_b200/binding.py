@@ -911,7 +911,8 @@ class Engine:
                      weights=None, keep=1.0, out=None):
         """Attention weight per block, float32 [sequences, blocks of a table row]: keep * weights plus the sum, over the sequence's new
         tokens, query heads and the block's keys, of the weights exp(scale q k - lse) that attend gave them. q, lse, causal, window
-        and scale are those of that call of attend. weights: from earlier steps or layers (none: zeros); out: written if given, may be
+        and scale are those of that call of attend; the lse of attend_blocks will not do, which is of the listed keys alone (blocks that
+        were not listed would be weighed too heavily). weights: from earlier steps or layers (none: zeros); out: written if given, may be
         `weights`. Blocks behind kv_len get 0. max_q_len: most new tokens of one sequence, if known (chooses the kernel; results agree
         within their rounding). Asynchronous on the current stream. No backward pass, as in attend."""
         done = self._weigh_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,

@@ -521,9 +521,10 @@ typedef struct kvt_select_args {
 /* For each new token and KV head: the blocks its queries attend to, in ascending order, -1 behind the last. A token whose own
  * block is among the first n_blocks gets all up to it. Otherwise, of the blocks between the first and the last ones, those of
  * the largest scores; of equal scores the lower number. With the group's query heads g, u+_d = sum_g max(q_gd, 0) and u-_d =
- * sum_g max(-q_gd, 0), both rounded to whole steps of 2^f, f the least for which all are at most 255 steps (Inf counts as the
- * largest finite number, NaN as 0): score = 2^e sum_d u+_d up_d + u-_d down_d, a bound of the sum of the group's products
- * with any key of the block. It is exact in 32 bits, so the lists do not depend on the batch. A block whose slot is n_slots
+ * sum_g max(-q_gd, 0), both rounded to the nearest whole steps of 2^f, f the least for which all are at most 255 steps (Inf counts as the
+ * largest finite number, NaN as 0): score = 2^e sum_d u+_d up_d + u-_d down_d. With u before rounding it would bound the sum of the group's
+ * products with any key of the block; rounded it is an estimate of that bound, off by half a step of 2^f in each channel at most. It is exact in
+ * 32 bits, so the lists do not depend on the batch. A block whose slot is n_slots
  * or more comes last and sets the error word; one whose bounds were never written (zeros) scores 0. Rows behind
  * q_start[n_seqs] are not written. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. */
 int32_t kvt_select_blocks(kvt_engine *e, const kvt_select_args *a, void *stream);

@@ -249,8 +249,8 @@ __device__ __forceinline__ u32 ordered(float x) {
 // Selection of blocks. The group's queries of a token and KV head are added up, what is above zero and what is below apart, and
 // rounded to 8 bits without sign: u = rint(2^-f sum), f the least with max <= 255 * 2^f. With the bounds (up, down, e) of a block
 //   score = 2^e sum_d u+_d up_d + u-_d down_d,
-// the sum over the group's heads of what bounds their products with any key of the block (in steps of 2^f, which all blocks of the
-// query share). The sum is of at most 512 products of 255 * 127, a whole number below 2^24, so it is a 32-bit floating number
+// an estimate of what bounds the sum of the group's products with any key of the block (in steps of 2^f, which all blocks of the query
+// share; the bounds are rounded up, but the queries to the nearest, so it may be short of that by half a step per channel). The sum is of at most 512 products of 255 * 127, a whole number below 2^24, so it is a 32-bit floating number
 // exactly, and so is the score: all kernels, batches and orders of summation give the same selection, bit by bit.
 // Two kernels: scores into scratch, then each list from its scores. 8 KV heads of 128, groups of 4, lists of 64, in a captured graph: one
 // token on 258,047 17.3 us (floor 5.1: 33 MB of codes; the kernels take 8 and 7 us, each of them a chain of dependent loads), 500 tokens

@@ -505,7 +505,7 @@ typedef struct kvt_bound_args {
 int32_t kvt_bound_keys(kvt_engine *e, const kvt_bound_args *a, void *stream);
 
 typedef struct kvt_select_args {
-  kvt_batch b;
+  kvt_batch b;                  /* max_q_len is not used */
   uint32_t layer, dtype;
   uint32_t n_q_heads;           /* as in kvt_attend */
   uint32_t n_blocks;            /* entries of a list */

@@ -841,8 +841,8 @@ class Engine:
         """For each new token and KV head the numbers of the n_blocks blocks of its sequence that its queries are to attend to: int32
         [tokens, KV heads, n_blocks], ascending, -1 behind the last. Always among them: the first `first` blocks and the `last` last up
         to the token's own; the others are those of the largest scores by `bounds` (include/kvt.h says how they are reckoned; they are
-        exact, so that neither the batch nor the kernel has a say). q: rotated queries, batch as in attend; rows behind the last
-        sequence stay as they are. Asynchronous on the current stream."""
+        exact, so that neither the batch nor the kernel has a say). q: rotated queries, batch as in attend (max_q_len is taken and has no
+        effect); rows behind the last sequence stay as they are. Asynchronous on the current stream."""
         done = self._select_native(self.h and self.h.value, self._raw_stream(self._dev_index), self._dev_index, self.n_kv_heads, self.head_dim,
                                    self.n_layers, layer, self._kv_dtypes.get(bounds.dtype), q, bounds.codes, bounds.exps, block_table,
                                    q_start, kv_len, n_blocks, first, last, max_q_len, out)

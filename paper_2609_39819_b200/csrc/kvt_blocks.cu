@@ -1379,7 +1379,7 @@ __global__ void __launch_bounds__(WS_THREADS, 2) k_weigh_split(const __grid_cons
 // Heads of every other size, any number of rows. `share` warps, no more than there are KV heads, work on a block, each on every so many-th head; a lane's 16 bytes of a key and
 // of a query are operands of the matrix instruction if channels are counted in that order on both sides, so both go from memory to
 // registers. The next (block, head)'s keys are on their way while one is worked on. Heads of 96: one token on 100,000 61 us (floor 24), 1000
-// tokens 618 us (floor 2: rows go by eight, and a block's rows are not divided).
+// tokens 620 us (floor 2: rows go by eight, and a block's rows are not divided).
 constexpr u32 WEIGH_LSE = 512;
 template <class T, u32 G>      // G: 64-byte parts of a head
 __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n_tile, u32 share) {
@@ -1501,10 +1501,11 @@ __global__ void __launch_bounds__(256, G > 4 ? 1 : 2) k_weigh(WeighArgs x, u32 n
 // constants on the side of K and the parts of -lse / scale in bf16 on the side of Q, S^T is (s - lse / scale) in 32 bits,
 // and a power is one multiplication and ex2. (With lse from shared memory and a fused multiply-add it was bound by shared memory, which
 // the products alone keep busy half of the time: 8192 tokens, 8 x 4 heads of 128, 352 us.)
-// Bound by the exponentials: 256 keys by 128 rows take 2600 cycles, of which the special-function units need 2048 for all of them (every
-// eighth pair is made on the FMA pipes: 341 -> 331 us; every fourth 331, three of eight 343) and the tensor cores 1160. In a captured graph:
-// 8192 tokens, 8 KV heads of 128, groups of 4 334 us (275 TFLOP: 823 TFLOP/s, half of the measured matrix rate), 500 tokens on 130,500 599 us,
-// the last 32 of 32,000 26 us. One thread per key instead of two 410 us, K in stages of 256 keys and two stages of queries 339, lse in parts
+// 256 keys by 128 rows take 2600 cycles. The special-function units need 1792 of them (2048 for all powers; every eighth pair is made on the
+// FMA pipes: 341 -> 331 us; every fourth 331, three of eight 343), the tensor cores 1160, so neither is the limit: without the powers a step takes 1710
+// cycles, without most of the products 2470. What is left is each thread's chain from tensor memory to the sum, four warps per scheduler. In a
+// captured graph: 8192 tokens, 8 KV heads of 128, groups of 4 324 us (0.275 TFLOP: 849 TFLOP/s, half of the measured matrix rate), 500 tokens on 130,500
+// 601 us, the last 32 of 32,000 26 us. One thread per key instead of two 410 us, K in stages of 256 keys and two stages of queries 339, lse in parts
 // by 64-bit arithmetic 339, 32 columns of S at a time 375.
 //   warps 0-15   two threads per key, each for half of the rows: powers and their sum
 //   warp 16      issues the products, S^T in tensor memory, held twice: 2 x 2 x 128 columns

@@ -568,20 +568,21 @@ typedef struct kvt_weigh_args {
   void *scratch;                /* device, 16-byte aligned, kvt_weigh_scratch_bytes(e, a) bytes */
   uint64_t scratch_bytes;
 } kvt_weigh_args;
-/* (lse has to be of all keys that a row sees. That of kvt_attend_blocks is of the listed keys: with it every key of a block that was not listed
- * would be weighed too, against a sum that it is not in, and so too heavily. Steps that attend to some blocks only add nothing to the
- * weights unless kvt_attend gives the lse of their rows as well.)
- * Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
+/* Attention weight per block: out[s][b] = keep * weights[s][b] + the sum over the sequence's new tokens, all query heads and the
  * keys of block b that the token sees of exp(scale q.k - lse); 0 for blocks behind kv_len[s]. Sums of all layers come from
- * calls with the same weights, one per layer. Sums of up to a hundred powers are in 32 bits, sums of those in 64 or with what their rounding
- * took, the result in 32; all in an order that is fixed by the sizes and lengths, without atomics: a call gives the same bits every time (another max_q_len may choose another kernel, whose results agree within
- * their rounding). The exponent is off by up to some 2^-22 of |scale q.k| and |lse|, so from 2^20 on little is left of a weight; where
- * scale q.k - lse is far from 0 all the same, it is 0 or Inf as it should be. A row with lse = -inf, whose products are not Inf or NaN, adds
- * nothing. Keys a row does not see have no
- * effect; blocks that no row of a sequence sees, in front of a window, are not read and need no valid slot. Other slot ids
- * beyond both pools set the error word, and their keys count as zeros. Errors: KVT_E_INVAL, KVT_E_BUFSZ. Asynchronous. Where
- * kvt_kv_check reports a wait that ran out (KVT_E_DEVICE), `out` holds, of each sequence's blocks, new weights or what it held
- * before, and with many rows (max_q_len) what it held before. */
+ * calls with the same weights, one per layer.
+ * lse has to be of all keys that a row sees. That of kvt_attend_blocks is of the listed keys: with it every key of a block that was
+ * not listed would be weighed too, against a sum that it is not in, and so too heavily. Steps that attend to some blocks only add
+ * nothing to the weights unless kvt_attend gives the lse of their rows as well.
+ * Sums of up to a hundred powers are in 32 bits, sums of those in 64 or with what their rounding took, the result in 32; all in an
+ * order that is fixed by the sizes and lengths, without atomics: a call gives the same bits every time (another max_q_len may choose
+ * another kernel, whose results agree within their rounding). The exponent is off by up to some 2^-22 of |scale q.k| and |lse|, so
+ * from 2^20 on little is left of a weight; where scale q.k - lse is far from 0 all the same, it is 0 or Inf as it should be. A row
+ * with lse = -inf, whose products are not Inf or NaN, adds nothing. Keys a row does not see have no effect; blocks that no row of a
+ * sequence sees, in front of a window, are not read and need no valid slot. Other slot ids beyond both pools set the error word, and
+ * their keys count as zeros. Where kvt_kv_check reports a wait that ran out (KVT_E_DEVICE), `out` holds, of each sequence's blocks,
+ * new weights or what it held before, and with many rows (max_q_len) what it held before. Errors: KVT_E_INVAL, KVT_E_BUFSZ.
+ * Asynchronous. */
 int32_t kvt_weigh_blocks(kvt_engine *e, const kvt_weigh_args *a, void *stream);
 /* Depends on sizes only. 0 for arguments kvt_weigh_blocks refuses and where none is needed. */
 uint64_t kvt_weigh_scratch_bytes(kvt_engine *e, const kvt_weigh_args *a);
